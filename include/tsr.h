@@ -236,6 +236,89 @@ typedef struct {
  * workspace.  Errors (null pointers, negative counts, bad dtype) are found before any launch. */
 TSR_API tsr_status tsr_dense_adamw(const tsr_dense_tensor *tensors, int32_t count, const tsr_hyper *hyper, void *stream);
 
+/* ---- dense parameters: a kept plan, 8-bit states, clipping ------------------------------------- */
+
+/* What a training loop does with everything that is not a TSR block (Section 3.4 "in dense form"),
+ * and the dense AdamW baseline of whole models: a plan over many tensors is bound once and stepped
+ * with one call.  Per element, with s the optional factor on the gradient (see grad_scale below):
+ *     g = s * grad;   m <- b1 m + (1-b1) g;   v <- b2 v + (1-b2) g o g
+ *     p <- (1 - lr' wd') p - lr' (m / (1-b1^t)) / (sqrt(v / (1-b2^t)) + eps)
+ * with lr' = lr * lr_mult and wd' = weight_decay * wd_mult of the tensor.  Parameters are FP32 or BF16
+ * (the update is formed in FP32 and rounded once), gradients FP32 or BF16.
+ *
+ * TSR_STATE_F32 keeps m and v as FP32 arrays (for contiguous FP32 parameters without factor the
+ * results are those of tsr_dense_adamw, bit for bit).
+ *
+ * TSR_STATE_Q8 keeps m and r = sqrt(v) in 8 bits.  The rows*cols elements of a tensor, row after row,
+ * form blocks of TSR_DENSE_BLOCK; element x of a block with power-of-two scale S is held as the E4M3
+ * value of x / S (1 sign, 4 exponent, 3 mantissa bits; largest value 448), S being the smallest power of
+ * two, not below 2^-126, with max |x| <= 448 S.  m and r have a scale each, FP32, in pairs.  The root
+ * and not v itself is held because E4M3 spans 2^17: enough for a root, half of what a square needs.  A
+ * root above zero is never held as zero (it would leave m / eps as the next update); it is held as
+ * S 2^-9 at least.  A block with an entry that is not finite gets the scale NaN and reads as NaN.
+ *
+ * tsr_rounding says how values that are kept in fewer than 32 bits (BF16 parameters, E4M3 states) are
+ * rounded.  To nearest even: a moment that changes by less than half a unit in its last place per step
+ * (b2 = 0.999 decays v by 1/1000; a unit is 1/8 to 1/16) stays where it is.  Stochastic: up with the
+ * probability of the remainder, so that such changes accumulate in the mean; the 16 random bits per
+ * value are a function of (seed, step, position of the tensor in the plan, element) and nothing else. */
+typedef enum { TSR_STATE_F32 = 0, TSR_STATE_Q8 = 1 } tsr_dense_state;
+typedef enum { TSR_ROUND_NEAREST = 0, TSR_ROUND_STOCHASTIC = 1 } tsr_rounding;
+/* TSR_DENSE_NORM_ONLY: a gradient that counts in tsr_dense_plan_grad_norm and is not stepped (the G of a TSR
+ * block).  TSR_DENSE_STATE_ONLY: moments without parameter and gradient, for tsr_dense_plan_copy_state. */
+typedef enum { TSR_DENSE_NORM_ONLY = 1, TSR_DENSE_STATE_ONLY = 2 } tsr_dense_flags;
+#define TSR_DENSE_BLOCK 256
+
+typedef struct tsr_dense_plan tsr_dense_plan; /* opaque */
+
+typedef struct {
+    int64_t rows, cols;         /* a vector has one row; either may be 0 (nothing to do)            */
+    int64_t ldp, ldg, ldi;      /* elements from row to row of param, grad and image (>= cols)      */
+    int32_t p_dtype, g_dtype;   /* tsr_dtype of param and grad                                      */
+    int32_t state;              /* tsr_dense_state                                                  */
+    int32_t flags;              /* 0 or one of tsr_dense_flags                                      */
+    float lr_mult, wd_mult;     /* factors on hyper->lr and hyper->weight_decay, finite             */
+} tsr_dense_desc;
+
+/* DEVICE pointers of one tensor, each aligned to its own element type; m, v and scale are dense. */
+typedef struct {
+    void *param;        /* updated in place                                                         */
+    const void *grad;
+    void *m, *v;        /* FP32, or E4M3 values of m and of r = sqrt(v) (one byte each)              */
+    float *scale;       /* TSR_STATE_Q8: pairs (scale of m, scale of r), one per block; 8-byte aligned */
+    void *image;        /* NULL, or a BF16 copy of the updated FP32 param, written by every step     */
+} tsr_dense_ptrs;
+
+/* Plan over `count` (>= 0) tensors; descs is copied.  TSR_ERR_SHAPE / _UNSUPPORTED / _INVALID_ARG and
+ * *plan = NULL on failure. */
+TSR_API tsr_status tsr_dense_plan_create(tsr_dense_plan **plan, const tsr_dense_desc *descs, int32_t count);
+TSR_API tsr_status tsr_dense_plan_destroy(tsr_dense_plan *plan);
+/* Text of the last error of a call on this plan (empty string if none); valid until the next call. */
+TSR_API const char *tsr_dense_plan_last_error(const tsr_dense_plan *plan);
+/* Bytes of device scratch (tables and partial sums) that tsr_dense_plan_bind wants. */
+TSR_API tsr_status tsr_dense_plan_workspace_bytes(const tsr_dense_plan *plan, size_t *bytes);
+/* Attaches the caller's buffers and the scratch buffer (256-byte aligned) on the current device and uploads the
+ * tables.  Synchronises the device; may be called again to re-point the plan.  Buffers are not read. */
+TSR_API tsr_status tsr_dense_plan_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, int32_t count, void *workspace,
+                                       size_t workspace_bytes);
+
+/* One AdamW step of every tensor that has neither flag.  hyper->scale is ignored and hyper->rule must be
+ * TSR_RULE_ADAM.  grad_scale: NULL, or a DEVICE float that multiplies every gradient, such as out + 1 of
+ * tsr_dense_plan_grad_norm; where it is not finite when the step runs, the step changes nothing.  seed is read for
+ * TSR_ROUND_STOCHASTIC only. */
+TSR_API tsr_status tsr_dense_plan_step(tsr_dense_plan *plan, const tsr_hyper *hyper, const float *grad_scale,
+                                       int32_t rounding, uint64_t seed, void *stream);
+
+/* Global norm and clipping factor, on the device: out[0] = n = sqrt(sum of g^2 over all tensors but state-only
+ * ones), out[1] = min(1, max_norm / (n + 1e-6)), or NaN where n is not a finite FP32 number.  max_norm > 0, may be
+ * infinite.  Sums are FP64 and in a fixed order: the same gradients give the same bits on the same kind of GPU. */
+TSR_API tsr_status tsr_dense_plan_grad_norm(tsr_dense_plan *plan, float max_norm, float *out, void *stream);
+
+/* Moments of src into dst, tensor by tensor, converted where the two keep them in different forms (rounded to nearest
+ * into TSR_STATE_Q8; equal forms are copied as they are).  Both plans are bound, on the same device; their tensors
+ * agree in rows * cols and in whether they have a state. */
+TSR_API tsr_status tsr_dense_plan_copy_state(tsr_dense_plan *dst, const tsr_dense_plan *src, void *stream);
+
 /* ---- reporting -------------------------------------------------------------------------- */
 
 /* Section 3.2: bytes one worker would hand to the all-reduce in one step, summed over blocks:

@@ -22,6 +22,10 @@ TSR_F32, TSR_BF16 = 0, 1
 TSR_RULE_ADAM, TSR_RULE_SGD = 0, 1
 TSR_BLOCK_REEXPRESS_MOMENT = 1
 TSR_BLOCK_ONE_SIDED = 2
+TSR_STATE_F32, TSR_STATE_Q8 = 0, 1
+TSR_ROUND_NEAREST, TSR_ROUND_STOCHASTIC = 0, 1
+TSR_DENSE_NORM_ONLY, TSR_DENSE_STATE_ONLY = 1, 2
+DENSE_BLOCK = 256
 
 STATUS_NAMES = {
     0: "TSR_OK", 1: "TSR_ERR_INVALID_ARG", 2: "TSR_ERR_SHAPE", 3: "TSR_ERR_ALIGNMENT", 4: "TSR_ERR_WORKSPACE",
@@ -47,6 +51,17 @@ class DenseTensor(ctypes.Structure):
                 ("count", ctypes.c_int64), ("g_dtype", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class DenseDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("ldp", ctypes.c_int64), ("ldg", ctypes.c_int64),
+                ("ldi", ctypes.c_int64), ("p_dtype", ctypes.c_int32), ("g_dtype", ctypes.c_int32), ("state", ctypes.c_int32),
+                ("flags", ctypes.c_int32), ("lr_mult", ctypes.c_float), ("wd_mult", ctypes.c_float)]
+
+
+class DensePtrs(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("scale", ctypes.c_void_p), ("image", ctypes.c_void_p)]
+
+
 class Hyper(ctypes.Structure):
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float), ("eps", ctypes.c_float),
                 ("weight_decay", ctypes.c_float), ("scale", ctypes.c_float), ("step", ctypes.c_int64),
@@ -66,7 +81,9 @@ EXPORTS = [
     "tsr_rsvd_refresh_grouped", "tsr_embed_step_grouped", "tsr_step_grouped", "tsr_step_grouped_host",
     "tsr_comm_bytes", "tsr_state_elems", "tsr_poll_status", "tsr_generate_omega", "tsr_block_uses_tensor_cores",
     "tsr_set_profiling", "tsr_get_stage_ms", "tsr_launch_count", "tsr_project_core_static", "tsr_dense_adamw",
-    "tsr_set_limits", "tsr_refresh_gram",
+    "tsr_set_limits", "tsr_refresh_gram", "tsr_dense_plan_create", "tsr_dense_plan_destroy",
+    "tsr_dense_plan_last_error", "tsr_dense_plan_workspace_bytes", "tsr_dense_plan_bind", "tsr_dense_plan_step",
+    "tsr_dense_plan_grad_norm", "tsr_dense_plan_copy_state",
 ]
 
 
@@ -127,6 +144,15 @@ def lib():
         L.tsr_dense_adamw.argtypes = [P(DenseTensor), i32, P(Hyper), vp]
         L.tsr_set_limits.argtypes = [vp, P(Limits)]
         L.tsr_refresh_gram.argtypes = [vp, i32, i32, vp, vp, vp]
+        L.tsr_dense_plan_create.argtypes = [P(vp), P(DenseDesc), i32]
+        L.tsr_dense_plan_destroy.argtypes = [vp]
+        L.tsr_dense_plan_last_error.restype = ctypes.c_char_p
+        L.tsr_dense_plan_last_error.argtypes = [vp]
+        L.tsr_dense_plan_workspace_bytes.argtypes = [vp, P(ctypes.c_size_t)]
+        L.tsr_dense_plan_bind.argtypes = [vp, P(DensePtrs), i32, vp, ctypes.c_size_t]
+        L.tsr_dense_plan_step.argtypes = [vp, P(Hyper), vp, i32, u64, vp]
+        L.tsr_dense_plan_grad_norm.argtypes = [vp, ctypes.c_float, vp, vp]
+        L.tsr_dense_plan_copy_state.argtypes = [vp, vp, vp]
         _lib = L
     return _lib
 
