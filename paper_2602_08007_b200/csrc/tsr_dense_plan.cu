@@ -4,7 +4,7 @@
 // Everything here streams: a step reads parameter, gradient and moments once and writes parameter and moments once, so
 // HBM bounds it (bytes per element: FP32 state 16, 8-bit state 4 + 16/256, plus the parameter twice and the gradient).
 // Work is laid out in UNITS of 256 consecutive elements of one tensor, one warp each -- the block of the 8-bit state, so
-// that a block's maximum is one warp reduction -- and CHUNKS of units, one CTA each, listed in a table.
+// that a block's maximum is one warp reduction -- and CHUNKS of up to 8 units per warp, one CTA each, listed in a table.
 #include <cuda_fp8.h>
 #include <math.h>
 #include <string.h>
@@ -23,17 +23,17 @@ namespace tsr {
 constexpr int UNIT = TSR_DENSE_BLOCK;      // elements of a warp's piece of work
 static_assert(UNIT == 32 * 8, "a lane holds eight elements of a unit");
 constexpr int WARPS = 8;                   // per CTA
-constexpr int UNITS_PER_WARP = 2;
-constexpr int CHUNK = UNIT * WARPS * UNITS_PER_WARP;
+constexpr int MAX_UNITS = 8;               // units of a warp in one chunk: 1, 2, 4 or 8 (chosen per plan)
+constexpr int MANY_CHUNKS = 2048;
 constexpr int NORM_CTAS = 1184;            // most CTAs of a norm launch (8 on each of 148 SMs)
 
 enum DenseRecFlags : uint32_t {
-    REC_VEC = 1,         // all that a step touches can be read in vectors of eight elements
-    REC_VEC_STATE = 2,   // the moments can
-    REC_VEC_GRAD = 4,    // the gradient can
-    REC_PITCHED = 8,     // rows that do not follow one another directly
-    REC_Q8 = 16,
-    REC_G_BF16 = 32,
+    REC_VEC_STATE = 1,   // the moments can be read in vectors of eight elements
+    REC_VEC_GRAD = 2,    // so can the gradient, which is contiguous
+    REC_PITCHED = 4,     // rows that do not follow one another directly
+    REC_Q8 = 8,
+    REC_G_BF16 = 16,
+    REC_PAIR_STATE = 32, // the moments can be read in pairs
 };
 
 struct alignas(16) DenseRec {   // one tensor on the device
@@ -48,7 +48,9 @@ struct alignas(16) DenseRec {   // one tensor on the device
     int32_t index;              // position in the plan
 };
 
-struct DenseChunk { int32_t rec, at; };   // elements [at * CHUNK, (at + 1) * CHUNK) of a tensor
+// Units [first, first + units) of tensor rec.  vector: every one of them is whole, and everything that a step touches is
+// contiguous and aligned to vectors of eight elements.
+struct alignas(16) DenseChunk { int32_t rec; uint32_t first; int32_t units; int32_t vector; };
 
 struct DenseStep {
     StepScalars sc;
@@ -88,42 +90,39 @@ __device__ __forceinline__ uint2 load8(const void *p)
     return r;
 }
 
-// Eight elements of type T as they lie in memory, and as FP32.
+// Eight elements of type T as they lie in memory, and as FP32 pairs.
 template <typename T> struct Eight;
 template <> struct Eight<float> {
     Vec32 r;
     __device__ __forceinline__ void load(const float *p) { r = load32(p); }
-    __device__ __forceinline__ void get(float (&x)[8]) const
+    __device__ __forceinline__ void get(float2 (&x)[4]) const
     {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(r.w[j]);
+        for (int j = 0; j < 4; ++j) x[j] = make_float2(__uint_as_float(r.w[2 * j]), __uint_as_float(r.w[2 * j + 1]));
     }
-    static __device__ __forceinline__ void put(float *p, const float (&x)[8])
+    static __device__ __forceinline__ void put(float *p, const float2 (&x)[4])
     {
         Vec32 r;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r.w[j] = __float_as_uint(x[j]);
+        for (int j = 0; j < 4; ++j) { r.w[2 * j] = __float_as_uint(x[j].x); r.w[2 * j + 1] = __float_as_uint(x[j].y); }
         store32(p, r);
     }
 };
 template <> struct Eight<bf16> {
     uint4 r;
     __device__ __forceinline__ void load(const bf16 *p) { r = load16(p); }
-    __device__ __forceinline__ void get(float (&x)[8]) const
+    __device__ __forceinline__ void get(float2 (&x)[4]) const
     {
         const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            x[2 * j] = __uint_as_float(w[j] << 16);
-            x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
-        }
+        for (int j = 0; j < 4; ++j) x[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
     }
-    static __device__ __forceinline__ void put(bf16 *p, const float (&x)[8])
+    static __device__ __forceinline__ void put(bf16 *p, const float2 (&x)[4])
     {
         uint32_t w[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * j], x[2 * j + 1]);
+            const __nv_bfloat162 b = __floats2bfloat162_rn(x[j].x, x[j].y);
             w[j] = *(const uint32_t *)&b;
         }
         *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]);
@@ -134,26 +133,26 @@ __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(bf16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ void from_f32(float &d, float x) { d = x; }
 __device__ __forceinline__ void from_f32(bf16 &d, float x) { d = __float2bfloat16_rn(x); }
+__device__ __forceinline__ float &at(float2 (&x)[4], int j) { return (j & 1) ? x[j >> 1].y : x[j >> 1].x; }
 
 // ---- 8-bit values ---------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ void e4m3_unpack(uint2 c, float (&x)[8])
+__device__ __forceinline__ float e4m3_value(uint8_t c) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3))); }
+__device__ __forceinline__ uint8_t e4m3_code(float x) { return __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3); }
+
+__device__ __forceinline__ void e4m3_unpack(uint2 c, float2 (&x)[4])
 {
     const uint32_t w[2] = {c.x, c.y};
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j >> 1] >> (16 * (j & 1))), __NV_E4M3);
-        const float2 f = __half22float2(__half2(h));
-        x[2 * j] = f.x;
-        x[2 * j + 1] = f.y;
-    }
+    for (int j = 0; j < 4; ++j)
+        x[j] = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(w[j >> 1] >> (16 * (j & 1))), __NV_E4M3)));
 }
 
-__device__ __forceinline__ uint2 e4m3_pack(const float (&x)[8])
+__device__ __forceinline__ uint2 e4m3_pack(const float2 (&x)[4])
 {
     uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) w[j] = __nv_cvt_float2_to_fp8x2(make_float2(x[2 * j], x[2 * j + 1]), __NV_SATFINITE, __NV_E4M3);
+    for (int j = 0; j < 4; ++j) w[j] = __nv_cvt_float2_to_fp8x2(x[j], __NV_SATFINITE, __NV_E4M3);
     return make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
 }
 
@@ -187,92 +186,160 @@ __device__ __forceinline__ uint32_t random_word(uint32_t counter, uint32_t key1,
     return x ^ (x >> 16);
 }
 
-// |y| <= 448 rounded to an E4M3 value, away from zero with probability (remainder / spacing): 16 random bits are added
-// below the three mantissa bits and the rest is cut off.  Below 2^-6 the spacing is 2^-9 throughout; adding 2^-6 first
-// puts such values where FP32 numbers with three mantissa bits have that spacing.
-__device__ __forceinline__ float e4m3_stochastic(float y, uint32_t bits16)
+// a in [0, 448] rounded to an E4M3 value, up with probability (remainder / spacing): 16 random bits (`bits20`: with four
+// zeros below them) are added below the three mantissa bits and the rest is cut off.  Below 2^-6 the spacing is 2^-9
+// throughout; adding 2^-6 first puts such values where FP32 numbers with three mantissa bits have that spacing.
+__device__ __forceinline__ float e4m3_stochastic(float a, uint32_t bits20)
 {
-    const float a = fabsf(y);
     const float c = a < 0x1p-6f ? 0x1p-6f : 0.f;
-    const uint32_t z = __float_as_uint(__fadd_rn(a, c)) + (bits16 << 4);
-    return copysignf(__fsub_rn(__uint_as_float(z & 0xfff00000u), c), y);
-}
-
-__device__ __forceinline__ float bf16_stochastic(float x, uint32_t bits16)
-{
-    uint32_t b = __float_as_uint(x);
-    if ((b & 0x7f800000u) != 0x7f800000u) b += bits16;   // Inf and NaN stay what they are
-    return __uint_as_float(b & 0xffff0000u);
+    const uint32_t z = __float_as_uint(__fadd_rn(a, c)) + bits20;
+    return __fsub_rn(__uint_as_float(z & 0xfff00000u), c);
 }
 
 // ---- one unit's arithmetic ------------------------------------------------------------------------------------------
+//
+// A lane's eight elements are four pairs, because sm_100 multiplies and adds FP32 pairs in one instruction (each half
+// rounded as the scalar operation).  The 8-bit form is bound by instruction issue before it is by HBM, so the pairs and
+// the three-operand maximum matter.
 
 struct UnitKeys { uint32_t k1, k2; };
 
-// The update of one lane's eight elements.  On entry m, v are the held moments (8-bit state: m and r = sqrt(v)), on exit
-// the new ones in FP32.  Every rounding of the 8-bit form is one IEEE operation, so its stored bits are well defined; the
-// update itself takes the approximate quotient.
-template <bool Q8>
-__device__ __forceinline__ void update_eight(float (&p)[8], const float (&g)[8], float (&m)[8], float (&v)[8], const DenseStep &a, float lr, float decay)
+__device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
+__device__ __forceinline__ unsigned long long bits_of(float2 a) { return *(const unsigned long long *)&a; }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    unsigned long long d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return *(const float2 *)&d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)), "l"(bits_of(c)));
+    return *(const float2 *)&d;
+}
+// a + b; results and operands below 2^-126 count as zero.  The flush is there for the roots, and it keeps a product and its
+// sum two operations: without it the assembler joins a pair's mul.rn and add.rn into one multiply-add (seen as other
+// stored bits where the rounded product lies halfway between two 8-bit values).
+__device__ __forceinline__ float2 add_flush(float2 a, float2 b)
+{
+    unsigned long long d;
+    asm("add.rn.ftz.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return *(const float2 *)&d;
+}
+__device__ __forceinline__ float max_abs3(float a, float b, float c)   // NaN if any is NaN
+{
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+__device__ __forceinline__ float max_abs8(const float2 (&x)[4])
+{
+    return max_abs3(max_abs3(x[0].x, x[0].y, x[1].x), max_abs3(x[1].y, x[2].x, x[2].y), max_abs3(x[3].x, x[3].y, 0.f));
+}
+__device__ __forceinline__ float warp_max_abs(float x)
+{
+    float d;
+    asm("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(d) : "f"(x));
+    return d;
+}
+__device__ __forceinline__ float rcp_approx(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// The correctly rounded root of x = 0 or x >= 2^-126, without a branch: with y ~ 1 / sqrt(x) from the hardware's
+// approximation, s = x y is the root to about 2^-22, and s + (x - s^2) y / 2 is one Newton step whose residual the fused
+// multiply-add forms exactly (Markstein's square root, IBM J. Res. Dev. 34, 1990).  Compared with __fsqrt_rn on every
+// positive FP32 number from 2^-126 on: equal.  Infinity gives NaN here; its block reads as NaN either way.
+__device__ __forceinline__ float2 sqrt_pair(float2 x)
+{
+    float2 y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(x.x, 0x1p-126f)));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(x.y, 0x1p-126f)));
+    const float2 s = mul2(x, y);
+    const float2 h = mul2(pair(0.5f), y);
+    const float2 d = fma2(make_float2(-s.x, -s.y), s, x);
+    return fma2(d, h, s);
+}
+
+// FP32 state: moments in, moments out (the arithmetic of tsr_dense_adamw).
+__device__ __forceinline__ void update_f32(float2 (&p)[4], const float2 (&g)[4], float2 (&m)[4], float2 (&v)[4], const DenseStep &a, float lr, float decay)
 {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        float d;
-        if constexpr (Q8) {
-            m[j] = __fadd_rn(__fmul_rn(a.sc.beta1, m[j]), __fmul_rn(a.sc.omb1, g[j]));
-            v[j] = __fsqrt_rn(__fadd_rn(__fmul_rn(a.sc.beta2, __fmul_rn(v[j], v[j])), __fmul_rn(a.sc.omb2, __fmul_rn(g[j], g[j]))));
-            d = __fdividef(__fmul_rn(m[j], a.sc.inv_bc1), __fmaf_rn(v[j], a.sqrt_inv_bc2, a.sc.eps));
-        } else {
-            d = core_update_elem(g[j], m[j], v[j], a.sc);
-        }
-        p[j] = __fmaf_rn(-lr, d, __fmul_rn(decay, p[j]));
+    for (int j = 0; j < 4; ++j) {
+        float2 d;
+        d.x = core_update_elem(g[j].x, m[j].x, v[j].x, a.sc);
+        d.y = core_update_elem(g[j].y, m[j].y, v[j].y, a.sc);
+        p[j] = fma2(pair(-lr), d, mul2(pair(decay), p[j]));
     }
 }
 
-// New scales of the warp's block, and its values scaled and (stochastic) rounded to E4M3 values; element(j) is the
-// position of x[j] in the tensor.
-template <bool SR, typename Elem>
-__device__ __forceinline__ float2 quantise_eight(float (&m)[8], float (&r)[8], UnitKeys k, Elem element)
+// 8-bit state: m and r = sqrt(v) in, as E4M3 values and their scales; new m and r in FP32 out.  Every rounding on the way
+// to the stored bits is one IEEE operation, so that they are well defined; the update itself takes the approximate
+// quotient.  (beta1 scale) code is exactly beta1 (scale code), scale being a power of two.
+__device__ __forceinline__ void update_q8(float2 (&p)[4], const float2 (&g)[4], float2 (&m)[4], float2 (&r)[4], float2 scale, const DenseStep &a, float lr,
+                                          float decay)
 {
-    uint32_t bm = 0, br = 0;
+    const float b1s = __fmul_rn(a.sc.beta1, scale.x);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        bm = max(bm, __float_as_uint(m[j]) & 0x7fffffffu);
-        br = max(br, __float_as_uint(r[j]) & 0x7fffffffu);
+    for (int j = 0; j < 4; ++j) {
+        m[j] = add_flush(mul2(pair(b1s), m[j]), mul2(pair(a.sc.omb1), g[j]));
+        r[j] = mul2(pair(scale.y), r[j]);
+        r[j] = sqrt_pair(add_flush(mul2(pair(a.sc.beta2), mul2(r[j], r[j])), mul2(pair(a.sc.omb2), mul2(g[j], g[j]))));
+        const float2 den = fma2(r[j], pair(a.sqrt_inv_bc2), pair(a.sc.eps));
+        const float2 d = mul2(mul2(m[j], pair(a.sc.inv_bc1)), make_float2(rcp_approx(den.x), rcp_approx(den.y)));
+        p[j] = fma2(pair(-lr), d, mul2(pair(decay), p[j]));
     }
-    bm = __reduce_max_sync(0xffffffffu, bm);
-    br = __reduce_max_sync(0xffffffffu, br);
+}
+
+// New scales of the warp's block; m and r become x / scale, rounded to E4M3 values where the rounding is stochastic
+// (the conversion to 8 bits rounds to nearest).  element(j) is the position of element j of the lane in the tensor.
+template <bool SR, typename Elem>
+__device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&r)[4], UnitKeys k, Elem element)
+{
     float2 scale, inv;
-    block_scale(bm, scale.x, inv.x);
-    block_scale(br, scale.y, inv.y);
+    block_scale(__float_as_uint(warp_max_abs(max_abs8(m))), scale.x, inv.x);
+    block_scale(__float_as_uint(warp_max_abs(max_abs8(r))), scale.y, inv.y);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const bool some = r[j] > 0.f;
-        m[j] = __fmul_rn(m[j], inv.x);
-        r[j] = __fmul_rn(r[j], inv.y);
+    for (int j = 0; j < 4; ++j) {
+        // 0 for r = 0, at least 2^-9 for any other r (those are above 2^-75)
+        const float2 some = mul2(r[j], pair(0x1p100f));
+        m[j] = mul2(m[j], pair(inv.x));
+        r[j] = mul2(r[j], pair(inv.y));
         if constexpr (SR) {
-            const uint32_t w = random_word((uint32_t)element(j), k.k1, k.k2);
-            m[j] = e4m3_stochastic(m[j], w & 0xffffu);
-            r[j] = e4m3_stochastic(r[j], w >> 16);
+            const uint32_t w0 = random_word((uint32_t)element(2 * j), k.k1, k.k2);
+            const uint32_t w1 = random_word((uint32_t)element(2 * j + 1), k.k1, k.k2);
+            m[j].x = copysignf(e4m3_stochastic(fabsf(m[j].x), (w0 << 4) & 0xffff0u), m[j].x);
+            m[j].y = copysignf(e4m3_stochastic(fabsf(m[j].y), (w1 << 4) & 0xffff0u), m[j].y);
+            r[j].x = e4m3_stochastic(r[j].x, (w0 >> 12) & 0xffff0u);
+            r[j].y = e4m3_stochastic(r[j].y, (w1 >> 12) & 0xffff0u);
         }
-        if (some) r[j] = fmaxf(r[j], 0x1p-9f);
+        r[j].x = fmaxf(r[j].x, fminf(some.x, 0x1p-9f));
+        r[j].y = fmaxf(r[j].y, fminf(some.y, 0x1p-9f));
     }
     return scale;
 }
 
-// BF16 parameters, stochastic: one random word serves elements 2i and 2i + 1.
+// BF16 parameters, stochastic: 16 random bits are added below the seven mantissa bits and the rest is cut off; one random
+// word serves elements 2i and 2i + 1.  A lane that holds Inf or NaN rounds its eight to nearest.
 template <typename Elem>
-__device__ __forceinline__ void round_params(float (&p)[8], UnitKeys k, Elem element)
+__device__ __forceinline__ void round_params(float2 (&p)[4], UnitKeys k, Elem element)
 {
+    if (!(max_abs8(p) < __uint_as_float(0x7f800000u))) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const int64_t e = element(j);
-        const uint32_t w = random_word((uint32_t)(e >> 1), k.k1 ^ 0x5bd1e995u, k.k2);
-        p[j] = bf16_stochastic(p[j], (e & 1) ? w >> 16 : w & 0xffffu);
+    for (int j = 0; j < 4; ++j) {   // a pair starts at an even position
+        const uint32_t w = random_word((uint32_t)(element(2 * j) >> 1), k.k1 ^ 0x5bd1e995u, k.k2);
+        p[j].x = __uint_as_float((__float_as_uint(p[j].x) + (w & 0xffffu)) & 0xffff0000u);
+        p[j].y = __uint_as_float((__float_as_uint(p[j].y) + (w >> 16)) & 0xffff0000u);
     }
 }
 
-// Where elements base + lane + 32 j of a tensor lie: row and column of the first by one division, the others by steps.
+// The path for any alignment and any pitch, and for the last, partial unit of a tensor: a lane has the pairs of
+// neighbours at base + 2 lane + 64 j, so that the warp's accesses stay together.  Walk says where a pair lies in a matrix
+// with row pitch: row and column of the first by one division, the others by steps of 64.
 struct Walk {
     int64_t row, col;
     const DenseRec &t;
@@ -290,23 +357,222 @@ struct Walk {
             col = e - row * t.cols;
         }
     }
-    __device__ __forceinline__ void next()   // 32 elements on
+    __device__ __forceinline__ void next()   // 64 elements on
     {
-        col += 32;
+        col += 64;
         if ((t.flags & REC_PITCHED) && col >= t.cols) {
-            if (t.cols >= 32) { col -= t.cols; ++row; } else split(row * t.cols + col);
+            if (t.cols >= 64) { col -= t.cols; ++row; } else split(row * t.cols + col);
         }
     }
-    __device__ __forceinline__ int64_t at(int64_t ld) const { return row * ld + col; }
+    // the pair's elements, in a matrix of pitch ld
+    __device__ __forceinline__ int64_t one(int64_t ld) const { return row * ld + col; }
+    __device__ __forceinline__ int64_t two(int64_t ld) const
+    {
+        return (t.flags & REC_PITCHED) && col + 1 == t.cols ? (row + 1) * ld : row * ld + col + 1;
+    }
+};
+__device__ __forceinline__ int64_t pair_at(int64_t base, int lane, int j) { return base + 2 * lane + 64 * j; }
+
+// Pairs of moments of that path; elements from n on are zero, and not written.
+template <bool Q8>
+__device__ __forceinline__ void load_pairs(const void *src, bool both, int64_t base, int lane, int64_t n, float2 (&x)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t e = pair_at(base, lane, j);
+        x[j] = pair(0.f);
+        if constexpr (Q8) {
+            const uint8_t *c = (const uint8_t *)src + e;
+            uint32_t w = 0;
+            if (both && e + 1 < n) w = *(const uint16_t *)c;
+            else {
+                if (e < n) w = c[0];
+                if (e + 1 < n) w |= (uint32_t)c[1] << 8;
+            }
+            x[j] = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3)));
+        } else {
+            const float *f = (const float *)src + e;
+            if (both && e + 1 < n) x[j] = *(const float2 *)f;
+            else {
+                if (e < n) x[j].x = f[0];
+                if (e + 1 < n) x[j].y = f[1];
+            }
+        }
+    }
+}
+template <bool Q8>
+__device__ __forceinline__ void store_pairs(void *dst, bool both, int64_t base, int lane, int64_t n, const float2 (&x)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t e = pair_at(base, lane, j);
+        if constexpr (Q8) {
+            uint8_t *c = (uint8_t *)dst + e;
+            const uint32_t w = __nv_cvt_float2_to_fp8x2(x[j], __NV_SATFINITE, __NV_E4M3);
+            if (both && e + 1 < n) *(uint16_t *)c = (uint16_t)w;
+            else {
+                if (e < n) c[0] = (uint8_t)w;
+                if (e + 1 < n) c[1] = (uint8_t)(w >> 8);
+            }
+        } else {
+            float *f = (float *)dst + e;
+            if (both && e + 1 < n) *(float2 *)f = x[j];
+            else {
+                if (e < n) f[0] = x[j].x;
+                if (e + 1 < n) f[1] = x[j].y;
+            }
+        }
+    }
+}
+
+template <typename PT, typename GT, bool Q8, bool SR>
+__device__ __forceinline__ void step_any_unit(const DenseRec &t, int64_t base, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key)
+{
+    PT *P = (PT *)t.p;
+    const GT *G = (const GT *)t.g;
+    const bool both = t.flags & REC_PAIR_STATE;
+    float2 p[4], g[4], m[4], v[4];
+    float2 scale = make_float2(0.f, 0.f);
+    if constexpr (Q8) scale = t.scale[base / UNIT];
+    load_pairs<Q8>(t.m, both, base, lane, t.n, m);
+    load_pairs<Q8>(t.v, both, base, lane, t.n, v);
+    {
+        Walk w(t, pair_at(base, lane, 0));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t e = pair_at(base, lane, j);
+            p[j] = g[j] = pair(0.f);
+            if (e < t.n) {
+                p[j].x = to_f32(P[w.one(t.ldp)]);
+                g[j].x = to_f32(G[w.one(t.ldg)]);
+            }
+            if (e + 1 < t.n) {
+                p[j].y = to_f32(P[w.two(t.ldp)]);
+                g[j].y = to_f32(G[w.two(t.ldg)]);
+            }
+            w.next();
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) g[j] = mul2(g[j], pair(gs));
+    if constexpr (Q8) update_q8(p, g, m, v, scale, a, lr, decay);
+    else update_f32(p, g, m, v, a, lr, decay);
+    auto element = [&](int j) { return pair_at(base, lane, j >> 1) + (j & 1); };
+    if constexpr (SR && sizeof(PT) == 2) round_params(p, key, element);
+    {
+        Walk w(t, pair_at(base, lane, 0));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t e = pair_at(base, lane, j);
+            if (e < t.n) from_f32(P[w.one(t.ldp)], p[j].x);
+            if (e + 1 < t.n) from_f32(P[w.two(t.ldp)], p[j].y);
+            if (sizeof(PT) == 4 && t.image) {
+                if (e < t.n) from_f32(t.image[w.one(t.ldi)], p[j].x);
+                if (e + 1 < t.n) from_f32(t.image[w.two(t.ldi)], p[j].y);
+            }
+            w.next();
+        }
+    }
+    if constexpr (Q8) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (element(j) >= t.n) at(m, j) = at(v, j) = 0.f;   // (0 * NaN of a poisoned block)
+        const float2 s = quantise<SR>(m, v, key, element);
+        if (lane == 0) t.scale[base / UNIT] = s;
+    }
+    store_pairs<Q8>(t.m, both, base, lane, t.n, m);
+    store_pairs<Q8>(t.v, both, base, lane, t.n, v);
+}
+
+// One whole unit of the vector path as it lies in memory: the lane's eight elements of everything.
+template <typename PT, typename GT, bool Q8> struct RawUnit {
+    Eight<PT> p;
+    Eight<GT> g;
+    uint2 cm, cr;
+    Eight<float> m, v;
+    float2 scale;
+};
+
+template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers to the lane's elements of a unit
+    PT *p;
+    const GT *g;
+    char *m, *v;
+    float2 *scale;
+    bf16 *image;
+    static constexpr int MOMENT = Q8 ? 1 : 4;
+
+    __device__ __forceinline__ VectorUnit(const DenseRec &t, int64_t base, int lane)
+    {
+        const int64_t e = base + lane * 8;
+        p = (PT *)t.p + e;
+        g = (const GT *)t.g + e;
+        m = (char *)t.m + e * MOMENT;
+        v = (char *)t.v + e * MOMENT;
+        if constexpr (Q8) scale = t.scale + base / UNIT;
+        image = sizeof(PT) == 4 && t.image ? t.image + e : nullptr;
+    }
+    __device__ __forceinline__ void load(RawUnit<PT, GT, Q8> &r, int64_t off) const   // off: elements ahead, whole units
+    {
+        r.p.load(p + off);
+        r.g.load(g + off);
+        if constexpr (Q8) {
+            r.cm = load8(m + off);
+            r.cr = load8(v + off);
+            r.scale = scale[off / UNIT];
+        } else {
+            r.m.load((const float *)m + off);
+            r.v.load((const float *)v + off);
+        }
+    }
+    __device__ __forceinline__ void advance(int64_t off)
+    {
+        p += off;
+        g += off;
+        m += off * MOMENT;
+        v += off * MOMENT;
+        if constexpr (Q8) scale += off / UNIT;
+        if (sizeof(PT) == 4 && image) image += off;
+    }
+    template <bool SR>
+    __device__ __forceinline__ void step(const RawUnit<PT, GT, Q8> &raw, uint32_t e, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key) const
+    {
+        float2 xp[4], xg[4], xm[4], xv[4];
+        raw.p.get(xp);
+        raw.g.get(xg);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) xg[j] = mul2(xg[j], pair(gs));
+        if constexpr (Q8) {
+            e4m3_unpack(raw.cm, xm);
+            e4m3_unpack(raw.cr, xv);
+            update_q8(xp, xg, xm, xv, raw.scale, a, lr, decay);
+        } else {
+            raw.m.get(xm);
+            raw.v.get(xv);
+            update_f32(xp, xg, xm, xv, a, lr, decay);
+        }
+        auto element = [&](int j) { return e + j; };
+        if constexpr (SR && sizeof(PT) == 2) round_params(xp, key, element);
+        Eight<PT>::put(p, xp);
+        if (sizeof(PT) == 4 && image) Eight<bf16>::put(image, xp);
+        if constexpr (Q8) {
+            const float2 s = quantise<SR>(xm, xv, key, element);
+            *(uint2 *)m = e4m3_pack(xm);
+            *(uint2 *)v = e4m3_pack(xv);
+            if (lane == 0) *scale = s;
+        } else {
+            Eight<float>::put((float *)m, xm);
+            Eight<float>::put((float *)v, xv);
+        }
+    }
 };
 
 template <typename PT, typename GT, bool Q8, bool SR>
-__global__ void __launch_bounds__(WARPS * 32)
+__global__ void __launch_bounds__(WARPS * 32, Q8 ? 3 : 4)
 dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restrict__ chunks, const DenseStep a)
 {
     pdl_trigger();
     const DenseChunk ch = chunks[blockIdx.x];
-    const DenseRec t = recs[ch.rec];
+    const DenseRec &t = recs[ch.rec];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const float lr = __fmul_rn(a.lr, t.lr_mult);
     const float decay = __fsub_rn(1.f, __fmul_rn(lr, __fmul_rn(a.wd, t.wd_mult)));
@@ -321,104 +587,38 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
         gs = *(const volatile float *)a.grad_scale;
         if (!isfinite(gs)) return;
     }
-    PT *P = (PT *)t.p;
-    const GT *G = (const GT *)t.g;
+    constexpr int64_t STRIDE = WARPS * UNIT;
+    int64_t base = ((int64_t)ch.first + warp) * UNIT;
+    int todo = (ch.units - warp + WARPS - 1) / WARPS;   // units of this warp
+    if (ch.vector) {
+        if (todo <= 0) return;
+        VectorUnit<PT, GT, Q8> u(t, base, lane);
+        uint32_t e = (uint32_t)base + lane * 8;
+        RawUnit<PT, GT, Q8> raw;
+        if constexpr (Q8) {
+            // the next unit's loads are on their way while this one is worked on
+            RawUnit<PT, GT, Q8> next;
+            u.load(next, 0);
 #pragma unroll 1
-    for (int u = 0; u < UNITS_PER_WARP; ++u) {
-        const int64_t base = (int64_t)ch.at * CHUNK + (u * WARPS + warp) * UNIT;
-        if (base >= t.n) return;
-        float p[8], g[8], m[8], v[8];
-        float2 scale = make_float2(0.f, 0.f);
-        if constexpr (Q8) scale = t.scale[base / UNIT];
-        if ((t.flags & REC_VEC) && base + UNIT <= t.n) {
-            const int64_t e = base + lane * 8;
-            Walk w(t, e);
-            Eight<PT> rp; rp.load(P + w.at(t.ldp));
-            Eight<GT> rg; rg.load(G + w.at(t.ldg));
-            if constexpr (Q8) {
-                const uint2 cm = load8((const uint8_t *)t.m + e), cv = load8((const uint8_t *)t.v + e);
-                e4m3_unpack(cm, m);
-                e4m3_unpack(cv, v);
-            } else {
-                Eight<float> rm, rv;
-                rm.load((const float *)t.m + e);
-                rv.load((const float *)t.v + e);
-                rm.get(m);
-                rv.get(v);
-            }
-            rp.get(p);
-            rg.get(g);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                g[j] = __fmul_rn(g[j], gs);
-                if constexpr (Q8) { m[j] *= scale.x; v[j] *= scale.y; }
-            }
-            update_eight<Q8>(p, g, m, v, a, lr, decay);
-            auto element = [&](int j) { return e + j; };
-            if constexpr (SR && sizeof(PT) == 2) round_params(p, key, element);
-            Eight<PT>::put(P + w.at(t.ldp), p);
-            if (sizeof(PT) == 4 && t.image) Eight<bf16>::put(t.image + w.at(t.ldi), p);
-            if constexpr (Q8) {
-                const float2 s = quantise_eight<SR>(m, v, key, element);
-                *(uint2 *)((uint8_t *)t.m + e) = e4m3_pack(m);
-                *(uint2 *)((uint8_t *)t.v + e) = e4m3_pack(v);
-                if (lane == 0) t.scale[base / UNIT] = s;
-            } else {
-                Eight<float>::put((float *)t.m + e, m);
-                Eight<float>::put((float *)t.v + e, v);
+            for (; todo > 0; --todo) {
+                raw = next;
+                if (todo > 1) u.load(next, STRIDE);
+                u.template step<SR>(raw, e, lane, gs, a, lr, decay, key);
+                u.advance(STRIDE);
+                e += STRIDE;
             }
         } else {
-            // any alignment, any pitch, and the last unit of a tensor: element by element, 32 neighbours at a time
-            auto element = [&](int j) { return base + lane + 32 * j; };
-            Walk w(t, element(0));
-            int64_t at_p[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int64_t e = element(j);
-                p[j] = g[j] = m[j] = v[j] = 0.f;
-                at_p[j] = 0;
-                if (e < t.n) {
-                    at_p[j] = w.at(t.ldp);
-                    p[j] = to_f32(P[at_p[j]]);
-                    g[j] = __fmul_rn(to_f32(G[w.at(t.ldg)]), gs);
-                    if constexpr (Q8) {
-                        m[j] = scale.x * __half2float(__half(__nv_cvt_fp8_to_halfraw(((const uint8_t *)t.m)[e], __NV_E4M3)));
-                        v[j] = scale.y * __half2float(__half(__nv_cvt_fp8_to_halfraw(((const uint8_t *)t.v)[e], __NV_E4M3)));
-                    } else {
-                        m[j] = ((const float *)t.m)[e];
-                        v[j] = ((const float *)t.v)[e];
-                    }
-                }
-                w.next();
+#pragma unroll 1
+            for (; todo > 0; --todo) {
+                u.load(raw, 0);
+                u.template step<SR>(raw, e, lane, gs, a, lr, decay, key);
+                u.advance(STRIDE);
+                e += STRIDE;
             }
-            update_eight<Q8>(p, g, m, v, a, lr, decay);
-            if constexpr (SR && sizeof(PT) == 2) round_params(p, key, element);
-            float2 s = make_float2(0.f, 0.f);
-            if constexpr (Q8) {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (element(j) >= t.n) m[j] = v[j] = 0.f;   // (0 * NaN of a poisoned block)
-                s = quantise_eight<SR>(m, v, key, element);
-            }
-            Walk wi(t, element(0));
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int64_t e = element(j);
-                if (e < t.n) {
-                    from_f32(P[at_p[j]], p[j]);
-                    if (sizeof(PT) == 4 && t.image) from_f32(t.image[wi.at(t.ldi)], p[j]);
-                    if constexpr (Q8) {
-                        ((uint8_t *)t.m)[e] = __nv_cvt_float_to_fp8(m[j], __NV_SATFINITE, __NV_E4M3);
-                        ((uint8_t *)t.v)[e] = __nv_cvt_float_to_fp8(v[j], __NV_SATFINITE, __NV_E4M3);
-                    } else {
-                        ((float *)t.m)[e] = m[j];
-                        ((float *)t.v)[e] = v[j];
-                    }
-                }
-                wi.next();
-            }
-            if (Q8 && lane == 0) t.scale[base / UNIT] = s;
         }
+    } else {
+#pragma unroll 1
+        for (; todo > 0; --todo, base += STRIDE) step_any_unit<PT, GT, Q8, SR>(t, base, lane, gs, a, lr, decay, key);
     }
 }
 
@@ -426,15 +626,16 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
 
 // Sum of eight squares.  FP32 squares overflow above 1.8e19 and lose bits below 1e-19: where the FP32 sum is outside a
 // range that rules both out, it is taken again in FP64 (the values are still in registers).
-__device__ __forceinline__ double square_sum(const float (&g)[8])
+__device__ __forceinline__ double square_sum(float2 (&x)[4])
 {
-    float s = 0.f;
+    float2 q = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) s = __fmaf_rn(g[j], g[j], s);
+    for (int j = 0; j < 4; ++j) q = fma2(x[j], x[j], q);
+    const float s = __fadd_rn(q.x, q.y);
     if (s >= 1e-25f && s <= 1e37f) return (double)s;
     double d = 0.0;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) d += (double)g[j] * (double)g[j];
+    for (int j = 0; j < 8; ++j) d += (double)at(x, j) * (double)at(x, j);
     return d;
 }
 
@@ -451,7 +652,59 @@ __device__ __forceinline__ double cta_sum(double x, double *sh)   // valid in th
     return x;
 }
 
-__global__ void __launch_bounds__(WARPS * 32)
+// Gradient elements of a unit, any alignment and pitch.
+template <typename GT>
+__device__ __forceinline__ void load_any_grad(const DenseRec &t, int64_t base, int lane, float2 (&g)[4])
+{
+    const GT *G = (const GT *)t.g;
+    Walk w(t, pair_at(base, lane, 0));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t e = pair_at(base, lane, j);
+        g[j] = pair(0.f);
+        if (e < t.n) g[j].x = to_f32(G[w.one(t.ldg)]);
+        if (e + 1 < t.n) g[j].y = to_f32(G[w.two(t.ldg)]);
+        w.next();
+    }
+}
+
+// A warp's sum over its units of a chunk: four units' loads at a time.
+template <typename GT>
+__device__ __forceinline__ double chunk_squares(const DenseRec &t, const DenseChunk &ch, int warp, int lane)
+{
+    double sum = 0.0;
+    int64_t base = ((int64_t)ch.first + warp) * UNIT;
+    int todo = (ch.units - warp + WARPS - 1) / WARPS;
+    constexpr int64_t STRIDE = WARPS * UNIT;
+    if (t.flags & REC_VEC_GRAD) {
+        while (todo > 0) {
+            Eight<GT> r[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (k < todo && base + k * STRIDE + UNIT <= t.n) r[k].load((const GT *)t.g + base + k * STRIDE + lane * 8);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if (k >= todo || base + k * STRIDE + UNIT > t.n) break;
+                float2 g[4];
+                r[k].get(g);
+                sum += square_sum(g);
+            }
+            base += 4 * STRIDE;
+            todo -= 4;
+        }
+        base = ((int64_t)ch.first + ch.units - 1) * UNIT;   // what is left: the tensor's last unit, where it is partial
+        if (base + UNIT <= t.n || warp != (ch.units - 1) % WARPS) return sum;
+        todo = 1;
+    }
+    for (; todo > 0; --todo, base += STRIDE) {
+        float2 g[4];
+        load_any_grad<GT>(t, base, lane, g);
+        sum += square_sum(g);
+    }
+    return sum;
+}
+
+__global__ void __launch_bounds__(WARPS * 32, 4)
 dense_norm_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restrict__ chunks, int count, float max_norm,
                   double *partial, uint32_t *ticket, float *out)
 {
@@ -464,30 +717,7 @@ dense_norm_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
     for (int c = blockIdx.x; c < count; c += gridDim.x) {
         const DenseChunk ch = chunks[c];
         const DenseRec &t = recs[ch.rec];
-#pragma unroll 1
-        for (int u = 0; u < UNITS_PER_WARP; ++u) {
-            const int64_t base = (int64_t)ch.at * CHUNK + (u * WARPS + warp) * UNIT;
-            if (base >= t.n) break;
-            float g[8];
-            if ((t.flags & REC_VEC_GRAD) && base + UNIT <= t.n) {
-                const Walk w(t, base + lane * 8);
-                if (t.flags & REC_G_BF16) {
-                    Eight<bf16> r; r.load((const bf16 *)t.g + w.at(t.ldg)); r.get(g);
-                } else {
-                    Eight<float> r; r.load((const float *)t.g + w.at(t.ldg)); r.get(g);
-                }
-            } else {
-                Walk w(t, base + lane);
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    g[j] = 0.f;
-                    if (base + lane + 32 * j < t.n)
-                        g[j] = (t.flags & REC_G_BF16) ? to_f32(((const bf16 *)t.g)[w.at(t.ldg)]) : ((const float *)t.g)[w.at(t.ldg)];
-                    w.next();
-                }
-            }
-            sum += square_sum(g);
-        }
+        sum += (t.flags & REC_G_BF16) ? chunk_squares<bf16>(t, ch, warp, lane) : chunk_squares<float>(t, ch, warp, lane);
     }
     sum = cta_sum(sum, sh);
     if (threadIdx.x == 0) {
@@ -511,6 +741,56 @@ dense_norm_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
 
 // ---- conversion -----------------------------------------------------------------------------------------------------
 
+template <bool DQ, bool SQ>
+__device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s, const DenseChunk &ch, int warp, int lane)
+{
+    const bool vectors = d.flags & s.flags & REC_VEC_STATE;
+    for (int k = warp; k < ch.units; k += WARPS) {
+        const int64_t base = ((int64_t)ch.first + k) * UNIT, e = base + lane * 8;
+        const bool vec = vectors && base + UNIT <= d.n;
+        float2 m[4], v[4];
+        float2 scale = make_float2(1.f, 1.f);
+        if constexpr (SQ) scale = s.scale[base / UNIT];
+        if (!vec) {
+            load_pairs<SQ>(s.m, s.flags & REC_PAIR_STATE, base, lane, d.n, m);
+            load_pairs<SQ>(s.v, s.flags & REC_PAIR_STATE, base, lane, d.n, v);
+        } else if constexpr (SQ) {
+            const uint2 cm = load8((const uint8_t *)s.m + e), cr = load8((const uint8_t *)s.v + e);
+            e4m3_unpack(cm, m);
+            e4m3_unpack(cr, v);
+        } else {
+            Eight<float> rm, rv;
+            rm.load((const float *)s.m + e);
+            rv.load((const float *)s.v + e);
+            rm.get(m);
+            rv.get(v);
+        }
+        if constexpr (!DQ && SQ) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                m[j] = mul2(m[j], pair(scale.x));
+                v[j] = mul2(v[j], pair(scale.y));
+                v[j] = mul2(v[j], v[j]);
+            }
+        } else if constexpr (DQ && !SQ) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) at(v, j) = __fsqrt_rn(at(v, j));
+            scale = quantise<false>(m, v, UnitKeys{0, 0}, [](int j) { return j; });
+        }
+        if (!vec) {
+            store_pairs<DQ>(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, m);
+            store_pairs<DQ>(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, v);
+        } else if constexpr (DQ) {
+            *(uint2 *)((uint8_t *)d.m + e) = e4m3_pack(m);
+            *(uint2 *)((uint8_t *)d.v + e) = e4m3_pack(v);
+        } else {
+            Eight<float>::put((float *)d.m + e, m);
+            Eight<float>::put((float *)d.v + e, v);
+        }
+        if (DQ && lane == 0) d.scale[base / UNIT] = scale;
+    }
+}
+
 __global__ void __launch_bounds__(WARPS * 32)
 dense_copy_state_kernel(const DenseRec *__restrict__ drecs, const DenseRec *__restrict__ srecs, const DenseChunk *__restrict__ chunks)
 {
@@ -520,64 +800,12 @@ dense_copy_state_kernel(const DenseRec *__restrict__ drecs, const DenseRec *__re
     const DenseRec &s = srecs[ch.rec];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
-    const bool dq = d.flags & REC_Q8, sq = s.flags & REC_Q8;
-#pragma unroll 1
-    for (int u = 0; u < UNITS_PER_WARP; ++u) {
-        const int64_t base = (int64_t)ch.at * CHUNK + (u * WARPS + warp) * UNIT;
-        if (base >= d.n) return;
-        const bool vec = (d.flags & s.flags & REC_VEC_STATE) && base + UNIT <= d.n;
-        float m[8], v[8];
-        auto element = [&](int j) { return vec ? base + lane * 8 + j : base + lane + 32 * j; };
-        float2 scale = make_float2(1.f, 1.f);
-        if (sq) scale = s.scale[base / UNIT];
-        if (vec && sq) {
-            e4m3_unpack(load8((const uint8_t *)s.m + element(0)), m);
-            e4m3_unpack(load8((const uint8_t *)s.v + element(0)), v);
-        } else if (vec) {
-            Eight<float> r;
-            r.load((const float *)s.m + element(0)); r.get(m);
-            r.load((const float *)s.v + element(0)); r.get(v);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int64_t e = element(j);
-                m[j] = v[j] = 0.f;
-                if (e < d.n) {
-                    m[j] = sq ? __half2float(__half(__nv_cvt_fp8_to_halfraw(((const uint8_t *)s.m)[e], __NV_E4M3))) : ((const float *)s.m)[e];
-                    v[j] = sq ? __half2float(__half(__nv_cvt_fp8_to_halfraw(((const uint8_t *)s.v)[e], __NV_E4M3))) : ((const float *)s.v)[e];
-                }
-            }
-        }
-        float2 out_scale = scale;
-        if (!dq && sq) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) { m[j] *= scale.x; v[j] *= scale.y; v[j] = __fmul_rn(v[j], v[j]); }
-        } else if (dq && !sq) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[j] = __fsqrt_rn(v[j]);
-            out_scale = quantise_eight<false>(m, v, UnitKeys{0, 0}, element);
-        }
-        if (vec && dq) {
-            *(uint2 *)((uint8_t *)d.m + element(0)) = e4m3_pack(m);
-            *(uint2 *)((uint8_t *)d.v + element(0)) = e4m3_pack(v);
-        } else if (vec) {
-            Eight<float>::put((float *)d.m + element(0), m);
-            Eight<float>::put((float *)d.v + element(0), v);
-        } else {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int64_t e = element(j);
-                if (e >= d.n) continue;
-                if (dq) {
-                    ((uint8_t *)d.m)[e] = __nv_cvt_float_to_fp8(m[j], __NV_SATFINITE, __NV_E4M3);
-                    ((uint8_t *)d.v)[e] = __nv_cvt_float_to_fp8(v[j], __NV_SATFINITE, __NV_E4M3);
-                } else {
-                    ((float *)d.m)[e] = m[j];
-                    ((float *)d.v)[e] = v[j];
-                }
-            }
-        }
-        if (dq && lane == 0) d.scale[base / UNIT] = out_scale;
+    if (d.flags & REC_Q8) {
+        if (s.flags & REC_Q8) copy_units<true, true>(d, s, ch, warp, lane);
+        else copy_units<true, false>(d, s, ch, warp, lane);
+    } else {
+        if (s.flags & REC_Q8) copy_units<false, true>(d, s, ch, warp, lane);
+        else copy_units<false, false>(d, s, ch, warp, lane);
     }
 }
 
@@ -589,11 +817,12 @@ using namespace tsr;
 
 struct tsr_dense_plan {
     std::vector<tsr_dense_desc> descs;
-    std::vector<DenseRec> recs;
-    std::vector<DenseChunk> chunks;         // state-only tensors, then the stepped ones group by group, then norm-only ones
+    int chunk_units = 0;                    // units of a chunk
+    size_t most_chunks = 0;                 // room for so many in the table
+    // The table lists the chunks of state-only tensors, then of the stepped ones group by group, then of norm-only ones.
     struct Group { int key, first, count; };
     std::vector<Group> groups;              // chunks of tensors that share types: one launch each
-    int step_first = 0, step_end = 0;
+    int step_first = 0, step_end = 0, chunk_count = 0;
     size_t workspace_bytes = 0;
     bool bound = false;
     int device = -1, norm_ctas = 0;
@@ -662,16 +891,10 @@ tsr_status dense_ready(const tsr_dense_plan *plan)
 bool aligned(const void *p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 int64_t size_of(int32_t dtype) { return dtype == TSR_BF16 ? 2 : 4; }
 
-// A matrix whose lanes' vectors of eight elements each lie in one row, aligned to their size.
-bool vector_rows(const void *p, int64_t es, int64_t rows, int64_t cols, int64_t ld)
-{
-    if (!aligned(p, 8 * es)) return false;
-    return ld == cols || rows == 1 || (cols % 8 == 0 && ld % 8 == 0);
-}
-
 tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *workspace)
 {
     std::vector<DenseRec> recs(plan->descs.size());
+    std::vector<char> vector(recs.size(), 0);
     for (size_t i = 0; i < recs.size(); ++i) {
         const tsr_dense_desc &d = plan->descs[i];
         const tsr_dense_ptrs &p = ptrs[i];
@@ -698,28 +921,47 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
         bool dense = true;
         if (grad) {
             r.g = p.grad;
-            dense = dense && d.ldg == d.cols;
-            if (vector_rows(p.grad, gs, d.rows, d.cols, d.ldg)) r.flags |= REC_VEC_GRAD;
+            dense = d.rows <= 1 || d.ldg == d.cols;
+            if (dense && aligned(p.grad, 8 * gs)) r.flags |= REC_VEC_GRAD;
         }
         if (state) {
             r.m = p.m; r.v = p.v;
+            const int64_t es = q8 ? 1 : 4;
             if (q8) r.scale = (float2 *)p.scale;
-            if (aligned(p.m, q8 ? 8 : 32) && aligned(p.v, q8 ? 8 : 32)) r.flags |= REC_VEC_STATE;
+            if (aligned(p.m, 8 * es) && aligned(p.v, 8 * es)) r.flags |= REC_VEC_STATE;
+            if (aligned(p.m, 2 * es) && aligned(p.v, 2 * es)) r.flags |= REC_PAIR_STATE;
         }
         if (step) {
             r.p = p.param;
             r.image = (bf16 *)p.image;
-            dense = dense && d.ldp == d.cols && (!p.image || d.ldi == d.cols);
-            if ((r.flags & REC_VEC_GRAD) && (r.flags & REC_VEC_STATE) && vector_rows(p.param, ps, d.rows, d.cols, d.ldp) &&
-                (!p.image || vector_rows(p.image, 2, d.rows, d.cols, d.ldi)))
-                r.flags |= REC_VEC;
+            dense = dense && (d.rows <= 1 || (d.ldp == d.cols && (!p.image || d.ldi == d.cols)));
+            vector[i] = dense && (r.flags & REC_VEC_GRAD) && (r.flags & REC_VEC_STATE) && aligned(p.param, 8 * ps) && aligned(p.image, 16);
         }
-        if (!dense && d.rows > 1) {
-            r.flags |= REC_PITCHED;
-            // one pitched matrix among dense ones: vectors of the dense ones would cross its rows
-            if (d.cols % 8 != 0) r.flags &= ~(uint32_t)(REC_VEC | REC_VEC_GRAD);
-        }
+        if (!dense) r.flags |= REC_PITCHED;
     }
+    std::vector<DenseChunk> chunks;
+    std::vector<tsr_dense_plan::Group> groups;
+    chunks.reserve(plan->most_chunks);
+    // Whole units of a tensor in chunks of chunk_units; on the vector path its partial last unit is a chunk of its own.
+    auto add = [&](size_t i) {
+        const int64_t units = (recs[i].n + UNIT - 1) / UNIT, whole = vector[i] ? recs[i].n / UNIT : units;
+        for (int64_t k = 0; k < whole; k += plan->chunk_units)
+            chunks.push_back({(int32_t)i, (uint32_t)k, (int32_t)std::min<int64_t>(plan->chunk_units, whole - k), vector[i] ? 1 : 0});
+        if (whole < units) chunks.push_back({(int32_t)i, (uint32_t)whole, 1, 0});
+    };
+    for (size_t i = 0; i < recs.size(); ++i)
+        if (plan->descs[i].flags == TSR_DENSE_STATE_ONLY) add(i);
+    const int step_first = (int)chunks.size();
+    for (int key = 0; key < KEY_COUNT; ++key) {
+        const int first = (int)chunks.size();
+        for (size_t i = 0; i < recs.size(); ++i)
+            if (plan->descs[i].flags == 0 && key_of(plan->descs[i]) == key) add(i);
+        const int got = (int)chunks.size() - first;
+        if (got) groups.push_back({key, first, got});
+    }
+    const int step_end = (int)chunks.size();
+    for (size_t i = 0; i < recs.size(); ++i)
+        if (plan->descs[i].flags == TSR_DENSE_NORM_ONLY) add(i);
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return dense_fail(plan, TSR_ERR_CUDA, "no CUDA device available");
     DENSE_CUDA(plan, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
@@ -729,16 +971,18 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     plan->d_recs = (DenseRec *)at;
     at += round_up((int64_t)(recs.size() * sizeof(DenseRec)), 256);
     plan->d_chunks = (DenseChunk *)at;
-    at += round_up((int64_t)(plan->chunks.size() * sizeof(DenseChunk)), 256);
+    at += round_up((int64_t)(plan->most_chunks * sizeof(DenseChunk)), 256);
     plan->d_partial = (double *)at;
     at += NORM_CTAS * sizeof(double);
     plan->d_ticket = (uint32_t *)at;
     if (!recs.empty()) DENSE_CUDA(plan, cudaMemcpy(plan->d_recs, recs.data(), recs.size() * sizeof(DenseRec), cudaMemcpyHostToDevice));
-    if (!plan->chunks.empty())
-        DENSE_CUDA(plan, cudaMemcpy(plan->d_chunks, plan->chunks.data(), plan->chunks.size() * sizeof(DenseChunk), cudaMemcpyHostToDevice));
+    if (!chunks.empty()) DENSE_CUDA(plan, cudaMemcpy(plan->d_chunks, chunks.data(), chunks.size() * sizeof(DenseChunk), cudaMemcpyHostToDevice));
     DENSE_CUDA(plan, cudaMemset(plan->d_ticket, 0, sizeof(uint32_t)));
     DENSE_CUDA(plan, cudaDeviceSynchronize());
-    plan->recs.swap(recs);
+    plan->groups.swap(groups);
+    plan->chunk_count = (int)chunks.size();
+    plan->step_first = step_first;
+    plan->step_end = step_end;
     plan->device = dev;
     plan->norm_ctas = std::min(NORM_CTAS, 8 * sms);
     plan->bound = true;
@@ -748,25 +992,17 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
 void dense_layout(tsr_dense_plan *plan, const tsr_dense_desc *descs, int32_t count)
 {
     if (count > 0) plan->descs.assign(descs, descs + count);
-    auto add = [&](int i) {
-        const int64_t n = plan->descs[i].rows * plan->descs[i].cols;
-        for (int64_t k = 0; k * CHUNK < n; ++k) plan->chunks.push_back({i, (int32_t)k});
+    // Long chunks spread the cost of a CTA's start and let loads run ahead; short ones fill the GPU when there is little to do.
+    auto chunks_at = [&](int64_t units) {   // of so many units, and the last units of the vector path
+        int64_t k = 0;
+        for (const tsr_dense_desc &d : plan->descs) k += (d.rows * d.cols + units * UNIT - 1) / (units * UNIT) + 1;
+        return k;
     };
-    for (int i = 0; i < count; ++i)
-        if (plan->descs[i].flags == TSR_DENSE_STATE_ONLY) add(i);
-    plan->step_first = (int)plan->chunks.size();
-    for (int key = 0; key < KEY_COUNT; ++key) {
-        const int first = (int)plan->chunks.size();
-        for (int i = 0; i < count; ++i)
-            if (plan->descs[i].flags == 0 && key_of(plan->descs[i]) == key) add(i);
-        const int got = (int)plan->chunks.size() - first;
-        if (got) plan->groups.push_back({key, first, got});
-    }
-    plan->step_end = (int)plan->chunks.size();
-    for (int i = 0; i < count; ++i)
-        if (plan->descs[i].flags == TSR_DENSE_NORM_ONLY) add(i);
+    plan->chunk_units = WARPS * MAX_UNITS;
+    while (plan->chunk_units > WARPS && chunks_at(plan->chunk_units) < MANY_CHUNKS) plan->chunk_units /= 2;
+    plan->most_chunks = (size_t)chunks_at(plan->chunk_units);
     plan->workspace_bytes = (size_t)(round_up((int64_t)(plan->descs.size() * sizeof(DenseRec)), 256) +
-                                     round_up((int64_t)(plan->chunks.size() * sizeof(DenseChunk)), 256) +
+                                     round_up((int64_t)(plan->most_chunks * sizeof(DenseChunk)), 256) +
                                      NORM_CTAS * (int64_t)sizeof(double) + 256);
 }
 
@@ -793,7 +1029,7 @@ tsr_status tsr_dense_plan_create(tsr_dense_plan **out, const tsr_dense_desc *des
         const int64_t most = DENSE_MOST;
         if (d.rows > 0 && d.cols > most / d.rows) return TSR_ERR_SHAPE;
         if (d.rows > 0 && ((grad && d.ldg > most / d.rows) || (step && d.ldp > most / d.rows))) return TSR_ERR_SHAPE;
-        total += (d.rows * d.cols + CHUNK - 1) / CHUNK;
+        total += (d.rows * d.cols + WARPS * UNIT - 1) / (WARPS * UNIT) + 1;
         if (total > 0x7fffffff) return TSR_ERR_SHAPE;
     }
     tsr_dense_plan *plan = new (std::nothrow) tsr_dense_plan;
@@ -882,7 +1118,7 @@ tsr_status tsr_dense_plan_grad_norm(tsr_dense_plan *plan, float max_norm, float 
     if (!aligned(out, 4)) return dense_fail(plan, TSR_ERR_ALIGNMENT, "out is not aligned to a float");
     tsr_status st = dense_ready(plan);
     if (st != TSR_OK) return st;
-    const int count = (int)plan->chunks.size() - plan->step_first;
+    const int count = plan->chunk_count - plan->step_first;
     const int ctas = std::max(1, std::min(plan->norm_ctas, count));
     DENSE_CUDA(plan, launch_dependent(dense_norm_kernel, dim3(ctas), dim3(WARPS * 32), 0, (cudaStream_t)stream, 1,
                                       (const DenseRec *)plan->d_recs, (const DenseChunk *)plan->d_chunks + plan->step_first, count, max_norm,
