@@ -23,8 +23,11 @@ namespace tsr {
 constexpr int UNIT = TSR_DENSE_BLOCK;      // elements of a warp's piece of work
 static_assert(UNIT == 32 * 8, "a lane holds eight elements of a unit");
 constexpr int WARPS = 8;                   // per CTA
-constexpr int MAX_UNITS = 8;               // units of a warp in one chunk: 1, 2, 4 or 8 (chosen per plan)
-constexpr int MANY_CHUNKS = 2048;
+// Most units of a warp in one chunk, by what goes over the chunk.  FP32 steps overlap by having many CTAs at a time and
+// are faster short (1B set: 4.81 ms with 2 units, 4.96 with 8); the others have work per CTA or load ahead (130M set, 8-bit
+// step: 301 us with 1 unit, 232 with 2, 213 with 8; 1B norm: 1164, 705, 440 and 406 with 16).
+constexpr int STEP_F32_UNITS = 2, STEP_Q8_UNITS = 8, COPY_UNITS = 16, NORM_UNITS = 16;
+constexpr int MANY_CHUNKS = 2048;          // fewer than this: shorter chunks, so that the GPU fills
 constexpr int NORM_CTAS = 1184;            // most CTAs of a norm launch (8 on each of 148 SMs)
 
 enum DenseRecFlags : uint32_t {
@@ -137,9 +140,6 @@ __device__ __forceinline__ float &at(float2 (&x)[4], int j) { return (j & 1) ? x
 
 // ---- 8-bit values ---------------------------------------------------------------------------------------------------
 
-__device__ __forceinline__ float e4m3_value(uint8_t c) { return __half2float(__half(__nv_cvt_fp8_to_halfraw(c, __NV_E4M3))); }
-__device__ __forceinline__ uint8_t e4m3_code(float x) { return __nv_cvt_float_to_fp8(x, __NV_SATFINITE, __NV_E4M3); }
-
 __device__ __forceinline__ void e4m3_unpack(uint2 c, float2 (&x)[4])
 {
     const uint32_t w[2] = {c.x, c.y};
@@ -184,16 +184,6 @@ __device__ __forceinline__ uint32_t random_word(uint32_t counter, uint32_t key1,
     x = x ^ (x >> 13) ^ key2;
     x *= 0xc2b2ae35u;
     return x ^ (x >> 16);
-}
-
-// a in [0, 448] rounded to an E4M3 value, up with probability (remainder / spacing): 16 random bits (`bits20`: with four
-// zeros below them) are added below the three mantissa bits and the rest is cut off.  Below 2^-6 the spacing is 2^-9
-// throughout; adding 2^-6 first puts such values where FP32 numbers with three mantissa bits have that spacing.
-__device__ __forceinline__ float e4m3_stochastic(float a, uint32_t bits20)
-{
-    const float c = a < 0x1p-6f ? 0x1p-6f : 0.f;
-    const uint32_t z = __float_as_uint(__fadd_rn(a, c)) + bits20;
-    return __fsub_rn(__uint_as_float(z & 0xfff00000u), c);
 }
 
 // ---- one unit's arithmetic ------------------------------------------------------------------------------------------
@@ -295,30 +285,53 @@ __device__ __forceinline__ void update_q8(float2 (&p)[4], const float2 (&g)[4], 
     }
 }
 
-// New scales of the warp's block; m and r become x / scale, rounded to E4M3 values where the rounding is stochastic
-// (the conversion to 8 bits rounds to nearest).  element(j) is the position of element j of the lane in the tensor.
+// New scales of the warp's block, and the codes of x / scale for the lane's eight m and r; element(j) is the position of
+// element j of the lane in the tensor.
+//
+// To nearest, the conversion instruction does it.  Stochastic: 2^-120 x / scale has the E4M3 code of x / scale in its bits 20
+// to 26, FP32's exponent field running as E4M3's does and its denormal numbers being E4M3's (both have a spacing of one unit
+// below exponent 1), so 16 random bits are added below bit 20 and the rest is cut off: one multiply-add on the bits, which
+// also moves the code to the top byte.  Without this the integer pipe was the limit (81 % busy; 69 instructions an
+// element, now 53).
 template <bool SR, typename Elem>
-__device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&r)[4], UnitKeys k, Elem element)
+__device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&r)[4], UnitKeys k, Elem element, uint2 &cm, uint2 &cr)
 {
     float2 scale, inv;
     block_scale(__float_as_uint(warp_max_abs(max_abs8(m))), scale.x, inv.x);
     block_scale(__float_as_uint(warp_max_abs(max_abs8(r))), scale.y, inv.y);
+    if constexpr (SR) {
+        uint32_t um[8], ur[8];
+        float2 ym[4], yr[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        // 0 for r = 0, at least 2^-9 for any other r (those are above 2^-75)
-        const float2 some = mul2(r[j], pair(0x1p100f));
-        m[j] = mul2(m[j], pair(inv.x));
-        r[j] = mul2(r[j], pair(inv.y));
-        if constexpr (SR) {
-            const uint32_t w0 = random_word((uint32_t)element(2 * j), k.k1, k.k2);
-            const uint32_t w1 = random_word((uint32_t)element(2 * j + 1), k.k1, k.k2);
-            m[j].x = copysignf(e4m3_stochastic(fabsf(m[j].x), (w0 << 4) & 0xffff0u), m[j].x);
-            m[j].y = copysignf(e4m3_stochastic(fabsf(m[j].y), (w1 << 4) & 0xffff0u), m[j].y);
-            r[j].x = e4m3_stochastic(r[j].x, (w0 >> 12) & 0xffff0u);
-            r[j].y = e4m3_stochastic(r[j].y, (w1 >> 12) & 0xffff0u);
+        for (int j = 0; j < 4; ++j) {
+            ym[j] = mul2(mul2(m[j], pair(inv.x)), pair(0x1p-120f));
+            yr[j] = mul2(mul2(r[j], pair(inv.y)), pair(0x1p-120f));
         }
-        r[j].x = fmaxf(r[j].x, fminf(some.x, 0x1p-9f));
-        r[j].y = fmaxf(r[j].y, fminf(some.y, 0x1p-9f));
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t w = random_word((uint32_t)element(j), k.k1, k.k2);
+            // a root above zero (it is above 2^-75 then) has code 1 at least
+            const uint32_t some = min(__float_as_uint(at(r, j)), 1u << 24);
+            const uint32_t bm = __float_as_uint(at(ym, j)), br = __float_as_uint(at(yr, j));
+            um[j] = (bm * 16u + __byte_perm(w, 0, 0x4104)) | (bm & 0x80000000u);
+            ur[j] = max(br * 16u + __byte_perm(w, 0, 0x4324), some);
+        }
+        cm.x = __byte_perm(__byte_perm(um[0], um[1], 0x0073), __byte_perm(um[2], um[3], 0x0073), 0x5410);
+        cm.y = __byte_perm(__byte_perm(um[4], um[5], 0x0073), __byte_perm(um[6], um[7], 0x0073), 0x5410);
+        cr.x = __byte_perm(__byte_perm(ur[0], ur[1], 0x0073), __byte_perm(ur[2], ur[3], 0x0073), 0x5410);
+        cr.y = __byte_perm(__byte_perm(ur[4], ur[5], 0x0073), __byte_perm(ur[6], ur[7], 0x0073), 0x5410);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            // 0 for r = 0, at least 2^-9 for any other r (those are above 2^-75)
+            const float2 some = mul2(r[j], pair(0x1p100f));
+            m[j] = mul2(m[j], pair(inv.x));
+            r[j] = mul2(r[j], pair(inv.y));
+            r[j].x = fmaxf(r[j].x, fminf(some.x, 0x1p-9f));
+            r[j].y = fmaxf(r[j].y, fminf(some.y, 0x1p-9f));
+        }
+        cm = e4m3_pack(m);
+        cr = e4m3_pack(r);
     }
     return scale;
 }
@@ -400,27 +413,31 @@ __device__ __forceinline__ void load_pairs(const void *src, bool both, int64_t b
         }
     }
 }
-template <bool Q8>
+__device__ __forceinline__ void store_code_pairs(void *dst, bool both, int64_t base, int lane, int64_t n, uint2 codes)
+{
+    const uint32_t w[2] = {codes.x, codes.y};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int64_t e = pair_at(base, lane, j);
+        uint8_t *c = (uint8_t *)dst + e;
+        const uint32_t two = w[j >> 1] >> (16 * (j & 1));
+        if (both && e + 1 < n) *(uint16_t *)c = (uint16_t)two;
+        else {
+            if (e < n) c[0] = (uint8_t)two;
+            if (e + 1 < n) c[1] = (uint8_t)(two >> 8);
+        }
+    }
+}
 __device__ __forceinline__ void store_pairs(void *dst, bool both, int64_t base, int lane, int64_t n, const float2 (&x)[4])
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t e = pair_at(base, lane, j);
-        if constexpr (Q8) {
-            uint8_t *c = (uint8_t *)dst + e;
-            const uint32_t w = __nv_cvt_float2_to_fp8x2(x[j], __NV_SATFINITE, __NV_E4M3);
-            if (both && e + 1 < n) *(uint16_t *)c = (uint16_t)w;
-            else {
-                if (e < n) c[0] = (uint8_t)w;
-                if (e + 1 < n) c[1] = (uint8_t)(w >> 8);
-            }
-        } else {
-            float *f = (float *)dst + e;
-            if (both && e + 1 < n) *(float2 *)f = x[j];
-            else {
-                if (e < n) f[0] = x[j].x;
-                if (e + 1 < n) f[1] = x[j].y;
-            }
+        float *f = (float *)dst + e;
+        if (both && e + 1 < n) *(float2 *)f = x[j];
+        else {
+            if (e < n) f[0] = x[j].x;
+            if (e + 1 < n) f[1] = x[j].y;
         }
     }
 }
@@ -477,11 +494,15 @@ __device__ __forceinline__ void step_any_unit(const DenseRec &t, int64_t base, i
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (element(j) >= t.n) at(m, j) = at(v, j) = 0.f;   // (0 * NaN of a poisoned block)
-        const float2 s = quantise<SR>(m, v, key, element);
+        uint2 cm, cr;
+        const float2 s = quantise<SR>(m, v, key, element, cm, cr);
         if (lane == 0) t.scale[base / UNIT] = s;
+        store_code_pairs(t.m, both, base, lane, t.n, cm);
+        store_code_pairs(t.v, both, base, lane, t.n, cr);
+    } else {
+        store_pairs(t.m, both, base, lane, t.n, m);
+        store_pairs(t.v, both, base, lane, t.n, v);
     }
-    store_pairs<Q8>(t.m, both, base, lane, t.n, m);
-    store_pairs<Q8>(t.v, both, base, lane, t.n, v);
 }
 
 // One whole unit of the vector path as it lies in memory: the lane's eight elements of everything.
@@ -555,9 +576,10 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
         Eight<PT>::put(p, xp);
         if (sizeof(PT) == 4 && image) Eight<bf16>::put(image, xp);
         if constexpr (Q8) {
-            const float2 s = quantise<SR>(xm, xv, key, element);
-            *(uint2 *)m = e4m3_pack(xm);
-            *(uint2 *)v = e4m3_pack(xv);
+            uint2 cm, cr;
+            const float2 s = quantise<SR>(xm, xv, key, element, cm, cr);
+            *(uint2 *)m = cm;
+            *(uint2 *)v = cr;
             if (lane == 0) *scale = s;
         } else {
             Eight<float>::put((float *)m, xm);
@@ -668,7 +690,7 @@ __device__ __forceinline__ void load_any_grad(const DenseRec &t, int64_t base, i
     }
 }
 
-// A warp's sum over its units of a chunk: four units' loads at a time.
+// A warp's sum over its units of a chunk, 64 bytes of every lane at a time.
 template <typename GT>
 __device__ __forceinline__ double chunk_squares(const DenseRec &t, const DenseChunk &ch, int warp, int lane)
 {
@@ -676,21 +698,22 @@ __device__ __forceinline__ double chunk_squares(const DenseRec &t, const DenseCh
     int64_t base = ((int64_t)ch.first + warp) * UNIT;
     int todo = (ch.units - warp + WARPS - 1) / WARPS;
     constexpr int64_t STRIDE = WARPS * UNIT;
+    constexpr int AT_ONCE = 64 / (8 * (int)sizeof(GT));
     if (t.flags & REC_VEC_GRAD) {
         while (todo > 0) {
-            Eight<GT> r[4];
+            Eight<GT> r[AT_ONCE];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int k = 0; k < AT_ONCE; ++k)
                 if (k < todo && base + k * STRIDE + UNIT <= t.n) r[k].load((const GT *)t.g + base + k * STRIDE + lane * 8);
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < AT_ONCE; ++k) {
                 if (k >= todo || base + k * STRIDE + UNIT > t.n) break;
                 float2 g[4];
                 r[k].get(g);
                 sum += square_sum(g);
             }
-            base += 4 * STRIDE;
-            todo -= 4;
+            base += AT_ONCE * STRIDE;
+            todo -= AT_ONCE;
         }
         base = ((int64_t)ch.first + ch.units - 1) * UNIT;   // what is left: the tensor's last unit, where it is partial
         if (base + UNIT <= t.n || warp != (ch.units - 1) % WARPS) return sum;
@@ -750,12 +773,14 @@ __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s,
         const bool vec = vectors && base + UNIT <= d.n;
         float2 m[4], v[4];
         float2 scale = make_float2(1.f, 1.f);
+        uint2 cm, cr;
         if constexpr (SQ) scale = s.scale[base / UNIT];
         if (!vec) {
             load_pairs<SQ>(s.m, s.flags & REC_PAIR_STATE, base, lane, d.n, m);
             load_pairs<SQ>(s.v, s.flags & REC_PAIR_STATE, base, lane, d.n, v);
         } else if constexpr (SQ) {
-            const uint2 cm = load8((const uint8_t *)s.m + e), cr = load8((const uint8_t *)s.v + e);
+            cm = load8((const uint8_t *)s.m + e);
+            cr = load8((const uint8_t *)s.v + e);
             e4m3_unpack(cm, m);
             e4m3_unpack(cr, v);
         } else {
@@ -775,14 +800,22 @@ __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s,
         } else if constexpr (DQ && !SQ) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) at(v, j) = __fsqrt_rn(at(v, j));
-            scale = quantise<false>(m, v, UnitKeys{0, 0}, [](int j) { return j; });
+            scale = quantise<false>(m, v, UnitKeys{0, 0}, [](int j) { return j; }, cm, cr);
+        } else if constexpr (DQ) {   // codes of their own values
+            cm = e4m3_pack(m);
+            cr = e4m3_pack(v);
         }
-        if (!vec) {
-            store_pairs<DQ>(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, m);
-            store_pairs<DQ>(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, v);
-        } else if constexpr (DQ) {
-            *(uint2 *)((uint8_t *)d.m + e) = e4m3_pack(m);
-            *(uint2 *)((uint8_t *)d.v + e) = e4m3_pack(v);
+        if constexpr (DQ) {
+            if (vec) {
+                *(uint2 *)((uint8_t *)d.m + e) = cm;
+                *(uint2 *)((uint8_t *)d.v + e) = cr;
+            } else {
+                store_code_pairs(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, cm);
+                store_code_pairs(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, cr);
+            }
+        } else if (!vec) {
+            store_pairs(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, m);
+            store_pairs(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, v);
         } else {
             Eight<float>::put((float *)d.m + e, m);
             Eight<float>::put((float *)d.v + e, v);
@@ -817,12 +850,13 @@ using namespace tsr;
 
 struct tsr_dense_plan {
     std::vector<tsr_dense_desc> descs;
-    int chunk_units = 0;                    // units of a chunk
+    // Units of a chunk when stepping (FP32 and 8-bit states), taking the norm and copying states.
+    int step_units[2] = {}, norm_units = 0, copy_units = 0;
     size_t most_chunks = 0;                 // room for so many in the table
-    // The table lists the chunks of state-only tensors, then of the stepped ones group by group, then of norm-only ones.
+    // One table: the chunks of the stepped tensors group by group, then those of the norm, then those of copies.
     struct Group { int key, first, count; };
-    std::vector<Group> groups;              // chunks of tensors that share types: one launch each
-    int step_first = 0, step_end = 0, chunk_count = 0;
+    std::vector<Group> groups;              // tensors that share types: one launch each
+    int norm_first = 0, copy_first = 0, chunk_count = 0;
     size_t workspace_bytes = 0;
     bool bound = false;
     int device = -1, norm_ctas = 0;
@@ -942,26 +976,25 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     std::vector<DenseChunk> chunks;
     std::vector<tsr_dense_plan::Group> groups;
     chunks.reserve(plan->most_chunks);
-    // Whole units of a tensor in chunks of chunk_units; on the vector path its partial last unit is a chunk of its own.
-    auto add = [&](size_t i) {
-        const int64_t units = (recs[i].n + UNIT - 1) / UNIT, whole = vector[i] ? recs[i].n / UNIT : units;
-        for (int64_t k = 0; k < whole; k += plan->chunk_units)
-            chunks.push_back({(int32_t)i, (uint32_t)k, (int32_t)std::min<int64_t>(plan->chunk_units, whole - k), vector[i] ? 1 : 0});
+    auto add = [&](size_t i, bool vec, int at_once) {   // on the vector path, the partial last unit is a chunk of its own
+        const int64_t units = (recs[i].n + UNIT - 1) / UNIT, whole = vec ? recs[i].n / UNIT : units;
+        for (int64_t k = 0; k < whole; k += at_once)
+            chunks.push_back({(int32_t)i, (uint32_t)k, (int32_t)std::min<int64_t>(at_once, whole - k), vec ? 1 : 0});
         if (whole < units) chunks.push_back({(int32_t)i, (uint32_t)whole, 1, 0});
     };
-    for (size_t i = 0; i < recs.size(); ++i)
-        if (plan->descs[i].flags == TSR_DENSE_STATE_ONLY) add(i);
-    const int step_first = (int)chunks.size();
     for (int key = 0; key < KEY_COUNT; ++key) {
         const int first = (int)chunks.size();
         for (size_t i = 0; i < recs.size(); ++i)
-            if (plan->descs[i].flags == 0 && key_of(plan->descs[i]) == key) add(i);
+            if (plan->descs[i].flags == 0 && key_of(plan->descs[i]) == key) add(i, vector[i], plan->step_units[plan->descs[i].state]);
         const int got = (int)chunks.size() - first;
         if (got) groups.push_back({key, first, got});
     }
-    const int step_end = (int)chunks.size();
+    const int norm_first = (int)chunks.size();
     for (size_t i = 0; i < recs.size(); ++i)
-        if (plan->descs[i].flags == TSR_DENSE_NORM_ONLY) add(i);
+        if (plan->descs[i].flags != TSR_DENSE_STATE_ONLY) add(i, false, plan->norm_units);
+    const int copy_first = (int)chunks.size();
+    for (size_t i = 0; i < recs.size(); ++i)
+        if (plan->descs[i].flags != TSR_DENSE_NORM_ONLY) add(i, false, plan->copy_units);
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return dense_fail(plan, TSR_ERR_CUDA, "no CUDA device available");
     DENSE_CUDA(plan, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
@@ -981,8 +1014,8 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     DENSE_CUDA(plan, cudaDeviceSynchronize());
     plan->groups.swap(groups);
     plan->chunk_count = (int)chunks.size();
-    plan->step_first = step_first;
-    plan->step_end = step_end;
+    plan->norm_first = norm_first;
+    plan->copy_first = copy_first;
     plan->device = dev;
     plan->norm_ctas = std::min(NORM_CTAS, 8 * sms);
     plan->bound = true;
@@ -992,15 +1025,22 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
 void dense_layout(tsr_dense_plan *plan, const tsr_dense_desc *descs, int32_t count)
 {
     if (count > 0) plan->descs.assign(descs, descs + count);
-    // Long chunks spread the cost of a CTA's start and let loads run ahead; short ones fill the GPU when there is little to do.
-    auto chunks_at = [&](int64_t units) {   // of so many units, and the last units of the vector path
+    auto chunks_at = [&](int64_t units) {   // of so many units, with the last units of the vector path
         int64_t k = 0;
         for (const tsr_dense_desc &d : plan->descs) k += (d.rows * d.cols + units * UNIT - 1) / (units * UNIT) + 1;
         return k;
     };
-    plan->chunk_units = WARPS * MAX_UNITS;
-    while (plan->chunk_units > WARPS && chunks_at(plan->chunk_units) < MANY_CHUNKS) plan->chunk_units /= 2;
-    plan->most_chunks = (size_t)chunks_at(plan->chunk_units);
+    // Long chunks spread the cost of a CTA's start and let loads run ahead; short ones fill the GPU when there is little to do.
+    auto fit = [&](int units) {
+        units *= WARPS;
+        while (units > WARPS && chunks_at(units) < MANY_CHUNKS) units /= 2;
+        return units;
+    };
+    plan->step_units[TSR_STATE_F32] = fit(STEP_F32_UNITS);
+    plan->step_units[TSR_STATE_Q8] = fit(STEP_Q8_UNITS);
+    plan->norm_units = fit(NORM_UNITS);
+    plan->copy_units = fit(COPY_UNITS);
+    plan->most_chunks = (size_t)(chunks_at(plan->step_units[TSR_STATE_F32]) + chunks_at(plan->norm_units) + chunks_at(plan->copy_units));
     plan->workspace_bytes = (size_t)(round_up((int64_t)(plan->descs.size() * sizeof(DenseRec)), 256) +
                                      round_up((int64_t)(plan->most_chunks * sizeof(DenseChunk)), 256) +
                                      NORM_CTAS * (int64_t)sizeof(double) + 256);
@@ -1029,7 +1069,7 @@ tsr_status tsr_dense_plan_create(tsr_dense_plan **out, const tsr_dense_desc *des
         const int64_t most = DENSE_MOST;
         if (d.rows > 0 && d.cols > most / d.rows) return TSR_ERR_SHAPE;
         if (d.rows > 0 && ((grad && d.ldg > most / d.rows) || (step && d.ldp > most / d.rows))) return TSR_ERR_SHAPE;
-        total += (d.rows * d.cols + WARPS * UNIT - 1) / (WARPS * UNIT) + 1;
+        total += 3 * ((d.rows * d.cols + WARPS * UNIT - 1) / (WARPS * UNIT) + 1);
         if (total > 0x7fffffff) return TSR_ERR_SHAPE;
     }
     tsr_dense_plan *plan = new (std::nothrow) tsr_dense_plan;
@@ -1118,10 +1158,10 @@ tsr_status tsr_dense_plan_grad_norm(tsr_dense_plan *plan, float max_norm, float 
     if (!aligned(out, 4)) return dense_fail(plan, TSR_ERR_ALIGNMENT, "out is not aligned to a float");
     tsr_status st = dense_ready(plan);
     if (st != TSR_OK) return st;
-    const int count = plan->chunk_count - plan->step_first;
+    const int count = plan->copy_first - plan->norm_first;
     const int ctas = std::max(1, std::min(plan->norm_ctas, count));
     DENSE_CUDA(plan, launch_dependent(dense_norm_kernel, dim3(ctas), dim3(WARPS * 32), 0, (cudaStream_t)stream, 1,
-                                      (const DenseRec *)plan->d_recs, (const DenseChunk *)plan->d_chunks + plan->step_first, count, max_norm,
+                                      (const DenseRec *)plan->d_recs, (const DenseChunk *)plan->d_chunks + plan->norm_first, count, max_norm,
                                       plan->d_partial, plan->d_ticket, out));
     return TSR_OK;
 }
@@ -1140,9 +1180,10 @@ tsr_status tsr_dense_plan_copy_state(tsr_dense_plan *dst, const tsr_dense_plan *
     if (st != TSR_OK) return st;
     if (!src->bound) return dense_fail(dst, TSR_ERR_NOT_BOUND, "the source plan is not bound");
     if (src->device != dst->device) return dense_fail(dst, TSR_ERR_INVALID_ARG, "the plans are bound on different devices");
-    if (dst == src || dst->step_end == 0) return TSR_OK;
-    DENSE_CUDA(dst, launch_dependent(dense_copy_state_kernel, dim3(dst->step_end), dim3(WARPS * 32), 0, (cudaStream_t)stream, 1,
-                                     (const DenseRec *)dst->d_recs, (const DenseRec *)src->d_recs, (const DenseChunk *)dst->d_chunks));
+    const int count = dst->chunk_count - dst->copy_first;
+    if (dst == src || count == 0) return TSR_OK;
+    DENSE_CUDA(dst, launch_dependent(dense_copy_state_kernel, dim3(count), dim3(WARPS * 32), 0, (cudaStream_t)stream, 1,
+                                     (const DenseRec *)dst->d_recs, (const DenseRec *)src->d_recs, (const DenseChunk *)dst->d_chunks + dst->copy_first));
     return TSR_OK;
 }
 
