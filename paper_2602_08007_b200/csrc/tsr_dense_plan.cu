@@ -111,6 +111,16 @@ template <> struct Eight<float> {
         store32(p, r);
     }
 };
+__device__ __forceinline__ uint4 bf16_pack(const float2 (&x)[4])
+{
+    uint32_t w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const __nv_bfloat162 b = __floats2bfloat162_rn(x[j].x, x[j].y);
+        w[j] = *(const uint32_t *)&b;
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
 template <> struct Eight<bf16> {
     uint4 r;
     __device__ __forceinline__ void load(const bf16 *p) { r = load16(p); }
@@ -120,16 +130,7 @@ template <> struct Eight<bf16> {
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
     }
-    static __device__ __forceinline__ void put(bf16 *p, const float2 (&x)[4])
-    {
-        uint32_t w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const __nv_bfloat162 b = __floats2bfloat162_rn(x[j].x, x[j].y);
-            w[j] = *(const uint32_t *)&b;
-        }
-        *(uint4 *)p = make_uint4(w[0], w[1], w[2], w[3]);
-    }
+    static __device__ __forceinline__ void put(bf16 *p, const float2 (&x)[4]) { *(uint4 *)p = bf16_pack(x); }
 };
 
 __device__ __forceinline__ float to_f32(float x) { return x; }
@@ -176,14 +177,14 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x)
 {
     x ^= x >> 16; x *= 0x85ebca6bu; x ^= x >> 13; x *= 0xc2b2ae35u; return x ^ (x >> 16);
 }
+// The word before its last step x ^ (x >> 16): the upper half is final, the lower one is still to be combined with it.
 __device__ __forceinline__ uint32_t random_word(uint32_t counter, uint32_t key1, uint32_t key2)
 {
     uint32_t x = counter + key1;
     x ^= x >> 16;
     x *= 0x85ebca6bu;
     x = x ^ (x >> 13) ^ key2;
-    x *= 0xc2b2ae35u;
-    return x ^ (x >> 16);
+    return x * 0xc2b2ae35u;
 }
 
 // ---- one unit's arithmetic ------------------------------------------------------------------------------------------
@@ -227,6 +228,14 @@ __device__ __forceinline__ float max_abs8(const float2 (&x)[4])
 {
     return max_abs3(max_abs3(x[0].x, x[0].y, x[1].x), max_abs3(x[1].y, x[2].x, x[2].y), max_abs3(x[3].x, x[3].y, 0.f));
 }
+__device__ __forceinline__ float max8(const float2 (&x)[4])
+{
+    return fmaxf(fmaxf(fmaxf(x[0].x, x[0].y), fmaxf(x[1].x, x[1].y)), fmaxf(fmaxf(x[2].x, x[2].y), fmaxf(x[3].x, x[3].y)));
+}
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
 __device__ __forceinline__ float warp_max_abs(float x)
 {
     float d;
@@ -240,19 +249,19 @@ __device__ __forceinline__ float rcp_approx(float x)
     return y;
 }
 
-// The correctly rounded root of x = 0 or x >= 2^-126, without a branch: with y ~ 1 / sqrt(x) from the hardware's
-// approximation, s = x y is the root to about 2^-22, and s + (x - s^2) y / 2 is one Newton step whose residual the fused
-// multiply-add forms exactly (Markstein's square root, IBM J. Res. Dev. 34, 1990).  Compared with __fsqrt_rn on every
-// positive FP32 number from 2^-126 on: equal.  Infinity gives NaN here; its block reads as NaN either way.
-__device__ __forceinline__ float2 sqrt_pair(float2 x)
+// Minus the correctly rounded root of x = -nx, for x = 0 or x >= 2^-126, without a branch: with y ~ 1 / sqrt(x) from the
+// hardware's approximation, s = x y is the root to about 2^-22, and s + (x - s^2) y / 2 is one Newton step whose residual
+// the fused multiply-add forms exactly (Markstein's square root, IBM J. Res. Dev. 34, 1990).  Compared with __fsqrt_rn on
+// every positive FP32 number from 2^-126 on: equal.  Infinity gives NaN here; its block reads as NaN either way.  Everything
+// has its sign turned because a pair's sign costs two instructions, and the users of the root can turn a constant instead.
+__device__ __forceinline__ float2 minus_sqrt_pair(float2 nx)
 {
     float2 y;
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(x.x, 0x1p-126f)));
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(x.y, 0x1p-126f)));
-    const float2 s = mul2(x, y);
-    const float2 h = mul2(pair(0.5f), y);
-    const float2 d = fma2(make_float2(-s.x, -s.y), s, x);
-    return fma2(d, h, s);
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.x) : "f"(fmaxf(-nx.x, 0x1p-126f)));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y.y) : "f"(fmaxf(-nx.y, 0x1p-126f)));
+    const float2 s = mul2(nx, y);                 // -s
+    const float2 d = fma2(s, s, nx);              // s^2 - x
+    return fma2(d, mul2(pair(0.5f), y), s);
 }
 
 // FP32 state: moments in, moments out (the arithmetic of tsr_dense_adamw).
@@ -267,87 +276,102 @@ __device__ __forceinline__ void update_f32(float2 (&p)[4], const float2 (&g)[4],
     }
 }
 
-// 8-bit state: m and r = sqrt(v) in, as E4M3 values and their scales; new m and r in FP32 out.  Every rounding on the way
+// 8-bit state: m and r = sqrt(v) in, as E4M3 values and their scales; new m and -r in FP32 out.  Every rounding on the way
 // to the stored bits is one IEEE operation, so that they are well defined; the update itself takes the approximate
 // quotient.  (beta1 scale) code is exactly beta1 (scale code), scale being a power of two.
 __device__ __forceinline__ void update_q8(float2 (&p)[4], const float2 (&g)[4], float2 (&m)[4], float2 (&r)[4], float2 scale, const DenseStep &a, float lr,
                                           float decay)
 {
-    const float b1s = __fmul_rn(a.sc.beta1, scale.x);
+    const float b1s = __fmul_rn(a.sc.beta1, scale.x), rate = -__fmul_rn(lr, a.sc.inv_bc1);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         m[j] = add_flush(mul2(pair(b1s), m[j]), mul2(pair(a.sc.omb1), g[j]));
         r[j] = mul2(pair(scale.y), r[j]);
-        r[j] = sqrt_pair(add_flush(mul2(pair(a.sc.beta2), mul2(r[j], r[j])), mul2(pair(a.sc.omb2), mul2(g[j], g[j]))));
-        const float2 den = fma2(r[j], pair(a.sqrt_inv_bc2), pair(a.sc.eps));
-        const float2 d = mul2(mul2(m[j], pair(a.sc.inv_bc1)), make_float2(rcp_approx(den.x), rcp_approx(den.y)));
-        p[j] = fma2(pair(-lr), d, mul2(pair(decay), p[j]));
+        r[j] = minus_sqrt_pair(add_flush(mul2(pair(-a.sc.beta2), mul2(r[j], r[j])), mul2(pair(-a.sc.omb2), mul2(g[j], g[j]))));
+        const float2 den = fma2(r[j], pair(-a.sqrt_inv_bc2), pair(a.sc.eps));
+        p[j] = fma2(pair(rate), mul2(m[j], make_float2(rcp_approx(den.x), rcp_approx(den.y))), mul2(pair(decay), p[j]));
     }
 }
 
-// New scales of the warp's block, and the codes of x / scale for the lane's eight m and r; element(j) is the position of
-// element j of the lane in the tensor.
+// New scales of the warp's block, and the codes of m / scale and r / scale for the lane's eight (nr = -r); element(j) is the
+// position of element j of the lane in the tensor.
 //
 // To nearest, the conversion instruction does it.  Stochastic: 2^-120 x / scale has the E4M3 code of x / scale in its bits 20
 // to 26, FP32's exponent field running as E4M3's does and its denormal numbers being E4M3's (both have a spacing of one unit
 // below exponent 1), so 16 random bits are added below bit 20 and the rest is cut off: one multiply-add on the bits, which
-// also moves the code to the top byte.  Without this the integer pipe was the limit (81 % busy; 69 instructions an
-// element, now 53).
+// also moves the code to the top byte.
+//
+// A root above zero has code 1 at least.  That takes two instructions an element, and only a block that spans a factor of
+// 2^17 needs it: a warp without a root below 2^-9 scale skips them.
 template <bool SR, typename Elem>
-__device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&r)[4], UnitKeys k, Elem element, uint2 &cm, uint2 &cr)
+__device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&nr)[4], UnitKeys k, Elem element, uint2 &cm, uint2 &cr)
 {
     float2 scale, inv;
     block_scale(__float_as_uint(warp_max_abs(max_abs8(m))), scale.x, inv.x);
-    block_scale(__float_as_uint(warp_max_abs(max_abs8(r))), scale.y, inv.y);
+    block_scale(__float_as_uint(warp_max_abs(max_abs8(nr))), scale.y, inv.y);
+    // (NaN, which compares false, needs no floor either)
+    const bool floor = __any_sync(0xffffffffu, max8(nr) > -0x1p-9f * scale.y);
     if constexpr (SR) {
         uint32_t um[8], ur[8];
-        float2 ym[4], yr[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            ym[j] = mul2(mul2(m[j], pair(inv.x)), pair(0x1p-120f));
-            yr[j] = mul2(mul2(r[j], pair(inv.y)), pair(0x1p-120f));
+            const float2 ym = mul2(mul2(m[j], pair(inv.x)), pair(0x1p-120f));
+            const float2 yr = mul2(mul2(nr[j], pair(-inv.y)), pair(0x1p-120f));
+            um[2 * j] = __float_as_uint(ym.x);
+            um[2 * j + 1] = __float_as_uint(ym.y);
+            ur[2 * j] = __float_as_uint(yr.x);
+            ur[2 * j + 1] = __float_as_uint(yr.y);
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const uint32_t w = random_word((uint32_t)element(j), k.k1, k.k2);
-            // a root above zero (it is above 2^-75 then) has code 1 at least
-            const uint32_t some = min(__float_as_uint(at(r, j)), 1u << 24);
-            const uint32_t bm = __float_as_uint(at(ym, j)), br = __float_as_uint(at(yr, j));
-            um[j] = (bm * 16u + __byte_perm(w, 0, 0x4104)) | (bm & 0x80000000u);
-            ur[j] = max(br * 16u + __byte_perm(w, 0, 0x4324), some);
+            const uint32_t hi = __byte_perm(w, 0, 0x4324), lo = __byte_perm(w, 0, 0x4104) ^ hi;   // halves of the word, eight bits up
+            um[j] = (um[j] * 16u + lo) | (um[j] & 0x80000000u);
+            ur[j] = ur[j] * 16u + hi;
         }
-        cm.x = __byte_perm(__byte_perm(um[0], um[1], 0x0073), __byte_perm(um[2], um[3], 0x0073), 0x5410);
-        cm.y = __byte_perm(__byte_perm(um[4], um[5], 0x0073), __byte_perm(um[6], um[7], 0x0073), 0x5410);
-        cr.x = __byte_perm(__byte_perm(ur[0], ur[1], 0x0073), __byte_perm(ur[2], ur[3], 0x0073), 0x5410);
-        cr.y = __byte_perm(__byte_perm(ur[4], ur[5], 0x0073), __byte_perm(ur[6], ur[7], 0x0073), 0x5410);
+        if (floor) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (at(nr, j) < 0.f) ur[j] = max(ur[j], 1u << 24);
+        }
+        cm.x = top_bytes(um[0], um[1], um[2], um[3]);
+        cm.y = top_bytes(um[4], um[5], um[6], um[7]);
+        cr.x = top_bytes(ur[0], ur[1], ur[2], ur[3]);
+        cr.y = top_bytes(ur[4], ur[5], ur[6], ur[7]);
     } else {
+        float2 y[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            // 0 for r = 0, at least 2^-9 for any other r (those are above 2^-75)
-            const float2 some = mul2(r[j], pair(0x1p100f));
             m[j] = mul2(m[j], pair(inv.x));
-            r[j] = mul2(r[j], pair(inv.y));
-            r[j].x = fmaxf(r[j].x, fminf(some.x, 0x1p-9f));
-            r[j].y = fmaxf(r[j].y, fminf(some.y, 0x1p-9f));
+            y[j] = mul2(nr[j], pair(-inv.y));
+        }
+        if (floor) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (at(nr, j) < 0.f) at(y, j) = fmaxf(at(y, j), 0x1p-9f);
         }
         cm = e4m3_pack(m);
-        cr = e4m3_pack(r);
+        cr = e4m3_pack(y);
+        cr.x &= 0x7f7f7f7fu;   // a zero root may be -0
+        cr.y &= 0x7f7f7f7fu;
     }
     return scale;
 }
 
 // BF16 parameters, stochastic: 16 random bits are added below the seven mantissa bits and the rest is cut off; one random
-// word serves elements 2i and 2i + 1.  A lane that holds Inf or NaN rounds its eight to nearest.
+// word serves elements 2i and 2i + 1 (a pair starts at an even position).  A lane that holds Inf or NaN rounds its eight to
+// nearest.  Returns the BF16 values.
 template <typename Elem>
-__device__ __forceinline__ void round_params(float2 (&p)[4], UnitKeys k, Elem element)
+__device__ __forceinline__ uint4 round_params(const float2 (&p)[4], UnitKeys k, Elem element)
 {
-    if (!(max_abs8(p) < __uint_as_float(0x7f800000u))) return;
+    if (!(max_abs8(p) < __uint_as_float(0x7f800000u))) return bf16_pack(p);
+    uint32_t w[4];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {   // a pair starts at an even position
-        const uint32_t w = random_word((uint32_t)(element(2 * j) >> 1), k.k1 ^ 0x5bd1e995u, k.k2);
-        p[j].x = __uint_as_float((__float_as_uint(p[j].x) + (w & 0xffffu)) & 0xffff0000u);
-        p[j].y = __uint_as_float((__float_as_uint(p[j].y) + (w >> 16)) & 0xffff0000u);
+    for (int j = 0; j < 4; ++j) {
+        const uint32_t x = random_word((uint32_t)(element(2 * j) >> 1), k.k1 ^ 0x5bd1e995u, k.k2), hi = x >> 16;
+        w[j] = __byte_perm(__float_as_uint(p[j].x) + ((x ^ hi) & 0xffffu), __float_as_uint(p[j].y) + hi, 0x7632);
     }
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // The path for any alignment and any pitch, and for the last, partial unit of a tensor: a lane has the pairs of
@@ -475,7 +499,11 @@ __device__ __forceinline__ void step_any_unit(const DenseRec &t, int64_t base, i
     if constexpr (Q8) update_q8(p, g, m, v, scale, a, lr, decay);
     else update_f32(p, g, m, v, a, lr, decay);
     auto element = [&](int j) { return pair_at(base, lane, j >> 1) + (j & 1); };
-    if constexpr (SR && sizeof(PT) == 2) round_params(p, key, element);
+    if constexpr (SR && sizeof(PT) == 2) {
+        Eight<bf16> rounded;
+        rounded.r = round_params(p, key, element);
+        rounded.get(p);
+    }
     {
         Walk w(t, pair_at(base, lane, 0));
 #pragma unroll
@@ -532,18 +560,12 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
         if constexpr (Q8) scale = t.scale + base / UNIT;
         image = sizeof(PT) == 4 && t.image ? t.image + e : nullptr;
     }
-    __device__ __forceinline__ void load(RawUnit<PT, GT, Q8> &r, int64_t off) const   // off: elements ahead, whole units
+    __device__ __forceinline__ void load(RawUnit<PT, GT, Q8> &r) const
     {
-        r.p.load(p + off);
-        r.g.load(g + off);
-        if constexpr (Q8) {
-            r.cm = load8(m + off);
-            r.cr = load8(v + off);
-            r.scale = scale[off / UNIT];
-        } else {
-            r.m.load((const float *)m + off);
-            r.v.load((const float *)v + off);
-        }
+        r.p.load(p);
+        r.g.load(g);
+        r.m.load((const float *)m);
+        r.v.load((const float *)v);
     }
     __device__ __forceinline__ void advance(int64_t off)
     {
@@ -572,8 +594,8 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
             update_f32(xp, xg, xm, xv, a, lr, decay);
         }
         auto element = [&](int j) { return e + j; };
-        if constexpr (SR && sizeof(PT) == 2) round_params(xp, key, element);
-        Eight<PT>::put(p, xp);
+        if constexpr (SR && sizeof(PT) == 2) *(uint4 *)p = round_params(xp, key, element);
+        else Eight<PT>::put(p, xp);
         if (sizeof(PT) == 4 && image) Eight<bf16>::put(image, xp);
         if constexpr (Q8) {
             uint2 cm, cr;
@@ -588,8 +610,53 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
     }
 };
 
+// The 8-bit form reads so little per unit that a unit's loads in registers do not keep HBM busy.  So a lane's loads go to
+// slots of shared memory that only this lane reads (asynchronous copies of 16 and 8 bytes, no barrier between warps):
+// DEPTH slots, DEPTH - 1 of them on their way.
+template <typename PT, typename GT> struct Ring {
+    static constexpr int P_VECS = sizeof(PT) / 2, G_VECS = sizeof(GT) / 2;   // 16-byte vectors of a lane
+    static constexpr int THREADS = WARPS * 32;
+    static constexpr int SLOT = THREADS * (16 * (P_VECS + G_VECS) + 16) + WARPS * 8;
+    static constexpr int DEPTH = P_VECS + G_VECS == 2 ? 4 : P_VECS + G_VECS == 3 ? 3 : 2;
+    static constexpr int BYTES = DEPTH * SLOT;
+
+    static __device__ __forceinline__ void copy16(uint32_t to, const void *from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+    static __device__ __forceinline__ void copy8(uint32_t to, const void *from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
+    static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 2) : "memory"); }
+
+    // Fills slot `to` (a shared-memory address) with the unit that is `units` units of this warp after u.
+    static __device__ __forceinline__ void issue(uint32_t to, const VectorUnit<PT, GT, true> &u, int units, int lane)
+    {
+        const int off = units * WARPS * UNIT;
+        const uint32_t t16 = to + threadIdx.x * 16, t8 = to + THREADS * 16 * (P_VECS + G_VECS) + threadIdx.x * 8;
+#pragma unroll
+        for (int k = 0; k < P_VECS; ++k) copy16(t16 + k * THREADS * 16, (const char *)(u.p + off) + 16 * k);
+#pragma unroll
+        for (int k = 0; k < G_VECS; ++k) copy16(t16 + (P_VECS + k) * THREADS * 16, (const char *)(u.g + off) + 16 * k);
+        copy8(t8, u.m + off);
+        copy8(t8 + THREADS * 8, u.v + off);
+        if (lane == 0) copy8(to + THREADS * (16 * (P_VECS + G_VECS) + 16) + (threadIdx.x >> 5) * 8, u.scale + off / UNIT);
+    }
+    static __device__ __forceinline__ void fetch(const char *slot, RawUnit<PT, GT, true> &r)
+    {
+        const char *s16 = slot + threadIdx.x * 16, *s8 = slot + THREADS * 16 * (P_VECS + G_VECS) + threadIdx.x * 8;
+        get(s16, r.p);
+        get(s16 + P_VECS * THREADS * 16, r.g);
+        r.cm = *(const uint2 *)s8;
+        r.cr = *(const uint2 *)(s8 + THREADS * 8);
+        r.scale = *(const float2 *)(slot + THREADS * (16 * (P_VECS + G_VECS) + 16) + (threadIdx.x >> 5) * 8);
+    }
+    static __device__ __forceinline__ void get(const char *s, Eight<bf16> &x) { x.r = *(const uint4 *)s; }
+    static __device__ __forceinline__ void get(const char *s, Eight<float> &x)
+    {
+        const uint4 a = *(const uint4 *)s, b = *(const uint4 *)(s + THREADS * 16);
+        x.r = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    }
+};
+
 template <typename PT, typename GT, bool Q8, bool SR>
-__global__ void __launch_bounds__(WARPS * 32, Q8 ? 3 : 4)
+__global__ void __launch_bounds__(WARPS * 32, 4)
 dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restrict__ chunks, const DenseStep a)
 {
     pdl_trigger();
@@ -618,13 +685,24 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
         uint32_t e = (uint32_t)base + lane * 8;
         RawUnit<PT, GT, Q8> raw;
         if constexpr (Q8) {
-            // the next unit's loads are on their way while this one is worked on
-            RawUnit<PT, GT, Q8> next;
-            u.load(next, 0);
+            typedef Ring<PT, GT> R;
+            extern __shared__ __align__(16) char slots[];
+            const uint32_t first = (uint32_t)__cvta_generic_to_shared(slots);
+            int in = (R::DEPTH - 1) * R::SLOT, out = 0;   // byte offsets of the slots to fill and to read
+#pragma unroll
+            for (int k = 0; k < R::DEPTH - 1; ++k) {
+                if (k < todo) R::issue(first + k * R::SLOT, u, k, lane);
+                R::commit();
+            }
 #pragma unroll 1
             for (; todo > 0; --todo) {
-                raw = next;
-                if (todo > 1) u.load(next, STRIDE);
+                R::wait();
+                __syncwarp();   // lane 0's copy of the scale; and every lane has read the slot that is filled next
+                R::fetch(slots + out, raw);
+                if (todo >= R::DEPTH) R::issue(first + in, u, R::DEPTH - 1, lane);
+                R::commit();
+                in = in + R::SLOT == R::BYTES ? 0 : in + R::SLOT;
+                out = out + R::SLOT == R::BYTES ? 0 : out + R::SLOT;
                 u.template step<SR>(raw, e, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
                 e += STRIDE;
@@ -632,7 +710,7 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
         } else {
 #pragma unroll 1
             for (; todo > 0; --todo) {
-                u.load(raw, 0);
+                u.load(raw);
                 u.template step<SR>(raw, e, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
                 e += STRIDE;
@@ -799,7 +877,7 @@ __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s,
             }
         } else if constexpr (DQ && !SQ) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) at(v, j) = __fsqrt_rn(at(v, j));
+            for (int j = 0; j < 8; ++j) at(v, j) = -__fsqrt_rn(at(v, j));
             scale = quantise<false>(m, v, UnitKeys{0, 0}, [](int j) { return j; }, cm, cr);
         } else if constexpr (DQ) {   // codes of their own values
             cm = e4m3_pack(m);
@@ -897,20 +975,35 @@ int key_of(const tsr_dense_desc &d)
     return (d.p_dtype == TSR_BF16 ? KEY_P_BF16 : 0) | (d.g_dtype == TSR_BF16 ? KEY_G_BF16 : 0) | (d.state == TSR_STATE_Q8 ? KEY_Q8 : 0);
 }
 
-template <bool SR>
-cudaError_t step_launch(int key, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
+template <typename PT, typename GT, bool Q8> constexpr int step_smem() { return Q8 ? Ring<PT, GT>::BYTES : 0; }
+
+template <typename PT, typename GT, bool Q8>
+cudaError_t step_launch_as(bool sr, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
 {
-    const dim3 grid(count), block(WARPS * 32);
+    constexpr int smem = step_smem<PT, GT, Q8>();
+    return sr ? launch_dependent(dense_step_kernel<PT, GT, Q8, true>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a)
+              : launch_dependent(dense_step_kernel<PT, GT, Q8, false>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a);
+}
+
+cudaError_t step_launch(int key, bool sr, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
+{
     switch (key) {
-    case 0: return launch_dependent(dense_step_kernel<float, float, false, SR>, grid, block, 0, s, 1, recs, chunks, a);
-    case KEY_P_BF16: return launch_dependent(dense_step_kernel<bf16, float, false, SR>, grid, block, 0, s, 1, recs, chunks, a);
-    case KEY_G_BF16: return launch_dependent(dense_step_kernel<float, bf16, false, SR>, grid, block, 0, s, 1, recs, chunks, a);
-    case KEY_P_BF16 | KEY_G_BF16: return launch_dependent(dense_step_kernel<bf16, bf16, false, SR>, grid, block, 0, s, 1, recs, chunks, a);
-    case KEY_Q8: return launch_dependent(dense_step_kernel<float, float, true, SR>, grid, block, 0, s, 1, recs, chunks, a);
-    case KEY_Q8 | KEY_P_BF16: return launch_dependent(dense_step_kernel<bf16, float, true, SR>, grid, block, 0, s, 1, recs, chunks, a);
-    case KEY_Q8 | KEY_G_BF16: return launch_dependent(dense_step_kernel<float, bf16, true, SR>, grid, block, 0, s, 1, recs, chunks, a);
-    default: return launch_dependent(dense_step_kernel<bf16, bf16, true, SR>, grid, block, 0, s, 1, recs, chunks, a);
+    case 0: return step_launch_as<float, float, false>(sr, recs, chunks, count, a, s);
+    case KEY_P_BF16: return step_launch_as<bf16, float, false>(sr, recs, chunks, count, a, s);
+    case KEY_G_BF16: return step_launch_as<float, bf16, false>(sr, recs, chunks, count, a, s);
+    case KEY_P_BF16 | KEY_G_BF16: return step_launch_as<bf16, bf16, false>(sr, recs, chunks, count, a, s);
+    case KEY_Q8: return step_launch_as<float, float, true>(sr, recs, chunks, count, a, s);
+    case KEY_Q8 | KEY_P_BF16: return step_launch_as<bf16, float, true>(sr, recs, chunks, count, a, s);
+    case KEY_Q8 | KEY_G_BF16: return step_launch_as<float, bf16, true>(sr, recs, chunks, count, a, s);
+    default: return step_launch_as<bf16, bf16, true>(sr, recs, chunks, count, a, s);
     }
+}
+
+template <typename PT, typename GT> cudaError_t step_configure()   // shared memory of the 8-bit kernels
+{
+    cudaError_t e = cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
 }
 
 tsr_status dense_ready(const tsr_dense_plan *plan)
@@ -998,6 +1091,10 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return dense_fail(plan, TSR_ERR_CUDA, "no CUDA device available");
     DENSE_CUDA(plan, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
+    DENSE_CUDA(plan, (step_configure<float, float>()));
+    DENSE_CUDA(plan, (step_configure<bf16, float>()));
+    DENSE_CUDA(plan, (step_configure<float, bf16>()));
+    DENSE_CUDA(plan, (step_configure<bf16, bf16>()));
     plan->bound = false;
     DENSE_CUDA(plan, cudaDeviceSynchronize());   // nothing that still runs may see the tables change
     char *at = (char *)workspace;
@@ -1144,8 +1241,7 @@ tsr_status tsr_dense_plan_step(tsr_dense_plan *plan, const tsr_hyper *h, const f
     for (const tsr_dense_plan::Group &g : plan->groups) {
         const DenseChunk *chunks = plan->d_chunks + g.first;
         const bool sr = rounding == TSR_ROUND_STOCHASTIC && (g.key & (KEY_Q8 | KEY_P_BF16));   // else nothing is rounded
-        DENSE_CUDA(plan, sr ? step_launch<true>(g.key, plan->d_recs, chunks, g.count, a, (cudaStream_t)stream)
-                            : step_launch<false>(g.key, plan->d_recs, chunks, g.count, a, (cudaStream_t)stream));
+        DENSE_CUDA(plan, step_launch(g.key, sr, plan->d_recs, chunks, g.count, a, (cudaStream_t)stream));
     }
     return TSR_OK;
 }
