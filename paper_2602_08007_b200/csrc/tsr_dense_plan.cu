@@ -51,9 +51,13 @@ struct alignas(16) DenseRec {   // one tensor on the device
     int32_t index;              // position in the plan
 };
 
-// Units [first, first + units) of tensor rec.  vector: every one of them is whole, and everything that a step touches is
-// contiguous and aligned to vectors of eight elements.
-struct alignas(16) DenseChunk { int32_t rec; uint32_t first; int32_t units; int32_t vector; };
+// How a step goes over a chunk.  VECTORS: everything that it touches is contiguous and aligned to vectors of eight
+// elements.  PLAIN: contiguous, any alignment.  ROWS: rows of 256 elements or more, so that a unit meets the end of a row
+// once at most.  All three hold whole units only.  ANY: the rest, the last units of tensors and narrow matrices.
+enum DensePath : int32_t { PATH_ANY = 0, PATH_VECTORS = 1, PATH_PLAIN = 2, PATH_ROWS = 3 };
+
+// Units [first, first + units) of tensor rec.
+struct alignas(16) DenseChunk { int32_t rec; uint32_t first; int32_t units; int32_t path; };
 
 struct DenseStep {
     StepScalars sc;
@@ -374,9 +378,9 @@ __device__ __forceinline__ uint4 round_params(const float2 (&p)[4], UnitKeys k, 
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The path for any alignment and any pitch, and for the last, partial unit of a tensor: a lane has the pairs of
-// neighbours at base + 2 lane + 64 j, so that the warp's accesses stay together.  Walk says where a pair lies in a matrix
-// with row pitch: row and column of the first by one division, the others by steps of 64.
+// Where nothing is known of the alignment, a lane has the pairs of neighbours at base + 2 lane + 64 j, so that the warp's
+// accesses stay together.  Walk says where a pair lies in a matrix with row pitch: row and column of the first by one
+// division, the others by steps of 64.
 struct Walk {
     int64_t row, col;
     const DenseRec &t;
@@ -410,8 +414,8 @@ struct Walk {
 };
 __device__ __forceinline__ int64_t pair_at(int64_t base, int lane, int j) { return base + 2 * lane + 64 * j; }
 
-// Pairs of moments of that path; elements from n on are zero, and not written.
-template <bool Q8>
+// Pairs of moments; elements from n on are zero, and not written (WHOLE: there are none).
+template <bool Q8, bool WHOLE>
 __device__ __forceinline__ void load_pairs(const void *src, bool both, int64_t base, int lane, int64_t n, float2 (&x)[4])
 {
 #pragma unroll
@@ -421,22 +425,23 @@ __device__ __forceinline__ void load_pairs(const void *src, bool both, int64_t b
         if constexpr (Q8) {
             const uint8_t *c = (const uint8_t *)src + e;
             uint32_t w = 0;
-            if (both && e + 1 < n) w = *(const uint16_t *)c;
+            if (both && (WHOLE || e + 1 < n)) w = *(const uint16_t *)c;
             else {
-                if (e < n) w = c[0];
-                if (e + 1 < n) w |= (uint32_t)c[1] << 8;
+                if (WHOLE || e < n) w = c[0];
+                if (WHOLE || e + 1 < n) w |= (uint32_t)c[1] << 8;
             }
             x[j] = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)w, __NV_E4M3)));
         } else {
             const float *f = (const float *)src + e;
-            if (both && e + 1 < n) x[j] = *(const float2 *)f;
+            if (both && (WHOLE || e + 1 < n)) x[j] = *(const float2 *)f;
             else {
-                if (e < n) x[j].x = f[0];
-                if (e + 1 < n) x[j].y = f[1];
+                if (WHOLE || e < n) x[j].x = f[0];
+                if (WHOLE || e + 1 < n) x[j].y = f[1];
             }
         }
     }
 }
+template <bool WHOLE>
 __device__ __forceinline__ void store_code_pairs(void *dst, bool both, int64_t base, int lane, int64_t n, uint2 codes)
 {
     const uint32_t w[2] = {codes.x, codes.y};
@@ -445,55 +450,88 @@ __device__ __forceinline__ void store_code_pairs(void *dst, bool both, int64_t b
         const int64_t e = pair_at(base, lane, j);
         uint8_t *c = (uint8_t *)dst + e;
         const uint32_t two = w[j >> 1] >> (16 * (j & 1));
-        if (both && e + 1 < n) *(uint16_t *)c = (uint16_t)two;
+        if (both && (WHOLE || e + 1 < n)) *(uint16_t *)c = (uint16_t)two;
         else {
-            if (e < n) c[0] = (uint8_t)two;
-            if (e + 1 < n) c[1] = (uint8_t)(two >> 8);
+            if (WHOLE || e < n) c[0] = (uint8_t)two;
+            if (WHOLE || e + 1 < n) c[1] = (uint8_t)(two >> 8);
         }
     }
 }
+template <bool WHOLE>
 __device__ __forceinline__ void store_pairs(void *dst, bool both, int64_t base, int lane, int64_t n, const float2 (&x)[4])
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const int64_t e = pair_at(base, lane, j);
         float *f = (float *)dst + e;
-        if (both && e + 1 < n) *(float2 *)f = x[j];
+        if (both && (WHOLE || e + 1 < n)) *(float2 *)f = x[j];
         else {
-            if (e < n) f[0] = x[j].x;
-            if (e + 1 < n) f[1] = x[j].y;
+            if (WHOLE || e < n) f[0] = x[j].x;
+            if (WHOLE || e + 1 < n) f[1] = x[j].y;
         }
     }
 }
 
-template <typename PT, typename GT, bool Q8, bool SR>
-__device__ __forceinline__ void step_any_unit(const DenseRec &t, int64_t base, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key)
+// Pairs of a parameter, gradient or image (pitch ld).  row, col: where the unit starts (PLAIN, ROWS).
+template <int PATH, typename T>
+__device__ __forceinline__ void load_matrix(const T *x, const DenseRec &t, int64_t ld, int64_t base, int64_t row, int64_t col, int lane, float2 (&out)[4])
 {
-    PT *P = (PT *)t.p;
-    const GT *G = (const GT *)t.g;
-    const bool both = t.flags & REC_PAIR_STATE;
-    float2 p[4], g[4], m[4], v[4];
-    float2 scale = make_float2(0.f, 0.f);
-    if constexpr (Q8) scale = t.scale[base / UNIT];
-    load_pairs<Q8>(t.m, both, base, lane, t.n, m);
-    load_pairs<Q8>(t.v, both, base, lane, t.n, v);
-    {
+    if constexpr (PATH == PATH_ANY) {
         Walk w(t, pair_at(base, lane, 0));
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int64_t e = pair_at(base, lane, j);
-            p[j] = g[j] = pair(0.f);
-            if (e < t.n) {
-                p[j].x = to_f32(P[w.one(t.ldp)]);
-                g[j].x = to_f32(G[w.one(t.ldg)]);
-            }
-            if (e + 1 < t.n) {
-                p[j].y = to_f32(P[w.two(t.ldp)]);
-                g[j].y = to_f32(G[w.two(t.ldg)]);
-            }
+            out[j] = pair(0.f);
+            if (e < t.n) out[j].x = to_f32(x[w.one(ld)]);
+            if (e + 1 < t.n) out[j].y = to_f32(x[w.two(ld)]);
             w.next();
         }
+    } else {
+        const T *u = PATH == PATH_PLAIN ? x + base : x + row * ld + col;
+        const int left = (int)min(t.cols - col, (int64_t)UNIT), gap = (int)(ld - t.cols);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = 2 * lane + 64 * (j >> 1) + (j & 1);
+            at(out, j) = to_f32(u[PATH == PATH_PLAIN || i < left ? i : i + gap]);
+        }
     }
+}
+template <int PATH, typename T>
+__device__ __forceinline__ void store_matrix(T *x, const DenseRec &t, int64_t ld, int64_t base, int64_t row, int64_t col, int lane, const float2 (&in)[4])
+{
+    if constexpr (PATH == PATH_ANY) {
+        Walk w(t, pair_at(base, lane, 0));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int64_t e = pair_at(base, lane, j);
+            if (e < t.n) from_f32(x[w.one(ld)], in[j].x);
+            if (e + 1 < t.n) from_f32(x[w.two(ld)], in[j].y);
+            w.next();
+        }
+    } else {
+        T *u = PATH == PATH_PLAIN ? x + base : x + row * ld + col;
+        const int left = (int)min(t.cols - col, (int64_t)UNIT), gap = (int)(ld - t.cols);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = 2 * lane + 64 * (j >> 1) + (j & 1);
+            from_f32(u[PATH == PATH_PLAIN || i < left ? i : i + gap], (j & 1) ? in[j >> 1].y : in[j >> 1].x);
+        }
+    }
+}
+
+template <int PATH, typename PT, typename GT, bool Q8, bool SR>
+__device__ __forceinline__ void step_pairs_unit(const DenseRec &t, int64_t base, int64_t row, int64_t col, int lane, float gs, const DenseStep &a, float lr,
+                                                float decay, UnitKeys key)
+{
+    constexpr bool WHOLE = PATH != PATH_ANY;
+    const bool both = t.flags & REC_PAIR_STATE;
+    float2 p[4], g[4], m[4], v[4];
+    float2 scale = make_float2(0.f, 0.f);
+    if constexpr (Q8) scale = t.scale[base / UNIT];
+    load_pairs<Q8, WHOLE>(t.m, both, base, lane, t.n, m);
+    load_pairs<Q8, WHOLE>(t.v, both, base, lane, t.n, v);
+    load_matrix<PATH>((const PT *)t.p, t, t.ldp, base, row, col, lane, p);
+    load_matrix<PATH>((const GT *)t.g, t, t.ldg, base, row, col, lane, g);
 #pragma unroll
     for (int j = 0; j < 4; ++j) g[j] = mul2(g[j], pair(gs));
     if constexpr (Q8) update_q8(p, g, m, v, scale, a, lr, decay);
@@ -504,32 +542,38 @@ __device__ __forceinline__ void step_any_unit(const DenseRec &t, int64_t base, i
         rounded.r = round_params(p, key, element);
         rounded.get(p);
     }
-    {
-        Walk w(t, pair_at(base, lane, 0));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int64_t e = pair_at(base, lane, j);
-            if (e < t.n) from_f32(P[w.one(t.ldp)], p[j].x);
-            if (e + 1 < t.n) from_f32(P[w.two(t.ldp)], p[j].y);
-            if (sizeof(PT) == 4 && t.image) {
-                if (e < t.n) from_f32(t.image[w.one(t.ldi)], p[j].x);
-                if (e + 1 < t.n) from_f32(t.image[w.two(t.ldi)], p[j].y);
-            }
-            w.next();
-        }
-    }
+    store_matrix<PATH>((PT *)t.p, t, t.ldp, base, row, col, lane, p);
+    if (sizeof(PT) == 4 && t.image) store_matrix<PATH>(t.image, t, t.ldi, base, row, col, lane, p);
     if constexpr (Q8) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (element(j) >= t.n) at(m, j) = at(v, j) = 0.f;   // (0 * NaN of a poisoned block)
+            if (!WHOLE && element(j) >= t.n) at(m, j) = at(v, j) = 0.f;   // (0 * NaN of a poisoned block)
         uint2 cm, cr;
         const float2 s = quantise<SR>(m, v, key, element, cm, cr);
         if (lane == 0) t.scale[base / UNIT] = s;
-        store_code_pairs(t.m, both, base, lane, t.n, cm);
-        store_code_pairs(t.v, both, base, lane, t.n, cr);
+        store_code_pairs<WHOLE>(t.m, both, base, lane, t.n, cm);
+        store_code_pairs<WHOLE>(t.v, both, base, lane, t.n, cr);
     } else {
-        store_pairs(t.m, both, base, lane, t.n, m);
-        store_pairs(t.v, both, base, lane, t.n, v);
+        store_pairs<WHOLE>(t.m, both, base, lane, t.n, m);
+        store_pairs<WHOLE>(t.v, both, base, lane, t.n, v);
+    }
+}
+
+// The units of a warp on the paths without vectors.
+template <int PATH, typename PT, typename GT, bool Q8, bool SR>
+__device__ __forceinline__ void step_pairs(const DenseRec &t, int64_t base, int todo, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key)
+{
+    constexpr int64_t STRIDE = WARPS * UNIT;
+    int64_t row = 0, col = 0;
+    if constexpr (PATH == PATH_ROWS) {
+        row = base / t.cols;
+        col = base - row * t.cols;
+    }
+#pragma unroll 1
+    for (; todo > 0; --todo, base += STRIDE) {
+        step_pairs_unit<PATH, PT, GT, Q8, SR>(t, base, row, col, lane, gs, a, lr, decay, key);
+        if constexpr (PATH == PATH_ROWS)
+            for (col += STRIDE; col >= t.cols; col -= t.cols) ++row;
     }
 }
 
@@ -560,12 +604,18 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
         if constexpr (Q8) scale = t.scale + base / UNIT;
         image = sizeof(PT) == 4 && t.image ? t.image + e : nullptr;
     }
-    __device__ __forceinline__ void load(RawUnit<PT, GT, Q8> &r) const
+    __device__ __forceinline__ void load(RawUnit<PT, GT, Q8> &r, int off) const   // off: elements ahead, whole units
     {
-        r.p.load(p);
-        r.g.load(g);
-        r.m.load((const float *)m);
-        r.v.load((const float *)v);
+        r.p.load(p + off);
+        r.g.load(g + off);
+        if constexpr (Q8) {
+            r.cm = load8(m + off);
+            r.cr = load8(v + off);
+            r.scale = scale[off / UNIT];
+        } else {
+            r.m.load((const float *)m + off);
+            r.v.load((const float *)v + off);
+        }
     }
     __device__ __forceinline__ void advance(int64_t off)
     {
@@ -655,8 +705,10 @@ template <typename PT, typename GT> struct Ring {
     }
 };
 
-template <typename PT, typename GT, bool Q8, bool SR>
-__global__ void __launch_bounds__(WARPS * 32, 4)
+// MIXED: there are chunks of every path.  Where all chunks are vectors, a kernel without the other paths is launched: their
+// registers cost the FP32 form 1.5 % (1B set: 4.88 against 4.81 ms).
+template <typename PT, typename GT, bool Q8, bool SR, bool MIXED>
+__global__ void __launch_bounds__(WARPS * 32, Q8 ? 3 : 4)
 dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restrict__ chunks, const DenseStep a)
 {
     pdl_trigger();
@@ -677,14 +729,15 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
         if (!isfinite(gs)) return;
     }
     constexpr int64_t STRIDE = WARPS * UNIT;
+    constexpr bool RING = Q8 && !SR;
     int64_t base = ((int64_t)ch.first + warp) * UNIT;
     int todo = (ch.units - warp + WARPS - 1) / WARPS;   // units of this warp
-    if (ch.vector) {
-        if (todo <= 0) return;
+    if (todo <= 0) return;
+    if (!MIXED || ch.path == PATH_VECTORS) {
         VectorUnit<PT, GT, Q8> u(t, base, lane);
         uint32_t e = (uint32_t)base + lane * 8;
         RawUnit<PT, GT, Q8> raw;
-        if constexpr (Q8) {
+        if constexpr (RING) {
             typedef Ring<PT, GT> R;
             extern __shared__ __align__(16) char slots[];
             const uint32_t first = (uint32_t)__cvta_generic_to_shared(slots);
@@ -707,18 +760,32 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
                 u.advance(STRIDE);
                 e += STRIDE;
             }
+        } else if constexpr (Q8) {
+            RawUnit<PT, GT, Q8> next;   // on its way while this unit is worked on
+            u.load(next, 0);
+#pragma unroll 1
+            for (; todo > 0; --todo) {
+                raw = next;
+                if (todo > 1) u.load(next, STRIDE);
+                u.template step<SR>(raw, e, lane, gs, a, lr, decay, key);
+                u.advance(STRIDE);
+                e += STRIDE;
+            }
         } else {
 #pragma unroll 1
             for (; todo > 0; --todo) {
-                u.load(raw);
+                u.load(raw, 0);
                 u.template step<SR>(raw, e, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
                 e += STRIDE;
             }
         }
+    } else if (ch.path == PATH_PLAIN) {
+        step_pairs<PATH_PLAIN, PT, GT, Q8, SR>(t, base, todo, lane, gs, a, lr, decay, key);
+    } else if (ch.path == PATH_ROWS) {
+        step_pairs<PATH_ROWS, PT, GT, Q8, SR>(t, base, todo, lane, gs, a, lr, decay, key);
     } else {
-#pragma unroll 1
-        for (; todo > 0; --todo, base += STRIDE) step_any_unit<PT, GT, Q8, SR>(t, base, lane, gs, a, lr, decay, key);
+        step_pairs<PATH_ANY, PT, GT, Q8, SR>(t, base, todo, lane, gs, a, lr, decay, key);
     }
 }
 
@@ -752,22 +819,6 @@ __device__ __forceinline__ double cta_sum(double x, double *sh)   // valid in th
     return x;
 }
 
-// Gradient elements of a unit, any alignment and pitch.
-template <typename GT>
-__device__ __forceinline__ void load_any_grad(const DenseRec &t, int64_t base, int lane, float2 (&g)[4])
-{
-    const GT *G = (const GT *)t.g;
-    Walk w(t, pair_at(base, lane, 0));
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t e = pair_at(base, lane, j);
-        g[j] = pair(0.f);
-        if (e < t.n) g[j].x = to_f32(G[w.one(t.ldg)]);
-        if (e + 1 < t.n) g[j].y = to_f32(G[w.two(t.ldg)]);
-        w.next();
-    }
-}
-
 // A warp's sum over its units of a chunk, 64 bytes of every lane at a time.
 template <typename GT>
 __device__ __forceinline__ double chunk_squares(const DenseRec &t, const DenseChunk &ch, int warp, int lane)
@@ -799,7 +850,7 @@ __device__ __forceinline__ double chunk_squares(const DenseRec &t, const DenseCh
     }
     for (; todo > 0; --todo, base += STRIDE) {
         float2 g[4];
-        load_any_grad<GT>(t, base, lane, g);
+        load_matrix<PATH_ANY>((const GT *)t.g, t, t.ldg, base, 0, 0, lane, g);
         sum += square_sum(g);
     }
     return sum;
@@ -854,8 +905,8 @@ __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s,
         uint2 cm, cr;
         if constexpr (SQ) scale = s.scale[base / UNIT];
         if (!vec) {
-            load_pairs<SQ>(s.m, s.flags & REC_PAIR_STATE, base, lane, d.n, m);
-            load_pairs<SQ>(s.v, s.flags & REC_PAIR_STATE, base, lane, d.n, v);
+            load_pairs<SQ, false>(s.m, s.flags & REC_PAIR_STATE, base, lane, d.n, m);
+            load_pairs<SQ, false>(s.v, s.flags & REC_PAIR_STATE, base, lane, d.n, v);
         } else if constexpr (SQ) {
             cm = load8((const uint8_t *)s.m + e);
             cr = load8((const uint8_t *)s.v + e);
@@ -888,12 +939,12 @@ __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s,
                 *(uint2 *)((uint8_t *)d.m + e) = cm;
                 *(uint2 *)((uint8_t *)d.v + e) = cr;
             } else {
-                store_code_pairs(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, cm);
-                store_code_pairs(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, cr);
+                store_code_pairs<false>(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, cm);
+                store_code_pairs<false>(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, cr);
             }
         } else if (!vec) {
-            store_pairs(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, m);
-            store_pairs(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, v);
+            store_pairs<false>(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, m);
+            store_pairs<false>(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, v);
         } else {
             Eight<float>::put((float *)d.m + e, m);
             Eight<float>::put((float *)d.v + e, v);
@@ -932,7 +983,7 @@ struct tsr_dense_plan {
     int step_units[2] = {}, norm_units = 0, copy_units = 0;
     size_t most_chunks = 0;                 // room for so many in the table
     // One table: the chunks of the stepped tensors group by group, then those of the norm, then those of copies.
-    struct Group { int key, first, count; };
+    struct Group { int key, first, count; bool mixed; };
     std::vector<Group> groups;              // tensors that share types: one launch each
     int norm_first = 0, copy_first = 0, chunk_count = 0;
     size_t workspace_bytes = 0;
@@ -975,35 +1026,39 @@ int key_of(const tsr_dense_desc &d)
     return (d.p_dtype == TSR_BF16 ? KEY_P_BF16 : 0) | (d.g_dtype == TSR_BF16 ? KEY_G_BF16 : 0) | (d.state == TSR_STATE_Q8 ? KEY_Q8 : 0);
 }
 
-template <typename PT, typename GT, bool Q8> constexpr int step_smem() { return Q8 ? Ring<PT, GT>::BYTES : 0; }
-
-template <typename PT, typename GT, bool Q8>
-cudaError_t step_launch_as(bool sr, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
+template <typename PT, typename GT, bool Q8, bool SR>
+cudaError_t step_launch_as(bool mixed, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
 {
-    constexpr int smem = step_smem<PT, GT, Q8>();
-    return sr ? launch_dependent(dense_step_kernel<PT, GT, Q8, true>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a)
-              : launch_dependent(dense_step_kernel<PT, GT, Q8, false>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a);
+    const int smem = Q8 && !SR ? Ring<PT, GT>::BYTES : 0;
+    return mixed ? launch_dependent(dense_step_kernel<PT, GT, Q8, SR, true>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a)
+                 : launch_dependent(dense_step_kernel<PT, GT, Q8, SR, false>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a);
 }
 
-cudaError_t step_launch(int key, bool sr, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
+template <typename PT, typename GT>
+cudaError_t step_launch_as(bool q8, bool sr, bool mixed, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
 {
-    switch (key) {
-    case 0: return step_launch_as<float, float, false>(sr, recs, chunks, count, a, s);
-    case KEY_P_BF16: return step_launch_as<bf16, float, false>(sr, recs, chunks, count, a, s);
-    case KEY_G_BF16: return step_launch_as<float, bf16, false>(sr, recs, chunks, count, a, s);
-    case KEY_P_BF16 | KEY_G_BF16: return step_launch_as<bf16, bf16, false>(sr, recs, chunks, count, a, s);
-    case KEY_Q8: return step_launch_as<float, float, true>(sr, recs, chunks, count, a, s);
-    case KEY_Q8 | KEY_P_BF16: return step_launch_as<bf16, float, true>(sr, recs, chunks, count, a, s);
-    case KEY_Q8 | KEY_G_BF16: return step_launch_as<float, bf16, true>(sr, recs, chunks, count, a, s);
-    default: return step_launch_as<bf16, bf16, true>(sr, recs, chunks, count, a, s);
+    if (q8) return sr ? step_launch_as<PT, GT, true, true>(mixed, recs, chunks, count, a, s) : step_launch_as<PT, GT, true, false>(mixed, recs, chunks, count, a, s);
+    if constexpr (sizeof(PT) == 2)   // (FP32 parameters with FP32 states: nothing is rounded)
+        if (sr) return step_launch_as<PT, GT, false, true>(mixed, recs, chunks, count, a, s);
+    return step_launch_as<PT, GT, false, false>(mixed, recs, chunks, count, a, s);
+}
+
+cudaError_t step_launch(int key, bool sr, bool mixed, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
+{
+    const bool q8 = key & KEY_Q8;
+    switch (key & (KEY_P_BF16 | KEY_G_BF16)) {
+    case 0: return step_launch_as<float, float>(q8, sr, mixed, recs, chunks, count, a, s);
+    case KEY_P_BF16: return step_launch_as<bf16, float>(q8, sr, mixed, recs, chunks, count, a, s);
+    case KEY_G_BF16: return step_launch_as<float, bf16>(q8, sr, mixed, recs, chunks, count, a, s);
+    default: return step_launch_as<bf16, bf16>(q8, sr, mixed, recs, chunks, count, a, s);
     }
 }
 
-template <typename PT, typename GT> cudaError_t step_configure()   // shared memory of the 8-bit kernels
+template <typename PT, typename GT> cudaError_t step_configure()   // shared memory of the kernels with a ring
 {
-    cudaError_t e = cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
+    cudaError_t e = cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
+    return cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
 }
 
 tsr_status dense_ready(const tsr_dense_plan *plan)
@@ -1021,7 +1076,7 @@ int64_t size_of(int32_t dtype) { return dtype == TSR_BF16 ? 2 : 4; }
 tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *workspace)
 {
     std::vector<DenseRec> recs(plan->descs.size());
-    std::vector<char> vector(recs.size(), 0);
+    std::vector<DensePath> path(recs.size(), PATH_ANY);
     for (size_t i = 0; i < recs.size(); ++i) {
         const tsr_dense_desc &d = plan->descs[i];
         const tsr_dense_ptrs &p = ptrs[i];
@@ -1062,32 +1117,37 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
             r.p = p.param;
             r.image = (bf16 *)p.image;
             dense = dense && (d.rows <= 1 || (d.ldp == d.cols && (!p.image || d.ldi == d.cols)));
-            vector[i] = dense && (r.flags & REC_VEC_GRAD) && (r.flags & REC_VEC_STATE) && aligned(p.param, 8 * ps) && aligned(p.image, 16);
+            const int64_t far = std::max(std::max(d.ldp, d.ldg), p.image ? d.ldi : 0) - d.cols;
+            if (dense)
+                path[i] = (r.flags & REC_VEC_GRAD) && (r.flags & REC_VEC_STATE) && aligned(p.param, 8 * ps) && aligned(p.image, 16) ? PATH_VECTORS : PATH_PLAIN;
+            else if (d.cols >= UNIT && far < (1 << 30))
+                path[i] = PATH_ROWS;
         }
         if (!dense) r.flags |= REC_PITCHED;
     }
     std::vector<DenseChunk> chunks;
     std::vector<tsr_dense_plan::Group> groups;
     chunks.reserve(plan->most_chunks);
-    auto add = [&](size_t i, bool vec, int at_once) {   // on the vector path, the partial last unit is a chunk of its own
-        const int64_t units = (recs[i].n + UNIT - 1) / UNIT, whole = vec ? recs[i].n / UNIT : units;
+    auto add = [&](size_t i, DensePath how, int at_once) {   // the partial last unit is a chunk of its own on the paths for whole units
+        const int64_t units = (recs[i].n + UNIT - 1) / UNIT, whole = how != PATH_ANY ? recs[i].n / UNIT : units;
         for (int64_t k = 0; k < whole; k += at_once)
-            chunks.push_back({(int32_t)i, (uint32_t)k, (int32_t)std::min<int64_t>(at_once, whole - k), vec ? 1 : 0});
-        if (whole < units) chunks.push_back({(int32_t)i, (uint32_t)whole, 1, 0});
+            chunks.push_back({(int32_t)i, (uint32_t)k, (int32_t)std::min<int64_t>(at_once, whole - k), how});
+        if (whole < units) chunks.push_back({(int32_t)i, (uint32_t)whole, 1, PATH_ANY});
     };
     for (int key = 0; key < KEY_COUNT; ++key) {
         const int first = (int)chunks.size();
         for (size_t i = 0; i < recs.size(); ++i)
-            if (plan->descs[i].flags == 0 && key_of(plan->descs[i]) == key) add(i, vector[i], plan->step_units[plan->descs[i].state]);
+            if (plan->descs[i].flags == 0 && key_of(plan->descs[i]) == key) add(i, path[i], plan->step_units[plan->descs[i].state]);
         const int got = (int)chunks.size() - first;
-        if (got) groups.push_back({key, first, got});
+        const bool mixed = std::any_of(chunks.begin() + first, chunks.end(), [](const DenseChunk &c) { return c.path != PATH_VECTORS; });
+        if (got) groups.push_back({key, first, got, mixed});
     }
     const int norm_first = (int)chunks.size();
     for (size_t i = 0; i < recs.size(); ++i)
-        if (plan->descs[i].flags != TSR_DENSE_STATE_ONLY) add(i, false, plan->norm_units);
+        if (plan->descs[i].flags != TSR_DENSE_STATE_ONLY) add(i, PATH_ANY, plan->norm_units);
     const int copy_first = (int)chunks.size();
     for (size_t i = 0; i < recs.size(); ++i)
-        if (plan->descs[i].flags != TSR_DENSE_NORM_ONLY) add(i, false, plan->copy_units);
+        if (plan->descs[i].flags != TSR_DENSE_NORM_ONLY) add(i, PATH_ANY, plan->copy_units);
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return dense_fail(plan, TSR_ERR_CUDA, "no CUDA device available");
     DENSE_CUDA(plan, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
@@ -1122,7 +1182,7 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
 void dense_layout(tsr_dense_plan *plan, const tsr_dense_desc *descs, int32_t count)
 {
     if (count > 0) plan->descs.assign(descs, descs + count);
-    auto chunks_at = [&](int64_t units) {   // of so many units, with the last units of the vector path
+    auto chunks_at = [&](int64_t units) {   // of so many units, and one more for the last
         int64_t k = 0;
         for (const tsr_dense_desc &d : plan->descs) k += (d.rows * d.cols + units * UNIT - 1) / (units * UNIT) + 1;
         return k;
@@ -1240,8 +1300,7 @@ tsr_status tsr_dense_plan_step(tsr_dense_plan *plan, const tsr_hyper *h, const f
     a.step_lo = (uint32_t)h->step;
     for (const tsr_dense_plan::Group &g : plan->groups) {
         const DenseChunk *chunks = plan->d_chunks + g.first;
-        const bool sr = rounding == TSR_ROUND_STOCHASTIC && (g.key & (KEY_Q8 | KEY_P_BF16));   // else nothing is rounded
-        DENSE_CUDA(plan, step_launch(g.key, sr, plan->d_recs, chunks, g.count, a, (cudaStream_t)stream));
+        DENSE_CUDA(plan, step_launch(g.key, rounding == TSR_ROUND_STOCHASTIC, g.mixed, plan->d_recs, chunks, g.count, a, (cudaStream_t)stream));
     }
     return TSR_OK;
 }
