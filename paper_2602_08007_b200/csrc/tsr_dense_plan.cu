@@ -232,9 +232,15 @@ __device__ __forceinline__ float max_abs8(const float2 (&x)[4])
 {
     return max_abs3(max_abs3(x[0].x, x[0].y, x[1].x), max_abs3(x[1].y, x[2].x, x[2].y), max_abs3(x[3].x, x[3].y, 0.f));
 }
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
 __device__ __forceinline__ float max8(const float2 (&x)[4])
 {
-    return fmaxf(fmaxf(fmaxf(x[0].x, x[0].y), fmaxf(x[1].x, x[1].y)), fmaxf(fmaxf(x[2].x, x[2].y), fmaxf(x[3].x, x[3].y)));
+    return max3(max3(x[0].x, x[0].y, x[1].x), max3(x[1].y, x[2].x, x[2].y), fmaxf(x[3].x, x[3].y));
 }
 __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
 {
@@ -586,6 +592,8 @@ template <typename PT, typename GT, bool Q8> struct RawUnit {
     float2 scale;
 };
 
+struct Values { float2 p[4], g[4], m[4], v[4], scale; };   // the same in FP32
+
 template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers to the lane's elements of a unit
     PT *p;
     const GT *g;
@@ -626,36 +634,39 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
         if constexpr (Q8) scale += off / UNIT;
         if (sizeof(PT) == 4 && image) image += off;
     }
-    template <bool SR>
-    __device__ __forceinline__ void step(const RawUnit<PT, GT, Q8> &raw, uint32_t e, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key) const
+    static __device__ __forceinline__ void unpack(const RawUnit<PT, GT, Q8> &raw, Values &x)
     {
-        float2 xp[4], xg[4], xm[4], xv[4];
-        raw.p.get(xp);
-        raw.g.get(xg);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) xg[j] = mul2(xg[j], pair(gs));
+        raw.p.get(x.p);
+        raw.g.get(x.g);
         if constexpr (Q8) {
-            e4m3_unpack(raw.cm, xm);
-            e4m3_unpack(raw.cr, xv);
-            update_q8(xp, xg, xm, xv, raw.scale, a, lr, decay);
+            e4m3_unpack(raw.cm, x.m);
+            e4m3_unpack(raw.cr, x.v);
+            x.scale = raw.scale;
         } else {
-            raw.m.get(xm);
-            raw.v.get(xv);
-            update_f32(xp, xg, xm, xv, a, lr, decay);
+            raw.m.get(x.m);
+            raw.v.get(x.v);
         }
+    }
+    template <bool SR>
+    __device__ __forceinline__ void step(Values &x, uint32_t e, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key) const
+    {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.g[j] = mul2(x.g[j], pair(gs));
+        if constexpr (Q8) update_q8(x.p, x.g, x.m, x.v, x.scale, a, lr, decay);
+        else update_f32(x.p, x.g, x.m, x.v, a, lr, decay);
         auto element = [&](int j) { return e + j; };
-        if constexpr (SR && sizeof(PT) == 2) *(uint4 *)p = round_params(xp, key, element);
-        else Eight<PT>::put(p, xp);
-        if (sizeof(PT) == 4 && image) Eight<bf16>::put(image, xp);
+        if constexpr (SR && sizeof(PT) == 2) *(uint4 *)p = round_params(x.p, key, element);
+        else Eight<PT>::put(p, x.p);
+        if (sizeof(PT) == 4 && image) Eight<bf16>::put(image, x.p);
         if constexpr (Q8) {
             uint2 cm, cr;
-            const float2 s = quantise<SR>(xm, xv, key, element, cm, cr);
+            const float2 s = quantise<SR>(x.m, x.v, key, element, cm, cr);
             *(uint2 *)m = cm;
             *(uint2 *)v = cr;
             if (lane == 0) *scale = s;
         } else {
-            Eight<float>::put((float *)m, xm);
-            Eight<float>::put((float *)v, xv);
+            Eight<float>::put((float *)m, x.m);
+            Eight<float>::put((float *)v, x.v);
         }
     }
 };
@@ -667,7 +678,7 @@ template <typename PT, typename GT> struct Ring {
     static constexpr int P_VECS = sizeof(PT) / 2, G_VECS = sizeof(GT) / 2;   // 16-byte vectors of a lane
     static constexpr int THREADS = WARPS * 32;
     static constexpr int SLOT = THREADS * (16 * (P_VECS + G_VECS) + 16) + WARPS * 8;
-    static constexpr int DEPTH = P_VECS + G_VECS == 2 ? 4 : P_VECS + G_VECS == 3 ? 3 : 2;
+    static constexpr int DEPTH = P_VECS + G_VECS == 2 ? 5 : P_VECS + G_VECS == 3 ? 4 : 3;   // three CTAs on an SM
     static constexpr int BYTES = DEPTH * SLOT;
 
     static __device__ __forceinline__ void copy16(uint32_t to, const void *from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
@@ -737,6 +748,7 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
         VectorUnit<PT, GT, Q8> u(t, base, lane);
         uint32_t e = (uint32_t)base + lane * 8;
         RawUnit<PT, GT, Q8> raw;
+        Values x;
         if constexpr (RING) {
             typedef Ring<PT, GT> R;
             extern __shared__ __align__(16) char slots[];
@@ -756,18 +768,18 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
                 R::commit();
                 in = in + R::SLOT == R::BYTES ? 0 : in + R::SLOT;
                 out = out + R::SLOT == R::BYTES ? 0 : out + R::SLOT;
-                u.template step<SR>(raw, e, lane, gs, a, lr, decay, key);
+                u.unpack(raw, x);
+                u.template step<SR>(x, e, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
                 e += STRIDE;
             }
         } else if constexpr (Q8) {
-            RawUnit<PT, GT, Q8> next;   // on its way while this unit is worked on
-            u.load(next, 0);
+            u.load(raw, 0);
 #pragma unroll 1
             for (; todo > 0; --todo) {
-                raw = next;
-                if (todo > 1) u.load(next, STRIDE);
-                u.template step<SR>(raw, e, lane, gs, a, lr, decay, key);
+                u.unpack(raw, x);
+                if (todo > 1) u.load(raw, STRIDE);   // on its way while this unit is worked on
+                u.template step<SR>(x, e, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
                 e += STRIDE;
             }
@@ -775,7 +787,8 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
 #pragma unroll 1
             for (; todo > 0; --todo) {
                 u.load(raw, 0);
-                u.template step<SR>(raw, e, lane, gs, a, lr, decay, key);
+                u.unpack(raw, x);
+                u.template step<SR>(x, e, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
                 e += STRIDE;
             }
