@@ -182,6 +182,7 @@ __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x)
     x ^= x >> 16; x *= 0x85ebca6bu; x ^= x >> 13; x *= 0xc2b2ae35u; return x ^ (x >> 16);
 }
 // The word before its last step x ^ (x >> 16): the upper half is final, the lower one is still to be combined with it.
+// (Sharing x >> 16 among the lane's neighbours, which differ in it only across a carry, was measured: 3 % slower.)
 __device__ __forceinline__ uint32_t random_word(uint32_t counter, uint32_t key1, uint32_t key2)
 {
     uint32_t x = counter + key1;
@@ -190,6 +191,11 @@ __device__ __forceinline__ uint32_t random_word(uint32_t counter, uint32_t key1,
     x = x ^ (x >> 13) ^ key2;
     return x * 0xc2b2ae35u;
 }
+
+// Which elements of its tensor a lane holds: pairs of neighbours that follow one another, or that are 64 apart; half: half of
+// the first one's position.  Counters are taken modulo 2^32.
+struct EightFrom { uint32_t half; static constexpr int STEP = 2; };
+struct PairsFrom { uint32_t half; static constexpr int STEP = 64; };
 
 // ---- one unit's arithmetic ------------------------------------------------------------------------------------------
 //
@@ -303,8 +309,7 @@ __device__ __forceinline__ void update_q8(float2 (&p)[4], const float2 (&g)[4], 
     }
 }
 
-// New scales of the warp's block, and the codes of m / scale and r / scale for the lane's eight (nr = -r); element(j) is the
-// position of element j of the lane in the tensor.
+// New scales of the warp's block, and the codes of m / scale and r / scale for the lane's eight (nr = -r).
 //
 // To nearest, the conversion instruction does it.  Stochastic: 2^-120 x / scale has the E4M3 code of x / scale in its bits 20
 // to 26, FP32's exponent field running as E4M3's does and its denormal numbers being E4M3's (both have a spacing of one unit
@@ -313,8 +318,8 @@ __device__ __forceinline__ void update_q8(float2 (&p)[4], const float2 (&g)[4], 
 //
 // A root above zero has code 1 at least.  That takes two instructions an element, and only a block that spans a factor of
 // 2^17 needs it: a warp without a root below 2^-9 scale skips them.
-template <bool SR, typename Elem>
-__device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&nr)[4], UnitKeys k, Elem element, uint2 &cm, uint2 &cr)
+template <bool SR, typename Where>
+__device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&nr)[4], UnitKeys k, Where where, uint2 &cm, uint2 &cr)
 {
     float2 scale, inv;
     block_scale(__float_as_uint(warp_max_abs(max_abs8(m))), scale.x, inv.x);
@@ -334,7 +339,7 @@ __device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&nr)[4], Unit
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            const uint32_t w = random_word((uint32_t)element(j), k.k1, k.k2);
+            const uint32_t w = random_word(2 * where.half + Where::STEP * (j >> 1) + (j & 1), k.k1, k.k2);
             const uint32_t hi = __byte_perm(w, 0, 0x4324), lo = __byte_perm(w, 0, 0x4104) ^ hi;   // halves of the word, eight bits up
             um[j] = (um[j] * 16u + lo) | (um[j] & 0x80000000u);
             ur[j] = ur[j] * 16u + hi;
@@ -371,14 +376,14 @@ __device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&nr)[4], Unit
 // BF16 parameters, stochastic: 16 random bits are added below the seven mantissa bits and the rest is cut off; one random
 // word serves elements 2i and 2i + 1 (a pair starts at an even position).  A lane that holds Inf or NaN rounds its eight to
 // nearest.  Returns the BF16 values.
-template <typename Elem>
-__device__ __forceinline__ uint4 round_params(const float2 (&p)[4], UnitKeys k, Elem element)
+template <typename Where>
+__device__ __forceinline__ uint4 round_params(const float2 (&p)[4], UnitKeys k, Where where)
 {
     if (!(max_abs8(p) < __uint_as_float(0x7f800000u))) return bf16_pack(p);
     uint32_t w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const uint32_t x = random_word((uint32_t)(element(2 * j) >> 1), k.k1 ^ 0x5bd1e995u, k.k2), hi = x >> 16;
+        const uint32_t x = random_word(where.half + Where::STEP / 2 * j, k.k1 ^ 0x5bd1e995u, k.k2), hi = x >> 16;
         w[j] = __byte_perm(__float_as_uint(p[j].x) + ((x ^ hi) & 0xffffu), __float_as_uint(p[j].y) + hi, 0x7632);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
@@ -542,10 +547,10 @@ __device__ __forceinline__ void step_pairs_unit(const DenseRec &t, int64_t base,
     for (int j = 0; j < 4; ++j) g[j] = mul2(g[j], pair(gs));
     if constexpr (Q8) update_q8(p, g, m, v, scale, a, lr, decay);
     else update_f32(p, g, m, v, a, lr, decay);
-    auto element = [&](int j) { return pair_at(base, lane, j >> 1) + (j & 1); };
+    const PairsFrom where = {(uint32_t)(base >> 1) + lane};
     if constexpr (SR && sizeof(PT) == 2) {
         Eight<bf16> rounded;
-        rounded.r = round_params(p, key, element);
+        rounded.r = round_params(p, key, where);
         rounded.get(p);
     }
     store_matrix<PATH>((PT *)t.p, t, t.ldp, base, row, col, lane, p);
@@ -553,9 +558,9 @@ __device__ __forceinline__ void step_pairs_unit(const DenseRec &t, int64_t base,
     if constexpr (Q8) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (!WHOLE && element(j) >= t.n) at(m, j) = at(v, j) = 0.f;   // (0 * NaN of a poisoned block)
+            if (!WHOLE && pair_at(base, lane, j >> 1) + (j & 1) >= t.n) at(m, j) = at(v, j) = 0.f;   // (0 * NaN of a poisoned block)
         uint2 cm, cr;
-        const float2 s = quantise<SR>(m, v, key, element, cm, cr);
+        const float2 s = quantise<SR>(m, v, key, where, cm, cr);
         if (lane == 0) t.scale[base / UNIT] = s;
         store_code_pairs<WHOLE>(t.m, both, base, lane, t.n, cm);
         store_code_pairs<WHOLE>(t.v, both, base, lane, t.n, cr);
@@ -648,19 +653,19 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
         }
     }
     template <bool SR>
-    __device__ __forceinline__ void step(Values &x, uint32_t e, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key) const
+    __device__ __forceinline__ void step(Values &x, uint32_t half, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key) const
     {
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.g[j] = mul2(x.g[j], pair(gs));
         if constexpr (Q8) update_q8(x.p, x.g, x.m, x.v, x.scale, a, lr, decay);
         else update_f32(x.p, x.g, x.m, x.v, a, lr, decay);
-        auto element = [&](int j) { return e + j; };
-        if constexpr (SR && sizeof(PT) == 2) *(uint4 *)p = round_params(x.p, key, element);
+        const EightFrom where = {half};
+        if constexpr (SR && sizeof(PT) == 2) *(uint4 *)p = round_params(x.p, key, where);
         else Eight<PT>::put(p, x.p);
         if (sizeof(PT) == 4 && image) Eight<bf16>::put(image, x.p);
         if constexpr (Q8) {
             uint2 cm, cr;
-            const float2 s = quantise<SR>(x.m, x.v, key, element, cm, cr);
+            const float2 s = quantise<SR>(x.m, x.v, key, where, cm, cr);
             *(uint2 *)m = cm;
             *(uint2 *)v = cr;
             if (lane == 0) *scale = s;
@@ -746,7 +751,7 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
     if (todo <= 0) return;
     if (!MIXED || ch.path == PATH_VECTORS) {
         VectorUnit<PT, GT, Q8> u(t, base, lane);
-        uint32_t e = (uint32_t)base + lane * 8;
+        uint32_t half = (uint32_t)(base >> 1) + lane * 4;   // half of the position of the lane's first element
         RawUnit<PT, GT, Q8> raw;
         Values x;
         if constexpr (RING) {
@@ -769,9 +774,9 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
                 in = in + R::SLOT == R::BYTES ? 0 : in + R::SLOT;
                 out = out + R::SLOT == R::BYTES ? 0 : out + R::SLOT;
                 u.unpack(raw, x);
-                u.template step<SR>(x, e, lane, gs, a, lr, decay, key);
+                u.template step<SR>(x, half, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
-                e += STRIDE;
+                half += STRIDE / 2;
             }
         } else if constexpr (Q8) {
             u.load(raw, 0);
@@ -779,18 +784,18 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
             for (; todo > 0; --todo) {
                 u.unpack(raw, x);
                 if (todo > 1) u.load(raw, STRIDE);   // on its way while this unit is worked on
-                u.template step<SR>(x, e, lane, gs, a, lr, decay, key);
+                u.template step<SR>(x, half, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
-                e += STRIDE;
+                half += STRIDE / 2;
             }
         } else {
 #pragma unroll 1
             for (; todo > 0; --todo) {
                 u.load(raw, 0);
                 u.unpack(raw, x);
-                u.template step<SR>(x, e, lane, gs, a, lr, decay, key);
+                u.template step<SR>(x, half, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
-                e += STRIDE;
+                half += STRIDE / 2;
             }
         }
     } else if (ch.path == PATH_PLAIN) {
@@ -942,7 +947,7 @@ __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s,
         } else if constexpr (DQ && !SQ) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) at(v, j) = -__fsqrt_rn(at(v, j));
-            scale = quantise<false>(m, v, UnitKeys{0, 0}, [](int j) { return j; }, cm, cr);
+            scale = quantise<false>(m, v, UnitKeys{0, 0}, EightFrom{0}, cm, cr);
         } else if constexpr (DQ) {   // codes of their own values
             cm = e4m3_pack(m);
             cr = e4m3_pack(v);

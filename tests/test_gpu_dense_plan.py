@@ -403,6 +403,39 @@ def test_offsets_beyond_32_bits(tsr):
     assert torch.equal(back.states[0][0][-BLOCK:], (s[0].view(torch.uint8)[-BLOCK:].view(F8).float() * s[2][(n - BLOCK) // BLOCK:, 0].repeat_interleave(BLOCK)[(n - BLOCK) % BLOCK:][:BLOCK]))
 
 
+@pytest.mark.parametrize("shift", [0, 1])
+def test_random_words_beyond_32_bits(tsr, shift):
+    """More than 2^32 elements: the words of a BF16 parameter count pairs, modulo 2^32 pairs, those of the state elements,
+    modulo 2^32 elements, on both sides of the 32-bit border."""
+    n = (1 << 32) + 8192
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of free device memory")
+    p = torch.full((n + shift,), 1.2345, dtype=torch.bfloat16, device="cuda")[shift:]
+    g = torch.zeros(n + shift, dtype=torch.bfloat16, device="cuda")[shift:]
+    zero = lambda: torch.zeros(n, dtype=torch.uint8, device="cuda")  # noqa: E731
+    m8 = zero()
+    m8 += 0x51                                                         # the E4M3 value 9
+    plan = tsr.DensePlan([p], [g], states=[(m8.view(F8), zero().view(F8), torch.ones((n + BLOCK - 1) // BLOCK, 2, device="cuda"))])
+    start = np.float32(p[0].item())
+    seed, t = 77, 5
+    hy, h = hyper(tsr, t, eps=f32(1e30), wd=f32(0.3))
+    plan.step(hy, rounding=tsr.TSR_ROUND_STOCHASTIC, seed=seed)
+    k1, k2 = dm.keys(seed, t, 0)
+    F = np.float32
+    decayed = start * (F(1) - F(h["lr"]) * F(h["wd"]))
+    m1 = F(h["beta1"]) * F(9)
+    for at in (0, (1 << 32) - 4096, 1 << 32, n - 4096):
+        e = np.arange(at, at + 4096, dtype=np.uint64)
+        w = dm.random_words((e >> 1).astype(np.uint32), k1 ^ 0x5BD1E995, k2)
+        u = np.where(e & 1, w >> 16, w & 0xFFFF).astype(np.uint32)
+        want = ((decayed.view(np.uint32) + u) & np.uint32(0xFFFF0000)).view(np.float32)
+        assert np.array_equal(p[at:at + 4096].float().cpu().numpy(), want)
+        w = dm.random_words(e.astype(np.uint32), k1, k2)
+        scale = dm.scale_of(np.full((1, 1), m1))
+        code = dm.quantise(np.full(4096, m1, F), scale[0, 0], w & np.uint32(0xFFFF))
+        assert np.array_equal(codes(plan.states[0][0][at:at + 4096]), code)
+
+
 @pytest.mark.parametrize("cols,ld", [(5461, 5464), (1, 3), (31, 33)])
 def test_pitched_matrices_step_like_contiguous_ones(tsr, cols, ld):
     rows = 37
