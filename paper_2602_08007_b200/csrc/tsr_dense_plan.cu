@@ -676,9 +676,9 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
     }
 };
 
-// The 8-bit form reads so little per unit that a unit's loads in registers do not keep HBM busy.  So a lane's loads go to
-// slots of shared memory that only this lane reads (asynchronous copies of 16 and 8 bytes, no barrier between warps):
-// DEPTH slots, DEPTH - 1 of them on their way.
+// The 8-bit form reads so little per unit that a unit's loads in registers do not keep HBM busy.  So a warp's loads go to
+// slots of shared memory that only its warp reads (asynchronous copies of 16 and 8 bytes, no barrier between warps): DEPTH
+// slots, DEPTH - 1 of them on their way.
 template <typename PT, typename GT> struct Ring {
     static constexpr int P_VECS = sizeof(PT) / 2, G_VECS = sizeof(GT) / 2;   // 16-byte vectors of a lane
     static constexpr int THREADS = WARPS * 32;
@@ -695,28 +695,38 @@ template <typename PT, typename GT> struct Ring {
     static __device__ __forceinline__ void issue(uint32_t to, const VectorUnit<PT, GT, true> &u, int units, int lane)
     {
         const int off = units * WARPS * UNIT;
-        const uint32_t t16 = to + threadIdx.x * 16, t8 = to + THREADS * 16 * (P_VECS + G_VECS) + threadIdx.x * 8;
-#pragma unroll
-        for (int k = 0; k < P_VECS; ++k) copy16(t16 + k * THREADS * 16, (const char *)(u.p + off) + 16 * k);
-#pragma unroll
-        for (int k = 0; k < G_VECS; ++k) copy16(t16 + (P_VECS + k) * THREADS * 16, (const char *)(u.g + off) + 16 * k);
+        const uint32_t t8 = to + THREADS * 16 * (P_VECS + G_VECS) + threadIdx.x * 8;
+        put(to, u.p + off, lane);
+        put(to + P_VECS * THREADS * 16, u.g + off, lane);
         copy8(t8, u.m + off);
         copy8(t8 + THREADS * 8, u.v + off);
         if (lane == 0) copy8(to + THREADS * (16 * (P_VECS + G_VECS) + 16) + (threadIdx.x >> 5) * 8, u.scale + off / UNIT);
     }
-    static __device__ __forceinline__ void fetch(const char *slot, RawUnit<PT, GT, true> &r)
+    static __device__ __forceinline__ void fetch(const char *slot, int lane, RawUnit<PT, GT, true> &r)
     {
-        const char *s16 = slot + threadIdx.x * 16, *s8 = slot + THREADS * 16 * (P_VECS + G_VECS) + threadIdx.x * 8;
-        get(s16, r.p);
-        get(s16 + P_VECS * THREADS * 16, r.g);
+        const char *s8 = slot + THREADS * 16 * (P_VECS + G_VECS) + threadIdx.x * 8;
+        get(slot, lane, r.p);
+        get(slot + P_VECS * THREADS * 16, lane, r.g);
         r.cm = *(const uint2 *)s8;
         r.cr = *(const uint2 *)(s8 + THREADS * 8);
         r.scale = *(const float2 *)(slot + THREADS * (16 * (P_VECS + G_VECS) + 16) + (threadIdx.x >> 5) * 8);
     }
-    static __device__ __forceinline__ void get(const char *s, Eight<bf16> &x) { x.r = *(const uint4 *)s; }
-    static __device__ __forceinline__ void get(const char *s, Eight<float> &x)
+    // A warp's 256 BF16 elements: a vector of 16 bytes for each lane.
+    static __device__ __forceinline__ void put(uint32_t to, const bf16 *x, int lane) { copy16(to + threadIdx.x * 16, x); }
+    static __device__ __forceinline__ void get(const char *s, int lane, Eight<bf16> &x) { x.r = *(const uint4 *)(s + threadIdx.x * 16); }
+    // 256 FP32 elements, 64 vectors: copied in order (lanes 16 bytes apart, so that whole sectors travel), read two by two.  Vector
+    // c lies at place c ^ bit 3 of c, which keeps the reads, 32 bytes apart, free of bank conflicts.
+    static __device__ __forceinline__ void put(uint32_t to, const float *x, int lane)
     {
-        const uint4 a = *(const uint4 *)s, b = *(const uint4 *)(s + THREADS * 16);
+        to += (threadIdx.x >> 5) * 1024 + (lane ^ ((lane >> 3) & 1)) * 16;
+        copy16(to, (const char *)x - lane * 16);
+        copy16(to + 512, (const char *)x - lane * 16 + 512);
+    }
+    static __device__ __forceinline__ void get(const char *s, int lane, Eight<float> &x)
+    {
+        s += (threadIdx.x >> 5) * 1024;
+        const int bit = (lane >> 2) & 1;
+        const uint4 a = *(const uint4 *)(s + ((2 * lane) ^ bit) * 16), b = *(const uint4 *)(s + ((2 * lane + 1) ^ bit) * 16);
         x.r = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     }
 };
@@ -767,8 +777,8 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
 #pragma unroll 1
             for (; todo > 0; --todo) {
                 R::wait();
-                __syncwarp();   // lane 0's copy of the scale; and every lane has read the slot that is filled next
-                R::fetch(slots + out, raw);
+                __syncwarp();   // other lanes' copies; and every lane has read the slot that is filled next
+                R::fetch(slots + out, lane, raw);
                 if (todo >= R::DEPTH) R::issue(first + in, u, R::DEPTH - 1, lane);
                 R::commit();
                 in = in + R::SLOT == R::BYTES ? 0 : in + R::SLOT;
