@@ -731,6 +731,8 @@ template <typename PT, typename GT> struct Ring {
     }
 };
 
+template <typename PT> __host__ __device__ constexpr bool uses_ring(bool q8, bool sr) { return q8 && (!sr || sizeof(PT) == 4); }
+
 // MIXED: there are chunks of every path.  Where all chunks are vectors, a kernel without the other paths is launched: their
 // registers cost the FP32 form 1.5 % (1B set: 4.88 against 4.81 ms).
 template <typename PT, typename GT, bool Q8, bool SR, bool MIXED>
@@ -755,7 +757,7 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
         if (!isfinite(gs)) return;
     }
     constexpr int64_t STRIDE = WARPS * UNIT;
-    constexpr bool RING = Q8 && !SR;
+    constexpr bool RING = uses_ring<PT>(Q8, SR);
     int64_t base = ((int64_t)ch.first + warp) * UNIT;
     int todo = (ch.units - warp + WARPS - 1) / WARPS;   // units of this warp
     if (todo <= 0) return;
@@ -1057,7 +1059,7 @@ int key_of(const tsr_dense_desc &d)
 template <typename PT, typename GT, bool Q8, bool SR>
 cudaError_t step_launch_as(bool mixed, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
 {
-    const int smem = Q8 && !SR ? Ring<PT, GT>::BYTES : 0;
+    const int smem = uses_ring<PT>(Q8, SR) ? Ring<PT, GT>::BYTES : 0;
     return mixed ? launch_dependent(dense_step_kernel<PT, GT, Q8, SR, true>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a)
                  : launch_dependent(dense_step_kernel<PT, GT, Q8, SR, false>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a);
 }
@@ -1082,11 +1084,12 @@ cudaError_t step_launch(int key, bool sr, bool mixed, const DenseRec *recs, cons
     }
 }
 
-template <typename PT, typename GT> cudaError_t step_configure()   // shared memory of the kernels with a ring
+template <typename PT, typename GT, bool SR> cudaError_t step_configure()   // shared memory of the kernels with a ring
 {
-    cudaError_t e = cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, false, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
+    if (!uses_ring<PT>(true, SR)) return cudaSuccess;
+    cudaError_t e = cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, SR, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, false, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
+    return cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, SR, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
 }
 
 tsr_status dense_ready(const tsr_dense_plan *plan)
@@ -1179,10 +1182,12 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return dense_fail(plan, TSR_ERR_CUDA, "no CUDA device available");
     DENSE_CUDA(plan, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    DENSE_CUDA(plan, (step_configure<float, float>()));
-    DENSE_CUDA(plan, (step_configure<bf16, float>()));
-    DENSE_CUDA(plan, (step_configure<float, bf16>()));
-    DENSE_CUDA(plan, (step_configure<bf16, bf16>()));
+    DENSE_CUDA(plan, (step_configure<float, float, false>()));
+    DENSE_CUDA(plan, (step_configure<float, float, true>()));
+    DENSE_CUDA(plan, (step_configure<float, bf16, false>()));
+    DENSE_CUDA(plan, (step_configure<float, bf16, true>()));
+    DENSE_CUDA(plan, (step_configure<bf16, float, false>()));
+    DENSE_CUDA(plan, (step_configure<bf16, bf16, false>()));
     plan->bound = false;
     DENSE_CUDA(plan, cudaDeviceSynchronize());   // nothing that still runs may see the tables change
     char *at = (char *)workspace;
