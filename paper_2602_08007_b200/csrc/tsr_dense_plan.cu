@@ -1044,7 +1044,10 @@ tsr_status dense_fail(const tsr_dense_plan *plan, tsr_status s, const char *fmt,
 #define DENSE_CUDA(plan, call)                                                                                  \
     do {                                                                                                        \
         cudaError_t e__ = (call);                                                                               \
-        if (e__ != cudaSuccess) return dense_fail(plan, TSR_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e__)); \
+        if (e__ != cudaSuccess) {                                                                               \
+            (void)cudaGetLastError();   /* not left for the caller's next check */                             \
+            return dense_fail(plan, TSR_ERR_CUDA, "%s failed: %s", #call, cudaGetErrorString(e__));             \
+        }                                                                                                       \
     } while (0)
 
 constexpr int64_t DENSE_MOST = (int64_t)1 << 40;   // elements of a tensor with its pitch; keeps products in 64 bits

@@ -12,6 +12,8 @@ from .binding import (
 )
 
 _DTYPE = {torch.float32: TSR_F32, torch.bfloat16: TSR_BF16}
+# The handle of torch's current stream on a device, without a Stream object around it (2 us of the 6 us of a small call).
+_current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _matrix(t: torch.Tensor, what: str):
@@ -64,6 +66,8 @@ class DensePlan:
         self.device = first.device if first is not None else torch.device("cuda", torch.cuda.current_device())
         if self.device.type != "cuda":
             raise ValueError("tensors must live on a CUDA device")
+        self._index = self.device.index
+        self._lib = lib()
         self.states = self._zero_states(state_dtype) if states is None else [tuple(s) for s in states]
         self.images = list(images) if images is not None else [None] * n
         self.lr_mult = [1.0] * n if lr_mult is None else [float(x) for x in lr_mult]
@@ -161,7 +165,7 @@ class DensePlan:
             pass
 
     def _stream(self, stream):
-        return (torch.cuda.current_stream(self.device) if stream is None else stream).cuda_stream
+        return _current_stream(self._index) if stream is None else stream.cuda_stream
 
     # -- the C calls --------------------------------------------------------------------------
     def step(self, hyper: Hyper, grad_scale: Optional[torch.Tensor] = None, rounding: int = TSR_ROUND_NEAREST, seed: int = 0, stream=None):
@@ -172,7 +176,9 @@ class DensePlan:
             if grad_scale.dtype != torch.float32 or grad_scale.device != self.device or grad_scale.numel() < 1:
                 raise ValueError("grad_scale must be an FP32 tensor on %s" % self.device)
             scale = grad_scale.data_ptr()
-        self._check(lib().tsr_dense_plan_step(self.ctx, ctypes.byref(hyper), scale, rounding, seed, self._stream(stream)))
+        status = self._lib.tsr_dense_plan_step(self.ctx, ctypes.byref(hyper), scale, rounding, seed, self._stream(stream))
+        if status != TSR_OK:
+            self._check(status)
 
     def grad_norm(self, max_norm: float = float("inf"), out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """(norm, clipping factor) of all gradients as an FP32 tensor on the device: `out`, or one the plan owns and the next
@@ -181,9 +187,11 @@ class DensePlan:
             out = self._result
         elif out.dtype != torch.float32 or out.device != self.device or out.numel() < 2 or not out.is_contiguous():
             raise ValueError("out must be a contiguous FP32 tensor of two elements on %s" % self.device)
-        self._check(lib().tsr_dense_plan_grad_norm(self.ctx, max_norm, out.data_ptr(), self._stream(stream)))
+        status = self._lib.tsr_dense_plan_grad_norm(self.ctx, max_norm, out.data_ptr(), self._stream(stream))
+        if status != TSR_OK:
+            self._check(status)
         return out
 
     def copy_state(self, src: "DensePlan", stream=None):
         """Takes over the moments of `src`, a plan over tensors of the same sizes, converting between FP32 and 8 bits."""
-        self._check(lib().tsr_dense_plan_copy_state(self.ctx, src.ctx, self._stream(stream)))
+        self._check(self._lib.tsr_dense_plan_copy_state(self.ctx, src.ctx, self._stream(stream)))
