@@ -23,20 +23,24 @@ namespace tsr {
 constexpr int UNIT = TSR_DENSE_BLOCK;      // elements of a warp's piece of work
 static_assert(UNIT == 32 * 8, "a lane holds eight elements of a unit");
 constexpr int WARPS = 8;                   // per CTA
-// Most units of a warp in one chunk, by what goes over the chunk.  FP32 steps overlap by having many CTAs at a time and
-// are faster short (1B set: 4.81 ms with 2 units, 4.96 with 8); the others have work per CTA or load ahead (130M set, 8-bit
-// step: 301 us with 1 unit, 232 with 2, 213 with 8; 1B norm: 1164, 705, 440 and 406 with 16).
-constexpr int STEP_F32_UNITS = 2, STEP_Q8_UNITS = 8, COPY_UNITS = 16, NORM_UNITS = 16;
-constexpr int MANY_CHUNKS = 2048;          // fewer than this: shorter chunks, so that the GPU fills
-constexpr int NORM_CTAS = 1184;            // most CTAs of a norm launch (8 on each of 148 SMs)
+// Most units of a warp in one chunk, by what goes over it.  FP32 steps overlap by having many CTAs at a time and are faster
+// short (1B set: 4.81 ms with 2 units, 4.96 with 8); the others have work per CTA or load ahead (130M set, 8-bit step: 301 us
+// with 1 unit, 232 with 2, 213 with 8; 1B norm: 1164, 705, 440 and 406 with 16).  Without vectors nothing is loaded ahead
+// (two pitched 1B layers: 258 us with 4 units, 263 with 2), and chunks of narrow pitched matrices are slow ones.
+constexpr int STEP_F32_UNITS = 2, STEP_Q8_UNITS = 8, COPY_UNITS = 16, NORM_UNITS = 16, PAIRS_UNITS = 4, ANY_UNITS = 1;
+// CTAs on an SM of the kernels, whose registers are bounded for it.
+constexpr int STEP_F32_CTAS = 4, STEP_Q8_CTAS = 3, COPY_CTAS = 5, NORM_CTAS = 4;
+constexpr int SMS = 148;
+// Fewer chunks than this are made shorter, so that they fill the GPU (8-bit step of 4 M elements: 14.9 us, 20.1 with a bound of
+// 2048; conversions hold 5 CTAs on an SM and want twice as many: 30 M elements 53 us, 61 with 512).
+constexpr int MANY_CHUNKS = 512;
 
 enum DenseRecFlags : uint32_t {
     REC_VEC_STATE = 1,   // the moments can be read in vectors of eight elements
-    REC_VEC_GRAD = 2,    // so can the gradient, which is contiguous
+    REC_PAIR_STATE = 2,  // ... in pairs
     REC_PITCHED = 4,     // rows that do not follow one another directly
     REC_Q8 = 8,
     REC_G_BF16 = 16,
-    REC_PAIR_STATE = 32, // the moments can be read in pairs
 };
 
 struct alignas(16) DenseRec {   // one tensor on the device
@@ -736,7 +740,7 @@ template <typename PT> __host__ __device__ constexpr bool uses_ring(bool q8, boo
 // MIXED: there are chunks of every path.  Where all chunks are vectors, a kernel without the other paths is launched: their
 // registers cost the FP32 form 1.5 % (1B set: 4.88 against 4.81 ms).
 template <typename PT, typename GT, bool Q8, bool SR, bool MIXED>
-__global__ void __launch_bounds__(WARPS * 32, Q8 ? 3 : 4)
+__global__ void __launch_bounds__(WARPS * 32, Q8 ? STEP_Q8_CTAS : STEP_F32_CTAS)
 dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restrict__ chunks, const DenseStep a)
 {
     pdl_trigger();
@@ -849,44 +853,57 @@ __device__ __forceinline__ double cta_sum(double x, double *sh)   // valid in th
     return x;
 }
 
-// A warp's sum over its units of a chunk, 64 bytes of every lane at a time.
-template <typename GT>
-__device__ __forceinline__ double chunk_squares(const DenseRec &t, const DenseChunk &ch, int warp, int lane)
+// A warp's sum over its units of a chunk, without vectors.
+template <int PATH, typename GT>
+__device__ __forceinline__ double pairs_squares(const DenseRec &t, int64_t base, int todo, int lane)
 {
-    double sum = 0.0;
-    int64_t base = ((int64_t)ch.first + warp) * UNIT;
-    int todo = (ch.units - warp + WARPS - 1) / WARPS;
     constexpr int64_t STRIDE = WARPS * UNIT;
-    constexpr int AT_ONCE = 64 / (8 * (int)sizeof(GT));
-    if (t.flags & REC_VEC_GRAD) {
-        while (todo > 0) {
-            Eight<GT> r[AT_ONCE];
-#pragma unroll
-            for (int k = 0; k < AT_ONCE; ++k)
-                if (k < todo && base + k * STRIDE + UNIT <= t.n) r[k].load((const GT *)t.g + base + k * STRIDE + lane * 8);
-#pragma unroll
-            for (int k = 0; k < AT_ONCE; ++k) {
-                if (k >= todo || base + k * STRIDE + UNIT > t.n) break;
-                float2 g[4];
-                r[k].get(g);
-                sum += square_sum(g);
-            }
-            base += AT_ONCE * STRIDE;
-            todo -= AT_ONCE;
-        }
-        base = ((int64_t)ch.first + ch.units - 1) * UNIT;   // what is left: the tensor's last unit, where it is partial
-        if (base + UNIT <= t.n || warp != (ch.units - 1) % WARPS) return sum;
-        todo = 1;
+    double sum = 0.0;
+    int64_t row = 0, col = 0;
+    if constexpr (PATH == PATH_ROWS) {
+        row = base / t.cols;
+        col = base - row * t.cols;
     }
+#pragma unroll 4
     for (; todo > 0; --todo, base += STRIDE) {
         float2 g[4];
-        load_matrix<PATH_ANY>((const GT *)t.g, t, t.ldg, base, 0, 0, lane, g);
+        load_matrix<PATH>((const GT *)t.g, t, t.ldg, base, row, col, lane, g);
         sum += square_sum(g);
+        if constexpr (PATH == PATH_ROWS)
+            for (col += STRIDE; col >= t.cols; col -= t.cols) ++row;
     }
     return sum;
 }
 
-__global__ void __launch_bounds__(WARPS * 32, 4)
+// The same on any path; on the vector path, 64 bytes of every lane at a time.
+template <typename GT>
+__device__ __forceinline__ double chunk_squares(const DenseRec &t, const DenseChunk &ch, int warp, int lane)
+{
+    int64_t base = ((int64_t)ch.first + warp) * UNIT;
+    int todo = (ch.units - warp + WARPS - 1) / WARPS;
+    if (ch.path == PATH_PLAIN) return pairs_squares<PATH_PLAIN, GT>(t, base, todo, lane);
+    if (ch.path == PATH_ROWS) return pairs_squares<PATH_ROWS, GT>(t, base, todo, lane);
+    if (ch.path == PATH_ANY) return pairs_squares<PATH_ANY, GT>(t, base, todo, lane);
+    constexpr int64_t STRIDE = WARPS * UNIT;
+    constexpr int AT_ONCE = 64 / (8 * (int)sizeof(GT));
+    double sum = 0.0;
+    for (; todo > 0; todo -= AT_ONCE, base += AT_ONCE * STRIDE) {
+        Eight<GT> r[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k)
+            if (k < todo) r[k].load((const GT *)t.g + base + k * STRIDE + lane * 8);
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            if (k >= todo) break;
+            float2 g[4];
+            r[k].get(g);
+            sum += square_sum(g);
+        }
+    }
+    return sum;
+}
+
+__global__ void __launch_bounds__(WARPS * 32, NORM_CTAS)
 dense_norm_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restrict__ chunks, int count, float max_norm,
                   double *partial, uint32_t *ticket, float *out)
 {
@@ -983,7 +1000,7 @@ __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s,
     }
 }
 
-__global__ void __launch_bounds__(WARPS * 32)
+__global__ void __launch_bounds__(WARPS * 32, COPY_CTAS)
 dense_copy_state_kernel(const DenseRec *__restrict__ drecs, const DenseRec *__restrict__ srecs, const DenseChunk *__restrict__ chunks)
 {
     pdl_trigger();
@@ -1107,10 +1124,17 @@ tsr_status dense_ready(const tsr_dense_plan *plan)
 bool aligned(const void *p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
 int64_t size_of(int32_t dtype) { return dtype == TSR_BF16 ? 2 : 4; }
 
+// ld: the largest pitch in use
+DensePath path_of(bool contiguous, bool vectors, const tsr_dense_desc &d, int64_t ld)
+{
+    if (contiguous) return vectors ? PATH_VECTORS : PATH_PLAIN;
+    return d.cols >= UNIT && ld - d.cols < (1 << 30) ? PATH_ROWS : PATH_ANY;
+}
+
 tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *workspace)
 {
     std::vector<DenseRec> recs(plan->descs.size());
-    std::vector<DensePath> path(recs.size(), PATH_ANY);
+    std::vector<DensePath> path(recs.size(), PATH_ANY), grad_path(recs.size(), PATH_ANY);
     for (size_t i = 0; i < recs.size(); ++i) {
         const tsr_dense_desc &d = plan->descs[i];
         const tsr_dense_ptrs &p = ptrs[i];
@@ -1138,7 +1162,7 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
         if (grad) {
             r.g = p.grad;
             dense = d.rows <= 1 || d.ldg == d.cols;
-            if (dense && aligned(p.grad, 8 * gs)) r.flags |= REC_VEC_GRAD;
+            grad_path[i] = path_of(dense, aligned(p.grad, 8 * gs), d, d.ldg);
         }
         if (state) {
             r.m = p.m; r.v = p.v;
@@ -1151,18 +1175,17 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
             r.p = p.param;
             r.image = (bf16 *)p.image;
             dense = dense && (d.rows <= 1 || (d.ldp == d.cols && (!p.image || d.ldi == d.cols)));
-            const int64_t far = std::max(std::max(d.ldp, d.ldg), p.image ? d.ldi : 0) - d.cols;
-            if (dense)
-                path[i] = (r.flags & REC_VEC_GRAD) && (r.flags & REC_VEC_STATE) && aligned(p.param, 8 * ps) && aligned(p.image, 16) ? PATH_VECTORS : PATH_PLAIN;
-            else if (d.cols >= UNIT && far < (1 << 30))
-                path[i] = PATH_ROWS;
+            path[i] = path_of(dense, grad_path[i] == PATH_VECTORS && (r.flags & REC_VEC_STATE) && aligned(p.param, 8 * ps) && aligned(p.image, 16), d,
+                              std::max(std::max(d.ldp, d.ldg), p.image ? d.ldi : 0));
         }
         if (!dense) r.flags |= REC_PITCHED;
     }
     std::vector<DenseChunk> chunks;
     std::vector<tsr_dense_plan::Group> groups;
     chunks.reserve(plan->most_chunks);
-    auto add = [&](size_t i, DensePath how, int at_once) {   // the partial last unit is a chunk of its own on the paths for whole units
+    auto add = [&](size_t i, DensePath how, int at_once) {
+        if (how == PATH_ANY) at_once = std::min(at_once, WARPS * ANY_UNITS);
+        if (how == PATH_PLAIN || how == PATH_ROWS) at_once = std::min(at_once, WARPS * PAIRS_UNITS);   // the partial last unit is a chunk of its own on the paths for whole units
         const int64_t units = (recs[i].n + UNIT - 1) / UNIT, whole = how != PATH_ANY ? recs[i].n / UNIT : units;
         for (int64_t k = 0; k < whole; k += at_once)
             chunks.push_back({(int32_t)i, (uint32_t)k, (int32_t)std::min<int64_t>(at_once, whole - k), how});
@@ -1178,10 +1201,10 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     }
     const int norm_first = (int)chunks.size();
     for (size_t i = 0; i < recs.size(); ++i)
-        if (plan->descs[i].flags != TSR_DENSE_STATE_ONLY) add(i, PATH_ANY, plan->norm_units);
+        if (plan->descs[i].flags != TSR_DENSE_STATE_ONLY) add(i, grad_path[i], plan->norm_units);
     const int copy_first = (int)chunks.size();
     for (size_t i = 0; i < recs.size(); ++i)
-        if (plan->descs[i].flags != TSR_DENSE_NORM_ONLY) add(i, PATH_ANY, plan->copy_units);
+        if (plan->descs[i].flags != TSR_DENSE_NORM_ONLY) add(i, PATH_VECTORS, plan->copy_units);
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return dense_fail(plan, TSR_ERR_CUDA, "no CUDA device available");
     DENSE_CUDA(plan, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
@@ -1199,7 +1222,7 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     plan->d_chunks = (DenseChunk *)at;
     at += round_up((int64_t)(plan->most_chunks * sizeof(DenseChunk)), 256);
     plan->d_partial = (double *)at;
-    at += NORM_CTAS * sizeof(double);
+    at += NORM_CTAS * SMS * sizeof(double);
     plan->d_ticket = (uint32_t *)at;
     if (!recs.empty()) DENSE_CUDA(plan, cudaMemcpy(plan->d_recs, recs.data(), recs.size() * sizeof(DenseRec), cudaMemcpyHostToDevice));
     if (!chunks.empty()) DENSE_CUDA(plan, cudaMemcpy(plan->d_chunks, chunks.data(), chunks.size() * sizeof(DenseChunk), cudaMemcpyHostToDevice));
@@ -1210,7 +1233,7 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     plan->norm_first = norm_first;
     plan->copy_first = copy_first;
     plan->device = dev;
-    plan->norm_ctas = std::min(NORM_CTAS, 8 * sms);
+    plan->norm_ctas = NORM_CTAS * std::min(SMS, sms);
     plan->bound = true;
     return TSR_OK;
 }
@@ -1218,25 +1241,27 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
 void dense_layout(tsr_dense_plan *plan, const tsr_dense_desc *descs, int32_t count)
 {
     if (count > 0) plan->descs.assign(descs, descs + count);
-    auto chunks_at = [&](int64_t units) {   // of so many units, and one more for the last
-        int64_t k = 0;
-        for (const tsr_dense_desc &d : plan->descs) k += (d.rows * d.cols + units * UNIT - 1) / (units * UNIT) + 1;
-        return k;
+    auto tensor_chunks = [](const tsr_dense_desc &d, int64_t units) { return (d.rows * d.cols + units * UNIT - 1) / (units * UNIT) + 1; };
+    // As long as may be, but so many that the GPU fills.
+    auto fit = [&](int most, int many) {
+        for (;; most /= 2) {
+            int64_t chunks = 0;
+            for (const tsr_dense_desc &d : plan->descs) chunks += tensor_chunks(d, most * WARPS);
+            if (most == 1 || chunks >= many) return most * WARPS;
+        }
     };
-    // Long chunks spread the cost of a CTA's start and let loads run ahead; short ones fill the GPU when there is little to do.
-    auto fit = [&](int units) {
-        units *= WARPS;
-        while (units > WARPS && chunks_at(units) < MANY_CHUNKS) units /= 2;
-        return units;
-    };
-    plan->step_units[TSR_STATE_F32] = fit(STEP_F32_UNITS);
-    plan->step_units[TSR_STATE_Q8] = fit(STEP_Q8_UNITS);
-    plan->norm_units = fit(NORM_UNITS);
-    plan->copy_units = fit(COPY_UNITS);
-    plan->most_chunks = (size_t)(chunks_at(plan->step_units[TSR_STATE_F32]) + chunks_at(plan->norm_units) + chunks_at(plan->copy_units));
+    plan->step_units[TSR_STATE_F32] = fit(STEP_F32_UNITS, MANY_CHUNKS);
+    plan->step_units[TSR_STATE_Q8] = fit(STEP_Q8_UNITS, MANY_CHUNKS);
+    plan->norm_units = fit(NORM_UNITS, MANY_CHUNKS);
+    plan->copy_units = fit(COPY_UNITS, 2 * MANY_CHUNKS);
+    for (const tsr_dense_desc &d : plan->descs) {   // room for a step and the norm on the path that takes the shortest chunks
+        const int least = WARPS * (d.rows > 1 && d.cols < UNIT ? ANY_UNITS : PAIRS_UNITS);
+        plan->most_chunks += (size_t)(tensor_chunks(d, std::min(plan->step_units[d.state == TSR_STATE_Q8], least)) +
+                                      tensor_chunks(d, std::min(plan->norm_units, least)) + tensor_chunks(d, plan->copy_units));
+    }
     plan->workspace_bytes = (size_t)(round_up((int64_t)(plan->descs.size() * sizeof(DenseRec)), 256) +
                                      round_up((int64_t)(plan->most_chunks * sizeof(DenseChunk)), 256) +
-                                     NORM_CTAS * (int64_t)sizeof(double) + 256);
+                                     NORM_CTAS * SMS * (int64_t)sizeof(double) + 256);
 }
 
 }  // namespace
