@@ -25,8 +25,9 @@ static_assert(UNIT == 32 * 8, "a lane holds eight elements of a unit");
 constexpr int WARPS = 8;                   // per CTA
 // Most units of a warp in one chunk, by what goes over it.  FP32 steps overlap by having many CTAs at a time and are faster
 // short (1B set: 4.81 ms with 2 units, 4.96 with 8); the others have work per CTA or load ahead (130M set, 8-bit step: 301 us
-// with 1 unit, 232 with 2, 213 with 8; 1B norm: 1164, 705, 440 and 406 with 16).  Without vectors nothing is loaded ahead
-// (two pitched 1B layers: 258 us with 4 units, 263 with 2), and chunks of narrow pitched matrices are slow ones.
+// with 1 unit, 232 with 2, 213 with 8; 1B norm: 1164, 705, 440 and 406 with 16).  Without vectors
+// short chunks balance better (40 M pitched elements, 8-bit step: 101 us with 4 units, 105 with 8), and those of narrow pitched
+// matrices are slow ones.
 constexpr int STEP_F32_UNITS = 2, STEP_Q8_UNITS = 8, COPY_UNITS = 16, NORM_UNITS = 16, PAIRS_UNITS = 4, ANY_UNITS = 1;
 // CTAs on an SM of the kernels, whose registers are bounded for it.
 constexpr int STEP_F32_CTAS = 4, STEP_Q8_CTAS = 3, COPY_CTAS = 5, NORM_CTAS = 4;
@@ -487,8 +488,41 @@ __device__ __forceinline__ void store_pairs(void *dst, bool both, int64_t base, 
     }
 }
 
+__device__ __forceinline__ float2 load_two(const float *x) { return *(const float2 *)x; }
+__device__ __forceinline__ float2 load_two(const bf16 *x)
+{
+    const uint32_t w = *(const uint32_t *)x;
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+
+// The lane's pairs of a unit that lies at u, its elements from number `left` on `gap` places further.  TWO: whole pairs where u
+// is aligned to them and nothing moves (the norm of a pitched gradient is 4 % faster with it, the FP32 step 2.5 % slower).
+template <bool TWO, typename T>
+__device__ __forceinline__ void load_run(const T *u, int left, int gap, int lane, float2 (&out)[4])
+{
+    if (TWO && left == UNIT && ((uintptr_t)u & (2 * sizeof(T) - 1)) == 0) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[j] = load_two(u + 2 * lane + 64 * j);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = 2 * lane + 64 * (j >> 1) + (j & 1);
+            at(out, j) = to_f32(u[i < left ? i : i + gap]);
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_run(T *u, int left, int gap, int lane, const float2 (&in)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const int i = 2 * lane + 64 * (j >> 1) + (j & 1);
+        from_f32(u[i < left ? i : i + gap], (j & 1) ? in[j >> 1].y : in[j >> 1].x);
+    }
+}
+
 // Pairs of a parameter, gradient or image (pitch ld).  row, col: where the unit starts (PLAIN, ROWS).
-template <int PATH, typename T>
+template <int PATH, bool TWO, typename T>
 __device__ __forceinline__ void load_matrix(const T *x, const DenseRec &t, int64_t ld, int64_t base, int64_t row, int64_t col, int lane, float2 (&out)[4])
 {
     if constexpr (PATH == PATH_ANY) {
@@ -502,13 +536,8 @@ __device__ __forceinline__ void load_matrix(const T *x, const DenseRec &t, int64
             w.next();
         }
     } else {
-        const T *u = PATH == PATH_PLAIN ? x + base : x + row * ld + col;
-        const int left = (int)min(t.cols - col, (int64_t)UNIT), gap = (int)(ld - t.cols);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = 2 * lane + 64 * (j >> 1) + (j & 1);
-            at(out, j) = to_f32(u[PATH == PATH_PLAIN || i < left ? i : i + gap]);
-        }
+        if constexpr (PATH == PATH_PLAIN) load_run<TWO>(x + base, UNIT, 0, lane, out);
+        else load_run<TWO>(x + row * ld + col, (int)min(t.cols - col, (int64_t)UNIT), (int)(ld - t.cols), lane, out);
     }
 }
 template <int PATH, typename T>
@@ -524,61 +553,55 @@ __device__ __forceinline__ void store_matrix(T *x, const DenseRec &t, int64_t ld
             w.next();
         }
     } else {
-        T *u = PATH == PATH_PLAIN ? x + base : x + row * ld + col;
-        const int left = (int)min(t.cols - col, (int64_t)UNIT), gap = (int)(ld - t.cols);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int i = 2 * lane + 64 * (j >> 1) + (j & 1);
-            from_f32(u[PATH == PATH_PLAIN || i < left ? i : i + gap], (j & 1) ? in[j >> 1].y : in[j >> 1].x);
-        }
+        if constexpr (PATH == PATH_PLAIN) store_run(x + base, UNIT, 0, lane, in);
+        else store_run(x + row * ld + col, (int)min(t.cols - col, (int64_t)UNIT), (int)(ld - t.cols), lane, in);
     }
 }
 
-template <int PATH, typename PT, typename GT, bool Q8, bool SR>
-__device__ __forceinline__ void step_pairs_unit(const DenseRec &t, int64_t base, int64_t row, int64_t col, int lane, float gs, const DenseStep &a, float lr,
-                                                float decay, UnitKeys key)
+struct Values { float2 p[4], g[4], m[4], v[4], scale; };   // a lane's eight elements in FP32, and the block's scales
+
+// The step of pairs from their values on; returns the block's new scales.
+template <int PATH, typename PT, bool Q8, bool SR>
+__device__ __forceinline__ float2 update_pairs(Values &x, const DenseRec &t, int64_t base, int64_t row, int64_t col, int lane, float gs, const DenseStep &a,
+                                               float lr, float decay, UnitKeys key)
 {
     constexpr bool WHOLE = PATH != PATH_ANY;
     const bool both = t.flags & REC_PAIR_STATE;
-    float2 p[4], g[4], m[4], v[4];
-    float2 scale = make_float2(0.f, 0.f);
-    if constexpr (Q8) scale = t.scale[base / UNIT];
-    load_pairs<Q8, WHOLE>(t.m, both, base, lane, t.n, m);
-    load_pairs<Q8, WHOLE>(t.v, both, base, lane, t.n, v);
-    load_matrix<PATH>((const PT *)t.p, t, t.ldp, base, row, col, lane, p);
-    load_matrix<PATH>((const GT *)t.g, t, t.ldg, base, row, col, lane, g);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) g[j] = mul2(g[j], pair(gs));
-    if constexpr (Q8) update_q8(p, g, m, v, scale, a, lr, decay);
-    else update_f32(p, g, m, v, a, lr, decay);
+    for (int j = 0; j < 4; ++j) x.g[j] = mul2(x.g[j], pair(gs));
+    if constexpr (Q8) update_q8(x.p, x.g, x.m, x.v, x.scale, a, lr, decay);
+    else update_f32(x.p, x.g, x.m, x.v, a, lr, decay);
     const PairsFrom where = {(uint32_t)(base >> 1) + lane};
     if constexpr (SR && sizeof(PT) == 2) {
         Eight<bf16> rounded;
-        rounded.r = round_params(p, key, where);
-        rounded.get(p);
+        rounded.r = round_params(x.p, key, where);
+        rounded.get(x.p);
     }
-    store_matrix<PATH>((PT *)t.p, t, t.ldp, base, row, col, lane, p);
-    if (sizeof(PT) == 4 && t.image) store_matrix<PATH>(t.image, t, t.ldi, base, row, col, lane, p);
+    store_matrix<PATH>((PT *)t.p, t, t.ldp, base, row, col, lane, x.p);
+    if (sizeof(PT) == 4 && t.image) store_matrix<PATH>(t.image, t, t.ldi, base, row, col, lane, x.p);
+    float2 scale = make_float2(0.f, 0.f);
     if constexpr (Q8) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (!WHOLE && pair_at(base, lane, j >> 1) + (j & 1) >= t.n) at(m, j) = at(v, j) = 0.f;   // (0 * NaN of a poisoned block)
+            if (!WHOLE && pair_at(base, lane, j >> 1) + (j & 1) >= t.n) at(x.m, j) = at(x.v, j) = 0.f;   // (0 * NaN of a poisoned block)
         uint2 cm, cr;
-        const float2 s = quantise<SR>(m, v, key, where, cm, cr);
-        if (lane == 0) t.scale[base / UNIT] = s;
+        scale = quantise<SR>(x.m, x.v, key, where, cm, cr);
         store_code_pairs<WHOLE>(t.m, both, base, lane, t.n, cm);
         store_code_pairs<WHOLE>(t.v, both, base, lane, t.n, cr);
     } else {
-        store_pairs<WHOLE>(t.m, both, base, lane, t.n, m);
-        store_pairs<WHOLE>(t.v, both, base, lane, t.n, v);
+        store_pairs<WHOLE>(t.m, both, base, lane, t.n, x.m);
+        store_pairs<WHOLE>(t.v, both, base, lane, t.n, x.v);
     }
+    return scale;
 }
 
-// The units of a warp on the paths without vectors.
+// The units of a warp on the paths without vectors, loaded straight from memory.
 template <int PATH, typename PT, typename GT, bool Q8, bool SR>
 __device__ __forceinline__ void step_pairs(const DenseRec &t, int64_t base, int todo, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key)
 {
     constexpr int64_t STRIDE = WARPS * UNIT;
+    constexpr bool WHOLE = PATH != PATH_ANY;
+    const bool both = t.flags & REC_PAIR_STATE;
     int64_t row = 0, col = 0;
     if constexpr (PATH == PATH_ROWS) {
         row = base / t.cols;
@@ -586,7 +609,14 @@ __device__ __forceinline__ void step_pairs(const DenseRec &t, int64_t base, int 
     }
 #pragma unroll 1
     for (; todo > 0; --todo, base += STRIDE) {
-        step_pairs_unit<PATH, PT, GT, Q8, SR>(t, base, row, col, lane, gs, a, lr, decay, key);
+        Values x;
+        if constexpr (Q8) x.scale = t.scale[base / UNIT];
+        load_pairs<Q8, WHOLE>(t.m, both, base, lane, t.n, x.m);
+        load_pairs<Q8, WHOLE>(t.v, both, base, lane, t.n, x.v);
+        load_matrix<PATH, false>((const PT *)t.p, t, t.ldp, base, row, col, lane, x.p);
+        load_matrix<PATH, false>((const GT *)t.g, t, t.ldg, base, row, col, lane, x.g);
+        const float2 s = update_pairs<PATH, PT, Q8, SR>(x, t, base, row, col, lane, gs, a, lr, decay, key);
+        if (Q8 && lane == 0) t.scale[base / UNIT] = s;
         if constexpr (PATH == PATH_ROWS)
             for (col += STRIDE; col >= t.cols; col -= t.cols) ++row;
     }
@@ -600,8 +630,6 @@ template <typename PT, typename GT, bool Q8> struct RawUnit {
     Eight<float> m, v;
     float2 scale;
 };
-
-struct Values { float2 p[4], g[4], m[4], v[4], scale; };   // the same in FP32
 
 template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers to the lane's elements of a unit
     PT *p;
@@ -683,10 +711,13 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
 // The 8-bit form reads so little per unit that a unit's loads in registers do not keep HBM busy.  So a warp's loads go to
 // slots of shared memory that only its warp reads (asynchronous copies of 16 and 8 bytes, no barrier between warps): DEPTH
 // slots, DEPTH - 1 of them on their way.
-template <typename PT, typename GT> struct Ring {
+template <typename PT, typename GT, bool MIXED> struct Ring {
     static constexpr int P_VECS = sizeof(PT) / 2, G_VECS = sizeof(GT) / 2;   // 16-byte vectors of a lane
     static constexpr int THREADS = WARPS * 32;
-    static constexpr int SLOT = THREADS * (16 * (P_VECS + G_VECS) + 16) + WARPS * 8;
+    // a warp's parameters, gradients (MIXED: with room for two beginnings and ends off 16 bytes), codes of m and r, scales
+    static constexpr int P_WARP = 512 * P_VECS + (MIXED ? 48 : 0), G_WARP = 512 * G_VECS + (MIXED ? 48 : 0);
+    static constexpr int G_AT = WARPS * P_WARP, M_AT = G_AT + WARPS * G_WARP, V_AT = M_AT + THREADS * 8, S_AT = V_AT + THREADS * 8;
+    static constexpr int SLOT = S_AT + WARPS * 8;
     static constexpr int DEPTH = P_VECS + G_VECS == 2 ? 5 : P_VECS + G_VECS == 3 ? 4 : 3;   // three CTAs on an SM
     static constexpr int BYTES = DEPTH * SLOT;
 
@@ -696,46 +727,307 @@ template <typename PT, typename GT> struct Ring {
     static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 2) : "memory"); }
 
     // Fills slot `to` (a shared-memory address) with the unit that is `units` units of this warp after u.
-    static __device__ __forceinline__ void issue(uint32_t to, const VectorUnit<PT, GT, true> &u, int units, int lane)
+    static __device__ __forceinline__ void issue(uint32_t to, const VectorUnit<PT, GT, true> &u, int units, int warp, int lane)
     {
         const int off = units * WARPS * UNIT;
-        const uint32_t t8 = to + THREADS * 16 * (P_VECS + G_VECS) + threadIdx.x * 8;
-        put(to, u.p + off, lane);
-        put(to + P_VECS * THREADS * 16, u.g + off, lane);
-        copy8(t8, u.m + off);
-        copy8(t8 + THREADS * 8, u.v + off);
-        if (lane == 0) copy8(to + THREADS * (16 * (P_VECS + G_VECS) + 16) + (threadIdx.x >> 5) * 8, u.scale + off / UNIT);
+        put(to + warp * P_WARP, u.p + off, lane);
+        put(to + G_AT + warp * G_WARP, u.g + off, lane);
+        issue_state(to, u.m + off, u.v + off, u.scale + off / UNIT, warp, lane);
     }
-    static __device__ __forceinline__ void fetch(const char *slot, int lane, RawUnit<PT, GT, true> &r)
+    // m, v: the lane's eight codes
+    static __device__ __forceinline__ void issue_state(uint32_t to, const void *m, const void *v, const float2 *scale, int warp, int lane)
     {
-        const char *s8 = slot + THREADS * 16 * (P_VECS + G_VECS) + threadIdx.x * 8;
-        get(slot, lane, r.p);
-        get(slot + P_VECS * THREADS * 16, lane, r.g);
-        r.cm = *(const uint2 *)s8;
-        r.cr = *(const uint2 *)(s8 + THREADS * 8);
-        r.scale = *(const float2 *)(slot + THREADS * (16 * (P_VECS + G_VECS) + 16) + (threadIdx.x >> 5) * 8);
+        copy8(to + M_AT + (warp * 32 + lane) * 8, m);
+        copy8(to + V_AT + (warp * 32 + lane) * 8, v);
+        if (lane == 0) copy8(to + S_AT + warp * 8, scale);
+    }
+    static __device__ __forceinline__ void fetch(const char *slot, int warp, int lane, RawUnit<PT, GT, true> &r)
+    {
+        get(slot + warp * P_WARP, lane, r.p);
+        get(slot + G_AT + warp * G_WARP, lane, r.g);
+        r.cm = *(const uint2 *)(slot + M_AT + (warp * 32 + lane) * 8);
+        r.cr = *(const uint2 *)(slot + V_AT + (warp * 32 + lane) * 8);
+        r.scale = *(const float2 *)(slot + S_AT + warp * 8);
     }
     // A warp's 256 BF16 elements: a vector of 16 bytes for each lane.
-    static __device__ __forceinline__ void put(uint32_t to, const bf16 *x, int lane) { copy16(to + threadIdx.x * 16, x); }
-    static __device__ __forceinline__ void get(const char *s, int lane, Eight<bf16> &x) { x.r = *(const uint4 *)(s + threadIdx.x * 16); }
+    static __device__ __forceinline__ void put(uint32_t to, const bf16 *x, int lane) { copy16(to + lane * 16, x); }
+    static __device__ __forceinline__ void get(const char *s, int lane, Eight<bf16> &x) { x.r = *(const uint4 *)(s + lane * 16); }
     // 256 FP32 elements, 64 vectors: copied in order (lanes 16 bytes apart, so that whole sectors travel), read two by two.  Vector
     // c lies at place c ^ bit 3 of c, which keeps the reads, 32 bytes apart, free of bank conflicts.
     static __device__ __forceinline__ void put(uint32_t to, const float *x, int lane)
     {
-        to += (threadIdx.x >> 5) * 1024 + (lane ^ ((lane >> 3) & 1)) * 16;
+        to += (lane ^ ((lane >> 3) & 1)) * 16;
         copy16(to, (const char *)x - lane * 16);
         copy16(to + 512, (const char *)x - lane * 16 + 512);
     }
     static __device__ __forceinline__ void get(const char *s, int lane, Eight<float> &x)
     {
-        s += (threadIdx.x >> 5) * 1024;
         const int bit = (lane >> 2) & 1;
         const uint4 a = *(const uint4 *)(s + ((2 * lane) ^ bit) * 16), b = *(const uint4 *)(s + ((2 * lane + 1) ^ bit) * 16);
         x.r = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     }
 };
 
-template <typename PT> __host__ __device__ constexpr bool uses_ring(bool q8, bool sr) { return q8 && (!sr || sizeof(PT) == 4); }
+// A unit of any alignment travels as the 16-byte vectors that hold it, the first and last with neighbouring bytes that are not
+// looked at.  Every vector holds an element of the unit, so it lies in the same allocation granule.
+// 2 N words of shared memory from s + off on, off < 16 a multiple of 2, s a multiple of 8 bytes: aligned words, moved by one if
+// need be and, for an odd number of BF16 elements, by half a word.
+template <int N>
+__device__ __forceinline__ void read_shifted(const char *s, int off, uint32_t (&w)[2 * N])
+{
+    uint32_t x[2 * N + 2];
+#pragma unroll
+    for (int k = 0; k <= N; ++k) {
+        const uint2 d = *(const uint2 *)(s + (off & 8) + 8 * k);
+        x[2 * k] = d.x;
+        x[2 * k + 1] = d.y;
+    }
+    if (off & 4) {
+#pragma unroll
+        for (int k = 0; k <= 2 * N; ++k) x[k] = x[k + 1];
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * N; ++k) w[k] = N == 2 ? __funnelshift_r(x[k], x[k + 1], (off & 2) * 8) : x[k];
+}
+__device__ __forceinline__ void shifted(const char *s, int off, int lane, Eight<bf16> &x)
+{
+    uint32_t w[4];
+    read_shifted<2>(s + lane * 16, off, w);
+    x.r = make_uint4(w[0], w[1], w[2], w[3]);
+}
+__device__ __forceinline__ void shifted(const char *s, int off, int lane, Eight<float> &x) { read_shifted<4>(s + lane * 32, off, x.r.w); }
+
+// A warp's 256 elements, eight to a lane (words w), to an address of any alignment: through shared memory (the warp's own
+// `room`, 48 bytes more than they take), so that all but the elements off the 16-byte grid leave in vectors.
+template <typename T>
+__device__ __forceinline__ void store_shifted(T *to, char *room, int lane, const uint32_t (&w)[2 * (int)sizeof(T)])
+{
+    constexpr int ES = sizeof(T), PER = 16 / ES;   // elements of a vector
+    const int off = (int)((uintptr_t)to & 15);
+    if (off == 0) {
+#pragma unroll
+        for (int k = 0; k < ES / 2; ++k) ((uint4 *)to)[lane * (ES / 2) + k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+        return;
+    }
+    __syncwarp();   // what was here has been read
+#pragma unroll
+    for (int k = 0; k < ES / 2; ++k) ((uint4 *)room)[lane * (ES / 2) + k] = make_uint4(w[4 * k], w[4 * k + 1], w[4 * k + 2], w[4 * k + 3]);
+    __syncwarp();
+    uint32_t x[2 * ES];
+    read_shifted<ES>(room + lane * 8 * ES, 16 - off, x);
+    uint4 *v = (uint4 *)((char *)to - off) + 1 + lane * (ES / 2);
+#pragma unroll
+    for (int k = 0; k < ES / 2; ++k)
+        if (lane < 31 || k < ES / 2 - 1) v[k] = make_uint4(x[4 * k], x[4 * k + 1], x[4 * k + 2], x[4 * k + 3]);
+    if (lane < PER) {   // the first PER - off / ES elements and the last off / ES
+        const int i = lane < PER - off / ES ? lane : UNIT - PER + lane;
+        to[i] = ((const T *)room)[i];
+    }
+}
+
+// What the ring's units without vectors share: from a filled slot to the stores.  to: the unit's parameters in memory (one run);
+// g_off: bytes by which its gradients are off the 16-byte grid; m, v: the lane's eight codes.  `next` starts the next loads.
+template <typename PT, typename GT, bool SR, typename Next>
+__device__ __forceinline__ float2 step_shifted(char *slot, PT *to, bf16 *image, int g_off, char *m, char *v, uint32_t half, int warp, int lane, float gs,
+                                               const DenseStep &a, float lr, float decay, UnitKeys key, Next next)
+{
+    typedef Ring<PT, GT, true> R;
+    char *room = slot + warp * R::P_WARP;
+    RawUnit<PT, GT, true> raw;
+    shifted(room, (int)((uintptr_t)to & 15), lane, raw.p);
+    shifted(slot + R::G_AT + warp * R::G_WARP, g_off, lane, raw.g);
+    raw.cm = *(const uint2 *)(slot + R::M_AT + (warp * 32 + lane) * 8);
+    raw.cr = *(const uint2 *)(slot + R::V_AT + (warp * 32 + lane) * 8);
+    Values x;
+    x.scale = *(const float2 *)(slot + R::S_AT + warp * 8);
+    raw.p.get(x.p);
+    raw.g.get(x.g);
+    e4m3_unpack(raw.cm, x.m);
+    e4m3_unpack(raw.cr, x.v);
+    next();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x.g[j] = mul2(x.g[j], pair(gs));
+    update_q8(x.p, x.g, x.m, x.v, x.scale, a, lr, decay);
+    const EightFrom where = {half};
+    if constexpr (sizeof(PT) == 2) {
+        uint4 w;
+        if constexpr (SR) w = round_params(x.p, key, where);
+        else w = bf16_pack(x.p);
+        store_shifted(to, room, lane, {w.x, w.y, w.z, w.w});
+    } else {
+        store_shifted(to, room, lane, {__float_as_uint(x.p[0].x), __float_as_uint(x.p[0].y), __float_as_uint(x.p[1].x), __float_as_uint(x.p[1].y),
+                                       __float_as_uint(x.p[2].x), __float_as_uint(x.p[2].y), __float_as_uint(x.p[3].x), __float_as_uint(x.p[3].y)});
+        if (image) {
+            const uint4 w = bf16_pack(x.p);
+            store_shifted(image, room, lane, {w.x, w.y, w.z, w.w});
+        }
+    }
+    uint2 cm, cr;
+    const float2 scale = quantise<SR>(x.m, x.v, key, where, cm, cr);
+    *(uint2 *)m = cm;
+    *(uint2 *)v = cr;
+    return scale;
+}
+
+// The 8-bit step of a warp's units of a contiguous tensor off the 16-byte grid.
+template <typename PT, typename GT, bool SR>
+__device__ __forceinline__ void step_plain(const DenseRec &t, int64_t base, int todo, int warp, int lane, float gs, const DenseStep &a, float lr, float decay,
+                                           UnitKeys key, char *slots)
+{
+    typedef Ring<PT, GT, true> R;
+    constexpr int STRIDE = WARPS * UNIT;
+    const int p_off = (int)((uintptr_t)((const PT *)t.p + base) & 15), g_off = (int)((uintptr_t)((const GT *)t.g + base) & 15);   // of every unit
+    char *p = (char *)((PT *)t.p + base) - p_off + lane * 16;              // the lane's vector
+    const char *g = (const char *)((const GT *)t.g + base) - g_off + lane * 16;
+    char *m = (char *)t.m + base + lane * 8, *v = (char *)t.v + base + lane * 8;
+    float2 *scale = t.scale + base / UNIT;
+    bf16 *image = t.image ? t.image + base : nullptr;
+    uint32_t half = (uint32_t)(base >> 1) + lane * 4;
+    const uint32_t first = (uint32_t)__cvta_generic_to_shared(slots);
+    auto issue = [&](uint32_t to, int units) {
+        const int off = units * STRIDE;
+        const uint32_t to_p = to + warp * R::P_WARP + lane * 16, to_g = to + R::G_AT + warp * R::G_WARP + lane * 16;
+#pragma unroll
+        for (int k = 0; k < R::P_VECS; ++k) R::copy16(to_p + 512 * k, p + off * (int)sizeof(PT) + 512 * k);
+#pragma unroll
+        for (int k = 0; k < R::G_VECS; ++k) R::copy16(to_g + 512 * k, g + off * (int)sizeof(GT) + 512 * k);
+        if (lane == 0) {   // the vector of the last elements
+            if (p_off) R::copy16(to_p + 512 * R::P_VECS, p + off * (int)sizeof(PT) + 512 * R::P_VECS);
+            if (g_off) R::copy16(to_g + 512 * R::G_VECS, g + off * (int)sizeof(GT) + 512 * R::G_VECS);
+        }
+        R::issue_state(to, m + off, v + off, scale + off / UNIT, warp, lane);
+    };
+#pragma unroll
+    for (int k = 0; k < R::DEPTH - 1; ++k) {
+        if (k < todo) issue(first + k * R::SLOT, k);
+        R::commit();
+    }
+    int in = (R::DEPTH - 1) * R::SLOT, out = 0;
+#pragma unroll 1
+    for (; todo > 0; --todo) {
+        R::wait();
+        __syncwarp();   // other lanes' copies; and every lane has read the slot that is filled next
+        const float2 s = step_shifted<PT, GT, SR>(slots + out, (PT *)(p - lane * 16 + p_off), image, g_off, m, v, half, warp, lane, gs, a, lr, decay, key, [&]() {
+            if (todo >= R::DEPTH) issue(first + in, R::DEPTH - 1);
+            R::commit();
+        });
+        if (lane == 0) *scale = s;
+        in = in + R::SLOT == R::BYTES ? 0 : in + R::SLOT;
+        out = out + R::SLOT == R::BYTES ? 0 : out + R::SLOT;
+        p += STRIDE * sizeof(PT);
+        g += STRIDE * sizeof(GT);
+        m += STRIDE;
+        v += STRIDE;
+        scale += STRIDE / UNIT;
+        if (image) image += STRIDE;
+        half += STRIDE / 2;
+    }
+}
+
+// A unit of a matrix with a row pitch: one run of elements, or two where a row ends (the second from the start of the next
+// row, its vectors behind the first's).
+template <typename T> struct Runs {
+    const char *one, *two;   // vectors
+    int left;                // elements of the first run
+    int skip, gap;           // the first element's place in its vector, and the step from the first run's end to the second run
+    int vectors_one, vectors;
+
+    __device__ __forceinline__ Runs(const T *x, int ld, int cols, int row, int col)
+    {
+        constexpr int ES = sizeof(T);
+        const uintptr_t a = (uintptr_t)(x + (int64_t)row * ld + col);
+        left = min(cols - col, UNIT);
+        skip = (int)(a & 15) / ES;
+        one = (const char *)(a & ~(uintptr_t)15);
+        vectors = vectors_one = ((skip + left) * ES + 15) / 16;
+        two = one;
+        gap = 0;
+        if (left < UNIT) {
+            const uintptr_t b = (uintptr_t)(x + (int64_t)(row + 1) * ld);
+            const int skip_two = (int)(b & 15) / ES;
+            two = (const char *)(b & ~(uintptr_t)15) - 16 * vectors_one;
+            vectors += ((skip_two + UNIT - left) * ES + 15) / 16;
+            gap = 16 / ES * vectors_one + skip_two - skip - left;
+        }
+    }
+    __device__ __forceinline__ void copy(uint32_t to, int lane) const
+    {
+        constexpr int MOST = 16 * (int)sizeof(T);   // and up to three more
+#pragma unroll
+        for (int k = lane; k < MOST; k += 32)
+            if (k < vectors) Ring<T, T, true>::copy16(to + k * 16, (k < vectors_one ? one : two) + k * 16);
+        if (MOST + lane < vectors) Ring<T, T, true>::copy16(to + (MOST + lane) * 16, (MOST + lane < vectors_one ? one : two) + (MOST + lane) * 16);
+    }
+    __device__ __forceinline__ void read(const char *slot, int lane, float2 (&out)[4]) const { load_run<false>((const T *)slot + skip, left, gap, lane, out); }
+};
+
+// The 8-bit step of a warp's units of a matrix with long rows and a pitch.  A unit in one run goes on shifted to its alignment,
+// one with the end of a row in pairs 64 apart.
+template <typename PT, typename GT, bool SR>
+__device__ __forceinline__ void step_rows(const DenseRec &t, int64_t base, int todo, int warp, int lane, float gs, const DenseStep &a, float lr, float decay,
+                                          UnitKeys key, char *slots)
+{
+    typedef Ring<PT, GT, true> R;
+    constexpr int STRIDE = WARPS * UNIT;
+    const int cols = (int)t.cols, ldp = (int)t.ldp, ldg = (int)t.ldg;
+    PT *const P = (PT *)t.p;
+    const GT *const G = (const GT *)t.g;
+    char *m = (char *)t.m + base + lane * 8, *v = (char *)t.v + base + lane * 8;
+    float2 *scale = t.scale + base / UNIT;
+    uint32_t half = (uint32_t)(base >> 1) + lane * 4;
+    int row = (int)(base / t.cols), col = (int)(base - (int64_t)row * cols), in_row = row, in_col = col;
+    const uint32_t first = (uint32_t)__cvta_generic_to_shared(slots);
+    auto issue = [&](uint32_t to, int units) {
+        Runs<PT>(P, ldp, cols, in_row, in_col).copy(to + warp * R::P_WARP, lane);
+        Runs<GT>(G, ldg, cols, in_row, in_col).copy(to + R::G_AT + warp * R::G_WARP, lane);
+        R::issue_state(to, m + units * STRIDE, v + units * STRIDE, scale + units * (STRIDE / UNIT), warp, lane);
+        for (in_col += STRIDE; in_col >= cols; in_col -= cols) ++in_row;
+    };
+#pragma unroll 1
+    for (int k = 0; k < R::DEPTH - 1; ++k) {
+        if (k < todo) issue(first + k * R::SLOT, k);
+        R::commit();
+    }
+    int in = (R::DEPTH - 1) * R::SLOT, out = 0;
+#pragma unroll 1
+    for (; todo > 0; --todo) {
+        R::wait();
+        __syncwarp();   // other lanes' copies; and every lane has read the slot that is filled next
+        char *slot = slots + out;
+        auto next = [&]() {
+            if (todo >= R::DEPTH) issue(first + in, R::DEPTH - 1);
+            R::commit();
+        };
+        float2 s;
+        if (cols - col >= UNIT) {
+            bf16 *image = sizeof(PT) == 4 && t.image ? t.image + (int64_t)row * t.ldi + col : nullptr;
+            s = step_shifted<PT, GT, SR>(slot, P + (int64_t)row * ldp + col, image, (int)((uintptr_t)(G + (int64_t)row * ldg + col) & 15), m, v, half, warp, lane, gs, a,
+                                         lr, decay, key, next);
+        } else {
+            Values x;
+            Runs<PT>(P, ldp, cols, row, col).read(slot + warp * R::P_WARP, lane, x.p);
+            Runs<GT>(G, ldg, cols, row, col).read(slot + R::G_AT + warp * R::G_WARP, lane, x.g);
+            load_pairs<true, true>(slot + R::M_AT + warp * UNIT, true, 0, lane, 0, x.m);
+            load_pairs<true, true>(slot + R::V_AT + warp * UNIT, true, 0, lane, 0, x.v);
+            x.scale = *(const float2 *)(slot + R::S_AT + warp * 8);
+            next();
+            s = update_pairs<PATH_ROWS, PT, true, SR>(x, t, (int64_t)row * cols + col, row, col, lane, gs, a, lr, decay, key);
+        }
+        if (lane == 0) *scale = s;
+        in = in + R::SLOT == R::BYTES ? 0 : in + R::SLOT;
+        out = out + R::SLOT == R::BYTES ? 0 : out + R::SLOT;
+        m += STRIDE;
+        v += STRIDE;
+        scale += STRIDE / UNIT;
+        half += STRIDE / 2;
+        for (col += STRIDE; col >= cols; col -= cols) ++row;
+    }
+}
+
+// Which kernels load vectors through the ring (stochastic rounding of BF16 parameters is bound by instructions, and faster with
+// the next unit in registers: 1B set 2.45 against 2.51 ms), and which have one at all.
+template <typename PT> __host__ __device__ constexpr bool vectors_in_ring(bool q8, bool sr) { return q8 && (!sr || sizeof(PT) == 4); }
+template <typename PT> __host__ __device__ constexpr bool has_ring(bool q8, bool sr, bool mixed) { return q8 && (mixed || vectors_in_ring<PT>(q8, sr)); }
 
 // MIXED: there are chunks of every path.  Where all chunks are vectors, a kernel without the other paths is launched: their
 // registers cost the FP32 form 1.5 % (1B set: 4.88 against 4.81 ms).
@@ -743,6 +1035,7 @@ template <typename PT, typename GT, bool Q8, bool SR, bool MIXED>
 __global__ void __launch_bounds__(WARPS * 32, Q8 ? STEP_Q8_CTAS : STEP_F32_CTAS)
 dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restrict__ chunks, const DenseStep a)
 {
+    extern __shared__ __align__(16) char slots[];   // of the ring
     pdl_trigger();
     const DenseChunk ch = chunks[blockIdx.x];
     const DenseRec &t = recs[ch.rec];
@@ -761,7 +1054,7 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
         if (!isfinite(gs)) return;
     }
     constexpr int64_t STRIDE = WARPS * UNIT;
-    constexpr bool RING = uses_ring<PT>(Q8, SR);
+    constexpr bool RING = vectors_in_ring<PT>(Q8, SR);
     int64_t base = ((int64_t)ch.first + warp) * UNIT;
     int todo = (ch.units - warp + WARPS - 1) / WARPS;   // units of this warp
     if (todo <= 0) return;
@@ -771,21 +1064,20 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
         RawUnit<PT, GT, Q8> raw;
         Values x;
         if constexpr (RING) {
-            typedef Ring<PT, GT> R;
-            extern __shared__ __align__(16) char slots[];
+            typedef Ring<PT, GT, MIXED> R;
             const uint32_t first = (uint32_t)__cvta_generic_to_shared(slots);
             int in = (R::DEPTH - 1) * R::SLOT, out = 0;   // byte offsets of the slots to fill and to read
 #pragma unroll
             for (int k = 0; k < R::DEPTH - 1; ++k) {
-                if (k < todo) R::issue(first + k * R::SLOT, u, k, lane);
+                if (k < todo) R::issue(first + k * R::SLOT, u, k, warp, lane);
                 R::commit();
             }
 #pragma unroll 1
             for (; todo > 0; --todo) {
                 R::wait();
                 __syncwarp();   // other lanes' copies; and every lane has read the slot that is filled next
-                R::fetch(slots + out, lane, raw);
-                if (todo >= R::DEPTH) R::issue(first + in, u, R::DEPTH - 1, lane);
+                R::fetch(slots + out, warp, lane, raw);
+                if (todo >= R::DEPTH) R::issue(first + in, u, R::DEPTH - 1, warp, lane);
                 R::commit();
                 in = in + R::SLOT == R::BYTES ? 0 : in + R::SLOT;
                 out = out + R::SLOT == R::BYTES ? 0 : out + R::SLOT;
@@ -815,9 +1107,11 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
             }
         }
     } else if (ch.path == PATH_PLAIN) {
-        step_pairs<PATH_PLAIN, PT, GT, Q8, SR>(t, base, todo, lane, gs, a, lr, decay, key);
+        if constexpr (Q8) step_plain<PT, GT, SR>(t, base, todo, warp, lane, gs, a, lr, decay, key, slots);
+        else step_pairs<PATH_PLAIN, PT, GT, Q8, SR>(t, base, todo, lane, gs, a, lr, decay, key);
     } else if (ch.path == PATH_ROWS) {
-        step_pairs<PATH_ROWS, PT, GT, Q8, SR>(t, base, todo, lane, gs, a, lr, decay, key);
+        if constexpr (Q8) step_rows<PT, GT, SR>(t, base, todo, warp, lane, gs, a, lr, decay, key, slots);
+        else step_pairs<PATH_ROWS, PT, GT, Q8, SR>(t, base, todo, lane, gs, a, lr, decay, key);
     } else {
         step_pairs<PATH_ANY, PT, GT, Q8, SR>(t, base, todo, lane, gs, a, lr, decay, key);
     }
@@ -867,7 +1161,7 @@ __device__ __forceinline__ double pairs_squares(const DenseRec &t, int64_t base,
 #pragma unroll 4
     for (; todo > 0; --todo, base += STRIDE) {
         float2 g[4];
-        load_matrix<PATH>((const GT *)t.g, t, t.ldg, base, row, col, lane, g);
+        load_matrix<PATH, true>((const GT *)t.g, t, t.ldg, base, row, col, lane, g);
         sum += square_sum(g);
         if constexpr (PATH == PATH_ROWS)
             for (col += STRIDE; col >= t.cols; col -= t.cols) ++row;
@@ -1079,7 +1373,7 @@ int key_of(const tsr_dense_desc &d)
 template <typename PT, typename GT, bool Q8, bool SR>
 cudaError_t step_launch_as(bool mixed, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
 {
-    const int smem = uses_ring<PT>(Q8, SR) ? Ring<PT, GT>::BYTES : 0;
+    const int smem = !has_ring<PT>(Q8, SR, mixed) ? 0 : mixed ? Ring<PT, GT, true>::BYTES : Ring<PT, GT, false>::BYTES;
     return mixed ? launch_dependent(dense_step_kernel<PT, GT, Q8, SR, true>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a)
                  : launch_dependent(dense_step_kernel<PT, GT, Q8, SR, false>, dim3(count), dim3(WARPS * 32), smem, s, 1, recs, chunks, a);
 }
@@ -1104,12 +1398,18 @@ cudaError_t step_launch(int key, bool sr, bool mixed, const DenseRec *recs, cons
     }
 }
 
-template <typename PT, typename GT, bool SR> cudaError_t step_configure()   // shared memory of the kernels with a ring
+template <typename PT, typename GT, bool SR> cudaError_t step_configure_as()
 {
-    if (!uses_ring<PT>(true, SR)) return cudaSuccess;
-    cudaError_t e = cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, SR, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
+    cudaError_t e = cudaSuccess;
+    if (has_ring<PT>(true, SR, false))
+        e = cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, SR, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT, false>::BYTES);
     if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, SR, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT>::BYTES);
+    return cudaFuncSetAttribute(dense_step_kernel<PT, GT, true, SR, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, Ring<PT, GT, true>::BYTES);
+}
+template <typename PT, typename GT> cudaError_t step_configure()   // shared memory of the kernels with a ring
+{
+    const cudaError_t e = step_configure_as<PT, GT, false>();
+    return e != cudaSuccess ? e : step_configure_as<PT, GT, true>();
 }
 
 tsr_status dense_ready(const tsr_dense_plan *plan)
@@ -1128,7 +1428,7 @@ int64_t size_of(int32_t dtype) { return dtype == TSR_BF16 ? 2 : 4; }
 DensePath path_of(bool contiguous, bool vectors, const tsr_dense_desc &d, int64_t ld)
 {
     if (contiguous) return vectors ? PATH_VECTORS : PATH_PLAIN;
-    return d.cols >= UNIT && ld - d.cols < (1 << 30) ? PATH_ROWS : PATH_ANY;
+    return d.cols >= UNIT && ld < (1 << 30) && d.rows < (1 << 30) ? PATH_ROWS : PATH_ANY;   // (32-bit rows and columns)
 }
 
 tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *workspace)
@@ -1177,6 +1477,7 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
             dense = dense && (d.rows <= 1 || (d.ldp == d.cols && (!p.image || d.ldi == d.cols)));
             path[i] = path_of(dense, grad_path[i] == PATH_VECTORS && (r.flags & REC_VEC_STATE) && aligned(p.param, 8 * ps) && aligned(p.image, 16), d,
                               std::max(std::max(d.ldp, d.ldg), p.image ? d.ldi : 0));
+            if (q8 && !(r.flags & REC_VEC_STATE)) path[i] = PATH_ANY;   // the ring takes codes eight by eight
         }
         if (!dense) r.flags |= REC_PITCHED;
     }
@@ -1208,12 +1509,10 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return dense_fail(plan, TSR_ERR_CUDA, "no CUDA device available");
     DENSE_CUDA(plan, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
-    DENSE_CUDA(plan, (step_configure<float, float, false>()));
-    DENSE_CUDA(plan, (step_configure<float, float, true>()));
-    DENSE_CUDA(plan, (step_configure<float, bf16, false>()));
-    DENSE_CUDA(plan, (step_configure<float, bf16, true>()));
-    DENSE_CUDA(plan, (step_configure<bf16, float, false>()));
-    DENSE_CUDA(plan, (step_configure<bf16, bf16, false>()));
+    DENSE_CUDA(plan, (step_configure<float, float>()));
+    DENSE_CUDA(plan, (step_configure<bf16, float>()));
+    DENSE_CUDA(plan, (step_configure<float, bf16>()));
+    DENSE_CUDA(plan, (step_configure<bf16, bf16>()));
     plan->bound = false;
     DENSE_CUDA(plan, cudaDeviceSynchronize());   // nothing that still runs may see the tables change
     char *at = (char *)workspace;

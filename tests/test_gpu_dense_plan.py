@@ -459,6 +459,47 @@ def test_pitched_matrices_step_like_contiguous_ones(tsr, cols, ld):
                 assert torch.equal(u.view(torch.uint8), w.view(torch.uint8))
 
 
+@pytest.mark.parametrize("stochastic", [0, 1])
+@pytest.mark.parametrize("state", [torch.float32, F8])
+@pytest.mark.parametrize("pd,gd", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16")])
+def test_every_alignment_gives_the_same_bits(tsr, pd, gd, state, stochastic):
+    """Parameters, gradients and images at all distances from a 16-byte border, contiguous and with rows of many lengths,
+    against aligned contiguous copies; what lies before and behind a tensor and between its rows stays as it is."""
+    shapes = [(1, 3 * 2048 + 300), (9, 1000), (40, 257), (5, 256), (3, 4099), (30, 100)]
+    for rows, cols in shapes:
+        n = rows * cols
+        p0, g0 = rand((rows, cols), cols, 0.02).to(DT[pd]).cuda(), gradient(n, cols).view(rows, cols).to(DT[gd]).cuda()
+        ref = p0.clone()
+        image0 = torch.zeros(rows, cols, dtype=torch.bfloat16, device="cuda") if pd == "f32" else None
+        one = tsr.DensePlan([ref], [g0], state_dtype=state, images=[image0])
+        for t in (1, 2):
+            one.step(hyper(tsr, t)[0], rounding=stochastic, seed=t)
+        norm = float(one.grad_norm()[0])
+        for shift in range(9):
+            pitches = [cols] if rows == 1 else [cols, cols + 1 + shift % 5, cols + 3]
+            bufs, views = [], []
+            for k, (x, extra) in enumerate(((p0, 0), (g0, 1)) + (((image0, 2),) if image0 is not None else ())):
+                ld = pitches[(shift + k) % len(pitches)]
+                at = (shift * (k + 1) + k) % 9
+                buf = torch.full((at + rows * ld + 16,), 7.0, dtype=x.dtype, device="cuda")
+                view = torch.as_strided(buf, (rows, cols), (ld, 1), at)
+                view.copy_(x)
+                bufs.append(buf)
+                views.append(view)
+            plan = tsr.DensePlan([views[0]], [views[1]], state_dtype=state, images=[views[2]] if image0 is not None else None)
+            for t in (1, 2):
+                plan.step(hyper(tsr, t)[0], rounding=stochastic, seed=t)
+            assert torch.equal(views[0], ref) and (image0 is None or torch.equal(views[2], image0)), (rows, cols, shift)
+            assert torch.equal(views[1], g0)
+            for a, b in zip(plan.states[0], one.states[0]):
+                assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+            for buf, view in zip(bufs, views):
+                view.fill_(7.0)
+                assert (buf == 7.0).all()
+                view.copy_(g0 if view is views[1] else ref)
+            assert abs(float(plan.grad_norm()[0]) / norm - 1) <= 12 * U24
+
+
 def test_steps_are_ordered_on_their_stream_and_repeat_bit_for_bit(tsr):
     """norm -> step chains on a side stream, behind and before torch kernels, against the default stream."""
     def chain(stream):
