@@ -632,6 +632,25 @@ def test_states_convert_both_ways(tsr, shift):
         assert all(torch.equal(i, j) for i, j in zip(z, w))
 
 
+@pytest.mark.parametrize("shift", [0, 1, 2])
+def test_equal_forms_are_copied_as_they_are(tsr, shift):
+    """All 256 codes, NaN among them, NaN scales, and FP32 moments with NaN and infinities: byte for byte."""
+    for n in (1, 255, 1000, 5000):
+        def codes_of(k):
+            return (torch.arange(n + shift, device="cuda") * k).to(torch.uint8)[shift:].view(F8)
+        scale = torch.full(((n + 255) // 256, 2), 0.5, device="cuda")
+        scale[-1, 1] = math.nan
+        zeros = lambda: torch.zeros(n + 1, dtype=torch.uint8, device="cuda")[1:].view(F8)  # noqa: E731
+        a, b = tsr.DensePlan(None, None, states=[(codes_of(1), codes_of(7), scale)]), tsr.DensePlan(None, None, states=[(zeros(), zeros(), torch.zeros_like(scale))])
+        b.copy_state(a)
+        assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a.states[0], b.states[0]))
+        m, v = (rand(n + shift, k).cuda()[shift:] for k in (1, 2))
+        m[0], v[n // 2], v[-1] = math.nan, math.inf, -math.inf
+        a, b = (tsr.DensePlan(None, None, states=[s]) for s in ((m, v), (torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda"))))
+        b.copy_state(a)
+        assert all(torch.equal(x.contiguous().view(torch.int32), y.contiguous().view(torch.int32)) for x, y in zip(a.states[0], b.states[0]))
+
+
 def test_conversion_between_plans_that_step(tsr):
     """A run with FP32 states goes on with 8-bit ones: the first step afterwards starts from the converted moments."""
     ps, gs = [rand(n, n).cuda() for n in SIZES], [gradient(n, n).cuda() for n in SIZES]
