@@ -434,37 +434,48 @@ struct Walk {
 };
 __device__ __forceinline__ int64_t pair_at(int64_t base, int lane, int j) { return base + 2 * lane + 64 * j; }
 
-// Pairs of moments, as codes or FP32; elements from n on are zero, and not written (WHOLE: there are none).
+// Pairs of moments, as codes or FP32; elements from n on are zero, and not written (WHOLE: there are none).  Where there are,
+// every load is issued and the value dropped (the tensor's first element stands in): a load under a condition would be waited
+// for before the next, a memory latency each.
 template <bool WHOLE>
 __device__ __forceinline__ uint2 load_code_pairs(const void *src, bool both, int64_t base, int lane, int64_t n)
 {
+    const uint8_t *c = (const uint8_t *)src;
     uint32_t two[4];
+    if (WHOLE && both) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t e = pair_at(base, lane, j);
-        const uint8_t *c = (const uint8_t *)src + e;
-        two[j] = 0;
-        if (both && (WHOLE || e + 1 < n)) two[j] = *(const uint16_t *)c;
-        else {
-            if (WHOLE || e < n) two[j] = c[0];
-            if (WHOLE || e + 1 < n) two[j] |= (uint32_t)c[1] << 8;
+        for (int j = 0; j < 4; ++j) two[j] = *(const uint16_t *)(c + pair_at(base, lane, j));
+    } else {
+        uint32_t one[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t e = pair_at(base, lane, j >> 1) + (j & 1);
+            one[j] = c[WHOLE || e < n ? e : 0];
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (!WHOLE && pair_at(base, lane, j >> 1) + (j & 1) >= n) one[j] = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) two[j] = one[2 * j] | (one[2 * j + 1] << 8);
     }
     return make_uint2(two[0] | (two[1] << 16), two[2] | (two[3] << 16));
 }
 template <bool WHOLE>
 __device__ __forceinline__ void load_pairs(const void *src, bool both, int64_t base, int lane, int64_t n, float2 (&x)[4])
 {
+    const float *f = (const float *)src;
+    if (WHOLE && both) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const int64_t e = pair_at(base, lane, j);
-        const float *f = (const float *)src + e;
-        x[j] = pair(0.f);
-        if (both && (WHOLE || e + 1 < n)) x[j] = *(const float2 *)f;
-        else {
-            if (WHOLE || e < n) x[j].x = f[0];
-            if (WHOLE || e + 1 < n) x[j].y = f[1];
+        for (int j = 0; j < 4; ++j) x[j] = *(const float2 *)(f + pair_at(base, lane, j));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t e = pair_at(base, lane, j >> 1) + (j & 1);
+            at(x, j) = f[WHOLE || e < n ? e : 0];
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (!WHOLE && pair_at(base, lane, j >> 1) + (j & 1) >= n) at(x, j) = 0.f;
     }
 }
 template <bool WHOLE>
@@ -537,14 +548,16 @@ __device__ __forceinline__ void load_matrix(const T *x, const DenseRec &t, int64
 {
     if constexpr (PATH == PATH_ANY) {
         Walk w(t, pair_at(base, lane, 0));
+        T raw[8];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
             const int64_t e = pair_at(base, lane, j);
-            out[j] = pair(0.f);
-            if (e < t.n) out[j].x = to_f32(x[w.one(ld)]);
-            if (e + 1 < t.n) out[j].y = to_f32(x[w.two(ld)]);
+            raw[2 * j] = x[e < t.n ? w.one(ld) : 0];
+            raw[2 * j + 1] = x[e + 1 < t.n ? w.two(ld) : 0];
             w.next();
         }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) at(out, j) = pair_at(base, lane, j >> 1) + (j & 1) < t.n ? to_f32(raw[j]) : 0.f;
     } else {
         if constexpr (PATH == PATH_PLAIN) load_run<TWO>(x + base, UNIT, 0, lane, out);
         else load_run<TWO>(x + row * ld + col, (int)min(t.cols - col, (int64_t)UNIT), (int)(ld - t.cols), lane, out);
@@ -607,11 +620,13 @@ __device__ __forceinline__ float2 update_pairs(Values &x, const DenseRec &t, int
 
 // The units of a warp on the paths without vectors, loaded straight from memory.
 template <int PATH, typename PT, typename GT, bool Q8, bool SR>
-__device__ __forceinline__ void step_pairs(const DenseRec &t, int64_t base, int todo, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key)
+__device__ __forceinline__ void step_pairs(const DenseRec &rec, int64_t base, int todo, int lane, float gs, const DenseStep &a, float lr, float decay, UnitKeys key)
 {
+    const DenseRec t = rec;
     constexpr int64_t STRIDE = WARPS * UNIT;
     constexpr bool WHOLE = PATH != PATH_ANY;
     const bool both = t.flags & REC_PAIR_STATE;
+    if (WHOLE && !isfinite(gs)) return;   // (looking at it after the loads makes this path 3 % slower)
     int64_t row = 0, col = 0;
     if constexpr (PATH == PATH_ROWS) {
         row = base / t.cols;
@@ -620,17 +635,22 @@ __device__ __forceinline__ void step_pairs(const DenseRec &t, int64_t base, int 
 #pragma unroll 1
     for (; todo > 0; --todo, base += STRIDE) {
         Values x;
+        uint2 cm, cr;
         if constexpr (Q8) {
             x.scale = t.scale[base / UNIT];
-            const uint2 cm = load_code_pairs<WHOLE>(t.m, both, base, lane, t.n), cr = load_code_pairs<WHOLE>(t.v, both, base, lane, t.n);
-            e4m3_unpack(cm, x.m);
-            e4m3_unpack(cr, x.v);
+            cm = load_code_pairs<WHOLE>(t.m, both, base, lane, t.n);
+            cr = load_code_pairs<WHOLE>(t.v, both, base, lane, t.n);
         } else {
             load_pairs<WHOLE>(t.m, both, base, lane, t.n, x.m);
             load_pairs<WHOLE>(t.v, both, base, lane, t.n, x.v);
         }
         load_matrix<PATH, false>((const PT *)t.p, t, t.ldp, base, row, col, lane, x.p);
         load_matrix<PATH, false>((const GT *)t.g, t, t.ldg, base, row, col, lane, x.g);
+        if (!WHOLE && !isfinite(gs)) return;
+        if constexpr (Q8) {
+            e4m3_unpack(cm, x.m);
+            e4m3_unpack(cr, x.v);
+        }
         const float2 s = update_pairs<PATH, PT, Q8, SR>(x, t, base, row, col, lane, gs, a, lr, decay, key);
         if (Q8 && lane == 0) t.scale[base / UNIT] = s;
         if constexpr (PATH == PATH_ROWS)
@@ -740,6 +760,7 @@ template <typename PT, typename GT, bool MIXED> struct Ring {
     static __device__ __forceinline__ void copy16(uint32_t to, const void *from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
     static __device__ __forceinline__ void copy8(uint32_t to, const void *from) { asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory"); }
     static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    static __device__ __forceinline__ void drain() { asm volatile("cp.async.wait_all;" ::: "memory"); }
     static __device__ __forceinline__ void wait() { asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 2) : "memory"); }
 
     // Fills slot `to` (a shared-memory address) with the unit that is `units` units of this warp after u.
@@ -918,6 +939,7 @@ __device__ __forceinline__ void step_plain(const DenseRec &t, int64_t base, int 
         if (k < todo) issue(first + k * R::SLOT, k);
         R::commit();
     }
+    if (!isfinite(gs)) return R::drain();
     int in = (R::DEPTH - 1) * R::SLOT, out = 0;
 #pragma unroll 1
     for (; todo > 0; --todo) {
@@ -1004,6 +1026,7 @@ __device__ __forceinline__ void step_rows(const DenseRec &t, int64_t base, int t
         if (k < todo) issue(first + k * R::SLOT, k);
         R::commit();
     }
+    if (!isfinite(gs)) return R::drain();
     int in = (R::DEPTH - 1) * R::SLOT, out = 0;
 #pragma unroll 1
     for (; todo > 0; --todo) {
@@ -1064,11 +1087,9 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
         key.k2 = mix32(key.k1 ^ 0xa511e9b3u);
     }
     pdl_wait();
+    // A factor that is not finite ends the step; it is looked at once the first loads are on their way.
     float gs = 1.f;
-    if (a.grad_scale) {
-        gs = *(const volatile float *)a.grad_scale;
-        if (!isfinite(gs)) return;
-    }
+    if (a.grad_scale) gs = *(const volatile float *)a.grad_scale;
     constexpr int64_t STRIDE = WARPS * UNIT;
     constexpr bool RING = vectors_in_ring<PT>(Q8, SR);
     int64_t base = ((int64_t)ch.first + warp) * UNIT;
@@ -1088,6 +1109,7 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
                 if (k < todo) R::issue(first + k * R::SLOT, u, k, warp, lane);
                 R::commit();
             }
+            if (!isfinite(gs)) return R::drain();
 #pragma unroll 1
             for (; todo > 0; --todo) {
                 R::wait();
@@ -1104,6 +1126,7 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
             }
         } else if constexpr (Q8) {
             u.load(raw, 0);
+            if (!isfinite(gs)) return;
 #pragma unroll 1
             for (; todo > 0; --todo) {
                 u.unpack(raw, x);
@@ -1116,6 +1139,7 @@ dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
 #pragma unroll 1
             for (; todo > 0; --todo) {
                 u.load(raw, 0);
+                if (!isfinite(gs)) return;
                 u.unpack(raw, x);
                 u.template step<SR>(x, half, lane, gs, a, lr, decay, key);
                 u.advance(STRIDE);
@@ -1250,36 +1274,33 @@ dense_norm_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restric
 
 // ---- conversion -----------------------------------------------------------------------------------------------------
 
-template <bool DQ, bool SQ>
+// VEC: whole units, moments of both sides aligned to vectors.
+template <bool DQ, bool SQ, bool VEC>
 __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s, const DenseChunk &ch, int warp, int lane)
 {
-    const bool vectors = d.flags & s.flags & REC_VEC_STATE;
+    const bool from_pairs = s.flags & REC_PAIR_STATE, to_pairs = d.flags & REC_PAIR_STATE;
     for (int k = warp; k < ch.units; k += WARPS) {
         const int64_t base = ((int64_t)ch.first + k) * UNIT, e = base + lane * 8;
-        const bool vec = vectors && base + UNIT <= d.n;
         float2 m[4], v[4];
         float2 scale = make_float2(1.f, 1.f);
         uint2 cm, cr;
-        if constexpr (SQ) scale = s.scale[base / UNIT];
         if constexpr (SQ) {
-            const bool both = s.flags & REC_PAIR_STATE;
-            cm = vec ? load8((const uint8_t *)s.m + e) : load_code_pairs<false>(s.m, both, base, lane, d.n);
-            cr = vec ? load8((const uint8_t *)s.v + e) : load_code_pairs<false>(s.v, both, base, lane, d.n);
-            if constexpr (!DQ) {
-                e4m3_unpack(cm, m);
-                e4m3_unpack(cr, v);
-            }
-        } else if (vec) {
+            scale = s.scale[base / UNIT];
+            cm = VEC ? load8((const uint8_t *)s.m + e) : load_code_pairs<false>(s.m, from_pairs, base, lane, d.n);
+            cr = VEC ? load8((const uint8_t *)s.v + e) : load_code_pairs<false>(s.v, from_pairs, base, lane, d.n);
+        } else if constexpr (VEC) {
             Eight<float> rm, rv;
             rm.load((const float *)s.m + e);
             rv.load((const float *)s.v + e);
             rm.get(m);
             rv.get(v);
         } else {
-            load_pairs<false>(s.m, s.flags & REC_PAIR_STATE, base, lane, d.n, m);
-            load_pairs<false>(s.v, s.flags & REC_PAIR_STATE, base, lane, d.n, v);
+            load_pairs<false>(s.m, from_pairs, base, lane, d.n, m);
+            load_pairs<false>(s.v, from_pairs, base, lane, d.n, v);
         }
         if constexpr (!DQ && SQ) {
+            e4m3_unpack(cm, m);
+            e4m3_unpack(cr, v);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 m[j] = mul2(m[j], pair(scale.x));
@@ -1291,23 +1312,27 @@ __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s,
             for (int j = 0; j < 8; ++j) at(v, j) = -__fsqrt_rn(at(v, j));
             scale = quantise<false>(m, v, UnitKeys{0, 0}, EightFrom{0}, cm, cr);
         }
-        if constexpr (DQ) {
-            if (vec) {
-                *(uint2 *)((uint8_t *)d.m + e) = cm;
-                *(uint2 *)((uint8_t *)d.v + e) = cr;
-            } else {
-                store_code_pairs<false>(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, cm);
-                store_code_pairs<false>(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, cr);
-            }
-        } else if (!vec) {
-            store_pairs<false>(d.m, d.flags & REC_PAIR_STATE, base, lane, d.n, m);
-            store_pairs<false>(d.v, d.flags & REC_PAIR_STATE, base, lane, d.n, v);
-        } else {
+        if constexpr (DQ && VEC) {
+            *(uint2 *)((uint8_t *)d.m + e) = cm;
+            *(uint2 *)((uint8_t *)d.v + e) = cr;
+        } else if constexpr (DQ) {
+            store_code_pairs<false>(d.m, to_pairs, base, lane, d.n, cm);
+            store_code_pairs<false>(d.v, to_pairs, base, lane, d.n, cr);
+        } else if constexpr (VEC) {
             Eight<float>::put((float *)d.m + e, m);
             Eight<float>::put((float *)d.v + e, v);
+        } else {
+            store_pairs<false>(d.m, to_pairs, base, lane, d.n, m);
+            store_pairs<false>(d.v, to_pairs, base, lane, d.n, v);
         }
         if (DQ && lane == 0) d.scale[base / UNIT] = scale;
     }
+}
+template <bool DQ, bool SQ>
+__device__ __forceinline__ void copy_chunk(const DenseRec &d, const DenseRec &s, const DenseChunk &ch, int warp, int lane)
+{
+    if (ch.path == PATH_VECTORS && (d.flags & s.flags & REC_VEC_STATE)) copy_units<DQ, SQ, true>(d, s, ch, warp, lane);
+    else copy_units<DQ, SQ, false>(d, s, ch, warp, lane);
 }
 
 __global__ void __launch_bounds__(WARPS * 32, COPY_CTAS)
@@ -1320,11 +1345,11 @@ dense_copy_state_kernel(const DenseRec *__restrict__ drecs, const DenseRec *__re
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     pdl_wait();
     if (d.flags & REC_Q8) {
-        if (s.flags & REC_Q8) copy_units<true, true>(d, s, ch, warp, lane);
-        else copy_units<true, false>(d, s, ch, warp, lane);
+        if (s.flags & REC_Q8) copy_chunk<true, true>(d, s, ch, warp, lane);
+        else copy_chunk<true, false>(d, s, ch, warp, lane);
     } else {
-        if (s.flags & REC_Q8) copy_units<false, true>(d, s, ch, warp, lane);
-        else copy_units<false, false>(d, s, ch, warp, lane);
+        if (s.flags & REC_Q8) copy_chunk<false, true>(d, s, ch, warp, lane);
+        else copy_chunk<false, false>(d, s, ch, warp, lane);
     }
 }
 
