@@ -7,9 +7,9 @@
 // that a block's maximum is one warp reduction -- and CHUNKS of up to 16 units per warp, one CTA each, listed in a table.
 //
 // Measured (B200, copy rate 6.53 TB/s; LLaMA-shaped sets, clipping factor on the device): FP32 state, 1B set with FP32 masters
-// and BF16 gradients 4.81 ms (6.9 TB/s); 8-bit state, 130M set in BF16 0.173 to 0.180 ms (6.1 to 6.4 TB/s), with FP32 parameters 0.235
-// (6.6 TB/s); stochastic, 1B set in BF16 2.45 to 2.6 ms (4.9 to 5.2 TB/s, bound by the integer and multiply pipes); gradient norm
-// of the 1B set 0.37 to 0.39 ms; state conversion of the 350M set 0.51 to 0.52 ms.  Small calls take 2.1 us on the device.
+// and BF16 gradients 4.81 ms (6.9 TB/s); 8-bit state, 130M set in BF16 0.167 to 0.182 ms (6.1 to 6.6 TB/s), with FP32 parameters 0.235
+// (6.6 TB/s); stochastic, 1B set in BF16 2.45 to 2.65 ms (4.8 to 5.2 TB/s, bound by the integer and multiply pipes); gradient norm
+// of the 1B set 0.37 to 0.39 ms; state conversion of the 350M set 0.50 to 0.51 ms.  Small calls take 2.1 us on the device.
 #include <cuda_fp8.h>
 #include <math.h>
 #include <string.h>
@@ -29,15 +29,16 @@ constexpr int UNIT = TSR_DENSE_BLOCK;      // elements of a warp's piece of work
 static_assert(UNIT == 32 * 8, "a lane holds eight elements of a unit");
 constexpr int WARPS = 8;                   // per CTA
 // Most units of a warp in one chunk, by what goes over it.  FP32 steps overlap by having many CTAs at a time and are faster
-// short (1B set: 4.81 ms with 2 units, 4.96 with 8); the others have work per CTA or load ahead (130M set, 8-bit step: 301 us
-// with 1 unit, 232 with 2, 213 with 8; 1B norm: 1164, 705, 440 and 406 with 16).  Without vectors short chunks balance better
-// (40 M pitched elements, 8-bit step: 101 us with 4 units, 105 with 8), and those of narrow pitched matrices are slow ones.
+// short (1B set: 4.80 ms with 2 units, 4.96 with 8); the others have work per CTA or load ahead (8-bit step: 130M set 175 us
+// with 8 units, 213 with 2, 1B set stochastic 2.55 and 2.87 ms; 1B norm: 384 us with 16, 442 with 4).  Without vectors short
+// chunks balance better (40 M pitched elements, 8-bit step: 100 us with 4 units, 103 with 8), and those of narrow pitched
+// matrices are slow ones.
 constexpr int STEP_F32_UNITS = 2, STEP_Q8_UNITS = 8, COPY_UNITS = 16, NORM_UNITS = 16, PAIRS_UNITS = 4, ANY_UNITS = 1;
 // CTAs on an SM of the kernels, whose registers are bounded for it.
 constexpr int STEP_F32_CTAS = 4, STEP_Q8_CTAS = 3, COPY_CTAS = 5, NORM_CTAS = 4;
 constexpr int SMS = 148;
-// Fewer chunks than this are made shorter, so that they fill the GPU (8-bit step of 4 M elements: 14.9 us, 20.1 with a bound of
-// 2048; conversions hold 5 CTAs on an SM and want twice as many: 30 M elements 53 us, 61 with 512).
+// Fewer chunks than this are made shorter, so that they fill the GPU (8-bit step of 4 M elements: 11.0 us, 15.7 with a bound of
+// 2048).  Conversions hold more CTAs on an SM and want twice as many.
 constexpr int MANY_CHUNKS = 512;
 
 enum DenseRecFlags : uint32_t {
@@ -1064,12 +1065,12 @@ __device__ __forceinline__ void step_rows(const DenseRec &t, int64_t base, int t
 }
 
 // Which kernels load vectors through the ring (stochastic rounding of BF16 parameters is bound by instructions, and faster with
-// the next unit in registers: 1B set 2.45 against 2.51 ms), and which have one at all.
+// the next unit in registers: 1B set 2.55 against 2.68 ms), and which have one at all.
 template <typename PT> __host__ __device__ constexpr bool vectors_in_ring(bool q8, bool sr) { return q8 && (!sr || sizeof(PT) == 4); }
 template <typename PT> __host__ __device__ constexpr bool has_ring(bool q8, bool sr, bool mixed) { return q8 && (mixed || vectors_in_ring<PT>(q8, sr)); }
 
 // MIXED: there are chunks of every path.  Where all chunks are vectors, a kernel without the other paths is launched: their
-// registers cost the FP32 form 1.5 % (1B set: 4.88 against 4.81 ms).
+// registers and the wider slots cost the 8-bit form 3 % (130M set: 181 against 175 us; 1B set stochastic 2.61 against 2.55 ms).
 template <typename PT, typename GT, bool Q8, bool SR, bool MIXED>
 __global__ void __launch_bounds__(WARPS * 32, Q8 ? STEP_Q8_CTAS : STEP_F32_CTAS)
 dense_step_kernel(const DenseRec *__restrict__ recs, const DenseChunk *__restrict__ chunks, const DenseStep a)
