@@ -15,31 +15,19 @@
 #include <string.h>
 
 #include <algorithm>
-#include <new>
 #include <stdarg.h>
 #include <stdio.h>
 
+#include "tsr_dense_table.h"
 #include "tsr_device.cuh"
 #include "tsr_internal.h"
 #include "tsr_pdl.cuh"
 
 namespace tsr {
 
-constexpr int UNIT = TSR_DENSE_BLOCK;      // elements of a warp's piece of work
-static_assert(UNIT == 32 * 8, "a lane holds eight elements of a unit");
-constexpr int WARPS = 8;                   // per CTA
-// Most units of a warp in one chunk, by what goes over it.  FP32 steps overlap by having many CTAs at a time and are faster
-// short (1B set: 4.80 ms with 2 units, 4.96 with 8); the others have work per CTA or load ahead (8-bit step: 130M set 175 us
-// with 8 units, 213 with 2, 1B set stochastic 2.55 and 2.87 ms; 1B norm: 384 us with 16, 442 with 4).  Without vectors short
-// chunks balance better (40 M pitched elements, 8-bit step: 100 us with 4 units, 103 with 8), and those of narrow pitched
-// matrices are slow ones.
-constexpr int STEP_F32_UNITS = 2, STEP_Q8_UNITS = 8, COPY_UNITS = 16, NORM_UNITS = 16, PAIRS_UNITS = 4, ANY_UNITS = 1;
 // CTAs on an SM of the kernels, whose registers are bounded for it.
 constexpr int STEP_F32_CTAS = 4, STEP_Q8_CTAS = 3, COPY_CTAS = 5, NORM_CTAS = 4;
 constexpr int SMS = 148;
-// Fewer chunks than this are made shorter, so that they fill the GPU (8-bit step of 4 M elements: 11.0 us, 15.7 with a bound of
-// 2048).  Conversions hold more CTAs on an SM and want twice as many.
-constexpr int MANY_CHUNKS = 512;
 
 enum DenseRecFlags : uint32_t {
     REC_VEC_STATE = 1,   // the moments can be read in vectors of eight elements
@@ -60,14 +48,6 @@ struct alignas(16) DenseRec {   // one tensor on the device
     uint32_t flags;
     int32_t index;              // position in the plan
 };
-
-// How a step goes over a chunk.  VECTORS: everything that it touches is contiguous and aligned to vectors of eight
-// elements.  PLAIN: contiguous, any alignment.  ROWS: rows of 256 elements or more, so that a unit meets the end of a row
-// once at most.  All three hold whole units only.  ANY: the rest, the last units of tensors and narrow matrices.
-enum DensePath : int32_t { PATH_ANY = 0, PATH_VECTORS = 1, PATH_PLAIN = 2, PATH_ROWS = 3 };
-
-// Units [first, first + units) of tensor rec.
-struct alignas(16) DenseChunk { int32_t rec; uint32_t first; int32_t units; int32_t path; };
 
 struct DenseStep {
     StepScalars sc;
@@ -1362,12 +1342,8 @@ using namespace tsr;
 
 struct tsr_dense_plan {
     std::vector<tsr_dense_desc> descs;
-    // Units of a chunk when stepping (FP32 and 8-bit states), taking the norm and copying states.
-    int step_units[2] = {}, norm_units = 0, copy_units = 0;
-    size_t most_chunks = 0;                 // room for so many in the table
-    // One table: the chunks of the stepped tensors group by group, then those of the norm, then those of copies.
-    struct Group { int key, first, count; bool mixed; };
-    std::vector<Group> groups;              // tensors that share types: one launch each
+    DenseLayout layout;
+    std::vector<DenseTable::Group> groups;
     int norm_first = 0, copy_first = 0, chunk_count = 0;
     size_t workspace_bytes = 0;
     bool bound = false;
@@ -1377,6 +1353,7 @@ struct tsr_dense_plan {
     double *d_partial = nullptr;
     uint32_t *d_ticket = nullptr;
     mutable std::string err;
+    explicit tsr_dense_plan(const std::vector<tsr_dense_desc> &d) : descs(d), layout(d) {}
 };
 
 namespace {
@@ -1404,13 +1381,6 @@ tsr_status dense_fail(const tsr_dense_plan *plan, tsr_status s, const char *fmt,
     } while (0)
 
 constexpr int64_t DENSE_MOST = (int64_t)1 << 40;   // elements of a tensor with its pitch; keeps products in 64 bits
-
-enum { KEY_P_BF16 = 1, KEY_G_BF16 = 2, KEY_Q8 = 4, KEY_COUNT = 8 };
-
-int key_of(const tsr_dense_desc &d)
-{
-    return (d.p_dtype == TSR_BF16 ? KEY_P_BF16 : 0) | (d.g_dtype == TSR_BF16 ? KEY_G_BF16 : 0) | (d.state == TSR_STATE_Q8 ? KEY_Q8 : 0);
-}
 
 template <typename PT, typename GT, bool Q8, bool SR>
 cudaError_t step_launch_as(bool mixed, const DenseRec *recs, const DenseChunk *chunks, int count, const DenseStep &a, cudaStream_t s)
@@ -1463,20 +1433,9 @@ tsr_status dense_ready(const tsr_dense_plan *plan)
     return TSR_OK;
 }
 
-bool aligned(const void *p, int64_t bytes) { return ((uintptr_t)p & (uintptr_t)(bytes - 1)) == 0; }
-int64_t size_of(int32_t dtype) { return dtype == TSR_BF16 ? 2 : 4; }
-
-// ld: the largest pitch in use
-DensePath path_of(bool contiguous, bool vectors, const tsr_dense_desc &d, int64_t ld)
-{
-    if (contiguous) return vectors ? PATH_VECTORS : PATH_PLAIN;
-    return d.cols >= UNIT && ld < (1 << 30) && d.rows < (1 << 30) ? PATH_ROWS : PATH_ANY;   // (32-bit rows and columns)
-}
-
 tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *workspace)
 {
     std::vector<DenseRec> recs(plan->descs.size());
-    std::vector<DensePath> path(recs.size(), PATH_ANY), grad_path(recs.size(), PATH_ANY);
     for (size_t i = 0; i < recs.size(); ++i) {
         const tsr_dense_desc &d = plan->descs[i];
         const tsr_dense_ptrs &p = ptrs[i];
@@ -1485,12 +1444,12 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
         r.n = d.rows * d.cols;
         if (r.n == 0) continue;
         const bool grad = d.flags != TSR_DENSE_STATE_ONLY, state = d.flags != TSR_DENSE_NORM_ONLY, step = d.flags == 0;
-        const int64_t ps = size_of(d.p_dtype), gs = size_of(d.g_dtype);
+        const int64_t ps = dense_size_of(d.p_dtype), gs = dense_size_of(d.g_dtype);
         const bool q8 = d.state == TSR_STATE_Q8;
         if ((grad && !p.grad) || (state && (!p.m || !p.v || (q8 && !p.scale))) || (step && !p.param))
             return dense_fail(plan, TSR_ERR_INVALID_ARG, "tensor %zu: NULL pointer", i);
-        if ((grad && !aligned(p.grad, gs)) || (state && !q8 && (!aligned(p.m, 4) || !aligned(p.v, 4))) ||
-            (state && q8 && !aligned(p.scale, 8)) || (step && (!aligned(p.param, ps) || !aligned(p.image, 2))))
+        if ((grad && !dense_aligned(p.grad, gs)) || (state && !q8 && (!dense_aligned(p.m, 4) || !dense_aligned(p.v, 4))) ||
+            (state && q8 && !dense_aligned(p.scale, 8)) || (step && (!dense_aligned(p.param, ps) || !dense_aligned(p.image, 2))))
             return dense_fail(plan, TSR_ERR_ALIGNMENT, "tensor %zu: a buffer is not aligned to its element type", i);
         if (step && p.image && d.p_dtype != TSR_F32)
             return dense_fail(plan, TSR_ERR_INVALID_ARG, "tensor %zu: an image needs an FP32 parameter", i);
@@ -1500,54 +1459,29 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
         r.index = (int32_t)i;
         if (q8) r.flags |= REC_Q8;
         if (d.g_dtype == TSR_BF16) r.flags |= REC_G_BF16;
-        bool dense = true;
+        bool contiguous = true;
         if (grad) {
             r.g = p.grad;
-            dense = d.rows <= 1 || d.ldg == d.cols;
-            grad_path[i] = path_of(dense, aligned(p.grad, 8 * gs), d, d.ldg);
+            contiguous = dense_grad_contiguous(d);
         }
         if (state) {
             r.m = p.m; r.v = p.v;
             const int64_t es = q8 ? 1 : 4;
             if (q8) r.scale = (float2 *)p.scale;
-            if (aligned(p.m, 8 * es) && aligned(p.v, 8 * es)) r.flags |= REC_VEC_STATE;
-            if (aligned(p.m, 2 * es) && aligned(p.v, 2 * es)) r.flags |= REC_PAIR_STATE;
+            if (DenseLayout::state_vectors(d, p)) r.flags |= REC_VEC_STATE;
+            if (dense_aligned(p.m, 2 * es) && dense_aligned(p.v, 2 * es)) r.flags |= REC_PAIR_STATE;
         }
         if (step) {
             r.p = p.param;
             r.image = (bf16 *)p.image;
-            dense = dense && (d.rows <= 1 || (d.ldp == d.cols && (!p.image || d.ldi == d.cols)));
-            path[i] = path_of(dense, grad_path[i] == PATH_VECTORS && (r.flags & REC_VEC_STATE) && aligned(p.param, 8 * ps) && aligned(p.image, 16), d,
-                              std::max(std::max(d.ldp, d.ldg), p.image ? d.ldi : 0));
-            if (q8 && !(r.flags & REC_VEC_STATE)) path[i] = PATH_ANY;   // the ring takes codes eight by eight
+            contiguous = dense_step_contiguous(d, p.image != nullptr);
         }
-        if (!dense) r.flags |= REC_PITCHED;
+        if (!contiguous) r.flags |= REC_PITCHED;
     }
-    std::vector<DenseChunk> chunks;
-    std::vector<tsr_dense_plan::Group> groups;
-    chunks.reserve(plan->most_chunks);
-    auto add = [&](size_t i, DensePath how, int at_once) {
-        if (how == PATH_ANY) at_once = std::min(at_once, WARPS * ANY_UNITS);
-        if (how == PATH_PLAIN || how == PATH_ROWS) at_once = std::min(at_once, WARPS * PAIRS_UNITS);   // the partial last unit is a chunk of its own on the paths for whole units
-        const int64_t units = (recs[i].n + UNIT - 1) / UNIT, whole = how != PATH_ANY ? recs[i].n / UNIT : units;
-        for (int64_t k = 0; k < whole; k += at_once)
-            chunks.push_back({(int32_t)i, (uint32_t)k, (int32_t)std::min<int64_t>(at_once, whole - k), how});
-        if (whole < units) chunks.push_back({(int32_t)i, (uint32_t)whole, 1, PATH_ANY});
-    };
-    for (int key = 0; key < KEY_COUNT; ++key) {
-        const int first = (int)chunks.size();
-        for (size_t i = 0; i < recs.size(); ++i)
-            if (plan->descs[i].flags == 0 && key_of(plan->descs[i]) == key) add(i, path[i], plan->step_units[plan->descs[i].state]);
-        const int got = (int)chunks.size() - first;
-        const bool mixed = std::any_of(chunks.begin() + first, chunks.end(), [](const DenseChunk &c) { return c.path != PATH_VECTORS; });
-        if (got) groups.push_back({key, first, got, mixed});
-    }
-    const int norm_first = (int)chunks.size();
-    for (size_t i = 0; i < recs.size(); ++i)
-        if (plan->descs[i].flags != TSR_DENSE_STATE_ONLY) add(i, grad_path[i], plan->norm_units);
-    const int copy_first = (int)chunks.size();
-    for (size_t i = 0; i < recs.size(); ++i)
-        if (plan->descs[i].flags != TSR_DENSE_NORM_ONLY) add(i, PATH_VECTORS, plan->copy_units);
+    DenseTable table = plan->layout.fill(plan->descs, ptrs);
+    const std::vector<DenseChunk> &chunks = table.chunks;
+    if ((int64_t)chunks.size() > plan->layout.most_chunks)
+        return dense_fail(plan, TSR_ERR_WORKSPACE, "the table has %zu chunks, the workspace holds %lld", chunks.size(), (long long)plan->layout.most_chunks);
     int dev = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return dense_fail(plan, TSR_ERR_CUDA, "no CUDA device available");
     DENSE_CUDA(plan, cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev));
@@ -1561,7 +1495,7 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     plan->d_recs = (DenseRec *)at;
     at += round_up((int64_t)(recs.size() * sizeof(DenseRec)), 256);
     plan->d_chunks = (DenseChunk *)at;
-    at += round_up((int64_t)(plan->most_chunks * sizeof(DenseChunk)), 256);
+    at += round_up(plan->layout.most_chunks * (int64_t)sizeof(DenseChunk), 256);
     plan->d_partial = (double *)at;
     at += NORM_CTAS * SMS * sizeof(double);
     plan->d_ticket = (uint32_t *)at;
@@ -1569,40 +1503,14 @@ tsr_status dense_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs, void *wo
     if (!chunks.empty()) DENSE_CUDA(plan, cudaMemcpy(plan->d_chunks, chunks.data(), chunks.size() * sizeof(DenseChunk), cudaMemcpyHostToDevice));
     DENSE_CUDA(plan, cudaMemset(plan->d_ticket, 0, sizeof(uint32_t)));
     DENSE_CUDA(plan, cudaDeviceSynchronize());
-    plan->groups.swap(groups);
+    plan->groups.swap(table.groups);
     plan->chunk_count = (int)chunks.size();
-    plan->norm_first = norm_first;
-    plan->copy_first = copy_first;
+    plan->norm_first = table.norm_first;
+    plan->copy_first = table.copy_first;
     plan->device = dev;
     plan->norm_ctas = NORM_CTAS * std::min(SMS, sms);
     plan->bound = true;
     return TSR_OK;
-}
-
-void dense_layout(tsr_dense_plan *plan, const tsr_dense_desc *descs, int32_t count)
-{
-    if (count > 0) plan->descs.assign(descs, descs + count);
-    auto tensor_chunks = [](const tsr_dense_desc &d, int64_t units) { return (d.rows * d.cols + units * UNIT - 1) / (units * UNIT) + 1; };
-    // As long as may be, but so many that the GPU fills.
-    auto fit = [&](int most, int many) {
-        for (;; most /= 2) {
-            int64_t chunks = 0;
-            for (const tsr_dense_desc &d : plan->descs) chunks += tensor_chunks(d, most * WARPS);
-            if (most == 1 || chunks >= many) return most * WARPS;
-        }
-    };
-    plan->step_units[TSR_STATE_F32] = fit(STEP_F32_UNITS, MANY_CHUNKS);
-    plan->step_units[TSR_STATE_Q8] = fit(STEP_Q8_UNITS, MANY_CHUNKS);
-    plan->norm_units = fit(NORM_UNITS, MANY_CHUNKS);
-    plan->copy_units = fit(COPY_UNITS, 2 * MANY_CHUNKS);
-    for (const tsr_dense_desc &d : plan->descs) {   // room for a step and the norm on the path that takes the shortest chunks
-        const int least = WARPS * (d.rows > 1 && d.cols < UNIT ? ANY_UNITS : PAIRS_UNITS);
-        plan->most_chunks += (size_t)(tensor_chunks(d, std::min(plan->step_units[d.state == TSR_STATE_Q8], least)) +
-                                      tensor_chunks(d, std::min(plan->norm_units, least)) + tensor_chunks(d, plan->copy_units));
-    }
-    plan->workspace_bytes = (size_t)(round_up((int64_t)(plan->descs.size() * sizeof(DenseRec)), 256) +
-                                     round_up((int64_t)(plan->most_chunks * sizeof(DenseChunk)), 256) +
-                                     NORM_CTAS * SMS * (int64_t)sizeof(double) + 256);
 }
 
 }  // namespace
@@ -1631,15 +1539,15 @@ tsr_status tsr_dense_plan_create(tsr_dense_plan **out, const tsr_dense_desc *des
         total += 3 * ((d.rows * d.cols + WARPS * UNIT - 1) / (WARPS * UNIT) + 1);
         if (total > 0x7fffffff) return TSR_ERR_SHAPE;
     }
-    tsr_dense_plan *plan = new (std::nothrow) tsr_dense_plan;
-    if (!plan) return TSR_ERR_INVALID_ARG;
     try {
-        dense_layout(plan, descs, count);
+        tsr_dense_plan *plan = new tsr_dense_plan(std::vector<tsr_dense_desc>(descs, descs + count));
+        plan->workspace_bytes = (size_t)(round_up((int64_t)(plan->descs.size() * sizeof(DenseRec)), 256) +
+                                         round_up(plan->layout.most_chunks * (int64_t)sizeof(DenseChunk), 256) +
+                                         NORM_CTAS * SMS * (int64_t)sizeof(double) + 256);
+        *out = plan;
     } catch (...) {   // the host is out of memory
-        delete plan;
         return TSR_ERR_INVALID_ARG;
     }
-    *out = plan;
     return TSR_OK;
 }
 
@@ -1665,7 +1573,7 @@ tsr_status tsr_dense_plan_bind(tsr_dense_plan *plan, const tsr_dense_ptrs *ptrs,
     if (count != (int32_t)plan->descs.size() || (count > 0 && !ptrs)) return dense_fail(plan, TSR_ERR_INVALID_ARG, "ptrs/count mismatch");
     if (!workspace || workspace_bytes < plan->workspace_bytes)
         return dense_fail(plan, TSR_ERR_WORKSPACE, "workspace needs %zu bytes", plan->workspace_bytes);
-    if (!aligned(workspace, 256)) return dense_fail(plan, TSR_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
+    if (!dense_aligned(workspace, 256)) return dense_fail(plan, TSR_ERR_ALIGNMENT, "workspace must be 256-byte aligned");
     try {
         return dense_bind(plan, ptrs, workspace);
     } catch (...) {
@@ -1682,7 +1590,7 @@ tsr_status tsr_dense_plan_step(tsr_dense_plan *plan, const tsr_hyper *h, const f
     if (!(h->beta1 >= 0.f && h->beta1 < 1.f) || !(h->beta2 >= 0.f && h->beta2 < 1.f))
         return dense_fail(plan, TSR_ERR_INVALID_ARG, "betas must lie in [0, 1)");
     if (rounding != TSR_ROUND_NEAREST && rounding != TSR_ROUND_STOCHASTIC) return dense_fail(plan, TSR_ERR_INVALID_ARG, "unknown rounding");
-    if (!aligned(grad_scale, 4)) return dense_fail(plan, TSR_ERR_ALIGNMENT, "grad_scale is not aligned to a float");
+    if (!dense_aligned(grad_scale, 4)) return dense_fail(plan, TSR_ERR_ALIGNMENT, "grad_scale is not aligned to a float");
     tsr_status st = dense_ready(plan);
     if (st != TSR_OK) return st;
     DenseStep a;
@@ -1700,7 +1608,7 @@ tsr_status tsr_dense_plan_step(tsr_dense_plan *plan, const tsr_hyper *h, const f
     a.grad_scale = grad_scale;
     a.seed_key = mix32((uint32_t)seed ^ mix32((uint32_t)(seed >> 32) + 0x9e3779b9u));
     a.step_lo = (uint32_t)h->step;
-    for (const tsr_dense_plan::Group &g : plan->groups) {
+    for (const DenseTable::Group &g : plan->groups) {
         const DenseChunk *chunks = plan->d_chunks + g.first;
         DENSE_CUDA(plan, step_launch(g.key, rounding == TSR_ROUND_STOCHASTIC, g.mixed, plan->d_recs, chunks, g.count, a, (cudaStream_t)stream));
     }
@@ -1712,7 +1620,7 @@ tsr_status tsr_dense_plan_grad_norm(tsr_dense_plan *plan, float max_norm, float 
     if (!plan) return TSR_ERR_INVALID_ARG;
     if (!out) return dense_fail(plan, TSR_ERR_INVALID_ARG, "out is NULL");
     if (!(max_norm > 0.f)) return dense_fail(plan, TSR_ERR_INVALID_ARG, "max_norm must be positive");
-    if (!aligned(out, 4)) return dense_fail(plan, TSR_ERR_ALIGNMENT, "out is not aligned to a float");
+    if (!dense_aligned(out, 4)) return dense_fail(plan, TSR_ERR_ALIGNMENT, "out is not aligned to a float");
     tsr_status st = dense_ready(plan);
     if (st != TSR_OK) return st;
     const int count = plan->copy_first - plan->norm_first;

@@ -97,3 +97,27 @@ def test_the_models_of_the_8_bit_form_agree_with_each_other():
         c = dm.E4M3[dm.quantise(np.full(1 << 16, x, np.float32), 1.0, words)]
         assert np.all(np.abs(c - x) < dm.spacing(max(x, 1e-30)) + (x == 0))
         assert abs(c.mean() - x) <= dm.spacing(max(x, 1e-30)) * 2.0 ** -15
+
+
+def test_the_table_fits_its_room(tmp_path):
+    """Shapes, pitches, types and alignments: the table that a binding fills is never larger than the room planned for it."""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "dense_table")
+    subprocess.check_call(["g++", "-std=c++17", "-O2", "-I", os.path.join(root, "include"), "-I", os.path.join(root, "paper_2602_08007_b200", "csrc"),
+                           os.path.join(root, "tests", "dense_table.cpp"), "-o", exe])
+    run = subprocess.run([exe], capture_output=True, text=True)
+    assert run.returncode == 0, run.stdout
+
+
+@pytest.mark.parametrize("rows,cols,pitch", [(1, 40_000_000, 0), (32000, 2048, 0), (32000, 2048, 8), (2, 3_000_000, 1 << 30)])
+def test_the_workspace_holds_the_chunks_of_any_binding(tsr, rows, cols, pitch):
+    """Codes off an 8-byte border, or a pitch beyond 32 bits, make chunks of eight blocks, 16 bytes each in the table."""
+    rc, plan = create(tsr, [desc(tsr, rows=rows, cols=cols, ldp=cols + pitch, ldg=cols + pitch, ldi=cols, state=1)])
+    assert rc == 0
+    size = ctypes.c_size_t()
+    assert tsr.lib().tsr_dense_plan_workspace_bytes(plan, ctypes.byref(size)) == 0
+    blocks = -(-rows * cols // tsr.DENSE_BLOCK)
+    assert size.value >= 16 * -(-blocks // 8)
+    tsr.lib().tsr_dense_plan_destroy(plan)
