@@ -43,7 +43,12 @@ class DensePlan:
     images: per tensor None or a BF16 tensor that every step fills with the updated FP32 parameter.
     lr_mult, wd_mult: per-tensor factors on hyper.lr and hyper.weight_decay.
 
-    The tensors are taken as they lie: after replacing entries of .grads (or any other list), call bind()."""
+    The tensors are taken as they lie: after replacing entries of .grads (or any other list), call bind().
+
+    Calls go to torch's current stream, or to `stream`.  What the plan itself allocates (its tables, the result of grad_norm,
+    zero states) is handed back to torch's allocator only after the work that the calls put on their streams; tensors of the
+    caller need record_stream where they are dropped while another stream than their own uses them.  A captured graph holds
+    addresses of the plan and of its tensors: keep the plan, and do not bind() it again, while the graph is replayed."""
 
     def __init__(self, params: Optional[Sequence[torch.Tensor]], grads: Optional[Sequence[torch.Tensor]], states=None,
                  state_dtype=torch.float32, images=None, lr_mult: Optional[Sequence[float]] = None,
@@ -69,6 +74,7 @@ class DensePlan:
         self._index = self.device.index
         self._lib = lib()
         self.states = self._zero_states(state_dtype) if states is None else [tuple(s) for s in states]
+        self._made_states = states is None
         self.images = list(images) if images is not None else [None] * n
         self.lr_mult = [1.0] * n if lr_mult is None else [float(x) for x in lr_mult]
         self.wd_mult = [1.0] * n if wd_mult is None else [float(x) for x in wd_mult]
@@ -150,6 +156,7 @@ class DensePlan:
             size = ctypes.c_size_t()
             self._check(lib().tsr_dense_plan_workspace_bytes(self.ctx, ctypes.byref(size)))
             self.workspace = torch.empty(size.value + 256, dtype=torch.uint8, device=self.device)
+            self._met = set()      # streams that the allocator knows to use what the plan has allocated
             at = (self.workspace.data_ptr() + 255) // 256 * 256
             self._check(lib().tsr_dense_plan_bind(self.ctx, (DensePtrs * max(n, 1))(*ptrs), n, at, size.value))
 
@@ -165,7 +172,13 @@ class DensePlan:
             pass
 
     def _stream(self, stream):
-        return _current_stream(self._index) if stream is None else stream.cuda_stream
+        handle = _current_stream(self._index) if stream is None else stream.cuda_stream
+        if handle not in self._met:
+            s = torch.cuda.current_stream(self._index) if stream is None else stream
+            for t in [self.workspace, self._result] + ([t for st in self.states for t in st] if self._made_states else []):
+                t.record_stream(s)
+            self._met.add(handle)
+        return handle
 
     # -- the C calls --------------------------------------------------------------------------
     def step(self, hyper: Hyper, grad_scale: Optional[torch.Tensor] = None, rounding: int = TSR_ROUND_NEAREST, seed: int = 0, stream=None):
@@ -194,4 +207,5 @@ class DensePlan:
 
     def copy_state(self, src: "DensePlan", stream=None):
         """Takes over the moments of `src`, a plan over tensors of the same sizes, converting between FP32 and 8 bits."""
+        src._stream(stream)        # its tables are read there too
         self._check(self._lib.tsr_dense_plan_copy_state(self.ctx, src.ctx, self._stream(stream)))

@@ -1,0 +1,95 @@
+"""Dense plans on streams other than the one their memory belongs to (GPU)."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+F8 = torch.float8_e4m3fn
+BUSY = 200_000_000      # clock cycles for which a stream is held up: a tenth of a second
+
+
+@pytest.fixture(scope="module")
+def tsr():
+    import paper_2602_08007_b200 as t
+    return t
+
+
+def rand(n, seed):
+    return torch.randn(n, generator=torch.Generator().manual_seed(seed)).cuda()
+
+
+def spans(tensors):
+    return [(t.data_ptr(), t.data_ptr() + t.numel() * t.element_size()) for t in tensors if t.numel()]
+
+
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("call", ["step", "grad_norm", "copy_state"])
+def test_a_dropped_plan_keeps_its_memory_until_its_calls_are_done(tsr, call, given):
+    """A plan is called on a stream that is held up, and dropped: nothing that it allocated is given to anyone else before the
+    stream gets there.  The stream is an argument or torch's current one."""
+    p, g = rand(300_000, 1), rand(300_000, 2)
+    q = p.clone()
+    want = tsr.DensePlan([q], [g], state_dtype=F8)
+    want.step(tsr.make_hyper(1))
+    dst = [torch.zeros(300_000, device="cuda") for _ in (0, 1)]
+    out = torch.zeros(2, device="cuda")
+    plan = tsr.DensePlan([p], [g], state_dtype=F8)
+    into = tsr.DensePlan(None, None, states=[tuple(dst)])
+    plan.step(tsr.make_hyper(1))
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    mine = spans([plan.workspace, plan._result, into.workspace] + [t for s in plan.states for t in s])
+    sizes = [b - a for a, b in mine]
+    kw = dict(stream=side) if given else {}
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(BUSY)
+    with torch.cuda.stream(side if not given else torch.cuda.current_stream()):
+        if call == "step":
+            plan.step(tsr.make_hyper(2), **kw)
+        elif call == "grad_norm":
+            plan.grad_norm(1.0, out=out, **kw)
+        else:
+            into.copy_state(plan, **kw)
+    del plan, into
+    others = [torch.empty(n, dtype=torch.uint8, device="cuda") for n in sizes for _ in range(4)]
+    late = side.query()
+    if call == "step":
+        used = mine[0:1] + mine[3:]
+    elif call == "grad_norm":
+        used = mine[0:1]
+    else:
+        used = mine[0:1] + mine[2:]
+    clash = [(a, b) for a, b in spans(others) for c, d in used if a < d and c < b]
+    side.synchronize()
+    assert not late          # the stream was still held up when memory was asked for
+    assert not clash
+    if call == "step":
+        want.step(tsr.make_hyper(2))
+        assert torch.equal(p, q)
+    elif call == "grad_norm":
+        assert torch.equal(out, want.grad_norm(1.0))
+    else:
+        ref = [torch.zeros(300_000, device="cuda") for _ in (0, 1)]
+        tsr.DensePlan(None, None, states=[tuple(ref)]).copy_state(want)
+        assert torch.equal(dst[0], ref[0]) and torch.equal(dst[1], ref[1])
+
+
+def test_a_plan_bound_again_keeps_its_old_tables_until_its_calls_are_done(tsr):
+    """bind() waits for the device, so a step that is still to run sees the tables that it was called with."""
+    p, g = rand(100_000, 1), rand(100_000, 2)
+    q, h = p.clone(), rand(100_000, 3)
+    plan = tsr.DensePlan([p], [g])
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(BUSY)
+    plan.step(tsr.make_hyper(1), stream=side)
+    plan.grads[0] = h
+    plan.bind()
+    plan.step(tsr.make_hyper(2))
+    want = tsr.DensePlan([q], [g])
+    want.step(tsr.make_hyper(1))
+    want.grads[0] = h
+    want.bind()
+    want.step(tsr.make_hyper(2))
+    assert torch.equal(p, q)
