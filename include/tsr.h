@@ -25,7 +25,7 @@
  *   - G is read-only.  W, U, V, M, Vm, C are updated in place.
  *   - Calls are asynchronous on `stream` (a cudaStream_t passed as void*,
  *     NULL = the legacy default stream) unless stated otherwise, and calls on
- *     one context must be issued from one host thread at a time.
+ *     one context or dense plan must be issued from one host thread at a time.
  *   - Every call returns a tsr_status.  Argument errors are detected on the
  *     host before anything is launched and leave all buffers untouched.
  *     Conditions detected on the device (a rank-deficient sketch, an
@@ -312,7 +312,8 @@ TSR_API tsr_status tsr_dense_plan_step(tsr_dense_plan *plan, const tsr_hyper *hy
 
 /* Global norm and clipping factor, on the device: out[0] = n = sqrt(sum of g^2 over all tensors but state-only
  * ones), out[1] = min(1, max_norm / (n + 1e-6)), or NaN where n is not a finite FP32 number.  max_norm > 0, may be
- * infinite.  Sums are FP64 and in a fixed order: the same gradients give the same bits on the same kind of GPU. */
+ * infinite.  The norms of one plan share partial sums in its workspace: two of them must not run at the same time, so put
+ * them on one stream or order their streams by events (a captured norm by whoever replays it).  Sums are FP64 and in a fixed order: the same gradients give the same bits on the same kind of GPU. */
 TSR_API tsr_status tsr_dense_plan_grad_norm(tsr_dense_plan *plan, float max_norm, float *out, void *stream);
 
 /* Moments of src into dst, tensor by tensor, converted where the two keep them in different forms (rounded to nearest

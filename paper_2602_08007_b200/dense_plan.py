@@ -47,8 +47,9 @@ class DensePlan:
 
     Calls go to torch's current stream, or to `stream`.  What the plan itself allocates (its tables, the result of grad_norm,
     zero states) is handed back to torch's allocator only after the work that the calls put on their streams; tensors of the
-    caller need record_stream where they are dropped while another stream than their own uses them.  A captured graph holds
-    addresses of the plan and of its tensors: keep the plan, and do not bind() it again, while the graph is replayed."""
+    caller need record_stream where they are dropped while another stream than their own uses them.  The norms of one plan
+    run one after the other, whatever their streams.  A captured graph holds addresses of the plan and of its tensors: keep the
+    plan, do not bind() it again while the graph is replayed, and let no norm of the plan run beside a replayed one."""
 
     def __init__(self, params: Optional[Sequence[torch.Tensor]], grads: Optional[Sequence[torch.Tensor]], states=None,
                  state_dtype=torch.float32, images=None, lr_mult: Optional[Sequence[float]] = None,
@@ -156,6 +157,8 @@ class DensePlan:
             size = ctypes.c_size_t()
             self._check(lib().tsr_dense_plan_workspace_bytes(self.ctx, ctypes.byref(size)))
             self.workspace = torch.empty(size.value + 256, dtype=torch.uint8, device=self.device)
+            # the device is idle after a binding: no norm to wait for
+            self._norm_handle, self._norm_stream = None, None
             self._met = set()      # streams that the allocator knows to use what the plan has allocated
             at = (self.workspace.data_ptr() + 255) // 256 * 256
             self._check(lib().tsr_dense_plan_bind(self.ctx, (DensePtrs * max(n, 1))(*ptrs), n, at, size.value))
@@ -180,6 +183,19 @@ class DensePlan:
             self._met.add(handle)
         return handle
 
+    def _order_norms(self, handle: int, stream):
+        """The norms of a plan share its partial sums, so one on another stream than the last waits for that stream.  (A
+        capture cannot wait for work outside of it: whoever replays a captured norm orders it.)"""
+        s = torch.cuda.current_stream(self._index) if stream is None else stream
+        for x in (s, self._norm_stream):
+            if x is not None:
+                with torch.cuda.stream(x):
+                    if torch.cuda.is_current_stream_capturing():
+                        return
+        if self._norm_stream is not None:
+            s.wait_stream(self._norm_stream)
+        self._norm_handle, self._norm_stream = handle, s
+
     # -- the C calls --------------------------------------------------------------------------
     def step(self, hyper: Hyper, grad_scale: Optional[torch.Tensor] = None, rounding: int = TSR_ROUND_NEAREST, seed: int = 0, stream=None):
         """One AdamW step.  grad_scale: None or an FP32 tensor on the device whose first element multiplies every gradient
@@ -200,7 +216,10 @@ class DensePlan:
             out = self._result
         elif out.dtype != torch.float32 or out.device != self.device or out.numel() < 2 or not out.is_contiguous():
             raise ValueError("out must be a contiguous FP32 tensor of two elements on %s" % self.device)
-        status = self._lib.tsr_dense_plan_grad_norm(self.ctx, max_norm, out.data_ptr(), self._stream(stream))
+        handle = self._stream(stream)
+        if handle != self._norm_handle:
+            self._order_norms(handle, stream)
+        status = self._lib.tsr_dense_plan_grad_norm(self.ctx, max_norm, out.data_ptr(), handle)
         if status != TSR_OK:
             self._check(status)
         return out

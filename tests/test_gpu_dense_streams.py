@@ -93,3 +93,49 @@ def test_a_plan_bound_again_keeps_its_old_tables_until_its_calls_are_done(tsr):
     want.bind()
     want.step(tsr.make_hyper(2))
     assert torch.equal(p, q)
+
+
+def test_norms_of_a_plan_on_two_streams_run_one_after_the_other(tsr):
+    """They share partial sums.  While the first is held up, the second has not run either; both results are right."""
+    g = rand(3_000_000, 1)
+    plan = tsr.DensePlan(None, [g])
+    want = plan.grad_norm(1.0).clone()
+    side, other = torch.cuda.Stream(), torch.cuda.Stream()
+    a, b = torch.zeros(2, device="cuda"), torch.zeros(2, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(BUSY)
+        plan.grad_norm(1.0, out=a)
+        first = torch.cuda.Event()
+        first.record()
+    plan.grad_norm(1.0, out=b, stream=other)
+    held_up = not first.query()
+    other.synchronize()
+    assert held_up and first.query()      # the second was through only after the first
+    assert torch.equal(a, want) and torch.equal(b, want)
+    c = plan.grad_norm(1.0)               # back on the default stream, many times on either
+    for k in range(20):
+        with torch.cuda.stream((side, other)[k % 2]):
+            plan.grad_norm(1.0, out=(a, b)[k % 2])
+    torch.cuda.synchronize()
+    assert torch.equal(a, want) and torch.equal(b, want) and torch.equal(c, want)
+
+
+def test_a_norm_is_captured_after_norms_on_other_streams(tsr):
+    g = rand(100_000, 1)
+    plan = tsr.DensePlan(None, [g])
+    want = plan.grad_norm(1.0).clone()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        plan.grad_norm(1.0)
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = plan.grad_norm(1.0)
+    out.zero_()
+    graph.replay()
+    assert torch.equal(out, want)
+    with torch.cuda.stream(side):
+        plan.grad_norm(1.0, out=out)
+    torch.cuda.synchronize()
+    assert torch.equal(out, want)
