@@ -364,17 +364,26 @@ __device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&nr)[4], Unit
 }
 
 // BF16 parameters, stochastic: 16 random bits are added below the seven mantissa bits and the rest is cut off; one random
-// word serves elements 2i and 2i + 1 (a pair starts at an even position).  A lane that holds Inf or NaN rounds its eight to
-// nearest.  Returns the BF16 values.
+// word serves elements 2i and 2i + 1 (a pair starts at an even position).  Infinity, with nothing below those bits, stays as it
+// is; a NaN does once its lower bits, from which a carry could run into the sign, are cleared.  Returns the BF16 values.
 template <typename Where>
 __device__ __forceinline__ uint4 round_params(const float2 (&p)[4], UnitKeys k, Where where)
 {
-    if (!(max_abs8(p) < __uint_as_float(0x7f800000u))) return bf16_pack(p);
-    uint32_t w[4];
+    uint32_t w[4], b[8];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        b[2 * j] = __float_as_uint(p[j].x);
+        b[2 * j + 1] = __float_as_uint(p[j].y);
+    }
+    if (isnan(max_abs8(p))) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if ((b[j] & 0x7fffffffu) > 0x7f800000u) b[j] = 0x7fff0000u;
+    }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         const uint32_t x = random_word(where.half + Where::STEP / 2 * j, k.k1 ^ 0x5bd1e995u, k.k2), hi = x >> 16;
-        w[j] = __byte_perm(__float_as_uint(p[j].x) + ((x ^ hi) & 0xffffu), __float_as_uint(p[j].y) + hi, 0x7632);
+        w[j] = __byte_perm(b[2 * j] + ((x ^ hi) & 0xffffu), b[2 * j + 1] + hi, 0x7632);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
