@@ -255,8 +255,10 @@ TSR_API tsr_status tsr_dense_adamw(const tsr_dense_tensor *tensors, int32_t coun
  * two, not below 2^-126, with max |x| <= 448 S.  m and r have a scale each, FP32, in pairs.  The root
  * and not v itself is held because E4M3 spans 2^17: enough for a root, half of what a square needs.  A
  * root above zero is never held as zero (it would leave m / eps as the next update); it is held as
- * S 2^-9 at least.  New moments m and v below 2^-126 count as
- * zero.  A block with an entry that is not finite gets the scale NaN and reads as NaN.
+ * S 2^-9 at least.  The terms of a new m and v (b1 m, (1-b1) g and so on) and the moments themselves count as
+ * zero below 2^-126; everything else up to the stored bits is rounded as single IEEE FP32 operations, the root included.  A
+ * block with an entry that is not finite gets the scale NaN and reads as NaN.  A square beyond FP32 (|g| above 1.8e19) is
+ * such an entry, and makes its own parameter NaN at once.
  *
  * tsr_rounding says how values that are kept in fewer than 32 bits (BF16 parameters, E4M3 states) are
  * rounded.  To nearest even: a moment that changes by less than half a unit in its last place per step

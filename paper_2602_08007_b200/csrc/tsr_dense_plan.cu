@@ -255,11 +255,12 @@ __device__ __forceinline__ float rcp_approx(float x)
     return y;
 }
 
-// Minus the correctly rounded root of x = -nx, for x = 0 or x >= 2^-126, without a branch: with y ~ 1 / sqrt(x) from the
-// hardware's approximation, s = x y is the root to about 2^-22, and s + (x - s^2) y / 2 is one Newton step whose residual
-// the fused multiply-add forms exactly (Markstein's square root, IBM J. Res. Dev. 34, 1990).  Compared with __fsqrt_rn on
-// every positive FP32 number from 2^-126 on: equal.  Infinity gives NaN here; its block reads as NaN either way.  Everything
-// has its sign turned because a pair's sign costs two instructions, and the users of the root can turn a constant instead.
+// Minus the correctly rounded root of x = -nx, for x = 0 or 2^-102 <= x < infinity, without a branch: with y ~ 1 / sqrt(x)
+// from the hardware's approximation, s = x y is the root to about 2^-22, and s + (x - s^2) y / 2 is one Newton step whose residual
+// the fused multiply-add forms exactly (Markstein's square root, IBM J. Res. Dev. 34, 1990).  Between 2^-126 and 2^-102 the root may
+// be off by its last bit (a tenth are, at 2^-126): the residual then needs bits under 2^-149, the last that FP32 has.  Infinity
+// gives NaN; its block reads as NaN either way.  Everything has its sign turned because a pair's sign costs two instructions,
+// and the users of the root can turn a constant instead.
 __device__ __forceinline__ float2 minus_sqrt_pair(float2 nx)
 {
     float2 y;
@@ -268,6 +269,13 @@ __device__ __forceinline__ float2 minus_sqrt_pair(float2 nx)
     const float2 s = mul2(nx, y);                 // -s
     const float2 d = fma2(s, s, nx);              // s^2 - x
     return fma2(d, mul2(pair(0.5f), y), s);
+}
+
+// The same from 2^-126 on: small ones from 2^48 x.  Compared with __fsqrt_rn on all these numbers: equal.
+__device__ __forceinline__ float2 minus_sqrt_pair_any(float2 nx)
+{
+    const bool x = nx.x > -0x1p-98f, y = nx.y > -0x1p-98f;
+    return mul2(minus_sqrt_pair(mul2(nx, make_float2(x ? 0x1p48f : 1.f, y ? 0x1p48f : 1.f))), make_float2(x ? 0x1p-24f : 1.f, y ? 0x1p-24f : 1.f));
 }
 
 // FP32 state: moments in, moments out (the arithmetic of tsr_dense_adamw).
@@ -282,24 +290,26 @@ __device__ __forceinline__ void update_f32(float2 (&p)[4], const float2 (&g)[4],
     }
 }
 
-// 8-bit state: m and r = sqrt(v) in, as E4M3 values and their scales; new m and -r in FP32 out.  Every rounding on the way
+// 8-bit state: m and r = sqrt(v) in, as E4M3 values and their scales; new m, -v and -r in FP32 out (r as minus_sqrt_pair gives it).  Every rounding on the way
 // to the stored bits is one IEEE operation, so that they are well defined; the update itself takes the approximate
 // quotient.  (beta1 scale) code is exactly beta1 (scale code), scale being a power of two.
-__device__ __forceinline__ void update_q8(float2 (&p)[4], const float2 (&g)[4], float2 (&m)[4], float2 (&r)[4], float2 scale, const DenseStep &a, float lr,
-                                          float decay)
+__device__ __forceinline__ void update_q8(float2 (&p)[4], const float2 (&g)[4], float2 (&m)[4], float2 (&r)[4], float2 (&nv)[4], float2 scale, const DenseStep &a,
+                                          float lr, float decay)
 {
     const float b1s = __fmul_rn(a.sc.beta1, scale.x), rate = -__fmul_rn(lr, a.sc.inv_bc1);
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         m[j] = add_flush(mul2(pair(b1s), m[j]), mul2(pair(a.sc.omb1), g[j]));
         r[j] = mul2(pair(scale.y), r[j]);
-        r[j] = minus_sqrt_pair(add_flush(mul2(pair(-a.sc.beta2), mul2(r[j], r[j])), mul2(pair(-a.sc.omb2), mul2(g[j], g[j]))));
+        nv[j] = add_flush(mul2(pair(-a.sc.beta2), mul2(r[j], r[j])), mul2(pair(-a.sc.omb2), mul2(g[j], g[j])));
+        r[j] = minus_sqrt_pair(nv[j]);
         const float2 den = fma2(r[j], pair(-a.sqrt_inv_bc2), pair(a.sc.eps));
         p[j] = fma2(pair(rate), mul2(m[j], make_float2(rcp_approx(den.x), rcp_approx(den.y))), mul2(pair(decay), p[j]));
     }
 }
 
-// New scales of the warp's block, and the codes of m / scale and r / scale for the lane's eight (nr = -r).
+// New scales of the warp's block, and the codes of m / scale and r / scale for the lane's eight (nr = -r; unless ROUNDED, as
+// minus_sqrt_pair gives it for nv = -r^2).
 //
 // To nearest, the conversion instruction does it.  Stochastic: 2^-120 x / scale has the E4M3 code of x / scale in its bits 20
 // to 26, FP32's exponent field running as E4M3's does and its denormal numbers being E4M3's (both have a spacing of one unit
@@ -308,14 +318,22 @@ __device__ __forceinline__ void update_q8(float2 (&p)[4], const float2 (&g)[4], 
 //
 // A root above zero has code 1 at least.  That takes two instructions an element, and only a block that spans a factor of
 // 2^17 needs it: a warp without a root below 2^-9 scale skips them.
-template <bool SR, typename Where>
-__device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&nr)[4], UnitKeys k, Where where, uint2 &cm, uint2 &cr)
+// It asks for roots below 2^-51 as well, where minus_sqrt_pair may err: with a scale of 2^-42 or more these have code 1 whatever
+// their last bit, with a smaller one the roots are taken again.  v stays in registers for that (1B set stochastic: 1 % slower than
+// without; 3 % if squares are looked at, by a vote of its own, before any root is taken).
+template <bool SR, bool ROUNDED, typename Where>
+__device__ __forceinline__ float2 quantise(float2 (&m)[4], float2 (&nr)[4], const float2 (&nv)[4], UnitKeys k, Where where, uint2 &cm, uint2 &cr)
 {
     float2 scale, inv;
     block_scale(__float_as_uint(warp_max_abs(max_abs8(m))), scale.x, inv.x);
     block_scale(__float_as_uint(warp_max_abs(max_abs8(nr))), scale.y, inv.y);
     // (NaN, which compares false, needs no floor either)
-    const bool floor = __any_sync(0xffffffffu, max8(nr) > -0x1p-9f * scale.y);
+    const bool floor = __any_sync(0xffffffffu, max8(nr) > __fmaf_rn(-0x1p-9f, scale.y, -0x1p-51f));
+    if (!ROUNDED && floor && scale.y < 0x1p-42f && scale.y > 0x1p-126f) {   // (2^-126: all roots are zero)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) nr[j] = minus_sqrt_pair_any(nv[j]);
+        block_scale(__float_as_uint(warp_max_abs(max_abs8(nr))), scale.y, inv.y);
+    }
     if constexpr (SR) {
         uint32_t um[8], ur[8];
 #pragma unroll
@@ -582,7 +600,8 @@ __device__ __forceinline__ float2 update_pairs(Values &x, const DenseRec &t, int
     const bool both = t.flags & REC_PAIR_STATE;
 #pragma unroll
     for (int j = 0; j < 4; ++j) x.g[j] = mul2(x.g[j], pair(gs));
-    if constexpr (Q8) update_q8(x.p, x.g, x.m, x.v, x.scale, a, lr, decay);
+    float2 nv[4];
+    if constexpr (Q8) update_q8(x.p, x.g, x.m, x.v, nv, x.scale, a, lr, decay);
     else update_f32(x.p, x.g, x.m, x.v, a, lr, decay);
     const PairsFrom where = {(uint32_t)(base >> 1) + lane};
     if constexpr (SR && sizeof(PT) == 2) {
@@ -596,9 +615,9 @@ __device__ __forceinline__ float2 update_pairs(Values &x, const DenseRec &t, int
     if constexpr (Q8) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            if (!WHOLE && pair_at(base, lane, j >> 1) + (j & 1) >= t.n) at(x.m, j) = at(x.v, j) = 0.f;   // (0 * NaN of a poisoned block)
+            if (!WHOLE && pair_at(base, lane, j >> 1) + (j & 1) >= t.n) at(x.m, j) = at(x.v, j) = at(nv, j) = 0.f;   // (0 * NaN of a poisoned block)
         uint2 cm, cr;
-        scale = quantise<SR>(x.m, x.v, key, where, cm, cr);
+        scale = quantise<SR, false>(x.m, x.v, nv, key, where, cm, cr);
         store_code_pairs<WHOLE>(t.m, both, base, lane, t.n, cm);
         store_code_pairs<WHOLE>(t.v, both, base, lane, t.n, cr);
     } else {
@@ -715,7 +734,8 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
     {
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.g[j] = mul2(x.g[j], pair(gs));
-        if constexpr (Q8) update_q8(x.p, x.g, x.m, x.v, x.scale, a, lr, decay);
+        float2 nv[4];
+        if constexpr (Q8) update_q8(x.p, x.g, x.m, x.v, nv, x.scale, a, lr, decay);
         else update_f32(x.p, x.g, x.m, x.v, a, lr, decay);
         const EightFrom where = {half};
         if constexpr (SR && sizeof(PT) == 2) *(uint4 *)p = round_params(x.p, key, where);
@@ -723,7 +743,7 @@ template <typename PT, typename GT, bool Q8> struct VectorUnit {   // pointers t
         if (sizeof(PT) == 4 && image) Eight<bf16>::put(image, x.p);
         if constexpr (Q8) {
             uint2 cm, cr;
-            const float2 s = quantise<SR>(x.m, x.v, key, where, cm, cr);
+            const float2 s = quantise<SR, false>(x.m, x.v, nv, key, where, cm, cr);
             *(uint2 *)m = cm;
             *(uint2 *)v = cr;
             if (lane == 0) *scale = s;
@@ -874,7 +894,8 @@ __device__ __forceinline__ float2 step_shifted(char *slot, PT *to, bf16 *image, 
     next();
 #pragma unroll
     for (int j = 0; j < 4; ++j) x.g[j] = mul2(x.g[j], pair(gs));
-    update_q8(x.p, x.g, x.m, x.v, x.scale, a, lr, decay);
+    float2 nv[4];
+    update_q8(x.p, x.g, x.m, x.v, nv, x.scale, a, lr, decay);
     const EightFrom where = {half};
     if constexpr (sizeof(PT) == 2) {
         uint4 w;
@@ -890,7 +911,7 @@ __device__ __forceinline__ float2 step_shifted(char *slot, PT *to, bf16 *image, 
         }
     }
     uint2 cm, cr;
-    const float2 scale = quantise<SR>(x.m, x.v, key, where, cm, cr);
+    const float2 scale = quantise<SR, false>(x.m, x.v, nv, key, where, cm, cr);
     *(uint2 *)m = cm;
     *(uint2 *)v = cr;
     return scale;
@@ -1300,7 +1321,7 @@ __device__ __forceinline__ void copy_units(const DenseRec &d, const DenseRec &s,
         } else if constexpr (DQ && !SQ) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) at(v, j) = -__fsqrt_rn(at(v, j));
-            scale = quantise<false>(m, v, UnitKeys{0, 0}, EightFrom{0}, cm, cr);
+            scale = quantise<false, true>(m, v, v, UnitKeys{0, 0}, EightFrom{0}, cm, cr);
         }
         if constexpr (DQ && VEC) {
             *(uint2 *)((uint8_t *)d.m + e) = cm;
