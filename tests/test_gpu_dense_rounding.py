@@ -85,3 +85,36 @@ def test_a_bad_gradient_reaches_its_own_parameter_alone(tsr, bad, kind):
         out.append(p.float().cpu())
     same = torch.arange(n) != at
     assert torch.equal(out[0][same], out[1][same]) and not torch.isfinite(out[1][at])
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("kind", [torch.float32, F8])
+@pytest.mark.parametrize("gd", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("rows,cols,pitch", SHAPES)
+def test_parameters_are_cut_with_their_own_words(tsr, rows, cols, pitch, gd, kind, shift):
+    """A whole step: the FP32 result is within the error bound of the definition in 64 bits, and adding a parameter's own word
+    and cutting is monotonous in magnitude, so what is stored lies between the cut ends of that interval."""
+    n, seed, t = rows * cols, 1 << 40 | 12345, 3
+    h = dict(lr=f32(2e-3), beta1=f32(0.9), beta2=f32(0.99), eps=f32(1e-8), wd=f32(0.1), t=t)
+    p = rand(n, 1, 0.02).bfloat16()
+    g = (rand(n, 2) * torch.exp(2 * rand(n, 3) - 6)).to(gd)
+    xs, gs = ([placed(p, rows, cols, pitch, shift) for _ in (0, 1)], [placed(x, rows, cols, pitch, shift) for x in (g, g)])
+    plan = tsr.DensePlan(xs, gs, state_dtype=kind)
+    hy = lambda k: tsr.make_hyper(k, lr=h["lr"], beta1=h["beta1"], beta2=h["beta2"], eps=h["eps"], weight_decay=h["wd"])  # noqa: E731
+    plan.step(hy(2))       # moments that are not zero
+    before = [x.double().cpu().numpy().reshape(-1) for x in xs]
+    old = [[y.float().double().cpu().numpy() for y in s] for s in plan.states]
+    plan.step(hy(t), rounding=1, seed=seed)
+    for i in (0, 1):
+        m, v = old[i][:2]
+        if kind == F8:
+            scale = np.repeat(old[i][2].reshape(-1, 2), dm.BLOCK, axis=0)[:n]
+            m, v = m * scale[:, 0], (v * scale[:, 1]) ** 2
+        p1, _, _, tol, _, _ = dm.step64(before[i], g.double().numpy(), m, v, h)
+        u = words16(n, seed, t, i)
+        low = cut(np.maximum(np.abs(p1) - tol * (1 + 1e-6), 0.0), u)
+        high = cut(np.abs(p1) + tol * (1 + 1e-6), u)
+        got = xs[i].float().cpu().numpy().reshape(-1)
+        sure = np.abs(p1) > tol
+        assert np.all(np.signbit(got[sure]) == np.signbit(p1[sure]))
+        assert np.all((np.abs(got) >= low) & (np.abs(got) <= high))
