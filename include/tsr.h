@@ -308,14 +308,16 @@ TSR_API tsr_status tsr_dense_plan_bind(tsr_dense_plan *plan, const tsr_dense_ptr
 /* One AdamW step of every tensor that has neither flag.  hyper->scale is ignored and hyper->rule must be
  * TSR_RULE_ADAM.  grad_scale: NULL, or a DEVICE float that multiplies every gradient, such as out + 1 of
  * tsr_dense_plan_grad_norm; where it is not finite when the step runs, the step changes nothing.  seed is read for
- * TSR_ROUND_STOCHASTIC only. */
+ * TSR_ROUND_STOCHASTIC only.  A step captured in a CUDA graph repeats the hyper and the seed of its capture. */
 TSR_API tsr_status tsr_dense_plan_step(tsr_dense_plan *plan, const tsr_hyper *hyper, const float *grad_scale,
                                        int32_t rounding, uint64_t seed, void *stream);
 
 /* Global norm and clipping factor, on the device: out[0] = n = sqrt(sum of g^2 over all tensors but state-only
  * ones), out[1] = min(1, max_norm / (n + 1e-6)), or NaN where n is not a finite FP32 number.  max_norm > 0, may be
  * infinite.  The norms of one plan share partial sums in its workspace: two of them must not run at the same time, so put
- * them on one stream or order their streams by events (a captured norm by whoever replays it).  Sums are FP64 and in a fixed order: the same gradients give the same bits on the same kind of GPU. */
+ * them on one stream or order their streams by events (a captured norm by whoever replays it).  Groups of eight squares
+ * are summed in FP32 (relative error up to 9 * 2^-24; in FP64 where FP32 would over- or underflow), the rest in FP64, all in a
+ * fixed order: the same gradients at the same alignment and pitch give the same bits on the same kind of GPU. */
 TSR_API tsr_status tsr_dense_plan_grad_norm(tsr_dense_plan *plan, float max_norm, float *out, void *stream);
 
 /* Moments of src into dst, tensor by tensor, converted where the two keep them in different forms (rounded to nearest

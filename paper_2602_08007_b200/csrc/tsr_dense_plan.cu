@@ -7,9 +7,10 @@
 // that a block's maximum is one warp reduction -- and CHUNKS of up to 16 units per warp, one CTA each, listed in a table.
 //
 // Measured (B200, copy rate 6.53 TB/s; LLaMA-shaped sets, clipping factor on the device): FP32 state, 1B set with FP32 masters
-// and BF16 gradients 4.81 ms (6.9 TB/s); 8-bit state, 130M set in BF16 0.167 to 0.182 ms (6.1 to 6.6 TB/s), with FP32 parameters 0.235
-// (6.6 TB/s); stochastic, 1B set in BF16 2.45 to 2.65 ms (4.8 to 5.2 TB/s, bound by the integer and multiply pipes); gradient norm
-// of the 1B set 0.37 to 0.39 ms; state conversion of the 350M set 0.50 to 0.51 ms.  Small calls take 2.1 us on the device.
+// and BF16 gradients 4.81 ms (6.9 TB/s); 8-bit state, 130M set in BF16 0.169 to 0.182 ms (6.1 to 6.5 TB/s); stochastic, 1B set in
+// BF16 2.55 to 2.66 ms (4.8 to 5.0 TB/s, bound by instruction issue); gradient norm of the 1B set 0.37 to 0.39 ms; state conversion
+// of the 350M set 0.50 to 0.51 ms.  64 Mi elements, 8-bit state, BF16: 104 us to nearest, 131 stochastic; one element off the 16-byte
+// grid 134 and 174.  Small calls take 2.1 us on the device.
 #include <cuda_fp8.h>
 #include <math.h>
 #include <string.h>
