@@ -43,13 +43,15 @@ class DensePlan:
     images: per tensor None or a BF16 tensor that every step fills with the updated FP32 parameter.
     lr_mult, wd_mult: per-tensor factors on hyper.lr and hyper.weight_decay.
 
-    The tensors are taken as they lie: after replacing entries of .grads (or any other list), call bind().
+    The tensors are taken as they lie: after replacing entries of .grads (or any other list), call bind().  A plan over the .grad
+    of parameters goes on with the old tensors where torch's zero_grad has replaced them: use set_to_none=False.
 
     Calls go to torch's current stream, or to `stream`.  What the plan itself allocates (its tables, the result of grad_norm,
     zero states) is handed back to torch's allocator only after the work that the calls put on their streams; tensors of the
     caller need record_stream where they are dropped while another stream than their own uses them.  The norms of one plan
-    run one after the other, whatever their streams.  A captured graph holds addresses of the plan and of its tensors: keep the
-    plan, do not bind() it again while the graph is replayed, and let no norm of the plan run beside a replayed one."""
+    run one after the other, whatever their streams (the last one's stream has to exist when another takes over).  A captured
+    graph holds addresses of the plan and of its tensors, and repeats the hyper and the seed of its capture: keep the plan, do
+    not bind() it again while the graph is replayed, and let no norm of the plan run beside a replayed one."""
 
     def __init__(self, params: Optional[Sequence[torch.Tensor]], grads: Optional[Sequence[torch.Tensor]], states=None,
                  state_dtype=torch.float32, images=None, lr_mult: Optional[Sequence[float]] = None,
@@ -76,6 +78,7 @@ class DensePlan:
         self._lib = lib()
         self.states = self._zero_states(state_dtype) if states is None else [tuple(s) for s in states]
         self._made_states = states is None
+        self._home = _current_stream(self._index)      # on which the states and the result of grad_norm are allocated
         self.images = list(images) if images is not None else [None] * n
         self.lr_mult = [1.0] * n if lr_mult is None else [float(x) for x in lr_mult]
         self.wd_mult = [1.0] * n if wd_mult is None else [float(x) for x in wd_mult]
@@ -159,7 +162,8 @@ class DensePlan:
             self.workspace = torch.empty(size.value + 256, dtype=torch.uint8, device=self.device)
             # the device is idle after a binding: no norm to wait for
             self._norm_handle, self._norm_stream = None, None
-            self._met = set()      # streams that the allocator knows to use what the plan has allocated
+            # streams that the allocator knows to use what the plan has allocated
+            self._met = {self._home} if _current_stream(self._index) == self._home else set()
             at = (self.workspace.data_ptr() + 255) // 256 * 256
             self._check(lib().tsr_dense_plan_bind(self.ctx, (DensePtrs * max(n, 1))(*ptrs), n, at, size.value))
 
@@ -226,5 +230,5 @@ class DensePlan:
 
     def copy_state(self, src: "DensePlan", stream=None):
         """Takes over the moments of `src`, a plan over tensors of the same sizes, converting between FP32 and 8 bits."""
-        src._stream(stream)        # its tables are read there too
         self._check(self._lib.tsr_dense_plan_copy_state(self.ctx, src.ctx, self._stream(stream)))
+        src._stream(stream)        # its tables are read there too

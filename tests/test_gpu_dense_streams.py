@@ -139,3 +139,28 @@ def test_a_norm_is_captured_after_norms_on_other_streams(tsr):
         plan.grad_norm(1.0, out=out)
     torch.cuda.synchronize()
     assert torch.equal(out, want)
+
+
+def test_a_plan_made_on_a_side_stream_keeps_its_memory_too(tsr):
+    """Its memory belongs to the side stream; its calls are on the default one, which is held up when the plan is dropped."""
+    side = torch.cuda.Stream()
+    p, g = rand(300_000, 1), rand(300_000, 2)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        plan = tsr.DensePlan([p], [g], state_dtype=F8)
+        mine = spans([plan.workspace] + [t for s in plan.states for t in s])
+    q = p.clone()
+    torch.cuda.synchronize()
+    torch.cuda._sleep(BUSY)
+    plan.step(tsr.make_hyper(1))
+    done = torch.cuda.Event()
+    done.record()
+    del plan
+    with torch.cuda.stream(side):
+        others = [torch.empty(b - a, dtype=torch.uint8, device="cuda") for a, b in mine for _ in range(4)]
+    late = done.query()
+    clash = [(a, b) for a, b in spans(others) for c, d in mine if a < d and c < b]
+    torch.cuda.synchronize()
+    assert not late and not clash
+    tsr.DensePlan([q], [g], state_dtype=F8).step(tsr.make_hyper(1))
+    assert torch.equal(p, q)
