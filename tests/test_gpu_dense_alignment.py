@@ -112,3 +112,12 @@ def test_moments_off_their_alignment_in_millions_of_elements(tsr, pd, kind, rows
     """Enough for several blocks a warp and for thousands of entries in the plan's table."""
     for offsets in ((1, 1), (0, 3)):
         compare(tsr, rows, cols, kind, pd, torch.bfloat16, offsets, pitch, 1)
+
+
+@pytest.mark.parametrize("kind", [torch.float32, F8])
+def test_a_pitch_beyond_32_bits(tsr, kind):
+    """Rows 2^30 elements and more apart: chunks of eight blocks, too."""
+    if torch.cuda.mem_get_info()[0] < 40 << 30:
+        pytest.skip("needs 40 GB of free device memory")
+    for rows, cols in ((2, 3_000_000), (5, 300)):
+        compare(tsr, rows, cols, kind, torch.bfloat16, torch.bfloat16, (0, 0), (1 << 30) - cols + (rows == 2), 1)
