@@ -325,6 +325,93 @@ TSR_API tsr_status tsr_dense_plan_grad_norm(tsr_dense_plan *plan, float max_norm
  * agree in rows * cols and in whether they have a state. */
 TSR_API tsr_status tsr_dense_plan_copy_state(tsr_dense_plan *dst, const tsr_dense_plan *src, void *stream);
 
+/* ---- layers: what makes the gradients ---------------------------------------------------------- */
+
+/* The layers around the matrices that the optimizer steps, forward and backward, over token matrices with one row per token:
+ * a norm over rows, the linear layer with its epilogue, and dropout.  Their weight gradients go where the optimizer reads
+ * them: a bound G with its row pitch, a tensor of a dense plan, either written or added to (accumulation over micro batches).
+ *
+ *   - Matrices are row-major with a row pitch ld (elements, >= columns); pointers are aligned to their own element type.  Any
+ *     pitch and alignment is accepted; 16-byte aligned pointers and pitches are the fast case.  Activations (x, y, residual, pre,
+ *     their gradients) and the weight of a linear layer share one type, FP32 or BF16; vectors and weight gradients have types
+ *     of their own.  Sums, statistics and everything between load and store are FP32; results are rounded once.
+ *   - Buffers that are written must not overlap any other, except where a call says so.  Zero rows or columns are allowed.
+ *   - The calls need no context; they run on the current device, in stream order, and can be captured.  Scratch is
+ *     passed per call (256-byte aligned, DEVICE) and is free again when the call's work is done: two calls that may run at the
+ *     same time need one each.
+ *   - TSR_ERR_SHAPE: a negative size, ld < columns, a size beyond 2^31 - 1024 (rows of norm and dropout: 2^40).
+ *     TSR_ERR_UNSUPPORTED: an unknown type or activation.  TSR_ERR_INVALID_ARG: a missing pointer, a probability outside [0, 1], an
+ *     eps that is negative or not finite.  TSR_ERR_ALIGNMENT, TSR_ERR_WORKSPACE, TSR_ERR_CUDA as elsewhere. */
+
+typedef enum { TSR_ACT_NONE = 0, TSR_ACT_RELU = 1, TSR_ACT_GELU = 2 /* z Phi(z) */, TSR_ACT_GELU_TANH = 3, TSR_ACT_SILU = 4 } tsr_activation;
+
+/* A matrix on the device; data NULL: absent. */
+typedef struct { void *data; int64_t ld; } tsr_matrix;
+
+/* Dropout from a counter-based generator: entry (row, col) is zero with probability p' = round(65536 p) / 65536, decided by 16 bits
+ * that depend on (seed, offset, row, col) alone, and is multiplied by 1 / (1 - p') otherwise.  No mask is stored: the
+ * backward pass draws the same bits again, as does any other call with the same seed and offset.  step: NULL, or a
+ * DEVICE word that is added to offset when a kernel runs, so that a captured graph draws new bits at every replay. */
+typedef struct { float p; int32_t reserved; uint64_t seed, offset; const int64_t *step; } tsr_dropout_desc;
+
+/* Norm over the rows of x: with mu the mean of a row (center != 0; otherwise 0) and r = 1 / sqrt(mean((x - mu)^2) + eps),
+ *     y = (x - mu) r o weight + bias        (weight NULL: ones; bias NULL: zeros)
+ * stats (rows x 2, FP32, may be NULL) receives (mu, r) for the backward pass:  with h = (x - mu) r, g = dy o weight,
+ *     dx = r (g - center mean(g) - h mean(g o h)),   dweight = sum over rows of dy o h,   dbias = sum over rows of dy.
+ * y may be x itself, dx may be dy itself.  dx, dweight and dbias may each be NULL (not wanted). */
+typedef struct {
+    int64_t rows, cols;
+    int32_t dtype;        /* tsr_dtype of x, y, dy, dx                                   */
+    int32_t p_dtype;      /* ... of weight and bias                                      */
+    int32_t g_dtype;      /* ... of dweight and dbias                                    */
+    int32_t center;       /* 0 / 1                                                       */
+    int32_t accumulate;   /* dweight and dbias are added to                              */
+    float eps;
+} tsr_norm_desc;
+TSR_API tsr_status tsr_norm_forward(const tsr_norm_desc *desc, tsr_matrix x, const void *weight, const void *bias, tsr_matrix y,
+                                    float *stats, void *stream);
+/* Bytes of scratch of tsr_norm_backward. */
+TSR_API tsr_status tsr_norm_workspace_bytes(const tsr_norm_desc *desc, size_t *bytes);
+TSR_API tsr_status tsr_norm_backward(const tsr_norm_desc *desc, tsr_matrix dy, tsr_matrix x, const void *weight, const float *stats,
+                                     tsr_matrix dx, void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Linear layer, weight (outs x ins):
+ *     z = x weight^T + bias,   y = residual + dropout(act(z))
+ * bias, residual and pre may be absent; pre receives z (rounded), which the backward pass of a layer with an activation wants.
+ * y may be the residual itself.
+ * BF16 runs on the tensor cores with FP32 accumulation.  FP32 runs there as three TF32 products of the operands' high and
+ * low parts (about 21 bits of each operand); an infinite operand may come out as NaN.
+ * Backward:  dz = dropout(dy) o act'(pre) (rounded to the type of x, as an operand), dx = dz weight, dweight = dz^T x,
+ * dbias = sum over rows of dz (from FP32); the residual's gradient is dy.  dx, dweight and dbias may each be absent. */
+typedef struct {
+    int64_t rows, ins, outs;
+    int32_t dtype;        /* tsr_dtype of x, weight, residual, pre, y and of dy, dx      */
+    int32_t b_dtype;      /* ... of bias                                                 */
+    int32_t gw_dtype;     /* ... of dweight                                              */
+    int32_t gb_dtype;     /* ... of dbias                                                */
+    int32_t activation;   /* tsr_activation                                              */
+    int32_t accumulate;   /* dweight and dbias are added to                              */
+    tsr_dropout_desc dropout;  /* p = 0: none                                            */
+} tsr_linear_desc;
+typedef struct { tsr_matrix x, weight, residual, pre, y; const void *bias; } tsr_linear_io;
+typedef struct { tsr_matrix dy, x, weight, pre, dx, dweight; void *dbias; } tsr_linear_grads;
+/* Bytes of scratch of the call with these very arguments (they depend on the alignment of the matrices too). */
+TSR_API tsr_status tsr_linear_forward_bytes(const tsr_linear_desc *desc, const tsr_linear_io *io, size_t *bytes);
+TSR_API tsr_status tsr_linear_forward(const tsr_linear_desc *desc, const tsr_linear_io *io, void *workspace, size_t workspace_bytes,
+                                      void *stream);
+TSR_API tsr_status tsr_linear_backward_bytes(const tsr_linear_desc *desc, const tsr_linear_grads *io, size_t *bytes);
+TSR_API tsr_status tsr_linear_backward(const tsr_linear_desc *desc, const tsr_linear_grads *io, void *workspace, size_t workspace_bytes,
+                                       void *stream);
+
+/* y = residual + dropout(x) over rows x cols entries of one type; residual may be absent.  Without it, the same call on dy is
+ * the backward pass.  y may be x or the residual itself. */
+TSR_API tsr_status tsr_dropout(const tsr_dropout_desc *desc, int32_t dtype, int64_t rows, int64_t cols, tsr_matrix x, tsr_matrix residual,
+                               tsr_matrix y, void *stream);
+
+/* Reads and clears the status word of the layer calls on the current device (TSR_OK, or TSR_ERR_TIMEOUT if a bounded wait of a
+ * linear layer ran out since the last poll; its outputs are then undefined).  Synchronises `stream`; not for use in a capture. */
+TSR_API tsr_status tsr_layer_poll_status(int32_t *status, void *stream);
+
 /* ---- reporting -------------------------------------------------------------------------- */
 
 /* Section 3.2: bytes one worker would hand to the all-reduce in one step, summed over blocks:

@@ -10,3 +10,10 @@ from .binding import (  # noqa: F401
     lib, lib_path, make_hyper, dense_adamw, DenseTensor, project_core_static, STATIC_SCRATCH_FLOATS,
 )
 from .dense_plan import DensePlan  # noqa: F401
+from .binding import (  # noqa: F401
+    TSR_ACT_NONE, TSR_ACT_RELU, TSR_ACT_GELU, TSR_ACT_GELU_TANH, TSR_ACT_SILU, DropoutDesc, LinearDesc, LinearGrads, LinearIO, Matrix, NormDesc,
+)
+from .layers import (  # noqa: F401
+    Dropout, dropout, dropout_backward, dropout_forward, layer_norm, layer_poll_status, linear, linear_backward, linear_forward, norm_backward,
+    norm_forward, rms_norm,
+)

@@ -25,6 +25,7 @@ TSR_BLOCK_ONE_SIDED = 2
 TSR_STATE_F32, TSR_STATE_Q8 = 0, 1
 TSR_ROUND_NEAREST, TSR_ROUND_STOCHASTIC = 0, 1
 TSR_DENSE_NORM_ONLY, TSR_DENSE_STATE_ONLY = 1, 2
+TSR_ACT_NONE, TSR_ACT_RELU, TSR_ACT_GELU, TSR_ACT_GELU_TANH, TSR_ACT_SILU = 0, 1, 2, 3, 4
 DENSE_BLOCK = 256
 
 STATUS_NAMES = {
@@ -73,6 +74,33 @@ class Limits(ctypes.Structure):
                 ("starve_block", ctypes.c_int32), ("projection_launches", ctypes.c_int32)]
 
 
+class Matrix(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("ld", ctypes.c_int64)]
+
+
+class DropoutDesc(ctypes.Structure):
+    _fields_ = [("p", ctypes.c_float), ("reserved", ctypes.c_int32), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64), ("step", ctypes.c_void_p)]
+
+
+class NormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("dtype", ctypes.c_int32), ("p_dtype", ctypes.c_int32), ("g_dtype", ctypes.c_int32),
+                ("center", ctypes.c_int32), ("accumulate", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("ins", ctypes.c_int64), ("outs", ctypes.c_int64), ("dtype", ctypes.c_int32), ("b_dtype", ctypes.c_int32),
+                ("gw_dtype", ctypes.c_int32), ("gb_dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("accumulate", ctypes.c_int32),
+                ("dropout", DropoutDesc)]
+
+
+class LinearIO(ctypes.Structure):
+    _fields_ = [("x", Matrix), ("weight", Matrix), ("residual", Matrix), ("pre", Matrix), ("y", Matrix), ("bias", ctypes.c_void_p)]
+
+
+class LinearGrads(ctypes.Structure):
+    _fields_ = [("dy", Matrix), ("x", Matrix), ("weight", Matrix), ("pre", Matrix), ("dx", Matrix), ("dweight", Matrix), ("dbias", ctypes.c_void_p)]
+
+
 EXPORTS = [
     "tsr_version", "tsr_status_string", "tsr_last_error", "tsr_create", "tsr_destroy", "tsr_workspace_bytes",
     "tsr_bind", "tsr_bases_changed", "tsr_init_subspace", "tsr_project_core", "tsr_adam_core_step",
@@ -83,7 +111,9 @@ EXPORTS = [
     "tsr_set_profiling", "tsr_get_stage_ms", "tsr_launch_count", "tsr_project_core_static", "tsr_dense_adamw",
     "tsr_set_limits", "tsr_refresh_gram", "tsr_dense_plan_create", "tsr_dense_plan_destroy",
     "tsr_dense_plan_last_error", "tsr_dense_plan_workspace_bytes", "tsr_dense_plan_bind", "tsr_dense_plan_step",
-    "tsr_dense_plan_grad_norm", "tsr_dense_plan_copy_state",
+    "tsr_dense_plan_grad_norm", "tsr_dense_plan_copy_state", "tsr_norm_forward", "tsr_norm_workspace_bytes", "tsr_norm_backward",
+    "tsr_linear_forward_bytes", "tsr_linear_forward", "tsr_linear_backward_bytes", "tsr_linear_backward", "tsr_dropout",
+    "tsr_layer_poll_status",
 ]
 
 
@@ -153,6 +183,16 @@ def lib():
         L.tsr_dense_plan_step.argtypes = [vp, P(Hyper), vp, i32, u64, vp]
         L.tsr_dense_plan_grad_norm.argtypes = [vp, ctypes.c_float, vp, vp]
         L.tsr_dense_plan_copy_state.argtypes = [vp, vp, vp]
+        sz = ctypes.c_size_t
+        L.tsr_norm_forward.argtypes = [P(NormDesc), Matrix, vp, vp, Matrix, vp, vp]
+        L.tsr_norm_workspace_bytes.argtypes = [P(NormDesc), P(sz)]
+        L.tsr_norm_backward.argtypes = [P(NormDesc), Matrix, Matrix, vp, vp, Matrix, vp, vp, vp, sz, vp]
+        L.tsr_linear_forward_bytes.argtypes = [P(LinearDesc), P(LinearIO), P(sz)]
+        L.tsr_linear_forward.argtypes = [P(LinearDesc), P(LinearIO), vp, sz, vp]
+        L.tsr_linear_backward_bytes.argtypes = [P(LinearDesc), P(LinearGrads), P(sz)]
+        L.tsr_linear_backward.argtypes = [P(LinearDesc), P(LinearGrads), vp, sz, vp]
+        L.tsr_dropout.argtypes = [P(DropoutDesc), i32, i64, i64, Matrix, Matrix, Matrix, vp]
+        L.tsr_layer_poll_status.argtypes = [P(i32), vp]
         _lib = L
     return _lib
 

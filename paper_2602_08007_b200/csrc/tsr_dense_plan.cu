@@ -166,12 +166,7 @@ __device__ __forceinline__ void block_scale(uint32_t absmax_bits, float &scale, 
 }
 
 // Random words: 32-bit multiply-xorshift mixing of (element + key1), with a second key between the two multiplications
-// so that the words of two tensors or steps are not shifted copies of one sequence.  The multipliers are those of the
-// 32-bit finaliser of MurmurHash3 (A. Appleby, public domain).
-__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x)
-{
-    x ^= x >> 16; x *= 0x85ebca6bu; x ^= x >> 13; x *= 0xc2b2ae35u; return x ^ (x >> 16);
-}
+// so that the words of two tensors or steps are not shifted copies of one sequence (mix32 and its multipliers: tsr_device.cuh).
 // The word before its last step x ^ (x >> 16): the upper half is final, the lower one is still to be combined with it.
 // (Sharing x >> 16 among the lane's neighbours, which differ in it only across a carry, was measured: 3 % slower.)
 __device__ __forceinline__ uint32_t random_word(uint32_t counter, uint32_t key1, uint32_t key2)

@@ -30,4 +30,11 @@ __device__ __forceinline__ float core_update_elem(float c, float &m1, float &m2,
     return __fdividef(mh, __fadd_rn(sqrt_approx(vh), sc.eps));
 }
 
+// 32-bit mixing by multiplications and xor-shifts, the base of the library's counter-based random words.  The multipliers
+// are those of the 32-bit finaliser of MurmurHash3 (A. Appleby, public domain).
+__host__ __device__ __forceinline__ uint32_t mix32(uint32_t x)
+{
+    x ^= x >> 16; x *= 0x85ebca6bu; x ^= x >> 13; x *= 0xc2b2ae35u; return x ^ (x >> 16);
+}
+
 }  // namespace tsr

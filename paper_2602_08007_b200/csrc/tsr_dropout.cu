@@ -1,0 +1,92 @@
+// y = residual + dropout(x): one pass, bound by HBM (formulas in tsr.h; the random words in tsr_layers.cuh).  A thread takes eight
+// neighbours of a row: four words, one key of the row.  Matrices off the 16-byte grid go entry by entry, lanes side by side.
+#include <algorithm>
+
+#include "tsr_layers.cuh"
+
+namespace tsr {
+
+struct DropoutArgs {
+    const void *x, *res;
+    void *y;
+    int64_t ldx, ldr, ldy, rows;
+    int32_t cols, units;        // units per row: of eight entries (VEC), or single ones
+    DropArgs drop;
+};
+
+template <typename T, bool VEC, bool RES>
+__global__ void __launch_bounds__(256)
+dropout_kernel(const DropoutArgs a)
+{
+    pdl_trigger();
+    pdl_wait();
+    const uint32_t call_key = drop_call_key(a.drop);
+    const int64_t total = a.rows * a.units;
+    const bool small = total < ((int64_t)1 << 32);
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
+        const int64_t r = small ? (int64_t)((uint32_t)u / (uint32_t)a.units) : u / a.units;
+        const uint32_t c = (uint32_t)(u - r * a.units) * (VEC ? 8u : 1u);
+        const T *x = (const T *)a.x + r * a.ldx + c;
+        const T *res = (const T *)a.res + r * a.ldr + c;
+        T *y = (T *)a.y + r * a.ldy + c;
+        const DropRow key = drop_row_key(call_key, r);
+        if (VEC) {
+            float v[8], o[8];
+            load8(x, v);
+            if (RES) load8(res, o);
+#pragma unroll
+            for (int j = 0; j < 8; j += 2) {
+                const uint32_t w = drop_word(key, (c + j) >> 1);
+                v[j] = drop_lo(w, v[j], a.drop);
+                v[j + 1] = drop_hi(w, v[j + 1], a.drop);
+                if (RES) { v[j] += o[j]; v[j + 1] += o[j + 1]; }
+            }
+            store8(y, v);
+        } else {
+            float v = drop_entry(key, c, load_f(x), a.drop);
+            if (RES) v += load_f(res);
+            store_f(y, v);
+        }
+    }
+}
+
+template <typename T>
+static cudaError_t dropout_as(const DropoutArgs &a, bool vec, int sms, cudaStream_t s)
+{
+    const dim3 grid((unsigned)std::min<int64_t>((a.rows * a.units + 255) / 256, (int64_t)sms * 64));
+    if (a.res) return vec ? launch_dependent(dropout_kernel<T, true, true>, grid, dim3(256), 0, s, 1, a) : launch_dependent(dropout_kernel<T, false, true>, grid, dim3(256), 0, s, 1, a);
+    return vec ? launch_dependent(dropout_kernel<T, true, false>, grid, dim3(256), 0, s, 1, a) : launch_dependent(dropout_kernel<T, false, false>, grid, dim3(256), 0, s, 1, a);
+}
+
+}  // namespace tsr
+
+using namespace tsr;
+
+extern "C" tsr_status tsr_dropout(const tsr_dropout_desc *desc, int32_t dtype, int64_t rows, int64_t cols, tsr_matrix x, tsr_matrix residual, tsr_matrix y, void *stream)
+{
+    DropoutArgs a = {};
+    if (!desc) return TSR_ERR_INVALID_ARG;
+    if (!type_ok(dtype)) return TSR_ERR_UNSUPPORTED;
+    if (rows < 0 || cols < 0 || rows > (int64_t)1 << 40 || cols > 0x7fffffff - 1023) return TSR_ERR_SHAPE;
+    if (!drop_args(*desc, &a.drop)) return TSR_ERR_INVALID_ARG;
+    const tsr_matrix *all[3] = {&x, &residual, &y};
+    const int es = type_bytes(dtype);
+    bool vec = cols % 8 == 0;
+    for (int i = 0; i < 3; ++i) {
+        const tsr_matrix &m = *all[i];
+        if (!m.data) {
+            if (i != 1 && rows > 0 && cols > 0) return TSR_ERR_INVALID_ARG;
+            continue;
+        }
+        if (!extent_ok(rows, cols, m.ld)) return TSR_ERR_SHAPE;
+        if (!aligned_to(m.data, es)) return TSR_ERR_ALIGNMENT;
+        vec = vec && aligned_to(m.data, 16) && (rows <= 1 || m.ld * es % 16 == 0);
+    }
+    if (rows == 0 || cols == 0) return TSR_OK;
+    const int sms = device_sms();
+    if (!sms) return TSR_ERR_CUDA;
+    a.x = x.data; a.ldx = x.ld; a.res = residual.data; a.ldr = residual.ld; a.y = y.data; a.ldy = y.ld;
+    a.rows = rows; a.cols = (int)cols; a.units = vec ? (int)(cols / 8) : (int)cols;
+    const cudaError_t e = dtype == TSR_BF16 ? dropout_as<bf16>(a, vec, sms, (cudaStream_t)stream) : dropout_as<float>(a, vec, sms, (cudaStream_t)stream);
+    return e == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
+}

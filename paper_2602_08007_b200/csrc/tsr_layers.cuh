@@ -1,0 +1,160 @@
+// What the layer operators (norm, linear, dropout) share: the random words of dropout, activations and their slopes, typed
+// loads and stores, and the sum of column partials.
+#pragma once
+#include "tsr_device.cuh"
+#include "tsr_internal.h"
+#include "tsr_pdl.cuh"
+
+namespace tsr {
+
+// ---- dropout ----------------------------------------------------------------------------------------------------------
+//
+// Entry (row, col) of a matrix falls iff its 16 random bits are below threshold = round(65536 p); the others are multiplied by
+// 65536 / (65536 - threshold), so that the mean is kept for the probability that is drawn.  Two entries share a 32-bit word, a function of
+// (seed, offset, row, col / 2) alone: every kernel that holds an entry, in whatever layout, draws the same bits, and no mask
+// is stored.  A row has two keys, as the rows' words would otherwise be shifted copies of one sequence.
+struct DropArgs {
+    uint32_t threshold;      // 0: nothing falls (and nothing is drawn); 65536: everything
+    float scale;
+    uint32_t seed_key;       // from the seed, on the host
+    uint64_t offset;
+    const int64_t *step;     // NULL, or a device word added to offset when the kernel runs
+};
+struct DropRow { uint32_t k1, k2; };
+
+__device__ __forceinline__ uint32_t drop_call_key(const DropArgs &d)
+{
+    const uint64_t o = d.offset + (d.step ? (uint64_t)*(const volatile int64_t *)d.step : 0ull);
+    const uint32_t k = mix32(d.seed_key ^ mix32((uint32_t)o + 0x7f4a7c15u));
+    return mix32(k ^ ((uint32_t)(o >> 32) * 0x85ebca77u));
+}
+__device__ __forceinline__ DropRow drop_row_key(uint32_t call_key, int64_t row)
+{
+    DropRow r;
+    r.k1 = mix32(call_key ^ mix32((uint32_t)row + 0x9e3779b9u * ((uint32_t)((uint64_t)row >> 32) + 1u)));
+    r.k2 = mix32(r.k1 ^ 0xa511e9b3u);
+    return r;
+}
+// The word of columns 2 c and 2 c + 1 (low and high half).
+__device__ __forceinline__ uint32_t drop_word(const DropRow &r, uint32_t c)
+{
+    uint32_t x = c + r.k1;
+    x ^= x >> 16;
+    x *= 0x85ebca6bu;
+    x = x ^ (x >> 13) ^ r.k2;
+    x *= 0xc2b2ae35u;
+    return x ^ (x >> 16);
+}
+// A selection, not a product with zero: an entry that falls is zero whatever it was.
+__device__ __forceinline__ float drop_lo(uint32_t w, float x, const DropArgs &d) { return (w & 0xffffu) < d.threshold ? 0.f : x * d.scale; }
+__device__ __forceinline__ float drop_hi(uint32_t w, float x, const DropArgs &d) { return (w >> 16) < d.threshold ? 0.f : x * d.scale; }
+__device__ __forceinline__ float drop_entry(const DropRow &r, uint32_t col, float x, const DropArgs &d)
+{
+    const uint32_t w = drop_word(r, col >> 1);
+    return (col & 1u) ? drop_hi(w, x, d) : drop_lo(w, x, d);
+}
+
+// Host: checks and prepares; false on a bad probability.
+bool drop_args(const tsr_dropout_desc &d, DropArgs *out);
+
+// ---- activations ------------------------------------------------------------------------------------------------------
+// expf and erff with their full FP32 accuracy: FP32 layers are held to it, and the epilogues that call them run beside the MMAs.
+__device__ __forceinline__ float sigmoid_f(float x) { return __fdividef(1.f, 1.f + expf(-x)); }
+
+__device__ __forceinline__ float act_value(int act, float z)
+{
+    switch (act) {
+    case TSR_ACT_RELU: return z < 0.f ? 0.f : z;      // (NaN stays)
+    case TSR_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678f));
+    case TSR_ACT_GELU_TANH: return z * sigmoid_f(1.59576912f * fmaf(0.044715f * z * z, z, z));   // (1 + tanh u) / 2 = sigmoid(2 u)
+    case TSR_ACT_SILU: return z * sigmoid_f(z);
+    default: return z;
+    }
+}
+// Derivative.  Beyond the clamps it is 0 or 1 to FP32 accuracy, and products of an infinity with zero are kept out; NaN stays.
+__device__ __forceinline__ float act_slope(int act, float z)
+{
+    float s;
+    switch (act) {
+    case TSR_ACT_RELU: s = z > 0.f ? 1.f : 0.f; break;
+    case TSR_ACT_GELU: {
+        const float c = fminf(fmaxf(z, -16.f), 16.f);
+        s = fmaf(c * 0.39894228f, expf(-0.5f * c * c), 0.5f * (1.f + erff(c * 0.70710678f)));
+        break;
+    }
+    case TSR_ACT_GELU_TANH: {
+        const float c = fminf(fmaxf(z, -16.f), 16.f), c2 = c * c;
+        const float g = sigmoid_f(1.59576912f * fmaf(0.044715f * c2, c, c));
+        s = fmaf(c * g * (1.f - g), 1.59576912f * fmaf(0.134145f, c2, 1.f), g);
+        break;
+    }
+    case TSR_ACT_SILU: {
+        const float c = fminf(fmaxf(z, -100.f), 100.f), g = sigmoid_f(c);
+        s = g * fmaf(c, 1.f - g, 1.f);
+        break;
+    }
+    default: return 1.f;
+    }
+    return z != z ? z : s;
+}
+
+// ---- typed access -----------------------------------------------------------------------------------------------------
+__device__ __forceinline__ float load_f(const float *p) { return *p; }
+__device__ __forceinline__ float load_f(const bf16 *p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float load_as(const void *p, int64_t i, bool is_bf16)
+{
+    return is_bf16 ? __bfloat162float(((const bf16 *)p)[i]) : ((const float *)p)[i];
+}
+__device__ __forceinline__ void store_as(void *p, int64_t i, bool is_bf16, float v)
+{
+    if (is_bf16) ((bf16 *)p)[i] = __float2bfloat16_rn(v);
+    else ((float *)p)[i] = v;
+}
+__device__ __forceinline__ void store_f(float *p, float v) { *p = v; }
+__device__ __forceinline__ void store_f(bf16 *p, float v) { *p = __float2bfloat16_rn(v); }
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
+{
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *(const uint32_t *)&h;
+}
+// Eight consecutive entries; p aligned to 16 bytes.
+__device__ __forceinline__ void unpack8(const uint4 &r, float (&v)[8])
+{
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void load8(const bf16 *p, float (&v)[8]) { unpack8(*(const uint4 *)p, v); }
+__device__ __forceinline__ void load8(const float *p, float (&v)[8])
+{
+    const float4 a = *(const float4 *)p, b = *(const float4 *)(p + 4);
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ void store8(bf16 *p, const float (&v)[8])
+{
+    *(uint4 *)p = make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+}
+__device__ __forceinline__ void store8(float *p, const float (&v)[8])
+{
+    *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
+    *(float4 *)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// ---- host helpers -----------------------------------------------------------------------------------------------------
+inline int type_bytes(int32_t dtype) { return dtype == TSR_BF16 ? 2 : 4; }
+inline bool type_ok(int32_t dtype) { return dtype == TSR_F32 || dtype == TSR_BF16; }
+inline bool aligned_to(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+// a pitch that a tensor map can hold, and rows * ld entries that stay addressable in 63 bits
+inline bool extent_ok(int64_t rows, int64_t cols, int64_t ld)
+{
+    return ld >= cols && ld < ((int64_t)1 << 37) && (rows <= 1 || rows <= ((int64_t)1 << 56) / (ld > 0 ? ld : 1));
+}
+
+int device_sms();   // multiprocessors of the current device (looked up once per device); 0 without one
+
+// Sums of column partials: out[c] (= or +=) sum over p < parts of partial[p * ldp + c], in order of p.  Two sets at once (out2 may
+// be NULL; its partials follow the first set's `parts` rows).
+cudaError_t column_finish(const float *partial, int parts, int64_t ldp, int64_t cols, void *out, bool out_bf16, void *out2, bool out2_bf16,
+                          bool accumulate, cudaStream_t stream);
+
+}  // namespace tsr
