@@ -1,8 +1,8 @@
 // Linear layer: host side of its products (operand preparation, choice of tiles, split of K) and the kernels around them.
 // Formulas in tsr.h; the products themselves are in tsr_linear_gemm.cu.
 //
-//   linear_pack_kernel     BF16 operand whose pitch or address TMA does not take -> workspace with a 16-byte pitch (one pass over it)
-//   linear_split_kernel    FP32 operand -> high and low TF32 planes, K-major (transposed where the product contracts over rows)
+//   linear_pack_kernel     BF16 operand whose pitch or address TMA does not take -> workspace with a 128-byte pitch (one pass over it)
+//   linear_split_kernel    FP32 operand -> three BF16 planes whose sum it is
 //   linear_dz_kernel       dz = dropout(dy) o act'(pre) and the column sums of dz (the bias's gradient), one pass over dy and pre
 //   linear_finish_kernel   split K: slabs added in order, then the epilogue
 //   column_finish_kernel   partial column sums added in order (bias, and the norm's weight and bias)
@@ -16,6 +16,43 @@ namespace tsr {
 
 // ---- kernels ----------------------------------------------------------------------------------------------------------
 
+// Eight entries from an address of any alignment: the two 16-byte granules that hold them (each holds one of them at least, so neither
+// lies outside of what may be read), shifted into place.
+__device__ __forceinline__ uint4 load8_any(const bf16 *p)
+{
+    const uint32_t m = (uint32_t)(uintptr_t)p & 15u;
+    const uint4 *base = (const uint4 *)((uintptr_t)p & ~(uintptr_t)15);
+    const uint4 a = base[0];
+    if (m == 0) return a;
+    const uint4 b = base[1];
+    uint32_t w[5];
+    switch (m >> 2) {
+    case 0: w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; break;
+    case 1: w[0] = a.y; w[1] = a.z; w[2] = a.w; w[3] = b.x; w[4] = b.y; break;
+    case 2: w[0] = a.z; w[1] = a.w; w[2] = b.x; w[3] = b.y; w[4] = b.z; break;
+    default: w[0] = a.w; w[1] = b.x; w[2] = b.y; w[3] = b.z; w[4] = b.w; break;
+    }
+    const uint32_t s = (m & 2u) * 8u;
+    return make_uint4(__funnelshift_r(w[0], w[1], s), __funnelshift_r(w[1], w[2], s), __funnelshift_r(w[2], w[3], s), __funnelshift_r(w[3], w[4], s));
+}
+// The same of FP32 entries: plain loads, whose address a vector of four may not fit.
+__device__ __forceinline__ void load8_any(const bf16 *p, float (&v)[8]) { unpack8(load8_any(p), v); }
+__device__ __forceinline__ void load8_any(const float *p, float (&v)[8])
+{
+    if (((uintptr_t)p & 15) == 0) load8(p, v);
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p[i];
+    }
+}
+// ... of which n < 8 exist; the others are zero.
+template <typename T>
+__device__ __forceinline__ void load8_part(const T *p, int n, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? load_f(p + i) : 0.f;
+}
+
 // dst[r][0 .. cols) = src[r][..]; dst has a pitch of whole 16-byte units.  A thread writes one unit of eight entries.
 __global__ void __launch_bounds__(256)
 linear_pack_kernel(const bf16 *__restrict__ src, int64_t lds, bf16 *__restrict__ dst, int64_t ldd, int64_t rows, int cols, int units)
@@ -23,136 +60,141 @@ linear_pack_kernel(const bf16 *__restrict__ src, int64_t lds, bf16 *__restrict__
     pdl_trigger();
     pdl_wait();
     const int64_t total = rows * units;
+    const bool small = total < ((int64_t)1 << 32);
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
-        const int64_t r = u / units;
+        const int64_t r = small ? (int64_t)((uint32_t)u / (uint32_t)units) : u / units;
         const int c = (int)(u - r * units) * 8;
         const bf16 *s = src + r * lds + c;
-        uint32_t w[4];
-        if (c + 8 <= cols) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] = (uint32_t)__bfloat16_as_ushort(s[2 * i]) | ((uint32_t)__bfloat16_as_ushort(s[2 * i + 1]) << 16);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[i] = c + 2 * i < cols ? (uint32_t)__bfloat16_as_ushort(s[2 * i]) : 0u;
-                if (c + 2 * i + 1 < cols) w[i] |= (uint32_t)__bfloat16_as_ushort(s[2 * i + 1]) << 16;
-            }
+        bf16 *d = dst + r * ldd + c;
+        if (c + 8 <= cols) *(uint4 *)d = load8_any(s);
+        else {
+            for (int i = 0; i < cols - c; ++i) d[i] = s[i];
         }
-        *(uint4 *)(dst + r * ldd + c) = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
-// x = high + low: high is x rounded to TF32 (10 stored mantissa bits, to nearest with ties away from zero), low the remainder, rounded
-// the same way: together 2^-22 of x.  Values that would round to infinity keep their leading bits; an infinity or NaN has no remainder.
-__device__ __forceinline__ float tf32_round(float x)
+// x = p1 + p2 + p3 in BF16: each the rounded remainder of those before, 24 bits together (an entry below 2^-110 loses the bits that fall
+// below 2^-133).  A value that would round to infinity keeps its leading bits; an infinity or NaN has no remainder.
+__device__ __forceinline__ void split3(float x, bf16 (&p)[3])
 {
     const uint32_t b = __float_as_uint(x);
-    const uint32_t r = (b + 0x1000u) & 0xffffe000u;
-    const bool keep = (b & 0x7f800000u) == 0x7f800000u;               // infinity or NaN
-    const bool over = (r & 0x7f800000u) == 0x7f800000u;
-    return keep ? x : __uint_as_float(over ? (b & 0xffffe000u) : r);
+    const bool special = (b & 0x7f800000u) == 0x7f800000u;
+    p[0] = __float2bfloat16_rn(x);
+    if (!special && (__float_as_uint(__bfloat162float(p[0])) & 0x7f800000u) == 0x7f800000u) p[0] = __ushort_as_bfloat16((unsigned short)(b >> 16));
+    const float r1 = special ? 0.f : x - __bfloat162float(p[0]);
+    p[1] = __float2bfloat16_rn(r1);
+    p[2] = __float2bfloat16_rn(r1 - __bfloat162float(p[1]));
 }
-__device__ __forceinline__ void tf32_split(float x, float &hi, float &lo)
-{
-    hi = tf32_round(x);
-    lo = (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u ? 0.f : tf32_round(x - hi);
-}
-
-// src: rows x cols of a row-major FP32 matrix; dst: planes (high, then low) of `prow` rows each, pitch ldd.  TRANS: plane[c][r] = src[r][c].
-template <bool TRANS>
+// dst: three planes of rows x ldd, `plane` entries apart.  A thread takes eight neighbours of a row.
 __global__ void __launch_bounds__(256)
-linear_split_kernel(const float *__restrict__ src, int64_t lds, float *__restrict__ dst, int64_t ldd, int64_t prow, int rows, int cols)
+linear_split_kernel(const float *__restrict__ src, int64_t lds, bf16 *__restrict__ dst, int64_t ldd, int64_t plane, int64_t rows, int cols, int units)
 {
-    __shared__ float tile[32][33];
     pdl_trigger();
     pdl_wait();
-    const int tc = (cols + 31) / 32;
-    const int64_t tiles = (int64_t)((rows + 31) / 32) * tc;
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    for (int64_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        const int r0 = (int)(t / tc) * 32, c0 = (int)(t % tc) * 32;
+    const int64_t total = rows * units;
+    const bool small = total < ((int64_t)1 << 32);
+    for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
+        const int64_t r = small ? (int64_t)((uint32_t)u / (uint32_t)units) : u / units;
+        const int c = (int)(u - r * units) * 8;
+        const float *s = src + r * lds + c;
+        float v[8];
+        if (c + 8 <= cols) load8_any(s, v);
+        else load8_part(s, cols - c, v);
+        uint32_t w[3][4];
 #pragma unroll
-        for (int i = y; i < 32; i += 8) {
-            const int r = r0 + i, c = c0 + x;
-            const float v = r < rows && c < cols ? src[(int64_t)r * lds + c] : 0.f;
-            if (TRANS) tile[i][x] = v;
-            else if (r < rows && c < cols) {
-                float hi, lo;
-                tf32_split(v, hi, lo);
-                dst[(int64_t)r * ldd + c] = hi;
-                dst[(prow + r) * ldd + c] = lo;
-            }
-        }
-        if (TRANS) {
-            __syncthreads();
+        for (int i = 0; i < 4; ++i) {
+            bf16 a[3], b[3];
+            split3(v[2 * i], a);
+            split3(v[2 * i + 1], b);
 #pragma unroll
-            for (int i = y; i < 32; i += 8) {
-                const int r = c0 + i, c = r0 + x;      // row and column of the planes
-                if (r < cols && c < rows) {
-                    float hi, lo;
-                    tf32_split(tile[x][i], hi, lo);
-                    dst[(int64_t)r * ldd + c] = hi;
-                    dst[(prow + r) * ldd + c] = lo;
-                }
-            }
-            __syncthreads();
+            for (int k = 0; k < 3; ++k) w[k][i] = (uint32_t)__bfloat16_as_ushort(a[k]) | ((uint32_t)__bfloat16_as_ushort(b[k]) << 16);
         }
+        // (the pitch is whole units: what is written past the last column is zero and lies in the padding)
+#pragma unroll
+        for (int k = 0; k < 3; ++k) *(uint4 *)(dst + k * plane + r * ldd + c) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
     }
 }
 
-// Slabs (rows x ld, FP32) of a split product, added in order, then the epilogue.  splits = 0: the sum is zero (K = 0).
+// Split tiles: the slabs of a tile (tile_m x width, FP32, one behind the other) are added in order, then the epilogue runs.  With `slabs` NULL the
+// sum is zero and the tiles cover the whole matrix (K = 0).  A thread takes four neighbours of a row.
 struct FinishArgs {
+    LinearTiles g;
     const float *slabs;
-    int64_t slab_rows, ld;
-    int32_t splits, M, N, out_f32;     // out_f32: type of out, residual and pre
+    int32_t tile_m, tail, out_f32;     // tiles that were split; type of out, residual and pre
+    int32_t vec;                       // four neighbours of out, residual and pre can be moved at once
     LinearEpilogue e;
 };
+template <typename T>
+__device__ __forceinline__ void store4(T *p, const float (&v)[4], int n, bool vec)
+{
+    if (vec && n == 4) {
+        if (sizeof(T) == 2) *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+        else *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) if (j < n) store_f(p + j, v[j]);
+    }
+}
+template <typename T>
 __global__ void __launch_bounds__(256)
-linear_finish_kernel(const FinishArgs a)
+linear_finish_kernel(const __grid_constant__ FinishArgs a)
 {
     pdl_trigger();
     pdl_wait();
     const LinearEpilogue &e = a.e;
-    const bool b16 = !a.out_f32;
-    const int units = (a.N + 3) / 4;
-    const int64_t total = (int64_t)a.M * units;
+    const uint32_t per_row = a.g.width / 4, per_tile = a.tile_m * per_row;
+    const int64_t total = (int64_t)a.tail * per_tile;
     const uint32_t call_key = e.drop.threshold ? drop_call_key(e.drop) : 0u;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
-        const int64_t r = u / units;
-        const int c = (int)(u - r * units) * 4;
+        const int tail = (int)(u / per_tile);
+        const uint32_t in = (uint32_t)(u - (int64_t)tail * per_tile), rr = in / per_row, cc = (in - rr * per_row) * 4;
+        int m0, n0;
+        linear_tile_at(a.g, a.g.whole + tail, a.tile_m, m0, n0);
+        const int64_t r = m0 + (int64_t)rr;
+        const int c = n0 + (int)cc, n = min(4, a.g.N - c);
+        if (r >= a.g.M || n <= 0) continue;
         float v[4] = {0.f, 0.f, 0.f, 0.f};
-        const float *s = a.slabs + r * a.ld + c;
+        if (a.slabs) {
+            const float *s = a.slabs + (int64_t)tail * a.g.splits * a.tile_m * a.g.width + (int64_t)in * 4;
 #pragma unroll 4
-        for (int p = 0; p < a.splits; ++p) {
-            const float4 x = *(const float4 *)(s + p * a.slab_rows * a.ld);
-            v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+            for (int p = 0; p < a.g.splits; ++p) {
+                const float4 x = *(const float4 *)(s + (int64_t)p * a.tile_m * a.g.width);
+                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+            }
         }
-        const DropRow key = e.drop.threshold ? drop_row_key(call_key, r) : DropRow{0, 0};
+        if (e.bias) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            if (c + j >= a.N) break;
-            float z = v[j];
-            if (e.bias) z += load_as(e.bias, c + j, e.bias_bf16);
-            if (e.pre) store_as(e.pre, r * e.ldp + c + j, b16, z);
-            z = act_value(e.act, z);
-            if (e.drop.threshold) z = drop_entry(key, (uint32_t)(c + j), z, e.drop);
-            if (e.res) z += load_as(e.res, r * e.ldr + c + j, b16);
-            store_as(e.out, r * e.ldo + c + j, b16, z);
+            for (int j = 0; j < 4; ++j) if (j < n) v[j] += load_as(e.bias, c + j, e.bias_bf16);
         }
+        if (e.pre) store4((T *)e.pre + r * e.ldp + c, v, n, a.vec);
+        if (e.act) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = act_value(e.act, v[j]);
+        }
+        if (e.drop.threshold) {
+            const DropRow key = drop_row_key(call_key, r);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = drop_entry(key, (uint32_t)(c + j), v[j], e.drop);
+        }
+        if (e.res) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (j < n) v[j] += load_f((const T *)e.res + r * e.ldr + c + j);
+        }
+        store4((T *)e.out + r * e.ldo + c, v, n, a.vec);
     }
 }
 
-// dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns (side by side where VEC: everything
-// is in whole, aligned vectors; 32 apart otherwise), a warp every eighth row.  dz NULL: the sums alone.
+// dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row.  dy and pre
+// may lie at any alignment, dz has a pitch of whole 16-byte units.  dz NULL: the sums alone.
 struct DzArgs {
     const void *dy, *pre;
     void *dz;
-    float *partial;            // [gridDim.y][ldp], NULL: no sums
-    int64_t lddy, ldpre, lddz, ldp, rows;
+    float *partial;            // [gridDim.y][cols], NULL: no sums
+    int64_t lddy, ldpre, lddz, rows;
     int32_t cols, rows_per, act;
     DropArgs drop;
 };
-template <typename T, bool VEC>
+template <typename T>
 __global__ void __launch_bounds__(256)
 linear_dz_kernel(const DzArgs a)
 {
@@ -160,69 +202,51 @@ linear_dz_kernel(const DzArgs a)
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int c0 = blockIdx.x * 256 + (VEC ? lane * 8 : lane);
+    const int c0 = blockIdx.x * 256 + lane * 8, n = a.cols - c0;
     const int64_t r0 = (int64_t)blockIdx.y * a.rows_per, r1 = min(a.rows, r0 + a.rows_per);
     const uint32_t call_key = a.drop.threshold ? drop_call_key(a.drop) : 0u;
     float acc[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = 0.f;
-    if (c0 < a.cols) {
+    if (n > 0) {
 #pragma unroll 2
         for (int64_t r = r0 + warp; r < r1; r += 8) {
             const T *dy = (const T *)a.dy + r * a.lddy + c0;
-            const T *pre = (const T *)a.pre + r * a.ldpre + c0;
-            float g[8], z[8];
-            if (VEC) {
-                load8(dy, g);
-                if (a.act) load8(pre, z);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] = c0 + 32 * j < a.cols ? load_f(dy + 32 * j) : 0.f;
-                if (a.act) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) z[j] = c0 + 32 * j < a.cols ? load_f(pre + 32 * j) : 0.f;
-                }
-            }
+            float g[8];
+            if (n >= 8) load8_any(dy, g);
+            else load8_part(dy, n, g);
             if (a.act) {
+                const T *pre = (const T *)a.pre + r * a.ldpre + c0;
+                float z[8];
+                if (n >= 8) load8_any(pre, z);
+                else load8_part(pre, n, z);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) g[j] *= act_slope(a.act, z[j]);
             }
             if (a.drop.threshold) {      // last, as a selection: what fell is zero whatever pre holds
                 const DropRow key = drop_row_key(call_key, r);
-                if (VEC) {
 #pragma unroll
-                    for (int j = 0; j < 8; j += 2) {
-                        const uint32_t w = drop_word(key, (uint32_t)(c0 + j) >> 1);
-                        g[j] = drop_lo(w, g[j], a.drop);
-                        g[j + 1] = drop_hi(w, g[j + 1], a.drop);
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) g[j] = drop_entry(key, (uint32_t)(c0 + 32 * j), g[j], a.drop);
+                for (int j = 0; j < 8; j += 2) {
+                    const uint32_t w = drop_word(key, (uint32_t)(c0 + j) >> 1);
+                    g[j] = drop_lo(w, g[j], a.drop);
+                    g[j + 1] = drop_hi(w, g[j + 1], a.drop);
                 }
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[j] += g[j];
-            if (a.dz) {
-                T *dz = (T *)a.dz + r * a.lddz + c0;
-                if (VEC) store8(dz, g);
-                else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) if (c0 + 32 * j < a.cols) store_f(dz + 32 * j, g[j]);
-                }
-            }
+            if (a.dz) store8((T *)a.dz + r * a.lddz + c0, g);     // (past the last column: zeros, into the padding)
         }
     }
     if (!a.partial) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[warp][VEC ? lane * 8 + j : lane + 32 * j] = acc[j];
+    for (int j = 0; j < 8; ++j) sums[warp][lane * 8 + j] = acc[j];
     __syncthreads();
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c < a.cols) {
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
-        a.partial[blockIdx.y * a.ldp + c] = s;
+        a.partial[(int64_t)blockIdx.y * a.cols + c] = s;
     }
 }
 
@@ -306,16 +330,16 @@ EncodeTiledFn encoder()
     return fn;
 }
 
-// Row-major matrix, boxes of 128 bytes x box_rows with the 128-byte swizzle.
-bool encode(CUtensorMap *out, const void *base, int64_t rows, int64_t cols, int64_t ld, bool f32, int box_rows)
+// Row-major matrix, boxes of 128 bytes x box_rows with the 128-byte swizzle; planes > 1: that many of them, `plane` entries apart, in one box.
+bool encode(CUtensorMap *out, const void *base, int64_t rows, int64_t cols, int64_t ld, bool f32, int box_rows, int planes = 1, int64_t plane = 0)
 {
     EncodeTiledFn fn = encoder();
     if (!fn) return false;
     const int es = f32 ? 4 : 2;
     if (rows <= 1) ld = round_up(cols, 16 / es);         // a single row has no pitch
-    const cuuint64_t dims[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)ld * es};
-    const cuuint32_t box[2] = {(cuuint32_t)(128 / es), (cuuint32_t)box_rows}, step[2] = {1, 1};
-    return fn(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(base), dims, strides, box, step,
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)ld * es, (cuuint64_t)plane * es};
+    const cuuint32_t box[3] = {(cuuint32_t)(128 / es), (cuuint32_t)box_rows, (cuuint32_t)planes}, step[3] = {1, 1, 1};
+    return fn(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, planes > 1 ? 3 : 2, const_cast<void *>(base), dims, strides, box, step,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -331,31 +355,41 @@ struct Product {
     LinearEpilogue e;    // out, res, pre, bias with their pitches
 };
 
-struct Shape { int cg, width, splits, kb_per, kb_total; int64_t m_tiles, n_tiles; };
+struct Shape { int cg, width, splits, kb, kb_per; int64_t m_tiles, n_tiles, whole, tail; };   // tail: tiles that are split
 
-// Tile shape and split of K by a model in SM clocks.  A K block of 128 bytes costs the MMAs 2 width clocks (6 x as much
-// for the three FP32 products), and the SM's intake of 64 bytes a clock its share of the operands; a wave of tiles costs that
-// times the blocks of a split; a split pays for its slabs (about 3000 bytes a clock over all SMs) and for another launch.
+// Tile shape and split of K by a model in SM clocks.  A K block of 64 entries costs the MMAs 2 width clocks (six times that for FP32) and the SM's
+// intake of 64 bytes a clock its share of the operands; a wave of tiles costs the larger one times its blocks.  The tiles of the last wave
+// (and, where that is nearly full, of the one before) may be split, so that the last wave is short: for that their slabs are
+// written (32 bytes a clock and SM) and read again (3000 bytes a clock in all) by another launch.
 Shape choose(const Product &p, int sms)
 {
     Shape best = {};
     double best_cost = 1e300;
-    const int bk = p.f32 ? 32 : 64;
-    const int kb = (int)((p.K + bk - 1) / bk);
+    const int kb = (int)((p.K + 63) / 64);
     static const struct { int cg, width; } kinds[] = {{2, 256}, {2, 192}, {2, 128}, {2, 64}, {1, 128}, {1, 64}};
     for (const auto &k : kinds) {
-        const int64_t mt = (p.M + 128 * k.cg - 1) / (128 * k.cg), nt = (p.N + k.width - 1) / k.width;
+        if (p.f32 && k.width > 128) continue;
+        const int64_t mt = (p.M + 128 * k.cg - 1) / (128 * k.cg), nt = (p.N + k.width - 1) / k.width, tiles = mt * nt;
         const int slots = sms / k.cg;
-        const double mma = (p.f32 ? 6.0 : 2.0) * k.width, intake = (p.f32 ? 2.0 : 1.0) * 2.0 * (128 + k.width / k.cg);
-        const double per_kb = std::max(mma, intake);
-        const int most = (int)std::min<int64_t>(std::max(1, kb / 2), std::max<int64_t>(1, 2 * slots / std::max<int64_t>(1, mt * nt)));
-        for (int want = 1; want <= most; ++want) {
-            const int per = (kb + want - 1) / want, s = (kb + per - 1) / per;
-            if (s != want) continue;
-            const double waves = (double)((mt * nt * s + slots - 1) / slots);
-            double cost = 3000.0 + waves * (per * per_kb + 300.0) + 12.0 * k.width;
-            if (s > 1) cost += 5000.0 + (double)s * (double)p.M * (double)p.N * 8.0 / 3000.0;
-            if (cost < best_cost) { best_cost = cost; best = {k.cg, k.width, s, per, kb, mt, nt}; }
+        const double mma = (p.f32 ? 12.0 : 2.0) * k.width, intake = (p.f32 ? 6.0 : 2.0) * (128 + k.width / k.cg);
+        const int stage = (p.f32 ? 3 : 1) * 128 * (128 + k.width / k.cg), stages = linear_stages(stage, p.e.pre != nullptr);
+        // (with a single stage loads and MMAs take turns)
+        const double per_kb = stages > 1 ? std::max(mma, intake) : mma + intake + 1000.0, tile = kb * per_kb + 300.0, last = 3000.0 + 12.0 * k.width;
+        const int64_t full = tiles / slots, rem = tiles % slots;
+        auto offer = [&](double cost, int64_t tail, int s, int per) {
+            if (cost < best_cost) { best_cost = cost; best = {k.cg, k.width, s, kb, per, mt, nt, tiles - tail, tail}; }
+        };
+        offer(last + (double)(full + (rem ? 1 : 0)) * tile, 0, 1, kb);
+        for (int extra = 0; extra < 2; ++extra) {
+            const int64_t tail = rem + (extra ? slots : 0);
+            if (tail == 0 || tail > tiles) continue;
+            const int most = (int)std::min<int64_t>(kb / 2, 2 * slots / tail + 1);
+            for (int want = 2; want <= most; ++want) {
+                const int per = (kb + want - 1) / want, s = (kb + per - 1) / per;
+                if (s != want) continue;
+                const double waves = (double)((tail * s + slots - 1) / slots), slab = 128.0 * k.width * 4;
+                offer(last + (double)((tiles - tail) / slots) * tile + waves * (per * per_kb + 300.0 + slab / 32.0) + 4000.0 + (double)tail * s * slab * k.cg / 3000.0, tail, s, per);
+            }
         }
     }
     return best;
@@ -372,94 +406,92 @@ struct Room {      // walks the workspace; with base NULL it only counts
     }
 };
 
-// The product's scratch, and (run) its launches.  Slabs come last, so that two products after one another can share `room` from there on.
+// The product's scratch, and (run) its launches.
 tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t stream)
 {
     if (p.M == 0 || p.N == 0) return TSR_OK;
+    const int os = p.out_f32 ? 4 : 2;
+    const bool out_tma = tma_takes(p.e.out, p.M, p.e.ldo, os), res_tma = p.e.res && tma_takes(p.e.res, p.M, p.e.ldr, os), pre_tma = p.e.pre && tma_takes(p.e.pre, p.M, p.e.ldp, os);
     FinishArgs f = {};
-    f.M = (int)p.M; f.N = (int)p.N; f.out_f32 = p.out_f32;
+    f.out_f32 = p.out_f32;
     f.e = p.e;
+    f.vec = out_tma && (!p.e.pre || pre_tma);
     auto finish = [&]() -> tsr_status {
-        const int64_t units = p.M * ((p.N + 3) / 4);
-        const unsigned blocks = (unsigned)std::min<int64_t>((units + 255) / 256, (int64_t)sms * 16);
-        return launch_dependent(linear_finish_kernel, dim3(blocks), dim3(256), 0, stream, 1, f) == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
+        const int64_t units = (int64_t)f.tail * f.tile_m * (f.g.width / 4);
+        const dim3 grid((unsigned)std::min<int64_t>((units + 255) / 256, (int64_t)sms * 16));
+        const cudaError_t rc = f.out_f32 ? launch_dependent(linear_finish_kernel<float>, grid, dim3(256), 0, stream, 1, f) : launch_dependent(linear_finish_kernel<bf16>, grid, dim3(256), 0, stream, 1, f);
+        return rc == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
     };
-    if (p.K == 0) return run ? finish() : TSR_OK;
+    if (p.K == 0) {
+        f.tile_m = 128;
+        f.g.M = (int)p.M; f.g.N = (int)p.N; f.g.width = 64;
+        const int64_t mt = (p.M + 127) / 128, nt = (p.N + 63) / 64;
+        if (mt * nt > (int64_t)1 << 30) return TSR_ERR_SHAPE;
+        f.g.m_tiles = (int)mt; f.g.n_tiles = (int)nt; f.tail = (int)(mt * nt);
+        return run ? finish() : TSR_OK;
+    }
 
     const Shape s = choose(p, sms);
-    if (s.m_tiles * s.n_tiles * s.splits > (int64_t)1 << 30) return TSR_ERR_SHAPE;
-    const int es = p.f32 ? 4 : 2;
+    if (s.m_tiles * s.n_tiles > (int64_t)1 << 28) return TSR_ERR_SHAPE;
     LinearGemm g = {};
     g.M = (int)p.M; g.N = (int)p.N;
-    g.kb_total = s.kb_total; g.kb_per = s.kb_per;
-    g.width = s.width; g.m_tiles = (int)s.m_tiles; g.n_tiles = (int)s.n_tiles; g.tiles = (int)(s.m_tiles * s.n_tiles * s.splits);
+    g.width = s.width; g.m_tiles = (int)s.m_tiles; g.n_tiles = (int)s.n_tiles;
+    g.whole = (int)s.whole; g.splits = s.splits; g.items = (int)(s.whole + s.tail * s.splits);
+    g.kb_total = s.kb; g.kb_per = s.kb_per;
 
     // operands
+    const int planes = p.f32 ? 3 : 1;
     const Operand *op[2] = {&p.A, &p.B};
     const int64_t extent[2] = {p.M, p.N};
-    const int kbox[2] = {128, s.width / s.cg};            // rows of a K-major box
     for (int i = 0; i < 2; ++i) {
         const Operand &o = *op[i];
         const int64_t rows = o.mn ? p.K : extent[i], cols = o.mn ? extent[i] : p.K;    // as stored
-        CUtensorMap *map = i ? &g.tmB : &g.tmA;
-        if (p.f32) {
-            const int64_t ld = round_up(p.K, 4);
-            float *planes = (float *)room.take((size_t)2 * extent[i] * ld * 4);
-            if (run) {
-                const int64_t tiles = ((rows + 31) / 32) * ((cols + 31) / 32);
-                const dim3 grid((unsigned)std::min<int64_t>(tiles, (int64_t)sms * 32));
-                const cudaError_t rc = o.mn ? launch_dependent(linear_split_kernel<true>, grid, dim3(256), 0, stream, 1, (const float *)o.p, o.ld, planes, ld, extent[i], (int)rows, (int)cols)
-                                            : launch_dependent(linear_split_kernel<false>, grid, dim3(256), 0, stream, 1, (const float *)o.p, o.ld, planes, ld, extent[i], (int)rows, (int)cols);
-                if (rc != cudaSuccess) return TSR_ERR_CUDA;
-                if (!encode(map, planes, 2 * extent[i], p.K, ld, true, kbox[i])) return TSR_ERR_CUDA;
-            }
-            (i ? g.b_plane_rows : g.a_plane_rows) = (int)extent[i];
-            continue;
-        }
         const void *at = o.p;
-        int64_t ld = o.ld;
-        if (!tma_takes(o.p, rows, o.ld, es)) {
-            ld = round_up(cols, 8);
-            bf16 *packed = (bf16 *)room.take((size_t)rows * ld * 2);
+        int64_t ld = o.ld, plane = 0;
+        if (p.f32 || !tma_takes(o.p, rows, o.ld, 2)) {
+            ld = round_up(cols, 64);
+            plane = rows * ld;
+            bf16 *copy = (bf16 *)room.take((size_t)planes * plane * 2);
             if (run) {
-                const int units = (int)(ld / 8);
+                const int units = (int)((cols + 7) / 8);
                 const dim3 grid((unsigned)std::min<int64_t>((rows * units + 255) / 256, (int64_t)sms * 32));
-                if (launch_dependent(linear_pack_kernel, grid, dim3(256), 0, stream, 1, (const bf16 *)o.p, o.ld, packed, ld, rows, (int)cols, units) != cudaSuccess) return TSR_ERR_CUDA;
+                const cudaError_t rc = p.f32 ? launch_dependent(linear_split_kernel, grid, dim3(256), 0, stream, 1, (const float *)o.p, o.ld, copy, ld, plane, rows, (int)cols, units)
+                                             : launch_dependent(linear_pack_kernel, grid, dim3(256), 0, stream, 1, (const bf16 *)o.p, o.ld, copy, ld, rows, (int)cols, units);
+                if (rc != cudaSuccess) return TSR_ERR_CUDA;
             }
-            at = packed;
+            at = copy;
         }
-        if (run && !encode(map, at, rows, cols, ld, false, o.mn ? 64 : kbox[i])) return TSR_ERR_CUDA;
+        const int box_rows = o.mn ? 64 : i ? s.width / s.cg : 128;
+        if (run && !encode(i ? &g.tmB : &g.tmA, at, rows, cols, ld, false, box_rows, planes, plane)) return TSR_ERR_CUDA;
         (i ? g.b_mn : g.a_mn) = o.mn;
     }
-    const int planes = p.f32 ? 2 : 1;
     g.b_boxes = (s.width / s.cg + 63) / 64;
-    g.stage_tx = (uint32_t)(s.cg * planes * 128 * 128 + (g.b_mn ? s.cg * g.b_boxes * 8192 : planes * s.width * 128));
+    const int a_bytes = planes * 128 * 128, b_bytes = planes * (g.b_mn ? g.b_boxes * 8192 : s.width / s.cg * 128);
+    g.b_offset = a_bytes;
+    g.stage_bytes = a_bytes + b_bytes;
+    g.stage_tx = (uint32_t)(s.cg * g.stage_bytes);
+    g.stages = linear_stages(g.stage_bytes, p.e.pre != nullptr);
 
-    if (s.splits > 1) {
-        f.slab_rows = round_up(p.M, 32);
-        f.ld = round_up(p.N, 4);
-        f.splits = s.splits;
-        float *slabs = (float *)room.take((size_t)s.splits * f.slab_rows * f.ld * 4);
-        if (!run) return TSR_OK;
-        f.slabs = slabs;
-        g.slab_rows = (int)f.slab_rows;
-        g.whole_edge = 1;
-        g.e.out = slabs; g.e.ldo = f.ld; g.e.out_tma = 1;
-        if (!encode(&g.tmOut, slabs, s.splits * f.slab_rows, p.N, f.ld, true, 32)) return TSR_ERR_CUDA;
-        if (linear_gemm_launch(g, s.cg, p.f32, true, sms, stream) != cudaSuccess) return TSR_ERR_CUDA;
-        return finish();
-    }
+    float *slabs = s.tail ? (float *)room.take((size_t)s.tail * s.splits * 128 * s.cg * s.width * 4) : nullptr;
     if (!run) return TSR_OK;
+    if (s.tail && !encode(&g.tmSlab, slabs, s.tail * s.splits * 128 * s.cg, s.width, s.width, true, 32)) return TSR_ERR_CUDA;
     g.e = p.e;
-    const int os = p.out_f32 ? 4 : 2;
     g.whole_edge = p.N * os % 16 == 0;
-    g.e.out_tma = tma_takes(p.e.out, p.M, p.e.ldo, os);
-    if (g.e.out_tma && !encode(&g.tmOut, p.e.out, p.M, p.N, p.e.ldo, p.out_f32, 32)) return TSR_ERR_CUDA;
-    g.e.res_tma = p.e.res && tma_takes(p.e.res, p.M, p.e.ldr, os);
-    if (g.e.res_tma && !encode(&g.tmRes, p.e.res, p.M, p.N, p.e.ldr, p.out_f32, 32)) return TSR_ERR_CUDA;
-    g.e.pre_tma = p.e.pre && tma_takes(p.e.pre, p.M, p.e.ldp, os);
-    if (g.e.pre_tma && !encode(&g.tmPre, p.e.pre, p.M, p.N, p.e.ldp, p.out_f32, 32)) return TSR_ERR_CUDA;
-    return linear_gemm_launch(g, s.cg, p.f32, p.out_f32, sms, stream) == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
+    if (s.whole) {
+        g.e.out_tma = out_tma;
+        g.e.res_tma = res_tma;
+        g.e.pre_tma = pre_tma;
+        if (out_tma && !encode(&g.tmOut, p.e.out, p.M, p.N, p.e.ldo, p.out_f32, 32)) return TSR_ERR_CUDA;
+        if (res_tma && !encode(&g.tmRes, p.e.res, p.M, p.N, p.e.ldr, p.out_f32, 32)) return TSR_ERR_CUDA;
+        if (pre_tma && !encode(&g.tmPre, p.e.pre, p.M, p.N, p.e.ldp, p.out_f32, 32)) return TSR_ERR_CUDA;
+    }
+    if (linear_gemm_launch(g, s.cg, p.f32, p.out_f32, sms, stream) != cudaSuccess) return TSR_ERR_CUDA;
+    if (!s.tail) return TSR_OK;
+    f.g = g;
+    f.slabs = slabs;
+    f.tile_m = 128 * s.cg;
+    f.tail = (int)s.tail;
+    return finish();
 }
 
 constexpr int64_t MOST = 0x7fffffff - 1023;
@@ -469,8 +501,6 @@ tsr_status check_desc(const tsr_linear_desc &d, DropArgs *drop)
     if (!type_ok(d.dtype) || !type_ok(d.b_dtype) || !type_ok(d.gw_dtype) || !type_ok(d.gb_dtype)) return TSR_ERR_UNSUPPORTED;
     if (d.activation < TSR_ACT_NONE || d.activation > TSR_ACT_SILU) return TSR_ERR_UNSUPPORTED;
     if (d.rows < 0 || d.ins < 0 || d.outs < 0 || d.rows > MOST || d.ins > MOST || d.outs > MOST) return TSR_ERR_SHAPE;
-    // two FP32 planes of an operand, or the slabs of a split, are addressed by 32-bit row numbers
-    if (d.dtype == TSR_F32 && (d.rows > MOST / 2 || d.ins > MOST / 2 || d.outs > MOST / 2)) return TSR_ERR_SHAPE;
     if (!drop_args(d.dropout, drop)) return TSR_ERR_INVALID_ARG;
     return TSR_OK;
 }
@@ -559,7 +589,7 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
         }
         Room room = {run ? (char *)workspace : nullptr, 0};
         if (make_dz) {
-            dz.ld = round_up(O, 16 / (f32 ? 4 : 2));
+            dz.ld = round_up(O, 64);
             dz.data = room.take((size_t)T * dz.ld * (f32 ? 4 : 2));
         }
         float *partial = db ? (float *)room.take((size_t)parts * O * 4) : nullptr;
@@ -568,16 +598,11 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             a.dy = io->dy.data; a.lddy = io->dy.ld;
             a.pre = io->pre.data; a.ldpre = io->pre.ld;
             a.dz = make_dz ? dz.data : nullptr; a.lddz = dz.ld;
-            a.partial = partial; a.ldp = O;
+            a.partial = partial;
             a.rows = T; a.cols = (int)O; a.rows_per = (int)rows_per; a.act = d->activation;
             a.drop = drop;
-            const int es = f32 ? 4 : 2;
-            bool vec = O % 8 == 0 && aligned_to(a.dy, 16) && (a.lddy * es) % 16 == 0;
-            if (d->activation) vec = vec && aligned_to(a.pre, 16) && (a.ldpre * es) % 16 == 0;
             const dim3 grid((unsigned)col_blocks, (unsigned)parts);
-            cudaError_t rc;
-            if (f32) rc = vec ? launch_dependent(linear_dz_kernel<float, true>, grid, dim3(256), 0, stream, 1, a) : launch_dependent(linear_dz_kernel<float, false>, grid, dim3(256), 0, stream, 1, a);
-            else rc = vec ? launch_dependent(linear_dz_kernel<bf16, true>, grid, dim3(256), 0, stream, 1, a) : launch_dependent(linear_dz_kernel<bf16, false>, grid, dim3(256), 0, stream, 1, a);
+            const cudaError_t rc = f32 ? launch_dependent(linear_dz_kernel<float>, grid, dim3(256), 0, stream, 1, a) : launch_dependent(linear_dz_kernel<bf16>, grid, dim3(256), 0, stream, 1, a);
             if (rc != cudaSuccess) return TSR_ERR_CUDA;
         }
         if (run && db && column_finish(partial, T ? (int)parts : 0, O, O, io->dbias, d->gb_dtype == TSR_BF16, nullptr, false, d->accumulate != 0, stream) != cudaSuccess) return TSR_ERR_CUDA;
