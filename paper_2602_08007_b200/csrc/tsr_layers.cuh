@@ -58,8 +58,22 @@ __device__ __forceinline__ float drop_entry(const DropRow &r, uint32_t col, floa
 bool drop_args(const tsr_dropout_desc &d, DropArgs *out);
 
 // ---- activations ------------------------------------------------------------------------------------------------------
-// expf and erff with their full FP32 accuracy: FP32 layers are held to it, and the epilogues that call them run beside the MMAs.
-__device__ __forceinline__ float sigmoid_f(float x) { return __fdividef(1.f, 1.f + expf(-x)); }
+// The exponential and the reciprocal come from the special-function units (2^-22 of the value, and for the exponential 2^-24 of the argument on
+// top): below what FP32 products of a layer lose anyway, and a third of the instructions of the full forms, in kernels bound by them.
+__device__ __forceinline__ float rcp_f(float x)
+{
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ float sigmoid_f(float x) { return rcp_f(1.f + __expf(-x)); }
+// Limits |x| to `most`; NaN stays.
+__device__ __forceinline__ float limited(float x, float most)
+{
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(x), "f"(-most));
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(x) : "f"(x), "f"(most));
+    return x;
+}
 
 __device__ __forceinline__ float act_value(int act, float z)
 {
@@ -71,31 +85,26 @@ __device__ __forceinline__ float act_value(int act, float z)
     default: return z;
     }
 }
-// Derivative.  Beyond the clamps it is 0 or 1 to FP32 accuracy, and products of an infinity with zero are kept out; NaN stays.
+// Derivative.  Beyond the limits it is 0 or 1 to FP32 accuracy, and products of an infinity with zero are kept out; NaN stays.
 __device__ __forceinline__ float act_slope(int act, float z)
 {
-    float s;
     switch (act) {
-    case TSR_ACT_RELU: s = z > 0.f ? 1.f : 0.f; break;
+    case TSR_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
     case TSR_ACT_GELU: {
-        const float c = fminf(fmaxf(z, -16.f), 16.f);
-        s = fmaf(c * 0.39894228f, expf(-0.5f * c * c), 0.5f * (1.f + erff(c * 0.70710678f)));
-        break;
+        const float c = limited(z, 16.f);
+        return fmaf(c * 0.39894228f, __expf(-0.5f * c * c), 0.5f * (1.f + erff(c * 0.70710678f)));
     }
     case TSR_ACT_GELU_TANH: {
-        const float c = fminf(fmaxf(z, -16.f), 16.f), c2 = c * c;
+        const float c = limited(z, 16.f), c2 = c * c;
         const float g = sigmoid_f(1.59576912f * fmaf(0.044715f * c2, c, c));
-        s = fmaf(c * g * (1.f - g), 1.59576912f * fmaf(0.134145f, c2, 1.f), g);
-        break;
+        return fmaf(c * g * (1.f - g), 1.59576912f * fmaf(0.134145f, c2, 1.f), g);
     }
     case TSR_ACT_SILU: {
-        const float c = fminf(fmaxf(z, -100.f), 100.f), g = sigmoid_f(c);
-        s = g * fmaf(c, 1.f - g, 1.f);
-        break;
+        const float c = limited(z, 80.f), g = sigmoid_f(c);
+        return g * fmaf(c, 1.f - g, 1.f);
     }
     default: return 1.f;
     }
-    return z != z ? z : s;
 }
 
 // ---- typed access -----------------------------------------------------------------------------------------------------

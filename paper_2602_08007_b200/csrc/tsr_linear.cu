@@ -191,10 +191,10 @@ struct DzArgs {
     void *dz;
     float *partial;            // [gridDim.y][cols], NULL: no sums
     int64_t lddy, ldpre, lddz, rows;
-    int32_t cols, rows_per, act;
+    int32_t cols, rows_per;
     DropArgs drop;
 };
-template <typename T>
+template <typename T, int ACT>
 __global__ void __launch_bounds__(256)
 linear_dz_kernel(const DzArgs a)
 {
@@ -215,13 +215,13 @@ linear_dz_kernel(const DzArgs a)
             float g[8];
             if (n >= 8) load8_any(dy, g);
             else load8_part(dy, n, g);
-            if (a.act) {
+            if (ACT) {
                 const T *pre = (const T *)a.pre + r * a.ldpre + c0;
                 float z[8];
                 if (n >= 8) load8_any(pre, z);
                 else load8_part(pre, n, z);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] *= act_slope(a.act, z[j]);
+                for (int j = 0; j < 8; ++j) g[j] *= act_slope(ACT, z[j]);
             }
             if (a.drop.threshold) {      // last, as a selection: what fell is zero whatever pre holds
                 const DropRow key = drop_row_key(call_key, r);
@@ -247,6 +247,18 @@ linear_dz_kernel(const DzArgs a)
 #pragma unroll
         for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
         a.partial[(int64_t)blockIdx.y * a.cols + c] = s;
+    }
+}
+
+template <typename T>
+static cudaError_t dz_launch(const DzArgs &a, int act, dim3 grid, cudaStream_t s)
+{
+    switch (act) {
+    case TSR_ACT_RELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_RELU>, grid, dim3(256), 0, s, 1, a);
+    case TSR_ACT_GELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU>, grid, dim3(256), 0, s, 1, a);
+    case TSR_ACT_GELU_TANH: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU_TANH>, grid, dim3(256), 0, s, 1, a);
+    case TSR_ACT_SILU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_SILU>, grid, dim3(256), 0, s, 1, a);
+    default: return launch_dependent(linear_dz_kernel<T, TSR_ACT_NONE>, grid, dim3(256), 0, s, 1, a);
     }
 }
 
@@ -599,10 +611,10 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             a.pre = io->pre.data; a.ldpre = io->pre.ld;
             a.dz = make_dz ? dz.data : nullptr; a.lddz = dz.ld;
             a.partial = partial;
-            a.rows = T; a.cols = (int)O; a.rows_per = (int)rows_per; a.act = d->activation;
+            a.rows = T; a.cols = (int)O; a.rows_per = (int)rows_per;
             a.drop = drop;
             const dim3 grid((unsigned)col_blocks, (unsigned)parts);
-            const cudaError_t rc = f32 ? launch_dependent(linear_dz_kernel<float>, grid, dim3(256), 0, stream, 1, a) : launch_dependent(linear_dz_kernel<bf16>, grid, dim3(256), 0, stream, 1, a);
+            const cudaError_t rc = f32 ? dz_launch<float>(a, d->activation, grid, stream) : dz_launch<bf16>(a, d->activation, grid, stream);
             if (rc != cudaSuccess) return TSR_ERR_CUDA;
         }
         if (run && db && column_finish(partial, T ? (int)parts : 0, O, O, io->dbias, d->gb_dtype == TSR_BF16, nullptr, false, d->accumulate != 0, stream) != cudaSuccess) return TSR_ERR_CUDA;

@@ -60,6 +60,15 @@ def test_norm_refuses_matrices(tsr):
     assert L.tsr_norm_workspace_bytes(ctypes.byref(d), None) == 1
 
 
+@pytest.mark.parametrize("rows", [0, 1, 5, 1000, 1 << 30])
+@pytest.mark.parametrize("cols", [0, 1, 7, 8, 511, 2048, 4097, 8192, 8193, 100000])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_norm_scratch_of_any_size(tsr, rows, cols, dtype):
+    size = ctypes.c_size_t()
+    assert tsr.lib().tsr_norm_workspace_bytes(ctypes.byref(norm_desc(tsr, rows=rows, cols=cols, dtype=dtype)), ctypes.byref(size)) == 0
+    assert (size.value >= 8 * cols and size.value <= 8 * cols * 148 * 16) if cols else size.value == 0
+
+
 def linear_desc(tsr, drop=(0.0, 0, 0, 0, None), **kw):
     d = dict(rows=4, ins=8, outs=16, dtype=1, b_dtype=0, gw_dtype=0, gb_dtype=0, activation=0, accumulate=0)
     d.update(kw)
