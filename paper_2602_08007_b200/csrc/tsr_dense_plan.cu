@@ -191,20 +191,6 @@ struct PairsFrom { uint32_t half; static constexpr int STEP = 64; };
 
 struct UnitKeys { uint32_t k1, k2; };
 
-__device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
-__device__ __forceinline__ unsigned long long bits_of(float2 a) { return *(const unsigned long long *)&a; }
-__device__ __forceinline__ float2 mul2(float2 a, float2 b)
-{
-    unsigned long long d;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)));
-    return *(const float2 *)&d;
-}
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    unsigned long long d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)), "l"(bits_of(c)));
-    return *(const float2 *)&d;
-}
 // a + b; results and operands below 2^-126 count as zero.  The flush is there for the roots, and it keeps a product and its
 // sum two operations: without it the assembler joins a pair's mul.rn and add.rn into one multiply-add (seen as other
 // stored bits where the rounded product lies halfway between two 8-bit values).

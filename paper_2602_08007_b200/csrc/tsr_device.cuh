@@ -30,6 +30,21 @@ __device__ __forceinline__ float core_update_elem(float c, float &m1, float &m2,
     return __fdividef(mh, __fadd_rn(sqrt_approx(vh), sc.eps));
 }
 
+// sm_100 multiplies and adds FP32 pairs in one instruction, each half rounded as the scalar operation.
+__device__ __forceinline__ float2 pair(float x) { return make_float2(x, x); }
+__device__ __forceinline__ unsigned long long bits_of(float2 a) { return *(const unsigned long long *)&a; }
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    unsigned long long d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return *(const float2 *)&d;
+}
+__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
+{
+    unsigned long long d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)), "l"(bits_of(c)));
+    return *(const float2 *)&d;
+}
 // 32-bit mixing by multiplications and xor-shifts, the base of the library's counter-based random words.  The multipliers
 // are those of the 32-bit finaliser of MurmurHash3 (A. Appleby, public domain).
 __host__ __device__ __forceinline__ uint32_t mix32(uint32_t x)

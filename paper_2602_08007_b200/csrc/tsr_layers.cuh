@@ -107,6 +107,14 @@ __device__ __forceinline__ float act_slope(int act, float z)
     }
 }
 
+// ---- pairs (mul2, fma2: tsr_device.cuh) -----------------------------------------------------------------------------
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return *(const float2 *)&d;
+}
+
 // ---- typed access -----------------------------------------------------------------------------------------------------
 __device__ __forceinline__ float load_f(const float *p) { return *p; }
 __device__ __forceinline__ float load_f(const bf16 *p) { return __bfloat162float(*p); }

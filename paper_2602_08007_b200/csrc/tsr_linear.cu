@@ -274,7 +274,7 @@ column_finish_kernel(const float *__restrict__ partial, int parts, int64_t ldp, 
     const int64_t c = (int64_t)blockIdx.x * 32 + x;
     float s = 0.f;
     if (c < cols) {
-#pragma unroll 4
+#pragma unroll 16
         for (int p = y; p < parts; p += 32) s += partial[p * ldp + c];
     }
     sums[y][x] = s;

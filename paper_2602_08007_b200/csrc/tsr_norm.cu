@@ -1,11 +1,10 @@
 // Norm over rows, forward and backward (formulas in tsr.h).  Both passes are bound by HBM: forward reads x and writes y, backward reads
 // x and dy and writes dx, each once; a row stays in registers between its sums and its results.
 //
-// Forward: a warp per row up to 2048 columns (FP32 1024; no barrier), a CTA per row up to 8192.  The mean is formed from the distances from the
-// row's first entry and the variance from the distances from the mean, both from registers: a large mean costs no digits, and a row
-// of equal entries has variance zero.
-// Backward: a CTA walks over rows with fixed columns per thread, so that the sums for dweight and dbias stay in its registers; it leaves one
-// partial row each, and column_finish adds them in order.  Narrow rows share the barrier of their reductions two by two.
+// Forward and backward: rows up to 8192 columns stay in the registers of a warp or of a CTA, the next row in flight.  Distances are formed from the
+// row's first entry and then from means: a large mean costs no digits, and a row of equal entries has variance zero.
+// Backward: threads keep their columns from row to row, so that the sums for dweight and dbias stay in registers; a CTA leaves one partial row each, and
+// column_finish adds them in order.
 // Wider rows, and matrices that do not start at the same place in 16 bytes, are read several times (from L2, mostly); their column sums take a
 // pass of their own.
 #include <math.h>
@@ -86,125 +85,168 @@ __device__ __forceinline__ uint4 load_unit(const T *row, int col, int cols, T fi
     memcpy(&r, t, 16);
     return r;
 }
-__device__ __forceinline__ void unit_values(const uint4 &r, float (&v)[8]) { unpack8(r, v); }
-__device__ __forceinline__ void unit_values(const uint4 &r, float (&v)[4])
+// A unit as pairs of FP32 values, and back.
+__device__ __forceinline__ float2 bf16_pair(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
+__device__ __forceinline__ void unit_pairs(const uint4 &r, float2 (&v)[4]) { v[0] = bf16_pair(r.x); v[1] = bf16_pair(r.y); v[2] = bf16_pair(r.z); v[3] = bf16_pair(r.w); }
+__device__ __forceinline__ void unit_pairs(const uint4 &r, float2 (&v)[2])
 {
-    v[0] = __uint_as_float(r.x); v[1] = __uint_as_float(r.y); v[2] = __uint_as_float(r.z); v[3] = __uint_as_float(r.w);
+    v[0] = make_float2(__uint_as_float(r.x), __uint_as_float(r.y));
+    v[1] = make_float2(__uint_as_float(r.z), __uint_as_float(r.w));
 }
-__device__ __forceinline__ uint4 unit_of(const float (&v)[8])
+__device__ __forceinline__ uint4 unit_of(const float2 (&v)[4])
 {
-    return make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7]));
+    return make_uint4(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y), pack_bf16(v[2].x, v[2].y), pack_bf16(v[3].x, v[3].y));
 }
-__device__ __forceinline__ uint4 unit_of(const float (&v)[4])
+__device__ __forceinline__ uint4 unit_of(const float2 (&v)[2])
 {
-    return make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+    return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
 }
+// Keeps the compiler from holding on to values it could form again from a unit: registers are what bounds the rows in flight.
+__device__ __forceinline__ void forget(uint4 &r) { asm volatile("" : "+r"(r.x), "+r"(r.y), "+r"(r.z), "+r"(r.w)); }
 template <typename T, bool EDGE>
-__device__ __forceinline__ void store_unit(T *row, int col, int cols, const float (&v)[Unit<T>::V])
+__device__ __forceinline__ void store_unit(T *row, int col, int cols, const float2 (&v)[Unit<T>::V / 2])
 {
     constexpr int V = Unit<T>::V;
     if (!EDGE || (col >= 0 && col + V <= cols)) *(uint4 *)(row + col) = unit_of(v);
     else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) if (col + i >= 0 && col + i < cols) store_f(row + col + i, v[i]);
+        for (int i = 0; i < V; ++i) if (col + i >= 0 && col + i < cols) store_f(row + col + i, i & 1 ? v[i / 2].y : v[i / 2].x);
     }
 }
 __device__ __forceinline__ float param(const void *p, int c, bool is_bf16, float none) { return p ? load_as(p, c, is_bf16) : none; }
 
-// Places of a unit that hang over an end of the row read as the row's first entry x0: their distance from it is zero and the mean right; from the
-// mean m0 of the distances they are m0 away, which is taken out of the sum of squares again.  (That sum is m0^2 at least, by
-// the first entry itself, so the difference keeps its digits.)
-__device__ __forceinline__ float variance_of(float squares, float m0, const NormArgs &a, const int units, int V)
+// The entries of a unit less `from`; places that hold no entry become zero.  Without EDGE only whole units are missing.
+template <bool EDGE, int P>
+__device__ __forceinline__ void less(float2 (&v)[P], float from, int col, int cols)
 {
-    return fmaxf(squares - (float)(units * V - a.cols) * m0 * m0, 0.f) * a.inv_n;
+    if (EDGE ? col >= 0 && col + 2 * P <= cols : col < cols) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) v[i] = add2(v[i], pair(-from));
+    } else {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            v[i].x = EDGE && col + 2 * i >= 0 && col + 2 * i < cols ? v[i].x - from : 0.f;
+            v[i].y = EDGE && col + 2 * i + 1 >= 0 && col + 2 * i + 1 < cols ? v[i].y - from : 0.f;
+        }
+    }
 }
 
-// A warp per row, eight rows of the class per CTA at a time, U units per lane; weight and bias in shared memory, by unit.
-template <typename T, int U, bool EDGE>
-__global__ void __launch_bounds__(256, 2)
-norm_forward_kernel(const NormArgs a)
+// weight and bias of a row's units in shared memory, units * V values each: the first four values of every unit, then (BF16) the last four, so that
+// the lanes of a warp read 16 bytes side by side.
+__device__ __forceinline__ int shared_at(int unit, int half, int units) { return (half * units + unit) * 4; }
+template <typename T>
+__device__ __forceinline__ void share_params(const NormArgs &a, const RowClass &rc, float *w, float *b)
 {
     constexpr int V = Unit<T>::V;
-    __shared__ __align__(16) float w[U * 32 * V], b[U * 32 * V];
+    for (int i = threadIdx.x; i < rc.units * V; i += blockDim.x) {
+        const int c = i - rc.shift, at = shared_at(i / V, i % V / 4, rc.units) + i % 4;
+        const bool in = c >= 0 && c < a.cols;
+        w[at] = in ? param(a.weight, c, a.p_bf16, 1.f) : 0.f;
+        if (b) b[at] = in ? param(a.bias, c, a.p_bf16, 0.f) : 0.f;
+    }
+}
+// v <- (v - mean) rstd w + b over unit j
+template <int P>
+__device__ __forceinline__ void normed(float2 (&v)[P], float mean, float rstd, const float *w, const float *b, int j, int units)
+{
+#pragma unroll
+    for (int i = 0; i < P; i += 2) {
+        const float4 ww = *(const float4 *)(w + shared_at(j, i / 2, units)), bb = *(const float4 *)(b + shared_at(j, i / 2, units));
+        v[i] = fma2(mul2(add2(v[i], pair(-mean)), pair(rstd)), make_float2(ww.x, ww.y), make_float2(bb.x, bb.y));
+        v[i + 1] = fma2(mul2(add2(v[i + 1], pair(-mean)), pair(rstd)), make_float2(ww.z, ww.w), make_float2(bb.z, bb.w));
+    }
+}
+
+// A warp per row, U units per lane; the next row on its way while one is worked on.
+template <typename T, int U, bool EDGE>
+__global__ void __launch_bounds__(256, U > 4 || (EDGE && U > 2) ? 2 : U > 2 || EDGE ? 3 : 4)
+norm_forward_kernel(const NormArgs a)
+{
+    constexpr int V = Unit<T>::V, P = V / 2;
+    extern __shared__ float4 shared_params[];
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const RowClass rc = row_class<T>(a.x, a.ldx, a.cols, a.period, blockIdx.x, gridDim.x);
-    for (int i = threadIdx.x; i < rc.units * V; i += 256) {
-        const int c = i - rc.shift;
-        const bool in = c >= 0 && c < a.cols;
-        w[i] = in ? param(a.weight, c, a.p_bf16, 1.f) : 0.f;
-        b[i] = in ? param(a.bias, c, a.p_bf16, 0.f) : 0.f;
-    }
-    __syncthreads();
-    for (int64_t r = rc.first + rc.step * warp; r < a.rows; r += rc.step * 8) {
+    float *w = (float *)shared_params, *b = w + rc.units * V;
+    uint4 next[U];
+    T first = T(0.f);
+    auto fetch = [&](int64_t r) {
+        if (r >= a.rows) return;
         const T *x = (const T *)a.x + r * a.ldx;
-        const T first = a.center ? *x : T(0.f);
-        uint4 raw[U];
+        if (a.center) first = *x;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = u * 32 + lane;
-            raw[u] = j < rc.units ? load_unit<T, EDGE>(x, j * V - rc.shift, a.cols, first) : make_uint4(0, 0, 0, 0);
+            next[u] = j < rc.units ? load_unit<T, EDGE>(x, j * V - rc.shift, a.cols, T(0.f)) : make_uint4(0, 0, 0, 0);
         }
+    };
+    fetch(rc.first + rc.step * warp);
+    share_params<T>(a, rc, w, b);
+    __syncthreads();
+    for (int64_t r = rc.first + rc.step * warp; r < a.rows; r += rc.step * 8) {
         const float x0 = load_f(&first);
-        float v[U][V], m0 = 0.f, q = 0.f;
+        float2 v[U][P], sum = pair(0.f), q = pair(0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float from = u * 32 + lane < rc.units ? x0 : 0.f;
-            unit_values(raw[u], v[u]);
-#pragma unroll
-            for (int i = 0; i < V; ++i) { v[u][i] -= from; m0 += v[u][i]; }
+            unit_pairs(next[u], v[u]);
+            less<EDGE>(v[u], x0, (u * 32 + lane) * V - rc.shift, a.cols);
         }
-        m0 = a.center ? warp_sum(m0) * a.inv_n : 0.f;
+        fetch(r + rc.step * 8);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < P; ++i) sum = add2(sum, v[u][i]);
+        const float mean = a.center ? warp_sum(sum.x + sum.y) * a.inv_n : 0.f;
+        // squared distances from the mean; what holds no entry is left out
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float from = u * 32 + lane < rc.units ? m0 : 0.f;
+            const int col = (u * 32 + lane) * V - rc.shift;
+            if (EDGE ? col >= 0 && col + V <= a.cols : col < a.cols) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) { v[u][i] -= from; q = fmaf(v[u][i], v[u][i], q); }
+                for (int i = 0; i < P; ++i) {
+                    const float2 d = add2(v[u][i], pair(-mean));
+                    q = fma2(d, d, q);
+                }
+            } else if (EDGE) {
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float d = (i & 1 ? v[u][i / 2].y : v[u][i / 2].x) - mean;
+                    if (col + i >= 0 && col + i < a.cols) q.x = fmaf(d, d, q.x);
+                }
+            }
         }
-        const float rstd = 1.f / sqrtf((EDGE ? variance_of(warp_sum(q), m0, a, rc.units, V) : warp_sum(q) * a.inv_n) + a.eps);
-        if (a.stats && lane == 0) *(float2 *)(a.stats + 2 * r) = make_float2(x0 + m0, rstd);
+        const float rstd = rsqrtf(warp_sum(q.x + q.y) * a.inv_n + a.eps);
+        if (a.stats && lane == 0) *(float2 *)(a.stats + 2 * r) = make_float2(x0 + mean, rstd);
         T *y = (T *)a.y + r * a.ldy;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = u * 32 + lane;
             if (j >= rc.units) continue;
-            float o[V];
-#pragma unroll
-            for (int i = 0; i < V; i += 4) {
-                const float4 ww = *(const float4 *)(w + j * V + i), bb = *(const float4 *)(b + j * V + i);
-                o[i] = fmaf(v[u][i] * rstd, ww.x, bb.x);
-                o[i + 1] = fmaf(v[u][i + 1] * rstd, ww.y, bb.y);
-                o[i + 2] = fmaf(v[u][i + 2] * rstd, ww.z, bb.z);
-                o[i + 3] = fmaf(v[u][i + 3] * rstd, ww.w, bb.w);
-            }
-            store_unit<T, EDGE>(y, j * V - rc.shift, a.cols, o);
+            normed(v[u], mean, rstd, w, b, j, rc.units);
+            store_unit<T, EDGE>(y, j * V - rc.shift, a.cols, v[u]);
         }
     }
 }
 
-// A CTA per row, eight entries per thread; weight and bias in registers, the next row on its way while one is worked on.
-template <typename T, bool EDGE>
-__global__ void __launch_bounds__(1024, 1)
+// Wider rows: a CTA per row, U units per thread.  Each thread forms mean and sum of squared distances of its own entries; two sets of n1 and n2
+// entries join by
+//     mean = mean1 + d n2 / (n1 + n2),   squares = squares1 + squares2 + d^2 n1 n2 / (n1 + n2),   d = mean2 - mean1
+// (T. Chan, G. Golub, R. LeVeque 1979), so that a row takes one round of exchanges and one barrier, and digits are lost to neither a large mean nor an
+// outlier.  The factors are the same for every row.
+template <typename T, int U, bool EDGE, int THREADS, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS)
 norm_forward_row_kernel(const NormArgs a)
 {
-    constexpr int V = Unit<T>::V, U = 8 / V;
-    __shared__ float slots[2][32];
+    constexpr int V = Unit<T>::V, P = V / 2;
+    extern __shared__ float4 shared_params[];
+    __shared__ float2 slots[2][16], factors[16];
     pdl_trigger();
     pdl_wait();
-    const int tid = threadIdx.x, threads = blockDim.x;
+    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
     const RowClass rc = row_class<T>(a.x, a.ldx, a.cols, a.period, blockIdx.x, gridDim.x);
-    float w[U][V], b[U][V];
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = (u * threads + tid) * V - rc.shift + i;
-            const bool in = c >= 0 && c < a.cols;
-            w[u][i] = in ? param(a.weight, c, a.p_bf16, 1.f) : 0.f;
-            b[u][i] = in ? param(a.bias, c, a.p_bf16, 0.f) : 0.f;
-        }
-    uint4 raw[U];
+    float *w = (float *)shared_params, *b = w + rc.units * V;
+    uint4 next[U];
     T first = T(0.f);
     auto fetch = [&](int64_t r) {
         if (r >= a.rows) return;
@@ -213,42 +255,82 @@ norm_forward_row_kernel(const NormArgs a)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = u * threads + tid;
-            raw[u] = j < rc.units ? load_unit<T, EDGE>(x, j * V - rc.shift, a.cols, first) : make_uint4(0, 0, 0, 0);
+            next[u] = j < rc.units ? load_unit<T, EDGE>(x, j * V - rc.shift, a.cols, T(0.f)) : make_uint4(0, 0, 0, 0);
         }
     };
     fetch(rc.first);
-    for (int64_t r = rc.first; r < a.rows; r += rc.step) {
-        float v[U][V], m0 = 0.f, q = 0.f;
+    share_params<T>(a, rc, w, b);
+    int own = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int col = (u * threads + tid) * V - rc.shift;
+        own += max(0, min(col + V, a.cols) - max(col, 0));
+    }
+    const float inv_own = own ? 1.f / (float)own : 0.f;
+    float f2[5], f12[5], count = (float)own;      // n2 / (n1 + n2) and n1 n2 / (n1 + n2) of the five exchanges within a warp
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+        const float other = __shfl_xor_sync(0xffffffffu, count, 1 << k), both = count + other;
+        f2[k] = both > 0.f ? other / both : 0.f;
+        f12[k] = count * f2[k];
+        count = both;
+    }
+    if (lane == 0) slots[0][warp].x = count;
+    __syncthreads();
+    if (tid == 0) {
+        float before = 0.f;
+        for (int i = 0; i < warps; ++i) {
+            const float n = slots[0][i].x, both = before + n, f = both > 0.f ? n / both : 0.f;
+            factors[i] = make_float2(f, before * f);
+            before = both;
+        }
+    }
+    __syncthreads();
+    int turn = 0;
+    for (int64_t r = rc.first; r < a.rows; r += rc.step, turn ^= 1) {
         const float x0 = load_f(&first);
+        float2 v[U][P], sum = pair(0.f), q = pair(0.f);
 #pragma unroll
-        for (int u = 0; u < U; ++u) unit_values(raw[u], v[u]);
+        for (int u = 0; u < U; ++u) {
+            unit_pairs(next[u], v[u]);
+            less<EDGE>(v[u], x0, (u * threads + tid) * V - rc.shift, a.cols);
+#pragma unroll
+            for (int i = 0; i < P; ++i) sum = add2(sum, v[u][i]);
+        }
         fetch(r + rc.step);
+        const float mine = a.center ? (sum.x + sum.y) * inv_own : 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float from = u * threads + tid < rc.units ? x0 : 0.f;
+            less<EDGE>(v[u], mine, (u * threads + tid) * V - rc.shift, a.cols);
 #pragma unroll
-            for (int i = 0; i < V; ++i) { v[u][i] -= from; m0 += v[u][i]; }
+            for (int i = 0; i < P; ++i) q = fma2(v[u][i], v[u][i], q);
         }
-        if (a.center) m0 = cta_sum(m0, slots[0]) * a.inv_n;
-        else m0 = 0.f;
+        float mean = mine, squares = q.x + q.y;
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const float from = u * threads + tid < rc.units ? m0 : 0.f;
-#pragma unroll
-            for (int i = 0; i < V; ++i) { v[u][i] -= from; q = fmaf(v[u][i], v[u][i], q); }
+        for (int k = 0; k < 5; ++k) {
+            const float d = __shfl_xor_sync(0xffffffffu, mean, 1 << k) - mean;
+            squares = fmaf(d * d, f12[k], squares + __shfl_xor_sync(0xffffffffu, squares, 1 << k));
+            mean = fmaf(d, f2[k], mean);
         }
-        q = cta_sum(q, slots[1]);
-        const float rstd = 1.f / sqrtf((EDGE ? variance_of(q, m0, a, rc.units, V) : q * a.inv_n) + a.eps);
-        if (a.stats && tid == 0) *(float2 *)(a.stats + 2 * r) = make_float2(x0 + m0, rstd);
+        if (lane == 0) slots[turn][warp] = make_float2(mean, squares);
+        __syncthreads();      // one per turn: the slots of the turn before last are written again only after the last one's barrier
+        mean = slots[turn][0].x;
+        squares = slots[turn][0].y;
+        for (int i = 1; i < warps; ++i) {
+            const float2 t = slots[turn][i], f = factors[i];
+            const float d = t.x - mean;
+            squares = fmaf(d * d, f.y, squares + t.y);
+            mean = fmaf(d, f.x, mean);
+        }
+        const float rstd = rsqrtf(squares * a.inv_n + a.eps);
+        if (a.stats && tid == 0) *(float2 *)(a.stats + 2 * r) = make_float2(x0 + mean, rstd);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = u * threads + tid;
             if (j >= rc.units) continue;
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[u][i] = fmaf(v[u][i] * rstd, w[u][i], b[u][i]);
+            normed(v[u], mean - mine, rstd, w, b, j, rc.units);
             store_unit<T, EDGE>((T *)a.y + r * a.ldy, j * V - rc.shift, a.cols, v[u]);
         }
-        if (!a.center) __syncthreads();     // (the slot of the only sum is free again)
     }
 }
 
@@ -270,7 +352,7 @@ norm_forward_wide_kernel(const NormArgs a)
         }
         const float mu = x0 + m0;
         for (int c = threadIdx.x; c < a.cols; c += blockDim.x) { const float d = load_f(x + c) - x0 - m0; q = fmaf(d, d, q); }
-        const float rstd = 1.f / sqrtf(cta_sum(q, slots[1]) * a.inv_n + a.eps);
+        const float rstd = rsqrtf(cta_sum(q, slots[1]) * a.inv_n + a.eps);
         if (a.stats && threadIdx.x == 0) { a.stats[2 * r] = mu; a.stats[2 * r + 1] = rstd; }
         T *y = (T *)a.y + r * a.ldy;
         for (int c = threadIdx.x; c < a.cols; c += blockDim.x)
@@ -279,103 +361,110 @@ norm_forward_wide_kernel(const NormArgs a)
     }
 }
 
-// A CTA (up to 1024 threads) on R rows of its class at a time; U units per thread, whose columns stay the same, so that the column sums
-// stay in registers.  The next R rows are on their way while these are worked on.  DB: the sums of dy are wanted too.
-template <typename T, int U, int R, bool DB, bool EDGE, int THREADS, int CTAS>
+// A CTA walks over rows of its class; U units per thread, whose columns stay the same, so that the column sums stay in registers.  The next row is
+// on its way while one is worked on.  Rows are held as they were read and their values formed twice, for the sums and for
+// dx: registers bound how many rows are in flight.  weight is in shared memory, by unit.  DB: the sums of dy are wanted too.
+// Many entries per thread and few threads: what a row costs beside its entries (reductions, barrier, addresses) is some 150 instructions per warp.
+template <typename T, int U, bool DB, bool EDGE, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS)
 norm_backward_kernel(const NormArgs a)
 {
-    constexpr int V = Unit<T>::V;
-    __shared__ float2 slots[2][R][32];
+    constexpr int V = Unit<T>::V, P = V / 2;
+    extern __shared__ float4 shared_params[];
+    __shared__ float4 slots[2][8];       // the warps' pairs of sums, two in a vector
     pdl_trigger();
     pdl_wait();
     const int tid = threadIdx.x, threads = blockDim.x, warp = tid >> 5, lane = tid & 31, warps = threads >> 5;
     const RowClass rc = row_class<T>(a.x, a.ldx, a.cols, a.period, blockIdx.x, gridDim.x);
-    float w[U][V], dw[U][V], db[DB ? U : 1][V];
+    float *weight = (float *)shared_params;
+    share_params<T>(a, rc, weight, nullptr);
+    for (int i = tid; i < 2 * 8; i += threads) ((float4 *)slots)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float2 dw[U][P], db[DB ? U : 1][P];
 #pragma unroll
     for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-            const int c = (u * threads + tid) * V - rc.shift + i;
-            w[u][i] = c >= 0 && c < a.cols ? param(a.weight, c, a.p_bf16, 1.f) : 0.f;
-            dw[u][i] = 0.f;
-            if (DB) db[u][i] = 0.f;
+        for (int i = 0; i < P; ++i) {
+            dw[u][i] = pair(0.f);
+            if (DB) db[u][i] = pair(0.f);
         }
-    uint4 nx[R][U], ng[R][U];
-    float2 nst[R];
-    auto fetch = [&](int64_t r0) {
+    uint4 nx[U], ng[U];
+    float2 nst = pair(0.f);
+    auto fetch = [&](int64_t r) {
+        if (r >= a.rows) return;
+        nst = *(const float2 *)(a.stats_in + 2 * r);
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const int64_t r = r0 + k * rc.step;
-            const bool live = r < a.rows;       // a row that does not exist reads as dy = 0 with finite statistics: it adds nothing
-            nst[k] = live ? *(const float2 *)(a.stats_in + 2 * r) : make_float2(0.f, 0.f);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int j = u * threads + tid;
-                nx[k][u] = ng[k][u] = make_uint4(0, 0, 0, 0);
-                if (live && j < rc.units) {
-                    nx[k][u] = load_unit<T, EDGE>((const T *)a.x + r * a.ldx, j * V - rc.shift, a.cols, T(0.f));
-                    ng[k][u] = load_unit<T, EDGE>((const T *)a.dy + r * a.lddy, j * V - rc.shift, a.cols, T(0.f));
-                }
+        for (int u = 0; u < U; ++u) {
+            const int j = u * threads + tid;
+            nx[u] = ng[u] = make_uint4(0, 0, 0, 0);
+            if (j < rc.units) {
+                nx[u] = load_unit<T, EDGE>((const T *)a.x + r * a.ldx, j * V - rc.shift, a.cols, T(0.f));
+                ng[u] = load_unit<T, EDGE>((const T *)a.dy + r * a.lddy, j * V - rc.shift, a.cols, T(0.f));
             }
         }
     };
+    auto weights = [&](int u, float2 (&w)[P]) {
+        const int j = min(u * threads + tid, rc.units - 1);      // (a thread without a unit has dy = 0)
+#pragma unroll
+        for (int i = 0; i < P; i += 2) {
+            const float4 t = *(const float4 *)(weight + shared_at(j, i / 2, rc.units));
+            w[i] = make_float2(t.x, t.y);
+            w[i + 1] = make_float2(t.z, t.w);
+        }
+    };
     fetch(rc.first);
+    __syncthreads();
     int turn = 0;
-    for (int64_t r0 = rc.first; r0 < a.rows; r0 += R * rc.step, turn ^= 1) {
-        float x[R][U][V], g[R][U][V];
-        float2 s[R], st[R];
+    for (int64_t r = rc.first; r < a.rows; r += rc.step, turn ^= 1) {
+        uint4 x[U], g[U];
+        const float2 st = nst;
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-            st[k] = nst[k];
+        for (int u = 0; u < U; ++u) { x[u] = nx[u]; g[u] = ng[u]; }
+        fetch(r + rc.step);
+        float2 s1 = pair(0.f), s2 = pair(0.f);
 #pragma unroll
-            for (int u = 0; u < U; ++u) { unit_values(nx[k][u], x[k][u]); unit_values(ng[k][u], g[k][u]); }
+        for (int u = 0; u < U; ++u) {
+            float2 w[P], xv[P], gv[P];
+            weights(u, w);
+            unit_pairs(x[u], xv);
+            unit_pairs(g[u], gv);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                const float2 h = mul2(add2(xv[i], pair(-st.x)), pair(st.y));
+                dw[u][i] = fma2(gv[i], h, dw[u][i]);
+                if (DB) db[u][i] = add2(db[u][i], gv[i]);
+                const float2 gw = mul2(gv[i], w[i]);
+                s1 = add2(s1, gw);
+                s2 = fma2(gw, h, s2);
+            }
+            forget(x[u]);
+            forget(g[u]);
         }
-        fetch(r0 + R * rc.step);
+        float2 s = make_float2(s1.x + s1.y, s2.x + s2.y);
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-            s[k] = make_float2(0.f, 0.f);
-#pragma unroll
-            for (int u = 0; u < U; ++u)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float h = (x[k][u][i] - st[k].x) * st[k].y;
-                    x[k][u][i] = h;
-                    dw[u][i] = fmaf(g[k][u][i], h, dw[u][i]);
-                    if (DB) db[u][i] += g[k][u][i];
-                    g[k][u][i] *= w[u][i];
-                    s[k].x += g[k][u][i];
-                    s[k].y = fmaf(g[k][u][i], h, s[k].y);
-                }
-            s[k].x = warp_sum(s[k].x);
-            s[k].y = warp_sum(s[k].y);
-        }
+        for (int o = 16; o; o >>= 1) s = add2(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)));
         if (warps > 1) {
-            if (lane == 0) {
-#pragma unroll
-                for (int k = 0; k < R; ++k) slots[turn][k][warp] = s[k];
-            }
+            if (lane == 0) ((float2 *)slots[turn])[warp] = s;
             __syncthreads();      // one per turn: the slots of the turn before last are written again only after the last one's barrier
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                const float2 t = lane < warps ? slots[turn][k][lane] : make_float2(0.f, 0.f);
-                s[k].x = warp_sum(t.x);
-                s[k].y = warp_sum(t.y);
+            s = pair(0.f);
+            for (int i = 0; i < (warps + 1) / 2; ++i) {
+                const float4 t = slots[turn][i];
+                s = add2(s, add2(make_float2(t.x, t.y), make_float2(t.z, t.w)));
             }
         }
+        if (!a.y) continue;
+        // dx = r g w - r mean(g w) - (x - mu) r^2 mean(g w h)
+        const float2 c1 = pair(a.center ? -s.x * a.inv_n * st.y : 0.f), c2 = pair(-s.y * a.inv_n * st.y * st.y);
 #pragma unroll
-        for (int k = 0; k < R; ++k) {
-            const int64_t r = r0 + k * rc.step;
-            if (!a.y || r >= a.rows) continue;
-            const float c1 = a.center ? s[k].x * a.inv_n : 0.f, c2 = s[k].y * a.inv_n;
+        for (int u = 0; u < U; ++u) {
+            const int j = u * threads + tid;
+            if (j >= rc.units) continue;
+            float2 w[P], xv[P], gv[P];
+            weights(u, w);
+            unit_pairs(x[u], xv);
+            unit_pairs(g[u], gv);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int j = u * threads + tid;
-                if (j >= rc.units) continue;
-#pragma unroll
-                for (int i = 0; i < V; ++i) g[k][u][i] = st[k].y * (g[k][u][i] - fmaf(x[k][u][i], c2, c1));
-                store_unit<T, EDGE>((T *)a.y + r * a.ldy, j * V - rc.shift, a.cols, g[k][u]);
-            }
+            for (int i = 0; i < P; ++i) gv[i] = fma2(mul2(gv[i], w[i]), pair(st.y), fma2(add2(xv[i], pair(-st.x)), c2, c1));
+            store_unit<T, EDGE>((T *)a.y + r * a.ldy, j * V - rc.shift, a.cols, gv);
         }
     }
     // column sums of this CTA
@@ -385,8 +474,8 @@ norm_backward_kernel(const NormArgs a)
         for (int i = 0; i < V; ++i) {
             const int c = (u * threads + tid) * V - rc.shift + i;
             if (c < 0 || c >= a.cols) continue;
-            if (a.want_dw) a.partial[(int64_t)blockIdx.x * a.cols + c] = dw[u][i];
-            if (DB) a.partial[((int64_t)(a.want_dw ? gridDim.x : 0) + blockIdx.x) * a.cols + c] = db[u][i];
+            if (a.want_dw) a.partial[(int64_t)blockIdx.x * a.cols + c] = i & 1 ? dw[u][i / 2].y : dw[u][i / 2].x;
+            if (DB) a.partial[((int64_t)(a.want_dw ? gridDim.x : 0) + blockIdx.x) * a.cols + c] = i & 1 ? db[u][i / 2].y : db[u][i / 2].x;
         }
 }
 
@@ -473,17 +562,25 @@ template <typename T, bool EDGE>
 cudaError_t forward_as(const NormArgs &a, int units, int sms, cudaStream_t s)
 {
     constexpr int V = Unit<T>::V;
-    if (a.period && units * V <= 2048) {
+    const size_t smem = (size_t)units * V * 8;
+    if (a.period && units <= (EDGE ? 128 : 256)) {      // (eight units with edges do not fit the registers)
         const int u = (units + 31) / 32;
-        const dim3 grid((unsigned)shared_out(a.rows, a.period, 8, sms * 4));
-        if (u <= 1) return launch_dependent(norm_forward_kernel<T, 1, EDGE>, grid, dim3(256), 0, s, 1, a);
-        if (u <= 2) return launch_dependent(norm_forward_kernel<T, 2, EDGE>, grid, dim3(256), 0, s, 1, a);
-        if (u <= 4) return launch_dependent(norm_forward_kernel<T, 4, EDGE>, grid, dim3(256), 0, s, 1, a);
-        if (V == 8 || u <= 8) return launch_dependent(norm_forward_kernel<T, 8, EDGE>, grid, dim3(256), 0, s, 1, a);
+        const dim3 grid((unsigned)shared_out(a.rows, a.period, 8, sms * (u > 4 || (EDGE && u > 2) ? 2 : u > 2 || EDGE ? 3 : 4)));      // as many as are resident
+        if (u <= 1) return launch_dependent(norm_forward_kernel<T, 1, EDGE>, grid, dim3(256), smem, s, 1, a);
+        if (u <= 2) return launch_dependent(norm_forward_kernel<T, 2, EDGE>, grid, dim3(256), smem, s, 1, a);
+        if (u <= 4) return launch_dependent(norm_forward_kernel<T, 4, EDGE>, grid, dim3(256), smem, s, 1, a);
+        if constexpr (!EDGE) return launch_dependent(norm_forward_kernel<T, 8, false>, grid, dim3(256), smem, s, 1, a);
     }
     if (a.period && units * V <= ROW_COLS) {
-        const int threads = (int)round_up((units * V + 7) / 8, 32);
-        return launch_dependent(norm_forward_row_kernel<T, EDGE>, dim3((unsigned)shared_out(a.rows, a.period, 1, sms * std::max(1, 1024 / threads))), dim3(threads), 0, s, 1, a);
+        constexpr int CTAS = V == 8 ? 3 : 2;
+        const int threads = (int)round_up((units * V + 31) / 32, 32);
+        const dim3 grid((unsigned)shared_out(a.rows, a.period, 1, sms * std::max(1, std::min(256 * CTAS / threads, (int)(200 * 1024 / smem)))));
+        auto kernel = norm_forward_row_kernel<T, 32 / V, EDGE, 256, CTAS>;
+        if (smem > 48 * 1024) {
+            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e != cudaSuccess) return e;
+        }
+        return launch_dependent(kernel, grid, dim3(threads), smem, s, 1, a);
     }
     const int threads = any_threads(a.cols);
     const dim3 grid((unsigned)std::min<int64_t>(a.rows, (int64_t)sms * (2048 / threads)));
@@ -492,42 +589,41 @@ cudaError_t forward_as(const NormArgs &a, int units, int sms, cudaStream_t s)
 
 // The backward row kernel's form for a row of that many entries (whole units): entries per thread, threads, CTAs per SM.
 struct BackwardForm { int entries, threads, per_sm; };
-BackwardForm backward_form(int64_t entries_in_units)
+BackwardForm backward_form(int64_t entries_in_units, int V)
 {
     BackwardForm f;
-    f.entries = entries_in_units <= 4096 ? 8 : 16;
+    f.entries = entries_in_units <= 256 ? 8 : 16;
     f.threads = (int)std::max<int64_t>(32, round_up((entries_in_units + f.entries - 1) / f.entries, 32));
-    f.per_sm = f.threads <= 256 ? std::min(16, 768 / f.threads) : f.threads <= 384 ? 2 : 1;
+    f.per_sm = std::max(1, (f.entries == 8 ? 640 : V == 4 ? 512 : f.threads <= 128 ? 640 : 768) / f.threads);      // threads on an SM, by their registers
     return f;
 }
 // Partial rows of column sums that a backward pass leaves.
-int backward_parts(int64_t rows, int64_t entries_in_units, int period, int sms)
+int backward_parts(int64_t rows, int64_t entries_in_units, int V, int period, int sms)
 {
     if (entries_in_units > ROW_COLS || period == 0) return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, 2 * sms));
-    return (int)shared_out(rows, period, 2, (int64_t)sms * backward_form(entries_in_units).per_sm);
+    return (int)shared_out(rows, period, 1, (int64_t)sms * backward_form(entries_in_units, V).per_sm);
 }
 // ... and the most for any alignment of the matrices.
 int most_parts(const tsr_norm_desc &d, int sms)
 {
     const int V = 16 / type_bytes(d.dtype);
-    int most = backward_parts(d.rows, 0, 0, sms);
+    int most = backward_parts(d.rows, 0, V, 0, sms);
     for (int period = 1; period <= V; period *= 2)
-        for (int shift = 0; shift < V; ++shift) most = std::max(most, backward_parts(d.rows, round_up(d.cols + shift, V), period, sms));
+        for (int shift = 0; shift < V; ++shift) most = std::max(most, backward_parts(d.rows, round_up(d.cols + shift, V), V, period, sms));
     return most;
 }
 
 template <typename T, bool DB, bool EDGE>
 cudaError_t backward_as(const NormArgs &a, int units, int parts, cudaStream_t s)
 {
-    constexpr int V = Unit<T>::V, U8 = 8 / V, U16 = 16 / V;
-    const BackwardForm f = backward_form((int64_t)units * V);
+    constexpr int V = Unit<T>::V;
+    const BackwardForm f = backward_form((int64_t)units * V, V);
     const dim3 grid(parts), block(f.threads);
-    if (f.entries == 16) {
-        if (f.threads <= 384) return launch_dependent(norm_backward_kernel<T, U16, 1, DB, EDGE, 384, DB ? 1 : 2>, grid, block, 0, s, 1, a);
-        return launch_dependent(norm_backward_kernel<T, U16, 1, DB, EDGE, 512, 1>, grid, block, 0, s, 1, a);
-    }
-    if (f.threads <= 256) return launch_dependent(norm_backward_kernel<T, U8, 2, DB, EDGE, 256, V == 8 ? 3 : 2>, grid, block, 0, s, 1, a);
-    return launch_dependent(norm_backward_kernel<T, U8, 1, DB, EDGE, 512, V == 8 ? 2 : 1>, grid, block, 0, s, 1, a);
+    const size_t smem = (size_t)units * V * 4;
+    if (f.entries == 8) return launch_dependent(norm_backward_kernel<T, 8 / V, DB, EDGE, 32, 20>, grid, block, smem, s, 1, a);
+    if (f.threads <= 128) return launch_dependent(norm_backward_kernel<T, 16 / V, DB, EDGE, 128, V == 8 ? 5 : 4>, grid, block, smem, s, 1, a);
+    if (f.threads <= 384 && V == 8) return launch_dependent(norm_backward_kernel<T, 16 / V, DB, EDGE, 384, 2>, grid, block, smem, s, 1, a);
+    return launch_dependent(norm_backward_kernel<T, 16 / V, DB, EDGE, 512, 1>, grid, block, smem, s, 1, a);
 }
 
 template <typename T>
@@ -635,8 +731,9 @@ extern "C" tsr_status tsr_norm_backward(const tsr_norm_desc *desc, tsr_matrix dy
     const tsr_matrix *all[3] = {&x, &dy, &dx};
     int units = 0;
     a.period = d.rows > 0 ? common_period(d, all, 3, &units) : 0;
-    const int64_t entries = (int64_t)units * (16 / type_bytes(d.dtype));
-    const int parts = backward_parts(d.rows, entries, a.period, sms);
+    const int V = 16 / type_bytes(d.dtype);
+    const int64_t entries = (int64_t)units * V;
+    const int parts = backward_parts(d.rows, entries, V, a.period, sms);
     if (d.rows > 0) {
         const bool bf = d.dtype == TSR_BF16;
         cudaError_t e;

@@ -12,6 +12,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import functools
 import weakref
 from typing import Optional
 
@@ -77,10 +78,13 @@ def _matrix(t: torch.Tensor, what: str, shape, dtype: torch.dtype, device: torch
         raise ValueError("%s must be a %s tensor on %s" % (what, dtype, device))
     m = _layout(t)
     if m is None:
-        raise ValueError("%s must have a contiguous last dimension and rows of one pitch that do not overlap" % what)
+        raise ValueError(_ROWS % what)
     if t.shape != shape:
         raise ValueError("%s must have the shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
     return Matrix(t.data_ptr(), m[2])
+
+
+_ROWS = "%s must have a contiguous last dimension and rows of one pitch that do not overlap"
 
 
 def _vector(t: Optional[torch.Tensor], what: str, n: int, device: torch.device):
@@ -92,17 +96,15 @@ def _vector(t: Optional[torch.Tensor], what: str, n: int, device: torch.device):
     return t.data_ptr(), _DTYPE[t.dtype]
 
 
-def _type(x: torch.Tensor, what: str) -> int:
-    if x.dtype not in _DTYPE or not x.is_cuda:
+def _input(x: torch.Tensor, what: str):
+    """(type, (rows, columns, pitch), device) of a call's leading tensor."""
+    kind = _DTYPE.get(x.dtype)
+    if kind is None or not x.is_cuda:
         raise ValueError("%s must be an FP32 or BF16 tensor on a CUDA device" % what)
-    return _DTYPE[x.dtype]
-
-
-def _rows_of(x: torch.Tensor, what: str):
     m = _layout(x)
     if m is None:
-        raise ValueError("%s must have a contiguous last dimension and rows of one pitch that do not overlap" % what)
-    return m
+        raise ValueError(_ROWS % what)
+    return kind, m, x.device
 
 
 def _dropout_desc(drop: Optional[Dropout], device: torch.device) -> DropoutDesc:
@@ -121,25 +123,22 @@ def _activation(a) -> int:
     return ACTIVATIONS[a]
 
 
-class _Here:
-    """Nothing to enter: the tensors' device is the current one and no stream was given."""
-
-    def __enter__(self):
-        return None
-
-    def __exit__(self, *exc):
-        return False
-
-
-_HERE = _Here()
-
-
-def _on(device: torch.device, stream):
-    if stream is None:
-        return _HERE if device.index == torch.cuda.current_device() else torch.cuda.device(device)
-    if stream.device != device:
-        raise ValueError("stream must belong to %s" % device)
-    return torch.cuda.stream(stream)
+def _placed(call):
+    """Runs the call on the tensors' device and on `stream`, whatever is current.  (A wrapper that steps aside where nothing is to be changed: small
+    calls are bound by what the host does, and a context costs 1 us.)"""
+    @functools.wraps(call)
+    def placed(x, *args, stream=None, **kwargs):
+        index = x.device.index
+        if stream is None:
+            if index is None or index == torch.cuda.current_device():
+                return call(x, *args, **kwargs)
+            with torch.cuda.device(x.device):
+                return call(x, *args, **kwargs)
+        if stream.device != x.device:
+            raise ValueError("stream must belong to %s" % x.device)
+        with torch.cuda.stream(stream):
+            return call(x, *args, **kwargs)
+    return placed
 
 
 def _check(status: int, what: str):
@@ -157,65 +156,76 @@ def _scratch(size: int, device: torch.device):
 
 # ---- the C calls ----------------------------------------------------------------------------------------------------------
 
+# (`stream` is taken by the wrapper)
+
+@_placed
 def norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5, center: bool = True,
-                 out: Optional[torch.Tensor] = None, stream=None):
+                 out: Optional[torch.Tensor] = None):
     """(y, stats): the norm of every row of x (its last dimension) with weight and bias, and (mean, 1 / deviation) per row in FP32 for
-    norm_backward.  center False: without the mean.  out: where y goes; x itself is allowed."""
-    kind, (rows, cols, ld), dev = _type(x, "x"), _rows_of(x, "x"), x.device
+    norm_backward.  center False: without the mean.  out: where y goes; x itself is allowed.  stream: as in every call here."""
+    kind, (rows, cols, ld), dev = _input(x, "x")
     w, wt = _vector(weight, "weight", cols, dev)
     b, bt = _vector(bias, "bias", cols, dev)
-    if weight is not None and bias is not None and wt != bt:
-        raise ValueError("weight and bias must have the same type")
-    with _on(dev, stream):
-        y = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
-        my = _matrix(y, "out", x.shape, x.dtype, dev)
-        stats = torch.empty(rows, 2, dtype=torch.float32, device=dev)
-        desc = NormDesc(rows, cols, kind, wt if weight is not None else bt, TSR_F32, 1 if center else 0, 0, eps)
-        _check(lib().tsr_norm_forward(ctypes.byref(desc), Matrix(x.data_ptr(), ld), w, b, my, stats.data_ptr(), _current_stream(dev.index)), "tsr_norm_forward")
-    return y, stats
+    if wt != bt:
+        if w is not None and b is not None:
+            raise ValueError("weight and bias must have the same type")
+        wt = wt if w is not None else bt
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        my = Matrix(out.data_ptr(), cols)
+    else:
+        my = _matrix(out, "out", x.shape, x.dtype, dev)
+    stats = torch.empty((rows, 2), dtype=torch.float32, device=dev)
+    desc = NormDesc(rows, cols, kind, wt, TSR_F32, 1 if center else 0, 0, eps)
+    _check(lib().tsr_norm_forward(desc, Matrix(x.data_ptr(), ld), w, b, my, stats.data_ptr(), _current_stream(dev.index)), "tsr_norm_forward")
+    return out, stats
 
 
+@_placed
 def norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tensor], stats: torch.Tensor, center: bool = True, bias: bool = True,
                   dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None, accumulate: bool = False,
-                  want_dx: bool = True, want_dweight: Optional[bool] = None, stream=None):
+                  want_dx: bool = True, want_dweight: Optional[bool] = None):
     """(dx, dweight, dbias) for the dy of norm_forward's y.  dx, dweight, dbias: where they go (dx may be dy itself); otherwise they are new, dweight and
     dbias in FP32.  accumulate: the given dweight and dbias are added to.  bias, want_dx, want_dweight: what is not wanted is None (dweight is
     wanted where there is a weight)."""
-    kind, (rows, cols, ld), dev = _type(x, "x"), _rows_of(x, "x"), x.device
+    kind, (rows, cols, ld), dev = _input(x, "x")
     mdy = _matrix(dy, "dy", x.shape, x.dtype, dev)
     w, wt = _vector(weight, "weight", cols, dev)
     if stats.dtype != torch.float32 or stats.device != dev or tuple(stats.shape) != (rows, 2) or not stats.is_contiguous():
         raise ValueError("stats must be the second result of norm_forward")
-    want_dweight = (weight is not None or dweight is not None) if want_dweight is None else want_dweight
+    if want_dweight is None:
+        want_dweight = weight is not None or dweight is not None
     if accumulate and ((want_dweight and dweight is None) or (bias and dbias is None)):
         raise ValueError("accumulate needs the dweight and dbias to add to")
-    with _on(dev, stream):
-        if want_dx:
-            dx = torch.empty(x.shape, dtype=x.dtype, device=dev) if dx is None else dx
-            mdx = _matrix(dx, "dx", x.shape, x.dtype, dev)
-        else:
-            dx, mdx = None, _NO_MATRIX
-        dweight = (torch.empty(cols, dtype=torch.float32, device=dev) if dweight is None else dweight) if want_dweight else None
-        dbias = (torch.empty(cols, dtype=torch.float32, device=dev) if dbias is None else dbias) if bias else None
-        gw, gwt = _vector(dweight, "dweight", cols, dev)
-        gb, gbt = _vector(dbias, "dbias", cols, dev)
-        if gw is not None and gb is not None and gwt != gbt:
-            raise ValueError("dweight and dbias must have the same type")
-        desc = NormDesc(rows, cols, kind, wt, gwt if dweight is not None else gbt, 1 if center else 0, 1 if accumulate else 0, 0.0)
-        size = ctypes.c_size_t()
-        _check(lib().tsr_norm_workspace_bytes(ctypes.byref(desc), ctypes.byref(size)), "tsr_norm_workspace_bytes")
-        hold, at = _scratch(size.value if want_dweight or bias else 0, dev)
-        _check(lib().tsr_norm_backward(ctypes.byref(desc), mdy, Matrix(x.data_ptr(), ld), w, stats.data_ptr(), mdx, gw, gb, at, size.value, _current_stream(dev.index)),
-               "tsr_norm_backward")
+    if not want_dx:
+        dx, mdx = None, _NO_MATRIX
+    elif dx is None:
+        dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+        mdx = Matrix(dx.data_ptr(), cols)
+    else:
+        mdx = _matrix(dx, "dx", x.shape, x.dtype, dev)
+    dweight = (torch.empty(cols, dtype=torch.float32, device=dev) if dweight is None else dweight) if want_dweight else None
+    dbias = (torch.empty(cols, dtype=torch.float32, device=dev) if dbias is None else dbias) if bias else None
+    gw, gwt = _vector(dweight, "dweight", cols, dev)
+    gb, gbt = _vector(dbias, "dbias", cols, dev)
+    if gw is not None and gb is not None and gwt != gbt:
+        raise ValueError("dweight and dbias must have the same type")
+    desc = NormDesc(rows, cols, kind, wt, gwt if gw is not None else gbt, 1 if center else 0, 1 if accumulate else 0, 0.0)
+    hold, at, size = None, None, ctypes.c_size_t()
+    if want_dweight or bias:
+        _check(lib().tsr_norm_workspace_bytes(desc, size), "tsr_norm_workspace_bytes")
+        hold, at = _scratch(size.value, dev)
+    _check(lib().tsr_norm_backward(desc, mdy, Matrix(x.data_ptr(), ld), w, stats.data_ptr(), mdx, gw, gb, at, size.value, _current_stream(dev.index)), "tsr_norm_backward")
     return dx, dweight, dbias
 
 
+@_placed
 def linear_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, activation=None, dropout: Optional[Dropout] = None,
-                   residual: Optional[torch.Tensor] = None, keep_pre: bool = False, out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None, stream=None):
+                   residual: Optional[torch.Tensor] = None, keep_pre: bool = False, out: Optional[torch.Tensor] = None, pre: Optional[torch.Tensor] = None):
     """(y, pre): y = residual + dropout(act(x weight^T + bias)), and the argument of the activation where keep_pre asks for it or `pre` says where it
     goes (None otherwise).  weight: (outs, ins).  activation: None, "relu", "gelu", "gelu_tanh" or "silu".  out: where y goes;
     the residual itself is allowed."""
-    kind, (rows, ins, ld), dev = _type(x, "x"), _rows_of(x, "x"), x.device
+    kind, (rows, ins, ld), dev = _input(x, "x")
     if weight.dim() != 2 or weight.shape[1] != ins:
         raise ValueError("weight must be a matrix with x's last dimension as its columns")
     outs = weight.shape[0]
@@ -223,28 +233,35 @@ def linear_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.T
     mw = _matrix(weight, "weight", weight.shape, x.dtype, dev)
     b, bt = _vector(bias, "bias", outs, dev)
     mres = _matrix(residual, "residual", shape, x.dtype, dev) if residual is not None else _NO_MATRIX
+    if out is None:
+        out = x.new_empty(shape)
+        my = Matrix(out.data_ptr(), outs)
+    else:
+        my = _matrix(out, "out", shape, x.dtype, dev)
+    if pre is not None:
+        mpre = _matrix(pre, "pre", shape, x.dtype, dev)
+    elif keep_pre:
+        pre = x.new_empty(shape)
+        mpre = Matrix(pre.data_ptr(), outs)
+    else:
+        mpre = _NO_MATRIX
     desc = LinearDesc(rows, ins, outs, kind, bt, TSR_F32, TSR_F32, _activation(activation), 0, _dropout_desc(dropout, dev))
-    with _on(dev, stream):
-        y = torch.empty(shape, dtype=x.dtype, device=dev) if out is None else out
-        my = _matrix(y, "out", shape, x.dtype, dev)
-        if pre is None and keep_pre:
-            pre = torch.empty(shape, dtype=x.dtype, device=dev)
-        mpre = _matrix(pre, "pre", shape, x.dtype, dev) if pre is not None else _NO_MATRIX
-        io = LinearIO(Matrix(x.data_ptr(), ld), mw, mres, mpre, my, b)
-        size = ctypes.c_size_t()
-        _check(lib().tsr_linear_forward_bytes(ctypes.byref(desc), ctypes.byref(io), ctypes.byref(size)), "tsr_linear_forward_bytes")
-        hold, at = _scratch(size.value, dev)
-        _check(lib().tsr_linear_forward(ctypes.byref(desc), ctypes.byref(io), at, size.value, _current_stream(dev.index)), "tsr_linear_forward")
-    return y, pre
+    io = LinearIO(Matrix(x.data_ptr(), ld), mw, mres, mpre, my, b)
+    size = ctypes.c_size_t()
+    _check(lib().tsr_linear_forward_bytes(desc, io, size), "tsr_linear_forward_bytes")
+    hold, at = _scratch(size.value, dev)
+    _check(lib().tsr_linear_forward(desc, io, at, size.value, _current_stream(dev.index)), "tsr_linear_forward")
+    return out, pre
 
 
+@_placed
 def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], weight: torch.Tensor, pre: Optional[torch.Tensor] = None, activation=None,
                     dropout: Optional[Dropout] = None, dx: Optional[torch.Tensor] = None, dweight: Optional[torch.Tensor] = None, dbias: Optional[torch.Tensor] = None,
-                    accumulate: bool = False, want_dx: bool = True, want_dweight: bool = True, stream=None):
+                    accumulate: bool = False, want_dx: bool = True, want_dweight: bool = True):
     """(dx, dweight, dbias) for the dy of linear_forward's y; the residual's gradient is dy itself.  dx, dweight: where they go; otherwise they are
     new, in the type of x.  dweight may be FP32 or BF16 with any row pitch: the G of a TSR block, for instance.  dbias: where it goes, or None: not
     wanted.  accumulate: the given dweight and dbias are added to.  What want_dx and want_dweight leave out is None."""
-    kind, (rows, outs, ld), dev = _type(dy, "dy"), _rows_of(dy, "dy"), dy.device
+    kind, (rows, outs, ld), dev = _input(dy, "dy")
     if weight.dim() != 2 or weight.shape[0] != outs:
         raise ValueError("weight must be a matrix with dy's last dimension as its rows")
     ins = weight.shape[1]
@@ -260,38 +277,44 @@ def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], weight: torch.T
     if accumulate and want_dweight and dweight is None:
         raise ValueError("accumulate needs the dweight to add to")
     gb, gbt = _vector(dbias, "dbias", outs, dev)
-    with _on(dev, stream):
-        if want_dx:
-            dx = torch.empty(shape, dtype=dy.dtype, device=dev) if dx is None else dx
-            mdx = _matrix(dx, "dx", shape, dy.dtype, dev)
-        else:
-            dx, mdx = None, _NO_MATRIX
-        if want_dweight:
-            dweight = torch.empty(outs, ins, dtype=dy.dtype, device=dev) if dweight is None else dweight
-            if dweight.dtype not in _DTYPE:
-                raise ValueError("dweight must be FP32 or BF16")
-            mdw, gwt = _matrix(dweight, "dweight", weight.shape, dweight.dtype, dev), _DTYPE[dweight.dtype]
-        else:
-            dweight, mdw, gwt = None, _NO_MATRIX, TSR_F32
-        desc = LinearDesc(rows, ins, outs, kind, TSR_F32, gwt, gbt, act, 1 if accumulate else 0, _dropout_desc(dropout, dev))
-        io = LinearGrads(Matrix(dy.data_ptr(), ld), mx, mw, mpre, mdx, mdw, gb)
-        size = ctypes.c_size_t()
-        _check(lib().tsr_linear_backward_bytes(ctypes.byref(desc), ctypes.byref(io), ctypes.byref(size)), "tsr_linear_backward_bytes")
-        hold, at = _scratch(size.value, dev)
-        _check(lib().tsr_linear_backward(ctypes.byref(desc), ctypes.byref(io), at, size.value, _current_stream(dev.index)), "tsr_linear_backward")
+    if not want_dx:
+        dx, mdx = None, _NO_MATRIX
+    elif dx is None:
+        dx = dy.new_empty(shape)
+        mdx = Matrix(dx.data_ptr(), ins)
+    else:
+        mdx = _matrix(dx, "dx", shape, dy.dtype, dev)
+    gwt = TSR_F32
+    if not want_dweight:
+        dweight, mdw = None, _NO_MATRIX
+    else:
+        if dweight is None:
+            dweight = dy.new_empty((outs, ins))
+        gwt = _DTYPE.get(dweight.dtype)
+        if gwt is None:
+            raise ValueError("dweight must be FP32 or BF16")
+        mdw = _matrix(dweight, "dweight", weight.shape, dweight.dtype, dev)
+    desc = LinearDesc(rows, ins, outs, kind, TSR_F32, gwt, gbt, act, 1 if accumulate else 0, _dropout_desc(dropout, dev))
+    io = LinearGrads(Matrix(dy.data_ptr(), ld), mx, mw, mpre, mdx, mdw, gb)
+    size = ctypes.c_size_t()
+    _check(lib().tsr_linear_backward_bytes(desc, io, size), "tsr_linear_backward_bytes")
+    hold, at = _scratch(size.value, dev)
+    _check(lib().tsr_linear_backward(desc, io, at, size.value, _current_stream(dev.index)), "tsr_linear_backward")
     return dx, dweight, dbias
 
 
-def dropout_forward(x: torch.Tensor, dropout: Dropout, residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+@_placed
+def dropout_forward(x: torch.Tensor, dropout: Dropout, residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """residual + dropout(x); out: where it goes (x or the residual itself is allowed)."""
-    kind, (rows, cols, ld), dev = _type(x, "x"), _rows_of(x, "x"), x.device
+    kind, (rows, cols, ld), dev = _input(x, "x")
     mres = _matrix(residual, "residual", x.shape, x.dtype, dev) if residual is not None else _NO_MATRIX
-    desc = _dropout_desc(dropout, dev)
-    with _on(dev, stream):
-        y = torch.empty(x.shape, dtype=x.dtype, device=dev) if out is None else out
-        my = _matrix(y, "out", x.shape, x.dtype, dev)
-        _check(lib().tsr_dropout(ctypes.byref(desc), kind, rows, cols, Matrix(x.data_ptr(), ld), mres, my, _current_stream(dev.index)), "tsr_dropout")
-    return y
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        my = Matrix(out.data_ptr(), cols)
+    else:
+        my = _matrix(out, "out", x.shape, x.dtype, dev)
+    _check(lib().tsr_dropout(_dropout_desc(dropout, dev), kind, rows, cols, Matrix(x.data_ptr(), ld), mres, my, _current_stream(dev.index)), "tsr_dropout")
+    return out
 
 
 def dropout_backward(dy: torch.Tensor, dropout: Dropout, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
