@@ -409,7 +409,7 @@ TSR_API tsr_status tsr_dropout(const tsr_dropout_desc *desc, int32_t dtype, int6
                                tsr_matrix y, void *stream);
 
 /* Reads and clears the status word of the layer calls on the current device (TSR_OK, or TSR_ERR_TIMEOUT if a bounded wait of a
- * linear layer ran out since the last poll; its outputs are then undefined).  Synchronises `stream`; not for use in a capture. */
+ * norm or a linear layer ran out since the last poll; its outputs are then undefined).  Synchronises `stream`; not for use in a capture. */
 TSR_API tsr_status tsr_layer_poll_status(int32_t *status, void *stream);
 
 /* ---- reporting -------------------------------------------------------------------------- */

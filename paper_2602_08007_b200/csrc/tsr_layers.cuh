@@ -66,7 +66,13 @@ __device__ __forceinline__ float rcp_f(float x)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-__device__ __forceinline__ float sigmoid_f(float x) { return rcp_f(1.f + __expf(-x)); }
+__device__ __forceinline__ float exp_f(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x * 1.44269504f));
+    return y;
+}
+__device__ __forceinline__ float sigmoid_f(float x) { return rcp_f(1.f + exp_f(-x)); }
 // Limits |x| to `most`; NaN stays.
 __device__ __forceinline__ float limited(float x, float most)
 {
@@ -92,7 +98,7 @@ __device__ __forceinline__ float act_slope(int act, float z)
     case TSR_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
     case TSR_ACT_GELU: {
         const float c = limited(z, 16.f);
-        return fmaf(c * 0.39894228f, __expf(-0.5f * c * c), 0.5f * (1.f + erff(c * 0.70710678f)));
+        return fmaf(c * 0.39894228f, exp_f(-0.5f * c * c), 0.5f * (1.f + erff(c * 0.70710678f)));
     }
     case TSR_ACT_GELU_TANH: {
         const float c = limited(z, 16.f), c2 = c * c;
@@ -167,6 +173,7 @@ inline bool extent_ok(int64_t rows, int64_t cols, int64_t ld)
     return ld >= cols && ld < ((int64_t)1 << 37) && (rows <= 1 || rows <= ((int64_t)1 << 56) / (ld > 0 ? ld : 1));
 }
 
+cudaError_t norm_status_read(int32_t *status, cudaStream_t stream);
 int device_sms();   // multiprocessors of the current device (looked up once per device); 0 without one
 
 // Sums of column partials: out[c] (= or +=) sum over p < parts of partial[p * ldp + c], in order of p.  Two sets at once (out2 may

@@ -22,27 +22,30 @@ __device__ __forceinline__ uint4 load8_any(const bf16 *p)
 {
     const uint32_t m = (uint32_t)(uintptr_t)p & 15u;
     const uint4 *base = (const uint4 *)((uintptr_t)p & ~(uintptr_t)15);
-    const uint4 a = base[0];
+    const uint4 a = __ldg(base);
     if (m == 0) return a;
-    const uint4 b = base[1];
-    uint32_t w[5];
-    switch (m >> 2) {
-    case 0: w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; break;
-    case 1: w[0] = a.y; w[1] = a.z; w[2] = a.w; w[3] = b.x; w[4] = b.y; break;
-    case 2: w[0] = a.z; w[1] = a.w; w[2] = b.x; w[3] = b.y; w[4] = b.z; break;
-    default: w[0] = a.w; w[1] = b.x; w[2] = b.y; w[3] = b.z; w[4] = b.w; break;
-    }
+    const uint4 b = __ldg(base + 1);
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    // by one word, by two words, by half a word: selections, since code for each place (four of them, side by side on an SM) starved the warps of
+    // instructions
+    uint32_t t[7], u[5];
+#pragma unroll
+    for (int i = 0; i < 7; ++i) t[i] = m & 4u ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) u[i] = m & 8u ? t[i + 2] : t[i];
     const uint32_t s = (m & 2u) * 8u;
-    return make_uint4(__funnelshift_r(w[0], w[1], s), __funnelshift_r(w[1], w[2], s), __funnelshift_r(w[2], w[3], s), __funnelshift_r(w[3], w[4], s));
+    return make_uint4(__funnelshift_r(u[0], u[1], s), __funnelshift_r(u[1], u[2], s), __funnelshift_r(u[2], u[3], s), __funnelshift_r(u[3], u[4], s));
 }
 // The same of FP32 entries: plain loads, whose address a vector of four may not fit.
 __device__ __forceinline__ void load8_any(const bf16 *p, float (&v)[8]) { unpack8(load8_any(p), v); }
 __device__ __forceinline__ void load8_any(const float *p, float (&v)[8])
 {
-    if (((uintptr_t)p & 15) == 0) load8(p, v);
-    else {
+    if (((uintptr_t)p & 15) == 0) {
+        const float4 a = __ldg((const float4 *)p), b = __ldg((const float4 *)p + 1);
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = p[i];
+        for (int i = 0; i < 8; ++i) v[i] = __ldg(p + i);
     }
 }
 // ... of which n < 8 exist; the others are zero.
@@ -186,6 +189,9 @@ linear_finish_kernel(const __grid_constant__ FinishArgs a)
 
 // dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row.  dy and pre
 // may lie at any alignment, dz has a pitch of whole 16-byte units.  dz NULL: the sums alone.
+// The grid is what is resident at once (a third more left SMs idle for 40 % of the time), and what hides the loads is the number of warps: unrolled
+// loops were slower, the more so the further (8192 x 5461 with SiLU off the 16-byte grid: 72 us, unrolled twice 95, four times 131 at three CTAs).
+constexpr int DZ_CTAS = 4;     // on an SM
 struct DzArgs {
     const void *dy, *pre;
     void *dz;
@@ -195,7 +201,7 @@ struct DzArgs {
     DropArgs drop;
 };
 template <typename T, int ACT>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, DZ_CTAS)
 linear_dz_kernel(const DzArgs a)
 {
     __shared__ float sums[8][256];
@@ -203,25 +209,28 @@ linear_dz_kernel(const DzArgs a)
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c0 = blockIdx.x * 256 + lane * 8, n = a.cols - c0;
-    const int64_t r0 = (int64_t)blockIdx.y * a.rows_per, r1 = min(a.rows, r0 + a.rows_per);
+    const int64_t r0 = (int64_t)blockIdx.y * a.rows_per + warp, r1 = min(a.rows, (int64_t)(blockIdx.y + 1) * a.rows_per);
     const uint32_t call_key = a.drop.threshold ? drop_call_key(a.drop) : 0u;
     float acc[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) acc[j] = 0.f;
     if (n > 0) {
-#pragma unroll 2
-        for (int64_t r = r0 + warp; r < r1; r += 8) {
-            const T *dy = (const T *)a.dy + r * a.lddy + c0;
-            float g[8];
-            if (n >= 8) load8_any(dy, g);
-            else load8_part(dy, n, g);
+        const T *dy = (const T *)a.dy + r0 * a.lddy + c0, *pre = ACT ? (const T *)a.pre + r0 * a.ldpre + c0 : nullptr;
+        T *dz = a.dz ? (T *)a.dz + r0 * a.lddz + c0 : nullptr;
+#pragma unroll 1
+        for (int64_t r = r0; r < r1; r += 8) {
+            float g[8], z[8];
+            if (n >= 8) {
+                load8_any(dy, g);
+                if (ACT) load8_any(pre, z);
+            } else {
+                load8_part(dy, n, g);
+                if (ACT) load8_part(pre, n, z);
+            }
             if (ACT) {
-                const T *pre = (const T *)a.pre + r * a.ldpre + c0;
-                float z[8];
-                if (n >= 8) load8_any(pre, z);
-                else load8_part(pre, n, z);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) g[j] *= act_slope(ACT, z[j]);
+                pre += 8 * a.ldpre;
             }
             if (a.drop.threshold) {      // last, as a selection: what fell is zero whatever pre holds
                 const DropRow key = drop_row_key(call_key, r);
@@ -234,7 +243,11 @@ linear_dz_kernel(const DzArgs a)
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[j] += g[j];
-            if (a.dz) store8((T *)a.dz + r * a.lddz + c0, g);     // (past the last column: zeros, into the padding)
+            if (dz) {
+                store8(dz, g);     // (past the last column: zeros, into the padding)
+                dz += 8 * a.lddz;
+            }
+            dy += 8 * a.lddy;
         }
     }
     if (!a.partial) return;
@@ -581,12 +594,12 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
     const int64_t T = d->rows, I = d->ins, O = d->outs;
     const int known = device_sms(), sms = known ? known : 148;
 
-    // dz, and the partial sums of its columns: enough CTAs to fill the GPU four times, 32 rows each at least
+    // dz, and the partial sums of its columns (see the kernel): what is resident at once, 32 rows each at least
     const bool make_dz = (d->activation != TSR_ACT_NONE || drop.threshold) && (dx || dw) && T > 0 && O > 0;
     const int64_t col_blocks = (O + DZ_COLS - 1) / DZ_COLS;
-    int64_t parts = col_blocks ? std::max<int64_t>(1, std::min<int64_t>((T + 31) / 32, (4 * sms + col_blocks - 1) / col_blocks)) : 1;
-    const int64_t rows_per = T ? round_up((T + parts - 1) / parts, 8) : 8;
-    parts = std::max<int64_t>(1, (T + rows_per - 1) / rows_per);
+    const int64_t most = col_blocks ? std::max<int64_t>(1, std::min<int64_t>((T + 31) / 32, DZ_CTAS * sms / col_blocks)) : 1;
+    const int64_t rows_per = T ? round_up((T + most - 1) / most, 8) : 8;
+    const int64_t parts = std::max<int64_t>(1, (T + rows_per - 1) / rows_per);
 
     tsr_matrix dz = io->dy;
     Product px = {}, pw = {};
@@ -675,5 +688,8 @@ extern "C" tsr_status tsr_linear_backward(const tsr_linear_desc *desc, const tsr
 extern "C" tsr_status tsr_layer_poll_status(int32_t *status, void *stream)
 {
     if (!status) return TSR_ERR_INVALID_ARG;
-    return layer_status_read(status, (cudaStream_t)stream) == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
+    int32_t linear = 0, norm = 0;
+    if (linear_status_read(&linear, (cudaStream_t)stream) != cudaSuccess || norm_status_read(&norm, (cudaStream_t)stream) != cudaSuccess) return TSR_ERR_CUDA;
+    *status = linear ? linear : norm;
+    return TSR_OK;
 }

@@ -67,6 +67,6 @@ __device__ __forceinline__ LinearTile linear_tile(const LinearTiles &g, int item
 
 int linear_stages(int stage_bytes, bool pre);      // how many stages of the ring fit beside the epilogue's boxes
 cudaError_t linear_gemm_launch(const LinearGemm &g, int cg, bool f32_operands, bool f32_out, int sms, cudaStream_t stream);
-cudaError_t layer_status_read(int32_t *status, cudaStream_t stream);
+cudaError_t linear_status_read(int32_t *status, cudaStream_t stream);
 
 }  // namespace tsr

@@ -31,7 +31,7 @@
 namespace tsr {
 
 constexpr int LG_THREADS = 384, LG_EPI_WARPS = 8;
-__device__ int g_layer_status;
+__device__ int g_linear_status;
 
 // Shared memory: ring of stages (A, then B; geometry in LinearGemm), boxes, barriers.
 constexpr int LG_BOX_BYTES = 4096;
@@ -486,7 +486,7 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
         if constexpr (CG == 2) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
         else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(TMEM_COLS) : "memory");
     }
-    if (threadIdx.x == 0 && s_timeout) atomicMax(&g_layer_status, (int)TSR_ERR_TIMEOUT);
+    if (threadIdx.x == 0 && s_timeout) atomicMax(&g_linear_status, (int)TSR_ERR_TIMEOUT);
 }
 
 template <int CG, int PLANES, bool F32>
@@ -512,12 +512,12 @@ cudaError_t linear_gemm_launch(const LinearGemm &g, int cg, bool f32_operands, b
     return cg == 2 ? gemm_launch_as<2, 1, false>(g, sms, stream) : gemm_launch_as<1, 1, false>(g, sms, stream);
 }
 
-cudaError_t layer_status_read(int32_t *status, cudaStream_t stream)
+cudaError_t linear_status_read(int32_t *status, cudaStream_t stream)
 {
     int zero = 0, v = 0;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_layer_status, sizeof(int), 0, cudaMemcpyDeviceToHost, stream);
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_linear_status, sizeof(int), 0, cudaMemcpyDeviceToHost, stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
-    if (e == cudaSuccess && v) e = cudaMemcpyToSymbolAsync(g_layer_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, stream);
+    if (e == cudaSuccess && v) e = cudaMemcpyToSymbolAsync(g_linear_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, stream);
     if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
     *status = v;
     return e;

@@ -1,7 +1,7 @@
 // Norm over rows, forward and backward (formulas in tsr.h).  Both passes are bound by HBM: forward reads x and writes y, backward reads
 // x and dy and writes dx, each once; a row stays in registers between its sums and its results.
 //
-// Forward and backward: rows up to 8192 columns stay in the registers of a warp or of a CTA, the next row in flight.  Distances are formed from the
+// Forward and backward: rows up to 8192 columns are worked on by a warp or a CTA, the next ones in flight.  Distances are formed from the
 // row's first entry and then from means: a large mean costs no digits, and a row of equal entries has variance zero.
 // Backward: threads keep their columns from row to row, so that the sums for dweight and dbias stay in registers; a CTA leaves one partial row each, and
 // column_finish adds them in order.
@@ -13,6 +13,7 @@
 #include <algorithm>
 
 #include "tsr_layers.cuh"
+#include "tsr_umma.cuh"
 
 namespace tsr {
 
@@ -35,6 +36,8 @@ __device__ __forceinline__ float cta_sum(float x, float *slot)
     return s;
 }
 
+constexpr int NORM_STAGES = 8;      // most stages of a ring
+
 struct NormArgs {
     const void *x, *dy, *weight, *bias;
     void *y;                        // y, or dx
@@ -52,7 +55,9 @@ struct NormArgs {
 // A UNIT is 16 aligned bytes, V entries.  Rows whose pitch is no multiple of 16 bytes start anywhere in a unit, but rows that are `period` apart
 // start at the same place, and so do the rows of other matrices with the same offset and pitch modulo 16 bytes.  A CTA takes the rows
 // of one such class: unit j of each of them holds columns j V - shift ..., for the whole life of the CTA, so that everything is read and written in
-// aligned vectors, weight and column sums belong to fixed registers or addresses, and only the first and the last unit of a row go entry by entry.
+// aligned vectors, weight and column sums belong to fixed registers or addresses, and only the first and the last unit of a row need care.
+// Rows come as bulk copies of whole units into a ring in shared memory, a few rows ahead of where they are used: what is in flight then costs no
+// registers and no instructions.  (Every unit copied holds an entry of the row, so none lies outside of what may be read.)
 
 template <typename T> struct Unit { static constexpr int V = 16 / (int)sizeof(T); };
 
@@ -72,17 +77,39 @@ __device__ __forceinline__ RowClass row_class(const void *x, int64_t ldx, int co
     return c;
 }
 
-// EDGE: units may hang over an end of the row; the places that do read as `fill` and are not written.
+// Asks for a row: `units` units from the start of the one that holds its first entry.
+template <typename T>
+__device__ __forceinline__ void ask_row(uint32_t dst, const T *row, const RowClass &rc, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"((uint64_t)__cvta_generic_to_global(row - rc.shift)), "r"((uint32_t)rc.units * 16u), "r"(bar) : "memory");
+}
+// Waits for a stage of the ring; once a wait has run out nothing is waited for any more (the outputs are then undefined).
+__device__ __forceinline__ void await_row(uint32_t bar, uint32_t parity, bool &gave_up)
+{
+    if (!gave_up && !mbar_wait(bar, parity, UM_WAIT_CLOCKS)) gave_up = true;
+}
+__device__ int g_norm_status;
+__device__ __forceinline__ void note_gave_up(bool gave_up)
+{
+    if (!gave_up) return;
+    atomicMax(&g_norm_status, (int)TSR_ERR_TIMEOUT);
+    __nanosleep(2000000);      // let copies in flight land before the CTA goes away
+}
+
+// Unit j of a row in shared memory; EDGE: the places that hold no entry are zero.
 template <typename T, bool EDGE>
-__device__ __forceinline__ uint4 load_unit(const T *row, int col, int cols, T fill)
+__device__ __forceinline__ uint4 take_unit(const uint4 *row, int j, int col, int cols)
 {
     constexpr int V = Unit<T>::V;
-    if (!EDGE || (col >= 0 && col + V <= cols)) return *(const uint4 *)(row + col);
-    T t[V];
+    uint4 r = row[j];
+    if (EDGE && (col < 0 || col + V > cols)) {
+        T t[V];
+        memcpy(t, &r, 16);
 #pragma unroll
-    for (int i = 0; i < V; ++i) t[i] = col + i >= 0 && col + i < cols ? row[col + i] : fill;
-    uint4 r;
-    memcpy(&r, t, 16);
+        for (int i = 0; i < V; ++i) if (col + i < 0 || col + i >= cols) t[i] = T(0.f);
+        memcpy(&r, t, 16);
+    }
     return r;
 }
 // A unit as pairs of FP32 values, and back.
@@ -101,8 +128,7 @@ __device__ __forceinline__ uint4 unit_of(const float2 (&v)[2])
 {
     return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
 }
-// Keeps the compiler from holding on to values it could form again from a unit: registers are what bounds the rows in flight.
-__device__ __forceinline__ void forget(uint4 &r) { asm volatile("" : "+r"(r.x), "+r"(r.y), "+r"(r.z), "+r"(r.w)); }
+// EDGE: the places that hold no entry are left alone.
 template <typename T, bool EDGE>
 __device__ __forceinline__ void store_unit(T *row, int col, int cols, const float2 (&v)[Unit<T>::V / 2])
 {
@@ -157,46 +183,60 @@ __device__ __forceinline__ void normed(float2 (&v)[P], float mean, float rstd, c
     }
 }
 
-// A warp per row, U units per lane; the next row on its way while one is worked on.
+// A warp per row, U units per lane, a ring of `stages` rows per warp.
 template <typename T, int U, bool EDGE>
-__global__ void __launch_bounds__(256, U > 4 || (EDGE && U > 2) ? 2 : U > 2 || EDGE ? 3 : 4)
-norm_forward_kernel(const NormArgs a)
+__global__ void __launch_bounds__(256, U > 4 ? 2 : U > 2 ? 3 : 4)
+norm_forward_kernel(const NormArgs a, int stages)
 {
     constexpr int V = Unit<T>::V, P = V / 2;
-    extern __shared__ float4 shared_params[];
+    extern __shared__ float4 shared[];       // w, b, rings
+    __shared__ uint64_t bars[8 * NORM_STAGES];
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const RowClass rc = row_class<T>(a.x, a.ldx, a.cols, a.period, blockIdx.x, gridDim.x);
-    float *w = (float *)shared_params, *b = w + rc.units * V;
-    uint4 next[U];
-    T first = T(0.f);
-    auto fetch = [&](int64_t r) {
-        if (r >= a.rows) return;
-        const T *x = (const T *)a.x + r * a.ldx;
-        if (a.center) first = *x;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = u * 32 + lane;
-            next[u] = j < rc.units ? load_unit<T, EDGE>(x, j * V - rc.shift, a.cols, T(0.f)) : make_uint4(0, 0, 0, 0);
-        }
+    float *w = (float *)shared, *b = w + rc.units * V;
+    const uint4 *ring = (const uint4 *)(b + rc.units * V) + warp * stages * rc.units;
+    uint64_t *bar = bars + warp * NORM_STAGES;
+    const int64_t step = rc.step * 8, start = rc.first + rc.step * warp;
+    int64_t left = start < a.rows ? (a.rows - start + step - 1) / step : 0;     // rows of this warp
+    const T *ask = (const T *)a.x + start * a.ldx;
+    auto request = [&](int stage) {      // the next row, by lane 0
+        mbar_expect_tx(smem_u32(bar + stage), (uint32_t)rc.units * 16u);
+        ask_row<T>(smem_u32(ring + stage * rc.units), ask, rc, smem_u32(bar + stage));
+        ask += step * a.ldx;
     };
-    fetch(rc.first + rc.step * warp);
+    if (lane == 0) {
+        for (int i = 0; i < stages; ++i) mbar_init(smem_u32(bar + i), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int i = 0; i < stages && i < left; ++i) request(i);
+    }
     share_params<T>(a, rc, w, b);
     __syncthreads();
-    for (int64_t r = rc.first + rc.step * warp; r < a.rows; r += rc.step * 8) {
-        const float x0 = load_f(&first);
+    bool gave_up = false;
+    int stage = 0;
+    uint32_t phase = 0;
+    T *y = (T *)a.y + start * a.ldy;
+    float *stats = a.stats ? a.stats + 2 * start : nullptr;
+    for (; left > 0; --left) {
+        await_row(smem_u32(bar + stage), phase, gave_up);
+        const uint4 *row = ring + stage * rc.units;
+        const float x0 = a.center ? load_f((const T *)row + rc.shift) : 0.f;
         float2 v[U][P], sum = pair(0.f), q = pair(0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            unit_pairs(next[u], v[u]);
-            less<EDGE>(v[u], x0, (u * 32 + lane) * V - rc.shift, a.cols);
+            const int j = u * 32 + lane, col = j * V - rc.shift;
+            unit_pairs(j < rc.units ? take_unit<T, EDGE>(row, j, col, a.cols) : make_uint4(0, 0, 0, 0), v[u]);
         }
-        fetch(r + rc.step * 8);
+        __syncwarp();
+        if (lane == 0 && left > stages) request(stage);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
 #pragma unroll
-        for (int u = 0; u < U; ++u)
+        for (int u = 0; u < U; ++u) {
+            less<EDGE>(v[u], x0, (u * 32 + lane) * V - rc.shift, a.cols);
 #pragma unroll
             for (int i = 0; i < P; ++i) sum = add2(sum, v[u][i]);
+        }
         const float mean = a.center ? warp_sum(sum.x + sum.y) * a.inv_n : 0.f;
         // squared distances from the mean; what holds no entry is left out
 #pragma unroll
@@ -217,8 +257,7 @@ norm_forward_kernel(const NormArgs a)
             }
         }
         const float rstd = rsqrtf(warp_sum(q.x + q.y) * a.inv_n + a.eps);
-        if (a.stats && lane == 0) *(float2 *)(a.stats + 2 * r) = make_float2(x0 + mean, rstd);
-        T *y = (T *)a.y + r * a.ldy;
+        if (stats && lane == 0) *(float2 *)stats = make_float2(x0 + mean, rstd);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = u * 32 + lane;
@@ -226,7 +265,10 @@ norm_forward_kernel(const NormArgs a)
             normed(v[u], mean, rstd, w, b, j, rc.units);
             store_unit<T, EDGE>(y, j * V - rc.shift, a.cols, v[u]);
         }
+        y += step * a.ldy;
+        if (stats) stats += 2 * step;
     }
+    note_gave_up(gave_up);
 }
 
 // Wider rows: a CTA per row, U units per thread.  Each thread forms mean and sum of squared distances of its own entries; two sets of n1 and n2
@@ -236,29 +278,30 @@ norm_forward_kernel(const NormArgs a)
 // outlier.  The factors are the same for every row.
 template <typename T, int U, bool EDGE, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS)
-norm_forward_row_kernel(const NormArgs a)
+norm_forward_row_kernel(const NormArgs a, int stages)
 {
     constexpr int V = Unit<T>::V, P = V / 2;
-    extern __shared__ float4 shared_params[];
+    extern __shared__ float4 shared[];       // w, b, ring
+    __shared__ uint64_t bars[NORM_STAGES];
     __shared__ float2 slots[2][16], factors[16];
     pdl_trigger();
     pdl_wait();
     const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
     const RowClass rc = row_class<T>(a.x, a.ldx, a.cols, a.period, blockIdx.x, gridDim.x);
-    float *w = (float *)shared_params, *b = w + rc.units * V;
-    uint4 next[U];
-    T first = T(0.f);
-    auto fetch = [&](int64_t r) {
-        if (r >= a.rows) return;
-        const T *x = (const T *)a.x + r * a.ldx;
-        if (a.center) first = *x;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = u * threads + tid;
-            next[u] = j < rc.units ? load_unit<T, EDGE>(x, j * V - rc.shift, a.cols, T(0.f)) : make_uint4(0, 0, 0, 0);
-        }
+    float *w = (float *)shared, *b = w + rc.units * V;
+    const uint4 *ring = (const uint4 *)(b + rc.units * V);
+    int64_t left = rc.first < a.rows ? (a.rows - rc.first + rc.step - 1) / rc.step : 0;
+    const T *ask = (const T *)a.x + rc.first * a.ldx;
+    auto request = [&](int stage) {      // the next row, by one thread
+        mbar_expect_tx(smem_u32(bars + stage), (uint32_t)rc.units * 16u);
+        ask_row<T>(smem_u32(ring + stage * rc.units), ask, rc, smem_u32(bars + stage));
+        ask += rc.step * a.ldx;
     };
-    fetch(rc.first);
+    if (tid == 0) {
+        for (int i = 0; i < stages; ++i) mbar_init(smem_u32(bars + i), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int i = 0; i < stages && i < left; ++i) request(i);
+    }
     share_params<T>(a, rc, w, b);
     int own = 0;
 #pragma unroll
@@ -286,18 +329,24 @@ norm_forward_row_kernel(const NormArgs a)
         }
     }
     __syncthreads();
-    int turn = 0;
-    for (int64_t r = rc.first; r < a.rows; r += rc.step, turn ^= 1) {
-        const float x0 = load_f(&first);
+    bool gave_up = false;
+    int turn = 0, stage = 0;
+    uint32_t phase = 0;
+    T *y = (T *)a.y + rc.first * a.ldy;
+    float *stats = a.stats ? a.stats + 2 * rc.first : nullptr;
+    for (; left > 0; --left, turn ^= 1) {
+        await_row(smem_u32(bars + stage), phase, gave_up);
+        const uint4 *row = ring + stage * rc.units;
+        const float x0 = a.center ? load_f((const T *)row + rc.shift) : 0.f;
         float2 v[U][P], sum = pair(0.f), q = pair(0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            unit_pairs(next[u], v[u]);
-            less<EDGE>(v[u], x0, (u * threads + tid) * V - rc.shift, a.cols);
+            const int j = u * threads + tid, col = j * V - rc.shift;
+            unit_pairs(j < rc.units ? take_unit<T, EDGE>(row, j, col, a.cols) : make_uint4(0, 0, 0, 0), v[u]);
+            less<EDGE>(v[u], x0, col, a.cols);
 #pragma unroll
             for (int i = 0; i < P; ++i) sum = add2(sum, v[u][i]);
         }
-        fetch(r + rc.step);
         const float mine = a.center ? (sum.x + sum.y) * inv_own : 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -313,7 +362,10 @@ norm_forward_row_kernel(const NormArgs a)
             mean = fmaf(d, f2[k], mean);
         }
         if (lane == 0) slots[turn][warp] = make_float2(mean, squares);
-        __syncthreads();      // one per turn: the slots of the turn before last are written again only after the last one's barrier
+        // One barrier per turn: the slots of the turn before last are written again only after the last one's, and the row has left its stage.
+        __syncthreads();
+        if (tid == 0 && left > stages) request(stage);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
         mean = slots[turn][0].x;
         squares = slots[turn][0].y;
         for (int i = 1; i < warps; ++i) {
@@ -323,15 +375,18 @@ norm_forward_row_kernel(const NormArgs a)
             mean = fmaf(d, f.x, mean);
         }
         const float rstd = rsqrtf(squares * a.inv_n + a.eps);
-        if (a.stats && tid == 0) *(float2 *)(a.stats + 2 * r) = make_float2(x0 + mean, rstd);
+        if (stats && tid == 0) *(float2 *)stats = make_float2(x0 + mean, rstd);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = u * threads + tid;
             if (j >= rc.units) continue;
             normed(v[u], mean - mine, rstd, w, b, j, rc.units);
-            store_unit<T, EDGE>((T *)a.y + r * a.ldy, j * V - rc.shift, a.cols, v[u]);
+            store_unit<T, EDGE>(y, j * V - rc.shift, a.cols, v[u]);
         }
+        y += rc.step * a.ldy;
+        if (stats) stats += 2 * rc.step;
     }
+    note_gave_up(gave_up);
 }
 
 // Any width and alignment: three passes over the row.
@@ -361,24 +416,39 @@ norm_forward_wide_kernel(const NormArgs a)
     }
 }
 
-// A CTA walks over rows of its class; U units per thread, whose columns stay the same, so that the column sums stay in registers.  The next row is
-// on its way while one is worked on.  Rows are held as they were read and their values formed twice, for the sums and for
-// dx: registers bound how many rows are in flight.  weight is in shared memory, by unit.  DB: the sums of dy are wanted too.
-// Many entries per thread and few threads: what a row costs beside its entries (reductions, barrier, addresses) is some 150 instructions per warp.
+// A CTA walks over rows of its class; U units per thread, whose columns stay the same, so that the column sums stay in registers.  x and dy come
+// through a ring of `stages` rows; weight is in shared memory, by unit.  DB: the sums of dy are wanted too.
 template <typename T, int U, bool DB, bool EDGE, int THREADS, int CTAS>
 __global__ void __launch_bounds__(THREADS, CTAS)
-norm_backward_kernel(const NormArgs a)
+norm_backward_kernel(const NormArgs a, int stages)
 {
     constexpr int V = Unit<T>::V, P = V / 2;
-    extern __shared__ float4 shared_params[];
-    __shared__ float4 slots[2][8];       // the warps' pairs of sums, two in a vector
+    extern __shared__ float4 shared[];       // weight, ring
+    __shared__ uint64_t bars[NORM_STAGES];
+    __shared__ float4 slots[2][16];          // the warps' pairs of sums, two in a vector
     pdl_trigger();
     pdl_wait();
     const int tid = threadIdx.x, threads = blockDim.x, warp = tid >> 5, lane = tid & 31, warps = threads >> 5;
     const RowClass rc = row_class<T>(a.x, a.ldx, a.cols, a.period, blockIdx.x, gridDim.x);
-    float *weight = (float *)shared_params;
+    float *weight = (float *)shared;
+    const uint4 *ring = (const uint4 *)(weight + rc.units * V);      // per stage x, then dy
+    int64_t left = rc.first < a.rows ? (a.rows - rc.first + rc.step - 1) / rc.step : 0;
+    const T *ask_x = (const T *)a.x + rc.first * a.ldx, *ask_dy = (const T *)a.dy + rc.first * a.lddy;
+    auto request = [&](int stage) {      // the next row, by one thread
+        const uint32_t bar = smem_u32(bars + stage), at = smem_u32(ring + stage * 2 * rc.units);
+        mbar_expect_tx(bar, (uint32_t)rc.units * 32u);
+        ask_row<T>(at, ask_x, rc, bar);
+        ask_row<T>(at + (uint32_t)rc.units * 16u, ask_dy, rc, bar);
+        ask_x += rc.step * a.ldx;
+        ask_dy += rc.step * a.lddy;
+    };
+    if (tid == 0) {
+        for (int i = 0; i < stages; ++i) mbar_init(smem_u32(bars + i), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        for (int i = 0; i < stages && i < left; ++i) request(i);
+    }
     share_params<T>(a, rc, weight, nullptr);
-    for (int i = tid; i < 2 * 8; i += threads) ((float4 *)slots)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int i = tid; i < 2 * 16; i += threads) ((float4 *)slots)[i] = make_float4(0.f, 0.f, 0.f, 0.f);
     float2 dw[U][P], db[DB ? U : 1][P];
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -387,21 +457,6 @@ norm_backward_kernel(const NormArgs a)
             dw[u][i] = pair(0.f);
             if (DB) db[u][i] = pair(0.f);
         }
-    uint4 nx[U], ng[U];
-    float2 nst = pair(0.f);
-    auto fetch = [&](int64_t r) {
-        if (r >= a.rows) return;
-        nst = *(const float2 *)(a.stats_in + 2 * r);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = u * threads + tid;
-            nx[u] = ng[u] = make_uint4(0, 0, 0, 0);
-            if (j < rc.units) {
-                nx[u] = load_unit<T, EDGE>((const T *)a.x + r * a.ldx, j * V - rc.shift, a.cols, T(0.f));
-                ng[u] = load_unit<T, EDGE>((const T *)a.dy + r * a.lddy, j * V - rc.shift, a.cols, T(0.f));
-            }
-        }
-    };
     auto weights = [&](int u, float2 (&w)[P]) {
         const int j = min(u * threads + tid, rc.units - 1);      // (a thread without a unit has dy = 0)
 #pragma unroll
@@ -411,18 +466,29 @@ norm_backward_kernel(const NormArgs a)
             w[i + 1] = make_float2(t.z, t.w);
         }
     };
-    fetch(rc.first);
     __syncthreads();
-    int turn = 0;
-    for (int64_t r = rc.first; r < a.rows; r += rc.step, turn ^= 1) {
+    bool gave_up = false;
+    int turn = 0, stage = 0;
+    uint32_t phase = 0;
+    T *y = (T *)a.y + rc.first * a.ldy;
+    const float2 *stats = (const float2 *)a.stats_in + rc.first;
+    float2 next = left > 0 ? *stats : pair(0.f);
+    for (; left > 0; --left, turn ^= 1) {
+        const float2 st = next;
+        stats += rc.step;
+        if (left > 1) next = *stats;
+        await_row(smem_u32(bars + stage), phase, gave_up);
+        const uint4 *row = ring + stage * 2 * rc.units;
         uint4 x[U], g[U];
-        const float2 st = nst;
-#pragma unroll
-        for (int u = 0; u < U; ++u) { x[u] = nx[u]; g[u] = ng[u]; }
-        fetch(r + rc.step);
         float2 s1 = pair(0.f), s2 = pair(0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
+            const int j = u * threads + tid, col = j * V - rc.shift;
+            x[u] = g[u] = make_uint4(0, 0, 0, 0);
+            if (j < rc.units) {
+                x[u] = take_unit<T, EDGE>(row, j, col, a.cols);
+                g[u] = take_unit<T, EDGE>(row + rc.units, j, col, a.cols);
+            }
             float2 w[P], xv[P], gv[P];
             weights(u, w);
             unit_pairs(x[u], xv);
@@ -436,37 +502,41 @@ norm_backward_kernel(const NormArgs a)
                 s1 = add2(s1, gw);
                 s2 = fma2(gw, h, s2);
             }
-            forget(x[u]);
-            forget(g[u]);
         }
         float2 s = make_float2(s1.x + s1.y, s2.x + s2.y);
 #pragma unroll
         for (int o = 16; o; o >>= 1) s = add2(s, make_float2(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o)));
+        // One barrier per turn: the slots of the turn before last are written again only after the last one's, and the rows have left their stage.
         if (warps > 1) {
             if (lane == 0) ((float2 *)slots[turn])[warp] = s;
-            __syncthreads();      // one per turn: the slots of the turn before last are written again only after the last one's barrier
+            __syncthreads();
             s = pair(0.f);
             for (int i = 0; i < (warps + 1) / 2; ++i) {
                 const float4 t = slots[turn][i];
                 s = add2(s, add2(make_float2(t.x, t.y), make_float2(t.z, t.w)));
             }
-        }
-        if (!a.y) continue;
-        // dx = r g w - r mean(g w) - (x - mu) r^2 mean(g w h)
-        const float2 c1 = pair(a.center ? -s.x * a.inv_n * st.y : 0.f), c2 = pair(-s.y * a.inv_n * st.y * st.y);
+        } else __syncwarp();
+        if (tid == 0 && left > stages) request(stage);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+        if (a.y) {
+            // dx = r g w - r mean(g w) - (x - mu) r^2 mean(g w h)
+            const float2 c1 = pair(a.center ? -s.x * a.inv_n * st.y : 0.f), c2 = pair(-s.y * a.inv_n * st.y * st.y);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = u * threads + tid;
-            if (j >= rc.units) continue;
-            float2 w[P], xv[P], gv[P];
-            weights(u, w);
-            unit_pairs(x[u], xv);
-            unit_pairs(g[u], gv);
+            for (int u = 0; u < U; ++u) {
+                const int j = u * threads + tid;
+                if (j >= rc.units) continue;
+                float2 w[P], xv[P], gv[P];
+                weights(u, w);
+                unit_pairs(x[u], xv);
+                unit_pairs(g[u], gv);
 #pragma unroll
-            for (int i = 0; i < P; ++i) gv[i] = fma2(mul2(gv[i], w[i]), pair(st.y), fma2(add2(xv[i], pair(-st.x)), c2, c1));
-            store_unit<T, EDGE>((T *)a.y + r * a.ldy, j * V - rc.shift, a.cols, gv);
+                for (int i = 0; i < P; ++i) gv[i] = fma2(mul2(gv[i], w[i]), pair(st.y), fma2(add2(xv[i], pair(-st.x)), c2, c1));
+                store_unit<T, EDGE>(y, j * V - rc.shift, a.cols, gv);
+            }
+            y += rc.step * a.ldy;
         }
     }
+    note_gave_up(gave_up);
     // column sums of this CTA
 #pragma unroll
     for (int u = 0; u < U; ++u)
@@ -528,6 +598,17 @@ norm_columns_kernel(const NormArgs a, int64_t rows_per)
     if (a.want_db) a.partial[((int64_t)(a.want_dw ? gridDim.y : 0) + blockIdx.y) * a.cols + c] = db;
 }
 
+cudaError_t norm_status_read(int32_t *status, cudaStream_t stream)
+{
+    int zero = 0, v = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&v, g_norm_status, sizeof(int), 0, cudaMemcpyDeviceToHost, stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+    if (e == cudaSuccess && v) e = cudaMemcpyToSymbolAsync(g_norm_status, &zero, sizeof(int), 0, cudaMemcpyHostToDevice, stream);
+    if (e == cudaSuccess) e = cudaStreamSynchronize(stream);
+    *status = v;
+    return e;
+}
+
 namespace {
 
 constexpr int64_t ROW_COLS = 8192;          // widest row that the row kernels hold, in whole units
@@ -558,50 +639,69 @@ int any_threads(int64_t cols) { return (int)std::min<int64_t>(1024, std::max<int
 // Rows of whole units have no edges to look at.
 bool has_edges(const NormArgs &a, int V) { return a.period != 1 || a.cols % V || (uintptr_t)a.x % 16; }
 
+// Shared memory of an SM that its CTAs may share out, and a ring's stages in what one of them gets.
+constexpr int SM_SHARED = 216 * 1024;
+int ring_stages(int per_sm, size_t fixed, size_t stage)
+{
+    const int64_t n = (SM_SHARED / per_sm - (int64_t)fixed) / (int64_t)stage;
+    return (int)std::max<int64_t>(1, std::min<int64_t>(NORM_STAGES, n));
+}
+template <typename Kern>
+cudaError_t launch_with(Kern kernel, dim3 grid, int threads, size_t smem, cudaStream_t s, const NormArgs &a, int stages)
+{
+    if (smem > 48 * 1024) {
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_dependent(kernel, grid, dim3(threads), smem, s, 1, a, stages);
+}
+
 template <typename T, bool EDGE>
 cudaError_t forward_as(const NormArgs &a, int units, int sms, cudaStream_t s)
 {
     constexpr int V = Unit<T>::V;
-    const size_t smem = (size_t)units * V * 8;
-    if (a.period && units <= (EDGE ? 128 : 256)) {      // (eight units with edges do not fit the registers)
-        const int u = (units + 31) / 32;
-        const dim3 grid((unsigned)shared_out(a.rows, a.period, 8, sms * (u > 4 || (EDGE && u > 2) ? 2 : u > 2 || EDGE ? 3 : 4)));      // as many as are resident
-        if (u <= 1) return launch_dependent(norm_forward_kernel<T, 1, EDGE>, grid, dim3(256), smem, s, 1, a);
-        if (u <= 2) return launch_dependent(norm_forward_kernel<T, 2, EDGE>, grid, dim3(256), smem, s, 1, a);
-        if (u <= 4) return launch_dependent(norm_forward_kernel<T, 4, EDGE>, grid, dim3(256), smem, s, 1, a);
-        if constexpr (!EDGE) return launch_dependent(norm_forward_kernel<T, 8, false>, grid, dim3(256), smem, s, 1, a);
+    const size_t params = (size_t)units * V * 8, row = (size_t)units * 16;
+    if (a.period && units <= 256) {
+        const int u = (units + 31) / 32, per_sm = u > 4 ? 2 : u > 2 ? 3 : 4;      // as many as are resident
+        const dim3 grid((unsigned)shared_out(a.rows, a.period, 8, sms * per_sm));
+        const int stages = ring_stages(per_sm, params, 8 * row);
+        const size_t smem = params + 8 * stages * row;
+        if (u <= 1) return launch_with(norm_forward_kernel<T, 1, EDGE>, grid, 256, smem, s, a, stages);
+        if (u <= 2) return launch_with(norm_forward_kernel<T, 2, EDGE>, grid, 256, smem, s, a, stages);
+        if (u <= 4) return launch_with(norm_forward_kernel<T, 4, EDGE>, grid, 256, smem, s, a, stages);
+        return launch_with(norm_forward_kernel<T, 8, EDGE>, grid, 256, smem, s, a, stages);
     }
     if (a.period && units * V <= ROW_COLS) {
-        constexpr int CTAS = V == 8 ? 3 : 2;
-        const int threads = (int)round_up((units * V + 31) / 32, 32);
-        const dim3 grid((unsigned)shared_out(a.rows, a.period, 1, sms * std::max(1, std::min(256 * CTAS / threads, (int)(200 * 1024 / smem)))));
-        auto kernel = norm_forward_row_kernel<T, 32 / V, EDGE, 256, CTAS>;
-        if (smem > 48 * 1024) {
-            const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-            if (e != cudaSuccess) return e;
-        }
-        return launch_dependent(kernel, grid, dim3(threads), smem, s, 1, a);
+        constexpr int U = 32 / V, CTAS = V == 8 ? 3 : 2;
+        const int threads = (int)round_up((units + U - 1) / U, 32);
+        const int per_sm = std::max(1, std::min(256 * CTAS / threads, (int)(SM_SHARED / (params + 2 * row))));
+        const dim3 grid((unsigned)shared_out(a.rows, a.period, 1, sms * per_sm));
+        const int stages = ring_stages(per_sm, params, row);
+        return launch_with(norm_forward_row_kernel<T, U, EDGE, 256, CTAS>, grid, threads, params + stages * row, s, a, stages);
     }
     const int threads = any_threads(a.cols);
     const dim3 grid((unsigned)std::min<int64_t>(a.rows, (int64_t)sms * (2048 / threads)));
     return launch_dependent(norm_forward_wide_kernel<T>, grid, dim3(threads), 0, s, 1, a);
 }
 
-// The backward row kernel's form for a row of that many entries (whole units): entries per thread, threads, CTAs per SM.
-struct BackwardForm { int entries, threads, per_sm; };
-BackwardForm backward_form(int64_t entries_in_units, int V)
+// The backward row kernel's form for a row of that many units: units per thread, threads, CTAs per SM.
+struct BackwardForm { int per_thread, threads, per_sm; };
+BackwardForm backward_form(int64_t units, int V)
 {
     BackwardForm f;
-    f.entries = entries_in_units <= 256 ? 8 : 16;
-    f.threads = (int)std::max<int64_t>(32, round_up((entries_in_units + f.entries - 1) / f.entries, 32));
-    f.per_sm = std::max(1, (f.entries == 8 ? 640 : V == 4 ? 512 : f.threads <= 128 ? 640 : 768) / f.threads);      // threads on an SM, by their registers
+    f.per_thread = units <= 32 ? 1 : units <= 1024 ? 2 : 4;
+    f.threads = (int)std::max<int64_t>(32, round_up((units + f.per_thread - 1) / f.per_thread, 32));
+    f.per_sm = f.per_thread == 4 ? 1 : std::min(24, (f.threads > 128 ? 768 : V == 8 ? 640 : 896) / f.threads);      // by their registers
+    const int64_t least = units * (V * 4 + 2 * 32);      // weight and two stages
+    if (least > 0) f.per_sm = (int)std::min<int64_t>(f.per_sm, SM_SHARED / least);
+    f.per_sm = std::max(1, f.per_sm);
     return f;
 }
 // Partial rows of column sums that a backward pass leaves.
-int backward_parts(int64_t rows, int64_t entries_in_units, int V, int period, int sms)
+int backward_parts(int64_t rows, int64_t units, int V, int period, int sms)
 {
-    if (entries_in_units > ROW_COLS || period == 0) return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, 2 * sms));
-    return (int)shared_out(rows, period, 1, (int64_t)sms * backward_form(entries_in_units, V).per_sm);
+    if (units * V > ROW_COLS || period == 0) return (int)std::max<int64_t>(1, std::min<int64_t>((rows + 31) / 32, 2 * sms));
+    return (int)shared_out(rows, period, 2, (int64_t)sms * backward_form(units, V).per_sm);
 }
 // ... and the most for any alignment of the matrices.
 int most_parts(const tsr_norm_desc &d, int sms)
@@ -609,7 +709,7 @@ int most_parts(const tsr_norm_desc &d, int sms)
     const int V = 16 / type_bytes(d.dtype);
     int most = backward_parts(d.rows, 0, V, 0, sms);
     for (int period = 1; period <= V; period *= 2)
-        for (int shift = 0; shift < V; ++shift) most = std::max(most, backward_parts(d.rows, round_up(d.cols + shift, V), V, period, sms));
+        for (int shift = 0; shift < V; ++shift) most = std::max(most, backward_parts(d.rows, (d.cols + shift + V - 1) / V, V, period, sms));
     return most;
 }
 
@@ -617,13 +717,15 @@ template <typename T, bool DB, bool EDGE>
 cudaError_t backward_as(const NormArgs &a, int units, int parts, cudaStream_t s)
 {
     constexpr int V = Unit<T>::V;
-    const BackwardForm f = backward_form((int64_t)units * V, V);
-    const dim3 grid(parts), block(f.threads);
-    const size_t smem = (size_t)units * V * 4;
-    if (f.entries == 8) return launch_dependent(norm_backward_kernel<T, 8 / V, DB, EDGE, 32, 20>, grid, block, smem, s, 1, a);
-    if (f.threads <= 128) return launch_dependent(norm_backward_kernel<T, 16 / V, DB, EDGE, 128, V == 8 ? 5 : 4>, grid, block, smem, s, 1, a);
-    if (f.threads <= 384 && V == 8) return launch_dependent(norm_backward_kernel<T, 16 / V, DB, EDGE, 384, 2>, grid, block, smem, s, 1, a);
-    return launch_dependent(norm_backward_kernel<T, 16 / V, DB, EDGE, 512, 1>, grid, block, smem, s, 1, a);
+    const BackwardForm f = backward_form(units, V);
+    const size_t fixed = (size_t)units * V * 4, stage = (size_t)units * 32;
+    const int stages = ring_stages(f.per_sm, fixed, stage);
+    const size_t smem = fixed + stages * stage;
+    if (f.per_thread == 1) return launch_with(norm_backward_kernel<T, 1, DB, EDGE, 32, 24>, dim3(parts), f.threads, smem, s, a, stages);
+    if (f.per_thread == 4) return launch_with(norm_backward_kernel<T, 4, DB, EDGE, 512, 1>, dim3(parts), f.threads, smem, s, a, stages);
+    if (f.threads <= 128) return launch_with(norm_backward_kernel<T, 2, DB, EDGE, 128, V == 8 ? 5 : 7>, dim3(parts), f.threads, smem, s, a, stages);
+    if (f.threads <= 384) return launch_with(norm_backward_kernel<T, 2, DB, EDGE, 384, 2>, dim3(parts), f.threads, smem, s, a, stages);
+    return launch_with(norm_backward_kernel<T, 2, DB, EDGE, 512, 1>, dim3(parts), f.threads, smem, s, a, stages);
 }
 
 template <typename T>
@@ -732,12 +834,11 @@ extern "C" tsr_status tsr_norm_backward(const tsr_norm_desc *desc, tsr_matrix dy
     int units = 0;
     a.period = d.rows > 0 ? common_period(d, all, 3, &units) : 0;
     const int V = 16 / type_bytes(d.dtype);
-    const int64_t entries = (int64_t)units * V;
-    const int parts = backward_parts(d.rows, entries, V, a.period, sms);
+    const int parts = backward_parts(d.rows, units, V, a.period, sms);
     if (d.rows > 0) {
         const bool bf = d.dtype == TSR_BF16;
         cudaError_t e;
-        if (a.period == 0 || entries > ROW_COLS) e = bf ? backward_wide<bf16>(a, parts, sms, s) : backward_wide<float>(a, parts, sms, s);
+        if (a.period == 0 || units * V > ROW_COLS) e = bf ? backward_wide<bf16>(a, parts, sms, s) : backward_wide<float>(a, parts, sms, s);
         else e = bf ? backward_of<bf16>(a, units, parts, s) : backward_of<float>(a, units, parts, s);
         if (e != cudaSuccess) return TSR_ERR_CUDA;
     }
