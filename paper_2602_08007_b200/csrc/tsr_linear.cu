@@ -119,23 +119,21 @@ linear_split_kernel(const float *__restrict__ src, int64_t lds, bf16 *__restrict
 }
 
 // Split tiles: the slabs of a tile (tile_m x width, FP32, one behind the other) are added in order, then the epilogue runs.  With `slabs` NULL the
-// sum is zero and the tiles cover the whole matrix (K = 0).  A thread takes four neighbours of a row.
+// sum is zero and the tiles cover the whole matrix (K = 0).  A thread takes eight neighbours of a row.
 struct FinishArgs {
     LinearTiles g;
     const float *slabs;
     int32_t tile_m, tail, out_f32;     // tiles that were split; type of out, residual and pre
-    int32_t vec;                       // four neighbours of out, residual and pre can be moved at once
+    int32_t vec;                       // eight neighbours of out, residual and pre can be moved at once
     LinearEpilogue e;
 };
 template <typename T>
-__device__ __forceinline__ void store4(T *p, const float (&v)[4], int n, bool vec)
+__device__ __forceinline__ void store_some(T *p, const float (&v)[8], int n, bool vec)
 {
-    if (vec && n == 4) {
-        if (sizeof(T) == 2) *(uint2 *)p = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
-        else *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
-    } else {
+    if (vec && n == 8) store8(p, v);
+    else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) if (j < n) store_f(p + j, v[j]);
+        for (int j = 0; j < 8; ++j) if (j < n) store_f(p + j, v[j]);
     }
 }
 template <typename T>
@@ -145,45 +143,65 @@ linear_finish_kernel(const __grid_constant__ FinishArgs a)
     pdl_trigger();
     pdl_wait();
     const LinearEpilogue &e = a.e;
-    const uint32_t per_row = a.g.width / 4, per_tile = a.tile_m * per_row;
+    const uint32_t per_row = a.g.width / 8, per_tile = a.tile_m * per_row;
     const int64_t total = (int64_t)a.tail * per_tile;
     const uint32_t call_key = e.drop.threshold ? drop_call_key(e.drop) : 0u;
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
         const int tail = (int)(u / per_tile);
-        const uint32_t in = (uint32_t)(u - (int64_t)tail * per_tile), rr = in / per_row, cc = (in - rr * per_row) * 4;
+        const uint32_t in = (uint32_t)(u - (int64_t)tail * per_tile), rr = in / per_row, cc = (in - rr * per_row) * 8;
         int m0, n0;
         linear_tile_at(a.g, a.g.whole + tail, a.tile_m, m0, n0);
         const int64_t r = m0 + (int64_t)rr;
-        const int c = n0 + (int)cc, n = min(4, a.g.N - c);
+        const int c = n0 + (int)cc, n = min(8, a.g.N - c);
         if (r >= a.g.M || n <= 0) continue;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, o[8];
+        if (e.res) {
+            const T *res = (const T *)e.res + r * e.ldr + c;
+            if (a.vec && n == 8) load8(res, o);
+            else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = j < n ? load_f(res + j) : 0.f;
+            }
+        }
         if (a.slabs) {
-            const float *s = a.slabs + (int64_t)tail * a.g.splits * a.tile_m * a.g.width + (int64_t)in * 4;
+            const float *s = a.slabs + (int64_t)tail * a.g.splits * a.tile_m * a.g.width + (int64_t)in * 8;
 #pragma unroll 4
             for (int p = 0; p < a.g.splits; ++p) {
-                const float4 x = *(const float4 *)(s + (int64_t)p * a.tile_m * a.g.width);
-                v[0] += x.x; v[1] += x.y; v[2] += x.z; v[3] += x.w;
+                float x[8];
+                load8(s + (int64_t)p * a.tile_m * a.g.width, x);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] += x[j];
             }
         }
         if (e.bias) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) if (j < n) v[j] += load_as(e.bias, c + j, e.bias_bf16);
+            for (int j = 0; j < 8; ++j) if (j < n) v[j] += load_as(e.bias, c + j, e.bias_bf16);
         }
-        if (e.pre) store4((T *)e.pre + r * e.ldp + c, v, n, a.vec);
+        if (e.pre) store_some((T *)e.pre + r * e.ldp + c, v, n, a.vec);
         if (e.act) {
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j) {
+                // (one copy of the activation's code: rotated through the first place)
+                const float z = act_value(e.act, v[0]);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = act_value(e.act, v[j]);
+                for (int i = 0; i < 7; ++i) v[i] = v[i + 1];
+                v[7] = z;
+            }
         }
         if (e.drop.threshold) {
             const DropRow key = drop_row_key(call_key, r);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = drop_entry(key, (uint32_t)(c + j), v[j], e.drop);
+            for (int j = 0; j < 8; j += 2) {
+                const uint32_t w = drop_word(key, (uint32_t)(c + j) >> 1);
+                v[j] = drop_lo(w, v[j], e.drop);
+                v[j + 1] = drop_hi(w, v[j + 1], e.drop);
+            }
         }
         if (e.res) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) if (j < n) v[j] += load_f((const T *)e.res + r * e.ldr + c + j);
+            for (int j = 0; j < 8; ++j) v[j] += o[j];
         }
-        store4((T *)e.out + r * e.ldo + c, v, n, a.vec);
+        store_some((T *)e.out + r * e.ldo + c, v, n, a.vec);
     }
 }
 
@@ -355,22 +373,25 @@ EncodeTiledFn encoder()
     return fn;
 }
 
-// Row-major matrix, boxes of 128 bytes x box_rows with the 128-byte swizzle; planes > 1: that many of them, `plane` entries apart, in one box.
-bool encode(CUtensorMap *out, const void *base, int64_t rows, int64_t cols, int64_t ld, bool f32, int box_rows, int planes = 1, int64_t plane = 0)
+// Row-major matrix, boxes of `inner` bytes (128 or 64, with the swizzle of that width) x box_rows; planes > 1: that many of them, `plane` entries
+// apart, in one box.
+bool encode(CUtensorMap *out, const void *base, int64_t rows, int64_t cols, int64_t ld, bool f32, int box_rows, int inner = 128, int planes = 1, int64_t plane = 0)
 {
     EncodeTiledFn fn = encoder();
     if (!fn) return false;
     const int es = f32 ? 4 : 2;
     if (rows <= 1) ld = round_up(cols, 16 / es);         // a single row has no pitch
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)ld * es, (cuuint64_t)plane * es};
-    const cuuint32_t box[3] = {(cuuint32_t)(128 / es), (cuuint32_t)box_rows, (cuuint32_t)planes}, step[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {(cuuint32_t)(inner / es), (cuuint32_t)box_rows, (cuuint32_t)planes}, step[3] = {1, 1, 1};
     return fn(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, planes > 1 ? 3 : 2, const_cast<void *>(base), dims, strides, box, step,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+              CU_TENSOR_MAP_INTERLEAVE_NONE, inner == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 bool tma_takes(const void *p, int64_t rows, int64_t ld, int es) { return aligned_to(p, 16) && (rows <= 1 || (ld * es) % 16 == 0); }
 
-struct Operand { const void *p; int64_t ld; bool mn; };   // [rows x K], or (mn) stored as [K x rows]
+// [rows x K], or (mn) stored as [K x rows].  FP32 operands come as three BF16 planes, `plane` entries apart (see three_planes).
+struct Operand { const void *p; int64_t ld; bool mn; int64_t plane; };
 
 struct Product {
     int64_t M, N, K;
@@ -382,7 +403,7 @@ struct Product {
 
 struct Shape { int cg, width, splits, kb, kb_per; int64_t m_tiles, n_tiles, whole, tail; };   // tail: tiles that are split
 
-// Tile shape and split of K by a model in SM clocks.  A K block of 64 entries costs the MMAs 2 width clocks (six times that for FP32) and the SM's
+// Tile shape and split of K by a model in SM clocks.  A K block of 64 entries costs the MMAs 2 width clocks (32 of FP32: 6 width) and the SM's
 // intake of 64 bytes a clock its share of the operands; a wave of tiles costs the larger one times its blocks.  The tiles of the last wave
 // (and, where that is nearly full, of the one before) may be split, so that the last wave is short: for that their slabs are
 // written (32 bytes a clock and SM) and read again (3000 bytes a clock in all) by another launch.
@@ -390,14 +411,14 @@ Shape choose(const Product &p, int sms)
 {
     Shape best = {};
     double best_cost = 1e300;
-    const int kb = (int)((p.K + 63) / 64);
+    const int bk = p.f32 ? 32 : 64, kb = (int)((p.K + bk - 1) / bk);
     static const struct { int cg, width; } kinds[] = {{2, 256}, {2, 192}, {2, 128}, {2, 64}, {1, 128}, {1, 64}};
     for (const auto &k : kinds) {
         if (p.f32 && k.width > 128) continue;
         const int64_t mt = (p.M + 128 * k.cg - 1) / (128 * k.cg), nt = (p.N + k.width - 1) / k.width, tiles = mt * nt;
         const int slots = sms / k.cg;
-        const double mma = (p.f32 ? 12.0 : 2.0) * k.width, intake = (p.f32 ? 6.0 : 2.0) * (128 + k.width / k.cg);
-        const int stage = (p.f32 ? 3 : 1) * 128 * (128 + k.width / k.cg), stages = linear_stages(stage, p.e.pre != nullptr);
+        const double mma = (p.f32 ? 6.0 : 2.0) * k.width, intake = (p.f32 ? 3.0 : 2.0) * (128 + k.width / k.cg);
+        const int stage = (p.f32 ? 3 * 64 : 128) * (128 + k.width / k.cg), stages = linear_stages(stage, p.e.pre != nullptr);
         // (with a single stage loads and MMAs take turns)
         const double per_kb = stages > 1 ? std::max(mma, intake) : mma + intake + 1000.0, tile = kb * per_kb + 300.0, last = 3000.0 + 12.0 * k.width;
         const int64_t full = tiles / slots, rem = tiles % slots;
@@ -440,9 +461,9 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
     FinishArgs f = {};
     f.out_f32 = p.out_f32;
     f.e = p.e;
-    f.vec = out_tma && (!p.e.pre || pre_tma);
+    f.vec = out_tma && (!p.e.pre || pre_tma) && (!p.e.res || res_tma);
     auto finish = [&]() -> tsr_status {
-        const int64_t units = (int64_t)f.tail * f.tile_m * (f.g.width / 4);
+        const int64_t units = (int64_t)f.tail * f.tile_m * (f.g.width / 8);
         const dim3 grid((unsigned)std::min<int64_t>((units + 255) / 256, (int64_t)sms * 16));
         const cudaError_t rc = f.out_f32 ? launch_dependent(linear_finish_kernel<float>, grid, dim3(256), 0, stream, 1, f) : launch_dependent(linear_finish_kernel<bf16>, grid, dim3(256), 0, stream, 1, f);
         return rc == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
@@ -465,33 +486,32 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
     g.kb_total = s.kb; g.kb_per = s.kb_per;
 
     // operands
-    const int planes = p.f32 ? 3 : 1;
+    const int planes = p.f32 ? 3 : 1, inner = p.f32 ? 64 : 128;
     const Operand *op[2] = {&p.A, &p.B};
     const int64_t extent[2] = {p.M, p.N};
     for (int i = 0; i < 2; ++i) {
         const Operand &o = *op[i];
         const int64_t rows = o.mn ? p.K : extent[i], cols = o.mn ? extent[i] : p.K;    // as stored
         const void *at = o.p;
-        int64_t ld = o.ld, plane = 0;
-        if (p.f32 || !tma_takes(o.p, rows, o.ld, 2)) {
+        int64_t ld = o.ld;
+        if (!p.f32 && !tma_takes(o.p, rows, o.ld, 2)) {
             ld = round_up(cols, 64);
-            plane = rows * ld;
-            bf16 *copy = (bf16 *)room.take((size_t)planes * plane * 2);
+            bf16 *copy = (bf16 *)room.take((size_t)rows * ld * 2);
             if (run) {
                 const int units = (int)((cols + 7) / 8);
                 const dim3 grid((unsigned)std::min<int64_t>((rows * units + 255) / 256, (int64_t)sms * 32));
-                const cudaError_t rc = p.f32 ? launch_dependent(linear_split_kernel, grid, dim3(256), 0, stream, 1, (const float *)o.p, o.ld, copy, ld, plane, rows, (int)cols, units)
-                                             : launch_dependent(linear_pack_kernel, grid, dim3(256), 0, stream, 1, (const bf16 *)o.p, o.ld, copy, ld, rows, (int)cols, units);
-                if (rc != cudaSuccess) return TSR_ERR_CUDA;
+                if (launch_dependent(linear_pack_kernel, grid, dim3(256), 0, stream, 1, (const bf16 *)o.p, o.ld, copy, ld, rows, (int)cols, units) != cudaSuccess) return TSR_ERR_CUDA;
             }
             at = copy;
         }
-        const int box_rows = o.mn ? 64 : i ? s.width / s.cg : 128;
-        if (run && !encode(i ? &g.tmB : &g.tmA, at, rows, cols, ld, false, box_rows, planes, plane)) return TSR_ERR_CUDA;
+        // an MN-major box: 64 entries side by side (128 bytes) x the K block; a K-major one: the K block x the rows of a CTA
+        const bool ok = !run || (o.mn ? encode(i ? &g.tmB : &g.tmA, at, rows, cols, ld, false, inner / 2, 128, planes, o.plane)
+                                      : encode(i ? &g.tmB : &g.tmA, at, rows, cols, ld, false, i ? s.width / s.cg : 128, inner, planes, o.plane));
+        if (!ok) return TSR_ERR_CUDA;
         (i ? g.b_mn : g.a_mn) = o.mn;
     }
     g.b_boxes = (s.width / s.cg + 63) / 64;
-    const int a_bytes = planes * 128 * 128, b_bytes = planes * (g.b_mn ? g.b_boxes * 8192 : s.width / s.cg * 128);
+    const int a_bytes = planes * 128 * inner, b_bytes = planes * (g.b_mn ? g.b_boxes * 64 * inner : s.width / s.cg * inner);
     g.b_offset = a_bytes;
     g.stage_bytes = a_bytes + b_bytes;
     g.stage_tx = (uint32_t)(s.cg * g.stage_bytes);
@@ -517,6 +537,20 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
     f.tile_m = 128 * s.cg;
     f.tail = (int)s.tail;
     return finish();
+}
+
+// Three BF16 planes of an FP32 matrix (rows x cols) in the workspace, as an operand.
+tsr_status three_planes(const tsr_matrix &m, int64_t rows, int64_t cols, bool mn, Operand *o, Room &room, bool run, int sms, cudaStream_t stream)
+{
+    o->ld = round_up(std::max<int64_t>(cols, 1), 64);
+    o->plane = std::max<int64_t>(rows, 1) * o->ld;
+    o->mn = mn;
+    bf16 *copy = (bf16 *)room.take((size_t)3 * o->plane * 2);
+    o->p = copy;
+    if (!run || rows == 0 || cols == 0) return TSR_OK;
+    const int units = (int)((cols + 7) / 8);
+    const dim3 grid((unsigned)std::min<int64_t>((rows * units + 255) / 256, (int64_t)sms * 32));
+    return launch_dependent(linear_split_kernel, grid, dim3(256), 0, stream, 1, (const float *)m.data, m.ld, copy, o->ld, o->plane, rows, (int)cols, units) == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
 }
 
 constexpr int64_t MOST = 0x7fffffff - 1023;
@@ -554,16 +588,24 @@ tsr_status forward(const tsr_linear_desc *d, const tsr_linear_io *io, void *work
     if (!aligned_to(io->bias, type_bytes(d->b_dtype))) return TSR_ERR_ALIGNMENT;
     p.M = d->rows; p.N = d->outs; p.K = d->ins;
     p.f32 = p.out_f32 = d->dtype == TSR_F32;
-    p.A = {io->x.data, io->x.ld, false};
-    p.B = {io->weight.data, io->weight.ld, false};
+    p.A = {io->x.data, io->x.ld, false, 0};
+    p.B = {io->weight.data, io->weight.ld, false, 0};
     p.e.out = io->y.data; p.e.ldo = io->y.ld;
     p.e.res = io->residual.data; p.e.ldr = io->residual.ld;
     p.e.pre = io->pre.data; p.e.ldp = io->pre.ld;
     p.e.bias = io->bias; p.e.bias_bf16 = d->b_dtype == TSR_BF16;
     p.e.act = d->activation;
     const int sms = device_sms();
+    const auto all = [&](Room &room, bool run, int n) -> tsr_status {
+        if (p.f32 && p.M > 0 && p.N > 0 && p.K > 0) {
+            tsr_status e = three_planes(io->x, d->rows, d->ins, false, &p.A, room, run, n, stream);
+            if (e == TSR_OK) e = three_planes(io->weight, d->outs, d->ins, false, &p.B, room, run, n, stream);
+            if (e != TSR_OK) return e;
+        }
+        return product(p, room, run, n, stream);
+    };
     Room count = {nullptr, 0};
-    st = product(p, count, false, sms ? sms : 148, stream);
+    st = all(count, false, sms ? sms : 148);
     if (st != TSR_OK) return st;
     if (need) { *need = count.at; return TSR_OK; }
     if (count.at && (!workspace || bytes < count.at)) return TSR_ERR_WORKSPACE;
@@ -571,7 +613,7 @@ tsr_status forward(const tsr_linear_desc *d, const tsr_linear_io *io, void *work
     if (p.M == 0 || p.N == 0) return TSR_OK;
     if (!sms) return TSR_ERR_CUDA;
     Room room = {(char *)workspace, 0};
-    return product(p, room, true, sms, stream);
+    return all(room, true, sms);
 }
 
 constexpr int DZ_COLS = 256;
@@ -631,14 +673,22 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             if (rc != cudaSuccess) return TSR_ERR_CUDA;
         }
         if (run && db && column_finish(partial, T ? (int)parts : 0, O, O, io->dbias, d->gb_dtype == TSR_BF16, nullptr, false, d->accumulate != 0, stream) != cudaSuccess) return TSR_ERR_CUDA;
+        // FP32: planes of what both products, or one of them, read
+        Operand dz_op = {dz.data, dz.ld, false, 0}, w_op = {io->weight.data, io->weight.ld, true, 0}, x_op = {io->x.data, io->x.ld, true, 0};
+        if (f32 && T > 0 && O > 0 && I > 0) {
+            if (dx || dw) st = three_planes(dz, T, O, false, &dz_op, room, run, sms, stream);
+            if (st == TSR_OK && dx) st = three_planes(io->weight, O, I, true, &w_op, room, run, sms, stream);
+            if (st == TSR_OK && dw) st = three_planes(io->x, T, I, true, &x_op, room, run, sms, stream);
+            if (st != TSR_OK) return st;
+        }
         // the two products run one after the other: they share what is left of the workspace
         size_t after = room.at;
         if (dx) {
             px = {};
             px.M = T; px.N = I; px.K = O;
             px.f32 = px.out_f32 = f32;
-            px.A = {dz.data, dz.ld, false};
-            px.B = {io->weight.data, io->weight.ld, true};
+            px.A = dz_op;
+            px.B = w_op;
             px.e.out = io->dx.data; px.e.ldo = io->dx.ld;
             Room own = room;
             st = product(px, own, run, sms, stream);
@@ -650,8 +700,9 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             pw.M = O; pw.N = I; pw.K = T;
             pw.f32 = f32;
             pw.out_f32 = d->gw_dtype == TSR_F32;
-            pw.A = {dz.data, dz.ld, true};
-            pw.B = {io->x.data, io->x.ld, true};
+            pw.A = dz_op;
+            pw.A.mn = true;
+            pw.B = x_op;
             pw.e.out = io->dweight.data; pw.e.ldo = io->dweight.ld;
             if (d->accumulate) { pw.e.res = pw.e.out; pw.e.ldr = pw.e.ldo; }
             Room own = room;

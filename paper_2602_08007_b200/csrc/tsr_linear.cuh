@@ -20,12 +20,12 @@ struct LinearTiles {
     int32_t M, N;
     int32_t width, m_tiles, n_tiles;     // tile width, a multiple of 64
     int32_t whole, splits, items;
-    int32_t kb_total, kb_per;            // K blocks of 64 entries
+    int32_t kb_total, kb_per;            // K blocks (64 entries; 32 of FP32 operands)
 };
 
 struct alignas(64) LinearGemm : LinearTiles {
-    // operands: K-major boxes of 64 entries x (128 or width / CG) rows, MN-major boxes of 64 x 64, 128-byte swizzle; of FP32 operands all
-    // three planes (third dimension); out, residual, pre and slabs: boxes of 128 bytes x 32 rows, 128-byte swizzle
+    // operands: K-major boxes of 64 entries x (128 or width / CG) rows, MN-major boxes of 64 x 64, 128-byte swizzle; of FP32 operands half as
+    // much of K (K-major: 64-byte swizzle) of all three planes (third dimension); out, residual, pre and slabs: boxes of 128 bytes x 32 rows, 128-byte swizzle
     CUtensorMap tmA, tmB, tmOut, tmRes, tmPre, tmSlab;
     int32_t a_mn, b_mn, b_boxes;         // operand forms; MN-major boxes of B per CTA
     int32_t stages, stage_bytes, b_offset;   // the ring in shared memory

@@ -11,7 +11,8 @@
 // FP32 operands come as three BF16 planes (x = p1 + p2 + p3, 24 bits) and D = p1 q1 + (p1 q2 + p2 q1) + (p2 q2 + p1 q3 + p3 q1): six BF16 products
 // cost the tensor cores what three TF32 products cost, keep two bits more, move three quarters of the bytes and take MN-major operands.  The
 // tensor cores cut off what falls below the accumulator's last bit, which adds up over a long K (10^-5 of the result at K = 4096); the
-// accumulator is therefore emptied every 128 entries of K into FP32 registers of the epilogue warps, added to nearest.
+// accumulator is therefore emptied every 128 entries of K into FP32 registers of the epilogue warps, added to nearest.  K blocks are 32 entries there:
+// of blocks of 64 only two stages fit, which left the tensor cores waiting for half of the time.
 //
 // Epilogue: a lane holds a row.  A warp's 32 rows x 128 bytes of output form a box in shared memory (128-byte swizzle: free of bank
 // conflicts when the lanes walk their rows), of which it has two, and a third for pre.  The residual is fetched into the box by TMA
@@ -159,11 +160,11 @@ template <int CG, int PLANES, bool F32>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(LG_THREADS, 1)
 linear_gemm_kernel(const __grid_constant__ LinearGemm g)
 {
-    constexpr int TILE_M = CG * UM_BM, BK = 64;      // BK: entries of a 128-byte K block
+    constexpr int TILE_M = CG * UM_BM, BK = PLANES == 3 ? 32 : 64;      // entries of a K block
     constexpr uint32_t TMEM_COLS = CG == 2 && PLANES == 1 ? 512 : 256, ACC_COLS = TMEM_COLS / 2;
     constexpr int CW = F32 ? 32 : 64;                // columns of a box
     constexpr int PAIRS[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};   // planes of A and B, the small products first
-    constexpr int CHUNK = PLANES == 3 ? 2 : 1 << 30; // K blocks per emptying of the accumulator
+    constexpr int CHUNK = PLANES == 3 ? 4 : 1 << 30; // K blocks per emptying of the accumulator
 
     extern __shared__ uint8_t smem_raw[];
     uint8_t *smem = (uint8_t *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
@@ -242,8 +243,8 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
                     } else {      // the three planes at once; an MN-major operand's groups of 64 columns one after the other
                         if (mn) {
                             for (int j = 0; j < boxes; ++j) {
-                                if constexpr (CG == 2) tma_load_3d_pair(st + j * 3 * 8192, map, full, row + 64 * j, kx);
-                                else tma_load_3d(st + j * 3 * 8192, map, full, row + 64 * j, kx);
+                                if constexpr (CG == 2) tma_load_3d_pair(st + j * 3 * 4096, map, full, row + 64 * j, kx);
+                                else tma_load_3d(st + j * 3 * 4096, map, full, row + 64 * j, kx);
                             }
                         } else {
                             if constexpr (CG == 2) tma_load_3d_pair(st, map, full, kx, row);
@@ -259,12 +260,14 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
             uint32_t tc = 0, phase = 0;      // tc: accumulators filled so far
             int stage = 0;
             bool ok = true;
-            // MN-major: groups of 64 columns lie 8 KB apart, three planes of them 24 KB
-            constexpr uint64_t MN3 = ((uint64_t)(3 * 8192 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-            const uint64_t mn_hi = PLANES == 3 ? MN3 : UMMA_DESC_HI_MN;
-            const uint64_t a_hi = g.a_mn ? mn_hi : UMMA_DESC_HI_K, b_hi = g.b_mn ? mn_hi : UMMA_DESC_HI_K;
+            // Three planes: K-major rows of 64 bytes (64-byte swizzle, layout type 4; eight rows 512 bytes apart), MN-major groups of 64 columns x
+            // 32 rows, the three planes of a group one behind the other.
+            constexpr uint64_t K3 = ((uint64_t)1 << 16) | ((uint64_t)(512 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)4 << 61);
+            constexpr uint64_t MN3 = ((uint64_t)(3 * 4096 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+            const uint64_t mn_hi = PLANES == 3 ? MN3 : UMMA_DESC_HI_MN, k_hi = PLANES == 3 ? K3 : UMMA_DESC_HI_K;
+            const uint64_t a_hi = g.a_mn ? mn_hi : k_hi, b_hi = g.b_mn ? mn_hi : k_hi;
             const uint32_t a_step = g.a_mn ? 2048u : 32u, b_step = g.b_mn ? 2048u : 32u;
-            const uint32_t a_plane = g.a_mn ? 8192u : UM_BM * 128u, b_plane = g.b_mn ? 8192u : (uint32_t)(g.width / CG) * 128u;
+            const uint32_t a_plane = g.a_mn ? 4096u : UM_BM * 64u, b_plane = g.b_mn ? 4096u : (uint32_t)(g.width / CG) * 64u;
             // (M = 256 for a pair, 128 for one CTA; FP32 accumulator; BF16 operands)
             const uint32_t form = (g.a_mn ? UMMA_IDESC_A_MN_MAJOR : 0u) | (g.b_mn ? UMMA_IDESC_B_MN_MAJOR : 0u) | (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE_M >> 4) << 24);
             for (int t = first; ok && t < g.items; t += stride) {
@@ -285,7 +288,7 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
 #pragma unroll
                         for (int pr = PLANES == 3 ? 0 : 5; pr < 6; ++pr)
 #pragma unroll
-                            for (int k4 = 0; k4 < 4; ++k4) {
+                            for (int k4 = 0; k4 < BK / 16; ++k4) {
                                 const uint64_t ad = umma_desc_at(a_hi, a + PAIRS[pr][0] * a_plane + k4 * a_step);
                                 const uint64_t bd = umma_desc_at(b_hi, b + PAIRS[pr][1] * b_plane + k4 * b_step);
                                 const uint32_t acc = ((kb - k0) | (PLANES == 3 ? pr : 0) | k4) ? 1u : 0u;
