@@ -414,7 +414,6 @@ Shape choose(const Product &p, int sms)
     const int bk = p.f32 ? 32 : 64, kb = (int)((p.K + bk - 1) / bk);
     static const struct { int cg, width; } kinds[] = {{2, 256}, {2, 192}, {2, 128}, {2, 64}, {1, 128}, {1, 64}};
     for (const auto &k : kinds) {
-        if (p.f32 && k.width > 128) continue;
         const int64_t mt = (p.M + 128 * k.cg - 1) / (128 * k.cg), nt = (p.N + k.width - 1) / k.width, tiles = mt * nt;
         const int slots = sms / k.cg;
         const double mma = (p.f32 ? 6.0 : 2.0) * k.width, intake = (p.f32 ? 3.0 : 2.0) * (128 + k.width / k.cg);
@@ -485,6 +484,8 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
     g.whole = (int)s.whole; g.splits = s.splits; g.items = (int)(s.whole + s.tail * s.splits);
     g.kb_total = s.kb; g.kb_per = s.kb_per;
 
+    // A product with few rows fetches no more of A than exists (the MMAs then read what shared memory happens to hold: rows that nobody stores)
+    const int a_rows = s.cg == 1 && s.m_tiles == 1 ? (int)round_up(std::min<int64_t>(p.M, 128), 16) : 128;
     // operands
     const int planes = p.f32 ? 3 : 1, inner = p.f32 ? 64 : 128;
     const Operand *op[2] = {&p.A, &p.B};
@@ -506,15 +507,17 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
         }
         // an MN-major box: 64 entries side by side (128 bytes) x the K block; a K-major one: the K block x the rows of a CTA
         const bool ok = !run || (o.mn ? encode(i ? &g.tmB : &g.tmA, at, rows, cols, ld, false, inner / 2, 128, planes, o.plane)
-                                      : encode(i ? &g.tmB : &g.tmA, at, rows, cols, ld, false, i ? s.width / s.cg : 128, inner, planes, o.plane));
+                                      : encode(i ? &g.tmB : &g.tmA, at, rows, cols, ld, false, i ? s.width / s.cg : a_rows, inner, planes, o.plane));
         if (!ok) return TSR_ERR_CUDA;
         (i ? g.b_mn : g.a_mn) = o.mn;
     }
+    g.a_rows = a_rows;
+    g.a_boxes = (a_rows + 63) / 64;
     g.b_boxes = (s.width / s.cg + 63) / 64;
-    const int a_bytes = planes * 128 * inner, b_bytes = planes * (g.b_mn ? g.b_boxes * 64 * inner : s.width / s.cg * inner);
+    const int a_bytes = planes * 128 * inner, a_copied = planes * (g.a_mn ? g.a_boxes * 64 * inner : a_rows * inner), b_bytes = planes * (g.b_mn ? g.b_boxes * 64 * inner : s.width / s.cg * inner);
     g.b_offset = a_bytes;
     g.stage_bytes = a_bytes + b_bytes;
-    g.stage_tx = (uint32_t)(s.cg * g.stage_bytes);
+    g.stage_tx = (uint32_t)(s.cg * (a_copied + b_bytes));
     g.stages = linear_stages(g.stage_bytes, p.e.pre != nullptr);
 
     float *slabs = s.tail ? (float *)room.take((size_t)s.tail * s.splits * 128 * s.cg * s.width * 4) : nullptr;

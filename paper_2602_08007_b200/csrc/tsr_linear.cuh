@@ -27,7 +27,7 @@ struct alignas(64) LinearGemm : LinearTiles {
     // operands: K-major boxes of 64 entries x (128 or width / CG) rows, MN-major boxes of 64 x 64, 128-byte swizzle; of FP32 operands half as
     // much of K (K-major: 64-byte swizzle) of all three planes (third dimension); out, residual, pre and slabs: boxes of 128 bytes x 32 rows, 128-byte swizzle
     CUtensorMap tmA, tmB, tmOut, tmRes, tmPre, tmSlab;
-    int32_t a_mn, b_mn, b_boxes;         // operand forms; MN-major boxes of B per CTA
+    int32_t a_mn, b_mn, a_rows, a_boxes, b_boxes;   // operand forms; rows of a K-major box of A, MN-major boxes per CTA
     int32_t stages, stage_bytes, b_offset;   // the ring in shared memory
     uint32_t stage_tx;                   // bytes of a stage, of all CTAs of a tile
     int32_t whole_edge;                  // rows of out and pre may be written in whole 16-byte units

@@ -47,59 +47,12 @@ int linear_stages(int stage_bytes, bool pre)
     return n < LG_MAX_STAGES ? n : LG_MAX_STAGES;
 }
 
-// bias of 32 columns from col on, added to v (columns beyond N are left alone)
-__device__ __forceinline__ void add_bias(float (&v)[32], const LinearEpilogue &e, int col, int N)
+template <int ACT>
+__device__ __forceinline__ void activate(float (&v)[32])
 {
-    if (e.bias_bf16) {
-        const bf16 *b = (const bf16 *)e.bias + col;
-        if (col + 32 <= N && ((uintptr_t)b & 15) == 0) {
+    if (ACT == TSR_ACT_NONE) return;
 #pragma unroll
-            for (int j = 0; j < 32; j += 8) {
-                float x[8];
-                unpack8(__ldg((const uint4 *)(b + j)), x);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[j + i] += x[i];
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) if (col + j < N) v[j] += __bfloat162float(b[j]);
-        }
-    } else {
-        const float *b = (const float *)e.bias + col;
-        if (col + 32 <= N && ((uintptr_t)b & 15) == 0) {
-#pragma unroll
-            for (int j = 0; j < 32; j += 4) {
-                const float4 x = __ldg((const float4 *)(b + j));
-                v[j] += x.x; v[j + 1] += x.y; v[j + 2] += x.z; v[j + 3] += x.w;
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j) if (col + j < N) v[j] += b[j];
-        }
-    }
-}
-
-__device__ __forceinline__ void activate(float (&v)[32], int act)
-{
-    switch (act) {   // outside of the loop over the columns
-    case TSR_ACT_RELU:
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = act_value(TSR_ACT_RELU, v[j]);
-        break;
-    case TSR_ACT_GELU:
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = act_value(TSR_ACT_GELU, v[j]);
-        break;
-    case TSR_ACT_GELU_TANH:
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = act_value(TSR_ACT_GELU_TANH, v[j]);
-        break;
-    case TSR_ACT_SILU:
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = act_value(TSR_ACT_SILU, v[j]);
-        break;
-    default: break;
-    }
+    for (int j = 0; j < 32; ++j) v[j] = act_value(ACT, v[j]);
 }
 
 // A lane's row of a box: 16-byte unit u of row r lies at r * 128 + ((u ^ (r & 7)) << 4).
@@ -155,13 +108,16 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
                  ::"r"(dst), "l"((uint64_t)map), "r"(bar), "r"(x), "r"(y), "r"(0) : "memory");
 }
 
-// PLANES: 1, BF16 operands; 3, FP32 operands in three BF16 planes (width at most 128).  F32: type of out, residual and pre.
-template <int CG, int PLANES, bool F32>
+// PLANES: 1, BF16 operands; 3, FP32 operands in three BF16 planes.  F32: type of out, residual and pre.  EPI: the activation of a full epilogue, or
+// EPI_PLAIN: out = residual + D.  (One kernel for all of them spent a third of its time waiting for instructions.)
+constexpr int EPI_PLAIN = -1;
+template <int CG, int PLANES, bool F32, int EPI>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(LG_THREADS, 1)
 linear_gemm_kernel(const __grid_constant__ LinearGemm g)
 {
+    constexpr bool FULL = EPI != EPI_PLAIN;
     constexpr int TILE_M = CG * UM_BM, BK = PLANES == 3 ? 32 : 64;      // entries of a K block
-    constexpr uint32_t TMEM_COLS = CG == 2 && PLANES == 1 ? 512 : 256, ACC_COLS = TMEM_COLS / 2;
+    constexpr uint32_t TMEM_COLS = CG == 2 ? 512 : 256, ACC_COLS = TMEM_COLS / 2;
     constexpr int CW = F32 ? 32 : 64;                // columns of a box
     constexpr int PAIRS[6][2] = {{2, 0}, {0, 2}, {1, 1}, {1, 0}, {0, 1}, {0, 0}};   // planes of A and B, the small products first
     constexpr int CHUNK = PLANES == 3 ? 4 : 1 << 30; // K blocks per emptying of the accumulator
@@ -210,47 +166,42 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
     }
     pdl_wait();
 
+    // FP32: the sums of the epilogue warps (128 registers) come from the registers that loaders and MMA warp leave, 3 x 168 = 56 + 2 x 224.
+    if (warp < 4) {
+    if constexpr (PLANES == 3) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
     if (warp == 0 || warp == 2) {
         if (lane == 0) {
             int stage = 0;
             uint32_t phase = 0;
             bool ok = true;
-            const bool is_a = warp == 0;
-            const bool mn = is_a ? g.a_mn : g.b_mn;
-            const int boxes = is_a ? 2 : g.b_boxes;
-            const CUtensorMap *map = is_a ? &g.tmA : &g.tmB;
-            const uint32_t base = smem_u32(smem) + (is_a ? 0 : g.b_offset);
+            // one copy of an operand's K block: a K-major box, or an MN-major operand's groups of 64 columns one after the other
+            auto copy = [&](const CUtensorMap *map, bool mn, int boxes, uint32_t to, uint32_t full, int row, int kx) {
+                constexpr uint32_t GROUP = PLANES * 64 * BK * 2;
+                for (int j = 0; j < (mn ? boxes : 1); ++j) {
+                    const int x = mn ? row + 64 * j : kx, y = mn ? kx : row;
+                    if constexpr (PLANES == 1) {
+                        if constexpr (CG == 2) tma_load_2d_pair(to + j * GROUP, map, full, x, y);
+                        else tma_load_2d(to + j * GROUP, map, full, x, y);
+                    } else {      // the three planes at once
+                        if constexpr (CG == 2) tma_load_3d_pair(to + j * GROUP, map, full, x, y);
+                        else tma_load_3d(to + j * GROUP, map, full, x, y);
+                    }
+                }
+            };
+            const bool load_a = warp == 0, a_mn = g.a_mn, b_mn = g.b_mn;
+            const int a_boxes = g.a_boxes, b_boxes = g.b_boxes;
+            const uint32_t base = smem_u32(smem), b_offset = g.b_offset;
             for (int t = first; ok && t < g.items; t += stride) {
                 const LinearTile tile = linear_tile(g, t, TILE_M);
-                const int row = is_a ? tile.m0 + (int)rank * UM_BM : tile.n0 + (int)rank * (tile.n_eff / CG);
+                const int a_row = tile.m0 + (int)rank * UM_BM, b_row = tile.n0 + (int)rank * (tile.n_eff / CG);
                 for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
                     if (!mbar_wait(smem_u32(bar_empty + stage), phase ^ 1u, budget)) { s_timeout = 1; ok = false; break; }
                     // the copies of both CTAs of a pair report their bytes to the leader's barrier
                     const uint32_t full = CG == 2 ? leader_addr(smem_u32(bar_full + stage)) : smem_u32(bar_full + stage);
-                    if (is_a && rank == 0) mbar_expect_tx(smem_u32(bar_full + stage), g.stage_tx);
-                    const uint32_t st = base + stage * stage_bytes;
-                    const int kx = kb * BK;
-                    if constexpr (PLANES == 1) {
-                        if (mn) {
-                            for (int j = 0; j < boxes; ++j) {
-                                if constexpr (CG == 2) tma_load_2d_pair(st + j * 8192, map, full, row + 64 * j, kx);
-                                else tma_load_2d(st + j * 8192, map, full, row + 64 * j, kx);
-                            }
-                        } else {
-                            if constexpr (CG == 2) tma_load_2d_pair(st, map, full, kx, row);
-                            else tma_load_2d(st, map, full, kx, row);
-                        }
-                    } else {      // the three planes at once; an MN-major operand's groups of 64 columns one after the other
-                        if (mn) {
-                            for (int j = 0; j < boxes; ++j) {
-                                if constexpr (CG == 2) tma_load_3d_pair(st + j * 3 * 4096, map, full, row + 64 * j, kx);
-                                else tma_load_3d(st + j * 3 * 4096, map, full, row + 64 * j, kx);
-                            }
-                        } else {
-                            if constexpr (CG == 2) tma_load_3d_pair(st, map, full, kx, row);
-                            else tma_load_3d(st, map, full, kx, row);
-                        }
-                    }
+                    if (load_a && rank == 0) mbar_expect_tx(smem_u32(bar_full + stage), g.stage_tx);
+                    const uint32_t to = base + stage * stage_bytes;
+                    if (load_a) copy(&g.tmA, a_mn, a_boxes, to, full, a_row, kb * BK);
+                    else copy(&g.tmB, b_mn, b_boxes, to + b_offset, full, b_row, kb * BK);
                     if (++stage == stages) { stage = 0; phase ^= 1u; }
                 }
             }
@@ -267,7 +218,7 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
             const uint64_t mn_hi = PLANES == 3 ? MN3 : UMMA_DESC_HI_MN, k_hi = PLANES == 3 ? K3 : UMMA_DESC_HI_K;
             const uint64_t a_hi = g.a_mn ? mn_hi : k_hi, b_hi = g.b_mn ? mn_hi : k_hi;
             const uint32_t a_step = g.a_mn ? 2048u : 32u, b_step = g.b_mn ? 2048u : 32u;
-            const uint32_t a_plane = g.a_mn ? 4096u : UM_BM * 64u, b_plane = g.b_mn ? 4096u : (uint32_t)(g.width / CG) * 64u;
+            const uint32_t a_plane = g.a_mn ? 4096u : (uint32_t)g.a_rows * 64u, b_plane = g.b_mn ? 4096u : (uint32_t)(g.width / CG) * 64u;
             // (M = 256 for a pair, 128 for one CTA; FP32 accumulator; BF16 operands)
             const uint32_t form = (g.a_mn ? UMMA_IDESC_A_MN_MAJOR : 0u) | (g.b_mn ? UMMA_IDESC_B_MN_MAJOR : 0u) | (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE_M >> 4) << 24);
             for (int t = first; ok && t < g.items; t += stride) {
@@ -304,13 +255,16 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
                 }
             }
         }
-    } else if (warp >= 4) {
+    }
+    } else {
+        if constexpr (PLANES == 3) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         // warp e reads tensor-memory lanes 32 (e % 4) .. and the boxes of even or odd position in the tile's columns
         const LinearEpilogue &e = g.e;
         const int ew = warp - 4, q = warp & 3, half = ew >> 2;
-        uint8_t *boxes = box_area + ew * (e.pre ? 3 : 2) * LG_BOX_BYTES, *pre_box = boxes + 2 * LG_BOX_BYTES;
+        uint8_t *boxes = box_area + ew * (FULL && e.pre ? 3 : 2) * LG_BOX_BYTES, *pre_box = boxes + 2 * LG_BOX_BYTES;
         const uint32_t res_bar = smem_u32(bar_res + 2 * ew), lanes = tmem_base + ((uint32_t)(q * 32) << 16);
-        const uint32_t call_key = e.drop.threshold ? drop_call_key(e.drop) : 0u;
+        const bool drops = FULL && e.drop.threshold;
+        const uint32_t call_key = drops ? drop_call_key(e.drop) : 0u;
         uint32_t nb = 0, res_phase = 0;     // boxes taken so far (the next is nb & 1); phases of the two boxes' barriers
         uint32_t tc = 0;
         bool ok = true;
@@ -345,18 +299,27 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
                 __syncwarp();
                 for (int k = 0; k < min(2, cnt); ++k) fetch((nb + k) & 1u, k);
             }
-            const DropRow drop_row = e.drop.threshold && !slab ? drop_row_key(call_key, row0 + lane) : DropRow{0, 0};
+            const DropRow drop_row = drops && !slab ? drop_row_key(call_key, row0 + lane) : DropRow{0, 0};
+            // bias of the warp's groups of 32 columns, a column per lane
+            float bias[4] = {0.f, 0.f, 0.f, 0.f};
+            if (FULL && e.bias && !slab) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int c = F32 ? first_col + 64 * i + lane : first_col + 128 * (i >> 1) + 32 * (i & 1) + lane;
+                    if (c < n_end) bias[i] = load_as(e.bias, c, e.bias_bf16);
+                }
+            }
 
-            float sum[PLANES == 3 ? 2 : 1][32];
+            float sum[PLANES == 3 ? 4 : 1][32];
             if constexpr (PLANES == 3) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
                     for (int j = 0; j < 32; ++j) sum[k][j] = 0.f;
                 for (int k0 = tile.kb0; k0 < tile.kb1; k0 += CHUNK, ++tc) {
                     if (!acc_full(tc)) { ok = false; break; }
 #pragma unroll
-                    for (int k = 0; k < 2; ++k) {
+                    for (int k = 0; k < 4; ++k) {
                         if (k >= cnt) continue;
                         uint32_t r[32];
                         tc_ld_32x32(lanes + (tc & 1u) * ACC_COLS + (uint32_t)(first_col + 64 * k - tile.n0), r);
@@ -374,7 +337,7 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
             auto one_box = [&](int k, const float (&src)[32]) -> bool {
                 const int col0 = first_col + 2 * cw * k, ncols = min(cw, n_end - col0);
                 uint8_t *box = boxes + (nb & 1u) * LG_BOX_BYTES;
-                if (lane == 0) bulk_wait_read(e.pre ? 0 : 1);      // the box, and the pre box, have been read by the stores that used them last
+                if (lane == 0) bulk_wait_read(FULL && e.pre ? 0 : 1);      // the box, and the pre box, have been read by the stores that used them last
                 __syncwarp();
                 if (res) {
                     if (e.res_tma) {
@@ -405,8 +368,13 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
                         for (int u = 0; u < 8; ++u) *(float4 *)box_unit(box, lane, u) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
                         continue;
                     }
-                    if (e.bias) add_bias(v, e, col, g.N);
-                    if (e.pre) {
+                    if (FULL && e.bias) {
+                        const int i = F32 ? k : 2 * k + h;
+                        const float mine = i == 0 ? bias[0] : i == 1 ? bias[1] : i == 2 ? bias[2] : bias[3];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] += __shfl_sync(0xffffffffu, mine, j);
+                    }
+                    if (FULL && e.pre) {
 #pragma unroll
                         for (int u = 0; u < (F32 ? 8 : 4); ++u) {
                             if (F32) *(float4 *)box_unit(pre_box, lane, u) = make_float4(v[4 * u], v[4 * u + 1], v[4 * u + 2], v[4 * u + 3]);
@@ -414,8 +382,8 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
                                                                                  pack_bf16(v[8 * u + 4], v[8 * u + 5]), pack_bf16(v[8 * u + 6], v[8 * u + 7]));
                         }
                     }
-                    if (e.act) activate(v, e.act);
-                    if (e.drop.threshold) {
+                    if constexpr (FULL) activate<EPI>(v);
+                    if (drops) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
                             const uint32_t w = drop_word(drop_row, (uint32_t)(col + j) >> 1);
@@ -447,16 +415,16 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
                 __syncwarp();
                 // A TMA store is clipped at the matrix edge in units of 16 bytes: where the last one is not whole, the last box goes by rows.
                 const bool whole = g.whole_edge || col0 + cw <= g.N;
-                const bool out_tma = e.out_tma && whole, pre_tma = e.pre_tma && whole;
+                const bool out_tma = e.out_tma && whole, pre_tma = FULL && e.pre_tma && whole;
                 if (lane == 0) {
                     if (slab) tma_store_2d(&g.tmSlab, smem_u32(box), col0 - tile.n0, tile.part * TILE_M + (int)rank * UM_BM + q * 32);
                     else if (out_tma) tma_store_2d(&g.tmOut, smem_u32(box), col0, row0);
-                    if (e.pre && pre_tma && !slab) tma_store_2d(&g.tmPre, smem_u32(pre_box), col0, row0);
+                    if (FULL && e.pre && pre_tma && !slab) tma_store_2d(&g.tmPre, smem_u32(pre_box), col0, row0);
                     asm volatile("cp.async.bulk.commit_group;" ::: "memory");
                 }
                 if (!slab) {
                     if (!out_tma) box_to_rows<F32>(box, (uint8_t *)e.out + ((int64_t)row0 * e.ldo + col0) * (F32 ? 4 : 2), e.ldo, nrows, ncols, lane);
-                    if (e.pre && !pre_tma) box_to_rows<F32>(pre_box, (uint8_t *)e.pre + ((int64_t)row0 * e.ldp + col0) * (F32 ? 4 : 2), e.ldp, nrows, ncols, lane);
+                    if (FULL && e.pre && !pre_tma) box_to_rows<F32>(pre_box, (uint8_t *)e.pre + ((int64_t)row0 * e.ldp + col0) * (F32 ? 4 : 2), e.ldp, nrows, ncols, lane);
                 }
                 __syncwarp();
                 if (res && e.res_tma && k + 2 < cnt) {       // (FP32 out: four boxes of a 256-wide tile)
@@ -468,8 +436,14 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
                 return true;
             };
             if constexpr (PLANES == 3) {
+#pragma unroll 1
+                for (int k = 0; ok && k < cnt; ++k) {      // (one copy of the epilogue's code: the sums move up to the first place)
+                    ok = one_box(k, sum[0]);
 #pragma unroll
-                for (int k = 0; k < 2; ++k) if (ok && k < cnt) ok = one_box(k, sum[k]);
+                    for (int i = 0; i < 3; ++i)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[i][j] = sum[i + 1][j];
+                }
             } else {
 #pragma unroll 1
                 for (int k = 0; ok && k < cnt; ++k) ok = one_box(k, sum[0]);
@@ -492,7 +466,7 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
     if (threadIdx.x == 0 && s_timeout) atomicMax(&g_linear_status, (int)TSR_ERR_TIMEOUT);
 }
 
-template <int CG, int PLANES, bool F32>
+template <int CG, int PLANES, bool F32, int EPI>
 static cudaError_t gemm_launch_as(const LinearGemm &g, int sms, cudaStream_t stream)
 {
     static bool configured[64] = {};      // per device; setting it twice is harmless
@@ -500,19 +474,39 @@ static cudaError_t gemm_launch_as(const LinearGemm &g, int sms, cudaStream_t str
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
     if (dev >= 64 || !configured[dev]) {
-        e = cudaFuncSetAttribute(linear_gemm_kernel<CG, PLANES, F32>, cudaFuncAttributeMaxDynamicSharedMemorySize, LG_SMEM);
+        e = cudaFuncSetAttribute(linear_gemm_kernel<CG, PLANES, F32, EPI>, cudaFuncAttributeMaxDynamicSharedMemorySize, LG_SMEM);
         if (e != cudaSuccess) return e;
         if (dev < 64) configured[dev] = true;
     }
     const int slots = sms / CG, n = g.items < slots ? g.items : slots;
-    return launch_dependent(linear_gemm_kernel<CG, PLANES, F32>, dim3(CG * n), dim3(LG_THREADS), (size_t)LG_SMEM, stream, 1, g);
+    return launch_dependent(linear_gemm_kernel<CG, PLANES, F32, EPI>, dim3(CG * n), dim3(LG_THREADS), (size_t)LG_SMEM, stream, 1, g);
+}
+
+template <int PLANES, bool F32, int EPI>
+static cudaError_t gemm_launch_cg(const LinearGemm &g, int cg, int sms, cudaStream_t stream)
+{
+    return cg == 2 ? gemm_launch_as<2, PLANES, F32, EPI>(g, sms, stream) : gemm_launch_as<1, PLANES, F32, EPI>(g, sms, stream);
+}
+
+template <int PLANES, bool F32>
+static cudaError_t gemm_launch_epi(const LinearGemm &g, int cg, int sms, cudaStream_t stream)
+{
+    const LinearEpilogue &e = g.e;
+    if (!e.bias && !e.pre && !e.act && !e.drop.threshold) return gemm_launch_cg<PLANES, F32, EPI_PLAIN>(g, cg, sms, stream);
+    switch (e.act) {
+    case TSR_ACT_RELU: return gemm_launch_cg<PLANES, F32, TSR_ACT_RELU>(g, cg, sms, stream);
+    case TSR_ACT_GELU: return gemm_launch_cg<PLANES, F32, TSR_ACT_GELU>(g, cg, sms, stream);
+    case TSR_ACT_GELU_TANH: return gemm_launch_cg<PLANES, F32, TSR_ACT_GELU_TANH>(g, cg, sms, stream);
+    case TSR_ACT_SILU: return gemm_launch_cg<PLANES, F32, TSR_ACT_SILU>(g, cg, sms, stream);
+    default: return gemm_launch_cg<PLANES, F32, TSR_ACT_NONE>(g, cg, sms, stream);
+    }
 }
 
 cudaError_t linear_gemm_launch(const LinearGemm &g, int cg, bool f32_operands, bool f32_out, int sms, cudaStream_t stream)
 {
-    if (f32_operands) return cg == 2 ? gemm_launch_as<2, 3, true>(g, sms, stream) : gemm_launch_as<1, 3, true>(g, sms, stream);
-    if (f32_out) return cg == 2 ? gemm_launch_as<2, 1, true>(g, sms, stream) : gemm_launch_as<1, 1, true>(g, sms, stream);
-    return cg == 2 ? gemm_launch_as<2, 1, false>(g, sms, stream) : gemm_launch_as<1, 1, false>(g, sms, stream);
+    if (f32_operands) return gemm_launch_epi<3, true>(g, cg, sms, stream);
+    if (f32_out) return gemm_launch_cg<1, true, EPI_PLAIN>(g, cg, sms, stream);      // (a weight's gradient)
+    return gemm_launch_epi<1, false>(g, cg, sms, stream);
 }
 
 cudaError_t linear_status_read(int32_t *status, cudaStream_t stream)
