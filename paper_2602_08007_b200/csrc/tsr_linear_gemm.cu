@@ -92,6 +92,27 @@ __device__ __forceinline__ void box_to_rows(uint8_t *box, void *dst, int64_t ld,
     }
 }
 
+// One MMA, issued by the lane for which `leader` is set; the whole warp runs through here, so that the descriptors stay in uniform registers.  They are
+// given as halves: the lower one moves with the address (bits 0 .. 13 = address >> 4), the upper one is the operand's form.
+template <int CG>
+__device__ __forceinline__ void mma_bf16(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, uint32_t accumulate, uint32_t leader)
+{
+    if constexpr (CG == 2)
+        asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+                     "@q tcgen05.mma.cta_group::2.kind::f16 [%0], a, b, %5, p;\n\t}"
+                     ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\tmov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+                     "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n\t}"
+                     ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "r"(leader) : "memory");
+}
+__device__ __forceinline__ uint32_t elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r;
+}
+
 __device__ __forceinline__ void bulk_wait_read(int pending)
 {
     if (pending) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");
@@ -207,50 +228,59 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
             }
         }
     } else if (warp == 1) {
-        if (lane == 0 && rank == 0) {
+        if (rank == 0) {      // the whole warp; one lane issues
             uint32_t tc = 0, phase = 0;      // tc: accumulators filled so far
             int stage = 0;
             bool ok = true;
-            // Three planes: K-major rows of 64 bytes (64-byte swizzle, layout type 4; eight rows 512 bytes apart), MN-major groups of 64 columns x
-            // 32 rows, the three planes of a group one behind the other.
+            const uint32_t leader = elect_one();
+            // Operand forms.  K-major: rows of 128 bytes, eight of them 1024 apart; MN-major: groups of 64 columns 8 KB apart.  Three planes: K-major rows
+            // of 64 bytes (64-byte swizzle, layout type 4; eight rows 512 bytes apart), MN-major groups of 64 columns x 32 rows, the three
+            // planes of a group one behind the other.
             constexpr uint64_t K3 = ((uint64_t)1 << 16) | ((uint64_t)(512 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)4 << 61);
             constexpr uint64_t MN3 = ((uint64_t)(3 * 4096 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-            const uint64_t mn_hi = PLANES == 3 ? MN3 : UMMA_DESC_HI_MN, k_hi = PLANES == 3 ? K3 : UMMA_DESC_HI_K;
-            const uint64_t a_hi = g.a_mn ? mn_hi : k_hi, b_hi = g.b_mn ? mn_hi : k_hi;
-            const uint32_t a_step = g.a_mn ? 2048u : 32u, b_step = g.b_mn ? 2048u : 32u;
-            const uint32_t a_plane = g.a_mn ? 4096u : (uint32_t)g.a_rows * 64u, b_plane = g.b_mn ? 4096u : (uint32_t)(g.width / CG) * 64u;
+            const uint64_t mn_form = PLANES == 3 ? MN3 : UMMA_DESC_HI_MN, k_form = PLANES == 3 ? K3 : UMMA_DESC_HI_K;
+            const uint64_t a_form = g.a_mn ? mn_form : k_form, b_form = g.b_mn ? mn_form : k_form;
+            const uint32_t a_hi = (uint32_t)(a_form >> 32), b_hi = (uint32_t)(b_form >> 32);
+            // in units of 16 bytes: from one MMA's 16 entries of K to the next, from plane to plane
+            const uint32_t a_step = (g.a_mn ? 2048u : 32u) >> 4, b_step = (g.b_mn ? 2048u : 32u) >> 4;
+            const uint32_t a_plane = (g.a_mn ? 4096u : (uint32_t)g.a_rows * 64u) >> 4, b_plane = (g.b_mn ? 4096u : (uint32_t)(g.width / CG) * 64u) >> 4;
+            const uint32_t a_first = (uint32_t)a_form + (smem_u32(smem) >> 4), b_first = (uint32_t)b_form + ((smem_u32(smem) + g.b_offset) >> 4);
+            const uint32_t stage_step = (uint32_t)stage_bytes >> 4;
             // (M = 256 for a pair, 128 for one CTA; FP32 accumulator; BF16 operands)
             const uint32_t form = (g.a_mn ? UMMA_IDESC_A_MN_MAJOR : 0u) | (g.b_mn ? UMMA_IDESC_B_MN_MAJOR : 0u) | (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE_M >> 4) << 24);
+            uint32_t a = a_first, b = b_first;
             for (int t = first; ok && t < g.items; t += stride) {
                 const LinearTile tile = linear_tile(g, t, TILE_M);
                 const uint32_t idesc = form | ((uint32_t)(tile.n_eff >> 3) << 17);
                 for (int k0 = tile.kb0; ok && k0 < tile.kb1; ++tc) {
                     const int k1 = tile.kb1 - k0 > CHUNK ? k0 + CHUNK : tile.kb1;
                     const uint32_t buf = tc & 1u;
-                    if (!mbar_wait(smem_u32(bar_acc_empty + buf), ((tc >> 1) & 1u) ^ 1u, budget)) { s_timeout = 1; ok = false; break; }
+                    if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(bar_acc_empty + buf), ((tc >> 1) & 1u) ^ 1u, budget))) { s_timeout = 1; ok = false; break; }
                     tc_fence_after();
                     const uint32_t d = tmem_base + buf * ACC_COLS;
+                    uint32_t acc = 0;      // the first MMA overwrites
                     for (int kb = k0; kb < k1; ++kb) {
-                        const int s = stage;
-                        if (!mbar_wait(smem_u32(bar_full + s), phase, budget)) { s_timeout = 1; ok = false; break; }
-                        if (++stage == stages) { stage = 0; phase ^= 1u; }
+                        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(bar_full + stage), phase, budget))) { s_timeout = 1; ok = false; break; }
                         tc_fence_after();
-                        const uint32_t a = smem_u32(smem) + s * stage_bytes, b = a + g.b_offset;
 #pragma unroll
                         for (int pr = PLANES == 3 ? 0 : 5; pr < 6; ++pr)
 #pragma unroll
                             for (int k4 = 0; k4 < BK / 16; ++k4) {
-                                const uint64_t ad = umma_desc_at(a_hi, a + PAIRS[pr][0] * a_plane + k4 * a_step);
-                                const uint64_t bd = umma_desc_at(b_hi, b + PAIRS[pr][1] * b_plane + k4 * b_step);
-                                const uint32_t acc = ((kb - k0) | (PLANES == 3 ? pr : 0) | k4) ? 1u : 0u;
-                                if constexpr (CG == 2) tc_mma_bf16_pair(d, ad, bd, idesc, acc);
-                                else tc_mma_bf16(d, ad, bd, idesc, acc);
+                                mma_bf16<CG>(d, a + PAIRS[pr][0] * a_plane + k4 * a_step, a_hi, b + PAIRS[pr][1] * b_plane + k4 * b_step, b_hi, idesc, acc, leader);
+                                acc = 1;
                             }
-                        if constexpr (CG == 2) tc_commit_pair(smem_u32(bar_empty + s));
-                        else tc_commit(smem_u32(bar_empty + s));
+                        if (leader) {
+                            if constexpr (CG == 2) tc_commit_pair(smem_u32(bar_empty + stage));
+                            else tc_commit(smem_u32(bar_empty + stage));
+                        }
+                        a += stage_step;
+                        b += stage_step;
+                        if (++stage == stages) { stage = 0; phase ^= 1u; a = a_first; b = b_first; }
                     }
-                    if constexpr (CG == 2) tc_commit_pair(smem_u32(bar_acc_full + buf));
-                    else tc_commit(smem_u32(bar_acc_full + buf));
+                    if (leader) {
+                        if constexpr (CG == 2) tc_commit_pair(smem_u32(bar_acc_full + buf));
+                        else tc_commit(smem_u32(bar_acc_full + buf));
+                    }
                     k0 = k1;
                 }
             }
