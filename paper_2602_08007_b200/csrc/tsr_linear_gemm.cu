@@ -190,41 +190,39 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
     // FP32: the sums of the epilogue warps (128 registers) come from the registers that loaders and MMA warp leave, 3 x 168 = 56 + 2 x 224.
     if (warp < 4) {
     if constexpr (PLANES == 3) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 0 || warp == 2) {
-        if (lane == 0) {
-            int stage = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            // one copy of an operand's K block: a K-major box, or an MN-major operand's groups of 64 columns one after the other
-            auto copy = [&](const CUtensorMap *map, bool mn, int boxes, uint32_t to, uint32_t full, int row, int kx) {
-                constexpr uint32_t GROUP = PLANES * 64 * BK * 2;
-                for (int j = 0; j < (mn ? boxes : 1); ++j) {
-                    const int x = mn ? row + 64 * j : kx, y = mn ? kx : row;
-                    if constexpr (PLANES == 1) {
-                        if constexpr (CG == 2) tma_load_2d_pair(to + j * GROUP, map, full, x, y);
-                        else tma_load_2d(to + j * GROUP, map, full, x, y);
-                    } else {      // the three planes at once
-                        if constexpr (CG == 2) tma_load_3d_pair(to + j * GROUP, map, full, x, y);
-                        else tma_load_3d(to + j * GROUP, map, full, x, y);
+    if (warp == 0 || warp == 2) {      // the whole warp; one lane asks
+        const uint32_t leader = elect_one();
+        int stage = 0;
+        uint32_t phase = 0;
+        bool ok = true;
+        const bool is_a = warp == 0, mn = is_a ? g.a_mn : g.b_mn;
+        const int boxes = mn ? is_a ? g.a_boxes : g.b_boxes : 1;
+        const CUtensorMap *map = is_a ? &g.tmA : &g.tmB;
+        const uint32_t base = smem_u32(smem) + (is_a ? 0u : (uint32_t)g.b_offset);
+        constexpr uint32_t GROUP = PLANES * 64 * BK * 2;      // an MN-major operand's groups of 64 columns follow one another
+        for (int t = first; ok && t < g.items; t += stride) {
+            const LinearTile tile = linear_tile(g, t, TILE_M);
+            const int row = is_a ? tile.m0 + (int)rank * UM_BM : tile.n0 + (int)rank * (tile.n_eff / CG);
+            for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
+                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(bar_empty + stage), phase ^ 1u, budget))) { s_timeout = 1; ok = false; break; }
+                if (leader) {
+                    // the copies of both CTAs of a pair report their bytes to the leader CTA's barrier
+                    const uint32_t full = CG == 2 ? leader_addr(smem_u32(bar_full + stage)) : smem_u32(bar_full + stage);
+                    if (is_a && rank == 0) mbar_expect_tx(smem_u32(bar_full + stage), g.stage_tx);
+                    uint32_t to = base + stage * stage_bytes;
+                    int x = mn ? row : kb * BK;
+                    const int y = mn ? kb * BK : row;
+                    for (int j = 0; j < boxes; ++j, to += GROUP, x += 64) {
+                        if constexpr (PLANES == 1) {
+                            if constexpr (CG == 2) tma_load_2d_pair(to, map, full, x, y);
+                            else tma_load_2d(to, map, full, x, y);
+                        } else {      // the three planes at once
+                            if constexpr (CG == 2) tma_load_3d_pair(to, map, full, x, y);
+                            else tma_load_3d(to, map, full, x, y);
+                        }
                     }
                 }
-            };
-            const bool load_a = warp == 0, a_mn = g.a_mn, b_mn = g.b_mn;
-            const int a_boxes = g.a_boxes, b_boxes = g.b_boxes;
-            const uint32_t base = smem_u32(smem), b_offset = g.b_offset;
-            for (int t = first; ok && t < g.items; t += stride) {
-                const LinearTile tile = linear_tile(g, t, TILE_M);
-                const int a_row = tile.m0 + (int)rank * UM_BM, b_row = tile.n0 + (int)rank * (tile.n_eff / CG);
-                for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
-                    if (!mbar_wait(smem_u32(bar_empty + stage), phase ^ 1u, budget)) { s_timeout = 1; ok = false; break; }
-                    // the copies of both CTAs of a pair report their bytes to the leader's barrier
-                    const uint32_t full = CG == 2 ? leader_addr(smem_u32(bar_full + stage)) : smem_u32(bar_full + stage);
-                    if (load_a && rank == 0) mbar_expect_tx(smem_u32(bar_full + stage), g.stage_tx);
-                    const uint32_t to = base + stage * stage_bytes;
-                    if (load_a) copy(&g.tmA, a_mn, a_boxes, to, full, a_row, kb * BK);
-                    else copy(&g.tmB, b_mn, b_boxes, to + b_offset, full, b_row, kb * BK);
-                    if (++stage == stages) { stage = 0; phase ^= 1u; }
-                }
+                if (++stage == stages) { stage = 0; phase ^= 1u; }
             }
         }
     } else if (warp == 1) {
