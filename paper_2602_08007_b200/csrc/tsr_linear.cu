@@ -3,6 +3,7 @@
 //
 //   linear_pack_kernel     BF16 operand whose pitch or address TMA does not take -> workspace with a 128-byte pitch (one pass over it)
 //   linear_split_kernel    FP32 operand -> three BF16 planes whose sum it is
+//   linear_few_kernel      the whole layer for at most eight rows
 //   linear_dz_kernel       dz = dropout(dy) o act'(pre) and the column sums of dz (the bias's gradient), one pass over dy and pre
 //   linear_finish_kernel   split K: slabs added in order, then the epilogue
 //   column_finish_kernel   partial column sums added in order (bias, and the norm's weight and bias)
@@ -88,6 +89,20 @@ __device__ __forceinline__ void split3(float x, bf16 (&p)[3])
     p[1] = __float2bfloat16_rn(r1);
     p[2] = __float2bfloat16_rn(r1 - __bfloat162float(p[1]));
 }
+__device__ __forceinline__ void store_planes(bf16 *dst, int64_t plane, const float (&v)[8])
+{
+    uint32_t w[3][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        bf16 a[3], b[3];
+        split3(v[2 * i], a);
+        split3(v[2 * i + 1], b);
+#pragma unroll
+        for (int k = 0; k < 3; ++k) w[k][i] = (uint32_t)__bfloat16_as_ushort(a[k]) | ((uint32_t)__bfloat16_as_ushort(b[k]) << 16);
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *(uint4 *)(dst + k * plane) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+}
 // dst: three planes of rows x ldd, `plane` entries apart.  A thread takes eight neighbours of a row.
 __global__ void __launch_bounds__(256)
 linear_split_kernel(const float *__restrict__ src, int64_t lds, bf16 *__restrict__ dst, int64_t ldd, int64_t plane, int64_t rows, int cols, int units)
@@ -103,18 +118,7 @@ linear_split_kernel(const float *__restrict__ src, int64_t lds, bf16 *__restrict
         float v[8];
         if (c + 8 <= cols) load8_any(s, v);
         else load8_part(s, cols - c, v);
-        uint32_t w[3][4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bf16 a[3], b[3];
-            split3(v[2 * i], a);
-            split3(v[2 * i + 1], b);
-#pragma unroll
-            for (int k = 0; k < 3; ++k) w[k][i] = (uint32_t)__bfloat16_as_ushort(a[k]) | ((uint32_t)__bfloat16_as_ushort(b[k]) << 16);
-        }
-        // (the pitch is whole units: what is written past the last column is zero and lies in the padding)
-#pragma unroll
-        for (int k = 0; k < 3; ++k) *(uint4 *)(dst + k * plane + r * ldd + c) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
+        store_planes(dst + r * ldd + c, plane, v);      // (the pitch is whole units: what is written past the last column is zero)
     }
 }
 
@@ -205,6 +209,75 @@ linear_finish_kernel(const __grid_constant__ FinishArgs a)
     }
 }
 
+// Few rows (at most eight): the layer is bound by reading the weight once.  A warp per output column: lanes take eight entries of K each, at any
+// alignment, against the rows of x in shared memory (FP32, a chunk of K at a time), and join their sums; then a lane per row runs the epilogue.
+// FP32 stays in FP32 here.  One launch, nothing in the workspace.
+struct FewArgs {
+    const void *x, *w;
+    int64_t ldx, ldw;
+    int32_t M, N, K;
+    LinearEpilogue e;
+};
+constexpr int FEW_ROWS = 8, FEW_SHARED = 8192;      // entries of x in shared memory
+template <typename T, int ROWS>
+__global__ void __launch_bounds__(256)
+linear_few_kernel(const __grid_constant__ FewArgs a)
+{
+    constexpr int CHUNK = FEW_SHARED / ROWS;
+    __shared__ __align__(16) float xs[ROWS][CHUNK];
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, col = blockIdx.x * 8 + (threadIdx.x >> 5);
+    const T *w = (const T *)a.w + (int64_t)min(col, a.N - 1) * a.ldw;
+    float acc[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) acc[r] = 0.f;
+    for (int k0 = 0; k0 < a.K; k0 += CHUNK) {
+        const int len = min(CHUNK, a.K - k0), padded = (len + 7) & ~7;
+        if (k0) __syncthreads();
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+            for (int i = threadIdx.x; i < padded; i += 256) xs[r][i] = r < a.M && i < len ? load_f((const T *)a.x + r * a.ldx + k0 + i) : 0.f;
+        __syncthreads();
+#pragma unroll 4
+        for (int i = lane * 8; i < len; i += 256) {
+            float v[8];
+            if (i + 8 <= len) load8_any(w + k0 + i, v);
+            else load8_part(w + k0 + i, len - i, v);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const float4 p = *(const float4 *)&xs[r][i], q = *(const float4 *)&xs[r][i + 4];
+                acc[r] = fmaf(v[0], p.x, fmaf(v[1], p.y, fmaf(v[2], p.z, fmaf(v[3], p.w, acc[r]))));
+                acc[r] = fmaf(v[4], q.x, fmaf(v[5], q.y, fmaf(v[6], q.z, fmaf(v[7], q.w, acc[r]))));
+            }
+        }
+    }
+    float z = 0.f;      // of the lane's row
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+        for (int o = 16; o; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
+        if (lane == r) z = acc[r];
+    }
+    if (lane >= a.M || col >= a.N) return;
+    const LinearEpilogue &e = a.e;
+    if (e.bias) z += load_as(e.bias, col, e.bias_bf16);
+    if (e.pre) store_f((T *)e.pre + lane * e.ldp + col, z);
+    z = act_value(e.act, z);
+    if (e.drop.threshold) z = drop_entry(drop_row_key(drop_call_key(e.drop), lane), (uint32_t)col, z, e.drop);
+    if (e.res) z += load_f((const T *)e.res + lane * e.ldr + col);
+    store_f((T *)e.out + lane * e.ldo + col, z);
+}
+template <typename T>
+static cudaError_t few_launch(const FewArgs &a, cudaStream_t s)
+{
+    const dim3 grid((unsigned)((a.N + 7) / 8));
+    if (a.M <= 1) return launch_dependent(linear_few_kernel<T, 1>, grid, dim3(256), 0, s, 1, a);
+    if (a.M <= 2) return launch_dependent(linear_few_kernel<T, 2>, grid, dim3(256), 0, s, 1, a);
+    if (a.M <= 4) return launch_dependent(linear_few_kernel<T, 4>, grid, dim3(256), 0, s, 1, a);
+    return launch_dependent(linear_few_kernel<T, FEW_ROWS>, grid, dim3(256), 0, s, 1, a);
+}
+
 // dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row.  dy and pre
 // may lie at any alignment, dz has a pitch of whole 16-byte units.  dz NULL: the sums alone.
 // The grid is what is resident at once (a third more left SMs idle for 40 % of the time), and what hides the loads is the number of warps: unrolled
@@ -212,9 +285,9 @@ linear_finish_kernel(const __grid_constant__ FinishArgs a)
 constexpr int DZ_CTAS = 4;     // on an SM
 struct DzArgs {
     const void *dy, *pre;
-    void *dz;
+    void *dz;                  // BF16, or (FP32) three BF16 planes `plane` entries apart
     float *partial;            // [gridDim.y][cols], NULL: no sums
-    int64_t lddy, ldpre, lddz, rows;
+    int64_t lddy, ldpre, lddz, plane, rows;
     int32_t cols, rows_per;
     DropArgs drop;
 };
@@ -234,7 +307,7 @@ linear_dz_kernel(const DzArgs a)
     for (int j = 0; j < 8; ++j) acc[j] = 0.f;
     if (n > 0) {
         const T *dy = (const T *)a.dy + r0 * a.lddy + c0, *pre = ACT ? (const T *)a.pre + r0 * a.ldpre + c0 : nullptr;
-        T *dz = a.dz ? (T *)a.dz + r0 * a.lddz + c0 : nullptr;
+        bf16 *dz = a.dz ? (bf16 *)a.dz + r0 * a.lddz + c0 : nullptr;
 #pragma unroll 1
         for (int64_t r = r0; r < r1; r += 8) {
             float g[8], z[8];
@@ -262,7 +335,9 @@ linear_dz_kernel(const DzArgs a)
 #pragma unroll
             for (int j = 0; j < 8; ++j) acc[j] += g[j];
             if (dz) {
-                store8(dz, g);     // (past the last column: zeros, into the padding)
+                // (past the last column: zeros, into the padding)
+                if constexpr (sizeof(T) == 2) store8(dz, g);
+                else store_planes(dz, a.plane, g);
                 dz += 8 * a.lddz;
             }
             dy += 8 * a.lddy;
@@ -419,7 +494,7 @@ Shape choose(const Product &p, int sms)
         const double mma = (p.f32 ? 6.0 : 2.0) * k.width, intake = (p.f32 ? 3.0 : 2.0) * (128 + k.width / k.cg);
         const int stage = (p.f32 ? 3 * 64 : 128) * (128 + k.width / k.cg), stages = linear_stages(stage, p.e.pre != nullptr);
         // (with a single stage loads and MMAs take turns)
-        const double per_kb = stages > 1 ? std::max(mma, intake) : mma + intake + 1000.0, tile = kb * per_kb + 300.0, last = 3000.0 + 12.0 * k.width;
+        const double per_kb = stages > 1 ? std::max(mma, intake) : mma + intake + 1000.0, tile = kb * per_kb + 300.0, last = 3000.0 + 800.0 * (k.cg - 1) + 12.0 * k.width;
         const int64_t full = tiles / slots, rem = tiles % slots;
         auto offer = [&](double cost, int64_t tail, int s, int per) {
             if (cost < best_cost) { best_cost = cost; best = {k.cg, k.width, s, kb, per, mt, nt, tiles - tail, tail}; }
@@ -495,7 +570,10 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
         const int64_t rows = o.mn ? p.K : extent[i], cols = o.mn ? extent[i] : p.K;    // as stored
         const void *at = o.p;
         int64_t ld = o.ld;
-        if (!p.f32 && !tma_takes(o.p, rows, o.ld, 2)) {
+        // A K-major operand whose rows do not start on 128 bytes costs two lines per row and K block, a fifth of the product's time; copying
+        // it first pays where the other extent is long enough (8192 x 5464 -> 2048: weight copied 190 -> 168 us).
+        const bool straddles = !o.mn && rows > 1 && (o.ld % 64 || !aligned_to(o.p, 128)) && p.K >= 512 && extent[1 - i] >= 3200;
+        if (!p.f32 && (straddles || !tma_takes(o.p, rows, o.ld, 2))) {
             ld = round_up(cols, 64);
             bf16 *copy = (bf16 *)room.take((size_t)rows * ld * 2);
             if (run) {
@@ -600,6 +678,14 @@ tsr_status forward(const tsr_linear_desc *d, const tsr_linear_io *io, void *work
     p.e.act = d->activation;
     const int sms = device_sms();
     const auto all = [&](Room &room, bool run, int n) -> tsr_status {
+        if (p.M > 0 && p.M <= FEW_ROWS && p.N > 0 && p.K > 0) {
+            if (!run) return TSR_OK;
+            FewArgs a = {};
+            a.x = io->x.data; a.ldx = io->x.ld; a.w = io->weight.data; a.ldw = io->weight.ld;
+            a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K;
+            a.e = p.e;
+            return (p.f32 ? few_launch<float>(a, stream) : few_launch<bf16>(a, stream)) == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
+        }
         if (p.f32 && p.M > 0 && p.N > 0 && p.K > 0) {
             tsr_status e = three_planes(io->x, d->rows, d->ins, false, &p.A, room, run, n, stream);
             if (e == TSR_OK) e = three_planes(io->weight, d->outs, d->ins, false, &p.B, room, run, n, stream);
@@ -640,7 +726,7 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
     const int known = device_sms(), sms = known ? known : 148;
 
     // dz, and the partial sums of its columns (see the kernel): what is resident at once, 32 rows each at least
-    const bool make_dz = (d->activation != TSR_ACT_NONE || drop.threshold) && (dx || dw) && T > 0 && O > 0;
+    const bool make_dz = (d->activation != TSR_ACT_NONE || drop.threshold || f32) && (dx || dw) && T > 0 && O > 0;      // (FP32: dz in planes)
     const int64_t col_blocks = (O + DZ_COLS - 1) / DZ_COLS;
     const int64_t most = col_blocks ? std::max<int64_t>(1, std::min<int64_t>((T + 31) / 32, DZ_CTAS * sms / col_blocks)) : 1;
     const int64_t rows_per = T ? round_up((T + most - 1) / most, 8) : 8;
@@ -660,14 +746,14 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
         Room room = {run ? (char *)workspace : nullptr, 0};
         if (make_dz) {
             dz.ld = round_up(O, 64);
-            dz.data = room.take((size_t)T * dz.ld * (f32 ? 4 : 2));
+            dz.data = room.take((size_t)T * dz.ld * (f32 ? 6 : 2));
         }
         float *partial = db ? (float *)room.take((size_t)parts * O * 4) : nullptr;
         if (run && T > 0 && (make_dz || db)) {
             DzArgs a = {};
             a.dy = io->dy.data; a.lddy = io->dy.ld;
             a.pre = io->pre.data; a.ldpre = io->pre.ld;
-            a.dz = make_dz ? dz.data : nullptr; a.lddz = dz.ld;
+            a.dz = make_dz ? dz.data : nullptr; a.lddz = dz.ld; a.plane = T * dz.ld;
             a.partial = partial;
             a.rows = T; a.cols = (int)O; a.rows_per = (int)rows_per;
             a.drop = drop;
@@ -676,11 +762,10 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             if (rc != cudaSuccess) return TSR_ERR_CUDA;
         }
         if (run && db && column_finish(partial, T ? (int)parts : 0, O, O, io->dbias, d->gb_dtype == TSR_BF16, nullptr, false, d->accumulate != 0, stream) != cudaSuccess) return TSR_ERR_CUDA;
-        // FP32: planes of what both products, or one of them, read
-        Operand dz_op = {dz.data, dz.ld, false, 0}, w_op = {io->weight.data, io->weight.ld, true, 0}, x_op = {io->x.data, io->x.ld, true, 0};
+        // FP32: planes of the other operands
+        Operand dz_op = {dz.data, dz.ld, false, T * dz.ld}, w_op = {io->weight.data, io->weight.ld, true, 0}, x_op = {io->x.data, io->x.ld, true, 0};
         if (f32 && T > 0 && O > 0 && I > 0) {
-            if (dx || dw) st = three_planes(dz, T, O, false, &dz_op, room, run, sms, stream);
-            if (st == TSR_OK && dx) st = three_planes(io->weight, O, I, true, &w_op, room, run, sms, stream);
+            if (dx) st = three_planes(io->weight, O, I, true, &w_op, room, run, sms, stream);
             if (st == TSR_OK && dw) st = three_planes(io->x, T, I, true, &x_op, room, run, sms, stream);
             if (st != TSR_OK) return st;
         }
