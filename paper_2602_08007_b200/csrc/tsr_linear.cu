@@ -286,7 +286,9 @@ constexpr int DZ_CTAS = 4;     // on an SM
 struct DzArgs {
     const void *dy, *pre;
     void *dz;                  // BF16, or (FP32) three BF16 planes `plane` entries apart
-    float *partial;            // [gridDim.y][cols], NULL: no sums
+    float *partial;            // [gridDim.y][cols], NULL: no sums, or they go to `sums`
+    void *sums;                // with a single range of rows: the sums themselves
+    int32_t sums_bf16, accumulate;
     int64_t lddy, ldpre, lddz, plane, rows;
     int32_t cols, rows_per;
     DropArgs drop;
@@ -343,7 +345,7 @@ linear_dz_kernel(const DzArgs a)
             dy += 8 * a.lddy;
         }
     }
-    if (!a.partial) return;
+    if (!a.partial && !a.sums) return;
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[warp][lane * 8 + j] = acc[j];
     __syncthreads();
@@ -352,7 +354,8 @@ linear_dz_kernel(const DzArgs a)
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
-        a.partial[(int64_t)blockIdx.y * a.cols + c] = s;
+        if (a.partial) a.partial[(int64_t)blockIdx.y * a.cols + c] = s;
+        else store_as(a.sums, c, a.sums_bf16, a.accumulate ? s + load_as(a.sums, c, a.sums_bf16) : s);
     }
 }
 
@@ -482,7 +485,7 @@ struct Shape { int cg, width, splits, kb, kb_per; int64_t m_tiles, n_tiles, whol
 // intake of 64 bytes a clock its share of the operands; a wave of tiles costs the larger one times its blocks.  The tiles of the last wave
 // (and, where that is nearly full, of the one before) may be split, so that the last wave is short: for that their slabs are
 // written (32 bytes a clock and SM) and read again (3000 bytes a clock in all) by another launch.
-Shape choose(const Product &p, int sms)
+Shape search(const Product &p, int sms)
 {
     Shape best = {};
     double best_cost = 1e300;
@@ -513,6 +516,20 @@ Shape choose(const Product &p, int sms)
         }
     }
     return best;
+}
+
+// The search takes a few microseconds and a call needs its result several times: the last results of the host thread are kept, by sizes.
+Shape choose(const Product &p, int sms)
+{
+    struct Known { int64_t M, N, K; int f32, pre, sms; Shape shape; };
+    static thread_local Known known[8] = {};
+    static thread_local int next = 0;
+    const int f32 = p.f32, pre = p.e.pre != nullptr;
+    for (const Known &k : known)
+        if (k.M == p.M && k.N == p.N && k.K == p.K && k.f32 == f32 && k.pre == pre && k.sms == sms) return k.shape;
+    Known &k = known[next++ & 7];
+    k = {p.M, p.N, p.K, f32, pre, sms, search(p, sms)};
+    return k.shape;
 }
 
 struct Room {      // walks the workspace; with base NULL it only counts
@@ -728,7 +745,7 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
     // dz, and the partial sums of its columns (see the kernel): what is resident at once, 32 rows each at least
     const bool make_dz = (d->activation != TSR_ACT_NONE || drop.threshold || f32) && (dx || dw) && T > 0 && O > 0;      // (FP32: dz in planes)
     const int64_t col_blocks = (O + DZ_COLS - 1) / DZ_COLS;
-    const int64_t most = col_blocks ? std::max<int64_t>(1, std::min<int64_t>((T + 31) / 32, DZ_CTAS * sms / col_blocks)) : 1;
+    const int64_t most = col_blocks ? std::max<int64_t>(1, T <= 64 ? 1 : std::min<int64_t>((T + 31) / 32, DZ_CTAS * sms / col_blocks)) : 1;
     const int64_t rows_per = T ? round_up((T + most - 1) / most, 8) : 8;
     const int64_t parts = std::max<int64_t>(1, (T + rows_per - 1) / rows_per);
 
@@ -748,20 +765,22 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             dz.ld = round_up(O, 64);
             dz.data = room.take((size_t)T * dz.ld * (f32 ? 6 : 2));
         }
-        float *partial = db ? (float *)room.take((size_t)parts * O * 4) : nullptr;
+        const bool direct = parts == 1 && T > 0;      // a single range of rows: its sums are the result
+        float *partial = db && !direct ? (float *)room.take((size_t)parts * O * 4) : nullptr;
         if (run && T > 0 && (make_dz || db)) {
             DzArgs a = {};
             a.dy = io->dy.data; a.lddy = io->dy.ld;
             a.pre = io->pre.data; a.ldpre = io->pre.ld;
             a.dz = make_dz ? dz.data : nullptr; a.lddz = dz.ld; a.plane = T * dz.ld;
             a.partial = partial;
+            if (direct) { a.sums = io->dbias; a.sums_bf16 = d->gb_dtype == TSR_BF16; a.accumulate = d->accumulate; }
             a.rows = T; a.cols = (int)O; a.rows_per = (int)rows_per;
             a.drop = drop;
             const dim3 grid((unsigned)col_blocks, (unsigned)parts);
             const cudaError_t rc = f32 ? dz_launch<float>(a, d->activation, grid, stream) : dz_launch<bf16>(a, d->activation, grid, stream);
             if (rc != cudaSuccess) return TSR_ERR_CUDA;
         }
-        if (run && db && column_finish(partial, T ? (int)parts : 0, O, O, io->dbias, d->gb_dtype == TSR_BF16, nullptr, false, d->accumulate != 0, stream) != cudaSuccess) return TSR_ERR_CUDA;
+        if (run && db && !direct && column_finish(partial, T ? (int)parts : 0, O, O, io->dbias, d->gb_dtype == TSR_BF16, nullptr, false, d->accumulate != 0, stream) != cudaSuccess) return TSR_ERR_CUDA;
         // FP32: planes of the other operands
         Operand dz_op = {dz.data, dz.ld, false, T * dz.ld}, w_op = {io->weight.data, io->weight.ld, true, 0}, x_op = {io->x.data, io->x.ld, true, 0};
         if (f32 && T > 0 && O > 0 && I > 0) {

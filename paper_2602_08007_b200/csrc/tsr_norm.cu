@@ -43,7 +43,9 @@ struct NormArgs {
     void *y;                        // y, or dx
     float *stats;
     const float *stats_in;
-    float *partial;                 // [parts][cols] of dweight, then of dbias
+    float *partial;                 // [parts][cols] of dweight, then of dbias; NULL: one CTA, the sums go to dw and db
+    void *dw, *db;
+    int32_t g_bf16, accumulate;
     int64_t ldx, lddy, ldy, rows;
     int32_t cols, p_bf16, center, want_dw, want_db;
     int32_t period;                 // classes of rows that start at the same place in a unit; 0: the matrices differ in that
@@ -544,8 +546,14 @@ norm_backward_kernel(const NormArgs a, int stages)
         for (int i = 0; i < V; ++i) {
             const int c = (u * threads + tid) * V - rc.shift + i;
             if (c < 0 || c >= a.cols) continue;
-            if (a.want_dw) a.partial[(int64_t)blockIdx.x * a.cols + c] = i & 1 ? dw[u][i / 2].y : dw[u][i / 2].x;
-            if (DB) a.partial[((int64_t)(a.want_dw ? gridDim.x : 0) + blockIdx.x) * a.cols + c] = i & 1 ? db[u][i / 2].y : db[u][i / 2].x;
+            const float w = i & 1 ? dw[u][i / 2].y : dw[u][i / 2].x, b = !DB ? 0.f : i & 1 ? db[DB ? u : 0][i / 2].y : db[DB ? u : 0][i / 2].x;
+            if (a.partial) {
+                if (a.want_dw) a.partial[(int64_t)blockIdx.x * a.cols + c] = w;
+                if (DB) a.partial[((int64_t)(a.want_dw ? gridDim.x : 0) + blockIdx.x) * a.cols + c] = b;
+            } else {
+                if (a.want_dw) store_as(a.dw, c, a.g_bf16, a.accumulate ? w + load_as(a.dw, c, a.g_bf16) : w);
+                if (DB) store_as(a.db, c, a.g_bf16, a.accumulate ? b + load_as(a.db, c, a.g_bf16) : b);
+            }
         }
 }
 
@@ -835,8 +843,12 @@ extern "C" tsr_status tsr_norm_backward(const tsr_norm_desc *desc, tsr_matrix dy
     a.period = d.rows > 0 ? common_period(d, all, 3, &units) : 0;
     const int V = 16 / type_bytes(d.dtype);
     const int parts = backward_parts(d.rows, units, V, a.period, sms);
+    bool direct = false;      // a single CTA of the row kernel: its sums are the result
     if (d.rows > 0) {
         const bool bf = d.dtype == TSR_BF16;
+        direct = parts == 1 && a.period && units * V <= ROW_COLS;
+        if (direct) a.partial = nullptr;
+        a.dw = dweight; a.db = dbias; a.g_bf16 = d.g_dtype == TSR_BF16; a.accumulate = d.accumulate;
         cudaError_t e;
         if (a.period == 0 || units * V > ROW_COLS) e = bf ? backward_wide<bf16>(a, parts, sms, s) : backward_wide<float>(a, parts, sms, s);
         else e = bf ? backward_of<bf16>(a, units, parts, s) : backward_of<float>(a, units, parts, s);
@@ -844,6 +856,6 @@ extern "C" tsr_status tsr_norm_backward(const tsr_norm_desc *desc, tsr_matrix dy
     }
     const bool gb = d.g_dtype == TSR_BF16;
     void *one = dweight ? dweight : dbias, *two = dweight ? dbias : nullptr;
-    if (one && column_finish((const float *)workspace, d.rows ? parts : 0, d.cols, d.cols, one, gb, two, gb, d.accumulate != 0, s) != cudaSuccess) return TSR_ERR_CUDA;
+    if (one && !direct && column_finish((const float *)workspace, d.rows ? parts : 0, d.cols, d.cols, one, gb, two, gb, d.accumulate != 0, s) != cudaSuccess) return TSR_ERR_CUDA;
     return TSR_OK;
 }

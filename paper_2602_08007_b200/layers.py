@@ -26,6 +26,7 @@ from .binding import (
 _DTYPE = {torch.float32: TSR_F32, torch.bfloat16: TSR_BF16}
 ACTIVATIONS = {None: TSR_ACT_NONE, "none": TSR_ACT_NONE, "relu": TSR_ACT_RELU, "gelu": TSR_ACT_GELU, "gelu_tanh": TSR_ACT_GELU_TANH, "silu": TSR_ACT_SILU}
 _current_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 _NO_MATRIX = Matrix(None, 0)
 
 
@@ -76,11 +77,13 @@ def _layout(t: torch.Tensor):
 def _matrix(t: torch.Tensor, what: str, shape, dtype: torch.dtype, device: torch.device) -> Matrix:
     if t.dtype != dtype or t.device != device:
         raise ValueError("%s must be a %s tensor on %s" % (what, dtype, device))
+    if t.shape != shape:
+        raise ValueError("%s must have the shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
+    if t.is_contiguous():
+        return Matrix(t.data_ptr(), shape[-1])
     m = _layout(t)
     if m is None:
         raise ValueError(_ROWS % what)
-    if t.shape != shape:
-        raise ValueError("%s must have the shape %s, not %s" % (what, tuple(shape), tuple(t.shape)))
     return Matrix(t.data_ptr(), m[2])
 
 
@@ -91,9 +94,10 @@ def _vector(t: Optional[torch.Tensor], what: str, n: int, device: torch.device):
     """(pointer, type) of an optional vector."""
     if t is None:
         return None, TSR_F32
-    if t.dtype not in _DTYPE or t.device != device or t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    kind = _DTYPE.get(t.dtype)
+    if kind is None or t.shape != (n,) or t.device != device or not t.is_contiguous():
         raise ValueError("%s must be a contiguous FP32 or BF16 vector of %d elements on %s" % (what, n, device))
-    return t.data_ptr(), _DTYPE[t.dtype]
+    return t.data_ptr(), kind
 
 
 def _input(x: torch.Tensor, what: str):
@@ -130,7 +134,7 @@ def _placed(call):
     def placed(x, *args, stream=None, **kwargs):
         index = x.device.index
         if stream is None:
-            if index is None or index == torch.cuda.current_device():
+            if index is None or index == _current_device():
                 return call(x, *args, **kwargs)
             with torch.cuda.device(x.device):
                 return call(x, *args, **kwargs)
@@ -171,11 +175,11 @@ def norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: O
             raise ValueError("weight and bias must have the same type")
         wt = wt if w is not None else bt
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        out = x.new_empty(x.shape)
         my = Matrix(out.data_ptr(), cols)
     else:
         my = _matrix(out, "out", x.shape, x.dtype, dev)
-    stats = torch.empty((rows, 2), dtype=torch.float32, device=dev)
+    stats = x.new_empty((rows, 2), dtype=torch.float32)
     desc = NormDesc(rows, cols, kind, wt, TSR_F32, 1 if center else 0, 0, eps)
     _check(lib().tsr_norm_forward(desc, Matrix(x.data_ptr(), ld), w, b, my, stats.data_ptr(), _current_stream(dev.index)), "tsr_norm_forward")
     return out, stats
@@ -200,12 +204,12 @@ def norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tens
     if not want_dx:
         dx, mdx = None, _NO_MATRIX
     elif dx is None:
-        dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+        dx = x.new_empty(x.shape)
         mdx = Matrix(dx.data_ptr(), cols)
     else:
         mdx = _matrix(dx, "dx", x.shape, x.dtype, dev)
-    dweight = (torch.empty(cols, dtype=torch.float32, device=dev) if dweight is None else dweight) if want_dweight else None
-    dbias = (torch.empty(cols, dtype=torch.float32, device=dev) if dbias is None else dbias) if bias else None
+    dweight = (x.new_empty(cols, dtype=torch.float32) if dweight is None else dweight) if want_dweight else None
+    dbias = (x.new_empty(cols, dtype=torch.float32) if dbias is None else dbias) if bias else None
     gw, gwt = _vector(dweight, "dweight", cols, dev)
     gb, gbt = _vector(dbias, "dbias", cols, dev)
     if gw is not None and gb is not None and gwt != gbt:
@@ -309,7 +313,7 @@ def dropout_forward(x: torch.Tensor, dropout: Dropout, residual: Optional[torch.
     kind, (rows, cols, ld), dev = _input(x, "x")
     mres = _matrix(residual, "residual", x.shape, x.dtype, dev) if residual is not None else _NO_MATRIX
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        out = x.new_empty(x.shape)
         my = Matrix(out.data_ptr(), cols)
     else:
         my = _matrix(out, "out", x.shape, x.dtype, dev)

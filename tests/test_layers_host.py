@@ -66,11 +66,11 @@ def test_norm_refuses_matrices(tsr):
 def test_norm_scratch_of_any_size(tsr, rows, cols, dtype):
     size = ctypes.c_size_t()
     assert tsr.lib().tsr_norm_workspace_bytes(ctypes.byref(norm_desc(tsr, rows=rows, cols=cols, dtype=dtype)), ctypes.byref(size)) == 0
-    assert (size.value >= 8 * cols and size.value <= 8 * cols * 148 * 16) if cols else size.value == 0
+    assert (size.value >= 8 * cols and size.value <= 8 * cols * 148 * 24) if cols else size.value == 0
 
 
 def linear_desc(tsr, drop=(0.0, 0, 0, 0, None), **kw):
-    d = dict(rows=4, ins=8, outs=16, dtype=1, b_dtype=0, gw_dtype=0, gb_dtype=0, activation=0, accumulate=0)
+    d = dict(rows=100, ins=8, outs=16, dtype=1, b_dtype=0, gw_dtype=0, gb_dtype=0, activation=0, accumulate=0)
     d.update(kw)
     return tsr.LinearDesc(*d.values(), tsr.DropoutDesc(*drop))
 
@@ -106,7 +106,7 @@ def test_linear_refuses_matrices_and_scratch(tsr):
     assert fwd(x=M(AT, 7)) == 2 and fwd(weight=M(AT, 7)) == 2 and fwd(y=M(AT, 15)) == 2 and fwd(residual=M(AT, 15)) == 2 and fwd(pre=M(AT, 15)) == 2
     assert fwd(x=M(AT + 1, 8)) == 3 and fwd(y=M(AT + 1, 16)) == 3 and fwd(bias=AT + 2) == 3
     assert L.tsr_linear_forward_bytes(None, None, ctypes.byref(size)) == 1 and L.tsr_linear_forward_bytes(ctypes.byref(d), None, None) == 1
-    assert fwd(x=M(AT + 2, 8)) == 0 and size.value >= 4 * 8 * 2          # an operand that is copied needs scratch
+    assert fwd(x=M(AT + 2, 8)) == 0 and size.value >= 100 * 8 * 2        # an operand that is copied needs scratch
     io = tsr.LinearIO(*dict(base, x=M(AT + 2, 8)).values())
     assert L.tsr_linear_forward(ctypes.byref(d), ctypes.byref(io), None, 0, None) == 4
     assert L.tsr_linear_forward(ctypes.byref(d), ctypes.byref(io), AT, size.value - 1, None) == 4
