@@ -8,7 +8,10 @@
   projection being linear, onto the cores;
 * half-way the dense states are written out as FP32 moments and read back, as a checkpoint would.
 
-    python examples/pretrain_small.py [steps]
+With `layers` the model itself runs on the library's layer operators: norms, linear layers with activation, dropout and residual in their epilogue, and
+the matrices' gradients written by the backward pass straight into the G of their TSR blocks.
+
+    python examples/pretrain_small.py [steps] [layers]
 """
 import math
 import os
@@ -54,6 +57,24 @@ def logits_of(tokens, embed, mats, norms, head, rotary):
     return (norm(x, norms[-1]) @ head.t()).float()
 
 
+def logits_of_layers(tokens, embed, mats, norms, head, rotary, grads, drop):
+    """The same model on the layer operators.  grads: where the matrices' gradients go; drop: dropout of the k-th residual branch, or None."""
+    x = embed[tokens]
+    mask = torch.full((LENGTH, LENGTH), -math.inf, device=x.device).triu(1)
+    for layer in range(LAYERS):
+        q, k, v, o, gate, up, down = zip(mats[layer * 7:layer * 7 + 7], grads[layer * 7:layer * 7 + 7])
+        h = tsr.rms_norm(x, norms[2 * layer])
+        split = lambda t: t.view(t.shape[0], LENGTH, HEADS, HIDDEN // HEADS).transpose(1, 2)  # noqa: E731
+        project = lambda w: split(tsr.linear(h, w[0], weight_grad=w[1]))  # noqa: E731,B023
+        a = rotary(project(q)) @ rotary(project(k)).transpose(-1, -2)
+        a = torch.softmax(a.float() / math.sqrt(HIDDEN // HEADS) + mask, dim=-1).to(x.dtype) @ project(v)
+        x = tsr.linear(a.transpose(1, 2).reshape(x.shape), o[0], dropout=drop(2 * layer), residual=x, weight_grad=o[1])
+        h = tsr.rms_norm(x, norms[2 * layer + 1])
+        x = tsr.linear(tsr.linear(h, gate[0], activation="silu", weight_grad=gate[1]) * tsr.linear(h, up[0], weight_grad=up[1]), down[0],
+                       dropout=drop(2 * layer + 1), residual=x, weight_grad=down[1])
+    return tsr.linear(tsr.rms_norm(x, norms[-1]), head).float()
+
+
 def batches(device, seed):
     """Synthetic text: from every token one of four others follows, the first most often."""
     gen = torch.Generator(device="cpu").manual_seed(seed)
@@ -67,8 +88,9 @@ def batches(device, seed):
         yield t.to(device)
 
 
-def train(steps=60, seed=0, lr=3e-3, max_norm=1.0, log=None):
-    """Returns the losses and the gradient norms of all steps."""
+def train(steps=60, seed=0, lr=3e-3, max_norm=1.0, log=None, layers=False, dropout=0.0, seen=None):
+    """Returns the losses and the gradient norms of all steps.  layers: on the library's layer operators, with `dropout` on the residual branches.
+    seen: called with (step, gradients of the matrices, other gradients) before each step."""
     device = torch.device("cuda")
     torch.manual_seed(seed)
     blocks = [dict(m=m, n=n, r=RANK, p=8, q=1, K=20) for m, n in SHAPES * LAYERS]
@@ -87,11 +109,18 @@ def train(steps=60, seed=0, lr=3e-3, max_norm=1.0, log=None):
         tokens = next(data)
         mats = [W.bfloat16().requires_grad_() for W in plan.W]
         leaves = [(image if image is not None else p).detach().requires_grad_() for p, image in zip(params, images)]
-        out = logits_of(tokens[:, :-1], leaves[0], mats, leaves[2:], leaves[1], rotary)
+        if layers:
+            drop = lambda k: tsr.Dropout(dropout, seed, t * 2 * LAYERS + k) if dropout else None  # noqa: E731,B023
+            out = logits_of_layers(tokens[:, :-1], leaves[0], mats, leaves[2:], leaves[1], rotary, plan.G, drop)
+        else:
+            out = logits_of(tokens[:, :-1], leaves[0], mats, leaves[2:], leaves[1], rotary)
         loss = torch.nn.functional.cross_entropy(out.reshape(-1, VOCAB), tokens[:, 1:].reshape(-1))
         loss.backward()
         for G, w in zip(plan.G + grads, mats + leaves):
-            G.copy_(w.grad)
+            if not layers or w.grad is not None:
+                G.copy_(w.grad)
+        if seen:
+            seen(t, plan.G, grads)
 
         hyper = tsr.make_hyper(t, lr=lr * min(1.0, t / 10), beta2=0.99, weight_decay=0.01)
         clip = dense.grad_norm(max_norm)                  # (norm, factor) on the device; no host read
@@ -119,4 +148,4 @@ def train(steps=60, seed=0, lr=3e-3, max_norm=1.0, log=None):
 
 
 if __name__ == "__main__":
-    train(int(sys.argv[1]) if len(sys.argv) > 1 else 60, log=print)
+    train(int(sys.argv[1]) if len(sys.argv) > 1 else 60, log=print, layers="layers" in sys.argv[2:])
