@@ -351,12 +351,12 @@ typedef struct { void *data; int64_t ld; } tsr_matrix;
 /* Dropout from a counter-based generator: entry (row, col) is zero with probability p' = round(65536 p) / 65536, decided by 16 bits
  * that depend on (seed, offset, row, col) alone, and is multiplied by 1 / (1 - p') otherwise.  No mask is stored: the
  * backward pass draws the same bits again, as does any other call with the same seed and offset.  step: NULL, or a
- * DEVICE word that is added to offset when a kernel runs, so that a captured graph draws new bits at every replay. */
+ * DEVICE word (8-byte aligned) that is added to offset when a kernel runs, so that a captured graph draws new bits at every replay. */
 typedef struct { float p; int32_t reserved; uint64_t seed, offset; const int64_t *step; } tsr_dropout_desc;
 
 /* Norm over the rows of x: with mu the mean of a row (center != 0; otherwise 0) and r = 1 / sqrt(mean((x - mu)^2) + eps),
  *     y = (x - mu) r o weight + bias        (weight NULL: ones; bias NULL: zeros)
- * stats (rows x 2, FP32, may be NULL) receives (mu, r) for the backward pass:  with h = (x - mu) r, g = dy o weight,
+ * stats (rows x 2, FP32, 8-byte aligned, may be NULL) receives (mu, r) for the backward pass:  with h = (x - mu) r, g = dy o weight,
  *     dx = r (g - center mean(g) - h mean(g o h)),   dweight = sum over rows of dy o h,   dbias = sum over rows of dy.
  * y may be x itself, dx may be dy itself.  dx, dweight and dbias may each be NULL (not wanted). */
 typedef struct {

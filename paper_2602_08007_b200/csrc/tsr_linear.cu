@@ -219,6 +219,7 @@ struct FewArgs {
     LinearEpilogue e;
 };
 constexpr int FEW_ROWS = 8, FEW_SHARED = 8192;      // entries of x in shared memory
+constexpr int64_t FEW_MOST_K = 1 << 24;             // beyond that K has to be split, and the kernel counts in 32 bits
 template <typename T, int ROWS>
 __global__ void __launch_bounds__(256)
 linear_few_kernel(const __grid_constant__ FewArgs a)
@@ -415,6 +416,7 @@ bool drop_args(const tsr_dropout_desc &d, DropArgs *out)
     if (!(d.p >= 0.f && d.p <= 1.f)) return false;
     out->threshold = (uint32_t)floor((double)d.p * 65536.0 + 0.5);
     out->scale = out->threshold == 65536u ? 0.f : (float)(65536.0 / (65536 - (int)out->threshold));
+    if (!aligned_to(d.step, 8)) return false;
     out->seed_key = mix32((uint32_t)d.seed ^ mix32((uint32_t)(d.seed >> 32) + 0x9e3779b9u));
     out->offset = d.offset;
     out->step = d.step;
@@ -568,7 +570,14 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
         return run ? finish() : TSR_OK;
     }
 
-    const Shape s = choose(p, sms);
+    Shape s = choose(p, sms);
+    if (p.f32 && !p.out_f32 && s.whole) {
+        // FP32 operands, BF16 weight gradient: the kernel has FP32 boxes alone there, so all tiles go through slabs, as single parts where K needs no split
+        s.tail = s.m_tiles * s.n_tiles;
+        s.whole = 0;
+        s.splits = 1;
+        s.kb_per = s.kb;
+    }
     if (s.m_tiles * s.n_tiles > (int64_t)1 << 28) return TSR_ERR_SHAPE;
     LinearGemm g = {};
     g.M = (int)p.M; g.N = (int)p.N;
@@ -695,7 +704,7 @@ tsr_status forward(const tsr_linear_desc *d, const tsr_linear_io *io, void *work
     p.e.act = d->activation;
     const int sms = device_sms();
     const auto all = [&](Room &room, bool run, int n) -> tsr_status {
-        if (p.M > 0 && p.M <= FEW_ROWS && p.N > 0 && p.K > 0) {
+        if (p.M > 0 && p.M <= FEW_ROWS && p.N > 0 && p.K > 0 && p.K <= FEW_MOST_K) {
             if (!run) return TSR_OK;
             FewArgs a = {};
             a.x = io->x.data; a.ldx = io->x.ld; a.w = io->weight.data; a.ldw = io->weight.ld;

@@ -557,7 +557,7 @@ norm_backward_kernel(const NormArgs a, int stages)
         }
 }
 
-// Any width and alignment: dx alone, two passes over the row, ...
+// Any width and alignment: dx alone, two passes over the row (after the column sums, as it may replace dy), ...
 template <typename T>
 __global__ void __launch_bounds__(1024)
 norm_backward_wide_kernel(const NormArgs a)
@@ -751,13 +751,13 @@ cudaError_t backward_of(const NormArgs &a, int units, int parts, cudaStream_t s)
 template <typename T>
 cudaError_t backward_wide(const NormArgs &a, int parts, int sms, cudaStream_t s)
 {
-    if (a.y) {
-        const int threads = any_threads(a.cols);
-        const cudaError_t e = launch_dependent(norm_backward_wide_kernel<T>, dim3((unsigned)std::min<int64_t>(a.rows, (int64_t)sms * (2048 / threads))), dim3(threads), 0, s, 1, a);
+    if (a.want_dw || a.want_db) {      // first: dx may replace dy
+        const cudaError_t e = launch_dependent(norm_columns_kernel<T>, dim3((unsigned)((a.cols + 255) / 256), (unsigned)parts), dim3(256), 0, s, 1, a, (a.rows + parts - 1) / parts);
         if (e != cudaSuccess) return e;
     }
-    if (!a.want_dw && !a.want_db) return cudaSuccess;
-    return launch_dependent(norm_columns_kernel<T>, dim3((unsigned)((a.cols + 255) / 256), (unsigned)parts), dim3(256), 0, s, 1, a, (a.rows + parts - 1) / parts);
+    if (!a.y) return cudaSuccess;
+    const int threads = any_threads(a.cols);
+    return launch_dependent(norm_backward_wide_kernel<T>, dim3((unsigned)std::min<int64_t>(a.rows, (int64_t)sms * (2048 / threads))), dim3(threads), 0, s, 1, a);
 }
 
 constexpr int64_t MOST_COLS = 0x7fffffff - 1023, MOST_ROWS = (int64_t)1 << 40;
@@ -788,7 +788,7 @@ extern "C" tsr_status tsr_norm_forward(const tsr_norm_desc *desc, tsr_matrix x, 
     if (st != TSR_OK) return st;
     const tsr_norm_desc &d = *desc;
     if ((st = check_rows(x, d, true)) != TSR_OK || (st = check_rows(y, d, true)) != TSR_OK) return st;
-    if (!aligned_to(weight, type_bytes(d.p_dtype)) || !aligned_to(bias, type_bytes(d.p_dtype)) || !aligned_to(stats, 4)) return TSR_ERR_ALIGNMENT;
+    if (!aligned_to(weight, type_bytes(d.p_dtype)) || !aligned_to(bias, type_bytes(d.p_dtype)) || !aligned_to(stats, 8)) return TSR_ERR_ALIGNMENT;
     if (d.rows == 0 || d.cols == 0) return TSR_OK;
     const int sms = device_sms();
     if (!sms) return TSR_ERR_CUDA;
@@ -822,7 +822,7 @@ extern "C" tsr_status tsr_norm_backward(const tsr_norm_desc *desc, tsr_matrix dy
     const tsr_norm_desc &d = *desc;
     if ((st = check_rows(dy, d, true)) != TSR_OK || (st = check_rows(x, d, true)) != TSR_OK || (st = check_rows(dx, d, false)) != TSR_OK) return st;
     if (!stats && d.rows > 0 && d.cols > 0) return TSR_ERR_INVALID_ARG;
-    if (!aligned_to(weight, type_bytes(d.p_dtype)) || !aligned_to(dweight, type_bytes(d.g_dtype)) || !aligned_to(dbias, type_bytes(d.g_dtype)) || !aligned_to(stats, 4))
+    if (!aligned_to(weight, type_bytes(d.p_dtype)) || !aligned_to(dweight, type_bytes(d.g_dtype)) || !aligned_to(dbias, type_bytes(d.g_dtype)) || !aligned_to(stats, 8))
         return TSR_ERR_ALIGNMENT;
     const int known = device_sms(), sms = known ? known : 148;
     if (dweight || dbias) {

@@ -13,6 +13,7 @@ from __future__ import annotations
 import contextlib
 import ctypes
 import functools
+import inspect
 import weakref
 from typing import Optional
 
@@ -131,17 +132,19 @@ def _placed(call):
     """Runs the call on the tensors' device and on `stream`, whatever is current.  (A wrapper that steps aside where nothing is to be changed: small
     calls are bound by what the host does, and a context costs 1 us.)"""
     @functools.wraps(call)
-    def placed(x, *args, stream=None, **kwargs):
-        index = x.device.index
+    def placed(*args, stream=None, **kwargs):
+        device = (args[0] if args else kwargs[first]).device
         if stream is None:
-            if index is None or index == _current_device():
-                return call(x, *args, **kwargs)
-            with torch.cuda.device(x.device):
-                return call(x, *args, **kwargs)
-        if stream.device != x.device:
-            raise ValueError("stream must belong to %s" % x.device)
+            if device.index is None or device.index == _current_device():
+                return call(*args, **kwargs)
+            with torch.cuda.device(device):
+                return call(*args, **kwargs)
+        if stream.device != device:
+            raise ValueError("stream must belong to %s" % device)
         with torch.cuda.stream(stream):
-            return call(x, *args, **kwargs)
+            return call(*args, **kwargs)
+
+    first = next(iter(inspect.signature(call).parameters))
     return placed
 
 
@@ -341,27 +344,29 @@ def _lies(t: torch.Tensor) -> torch.Tensor:
     return t if _layout(t) is not None else t.contiguous()
 
 
-def _guard_capture(ctx, *tensors):
+_EAGER = weakref.WeakSet()     # graphs (their contexts) that were made outside of a capture and still live
+
+
+def _guard_capture(ctx, graph: bool, *tensors):
     """Torch keeps one gradient accumulator per leaf, bound to the stream of the graph that made it.  A backward pass that is captured
     while an eager graph of the same leaf is alive reaches that stream from within the capture and ends the process, so the capture is refused
-    here, where it can still be an error.  (Seen for leaves that are inputs of these functions themselves.)"""
-    leaves = [t for t in tensors if t is not None and t.requires_grad and t.is_leaf]
+    here, where it can still be an error.  (Seen for leaves that are inputs of these functions themselves.)  graph: whether torch records one."""
+    leaves = [t for t in tensors if graph and t is not None and t.requires_grad and t.is_leaf]
     if not leaves:
         return
     if torch.cuda.is_current_stream_capturing():
-        if any(len(getattr(t, "_tsr_eager_graphs", ())) for t in leaves):
+        ours = {id(t) for t in leaves}
+        if any(id(t) in ours for other in list(_EAGER) for t in other.leaves):
             raise RuntimeError("a graph of this tensor from outside of the capture is still alive: drop its outputs before capturing")
         return
-    for t in leaves:
-        if not hasattr(t, "_tsr_eager_graphs"):
-            t._tsr_eager_graphs = weakref.WeakSet()
-        t._tsr_eager_graphs.add(ctx)
+    ctx.leaves = leaves      # (held by the graph anyway)
+    _EAGER.add(ctx)
 
 
 class _Norm(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, eps, center):
-        _guard_capture(ctx, x, weight, bias)
+    def forward(ctx, graph, x, weight, bias, eps, center):
+        _guard_capture(ctx, graph, x, weight, bias)
         x = _lies(x)
         weight, bias = (None if t is None else t.contiguous() for t in (weight, bias))
         y, stats = norm_forward(x, weight, bias, eps=eps, center=center)
@@ -374,18 +379,18 @@ class _Norm(torch.autograd.Function):
     def backward(ctx, dy):
         x, weight, stats = ctx.saved_tensors
         need = ctx.needs_input_grad
-        dx, dw, db = norm_backward(_lies(dy), x, weight, stats, center=ctx.center, bias=need[2], want_dx=need[0], want_dweight=need[1])
+        dx, dw, db = norm_backward(_lies(dy), x, weight, stats, center=ctx.center, bias=need[3], want_dx=need[1], want_dweight=need[2])
         wt, bt = ctx.types
-        return dx, None if dw is None else dw.to(wt), None if db is None else db.to(bt), None, None
+        return None, dx, None if dw is None else dw.to(wt), None if db is None else db.to(bt), None, None
 
 
 class _Linear(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, weight, bias, residual, activation, drop, weight_grad, accumulate):
-        _guard_capture(ctx, x, weight, bias, residual)
+    def forward(ctx, graph, x, weight, bias, residual, activation, drop, weight_grad, accumulate):
+        _guard_capture(ctx, graph, x, weight, bias, residual)
         x, weight = _lies(x), _lies(weight)
         act = _activation(activation)
-        keep = act != TSR_ACT_NONE and any(ctx.needs_input_grad[:3])
+        keep = act != TSR_ACT_NONE and graph and any(ctx.needs_input_grad[1:4])
         y, pre = linear_forward(x, weight, None if bias is None else bias.contiguous(), act, drop, None if residual is None else _lies(residual), keep_pre=keep)
         ctx.save_for_backward(x, weight, pre)
         ctx.act, ctx.drop, ctx.weight_grad, ctx.accumulate = act, drop, weight_grad, accumulate
@@ -396,10 +401,10 @@ class _Linear(torch.autograd.Function):
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         x, weight, pre = ctx.saved_tensors
-        need = ctx.needs_input_grad
+        need = ctx.needs_input_grad[1:]
         dres = dy if need[3] else None
         if not any(need[:3]):
-            return None, None, None, dres, None, None, None, None
+            return None, None, None, None, dres, None, None, None, None
         g = _lies(dy)
         kept = ctx.weight_grad if need[1] else None
         db = torch.empty(weight.shape[0], dtype=torch.float32, device=dy.device) if need[2] else None
@@ -407,31 +412,31 @@ class _Linear(torch.autograd.Function):
             db.zero_()
         dx, dw, db = linear_backward(g, x, weight, pre, ctx.act, ctx.drop, dweight=kept, dbias=db, accumulate=kept is not None and ctx.accumulate,
                                      want_dx=need[0], want_dweight=need[1])
-        return dx, None if kept is not None else dw, None if db is None else db.to(ctx.bias_type), dres, None, None, None, None
+        return None, dx, None if kept is not None else dw, None if db is None else db.to(ctx.bias_type), dres, None, None, None, None
 
 
 class _Dropout(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, x, drop, residual):
-        _guard_capture(ctx, x, residual)
+    def forward(ctx, graph, x, drop, residual):
+        _guard_capture(ctx, graph, x, residual)
         ctx.drop = drop
         return dropout_forward(_lies(x), drop, None if residual is None else _lies(residual))
 
     @staticmethod
     @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
-        dx = dropout_backward(_lies(dy), ctx.drop) if ctx.needs_input_grad[0] else None
-        return dx, None, dy if ctx.needs_input_grad[2] else None
+        dx = dropout_backward(_lies(dy), ctx.drop) if ctx.needs_input_grad[1] else None
+        return None, dx, None, dy if ctx.needs_input_grad[3] else None
 
 
 def layer_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, eps: float = 1e-5) -> torch.Tensor:
     """Differentiable norm_forward."""
-    return _Norm.apply(x, weight, bias, eps, True)
+    return _Norm.apply(torch.is_grad_enabled(), x, weight, bias, eps, True)
 
 
 def rms_norm(x: torch.Tensor, weight: Optional[torch.Tensor] = None, eps: float = 1e-6) -> torch.Tensor:
     """Differentiable norm_forward without the mean."""
-    return _Norm.apply(x, weight, None, eps, False)
+    return _Norm.apply(torch.is_grad_enabled(), x, weight, None, eps, False)
 
 
 def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] = None, activation=None, dropout: Optional[Dropout] = None,
@@ -441,9 +446,9 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor] =
     more than once needs accumulate, over a matrix that was set to zero."""
     if weight_grad is not None and torch.is_grad_enabled() and not weight.requires_grad:
         raise ValueError("weight_grad needs a weight that requires a gradient")
-    return _Linear.apply(x, weight, bias, residual, activation, dropout, weight_grad, accumulate)
+    return _Linear.apply(torch.is_grad_enabled(), x, weight, bias, residual, activation, dropout, weight_grad, accumulate)
 
 
 def dropout(x: torch.Tensor, dropout: Dropout, residual: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Differentiable dropout_forward."""
-    return _Dropout.apply(x, dropout, residual)
+    return _Dropout.apply(torch.is_grad_enabled(), x, dropout, residual)

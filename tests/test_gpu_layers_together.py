@@ -1,5 +1,7 @@
 """The layer operators as they are used: in a row, under autograd, into the optimizer's gradients, on other streams, in captured graphs."""
+import copy
 import importlib.util
+import io
 import os
 
 import pytest
@@ -241,6 +243,59 @@ def test_a_capture_beside_a_living_eager_graph_is_refused(tsr):
     torch.cuda.synchronize()
     assert float((w.grad - 2 * first).abs().max()) <= 2.0 ** -16 * float(first.abs().max())
     g.reset()
+
+
+def test_inference_is_captured_beside_a_living_graph(tsr):
+    """What records no graph is not refused; and a leaf that was used stays an ordinary tensor, to copy and to save."""
+    x, w = normal(64, 32, seed=1), torch.nn.Parameter(normal(48, 32, seed=2))
+    eager = tsr.linear(x, w, activation="gelu")
+    g = torch.cuda.CUDAGraph()
+    with torch.no_grad():
+        tsr.linear(x, w, activation="gelu")
+        torch.cuda.synchronize()
+        with torch.cuda.graph(g):
+            y = tsr.linear(x, w, activation="gelu")
+    g.replay()
+    assert torch.equal(y, eager.detach())
+    g.reset()
+    assert torch.equal(copy.deepcopy(w), w)
+    buffer = io.BytesIO()
+    torch.save(w, buffer)
+    buffer.seek(0)
+    assert torch.equal(torch.load(buffer, weights_only=True), w)
+    eager.sum().backward()
+
+
+def test_vectors_and_batches(tsr):
+    """One dimension, three, none of one of them."""
+    w, nw = normal(24, 40, seed=1), normal(40, seed=2)
+    x = normal(6, 5, 40, seed=3)
+    y = tsr.linear(tsr.rms_norm(x, nw), w)
+    assert y.shape == (6, 5, 24)
+    for i, j in ((0, 0), (5, 4)):
+        one = tsr.linear(tsr.rms_norm(x[i, j], nw), w)
+        assert one.shape == (24,) and float((one - y[i, j]).abs().max()) <= 2.0 ** -18 * float(y.abs().max())
+    assert tsr.linear(x[:0], w).shape == (0, 5, 24) and tsr.dropout(x[0, 0], tsr.Dropout(0.5, 1)).shape == (40,)
+    e = x[:, :0].detach().requires_grad_()
+    tsr.layer_norm(e).sum().backward()
+    assert e.grad.shape == (6, 0, 40)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    z, _ = tsr.linear_forward(x=x, weight=w, stream=s)
+    s.synchronize()
+    assert torch.equal(z, tsr.linear_forward(x, w)[0])
+
+
+@pytest.mark.parametrize("cols,shift", [(9001, 0), (9001, 1), (520, 1), (8193, 0)])
+def test_norm_gradient_in_place(tsr, cols, shift):
+    """dx replaces dy, on the paths that read dy more than once too (wide rows, matrices that start at different places)."""
+    x, dy, w = normal(70, cols, dtype=BF, seed=1), normal(70, cols + 8, dtype=BF, seed=2)[:, shift:shift + cols], normal(cols, seed=3)
+    _, stats = tsr.norm_forward(x, w)
+    want = [t.clone() for t in tsr.norm_backward(dy, x, w, stats)]
+    got = tsr.norm_backward(dy, x, w, stats, dx=dy)
+    assert got[0] is dy
+    for a, b in zip(want, got):
+        assert torch.equal(a, b)
 
 
 def test_same_bits_every_time(tsr):

@@ -127,6 +127,12 @@ def test_backward_accumulates_into_given_gradients(tsr, gw, T, I, O):
     check_backward(tsr, T, I, O, gw=gw, accumulate=True, pitched=True)
 
 
+@pytest.mark.parametrize("accumulate", [False, True])
+@pytest.mark.parametrize("T,I,O", [(100, 72, 40), (1000, 520, 264), (64, 2048, 2050), (3000, 129, 65), (9, 5461, 300)])
+def test_backward_of_fp32_layers_into_bf16_gradients(tsr, T, I, O, accumulate):
+    check_backward(tsr, T, I, O, dt=F32, gw=BF, accumulate=accumulate, pitched=accumulate)
+
+
 @pytest.mark.parametrize("wants", [(True, False), (False, True), (False, False)])
 @pytest.mark.parametrize("kind", ["none", "gelu"])
 def test_backward_leaves_out_what_is_not_wanted(tsr, wants, kind):

@@ -196,3 +196,35 @@ def test_words_of_dropout():
             x ^= x >> 16
             bits = x >> 16 if c & 1 else x & 0xFFFF
             assert got[i, c] == (bits >= int(np.floor(float(np.float32(p)) * 65536 + 0.5)))
+
+
+def test_addresses_that_are_read_in_pairs(tsr):
+    """(mu, r) and the dropout word are eight bytes each."""
+    L, M = tsr.lib(), tsr.Matrix
+    d, m, none = norm_desc(tsr), M(AT, 8), M(None, 0)
+    assert L.tsr_norm_forward(ctypes.byref(d), m, None, None, m, AT + 4, None) == 3
+    assert L.tsr_norm_backward(ctypes.byref(d), m, m, None, AT + 4, m, None, None, AT, 1 << 30, None) == 3
+    drop = tsr.DropoutDesc(0.5, 0, 0, 0, AT + 4)
+    assert L.tsr_dropout(ctypes.byref(drop), 0, 4, 8, m, none, m, None) == 1
+
+
+def test_one_row_of_the_longest_length_is_split(tsr):
+    """The kernel for few rows counts K in 32 bits; beyond its limit a product that splits K takes over, with scratch for the parts."""
+    L, M = tsr.lib(), tsr.Matrix
+    none, size = M(None, 0), ctypes.c_size_t()
+    for K, scratch in ((1 << 24, False), ((1 << 24) + 8, True), (0x7fffffff - 1023, True)):
+        d = tsr.LinearDesc(1, K, 8, 1, 0, 0, 0, 0, 0, tsr.DropoutDesc(0.0, 0, 0, 0, None))
+        io = tsr.LinearIO(M(AT, K), M(AT, K), none, none, M(AT, 8), None)
+        assert L.tsr_linear_forward_bytes(ctypes.byref(d), ctypes.byref(io), ctypes.byref(size)) == 0
+        assert (size.value > 0) == scratch
+
+
+def test_calls_by_keyword(tsr):
+    """Every argument has a name, the one that says where to run too (CPU tensors get as far as the check)."""
+    t = torch.zeros(4, 8)
+    calls = [lambda: tsr.norm_forward(x=t, weight=None), lambda: tsr.norm_backward(dy=t, x=t, weight=None, stats=t), lambda: tsr.linear_forward(x=t, weight=t),
+             lambda: tsr.linear_backward(dy=t, x=t, weight=t), lambda: tsr.dropout_forward(x=t, dropout=tsr.Dropout(0.1, 0)),
+             lambda: tsr.dropout_backward(dy=t, dropout=tsr.Dropout(0.1, 0))]
+    for call in calls:
+        with pytest.raises(ValueError, match="CUDA device"):
+            call()
