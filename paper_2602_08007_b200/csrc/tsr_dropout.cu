@@ -1,5 +1,6 @@
 // y = residual + dropout(x): one pass, bound by HBM (formulas in tsr.h; the random words in tsr_layers.cuh).  A thread takes eight
-// neighbours of a row: four words, one key of the row.  Matrices off the 16-byte grid go entry by entry, lanes side by side.
+// neighbours of a row: four words, one key of the row.  Where rows do not start on 16 bytes, the eight are those that leave y as whole vectors, whatever
+// the alignment of x and residual (then shifted into place); only the first and the last ones of a row go entry by entry.
 #include <algorithm>
 
 #include "tsr_layers.cuh"
@@ -10,14 +11,16 @@ struct DropoutArgs {
     const void *x, *res;
     void *y;
     int64_t ldx, ldr, ldy, rows;
-    int32_t cols, units;        // units per row: of eight entries (VEC), or single ones
+    int32_t cols, units;        // units of eight entries per row, the most of any row
     DropArgs drop;
 };
 
-template <typename T, bool VEC, bool RES>
+// WHOLE: all rows start on 16 bytes and are multiples of eight entries.
+template <typename T, bool WHOLE, bool RES>
 __global__ void __launch_bounds__(256)
 dropout_kernel(const DropoutArgs a)
 {
+    constexpr int A = 16 / (int)sizeof(T);
     pdl_trigger();
     pdl_wait();
     const uint32_t call_key = drop_call_key(a.drop);
@@ -25,37 +28,58 @@ dropout_kernel(const DropoutArgs a)
     const bool small = total < ((int64_t)1 << 32);
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
         const int64_t r = small ? (int64_t)((uint32_t)u / (uint32_t)a.units) : u / a.units;
-        const uint32_t c = (uint32_t)(u - r * a.units) * (VEC ? 8u : 1u);
+        T *y = (T *)a.y + r * a.ldy;
+        const int c = (int)(u - r * a.units) * 8 - (WHOLE ? 0 : (int)((uintptr_t)y / sizeof(T) % A)), n = a.cols - c;
+        if (!WHOLE && n <= 0) continue;
+        const bool full = WHOLE || (c >= 0 && n >= 8);
         const T *x = (const T *)a.x + r * a.ldx + c;
         const T *res = (const T *)a.res + r * a.ldr + c;
-        T *y = (T *)a.y + r * a.ldy + c;
+        y += c;
         const DropRow key = drop_row_key(call_key, r);
-        if (VEC) {
-            float v[8], o[8];
+        float v[8], o[8];
+        if (WHOLE) {
             load8(x, v);
             if (RES) load8(res, o);
-#pragma unroll
-            for (int j = 0; j < 8; j += 2) {
-                const uint32_t w = drop_word(key, (c + j) >> 1);
-                v[j] = drop_lo(w, v[j], a.drop);
-                v[j + 1] = drop_hi(w, v[j + 1], a.drop);
-                if (RES) { v[j] += o[j]; v[j + 1] += o[j + 1]; }
-            }
-            store8(y, v);
+        } else if (full) {
+            load8_any<false>(x, v);      // (y may be x or the residual)
+            if (RES) load8_any<false>(res, o);
         } else {
-            float v = drop_entry(key, c, load_f(x), a.drop);
-            if (RES) v += load_f(res);
-            store_f(y, v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const bool in = c + j >= 0 && j < n;
+                v[j] = in ? load_f(x + j) : 0.f;
+                if (RES) o[j] = in ? load_f(res + j) : 0.f;
+            }
+        }
+        // the words from column c on; of an odd column they begin with a word's high half
+        uint32_t w[5];
+#pragma unroll
+        for (int j = 0; j < (WHOLE ? 4 : 5); ++j) w[j] = drop_word(key, (uint32_t)((c >> 1) + j));
+        if (!WHOLE) {
+            const uint32_t odd = (uint32_t)(c & 1) * 16u;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(w[j], w[j + 1], odd);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            v[j] = drop_lo(w[j / 2], v[j], a.drop);
+            v[j + 1] = drop_hi(w[j / 2], v[j + 1], a.drop);
+            if (RES) { v[j] += o[j]; v[j + 1] += o[j + 1]; }
+        }
+        if (full) store8(y, v);
+        else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) if (c + j >= 0 && j < n) store_f(y + j, v[j]);
         }
     }
 }
 
 template <typename T>
-static cudaError_t dropout_as(const DropoutArgs &a, bool vec, int sms, cudaStream_t s)
+static cudaError_t dropout_as(const DropoutArgs &a, bool whole, int sms, cudaStream_t s)
 {
     const dim3 grid((unsigned)std::min<int64_t>((a.rows * a.units + 255) / 256, (int64_t)sms * 64));
-    if (a.res) return vec ? launch_dependent(dropout_kernel<T, true, true>, grid, dim3(256), 0, s, 1, a) : launch_dependent(dropout_kernel<T, false, true>, grid, dim3(256), 0, s, 1, a);
-    return vec ? launch_dependent(dropout_kernel<T, true, false>, grid, dim3(256), 0, s, 1, a) : launch_dependent(dropout_kernel<T, false, false>, grid, dim3(256), 0, s, 1, a);
+    if (a.res) return whole ? launch_dependent(dropout_kernel<T, true, true>, grid, dim3(256), 0, s, 1, a) : launch_dependent(dropout_kernel<T, false, true>, grid, dim3(256), 0, s, 1, a);
+    return whole ? launch_dependent(dropout_kernel<T, true, false>, grid, dim3(256), 0, s, 1, a) : launch_dependent(dropout_kernel<T, false, false>, grid, dim3(256), 0, s, 1, a);
 }
 
 }  // namespace tsr
@@ -71,7 +95,7 @@ extern "C" tsr_status tsr_dropout(const tsr_dropout_desc *desc, int32_t dtype, i
     if (!drop_args(*desc, &a.drop)) return TSR_ERR_INVALID_ARG;
     const tsr_matrix *all[3] = {&x, &residual, &y};
     const int es = type_bytes(dtype);
-    bool vec = cols % 8 == 0;
+    bool whole = cols % 8 == 0;
     for (int i = 0; i < 3; ++i) {
         const tsr_matrix &m = *all[i];
         if (!m.data) {
@@ -80,13 +104,13 @@ extern "C" tsr_status tsr_dropout(const tsr_dropout_desc *desc, int32_t dtype, i
         }
         if (!extent_ok(rows, cols, m.ld)) return TSR_ERR_SHAPE;
         if (!aligned_to(m.data, es)) return TSR_ERR_ALIGNMENT;
-        vec = vec && aligned_to(m.data, 16) && (rows <= 1 || m.ld * es % 16 == 0);
+        whole = whole && aligned_to(m.data, 16) && (rows <= 1 || m.ld * es % 16 == 0);
     }
     if (rows == 0 || cols == 0) return TSR_OK;
     const int sms = device_sms();
     if (!sms) return TSR_ERR_CUDA;
     a.x = x.data; a.ldx = x.ld; a.res = residual.data; a.ldr = residual.ld; a.y = y.data; a.ldy = y.ld;
-    a.rows = rows; a.cols = (int)cols; a.units = vec ? (int)(cols / 8) : (int)cols;
-    const cudaError_t e = dtype == TSR_BF16 ? dropout_as<bf16>(a, vec, sms, (cudaStream_t)stream) : dropout_as<float>(a, vec, sms, (cudaStream_t)stream);
+    a.rows = rows; a.cols = (int)cols; a.units = (int)((cols + (whole ? 0 : 16 / es - 1) + 7) / 8);
+    const cudaError_t e = dtype == TSR_BF16 ? dropout_as<bf16>(a, whole, sms, (cudaStream_t)stream) : dropout_as<float>(a, whole, sms, (cudaStream_t)stream);
     return e == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
 }

@@ -4,6 +4,7 @@
 #include "tsr_device.cuh"
 #include "tsr_internal.h"
 #include "tsr_pdl.cuh"
+#include "tsr_umma.cuh"
 
 namespace tsr {
 
@@ -177,6 +178,59 @@ __device__ __forceinline__ void store8(float *p, const float (&v)[8])
 {
     *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
     *(float4 *)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+}
+
+// Eight entries from an address of any alignment: the two 16-byte granules that hold them (each holds one of them at least, so neither
+// lies outside of what may be read), shifted into place.  NC: nobody writes there while the kernel runs.
+template <bool NC = true>
+__device__ __forceinline__ uint4 load16_any(const bf16 *p)
+{
+    const uint32_t m = (uint32_t)(uintptr_t)p & 15u;
+    const uint4 *base = (const uint4 *)((uintptr_t)p & ~(uintptr_t)15);
+    const uint4 a = NC ? __ldg(base) : *base;
+    if (m == 0) return a;
+    const uint4 b = NC ? __ldg(base + 1) : base[1];
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    // by one word, by two words, by half a word: selections, since code for each place (four of them, side by side on an SM) starved the warps of
+    // instructions
+    uint32_t t[7], u[5];
+#pragma unroll
+    for (int i = 0; i < 7; ++i) t[i] = m & 4u ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) u[i] = m & 8u ? t[i + 2] : t[i];
+    const uint32_t s = (m & 2u) * 8u;
+    return make_uint4(__funnelshift_r(u[0], u[1], s), __funnelshift_r(u[1], u[2], s), __funnelshift_r(u[2], u[3], s), __funnelshift_r(u[3], u[4], s));
+}
+// The same of FP32 entries: plain loads, whose address a vector of four may not fit.
+template <bool NC = true>
+__device__ __forceinline__ void load8_any(const bf16 *p, float (&v)[8]) { unpack8(load16_any<NC>(p), v); }
+template <bool NC = true>
+__device__ __forceinline__ void load8_any(const float *p, float (&v)[8])
+{
+    if (((uintptr_t)p & 15) == 0) {
+        const float4 a = NC ? __ldg((const float4 *)p) : *(const float4 *)p, b = NC ? __ldg((const float4 *)p + 1) : ((const float4 *)p)[1];
+        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = NC ? __ldg(p + i) : p[i];
+    }
+}
+// ... of which n < 8 exist; the others are zero.
+template <typename T>
+__device__ __forceinline__ void load8_part(const T *p, int n, float (&v)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < n ? load_f(p + i) : 0.f;
+}
+
+// A float in the shared memory of the cluster's CTA `rank`, at the place of `here`.
+__device__ __forceinline__ float shared_of(const float *here, int rank)
+{
+    uint32_t at;
+    float v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(here)), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    return v;
 }
 
 // ---- host helpers -----------------------------------------------------------------------------------------------------

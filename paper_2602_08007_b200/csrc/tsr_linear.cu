@@ -17,46 +17,6 @@ namespace tsr {
 
 // ---- kernels ----------------------------------------------------------------------------------------------------------
 
-// Eight entries from an address of any alignment: the two 16-byte granules that hold them (each holds one of them at least, so neither
-// lies outside of what may be read), shifted into place.
-__device__ __forceinline__ uint4 load8_any(const bf16 *p)
-{
-    const uint32_t m = (uint32_t)(uintptr_t)p & 15u;
-    const uint4 *base = (const uint4 *)((uintptr_t)p & ~(uintptr_t)15);
-    const uint4 a = __ldg(base);
-    if (m == 0) return a;
-    const uint4 b = __ldg(base + 1);
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    // by one word, by two words, by half a word: selections, since code for each place (four of them, side by side on an SM) starved the warps of
-    // instructions
-    uint32_t t[7], u[5];
-#pragma unroll
-    for (int i = 0; i < 7; ++i) t[i] = m & 4u ? w[i + 1] : w[i];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) u[i] = m & 8u ? t[i + 2] : t[i];
-    const uint32_t s = (m & 2u) * 8u;
-    return make_uint4(__funnelshift_r(u[0], u[1], s), __funnelshift_r(u[1], u[2], s), __funnelshift_r(u[2], u[3], s), __funnelshift_r(u[3], u[4], s));
-}
-// The same of FP32 entries: plain loads, whose address a vector of four may not fit.
-__device__ __forceinline__ void load8_any(const bf16 *p, float (&v)[8]) { unpack8(load8_any(p), v); }
-__device__ __forceinline__ void load8_any(const float *p, float (&v)[8])
-{
-    if (((uintptr_t)p & 15) == 0) {
-        const float4 a = __ldg((const float4 *)p), b = __ldg((const float4 *)p + 1);
-        v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __ldg(p + i);
-    }
-}
-// ... of which n < 8 exist; the others are zero.
-template <typename T>
-__device__ __forceinline__ void load8_part(const T *p, int n, float (&v)[8])
-{
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < n ? load_f(p + i) : 0.f;
-}
-
 // dst[r][0 .. cols) = src[r][..]; dst has a pitch of whole 16-byte units.  A thread writes one unit of eight entries.
 __global__ void __launch_bounds__(256)
 linear_pack_kernel(const bf16 *__restrict__ src, int64_t lds, bf16 *__restrict__ dst, int64_t ldd, int64_t rows, int cols, int units)
@@ -70,7 +30,7 @@ linear_pack_kernel(const bf16 *__restrict__ src, int64_t lds, bf16 *__restrict__
         const int c = (int)(u - r * units) * 8;
         const bf16 *s = src + r * lds + c;
         bf16 *d = dst + r * ldd + c;
-        if (c + 8 <= cols) *(uint4 *)d = load8_any(s);
+        if (c + 8 <= cols) *(uint4 *)d = load16_any(s);
         else {
             for (int i = 0; i < cols - c; ++i) d[i] = s[i];
         }
@@ -279,19 +239,21 @@ static cudaError_t few_launch(const FewArgs &a, cudaStream_t s)
     return launch_dependent(linear_few_kernel<T, FEW_ROWS>, grid, dim3(256), 0, s, 1, a);
 }
 
-// dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row.  dy and pre
+// dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row; a cluster (along z)
+// adds its CTAs' sums before they leave (586 partial rows of 512 columns took column_finish_kernel 7.5 us, an eighth of them ZZZ).  dy and pre
 // may lie at any alignment, dz has a pitch of whole 16-byte units.  dz NULL: the sums alone.
 // The grid is what is resident at once (a third more left SMs idle for 40 % of the time), and what hides the loads is the number of warps: unrolled
 // loops were slower, the more so the further (8192 x 5461 with SiLU off the 16-byte grid: 72 us, unrolled twice 95, four times 131 at three CTAs).
 constexpr int DZ_CTAS = 4;     // on an SM
+constexpr int DZ_CLUSTER = 8;
 struct DzArgs {
     const void *dy, *pre;
     void *dz;                  // BF16, or (FP32) three BF16 planes `plane` entries apart
-    float *partial;            // [gridDim.y][cols], NULL: no sums, or they go to `sums`
+    float *partial;            // [clusters][cols], NULL: no sums, or they go to `sums`
     void *sums;                // with a single range of rows: the sums themselves
     int32_t sums_bf16, accumulate;
     int64_t lddy, ldpre, lddz, plane, rows;
-    int32_t cols, rows_per;
+    int32_t cols, rows_per, cluster;     // cluster: CTAs that add their sums; divides gridDim.z
     DropArgs drop;
 };
 template <typename T, int ACT>
@@ -303,7 +265,7 @@ linear_dz_kernel(const DzArgs a)
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c0 = blockIdx.x * 256 + lane * 8, n = a.cols - c0;
-    const int64_t r0 = (int64_t)blockIdx.y * a.rows_per + warp, r1 = min(a.rows, (int64_t)(blockIdx.y + 1) * a.rows_per);
+    const int64_t r0 = (int64_t)blockIdx.z * a.rows_per + warp, r1 = min(a.rows, (int64_t)(blockIdx.z + 1) * a.rows_per);
     const uint32_t call_key = a.drop.threshold ? drop_call_key(a.drop) : 0u;
     float acc[8];
 #pragma unroll
@@ -350,25 +312,31 @@ linear_dz_kernel(const DzArgs a)
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[warp][lane * 8 + j] = acc[j];
     __syncthreads();
-    const int c = blockIdx.x * 256 + threadIdx.x;
-    if (c < a.cols) {
-        float s = 0.f;
+    const int c = blockIdx.x * 256 + threadIdx.x, rank = blockIdx.z % a.cluster;
+    float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
-        if (a.partial) a.partial[(int64_t)blockIdx.y * a.cols + c] = s;
-        else store_as(a.sums, c, a.sums_bf16, a.accumulate ? s + load_as(a.sums, c, a.sums_bf16) : s);
+    for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
+    if (a.cluster > 1) {
+        sums[0][threadIdx.x] = s;      // (read by this thread alone so far)
+        cluster_sync();
+        if (rank == 0)
+            for (int k = 1; k < a.cluster; ++k) s += shared_of(&sums[0][threadIdx.x], k);
+        cluster_sync();      // no CTA leaves while its sums are read
     }
+    if (rank || c >= a.cols) return;
+    if (a.partial) a.partial[(int64_t)(blockIdx.z / a.cluster) * a.cols + c] = s;
+    else store_as(a.sums, c, a.sums_bf16, a.accumulate ? s + load_as(a.sums, c, a.sums_bf16) : s);
 }
 
 template <typename T>
 static cudaError_t dz_launch(const DzArgs &a, int act, dim3 grid, cudaStream_t s)
 {
     switch (act) {
-    case TSR_ACT_RELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_RELU>, grid, dim3(256), 0, s, 1, a);
-    case TSR_ACT_GELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU>, grid, dim3(256), 0, s, 1, a);
-    case TSR_ACT_GELU_TANH: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU_TANH>, grid, dim3(256), 0, s, 1, a);
-    case TSR_ACT_SILU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_SILU>, grid, dim3(256), 0, s, 1, a);
-    default: return launch_dependent(linear_dz_kernel<T, TSR_ACT_NONE>, grid, dim3(256), 0, s, 1, a);
+    case TSR_ACT_RELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_RELU>, grid, dim3(256), 0, s, a.cluster, a);
+    case TSR_ACT_GELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU>, grid, dim3(256), 0, s, a.cluster, a);
+    case TSR_ACT_GELU_TANH: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU_TANH>, grid, dim3(256), 0, s, a.cluster, a);
+    case TSR_ACT_SILU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_SILU>, grid, dim3(256), 0, s, a.cluster, a);
+    default: return launch_dependent(linear_dz_kernel<T, TSR_ACT_NONE>, grid, dim3(256), 0, s, a.cluster, a);
     }
 }
 
@@ -756,7 +724,9 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
     const int64_t col_blocks = (O + DZ_COLS - 1) / DZ_COLS;
     const int64_t most = col_blocks ? std::max<int64_t>(1, T <= 64 ? 1 : std::min<int64_t>((T + 31) / 32, DZ_CTAS * sms / col_blocks)) : 1;
     const int64_t rows_per = T ? round_up((T + most - 1) / most, 8) : 8;
-    const int64_t parts = std::max<int64_t>(1, (T + rows_per - 1) / rows_per);
+    const int64_t ranges = std::max<int64_t>(1, (T + rows_per - 1) / rows_per);
+    const int cluster = db ? (int)std::min<int64_t>(DZ_CLUSTER, ranges) : 1;
+    const int64_t parts = (ranges + cluster - 1) / cluster;      // (the last cluster's last CTAs may have no rows)
 
     tsr_matrix dz = io->dy;
     Product px = {}, pw = {};
@@ -785,7 +755,8 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             if (direct) { a.sums = io->dbias; a.sums_bf16 = d->gb_dtype == TSR_BF16; a.accumulate = d->accumulate; }
             a.rows = T; a.cols = (int)O; a.rows_per = (int)rows_per;
             a.drop = drop;
-            const dim3 grid((unsigned)col_blocks, (unsigned)parts);
+            a.cluster = cluster;
+            const dim3 grid((unsigned)col_blocks, 1, (unsigned)(parts * cluster));
             const cudaError_t rc = f32 ? dz_launch<float>(a, d->activation, grid, stream) : dz_launch<bf16>(a, d->activation, grid, stream);
             if (rc != cudaSuccess) return TSR_ERR_CUDA;
         }
