@@ -223,13 +223,13 @@ __device__ __forceinline__ void load8_part(const T *p, int n, float (&v)[8])
     for (int i = 0; i < 8; ++i) v[i] = i < n ? load_f(p + i) : 0.f;
 }
 
-// A float in the shared memory of the cluster's CTA `rank`, at the place of `here`.
+// A float in the shared memory of the cluster's CTA `rank`, at the place of `here` (between cluster barriers, which order it).
 __device__ __forceinline__ float shared_of(const float *here, int rank)
 {
     uint32_t at;
     float v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(here)), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at) : "memory");
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(at));
     return v;
 }
 

@@ -49,6 +49,7 @@ struct NormArgs {
     int32_t g_bf16, accumulate;
     int64_t ldx, lddy, ldy, rows;
     int32_t cols, p_bf16, center, want_dw, want_db;
+    int32_t team;                   // warps of a row
     int32_t period;                 // classes of rows that start at the same place in a unit; 0: the matrices differ in that
     float eps, inv_n;
 };
@@ -100,21 +101,46 @@ __device__ __forceinline__ void note_gave_up(bool gave_up)
     __nanosleep(2000000);      // let copies in flight land before the CTA goes away
 }
 
-// Unit j of a row in shared memory; EDGE: the places that hold no entry are `fill`.
-template <typename T, bool EDGE>
-__device__ __forceinline__ uint4 take_unit(const uint4 *row, int j, int col, int cols, T fill)
+// Where the entries of a row lie in its first and its last unit: bits that are set for them, kept in shared memory.  Only the units u = 0 and u = last of a
+// lane can be those, so that all others of a row are taken and stored without a look.
+struct Edges { uint4 first, last; };
+template <typename T>
+__device__ __forceinline__ uint4 unit_mask(int col, int cols)
 {
     constexpr int V = Unit<T>::V;
-    uint4 r = row[j];
-    if (EDGE && (col < 0 || col + V > cols)) {
-        T t[V];
-        memcpy(t, &r, 16);
+    uint32_t m[4];
 #pragma unroll
-        for (int i = 0; i < V; ++i) if (col + i < 0 || col + i >= cols) t[i] = fill;
-        memcpy(&r, t, 16);
+    for (int i = 0; i < 4; ++i) {
+        if (V == 4) m[i] = col + i >= 0 && col + i < cols ? 0xffffffffu : 0u;
+        else m[i] = (col + 2 * i >= 0 && col + 2 * i < cols ? 0xffffu : 0u) | (col + 2 * i + 1 >= 0 && col + 2 * i + 1 < cols ? 0xffff0000u : 0u);
     }
-    return r;
+    return make_uint4(m[0], m[1], m[2], m[3]);
 }
+template <typename T>
+__device__ __forceinline__ void find_edges(Edges *e, const RowClass &rc, int cols)      // by one thread
+{
+    e->first = unit_mask<T>(-rc.shift, cols);
+    e->last = unit_mask<T>((rc.units - 1) * Unit<T>::V - rc.shift, cols);
+}
+// Whether unit u of the lanes may hold an edge, and the mask of this lane's unit j there.
+__device__ __forceinline__ bool at_edge(int u, int last_u) { return u == 0 || u == last_u; }
+__device__ __forceinline__ uint4 edge_mask(const Edges &e, int j, int units)
+{
+    uint4 m = make_uint4(0xffffffffu, 0xffffffffu, 0xffffffffu, 0xffffffffu);
+    if (j == 0) m = e.first;
+    if (j == units - 1) {
+        const uint4 l = e.last;
+        m = make_uint4(m.x & l.x, m.y & l.y, m.z & l.z, m.w & l.w);
+    }
+    return m;
+}
+// The places that hold no entry become `fill` (a value, or two of them in a word).
+__device__ __forceinline__ uint4 filled(const uint4 &r, const uint4 &m, uint32_t fill)
+{
+    return make_uint4((r.x & m.x) | (fill & ~m.x), (r.y & m.y) | (fill & ~m.y), (r.z & m.z) | (fill & ~m.z), (r.w & m.w) | (fill & ~m.w));
+}
+__device__ __forceinline__ uint32_t fill_word(float x) { return __float_as_uint(x); }
+__device__ __forceinline__ uint32_t fill_word(bf16 x) { return (uint32_t)__bfloat16_as_ushort(x) * 0x10001u; }
 // A unit as pairs of FP32 values, and back.
 __device__ __forceinline__ float2 bf16_pair(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)); }
 __device__ __forceinline__ void unit_pairs(const uint4 &r, float2 (&v)[4]) { v[0] = bf16_pair(r.x); v[1] = bf16_pair(r.y); v[2] = bf16_pair(r.z); v[3] = bf16_pair(r.w); }
@@ -131,13 +157,13 @@ __device__ __forceinline__ uint4 unit_of(const float2 (&v)[2])
 {
     return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
 }
-// EDGE: the places that hold no entry are left alone.
-template <typename T, bool EDGE>
-__device__ __forceinline__ void store_unit(T *row, int col, int cols, const float2 (&v)[Unit<T>::V / 2])
+// To the unit that begins with column col; with `edge` the places that hold no entry are left alone.
+template <typename T>
+__device__ __forceinline__ void store_unit(T *row, int col, int cols, bool edge, const float2 (&v)[Unit<T>::V / 2])
 {
     constexpr int V = Unit<T>::V;
     const uint4 r = unit_of(v);
-    if (!EDGE || (col >= 0 && col + V <= cols)) *(uint4 *)(row + col) = r;
+    if (!edge || (col >= 0 && col + V <= cols)) *(uint4 *)(row + col) = r;
     else {
         T t[V];
         memcpy(t, &r, 16);
@@ -162,11 +188,23 @@ template <typename T>
 __device__ __forceinline__ void share_params(const NormArgs &a, const RowClass &rc, float *w, float *b)
 {
     constexpr int V = Unit<T>::V;
-    for (int i = threadIdx.x; i < rc.units * V; i += blockDim.x) {
-        const int c = i - rc.shift, at = shared_at(i / V, i % V / 4, rc.units) + i % 4;
-        const bool in = c >= 0 && c < a.cols;
-        w[at] = in ? param(a.weight, c, a.p_bf16, 1.f) : 0.f;
-        if (b) b[at] = in ? param(a.bias, c, a.p_bf16, 0.f) : 0.f;
+    constexpr int AT_ONCE = 8;      // loads in flight: one after the other they took 9 us of a row of 5461 columns
+    for (int i0 = threadIdx.x; i0 < rc.units * V; i0 += AT_ONCE * blockDim.x) {
+        float wv[AT_ONCE], bv[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int c = i0 + k * blockDim.x - rc.shift;
+            const bool in = c >= 0 && c < a.cols;
+            wv[k] = in ? param(a.weight, c, a.p_bf16, 1.f) : 0.f;
+            bv[k] = in && b ? param(a.bias, c, a.p_bf16, 0.f) : 0.f;
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int i = i0 + k * blockDim.x, at = shared_at(i / V, i % V / 4, rc.units) + i % 4;
+            if (i >= rc.units * V) break;
+            w[at] = wv[k];
+            if (b) b[at] = bv[k];
+        }
     }
 }
 // Squares without those of `empty` places, each of which had distance `mean` from the mean.  The pivot is an entry of the row, so that what is taken
@@ -210,48 +248,55 @@ __device__ __forceinline__ float2 lanes_sum(float2 x, int lane)
     return hi ? make_float2(other, k) : make_float2(k, other);
 }
 
-// Narrow and middling rows: L lanes per row (32 / L rows side by side in a warp), U units per lane, a ring of `stages` turns per warp; warps do not wait
-// for one another.  `Rows` says which rows a group of lanes works on: of all groups of the class, the g-th takes every n-th row.
-constexpr int ROW_WARPS = 8;
-template <int L>
+// Who works on a row: L lanes of a warp (32 / L rows side by side in it), or (TEAMS) several whole warps, U units per lane.  The groups do not wait for
+// one another; each has a ring of `stages` rows.  Of all groups of a class of rows, the g-th takes every n-th row.
+constexpr int ROW_WARPS = 8;       // most warps of a CTA
+template <int L, bool TEAMS>
 struct Rows {
-    int lane, group;               // within the row; of the CTA
+    int lane, lanes, group, groups;    // within the row; of the CTA
+    int warps;                     // ... of a team
     int left, turns;               // rows of the group, and the most of a group of the warp
     int64_t row, step;
     RowClass rc;
 };
-template <typename T, int L>
-__device__ __forceinline__ Rows<L> rows_of(const NormArgs &a, int cta, int ctas)
+template <typename T, int L, bool TEAMS>
+__device__ __forceinline__ Rows<L, TEAMS> rows_of(const NormArgs &a, int cta, int ctas)
 {
-    constexpr int G = 32 / L;
-    Rows<L> r;
+    Rows<L, TEAMS> r;
     r.rc = row_class<T>(a.x, a.ldx, a.cols, a.period, cta, ctas);
-    r.lane = threadIdx.x & (L - 1);
-    r.group = threadIdx.x / L;
-    r.step = r.rc.step * ROW_WARPS * G;      // (`step` of the class is that of a CTA with one row)
+    r.warps = TEAMS ? a.team : 1;
+    r.lanes = TEAMS ? 32 * r.warps : L;
+    r.group = (int)threadIdx.x / r.lanes;
+    r.groups = (int)blockDim.x / r.lanes;
+    r.lane = (int)threadIdx.x - r.group * r.lanes;
+    r.step = r.rc.step * r.groups;           // (`step` of the class is that of a CTA with one row)
     r.row = r.rc.first + r.rc.step * r.group;
     const int64_t left = r.row < a.rows ? (a.rows - r.row + r.step - 1) / r.step : 0;
     r.left = (int)left;                      // (at most 2^40 rows among the groups of a full grid)
     r.turns = __shfl_sync(0xffffffffu, r.left, 0);      // (the first group of a warp has the most)
     return r;
 }
+// Waits for the other warps of the team (barrier 0 is the CTA's).
+__device__ __forceinline__ void team_sync(int team, int threads) { asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "r"(threads) : "memory"); }
 
-template <typename T, int L, int U, bool EDGE>
+template <typename T, int L, int U, bool EDGE, bool TEAMS>
 __global__ void __launch_bounds__(256, U > 4 ? 2 : U > 2 ? 3 : 4)
 norm_forward_kernel(const NormArgs a, int stages)
 {
-    constexpr int V = Unit<T>::V, P = V / 2, G = 32 / L;
+    constexpr int V = Unit<T>::V, P = V / 2, G = 32 / L;      // G: groups of a warp (or of a team)
     extern __shared__ float4 shared[];       // w, b, rings
     __shared__ uint64_t bars[ROW_WARPS * NORM_STAGES];
+    __shared__ Edges edges;
+    __shared__ float slots[TEAMS ? 2 : 1][ROW_WARPS];      // sums of a team's warps: of the entries and of the squares, or of the squares by turns
     pdl_trigger();
     pdl_wait();
     const int warp = threadIdx.x >> 5;
-    const Rows<L> rows = rows_of<T, L>(a, blockIdx.x, gridDim.x);
+    const Rows<L, TEAMS> rows = rows_of<T, L, TEAMS>(a, blockIdx.x, gridDim.x);
     const RowClass &rc = rows.rc;
-    const int lane = rows.lane, left = rows.left;
+    const int lane = rows.lane, left = rows.left, lanes = rows.lanes, ring_at = TEAMS ? rows.group : warp;
     float *w = (float *)shared, *b = w + rc.units * V;
-    const uint4 *ring = (const uint4 *)(b + rc.units * V) + (warp * stages * G + rows.group % G) * rc.units;
-    uint64_t *bar = bars + warp * NORM_STAGES;
+    const uint4 *ring = (const uint4 *)(b + rc.units * V) + (ring_at * stages * G + rows.group % G) * rc.units;
+    uint64_t *bar = bars + ring_at * NORM_STAGES;
     const float empty = (float)(rc.units * V - a.cols);      // places of a row's units that hold no entry
     const T *ask = (const T *)a.x + rows.row * a.ldx;
     const int64_t next_ask = rows.step * a.ldx, next_y = rows.step * a.ldy;
@@ -263,10 +308,23 @@ norm_forward_kernel(const NormArgs a, int stages)
         ask_row<T>(smem_u32(ring + stage * G * rc.units), ask, rc, smem_u32(bar + stage));
         ask += next_ask;
     };
-    if ((threadIdx.x & 31) == 0) {
+    // over the whole row, from every lane's sum
+    auto row_sum = [&](float x, float *slot) -> float {
+        x = lanes_sum<L>(x);
+        if constexpr (TEAMS) {      // (slots are written again after another barrier at the earliest)
+            if ((threadIdx.x & 31) == 0) slot[warp] = x;
+            team_sync(rows.group, lanes);
+            x = 0.f;
+            for (int i = 0; i < rows.warps; ++i) x += slot[rows.group * rows.warps + i];
+        }
+        return x;
+    };
+    if (TEAMS ? lane == 0 : (threadIdx.x & 31) == 0) {
         for (int i = 0; i < stages; ++i) mbar_init(smem_u32(bar + i), G);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (EDGE && threadIdx.x == 0) find_edges<T>(&edges, rc, a.cols);
+    const int last_u = (rc.units - 1) / lanes;
     __syncwarp();
     if (lane == 0)
         for (int i = 0; i < stages && i < rows.turns; ++i) request(i);
@@ -286,162 +344,46 @@ norm_forward_kernel(const NormArgs a, int stages)
         float2 v[U][P], sum = pair(0.f), q = pair(0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int j = u * L + lane;
-            unit_pairs(j < rc.units ? take_unit<T, EDGE>(row, j, j * V - rc.shift, a.cols, pivot) : make_uint4(0, 0, 0, 0), v[u]);
+            const int j = u * lanes + lane;
+            uint4 r = make_uint4(0, 0, 0, 0);
+            if (j < rc.units) {
+                r = row[j];
+                if (EDGE && at_edge(u, last_u)) r = filled(r, edge_mask(edges, j, rc.units), fill_word(pivot));
+            }
+            unit_pairs(r, v[u]);
         }
-        __syncwarp();
-        if (lane == 0 && turn + stages < rows.turns) request(stage);
-        if (++stage == stages) { stage = 0; phase ^= 1u; }
+        if constexpr (!TEAMS) {      // (a team: after its barrier)
+            __syncwarp();
+            if (lane == 0 && turn + stages < rows.turns) request(stage);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (u * L + lane >= rc.units) continue;
+            if (u * lanes + lane >= rc.units) continue;
             less(v[u], x0);
 #pragma unroll
             for (int i = 0; i < P; ++i) sum = add2(sum, v[u][i]);
         }
-        const float mean = a.center ? lanes_sum<L>(sum.x + sum.y) * a.inv_n : 0.f;
+        const float mean = a.center ? row_sum(sum.x + sum.y, slots[0]) * a.inv_n : 0.f;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            if (u * L + lane >= rc.units) continue;
+            if (u * lanes + lane >= rc.units) continue;
             less(v[u], mean);
 #pragma unroll
             for (int i = 0; i < P; ++i) q = fma2(v[u][i], v[u][i], q);
         }
-        const float rstd = rsqrtf(less_empty<EDGE>(lanes_sum<L>(q.x + q.y), mean, empty) * a.inv_n + a.eps);
+        const float rstd = rsqrtf(less_empty<EDGE>(row_sum(q.x + q.y, slots[TEAMS && (a.center || turn & 1) ? 1 : 0]), mean, empty) * a.inv_n + a.eps);
+        if (TEAMS && lane == 0 && turn + stages < rows.turns) request(stage);
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
         if (stats && lane == 0 && mine) *(float2 *)stats = make_float2(x0 + mean, rstd);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int j = u * L + lane;
+            const int j = u * lanes + lane;
             if (j >= rc.units || !mine) continue;
             normed(v[u], rstd, w, b, j, rc.units);
-            store_unit<T, EDGE>(y, j * V - rc.shift, a.cols, v[u]);
+            store_unit<T>(y, j * V - rc.shift, a.cols, EDGE && at_edge(u, last_u), v[u]);
         }
         y += next_y;
         if (stats) stats += 2 * rows.step;
-    }
-    note_gave_up(gave_up);
-}
-
-// Wider rows: a CTA per row, U units per thread.  Each thread forms mean and sum of squared distances of its own entries; two sets of n1 and n2
-// entries join by
-//     mean = mean1 + d n2 / (n1 + n2),   squares = squares1 + squares2 + d^2 n1 n2 / (n1 + n2),   d = mean2 - mean1
-// (T. Chan, G. Golub, R. LeVeque 1979), so that a row takes one round of exchanges and one barrier, and digits are lost to neither a large mean nor an
-// outlier.  The factors are the same for every row.
-template <typename T, int U, bool EDGE, int THREADS, int CTAS>
-__global__ void __launch_bounds__(THREADS, CTAS)
-norm_forward_row_kernel(const NormArgs a, int stages)
-{
-    constexpr int V = Unit<T>::V, P = V / 2;
-    extern __shared__ float4 shared[];       // w, b, ring
-    __shared__ uint64_t bars[NORM_STAGES];
-    __shared__ float2 slots[2][16], factors[16];
-    pdl_trigger();
-    pdl_wait();
-    const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 31, warp = tid >> 5, warps = threads >> 5;
-    const RowClass rc = row_class<T>(a.x, a.ldx, a.cols, a.period, blockIdx.x, gridDim.x);
-    float *w = (float *)shared, *b = w + rc.units * V;
-    const uint4 *ring = (const uint4 *)(b + rc.units * V);
-    int64_t left = rc.first < a.rows ? (a.rows - rc.first + rc.step - 1) / rc.step : 0;
-    const T *ask = (const T *)a.x + rc.first * a.ldx;
-    auto request = [&](int stage) {      // the next row, by one thread
-        mbar_expect_tx(smem_u32(bars + stage), (uint32_t)rc.units * 16u);
-        ask_row<T>(smem_u32(ring + stage * rc.units), ask, rc, smem_u32(bars + stage));
-        ask += rc.step * a.ldx;
-    };
-    if (tid == 0) {
-        for (int i = 0; i < stages; ++i) mbar_init(smem_u32(bars + i), 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int i = 0; i < stages && i < left; ++i) request(i);
-    }
-    share_params<T>(a, rc, w, b);
-    int own = 0, places = 0;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int j = u * threads + tid, col = j * V - rc.shift;
-        own += max(0, min(col + V, a.cols) - max(col, 0));
-        if (j < rc.units) places += V;
-    }
-    const float empty = (float)(places - own);
-    const float inv_own = own ? 1.f / (float)own : 0.f;
-    float f2[5], f12[5], count = (float)own;      // n2 / (n1 + n2) and n1 n2 / (n1 + n2) of the five exchanges within a warp
-#pragma unroll
-    for (int k = 0; k < 5; ++k) {
-        const float other = __shfl_xor_sync(0xffffffffu, count, 1 << k), both = count + other;
-        f2[k] = both > 0.f ? other / both : 0.f;
-        f12[k] = count * f2[k];
-        count = both;
-    }
-    if (lane == 0) slots[0][warp].x = count;
-    __syncthreads();
-    if (tid == 0) {
-        float before = 0.f;
-        for (int i = 0; i < warps; ++i) {
-            const float n = slots[0][i].x, both = before + n, f = both > 0.f ? n / both : 0.f;
-            factors[i] = make_float2(f, before * f);
-            before = both;
-        }
-    }
-    __syncthreads();
-    bool gave_up = false;
-    int turn = 0, stage = 0;
-    uint32_t phase = 0;
-    T *y = (T *)a.y + rc.first * a.ldy;
-    float *stats = a.stats ? a.stats + 2 * rc.first : nullptr;
-    for (; left > 0; --left, turn ^= 1) {
-        await_row(smem_u32(bars + stage), phase, gave_up);
-        const uint4 *row = ring + stage * rc.units;
-        const T pivot = a.center ? *((const T *)row + rc.shift) : T(0.f);      // also stands in the places that hold no entry
-        const float x0 = load_f(&pivot);
-        float2 v[U][P], sum = pair(0.f), q = pair(0.f);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = u * threads + tid;
-            if (j >= rc.units) continue;
-            unit_pairs(take_unit<T, EDGE>(row, j, j * V - rc.shift, a.cols, pivot), v[u]);
-            less(v[u], x0);
-#pragma unroll
-            for (int i = 0; i < P; ++i) sum = add2(sum, v[u][i]);
-        }
-        const float mine = a.center ? (sum.x + sum.y) * inv_own : 0.f;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u * threads + tid >= rc.units) continue;
-            less(v[u], mine);
-#pragma unroll
-            for (int i = 0; i < P; ++i) q = fma2(v[u][i], v[u][i], q);
-        }
-        float mean = mine, squares = less_empty<EDGE>(q.x + q.y, mine, empty);
-#pragma unroll
-        for (int k = 0; k < 5; ++k) {
-            const float d = __shfl_xor_sync(0xffffffffu, mean, 1 << k) - mean;
-            squares = fmaf(d * d, f12[k], squares + __shfl_xor_sync(0xffffffffu, squares, 1 << k));
-            mean = fmaf(d, f2[k], mean);
-        }
-        if (lane == 0) slots[turn][warp] = make_float2(mean, squares);
-        // One barrier per turn: the slots of the turn before last are written again only after the last one's, and the row has left its stage.
-        __syncthreads();
-        if (tid == 0 && left > stages) request(stage);
-        if (++stage == stages) { stage = 0; phase ^= 1u; }
-        mean = slots[turn][0].x;
-        squares = slots[turn][0].y;
-        for (int i = 1; i < warps; ++i) {
-            const float2 t = slots[turn][i], f = factors[i];
-            const float d = t.x - mean;
-            squares = fmaf(d * d, f.y, squares + t.y);
-            mean = fmaf(d, f.x, mean);
-        }
-        const float rstd = rsqrtf(squares * a.inv_n + a.eps);
-        if (stats && tid == 0) *(float2 *)stats = make_float2(x0 + mean, rstd);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = u * threads + tid;
-            if (j >= rc.units) continue;
-            less(v[u], mean - mine);
-            normed(v[u], rstd, w, b, j, rc.units);
-            store_unit<T, EDGE>(y, j * V - rc.shift, a.cols, v[u]);
-        }
-        y += rc.step * a.ldy;
-        if (stats) stats += 2 * rc.step;
     }
     note_gave_up(gave_up);
 }
@@ -496,6 +438,7 @@ __device__ __forceinline__ void add_up(const NormArgs &a, const float *sums)
         from[k] = other.shift;
         half[k] = other.units * V;
     }
+#pragma unroll 2
     for (int c = rank * blockDim.x + threadIdx.x; c < a.cols; c += cluster * blockDim.x) {
         float w = 0.f, b = 0.f;
 #pragma unroll
@@ -515,33 +458,41 @@ __device__ __forceinline__ void add_up(const NormArgs &a, const float *sums)
     if (cluster > 1) cluster_sync();      // no CTA leaves while its sums are read
 }
 
-// Rows of up to 256 units: L lanes per row, U units per lane, as in the forward pass; x and dy come through the ring.  A lane keeps its columns from
-// row to row, so that the column sums stay in registers (128 of them at U = 8 and BF16).  Weight is in registers up to two units, else in shared
-// memory.  DB: the sums of dy are wanted too.
-template <typename T, int L, int U, bool DB, bool EDGE, int CTAS>
+// Groups and rings as in the forward pass; x and dy come through the ring.  A lane keeps its columns from row to row, so that the column sums stay in
+// registers (128 of them at U = 8 and BF16: eight warps per SM, whose eight units per lane hide what little there is to wait for; two units per thread
+// in five CTAs of four warps per row took 69 us for 16384 x 2048, where half of the instructions were those of barriers and sums).  Weight is in
+// registers up to two units, else in shared memory.  DB: the sums of dy are wanted too.
+// Units of x and dy of one row in the ring; groups of four lanes, two of which are served at a time, get slots half a cycle of the banks apart.
+template <int L>
+__host__ __device__ __forceinline__ int slot_units(int units) { return 2 * units + (L == 4 ? (4 - 2 * units % 8 + 8) % 8 : 0); }
+
+template <typename T, int L, int U, bool DB, bool EDGE, bool TEAMS, int CTAS>
 __global__ void __launch_bounds__(256, CTAS)
-norm_backward_lanes_kernel(const NormArgs a, int stages)
+norm_backward_kernel(const NormArgs a, int stages)
 {
     constexpr int V = Unit<T>::V, P = V / 2, G = 32 / L;
     constexpr bool KEEP = U <= 2;
     extern __shared__ float4 shared[];       // weight (unless kept), rings; at the end the column sums
     __shared__ uint64_t bars[ROW_WARPS * NORM_STAGES];
+    __shared__ Edges edges;
+    __shared__ float2 slots[2][TEAMS ? ROW_WARPS : 1];      // sums of a team's warps
     pdl_trigger();
     pdl_wait();
     const int warp = threadIdx.x >> 5;
     const int cta = blockIdx.x * gridDim.z + blockIdx.z;
-    const Rows<L> rows = rows_of<T, L>(a, cta, gridDim.x * gridDim.z);
+    const Rows<L, TEAMS> rows = rows_of<T, L, TEAMS>(a, cta, gridDim.x * gridDim.z);
     const RowClass &rc = rows.rc;
-    const int lane = rows.lane, left = rows.left;
+    const int lane = rows.lane, left = rows.left, lanes = rows.lanes, ring_at = TEAMS ? rows.group : warp;
     float *weight = (float *)shared;
-    const uint4 *ring = (const uint4 *)(KEEP ? weight : weight + rc.units * V) + (warp * stages * G + rows.group % G) * 2 * rc.units;
-    uint64_t *bar = bars + warp * NORM_STAGES;
+    const int slot = slot_units<L>(rc.units);
+    const uint4 *ring = (const uint4 *)(KEEP ? weight : weight + rc.units * V) + (ring_at * stages * G + rows.group % G) * slot;
+    uint64_t *bar = bars + ring_at * NORM_STAGES;
     const T *ask_x = (const T *)a.x + rows.row * a.ldx, *ask_dy = (const T *)a.dy + rows.row * a.lddy;
     const int64_t next_x = rows.step * a.ldx, next_dy = rows.step * a.lddy, next_y = rows.step * a.ldy;
     int asked = 0;
     auto request = [&](int stage) {      // the next row, by the first lane of a group
         const bool any = asked++ < left;
-        const uint32_t to = smem_u32(bar + stage), bytes = (uint32_t)rc.units * 16u, at = smem_u32(ring + stage * G * 2 * rc.units);
+        const uint32_t to = smem_u32(bar + stage), bytes = (uint32_t)rc.units * 16u, at = smem_u32(ring + stage * G * slot);
         mbar_expect_tx(to, any ? 2 * bytes : 0u);
         if (!any) return;
         ask_row<T>(at, ask_x, rc, to);
@@ -549,10 +500,12 @@ norm_backward_lanes_kernel(const NormArgs a, int stages)
         ask_x += next_x;
         ask_dy += next_dy;
     };
-    if ((threadIdx.x & 31) == 0) {
+    if (TEAMS ? lane == 0 : (threadIdx.x & 31) == 0) {
         for (int i = 0; i < stages; ++i) mbar_init(smem_u32(bar + i), G);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (EDGE && threadIdx.x == 0) find_edges<T>(&edges, rc, a.cols);
+    const int last_u = (rc.units - 1) / lanes;
     __syncwarp();
     if (lane == 0)
         for (int i = 0; i < stages && i < rows.turns; ++i) request(i);
@@ -564,14 +517,12 @@ norm_backward_lanes_kernel(const NormArgs a, int stages)
             dw[u][i] = pair(0.f);
             if (DB) db[u][i] = pair(0.f);
             if (KEEP) {
-                const int c = (u * L + lane) * V - rc.shift + 2 * i;
+                const int c = (u * lanes + lane) * V - rc.shift + 2 * i;
                 kept[u][i] = make_float2(c >= 0 && c < a.cols ? param(a.weight, c, a.p_bf16, 1.f) : 0.f, c + 1 >= 0 && c + 1 < a.cols ? param(a.weight, c + 1, a.p_bf16, 1.f) : 0.f);
             }
         }
-    if (!KEEP) {
-        share_params<T>(a, rc, weight, nullptr);
-        __syncthreads();
-    }
+    if (!KEEP) share_params<T>(a, rc, weight, nullptr);
+    if (!KEEP || EDGE) __syncthreads();      // (teams keep none: their other warps see the barriers initialised)
     auto weights = [&](int u, float2 (&w)[P]) {
 #pragma unroll
         for (int i = 0; i < P; i += 2) {
@@ -579,7 +530,7 @@ norm_backward_lanes_kernel(const NormArgs a, int stages)
                 w[i] = kept[u][i];
                 w[i + 1] = kept[u][i + 1];
             } else {
-                const float4 t = *(const float4 *)(weight + shared_at(u * L + lane, i / 2, rc.units));
+                const float4 t = *(const float4 *)(weight + shared_at(u * lanes + lane, i / 2, rc.units));
                 w[i] = make_float2(t.x, t.y);
                 w[i + 1] = make_float2(t.z, t.w);
             }
@@ -596,17 +547,22 @@ norm_backward_lanes_kernel(const NormArgs a, int stages)
         stats += rows.step;
         next = turn + 1 < left ? *stats : pair(0.f);
         await_row(smem_u32(bar + stage), phase, gave_up);
-        const uint4 *row = ring + stage * G * 2 * rc.units;
+        const uint4 *row = ring + stage * G * slot;
         const bool mine = G == 1 || turn < left;
         uint4 x[U], g[U];
         float2 s1 = pair(0.f), s2 = pair(0.f);
         const float2 less_mu = pair(-st.x), r = pair(st.y);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int j = u * L + lane, col = j * V - rc.shift;
+            const int j = u * lanes + lane;
             if (j >= rc.units || !mine) continue;
-            x[u] = take_unit<T, EDGE>(row, j, col, a.cols, T(0.f));
-            g[u] = take_unit<T, EDGE>(row + rc.units, j, col, a.cols, T(0.f));
+            x[u] = row[j];
+            g[u] = row[rc.units + j];
+            if (EDGE && at_edge(u, last_u)) {
+                const uint4 m = edge_mask(edges, j, rc.units);
+                x[u] = filled(x[u], m, 0u);
+                g[u] = filled(g[u], m, 0u);
+            }
             float2 w[P], xv[P], gv[P];
             weights(u, w);
             unit_pairs(x[u], xv);
@@ -621,15 +577,21 @@ norm_backward_lanes_kernel(const NormArgs a, int stages)
                 s2 = fma2(gw, h, s2);
             }
         }
-        const float2 s = lanes_sum<L>(make_float2(s1.x + s1.y, s2.x + s2.y), lane);
-        if (lane == 0 && turn + stages < rows.turns) request(stage);      // (after the shuffles: every lane has read its units)
+        float2 s = lanes_sum<L>(make_float2(s1.x + s1.y, s2.x + s2.y), lane);
+        if constexpr (TEAMS) {      // (one barrier per turn: the slots of the turn before last are written again only after the last one's)
+            if ((threadIdx.x & 31) == 0) slots[turn & 1][warp] = s;
+            team_sync(rows.group, lanes);
+            s = pair(0.f);
+            for (int i = 0; i < rows.warps; ++i) s = add2(s, slots[turn & 1][rows.group * rows.warps + i]);
+        }
+        if (lane == 0 && turn + stages < rows.turns) request(stage);      // (after shuffles or barrier: every lane has read its units)
         if (++stage == stages) { stage = 0; phase ^= 1u; }
         if (a.y && mine) {
             // dx = r g w - r mean(g w) - (x - mu) r^2 mean(g w h)
             const float2 c1 = pair(a.center ? -s.x * a.inv_n * st.y : 0.f), c2 = pair(-s.y * a.inv_n * st.y * st.y);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int j = u * L + lane;
+                const int j = u * lanes + lane;
                 if (j >= rc.units) continue;
                 float2 w[P], xv[P], gv[P];
                 weights(u, w);
@@ -637,20 +599,20 @@ norm_backward_lanes_kernel(const NormArgs a, int stages)
                 unit_pairs(g[u], gv);
 #pragma unroll
                 for (int i = 0; i < P; ++i) gv[i] = fma2(mul2(gv[i], w[i]), r, fma2(add2(xv[i], less_mu), c2, c1));
-                store_unit<T, EDGE>(y, j * V - rc.shift, a.cols, gv);
+                store_unit<T>(y, j * V - rc.shift, a.cols, EDGE && at_edge(u, last_u), gv);
             }
         }
         y += next_y;
     }
     note_gave_up(gave_up);
     if (!a.want_dw && !DB) return;
-    // The column sums: over the groups of a warp, then (in the place of weight and rings) over the warps.
+    // The column sums: over the groups of a warp, then (in the place of weight and rings) over warps or teams.
     const int width = rc.units * V, set = DB ? 2 * width : width;
     float *sums = (float *)shared;
     __syncthreads();
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const int j = u * L + lane;
+        const int j = u * lanes + lane;
 #pragma unroll
         for (int o = L; o < 32; o <<= 1)
 #pragma unroll
@@ -658,214 +620,18 @@ norm_backward_lanes_kernel(const NormArgs a, int stages)
                 dw[u][i] = add2(dw[u][i], make_float2(__shfl_xor_sync(0xffffffffu, dw[u][i].x, o), __shfl_xor_sync(0xffffffffu, dw[u][i].y, o)));
                 if (DB) db[DB ? u : 0][i] = add2(db[DB ? u : 0][i], make_float2(__shfl_xor_sync(0xffffffffu, db[DB ? u : 0][i].x, o), __shfl_xor_sync(0xffffffffu, db[DB ? u : 0][i].y, o)));
             }
-        if (j >= rc.units || rows.group % G) continue;
-        keep_sums(sums + warp * set + j * V, dw[u]);
-        if (DB) keep_sums(sums + warp * set + width + j * V, db[DB ? u : 0]);
+        if (j >= rc.units || (!TEAMS && rows.group % G)) continue;
+        keep_sums(sums + ring_at * set + j * V, dw[u]);
+        if (DB) keep_sums(sums + ring_at * set + width + j * V, db[DB ? u : 0]);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < set; i += 256) {
+    const int sets = rows.groups / G;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < set; i += blockDim.x) {
         float t = sums[i];
 #pragma unroll
-        for (int k = 1; k < ROW_WARPS; ++k) t += sums[k * set + i];
+        for (int k = 1; k < ROW_WARPS; ++k) if (k < sets) t += sums[k * set + i];
         sums[i] = t;
-    }
-    add_up<T, DB>(a, sums);
-}
-
-// Wider rows: a CTA walks over rows of its class, R of them at a time; U units per thread, whose columns stay the same, so that weight and column sums
-// stay in registers.  x and dy come through a ring of `stages`, R rows of each in one.  Two rows at a time share one wait, one barrier, and six shuffles
-// (instead of twenty) for their four sums: what surrounds the arithmetic was half of the instructions with one.
-//
-// The sums of a warp, R pairs (s1, s2), over its lanes: with each exchange a lane keeps half of the values; lane 8 k has the k-th at last.
-template <int R>
-__device__ __forceinline__ float sums_of_warp(const float (&v)[2 * R], int lane)
-{
-    float k0, k1;
-    if constexpr (R == 2) {
-        const bool hi = lane & 16;
-        k0 = (hi ? v[2] : v[0]) + __shfl_xor_sync(0xffffffffu, hi ? v[0] : v[2], 16);
-        k1 = (hi ? v[3] : v[1]) + __shfl_xor_sync(0xffffffffu, hi ? v[1] : v[3], 16);
-    } else {
-        k0 = v[0] + __shfl_xor_sync(0xffffffffu, v[0], 16);
-        k1 = v[1] + __shfl_xor_sync(0xffffffffu, v[1], 16);
-    }
-    const bool hi = lane & 8;
-    float k = (hi ? k1 : k0) + __shfl_xor_sync(0xffffffffu, hi ? k0 : k1, 8);
-#pragma unroll
-    for (int o = 4; o; o >>= 1) k += __shfl_xor_sync(0xffffffffu, k, o);
-    return k;
-}
-template <typename T, int U, bool DB, bool EDGE, int THREADS, int CTAS>
-__global__ void __launch_bounds__(THREADS, CTAS)
-norm_backward_kernel(const NormArgs a, int stages)
-{
-    constexpr int V = Unit<T>::V, P = V / 2, R = U <= 2 ? 2 : 1;      // (rows of four units per thread fill the registers one at a time)
-    constexpr bool KEEP = U <= 2;                                     // weight in registers; otherwise in shared memory
-    extern __shared__ float4 shared[];       // weight (unless kept), ring; at the end the column sums
-    __shared__ uint64_t bars[NORM_STAGES];
-    __shared__ float4 slots[2][THREADS / 32];      // the sums of every warp, (s1, s2) of R rows
-    pdl_trigger();
-    pdl_wait();
-    const int tid = threadIdx.x, threads = blockDim.x, warp = tid >> 5, lane = tid & 31, warps = threads >> 5;
-    const int ctas = gridDim.x * gridDim.z, cta = blockIdx.x * gridDim.z + blockIdx.z;
-    const RowClass rc = row_class<T>(a.x, a.ldx, a.cols, a.period, cta, ctas);
-    float *weight = (float *)shared;
-    const uint4 *ring = (const uint4 *)(KEEP ? weight : weight + rc.units * V);      // per stage and row x, then dy
-    int64_t left = rc.first < a.rows ? (a.rows - rc.first + rc.step - 1) / rc.step : 0;
-    int64_t to_ask = left;
-    const T *ask_x = (const T *)a.x + rc.first * a.ldx, *ask_dy = (const T *)a.dy + rc.first * a.lddy;
-    auto request = [&](int stage) {      // the next rows, by one thread
-        const uint32_t bar = smem_u32(bars + stage), bytes = (uint32_t)rc.units * 16u;
-        uint32_t at = smem_u32(ring + stage * R * 2 * rc.units);
-        const int n = to_ask < R ? (int)to_ask : R;
-        mbar_expect_tx(bar, n * 2 * bytes);
-        for (int k = 0; k < n; ++k, at += 2 * bytes) {
-            ask_row<T>(at, ask_x, rc, bar);
-            ask_row<T>(at + bytes, ask_dy, rc, bar);
-            ask_x += rc.step * a.ldx;
-            ask_dy += rc.step * a.lddy;
-        }
-        to_ask -= n;
-    };
-    if (tid == 0) {
-        for (int i = 0; i < stages; ++i) mbar_init(smem_u32(bars + i), 1);
-        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int i = 0; i < stages && to_ask > 0; ++i) request(i);
-    }
-    float2 kept[KEEP ? U : 1][P], dw[U][P], db[DB ? U : 1][P];
-    if constexpr (KEEP) {
-#pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int i = 0; i < P; ++i) {
-                const int c = (u * threads + tid) * V - rc.shift + 2 * i;
-                kept[u][i] = make_float2(c >= 0 && c < a.cols ? param(a.weight, c, a.p_bf16, 1.f) : 0.f, c + 1 >= 0 && c + 1 < a.cols ? param(a.weight, c + 1, a.p_bf16, 1.f) : 0.f);
-            }
-    } else share_params<T>(a, rc, weight, nullptr);
-#pragma unroll
-    for (int u = 0; u < U; ++u)
-#pragma unroll
-        for (int i = 0; i < P; ++i) {
-            dw[u][i] = pair(0.f);
-            if (DB) db[u][i] = pair(0.f);
-        }
-    auto weights = [&](int u, float2 (&w)[P]) {
-#pragma unroll
-        for (int i = 0; i < P; i += 2) {
-            if constexpr (KEEP) {
-                w[i] = kept[u][i];
-                w[i + 1] = kept[u][i + 1];
-            } else {
-                const float4 t = *(const float4 *)(weight + shared_at(u * threads + tid, i / 2, rc.units));
-                w[i] = make_float2(t.x, t.y);
-                w[i + 1] = make_float2(t.z, t.w);
-            }
-        }
-    };
-    __syncthreads();
-    bool gave_up = false;
-    int turn = 0, stage = 0;
-    uint32_t phase = 0;
-    T *y = (T *)a.y + rc.first * a.ldy;
-    const int64_t next_y = rc.step * a.ldy;
-    const float2 *stats = (const float2 *)a.stats_in + rc.first;
-    float2 next[R];
-    auto ask_stats = [&](int64_t n) {      // of the coming rows, n of which exist
-#pragma unroll
-        for (int k = 0; k < R; ++k) next[k] = k < n ? stats[k * rc.step] : pair(0.f);
-        stats += R * rc.step;
-    };
-    ask_stats(left);
-    for (; left > 0; left -= R, turn ^= 1) {
-        float2 st[R];
-#pragma unroll
-        for (int k = 0; k < R; ++k) st[k] = next[k];
-        ask_stats(left - R);
-        await_row(smem_u32(bars + stage), phase, gave_up);
-        const uint4 *row = ring + stage * R * 2 * rc.units;
-        const bool both = left > 1;
-        uint4 x[R][U], g[R][U];
-        float2 s1[R], s2[R];
-#pragma unroll
-        for (int k = 0; k < R; ++k) s1[k] = s2[k] = pair(0.f);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int j = u * threads + tid, col = j * V - rc.shift;
-            if (j >= rc.units) continue;
-            float2 w[P];
-            weights(u, w);
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                if (k == 0 || both) {
-                    x[k][u] = take_unit<T, EDGE>(row + 2 * k * rc.units, j, col, a.cols, T(0.f));
-                    g[k][u] = take_unit<T, EDGE>(row + (2 * k + 1) * rc.units, j, col, a.cols, T(0.f));
-                } else x[k][u] = g[k][u] = make_uint4(0, 0, 0, 0);
-                float2 xv[P], gv[P];
-                unit_pairs(x[k][u], xv);
-                unit_pairs(g[k][u], gv);
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    const float2 h = mul2(add2(xv[i], pair(-st[k].x)), pair(st[k].y));
-                    dw[u][i] = fma2(gv[i], h, dw[u][i]);
-                    if (DB) db[u][i] = add2(db[u][i], gv[i]);
-                    const float2 gw = mul2(gv[i], w[i]);
-                    s1[k] = add2(s1[k], gw);
-                    s2[k] = fma2(gw, h, s2[k]);
-                }
-            }
-        }
-        float v[2 * R];
-#pragma unroll
-        for (int k = 0; k < R; ++k) {
-            v[2 * k] = s1[k].x + s1[k].y;
-            v[2 * k + 1] = s2[k].x + s2[k].y;
-        }
-        // One barrier per turn: the slots of the turn before last are written again only after the last one's, and the rows have left their stage.
-        const float mine = sums_of_warp<R>(v, lane);
-        if ((lane & 7) == 0 && (lane >> 3) < 2 * R) ((float *)&slots[turn][warp])[lane >> 3] = mine;
-        if (warps > 1) __syncthreads();
-        else __syncwarp();
-        if (tid == 0 && to_ask > 0) request(stage);
-        if (++stage == stages) { stage = 0; phase ^= 1u; }
-        if (a.y) {
-            float2 c1 = pair(0.f), c2 = pair(0.f);      // of the two rows
-            for (int i = 0; i < warps; ++i) {
-                const float4 t = slots[turn][i];
-                c1 = add2(c1, make_float2(t.x, R == 2 ? t.z : 0.f));
-                c2 = add2(c2, make_float2(t.y, R == 2 ? t.w : 0.f));
-            }
-#pragma unroll
-            for (int k = 0; k < R; ++k) {
-                if (k && !both) break;
-                // dx = r g w - r mean(g w) - (x - mu) r^2 mean(g w h)
-                const float f1 = a.center ? -(k ? c1.y : c1.x) * a.inv_n * st[k].y : 0.f, f2 = -(k ? c2.y : c2.x) * a.inv_n * st[k].y * st[k].y;
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int j = u * threads + tid;
-                    if (j >= rc.units) continue;
-                    float2 w[P], xv[P], gv[P];
-                    weights(u, w);
-                    unit_pairs(x[k][u], xv);
-                    unit_pairs(g[k][u], gv);
-#pragma unroll
-                    for (int i = 0; i < P; ++i) gv[i] = fma2(mul2(gv[i], w[i]), pair(st[k].y), fma2(add2(xv[i], pair(-st[k].x)), pair(f2), pair(f1)));
-                    store_unit<T, EDGE>(y, j * V - rc.shift, a.cols, gv);
-                }
-                y += next_y;
-            }
-        }
-    }
-    note_gave_up(gave_up);
-    if (!a.want_dw && !DB) return;
-    // Column sums of this CTA, by unit: dweight's, then dbias's, in the place of weight and ring.
-    __syncthreads();
-    float *sums = (float *)shared;
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-        const int j = u * threads + tid;
-        if (j >= rc.units) continue;
-        keep_sums(sums + j * V, dw[u]);
-        if (DB) keep_sums(sums + rc.units * V + j * V, db[DB ? u : 0]);
     }
     add_up<T, DB>(a, sums);
 }
@@ -977,6 +743,17 @@ cudaError_t launch_with(Kern kernel, dim3 grid, int threads, size_t smem, cudaSt
     return launch_dependent(kernel, grid, dim3(threads), smem, s, cluster, a, stages);
 }
 
+// Rows of more units than a warp takes: two, four or eight warps with up to eight units per lane (five or six where that is enough).
+struct Team { int warps, teams, per_lane; };
+Team team_of(int64_t units)
+{
+    Team t;
+    t.warps = units <= 512 ? 2 : units <= 1024 ? 4 : 8;
+    t.teams = ROW_WARPS / t.warps;
+    t.per_lane = units <= 160 * t.warps ? 5 : units <= 192 * t.warps ? 6 : 8;
+    return t;
+}
+
 template <typename T, bool EDGE>
 cudaError_t forward_as(const NormArgs &a, int units, int sms, cudaStream_t s)
 {
@@ -988,45 +765,48 @@ cudaError_t forward_as(const NormArgs &a, int units, int sms, cudaStream_t s)
         const dim3 grid((unsigned)shared_out(a.rows, a.period, ROW_WARPS * beside, sms * per_sm));
         const int stages = ring_stages(per_sm, params, ROW_WARPS * beside * row);
         const size_t smem = params + ROW_WARPS * beside * stages * row;
-        if (beside == 8) return launch_with(norm_forward_kernel<T, 4, 1, EDGE>, grid, 256, smem, s, a, stages);
-        if (beside == 4) return launch_with(norm_forward_kernel<T, 8, 1, EDGE>, grid, 256, smem, s, a, stages);
-        if (beside == 2) return launch_with(norm_forward_kernel<T, 16, 1, EDGE>, grid, 256, smem, s, a, stages);
-        if (u <= 1) return launch_with(norm_forward_kernel<T, 32, 1, EDGE>, grid, 256, smem, s, a, stages);
-        if (u <= 2) return launch_with(norm_forward_kernel<T, 32, 2, EDGE>, grid, 256, smem, s, a, stages);
-        if (u <= 4) return launch_with(norm_forward_kernel<T, 32, 4, EDGE>, grid, 256, smem, s, a, stages);
-        return launch_with(norm_forward_kernel<T, 32, 8, EDGE>, grid, 256, smem, s, a, stages);
+        if (beside == 8) return launch_with(norm_forward_kernel<T, 4, 1, EDGE, false>, grid, 256, smem, s, a, stages);
+        if (beside == 4) return launch_with(norm_forward_kernel<T, 8, 1, EDGE, false>, grid, 256, smem, s, a, stages);
+        if (beside == 2) return launch_with(norm_forward_kernel<T, 16, 1, EDGE, false>, grid, 256, smem, s, a, stages);
+        if (u <= 1) return launch_with(norm_forward_kernel<T, 32, 1, EDGE, false>, grid, 256, smem, s, a, stages);
+        if (u <= 2) return launch_with(norm_forward_kernel<T, 32, 2, EDGE, false>, grid, 256, smem, s, a, stages);
+        if (u <= 4) return launch_with(norm_forward_kernel<T, 32, 4, EDGE, false>, grid, 256, smem, s, a, stages);
+        return launch_with(norm_forward_kernel<T, 32, 8, EDGE, false>, grid, 256, smem, s, a, stages);
     }
     if (a.period && units <= ROW_UNITS) {
-        constexpr int U = 32 / V, CTAS = V == 8 ? 3 : 2;
-        const int threads = (int)round_up((units + U - 1) / U, 32);
-        const int per_sm = std::max(1, std::min(256 * CTAS / threads, (int)(SM_SHARED / (params + 2 * row))));
-        const dim3 grid((unsigned)shared_out(a.rows, a.period, 1, sms * per_sm));
-        const int stages = ring_stages(per_sm, params, row);
-        if constexpr (V == 8)
-            if (threads > 256) return launch_with(norm_forward_row_kernel<T, U, EDGE, 512, 1>, grid, threads, params + stages * row, s, a, stages);
-        return launch_with(norm_forward_row_kernel<T, U, EDGE, 256, CTAS>, grid, threads, params + stages * row, s, a, stages);
+        const Team t = team_of(units);
+        NormArgs b = a;
+        b.team = t.warps;
+        const int per_sm = std::max(1, std::min(2, (int)(SM_SHARED / (params + 2 * t.teams * row))));
+        const dim3 grid((unsigned)shared_out(a.rows, a.period, t.teams, sms * per_sm));
+        const int stages = ring_stages(per_sm, params, t.teams * row);
+        const size_t smem = params + t.teams * stages * row;
+        if (t.per_lane == 5) return launch_with(norm_forward_kernel<T, 32, 5, EDGE, true>, grid, 32 * t.warps * t.teams, smem, s, b, stages);
+        if (t.per_lane == 6) return launch_with(norm_forward_kernel<T, 32, 6, EDGE, true>, grid, 32 * t.warps * t.teams, smem, s, b, stages);
+        return launch_with(norm_forward_kernel<T, 32, 8, EDGE, true>, grid, 32 * t.warps * t.teams, smem, s, b, stages);
     }
     const int threads = any_threads(a.cols);
     const dim3 grid((unsigned)std::min<int64_t>(a.rows, (int64_t)sms * (2048 / threads)));
     return launch_dependent(norm_forward_wide_kernel<T>, grid, dim3(threads), 0, s, 1, a);
 }
 
-// The backward row kernels' form for rows of that many units: rows at a time in a CTA, units per thread, threads and CTAs per SM (by their registers), and
-// CTAs of a cluster: as many as fill the SMs of a GPC whatever its number of SMs.
-struct BackwardForm { int rows, per_thread, threads, per_sm, cluster; };
+// The backward row kernel's form for rows of that many units: rows at a time in a CTA, lanes per row (eight units per lane: with fewer, what a row costs
+// besides them counted for more; 32768 x 1024 in four units 75 us, ZZZ in eight), threads and CTAs per SM (by their registers), and CTAs of a cluster: as many as fill the SMs of a GPC whatever its number of SMs.
+struct BackwardForm { int rows, lanes, per_lane, threads, team, per_sm, cluster; };
 BackwardForm backward_form(int64_t units)
 {
-    BackwardForm f;
+    BackwardForm f = {1, 32, 8, 32 * ROW_WARPS, 1, 1, 0};
     if (units <= 256) {
-        f.rows = ROW_WARPS * (units <= 4 ? 8 : units <= 8 ? 4 : units <= 16 ? 2 : 1);
-        f.per_thread = units <= 32 ? 1 : units <= 64 ? 2 : units <= 128 ? 4 : 8;
-        f.threads = 32 * ROW_WARPS;
-        f.per_sm = f.per_thread == 1 ? 3 : f.per_thread < 8 ? 2 : 1;
+        f.lanes = units <= 32 ? 4 : units <= 64 ? 8 : units <= 128 ? 16 : 32;
+        f.rows = ROW_WARPS * 32 / f.lanes;
+        f.per_lane = units <= 4 ? 1 : units <= 8 ? 2 : units <= 16 ? 4 : 8;
+        f.per_sm = f.per_lane == 1 ? 3 : f.per_lane < 8 ? 2 : 1;
     } else {
-        f.per_thread = units <= 768 ? 1 : units <= 1024 ? 2 : 4;
-        f.rows = f.per_thread == 4 ? 1 : 2;
-        f.threads = (int)round_up((units + f.per_thread - 1) / f.per_thread, 32);
-        f.per_sm = units <= 384 ? 2 : 1;
+        const Team t = team_of(units);
+        f.rows = t.teams;
+        f.per_lane = t.per_lane;
+        f.team = t.warps;
+        f.threads = 32 * t.warps * t.teams;
     }
     f.cluster = f.per_sm == 1 ? 2 : f.per_sm == 2 ? 4 : 8;
     return f;
@@ -1067,23 +847,25 @@ cudaError_t backward_as(const NormArgs &a, int units, int sms, cudaStream_t s)
     const BackwardForm f = backward_form(units);
     int cluster;
     const int64_t ctas = backward_ctas(a.rows, units, a.period, sms, &cluster);
-    const size_t fixed = f.per_thread > 2 ? (size_t)units * V * 4 : 0, stage = (size_t)units * 32 * f.rows;
+    const size_t fixed = f.per_lane > 2 ? (size_t)units * V * 4 : 0, stage = (size_t)16 * f.rows * (f.lanes == 4 ? slot_units<4>(units) : 2 * units);
     const int stages = ring_stages(f.per_sm, fixed, stage);
-    // (the sums of eight warps need two stages)
-    const size_t smem = std::max(fixed + stages * stage, units <= 256 ? (size_t)units * V * (DB ? 64 : 32) : 0);
+    // (the sums at the end take up to two stages)
+    const int sets = f.team > 1 ? f.rows : ROW_WARPS;
+    const size_t smem = std::max(fixed + stages * stage, (size_t)units * V * sets * (DB ? 8 : 4));
     const dim3 grid((unsigned)(ctas / cluster), 1, cluster);
-    const auto launch = [&](auto kernel) { return launch_with(kernel, grid, f.threads, smem, s, a, stages, cluster); };
-    if (units <= 4) return launch(norm_backward_lanes_kernel<T, 4, 1, DB, EDGE, 3>);
-    if (units <= 8) return launch(norm_backward_lanes_kernel<T, 8, 1, DB, EDGE, 3>);
-    if (units <= 16) return launch(norm_backward_lanes_kernel<T, 16, 1, DB, EDGE, 3>);
-    if (units <= 32) return launch(norm_backward_lanes_kernel<T, 32, 1, DB, EDGE, 3>);
-    if (units <= 64) return launch(norm_backward_lanes_kernel<T, 32, 2, DB, EDGE, 2>);
-    if (units <= 128) return launch(norm_backward_lanes_kernel<T, 32, 4, DB, EDGE, 2>);
-    if (units <= 256) return launch(norm_backward_lanes_kernel<T, 32, 8, DB, EDGE, 1>);
-    if (units <= 384) return launch(norm_backward_kernel<T, 1, DB, EDGE, 384, 2>);
-    if (units <= 768) return launch(norm_backward_kernel<T, 1, DB, EDGE, 768, 1>);
-    if (units <= 1024) return launch(norm_backward_kernel<T, 2, DB, EDGE, 512, 1>);
-    return launch(norm_backward_kernel<T, 4, DB, EDGE, 512, 1>);
+    NormArgs b = a;
+    b.team = f.team;
+    const auto launch = [&](auto kernel) { return launch_with(kernel, grid, f.threads, smem, s, b, stages, cluster); };
+    if (units <= 4) return launch(norm_backward_kernel<T, 4, 1, DB, EDGE, false, 3>);
+    if (units <= 8) return launch(norm_backward_kernel<T, 4, 2, DB, EDGE, false, 2>);
+    if (units <= 16) return launch(norm_backward_kernel<T, 4, 4, DB, EDGE, false, 2>);
+    if (units <= 32) return launch(norm_backward_kernel<T, 4, 8, DB, EDGE, false, 1>);
+    if (units <= 64) return launch(norm_backward_kernel<T, 8, 8, DB, EDGE, false, 1>);
+    if (units <= 128) return launch(norm_backward_kernel<T, 16, 8, DB, EDGE, false, 1>);
+    if (units <= 256) return launch(norm_backward_kernel<T, 32, 8, DB, EDGE, false, 1>);
+    if (f.per_lane == 5) return launch(norm_backward_kernel<T, 32, 5, DB, EDGE, true, 1>);
+    if (f.per_lane == 6) return launch(norm_backward_kernel<T, 32, 6, DB, EDGE, true, 1>);
+    return launch(norm_backward_kernel<T, 32, 8, DB, EDGE, true, 1>);
 }
 
 template <typename T>
