@@ -239,21 +239,19 @@ static cudaError_t few_launch(const FewArgs &a, cudaStream_t s)
     return launch_dependent(linear_few_kernel<T, FEW_ROWS>, grid, dim3(256), 0, s, 1, a);
 }
 
-// dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row; a cluster (along z)
-// adds its CTAs' sums before they leave (586 partial rows of 512 columns took column_finish_kernel 7.5 us, an eighth of them ZZZ).  dy and pre
+// dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row.  dy and pre
 // may lie at any alignment, dz has a pitch of whole 16-byte units.  dz NULL: the sums alone.
 // The grid is what is resident at once (a third more left SMs idle for 40 % of the time), and what hides the loads is the number of warps: unrolled
 // loops were slower, the more so the further (8192 x 5461 with SiLU off the 16-byte grid: 72 us, unrolled twice 95, four times 131 at three CTAs).
 constexpr int DZ_CTAS = 4;     // on an SM
-constexpr int DZ_CLUSTER = 8;
 struct DzArgs {
     const void *dy, *pre;
     void *dz;                  // BF16, or (FP32) three BF16 planes `plane` entries apart
-    float *partial;            // [clusters][cols], NULL: no sums, or they go to `sums`
+    float *partial;            // [gridDim.y][cols], NULL: no sums, or they go to `sums`
     void *sums;                // with a single range of rows: the sums themselves
     int32_t sums_bf16, accumulate;
     int64_t lddy, ldpre, lddz, plane, rows;
-    int32_t cols, rows_per, cluster;     // cluster: CTAs that add their sums; divides gridDim.z
+    int32_t cols, rows_per;
     DropArgs drop;
 };
 template <typename T, int ACT>
@@ -265,7 +263,7 @@ linear_dz_kernel(const DzArgs a)
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int c0 = blockIdx.x * 256 + lane * 8, n = a.cols - c0;
-    const int64_t r0 = (int64_t)blockIdx.z * a.rows_per + warp, r1 = min(a.rows, (int64_t)(blockIdx.z + 1) * a.rows_per);
+    const int64_t r0 = (int64_t)blockIdx.y * a.rows_per + warp, r1 = min(a.rows, (int64_t)(blockIdx.y + 1) * a.rows_per);
     const uint32_t call_key = a.drop.threshold ? drop_call_key(a.drop) : 0u;
     float acc[8];
 #pragma unroll
@@ -312,50 +310,48 @@ linear_dz_kernel(const DzArgs a)
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[warp][lane * 8 + j] = acc[j];
     __syncthreads();
-    const int c = blockIdx.x * 256 + threadIdx.x, rank = blockIdx.z % a.cluster;
-    float s = 0.f;
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c < a.cols) {
+        float s = 0.f;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
-    if (a.cluster > 1) {
-        sums[0][threadIdx.x] = s;      // (read by this thread alone so far)
-        cluster_sync();
-        if (rank == 0)
-            for (int k = 1; k < a.cluster; ++k) s += shared_of(&sums[0][threadIdx.x], k);
-        cluster_sync();      // no CTA leaves while its sums are read
+        for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
+        if (a.partial) a.partial[(int64_t)blockIdx.y * a.cols + c] = s;
+        else store_as(a.sums, c, a.sums_bf16, a.accumulate ? s + load_as(a.sums, c, a.sums_bf16) : s);
     }
-    if (rank || c >= a.cols) return;
-    if (a.partial) a.partial[(int64_t)(blockIdx.z / a.cluster) * a.cols + c] = s;
-    else store_as(a.sums, c, a.sums_bf16, a.accumulate ? s + load_as(a.sums, c, a.sums_bf16) : s);
 }
 
 template <typename T>
 static cudaError_t dz_launch(const DzArgs &a, int act, dim3 grid, cudaStream_t s)
 {
     switch (act) {
-    case TSR_ACT_RELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_RELU>, grid, dim3(256), 0, s, a.cluster, a);
-    case TSR_ACT_GELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU>, grid, dim3(256), 0, s, a.cluster, a);
-    case TSR_ACT_GELU_TANH: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU_TANH>, grid, dim3(256), 0, s, a.cluster, a);
-    case TSR_ACT_SILU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_SILU>, grid, dim3(256), 0, s, a.cluster, a);
-    default: return launch_dependent(linear_dz_kernel<T, TSR_ACT_NONE>, grid, dim3(256), 0, s, a.cluster, a);
+    case TSR_ACT_RELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_RELU>, grid, dim3(256), 0, s, 1, a);
+    case TSR_ACT_GELU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU>, grid, dim3(256), 0, s, 1, a);
+    case TSR_ACT_GELU_TANH: return launch_dependent(linear_dz_kernel<T, TSR_ACT_GELU_TANH>, grid, dim3(256), 0, s, 1, a);
+    case TSR_ACT_SILU: return launch_dependent(linear_dz_kernel<T, TSR_ACT_SILU>, grid, dim3(256), 0, s, 1, a);
+    default: return launch_dependent(linear_dz_kernel<T, TSR_ACT_NONE>, grid, dim3(256), 0, s, 1, a);
     }
 }
 
-// 32 columns per CTA; warp w adds rows w, w + 32, ..., then one warp adds the 32 sums: the order depends on `parts` alone.
+// CW columns per CTA of 1024 threads: 32, or 8 where 32 would leave SMs without work.  Threads of a column add every (1024 / CW)-th row, their sums are
+// added over the lanes of a warp and then over the warps: the order depends on sizes alone.  (586 rows of 512 columns: 7.5 us with 32, XXX with 8.)
+template <int CW>
 __global__ void __launch_bounds__(1024)
 column_finish_kernel(const float *__restrict__ partial, int parts, int64_t ldp, int64_t cols, void *out, int out_bf16, void *out2, int out2_bf16, int accumulate)
 {
-    __shared__ float sums[32][33];
+    __shared__ float sums[32][CW + 1];
     pdl_trigger();
     pdl_wait();
     if (blockIdx.y) { partial += parts * ldp; out = out2; out_bf16 = out2_bf16; }
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int64_t c = (int64_t)blockIdx.x * 32 + x;
+    const int x = threadIdx.x % CW, y = threadIdx.x / CW, warp = threadIdx.x >> 5;
+    const int64_t c = (int64_t)blockIdx.x * CW + x;
     float s = 0.f;
     if (c < cols) {
 #pragma unroll 16
-        for (int p = y; p < parts; p += 32) s += partial[p * ldp + c];
+        for (int p = y; p < parts; p += 1024 / CW) s += partial[p * ldp + c];
     }
-    sums[y][x] = s;
+#pragma unroll
+    for (int o = CW; o < 32; o <<= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) < CW) sums[warp][x] = s;
     __syncthreads();
     if (y == 0 && c < cols) {
         s = 0.f;
@@ -395,8 +391,12 @@ cudaError_t column_finish(const float *partial, int parts, int64_t ldp, int64_t 
                           bool accumulate, cudaStream_t stream)
 {
     if (cols <= 0) return cudaSuccess;
-    const dim3 grid((unsigned)((cols + 31) / 32), out2 ? 2 : 1);
-    return launch_dependent(column_finish_kernel, grid, dim3(1024), 0, stream, 1, partial, parts, ldp, cols, out, (int)out_bf16, out2, (int)out2_bf16, (int)accumulate);
+    const int sets = out2 ? 2 : 1;
+    const bool narrow = (cols + 31) / 32 * sets < device_sms();
+    const auto launch = [&](auto kernel, int cw) {
+        return launch_dependent(kernel, dim3((unsigned)((cols + cw - 1) / cw), sets), dim3(1024), 0, stream, 1, partial, parts, ldp, cols, out, (int)out_bf16, out2, (int)out2_bf16, (int)accumulate);
+    };
+    return narrow ? launch(column_finish_kernel<8>, 8) : launch(column_finish_kernel<32>, 32);
 }
 
 // ---- one product ------------------------------------------------------------------------------------------------------
@@ -724,9 +724,7 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
     const int64_t col_blocks = (O + DZ_COLS - 1) / DZ_COLS;
     const int64_t most = col_blocks ? std::max<int64_t>(1, T <= 64 ? 1 : std::min<int64_t>((T + 31) / 32, DZ_CTAS * sms / col_blocks)) : 1;
     const int64_t rows_per = T ? round_up((T + most - 1) / most, 8) : 8;
-    const int64_t ranges = std::max<int64_t>(1, (T + rows_per - 1) / rows_per);
-    const int cluster = db ? (int)std::min<int64_t>(DZ_CLUSTER, ranges) : 1;
-    const int64_t parts = (ranges + cluster - 1) / cluster;      // (the last cluster's last CTAs may have no rows)
+    const int64_t parts = std::max<int64_t>(1, (T + rows_per - 1) / rows_per);
 
     tsr_matrix dz = io->dy;
     Product px = {}, pw = {};
@@ -755,8 +753,7 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             if (direct) { a.sums = io->dbias; a.sums_bf16 = d->gb_dtype == TSR_BF16; a.accumulate = d->accumulate; }
             a.rows = T; a.cols = (int)O; a.rows_per = (int)rows_per;
             a.drop = drop;
-            a.cluster = cluster;
-            const dim3 grid((unsigned)col_blocks, 1, (unsigned)(parts * cluster));
+            const dim3 grid((unsigned)col_blocks, (unsigned)parts);
             const cudaError_t rc = f32 ? dz_launch<float>(a, d->activation, grid, stream) : dz_launch<bf16>(a, d->activation, grid, stream);
             if (rc != cudaSuccess) return TSR_ERR_CUDA;
         }
