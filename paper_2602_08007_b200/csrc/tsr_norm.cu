@@ -250,7 +250,7 @@ __device__ __forceinline__ float2 lanes_sum(float2 x, int lane)
 
 // Who works on a row: L lanes of a warp (32 / L rows side by side in it), or (TEAMS) several whole warps, U units per lane.  The groups do not wait for
 // one another; each has a ring of `stages` rows.  Of all groups of a class of rows, the g-th takes every n-th row.
-constexpr int ROW_WARPS = 8;       // most warps of a CTA
+constexpr int ROW_WARPS = 8;       // warps of a CTA, and most groups of them
 template <int L, bool TEAMS>
 struct Rows {
     int lane, lanes, group, groups;    // within the row; of the CTA
@@ -466,8 +466,8 @@ __device__ __forceinline__ void add_up(const NormArgs &a, const float *sums)
 template <int L>
 __host__ __device__ __forceinline__ int slot_units(int units) { return 2 * units + (L == 4 ? (4 - 2 * units % 8 + 8) % 8 : 0); }
 
-template <typename T, int L, int U, bool DB, bool EDGE, bool TEAMS, int CTAS>
-__global__ void __launch_bounds__(256, CTAS)
+template <typename T, int L, int U, bool DB, bool EDGE, bool TEAMS, int CTAS, int WARPS = ROW_WARPS>
+__global__ void __launch_bounds__(32 * WARPS, CTAS)
 norm_backward_kernel(const NormArgs a, int stages)
 {
     constexpr int V = Unit<T>::V, P = V / 2, G = 32 / L;
@@ -475,7 +475,7 @@ norm_backward_kernel(const NormArgs a, int stages)
     extern __shared__ float4 shared[];       // weight (unless kept), rings; at the end the column sums
     __shared__ uint64_t bars[ROW_WARPS * NORM_STAGES];
     __shared__ Edges edges;
-    __shared__ float2 slots[2][TEAMS ? ROW_WARPS : 1];      // sums of a team's warps
+    __shared__ float2 slots[2][TEAMS ? WARPS : 1];      // sums of a team's warps
     pdl_trigger();
     pdl_wait();
     const int warp = threadIdx.x >> 5;
@@ -791,7 +791,7 @@ cudaError_t forward_as(const NormArgs &a, int units, int sms, cudaStream_t s)
 }
 
 // The backward row kernel's form for rows of that many units: rows at a time in a CTA, lanes per row (eight units per lane: with fewer, what a row costs
-// besides them counted for more; 32768 x 1024 in four units 75 us, ZZZ in eight), threads and CTAs per SM (by their registers), and CTAs of a cluster: as many as fill the SMs of a GPC whatever its number of SMs.
+// besides them counted for more; 32768 x 1024 in four units 75 us, in eight 40), threads and CTAs per SM (by their registers), and CTAs of a cluster: as many as fill the SMs of a GPC whatever its number of SMs.
 struct BackwardForm { int rows, lanes, per_lane, threads, team, per_sm, cluster; };
 BackwardForm backward_form(int64_t units)
 {
@@ -807,6 +807,7 @@ BackwardForm backward_form(int64_t units)
         f.per_lane = t.per_lane;
         f.team = t.warps;
         f.threads = 32 * t.warps * t.teams;
+        if (t.per_lane == 6) { f.per_lane = 3; f.team *= 2; f.threads *= 2; }      // sixteen warps fit: 6007 x 5461 without dbias 64 us as six units, 58 as three
     }
     f.cluster = f.per_sm == 1 ? 2 : f.per_sm == 2 ? 4 : 8;
     return f;
@@ -863,8 +864,8 @@ cudaError_t backward_as(const NormArgs &a, int units, int sms, cudaStream_t s)
     if (units <= 64) return launch(norm_backward_kernel<T, 8, 8, DB, EDGE, false, 1>);
     if (units <= 128) return launch(norm_backward_kernel<T, 16, 8, DB, EDGE, false, 1>);
     if (units <= 256) return launch(norm_backward_kernel<T, 32, 8, DB, EDGE, false, 1>);
+    if (f.per_lane == 3) return launch(norm_backward_kernel<T, 32, 3, DB, EDGE, true, 1, 16>);
     if (f.per_lane == 5) return launch(norm_backward_kernel<T, 32, 5, DB, EDGE, true, 1>);
-    if (f.per_lane == 6) return launch(norm_backward_kernel<T, 32, 6, DB, EDGE, true, 1>);
     return launch(norm_backward_kernel<T, 32, 8, DB, EDGE, true, 1>);
 }
 

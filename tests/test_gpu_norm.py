@@ -55,6 +55,30 @@ def test_forward_and_backward(tsr, rows, cols, dt, layout, center):
             assert torch.isnan(torch.as_strided(t, (rows, pitch - cols), (pitch, 1), shift + cols)).all()
 
 
+# every form of the row kernels (lanes per row, units per lane, teams of warps), over many turns of their rings, with groups that run out earlier than others
+MANY = [(30011, 8), (30011, 9), (30011, 31), (20011, 64), (20011, 100), (20011, 129), (20011, 257), (12011, 500), (9011, 1000), (9011, 1023), (6011, 2047), (6011, 2048),
+        (5011, 2500), (4011, 3500), (3011, 4096), (3011, 4500), (3011, 5461), (2511, 7000), (2011, 8192), (2011, 8190), (1511, 10001), (1511, 12000), (1211, 16001)]
+
+
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("rows,cols", MANY)
+def test_many_rows(tsr, rows, cols, dt):
+    x, dy, w, b = make(rows, cols, dt, 1, 2.0, 0.5), make(rows, cols, dt, 2), make(1, cols, F32, 3)[0], make(1, cols, F32, 4)[0]
+    for center in (True, False):
+        y, stats = tsr.norm_forward(x, w, b, center=center)
+        want, sy, mu, smu, rstd, srstd = lm.norm(x, w, b, 1e-5, center)
+        lm.close(y, want, sy)
+        lm.close(stats[:, :1], mu, smu)
+        lm.close(stats[:, 1:], rstd, srstd)
+        rx, rw, rb = tsr.norm_backward(dy, x, w, stats, center=center, bias=center)
+        (ex, sx), (ew, sw), (eb, sb) = lm.norm_grads(dy, x, w, stats, center)
+        lm.close(rx, ex, sx)
+        lm.close(rw, ew, sw)
+        if center:
+            lm.close(rb, eb, sb)
+    assert tsr.layer_poll_status() == tsr.TSR_OK
+
+
 @pytest.mark.parametrize("rows,cols", [(50, 96), (20, 3000), (3, 20000)])
 def test_parts_that_are_left_out(tsr, rows, cols):
     x, dy = make(rows, cols, F32, 1), make(rows, cols, F32, 2)
