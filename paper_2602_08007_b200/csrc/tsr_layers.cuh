@@ -82,6 +82,14 @@ __device__ __forceinline__ float limited(float x, float most)
     return x;
 }
 
+// ---- pairs (mul2, fma2: tsr_device.cuh) -----------------------------------------------------------------------------
+__device__ __forceinline__ float2 add2(float2 a, float2 b)
+{
+    unsigned long long d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)));
+    return *(const float2 *)&d;
+}
+
 // Normal distribution: Phi(z) and e = exp(-z^2 / 2).  The tail is t (a1 + t (a2 + ... a5 t^4)) e / 2 with t = 1 / (1 + p |z| / sqrt 2), formula 7.1.26 of
 // Abramowitz and Stegun's handbook (C. Hastings): off by 0.75e-7 at most, with two uses of the special-function units and half of the instructions
 // of erff, which bound the epilogue of a GELU layer.
@@ -93,14 +101,41 @@ __device__ __forceinline__ float normal_cdf(float z, float &e)
     return z >= 0.f ? 1.f - tail : tail;
 }
 
+// Two values at a time, for epilogues that are bound by instructions.
+template <int ACT>
+__device__ __forceinline__ float2 act_pair(float2 z)
+{
+    const auto logistic = [](float2 x) {      // 1 / (1 + 2^x)
+        float2 e;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(x.x));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(x.y));
+        e = add2(e, pair(1.f));
+        return make_float2(rcp_f(e.x), rcp_f(e.y));
+    };
+    if constexpr (ACT == TSR_ACT_RELU) return make_float2(z.x < 0.f ? 0.f : z.x, z.y < 0.f ? 0.f : z.y);      // (NaN stays)
+    else if constexpr (ACT == TSR_ACT_SILU) return mul2(z, logistic(mul2(z, pair(-1.44269504f))));
+    else if constexpr (ACT == TSR_ACT_GELU_TANH)      // (1 + tanh u) / 2 = 1 / (1 + e^(-2 u))
+        return mul2(z, logistic(mul2(z, fma2(mul2(z, z), pair(-0.102943240f), pair(-2.30220819f)))));
+    else if constexpr (ACT == TSR_ACT_GELU) {
+        // z Phi(z) = max(z, 0) - |z| tail(|z|), the tail as in normal_cdf; an infinite z above zero keeps its tail finite
+        const float2 a = make_float2(fabsf(z.x == INFINITY ? 3e38f : z.x), fabsf(z.y == INFINITY ? 3e38f : z.y));
+        float2 t = fma2(a, pair(0.23164190f), pair(1.f)), e = mul2(mul2(a, a), pair(-0.72134752f));
+        t = make_float2(rcp_f(t.x), rcp_f(t.y));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(e.x));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(e.y));
+        float2 p = fma2(t, pair(0.5307027145f), pair(-0.7265760135f));
+        p = fma2(t, p, pair(0.7107068705f));
+        p = fma2(t, p, pair(-0.142248368f));
+        p = fma2(t, p, pair(0.127414796f));
+        p = mul2(mul2(p, t), mul2(e, make_float2(-a.x, -a.y)));
+        return add2(make_float2(fmaxf(z.x, 0.f), fmaxf(z.y, 0.f)), p);
+    } else return z;
+}
 __device__ __forceinline__ float act_value(int act, float z)
 {
     switch (act) {
     case TSR_ACT_RELU: return z < 0.f ? 0.f : z;      // (NaN stays)
-    case TSR_ACT_GELU: {
-        float e;
-        return z * normal_cdf(z, e);
-    }
+    case TSR_ACT_GELU: return act_pair<TSR_ACT_GELU>(pair(z)).x;
     case TSR_ACT_GELU_TANH: return z * sigmoid_f(1.59576912f * fmaf(0.044715f * z * z, z, z));   // (1 + tanh u) / 2 = sigmoid(2 u)
     case TSR_ACT_SILU: return z * sigmoid_f(z);
     default: return z;
@@ -128,14 +163,6 @@ __device__ __forceinline__ float act_slope(int act, float z)
     }
     default: return 1.f;
     }
-}
-
-// ---- pairs (mul2, fma2: tsr_device.cuh) -----------------------------------------------------------------------------
-__device__ __forceinline__ float2 add2(float2 a, float2 b)
-{
-    unsigned long long d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(bits_of(a)), "l"(bits_of(b)));
-    return *(const float2 *)&d;
 }
 
 // ---- typed access -----------------------------------------------------------------------------------------------------

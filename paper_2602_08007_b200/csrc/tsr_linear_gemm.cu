@@ -50,9 +50,14 @@ int linear_stages(int stage_bytes, bool pre)
 template <int ACT>
 __device__ __forceinline__ void activate(float (&v)[32])
 {
-    if (ACT == TSR_ACT_NONE) return;
+    if constexpr (ACT != TSR_ACT_NONE) {
 #pragma unroll
-    for (int j = 0; j < 32; ++j) v[j] = act_value(ACT, v[j]);
+        for (int j = 0; j < 32; j += 2) {
+            const float2 z = act_pair<ACT>(make_float2(v[j], v[j + 1]));
+            v[j] = z.x;
+            v[j + 1] = z.y;
+        }
+    }
 }
 
 // A lane's row of a box: 16-byte unit u of row r lies at r * 128 + ((u ^ (r & 7)) << 4).
