@@ -242,7 +242,7 @@ static cudaError_t few_launch(const FewArgs &a, cudaStream_t s)
 // dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row.  dy and pre
 // may lie at any alignment, dz has a pitch of whole 16-byte units.  dz NULL: the sums alone.
 // The grid is what is resident at once (a third more left SMs idle for 40 % of the time), and what hides the loads is the number of warps: unrolled
-// loops were slower, the more so the further (8192 x 5461 with SiLU off the 16-byte grid: 72 us, unrolled twice 95, four times 131 at three CTAs).
+// loops were slower, the more so the further (8192 x 5461 with SiLU off the 16-byte grid: 58 us; at an earlier stage 72, unrolled twice 95, four times 131 at three CTAs).
 constexpr int DZ_CTAS = 4;     // on an SM
 struct DzArgs {
     const void *dy, *pre;

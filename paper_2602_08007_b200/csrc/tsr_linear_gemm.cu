@@ -11,8 +11,8 @@
 // FP32 operands come as three BF16 planes (x = p1 + p2 + p3, 24 bits) and D = p1 q1 + (p1 q2 + p2 q1) + (p2 q2 + p1 q3 + p3 q1): six BF16 products
 // cost the tensor cores what three TF32 products cost, keep two bits more, move three quarters of the bytes and take MN-major operands.  The
 // tensor cores cut off what falls below the accumulator's last bit, which adds up over a long K (10^-5 of the result at K = 4096); the
-// accumulator is therefore emptied every 128 entries of K into FP32 registers of the epilogue warps, added to nearest.  K blocks are 32 entries there:
-// of blocks of 64 only two stages fit, which left the tensor cores waiting for half of the time.
+// accumulator is therefore emptied every 128 entries of K into FP32 registers of the epilogue warps, added to nearest.  K blocks are 32 entries there,
+// of which three stages fit beside the boxes.
 //
 // Epilogue: a lane holds a row.  A warp's 32 rows x 128 bytes of output form a box in shared memory (128-byte swizzle: free of bank
 // conflicts when the lanes walk their rows), of which it has two, and a third for pre.  The residual is fetched into the box by TMA
@@ -22,8 +22,10 @@
 // Work items: whole tiles first, a multiple of what runs at once; the tiles of the last, partly filled wave (all of them in a small product) may be
 // split along K.  The parts store FP32 slabs, and linear_finish_kernel adds a tile's slabs in order and runs its epilogue.
 //
-// What bounds it: an SM takes in 64 bytes of operands a clock, which 256 x 256 tiles of a pair just feed (64 bytes per clock of MMA);
-// narrower tiles are bound by that intake.  The ring takes what shared memory the boxes leave: five stages of 32 KB rather than four are worth 3 to 6 %.
+// What bounds it: in the main loop the tensor cores (a K block of 256 x 256 takes a pair 493 clocks, of FP32 operands 764; 512 and 768 nominal, at the
+// 1.5 to 1.7 GHz that the power limit leaves).  An SM takes in 64 bytes of operands a clock, which 256 x 256 tiles of a pair just feed (64 bytes per
+// clock of MMA); narrower tiles are bound by that intake, and tiles with a short K by the epilogue (5003 x 768 -> 2048: 20 us, with GELU 28: two uses
+// of the special-function units per entry).  Measured: 8192^3 BF16 at 0.96 of the library's product, 8192 x 2048 -> 2048 at 1.0.  The ring takes what shared memory the boxes leave: five stages of 32 KB rather than four are worth 3 to 6 %.
 // Every mbarrier wait is bounded; on expiry the CTA notes it in the status
 // word, stops storing, waits for copies in flight, frees its tensor memory and returns.
 #include "tsr_linear.cuh"
@@ -194,101 +196,101 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
 
     // FP32: the sums of the epilogue warps (128 registers) come from the registers that loaders and MMA warp leave, 3 x 168 = 56 + 2 x 224.
     if (warp < 4) {
-    if constexpr (PLANES == 3) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
-    if (warp == 0 || warp == 2) {      // the whole warp; one lane asks
-        const uint32_t leader = elect_one();
-        int stage = 0;
-        uint32_t phase = 0;
-        bool ok = true;
-        const bool is_a = warp == 0, mn = is_a ? g.a_mn : g.b_mn;
-        const int boxes = mn ? is_a ? g.a_boxes : g.b_boxes : 1;
-        const CUtensorMap *map = is_a ? &g.tmA : &g.tmB;
-        const uint32_t base = smem_u32(smem) + (is_a ? 0u : (uint32_t)g.b_offset);
-        constexpr uint32_t GROUP = PLANES * 64 * BK * 2;      // an MN-major operand's groups of 64 columns follow one another
-        for (int t = first; ok && t < g.items; t += stride) {
-            const LinearTile tile = linear_tile(g, t, TILE_M);
-            const int row = is_a ? tile.m0 + (int)rank * UM_BM : tile.n0 + (int)rank * (tile.n_eff / CG);
-            for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
-                if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(bar_empty + stage), phase ^ 1u, budget))) { s_timeout = 1; ok = false; break; }
-                if (leader) {
-                    // the copies of both CTAs of a pair report their bytes to the leader CTA's barrier
-                    const uint32_t full = CG == 2 ? leader_addr(smem_u32(bar_full + stage)) : smem_u32(bar_full + stage);
-                    if (is_a && rank == 0) mbar_expect_tx(smem_u32(bar_full + stage), g.stage_tx);
-                    uint32_t to = base + stage * stage_bytes;
-                    int x = mn ? row : kb * BK;
-                    const int y = mn ? kb * BK : row;
-                    for (int j = 0; j < boxes; ++j, to += GROUP, x += 64) {
-                        if constexpr (PLANES == 1) {
-                            if constexpr (CG == 2) tma_load_2d_pair(to, map, full, x, y);
-                            else tma_load_2d(to, map, full, x, y);
-                        } else {      // the three planes at once
-                            if constexpr (CG == 2) tma_load_3d_pair(to, map, full, x, y);
-                            else tma_load_3d(to, map, full, x, y);
-                        }
-                    }
-                }
-                if (++stage == stages) { stage = 0; phase ^= 1u; }
-            }
-        }
-    } else if (warp == 1) {
-        if (rank == 0) {      // the whole warp; one lane issues
-            uint32_t tc = 0, phase = 0;      // tc: accumulators filled so far
-            int stage = 0;
-            bool ok = true;
+        if constexpr (PLANES == 3) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+        if (warp == 0 || warp == 2) {      // the whole warp; one lane asks
             const uint32_t leader = elect_one();
-            // Operand forms.  K-major: rows of 128 bytes, eight of them 1024 apart; MN-major: groups of 64 columns 8 KB apart.  Three planes: K-major rows
-            // of 64 bytes (64-byte swizzle, layout type 4; eight rows 512 bytes apart), MN-major groups of 64 columns x 32 rows, the three
-            // planes of a group one behind the other.
-            constexpr uint64_t K3 = ((uint64_t)1 << 16) | ((uint64_t)(512 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)4 << 61);
-            constexpr uint64_t MN3 = ((uint64_t)(3 * 4096 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
-            const uint64_t mn_form = PLANES == 3 ? MN3 : UMMA_DESC_HI_MN, k_form = PLANES == 3 ? K3 : UMMA_DESC_HI_K;
-            const uint64_t a_form = g.a_mn ? mn_form : k_form, b_form = g.b_mn ? mn_form : k_form;
-            const uint32_t a_hi = (uint32_t)(a_form >> 32), b_hi = (uint32_t)(b_form >> 32);
-            // in units of 16 bytes: from one MMA's 16 entries of K to the next, from plane to plane
-            const uint32_t a_step = (g.a_mn ? 2048u : 32u) >> 4, b_step = (g.b_mn ? 2048u : 32u) >> 4;
-            const uint32_t a_plane = (g.a_mn ? 4096u : (uint32_t)g.a_rows * 64u) >> 4, b_plane = (g.b_mn ? 4096u : (uint32_t)(g.width / CG) * 64u) >> 4;
-            const uint32_t a_first = (uint32_t)a_form + (smem_u32(smem) >> 4), b_first = (uint32_t)b_form + ((smem_u32(smem) + g.b_offset) >> 4);
-            const uint32_t stage_step = (uint32_t)stage_bytes >> 4;
-            // (M = 256 for a pair, 128 for one CTA; FP32 accumulator; BF16 operands)
-            const uint32_t form = (g.a_mn ? UMMA_IDESC_A_MN_MAJOR : 0u) | (g.b_mn ? UMMA_IDESC_B_MN_MAJOR : 0u) | (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE_M >> 4) << 24);
-            uint32_t a = a_first, b = b_first;
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            const bool is_a = warp == 0, mn = is_a ? g.a_mn : g.b_mn;
+            const int boxes = mn ? is_a ? g.a_boxes : g.b_boxes : 1;
+            const CUtensorMap *map = is_a ? &g.tmA : &g.tmB;
+            const uint32_t base = smem_u32(smem) + (is_a ? 0u : (uint32_t)g.b_offset);
+            constexpr uint32_t GROUP = PLANES * 64 * BK * 2;      // an MN-major operand's groups of 64 columns follow one another
             for (int t = first; ok && t < g.items; t += stride) {
                 const LinearTile tile = linear_tile(g, t, TILE_M);
-                const uint32_t idesc = form | ((uint32_t)(tile.n_eff >> 3) << 17);
-                for (int k0 = tile.kb0; ok && k0 < tile.kb1; ++tc) {
-                    const int k1 = tile.kb1 - k0 > CHUNK ? k0 + CHUNK : tile.kb1;
-                    const uint32_t buf = tc & 1u;
-                    if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(bar_acc_empty + buf), ((tc >> 1) & 1u) ^ 1u, budget))) { s_timeout = 1; ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t d = tmem_base + buf * ACC_COLS;
-                    uint32_t acc = 0;      // the first MMA overwrites
-                    for (int kb = k0; kb < k1; ++kb) {
-                        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(bar_full + stage), phase, budget))) { s_timeout = 1; ok = false; break; }
-                        tc_fence_after();
-#pragma unroll
-                        for (int pr = PLANES == 3 ? 0 : 5; pr < 6; ++pr)
-#pragma unroll
-                            for (int k4 = 0; k4 < BK / 16; ++k4) {
-                                mma_bf16<CG>(d, a + PAIRS[pr][0] * a_plane + k4 * a_step, a_hi, b + PAIRS[pr][1] * b_plane + k4 * b_step, b_hi, idesc, acc, leader);
-                                acc = 1;
-                            }
-                        if (leader) {
-                            if constexpr (CG == 2) tc_commit_pair(smem_u32(bar_empty + stage));
-                            else tc_commit(smem_u32(bar_empty + stage));
-                        }
-                        a += stage_step;
-                        b += stage_step;
-                        if (++stage == stages) { stage = 0; phase ^= 1u; a = a_first; b = b_first; }
-                    }
+                const int row = is_a ? tile.m0 + (int)rank * UM_BM : tile.n0 + (int)rank * (tile.n_eff / CG);
+                for (int kb = tile.kb0; kb < tile.kb1; ++kb) {
+                    if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(bar_empty + stage), phase ^ 1u, budget))) { s_timeout = 1; ok = false; break; }
                     if (leader) {
-                        if constexpr (CG == 2) tc_commit_pair(smem_u32(bar_acc_full + buf));
-                        else tc_commit(smem_u32(bar_acc_full + buf));
+                        // the copies of both CTAs of a pair report their bytes to the leader CTA's barrier
+                        const uint32_t full = CG == 2 ? leader_addr(smem_u32(bar_full + stage)) : smem_u32(bar_full + stage);
+                        if (is_a && rank == 0) mbar_expect_tx(smem_u32(bar_full + stage), g.stage_tx);
+                        uint32_t to = base + stage * stage_bytes;
+                        int x = mn ? row : kb * BK;
+                        const int y = mn ? kb * BK : row;
+                        for (int j = 0; j < boxes; ++j, to += GROUP, x += 64) {
+                            if constexpr (PLANES == 1) {
+                                if constexpr (CG == 2) tma_load_2d_pair(to, map, full, x, y);
+                                else tma_load_2d(to, map, full, x, y);
+                            } else {      // the three planes at once
+                                if constexpr (CG == 2) tma_load_3d_pair(to, map, full, x, y);
+                                else tma_load_3d(to, map, full, x, y);
+                            }
+                        }
                     }
-                    k0 = k1;
+                    if (++stage == stages) { stage = 0; phase ^= 1u; }
+                }
+            }
+        } else if (warp == 1) {
+            if (rank == 0) {      // the whole warp; one lane issues
+                uint32_t tc = 0, phase = 0;      // tc: accumulators filled so far
+                int stage = 0;
+                bool ok = true;
+                const uint32_t leader = elect_one();
+                // Operand forms.  K-major: rows of 128 bytes, eight of them 1024 apart; MN-major: groups of 64 columns 8 KB apart.  Three planes: K-major rows
+                // of 64 bytes (64-byte swizzle, layout type 4; eight rows 512 bytes apart), MN-major groups of 64 columns x 32 rows, the three
+                // planes of a group one behind the other.
+                constexpr uint64_t K3 = ((uint64_t)1 << 16) | ((uint64_t)(512 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)4 << 61);
+                constexpr uint64_t MN3 = ((uint64_t)(3 * 4096 >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) | ((uint64_t)1 << 46) | ((uint64_t)2 << 61);
+                const uint64_t mn_form = PLANES == 3 ? MN3 : UMMA_DESC_HI_MN, k_form = PLANES == 3 ? K3 : UMMA_DESC_HI_K;
+                const uint64_t a_form = g.a_mn ? mn_form : k_form, b_form = g.b_mn ? mn_form : k_form;
+                const uint32_t a_hi = (uint32_t)(a_form >> 32), b_hi = (uint32_t)(b_form >> 32);
+                // in units of 16 bytes: from one MMA's 16 entries of K to the next, from plane to plane
+                const uint32_t a_step = (g.a_mn ? 2048u : 32u) >> 4, b_step = (g.b_mn ? 2048u : 32u) >> 4;
+                const uint32_t a_plane = (g.a_mn ? 4096u : (uint32_t)g.a_rows * 64u) >> 4, b_plane = (g.b_mn ? 4096u : (uint32_t)(g.width / CG) * 64u) >> 4;
+                const uint32_t a_first = (uint32_t)a_form + (smem_u32(smem) >> 4), b_first = (uint32_t)b_form + ((smem_u32(smem) + g.b_offset) >> 4);
+                const uint32_t stage_step = (uint32_t)stage_bytes >> 4;
+                // (M = 256 for a pair, 128 for one CTA; FP32 accumulator; BF16 operands)
+                const uint32_t form = (g.a_mn ? UMMA_IDESC_A_MN_MAJOR : 0u) | (g.b_mn ? UMMA_IDESC_B_MN_MAJOR : 0u) | (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE_M >> 4) << 24);
+                uint32_t a = a_first, b = b_first;
+                for (int t = first; ok && t < g.items; t += stride) {
+                    const LinearTile tile = linear_tile(g, t, TILE_M);
+                    const uint32_t idesc = form | ((uint32_t)(tile.n_eff >> 3) << 17);
+                    for (int k0 = tile.kb0; ok && k0 < tile.kb1; ++tc) {
+                        const int k1 = tile.kb1 - k0 > CHUNK ? k0 + CHUNK : tile.kb1;
+                        const uint32_t buf = tc & 1u;
+                        if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(bar_acc_empty + buf), ((tc >> 1) & 1u) ^ 1u, budget))) { s_timeout = 1; ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t d = tmem_base + buf * ACC_COLS;
+                        uint32_t acc = 0;      // the first MMA overwrites
+                        for (int kb = k0; kb < k1; ++kb) {
+                            if (!__all_sync(0xffffffffu, mbar_wait(smem_u32(bar_full + stage), phase, budget))) { s_timeout = 1; ok = false; break; }
+                            tc_fence_after();
+    #pragma unroll
+                            for (int pr = PLANES == 3 ? 0 : 5; pr < 6; ++pr)
+    #pragma unroll
+                                for (int k4 = 0; k4 < BK / 16; ++k4) {
+                                    mma_bf16<CG>(d, a + PAIRS[pr][0] * a_plane + k4 * a_step, a_hi, b + PAIRS[pr][1] * b_plane + k4 * b_step, b_hi, idesc, acc, leader);
+                                    acc = 1;
+                                }
+                            if (leader) {
+                                if constexpr (CG == 2) tc_commit_pair(smem_u32(bar_empty + stage));
+                                else tc_commit(smem_u32(bar_empty + stage));
+                            }
+                            a += stage_step;
+                            b += stage_step;
+                            if (++stage == stages) { stage = 0; phase ^= 1u; a = a_first; b = b_first; }
+                        }
+                        if (leader) {
+                            if constexpr (CG == 2) tc_commit_pair(smem_u32(bar_acc_full + buf));
+                            else tc_commit(smem_u32(bar_acc_full + buf));
+                        }
+                        k0 = k1;
+                    }
                 }
             }
         }
-    }
     } else {
         if constexpr (PLANES == 3) asm volatile("setmaxnreg.inc.sync.aligned.u32 224;");
         // warp e reads tensor-memory lanes 32 (e % 4) .. and the boxes of even or odd position in the tile's columns

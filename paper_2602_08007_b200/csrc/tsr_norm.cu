@@ -1,12 +1,15 @@
 // Norm over rows, forward and backward (formulas in tsr.h).  Both passes are bound by HBM: forward reads x and writes y, backward reads
 // x and dy and writes dx, each once; a row stays in registers between its sums and its results.
 //
-// Forward and backward: rows up to 32 KB are worked on by a warp or a CTA, the next ones in flight.  Distances are formed from the
-// row's first entry and then from means: a large mean costs no digits, and a row of equal entries has variance zero.
-// Backward: threads keep their columns from row to row, so that the sums for dweight and dbias stay in registers; a CTA leaves one partial row each, and
-// column_finish adds them in order.
-// Wider rows, and matrices that do not start at the same place in 16 bytes, are read several times (from L2, mostly); their column sums take a
-// pass of their own.
+// Rows up to 32 KB are worked on by a group of lanes or a team of warps, the next ones in flight.  Distances are formed from the row's first
+// entry and then from means: a large mean costs no digits, and a row of equal entries has variance zero.  Backward: lanes keep their columns
+// from row to row, so that the sums for dweight and dbias stay in registers; a cluster of CTAs leaves one partial row of them, and
+// column_finish_kernel adds those in order.
+// Measured: forward 16384 x 2048 BF16 25 us (5.4 TB/s of 6.6 that a copy reaches), backward 8192 x 1024 FP32 23 us (4.3), backward without mean 6007 x
+// 5461 BF16 59 us (3.4: the rows start at eight different places, teams of eight warps wait for each other, and first and last rows of a CTA are alone).
+// Wider rows, and matrices that do not start at the same place in 16 bytes, are read several times (from L2, mostly), entry by entry; their column
+// sums take a pass of their own.  Those are bound by instructions: 6007 x 5461 from a pitch of 5464 into one of 5461 takes 159 us forward, 234 us
+// backward, against 36 and 68 with both alike.
 #include <math.h>
 #include <string.h>
 
