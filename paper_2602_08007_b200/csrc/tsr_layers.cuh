@@ -207,6 +207,19 @@ __device__ __forceinline__ void store8(float *p, const float (&v)[8])
     *(float4 *)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
 }
 
+// 16 bytes that begin m bytes (an even number) into a and reach into b: by one word, by two words, by half a word; selections, since code for each place
+// (four of them, side by side on an SM) starved the warps of instructions.
+__device__ __forceinline__ uint4 shift16(const uint4 &a, const uint4 &b, uint32_t m)
+{
+    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    uint32_t t[7], u[5];
+#pragma unroll
+    for (int i = 0; i < 7; ++i) t[i] = m & 4u ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < 5; ++i) u[i] = m & 8u ? t[i + 2] : t[i];
+    const uint32_t s = (m & 2u) * 8u;
+    return make_uint4(__funnelshift_r(u[0], u[1], s), __funnelshift_r(u[1], u[2], s), __funnelshift_r(u[2], u[3], s), __funnelshift_r(u[3], u[4], s));
+}
 // Eight entries from an address of any alignment: the two 16-byte granules that hold them (each holds one of them at least, so neither
 // lies outside of what may be read), shifted into place.  NC: nobody writes there while the kernel runs.
 template <bool NC = true>
@@ -215,18 +228,7 @@ __device__ __forceinline__ uint4 load16_any(const bf16 *p)
     const uint32_t m = (uint32_t)(uintptr_t)p & 15u;
     const uint4 *base = (const uint4 *)((uintptr_t)p & ~(uintptr_t)15);
     const uint4 a = NC ? __ldg(base) : *base;
-    if (m == 0) return a;
-    const uint4 b = NC ? __ldg(base + 1) : base[1];
-    const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    // by one word, by two words, by half a word: selections, since code for each place (four of them, side by side on an SM) starved the warps of
-    // instructions
-    uint32_t t[7], u[5];
-#pragma unroll
-    for (int i = 0; i < 7; ++i) t[i] = m & 4u ? w[i + 1] : w[i];
-#pragma unroll
-    for (int i = 0; i < 5; ++i) u[i] = m & 8u ? t[i + 2] : t[i];
-    const uint32_t s = (m & 2u) * 8u;
-    return make_uint4(__funnelshift_r(u[0], u[1], s), __funnelshift_r(u[1], u[2], s), __funnelshift_r(u[2], u[3], s), __funnelshift_r(u[3], u[4], s));
+    return m == 0 ? a : shift16(a, NC ? __ldg(base + 1) : base[1], m);
 }
 // The same of FP32 entries: plain loads, whose address a vector of four may not fit.
 template <bool NC = true>

@@ -169,74 +169,165 @@ linear_finish_kernel(const __grid_constant__ FinishArgs a)
     }
 }
 
-// Few rows (at most eight): the layer is bound by reading the weight once.  A warp per output column: lanes take eight entries of K each, at any
-// alignment, against the rows of x in shared memory (FP32, a chunk of K at a time), and join their sums; then a lane per row runs the epilogue.
-// FP32 stays in FP32 here.  One launch, nothing in the workspace.
+// Few rows (at most eight): the layer is bound by reading the weight once.  A warp takes four output columns at a time (what it reads of x counts for all
+// of them) and every n-th slice of 256 entries of K, eight per lane at any alignment, against the rows of x in shared memory (FP32, a chunk of K at a
+// time); FP32 stays in FP32 here.  Lanes, then the warps that share columns, join their sums, then a lane per entry runs the epilogue.  One launch,
+// nothing in the workspace.
 struct FewArgs {
     const void *x, *w;
     int64_t ldx, ldw;
-    int32_t M, N, K;
+    int32_t M, N, K, along_k, chunk;      // along_k: warps of a CTA that share columns; chunk: entries of K in shared memory at a time
     LinearEpilogue e;
 };
-constexpr int FEW_ROWS = 8, FEW_SHARED = 8192;      // entries of x in shared memory
-constexpr int64_t FEW_MOST_K = 1 << 24;             // beyond that K has to be split, and the kernel counts in 32 bits
-template <typename T, int ROWS>
-__global__ void __launch_bounds__(256)
-linear_few_kernel(const __grid_constant__ FewArgs a)
+constexpr int FEW_ROWS = 8, FEW_COLS = 4, FEW_SHARED = 24576;      // entries of x in shared memory: two CTAs fit an SM
+constexpr int64_t FEW_MOST_K = 1 << 24;                           // beyond that K has to be split further, and the kernel counts in 32 bits
+// N values of each lane (a power of two), summed over the lanes: with each exchange a lane keeps half of them; lane 32 / N * i has the i-th at last.
+template <int N>
+__device__ __forceinline__ float sums_over_lanes(const float (&v)[N], int lane, int step = 16)
 {
-    constexpr int CHUNK = FEW_SHARED / ROWS;
-    __shared__ __align__(16) float xs[ROWS][CHUNK];
-    pdl_trigger();
-    pdl_wait();
-    const int lane = threadIdx.x & 31, col = blockIdx.x * 8 + (threadIdx.x >> 5);
-    const T *w = (const T *)a.w + (int64_t)min(col, a.N - 1) * a.ldw;
-    float acc[ROWS];
+    if constexpr (N == 1) {
+        float x = v[0];
+        for (int o = step; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        return x;
+    } else {
+        const bool hi = lane & step;
+        float half[N / 2];
 #pragma unroll
-    for (int r = 0; r < ROWS; ++r) acc[r] = 0.f;
-    for (int k0 = 0; k0 < a.K; k0 += CHUNK) {
-        const int len = min(CHUNK, a.K - k0), padded = (len + 7) & ~7;
-        if (k0) __syncthreads();
+        for (int i = 0; i < N / 2; ++i) half[i] = (hi ? v[N / 2 + i] : v[i]) + __shfl_xor_sync(0xffffffffu, hi ? v[i] : v[N / 2 + i], step);
+        return sums_over_lanes<N / 2>(half, lane, step / 2);
+    }
+}
+// Eight entries of each of C rows from entry k on, all loads before the first use.
+template <bool ALIGNED, int C>
+__device__ __forceinline__ void load8_of(const bf16 *const (&w)[C], int k, float (&v)[C][8])
+{
+    uint4 a[C], b[C];
 #pragma unroll
-        for (int r = 0; r < ROWS; ++r)
-            for (int i = threadIdx.x; i < padded; i += 256) xs[r][i] = r < a.M && i < len ? load_f((const T *)a.x + r * a.ldx + k0 + i) : 0.f;
-        __syncthreads();
-#pragma unroll 4
-        for (int i = lane * 8; i < len; i += 256) {
-            float v[8];
-            if (i + 8 <= len) load8_any(w + k0 + i, v);
-            else load8_part(w + k0 + i, len - i, v);
+    for (int c = 0; c < C; ++c) {
+        const uintptr_t at = (uintptr_t)(w[c] + k);
+        const uint4 *base = (const uint4 *)(at & ~(uintptr_t)15);
+        a[c] = __ldg(base);
+        if (!ALIGNED) b[c] = __ldg(base + (at % 16 ? 1 : 0));
+    }
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
-                const float4 p = *(const float4 *)&xs[r][i], q = *(const float4 *)&xs[r][i + 4];
-                acc[r] = fmaf(v[0], p.x, fmaf(v[1], p.y, fmaf(v[2], p.z, fmaf(v[3], p.w, acc[r]))));
-                acc[r] = fmaf(v[4], q.x, fmaf(v[5], q.y, fmaf(v[6], q.z, fmaf(v[7], q.w, acc[r]))));
-            }
+    for (int c = 0; c < C; ++c) unpack8(ALIGNED ? a[c] : shift16(a[c], b[c], (uint32_t)(uintptr_t)(w[c] + k) & 15u), v[c]);
+}
+template <bool ALIGNED, int C>
+__device__ __forceinline__ void load8_of(const float *const (&w)[C], int k, float (&v)[C][8])
+{
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        if (ALIGNED) {
+            const float4 a = __ldg((const float4 *)(w[c] + k)), b = __ldg((const float4 *)(w[c] + k) + 1);
+            v[c][0] = a.x; v[c][1] = a.y; v[c][2] = a.z; v[c][3] = a.w; v[c][4] = b.x; v[c][5] = b.y; v[c][6] = b.z; v[c][7] = b.w;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[c][i] = __ldg(w[c] + k + i);
         }
     }
-    float z = 0.f;      // of the lane's row
-#pragma unroll
-    for (int r = 0; r < ROWS; ++r) {
-#pragma unroll
-        for (int o = 16; o; o >>= 1) acc[r] += __shfl_xor_sync(0xffffffffu, acc[r], o);
-        if (lane == r) z = acc[r];
-    }
-    if (lane >= a.M || col >= a.N) return;
-    const LinearEpilogue &e = a.e;
-    if (e.bias) z += load_as(e.bias, col, e.bias_bf16);
-    if (e.pre) store_f((T *)e.pre + lane * e.ldp + col, z);
-    z = act_value(e.act, z);
-    if (e.drop.threshold) z = drop_entry(drop_row_key(drop_call_key(e.drop), lane), (uint32_t)col, z, e.drop);
-    if (e.res) z += load_f((const T *)e.res + lane * e.ldr + col);
-    store_f((T *)e.out + lane * e.ldo + col, z);
 }
-template <typename T>
-static cudaError_t few_launch(const FewArgs &a, cudaStream_t s)
+// ALIGNED: the rows of the weight start on 16 bytes.
+template <typename T, int ROWS, bool ALIGNED>
+__global__ void __launch_bounds__(256, ROWS > 2 ? 2 : 3)
+linear_few_kernel(const __grid_constant__ FewArgs a)
 {
-    const dim3 grid((unsigned)((a.N + 7) / 8));
-    if (a.M <= 1) return launch_dependent(linear_few_kernel<T, 1>, grid, dim3(256), 0, s, 1, a);
-    if (a.M <= 2) return launch_dependent(linear_few_kernel<T, 2>, grid, dim3(256), 0, s, 1, a);
-    if (a.M <= 4) return launch_dependent(linear_few_kernel<T, 4>, grid, dim3(256), 0, s, 1, a);
-    return launch_dependent(linear_few_kernel<T, FEW_ROWS>, grid, dim3(256), 0, s, 1, a);
+    constexpr int C = FEW_COLS, VALUES = ROWS * C;
+    extern __shared__ __align__(16) float xs[];      // ROWS x chunk
+    __shared__ float parts[8][VALUES];
+    pdl_trigger();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kw = warp % a.along_k, per_cta = 8 / a.along_k * C, tiles = (a.N + per_cta - 1) / per_cta;
+    for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int col0 = tile * per_cta + warp / a.along_k * C;
+        const T *w[C];
+#pragma unroll
+        for (int c = 0; c < C; ++c) w[c] = (const T *)a.w + (int64_t)min(col0 + c, a.N - 1) * a.ldw;
+        float2 acc[ROWS][C];
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int c = 0; c < C; ++c) acc[r][c] = pair(0.f);
+        for (int k0 = 0; k0 < a.K; k0 += a.chunk) {
+            const int len = min(a.chunk, a.K - k0), padded = (len + 7) & ~7;
+            if (tile == (int)blockIdx.x || a.K > a.chunk) {      // (rows of one chunk stay)
+                __syncthreads();
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll 4
+                    for (int i = threadIdx.x; i < padded; i += 256) xs[r * a.chunk + i] = r < a.M && i < len ? load_f((const T *)a.x + r * a.ldx + k0 + i) : 0.f;
+                __syncthreads();
+            }
+#pragma unroll 2
+            for (int i = (kw * 32 + lane) * 8; i < len; i += a.along_k * 256) {
+                float v[C][8];
+                if (i + 8 <= len) load8_of<ALIGNED>(w, k0 + i, v);
+                else {
+#pragma unroll
+                    for (int c = 0; c < C; ++c) load8_part(w[c] + k0 + i, len - i, v[c]);
+                }
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const float4 p = *(const float4 *)&xs[r * a.chunk + i], q = *(const float4 *)&xs[r * a.chunk + i + 4];
+#pragma unroll
+                    for (int c = 0; c < C; ++c) {
+                        acc[r][c] = fma2(make_float2(v[c][0], v[c][1]), make_float2(p.x, p.y), acc[r][c]);
+                        acc[r][c] = fma2(make_float2(v[c][2], v[c][3]), make_float2(p.z, p.w), acc[r][c]);
+                        acc[r][c] = fma2(make_float2(v[c][4], v[c][5]), make_float2(q.x, q.y), acc[r][c]);
+                        acc[r][c] = fma2(make_float2(v[c][6], v[c][7]), make_float2(q.z, q.w), acc[r][c]);
+                    }
+                }
+            }
+        }
+        float sums[VALUES];
+#pragma unroll
+        for (int i = 0; i < VALUES; ++i) sums[i] = acc[i / C][i % C].x + acc[i / C][i % C].y;
+        float z = sums_over_lanes<VALUES>(sums, lane);
+        const int value = lane / (32 / VALUES), r = value / C, col = col0 + value % C;
+        if (a.along_k > 1) {
+            __syncthreads();      // (of the tile before, all have been read)
+            if (lane % (32 / VALUES) == 0) parts[warp][value] = z;
+            __syncthreads();
+            if (kw) continue;
+            z = 0.f;
+            for (int k = 0; k < a.along_k; ++k) z += parts[warp + k][value];
+        }
+        if (lane % (32 / VALUES) || r >= a.M || col >= a.N) continue;
+        const LinearEpilogue &e = a.e;
+        if (e.bias) z += load_as(e.bias, col, e.bias_bf16);
+        if (e.pre) store_f((T *)e.pre + r * e.ldp + col, z);
+        z = act_value(e.act, z);
+        if (e.drop.threshold) z = drop_entry(drop_row_key(drop_call_key(e.drop), r), (uint32_t)col, z, e.drop);
+        if (e.res) z += load_f((const T *)e.res + r * e.ldr + col);
+        store_f((T *)e.out + r * e.ldo + col, z);
+    }
+}
+// Rows of a matrix that start on 16 bytes.
+static bool tma_takes(const void *p, int64_t rows, int64_t ld, int es) { return aligned_to(p, 16) && (rows <= 1 || (ld * es) % 16 == 0); }
+template <typename T>
+static cudaError_t few_launch(FewArgs a, int sms, cudaStream_t s)
+{
+    // as many CTAs as SMs at least, as long as there is K to share
+    a.along_k = 1;
+    while (a.along_k < 8 && a.along_k * 256 < a.K && (int64_t)a.N * a.along_k < (int64_t)sms * 2 * 8 * FEW_COLS) a.along_k *= 2;
+    const int per_cta = 8 / a.along_k * FEW_COLS;
+    const dim3 grid((unsigned)std::min((a.N + per_cta - 1) / per_cta, sms * (a.M > 2 ? 2 : 3)));
+    const int rows = a.M <= 2 ? a.M : a.M <= 4 ? 4 : FEW_ROWS;
+    a.chunk = (int)std::min<int64_t>(FEW_SHARED / rows, round_up(a.K, 8));
+    const size_t smem = (size_t)rows * a.chunk * 4;
+    const auto launch = [&](auto kernel) {
+        const cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+        return e == cudaSuccess ? launch_dependent(kernel, grid, dim3(256), smem, s, 1, a) : e;
+    };
+    if (tma_takes(a.w, a.N, a.ldw, sizeof(T))) {
+        if (a.M <= 1) return launch(linear_few_kernel<T, 1, true>);
+        if (a.M <= 2) return launch(linear_few_kernel<T, 2, true>);
+        if (a.M <= 4) return launch(linear_few_kernel<T, 4, true>);
+        return launch(linear_few_kernel<T, FEW_ROWS, true>);
+    }
+    if (a.M <= 1) return launch(linear_few_kernel<T, 1, false>);
+    if (a.M <= 2) return launch(linear_few_kernel<T, 2, false>);
+    if (a.M <= 4) return launch(linear_few_kernel<T, 4, false>);
+    return launch(linear_few_kernel<T, FEW_ROWS, false>);
 }
 
 // dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row.  dy and pre
@@ -332,7 +423,7 @@ static cudaError_t dz_launch(const DzArgs &a, int act, dim3 grid, cudaStream_t s
     }
 }
 
-// CW columns per CTA of 1024 threads: 32, or 8 where 32 would leave SMs without work.  Threads of a column add every (1024 / CW)-th row, their sums are
+// CW columns per CTA of 1024 threads: 32, or 8 where 32 would leave half of the SMs without work.  Threads of a column add every (1024 / CW)-th row, their sums are
 // added over the lanes of a warp and then over the warps: the order depends on sizes alone.  (586 rows of 512 columns: 7.5 us with 32, 4.8 with 8.)
 template <int CW>
 __global__ void __launch_bounds__(1024)
@@ -392,7 +483,7 @@ cudaError_t column_finish(const float *partial, int parts, int64_t ldp, int64_t 
 {
     if (cols <= 0) return cudaSuccess;
     const int sets = out2 ? 2 : 1;
-    const bool narrow = (cols + 31) / 32 * sets < device_sms();
+    const bool narrow = (cols + 31) / 32 * sets <= device_sms() / 2;
     const auto launch = [&](auto kernel, int cw) {
         return launch_dependent(kernel, dim3((unsigned)((cols + cw - 1) / cw), sets), dim3(1024), 0, stream, 1, partial, parts, ldp, cols, out, (int)out_bf16, out2, (int)out2_bf16, (int)accumulate);
     };
@@ -436,7 +527,6 @@ bool encode(CUtensorMap *out, const void *base, int64_t rows, int64_t cols, int6
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool tma_takes(const void *p, int64_t rows, int64_t ld, int es) { return aligned_to(p, 16) && (rows <= 1 || (ld * es) % 16 == 0); }
 
 // [rows x K], or (mn) stored as [K x rows].  FP32 operands come as three BF16 planes, `plane` entries apart (see three_planes).
 struct Operand { const void *p; int64_t ld; bool mn; int64_t plane; };
@@ -500,6 +590,19 @@ Shape choose(const Product &p, int sms)
     Known &k = known[next++ & 7];
     k = {p.M, p.N, p.K, f32, pre, sms, search(p, sms)};
     return k.shape;
+}
+
+// Whether the kernel for few rows takes the product.  us, it / the tensor cores (which copy a weight that is not aligned, and split FP32 in three):
+//   BF16 aligned      2048 -> 2048, 1 row 4.8 / 7.9, 4 rows 7.1 / 7.9, 8 rows 10.4 / 8.0;  2048 -> 32768, 1 row 28.3 / 25.2
+//   BF16 not aligned  2047 -> 2047, 1 row 5.4 / 12.1, 8 rows 11.7 / 14.2;  5461 -> 2048, 4 rows 15.4 / 19.8, 8 rows (x does not fit) 40.9 / 19.7
+//   FP32              2048 -> 2048, 1 row 4.8 / 19.7, 8 rows 10.7 / 20.0;  5461 -> 2048, 4 rows 23.8 / 40.9, 8 rows (does not fit) 47.0 / 41.0
+bool few_rows(const Product &p)
+{
+    if (p.M <= 0 || p.M > FEW_ROWS || p.N <= 0 || p.K <= 0 || p.K > FEW_MOST_K) return false;
+    const bool fits = (p.M <= 2 ? p.M : p.M <= 4 ? 4 : FEW_ROWS) * p.K <= FEW_SHARED;
+    if (p.f32) return fits || p.M <= 4;
+    if (!tma_takes(p.B.p, p.N, p.B.ld, 2)) return fits;
+    return fits && p.M <= 4 && (double)p.M * p.N * p.K <= 33554432.0;
 }
 
 struct Room {      // walks the workspace; with base NULL it only counts
@@ -672,13 +775,13 @@ tsr_status forward(const tsr_linear_desc *d, const tsr_linear_io *io, void *work
     p.e.act = d->activation;
     const int sms = device_sms();
     const auto all = [&](Room &room, bool run, int n) -> tsr_status {
-        if (p.M > 0 && p.M <= FEW_ROWS && p.N > 0 && p.K > 0 && p.K <= FEW_MOST_K) {
+        if (few_rows(p)) {
             if (!run) return TSR_OK;
             FewArgs a = {};
             a.x = io->x.data; a.ldx = io->x.ld; a.w = io->weight.data; a.ldw = io->weight.ld;
             a.M = (int)p.M; a.N = (int)p.N; a.K = (int)p.K;
             a.e = p.e;
-            return (p.f32 ? few_launch<float>(a, stream) : few_launch<bf16>(a, stream)) == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
+            return (p.f32 ? few_launch<float>(a, n, stream) : few_launch<bf16>(a, n, stream)) == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
         }
         if (p.f32 && p.M > 0 && p.N > 0 && p.K > 0) {
             tsr_status e = three_planes(io->x, d->rows, d->ins, false, &p.A, room, run, n, stream);

@@ -64,6 +64,14 @@ def test_forward_epilogue(tsr, dt, kind, T, I, O, pitched):
     check_forward(tsr, T, I, O, dt=dt, kind=kind, p=0.3, residual=True, pitched=pitched, bias_type=BF)
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("pitched", [False, True])
+@pytest.mark.parametrize("T", [1, 2, 3, 4, 5, 8])
+@pytest.mark.parametrize("I,O", [(1, 1), (7, 33), (250, 100), (2048, 2050), (2047, 512), (5461, 77), (6144, 31), (30001, 9), (64, 20011)])
+def test_forward_few_rows(tsr, T, I, O, pitched, dt):
+    check_forward(tsr, T, I, O, dt=dt, kind="silu", p=0.2, residual=True, pitched=pitched)
+
+
 @pytest.mark.parametrize("residual", [False, True])
 @pytest.mark.parametrize("bias", [False, True])
 @pytest.mark.parametrize("p", [0.0, 0.1, 1.0])

@@ -213,7 +213,7 @@ def test_one_row_of_the_longest_length_is_split(tsr):
     L, M = tsr.lib(), tsr.Matrix
     none, size = M(None, 0), ctypes.c_size_t()
     for K, scratch in ((1 << 24, False), ((1 << 24) + 8, True), (0x7fffffff - 1023, True)):
-        d = tsr.LinearDesc(1, K, 8, 1, 0, 0, 0, 0, 0, tsr.DropoutDesc(0.0, 0, 0, 0, None))
+        d = tsr.LinearDesc(1, K, 8, 0, 0, 0, 0, 0, 0, tsr.DropoutDesc(0.0, 0, 0, 0, None))
         io = tsr.LinearIO(M(AT, K), M(AT, K), none, none, M(AT, 8), None)
         assert L.tsr_linear_forward_bytes(ctypes.byref(d), ctypes.byref(io), ctypes.byref(size)) == 0
         assert (size.value > 0) == scratch
