@@ -161,6 +161,11 @@ def _scratch(size: int, device: torch.device):
     return t, (t.data_ptr() + 255) // 256 * 256
 
 
+def _like(t: torch.Tensor) -> torch.Tensor:
+    """A new contiguous tensor of t's shape and type (empty_like costs half of what the other ways to make one do)."""
+    return torch.empty_like(t) if t.is_contiguous() else t.new_empty(t.shape)
+
+
 # ---- the C calls ----------------------------------------------------------------------------------------------------------
 
 # (`stream` is taken by the wrapper)
@@ -178,7 +183,7 @@ def norm_forward(x: torch.Tensor, weight: Optional[torch.Tensor] = None, bias: O
             raise ValueError("weight and bias must have the same type")
         wt = wt if w is not None else bt
     if out is None:
-        out = x.new_empty(x.shape)
+        out = _like(x)
         my = Matrix(out.data_ptr(), cols)
     else:
         my = _matrix(out, "out", x.shape, x.dtype, dev)
@@ -207,12 +212,15 @@ def norm_backward(dy: torch.Tensor, x: torch.Tensor, weight: Optional[torch.Tens
     if not want_dx:
         dx, mdx = None, _NO_MATRIX
     elif dx is None:
-        dx = x.new_empty(x.shape)
+        dx = _like(x)
         mdx = Matrix(dx.data_ptr(), cols)
     else:
         mdx = _matrix(dx, "dx", x.shape, x.dtype, dev)
-    dweight = (x.new_empty(cols, dtype=torch.float32) if dweight is None else dweight) if want_dweight else None
-    dbias = (x.new_empty(cols, dtype=torch.float32) if dbias is None else dbias) if bias else None
+    def vector():
+        return torch.empty_like(weight) if wt == TSR_F32 and weight is not None else x.new_empty(cols, dtype=torch.float32)
+
+    dweight = (vector() if dweight is None else dweight) if want_dweight else None
+    dbias = (vector() if dbias is None else dbias) if bias else None
     gw, gwt = _vector(dweight, "dweight", cols, dev)
     gb, gbt = _vector(dbias, "dbias", cols, dev)
     if gw is not None and gb is not None and gwt != gbt:
@@ -241,14 +249,14 @@ def linear_forward(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.T
     b, bt = _vector(bias, "bias", outs, dev)
     mres = _matrix(residual, "residual", shape, x.dtype, dev) if residual is not None else _NO_MATRIX
     if out is None:
-        out = x.new_empty(shape)
+        out = x.new_empty(shape) if residual is None else _like(residual)
         my = Matrix(out.data_ptr(), outs)
     else:
         my = _matrix(out, "out", shape, x.dtype, dev)
     if pre is not None:
         mpre = _matrix(pre, "pre", shape, x.dtype, dev)
     elif keep_pre:
-        pre = x.new_empty(shape)
+        pre = _like(out)
         mpre = Matrix(pre.data_ptr(), outs)
     else:
         mpre = _NO_MATRIX
@@ -287,7 +295,7 @@ def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], weight: torch.T
     if not want_dx:
         dx, mdx = None, _NO_MATRIX
     elif dx is None:
-        dx = dy.new_empty(shape)
+        dx = dy.new_empty(shape) if x is None else _like(x)
         mdx = Matrix(dx.data_ptr(), ins)
     else:
         mdx = _matrix(dx, "dx", shape, dy.dtype, dev)
@@ -296,7 +304,7 @@ def linear_backward(dy: torch.Tensor, x: Optional[torch.Tensor], weight: torch.T
         dweight, mdw = None, _NO_MATRIX
     else:
         if dweight is None:
-            dweight = dy.new_empty((outs, ins))
+            dweight = _like(weight)
         gwt = _DTYPE.get(dweight.dtype)
         if gwt is None:
             raise ValueError("dweight must be FP32 or BF16")
@@ -316,7 +324,7 @@ def dropout_forward(x: torch.Tensor, dropout: Dropout, residual: Optional[torch.
     kind, (rows, cols, ld), dev = _input(x, "x")
     mres = _matrix(residual, "residual", x.shape, x.dtype, dev) if residual is not None else _NO_MATRIX
     if out is None:
-        out = x.new_empty(x.shape)
+        out = _like(x)
         my = Matrix(out.data_ptr(), cols)
     else:
         my = _matrix(out, "out", x.shape, x.dtype, dev)
