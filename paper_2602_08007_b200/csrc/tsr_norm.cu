@@ -461,14 +461,14 @@ __device__ __forceinline__ void add_up(const NormArgs &a, const float *sums)
     if (cluster > 1) cluster_sync();      // no CTA leaves while its sums are read
 }
 
-// Groups and rings as in the forward pass; x and dy come through the ring.  A lane keeps its columns from row to row, so that the column sums stay in
-// registers (128 of them at U = 8 and BF16: eight warps per SM, whose eight units per lane hide what little there is to wait for; two units per thread
-// in five CTAs of four warps per row took 69 us for 16384 x 2048, where half of the instructions were those of barriers and sums).  Weight is in
-// registers up to two units, else in shared memory.  DB: the sums of dy are wanted too.
 // Units of x and dy of one row in the ring; groups of four lanes, two of which are served at a time, get slots half a cycle of the banks apart.
 template <int L>
 __host__ __device__ __forceinline__ int slot_units(int units) { return 2 * units + (L == 4 ? (4 - 2 * units % 8 + 8) % 8 : 0); }
 
+// Groups and rings as in the forward pass; x and dy come through the ring.  A lane keeps its columns from row to row, so that the column sums stay in
+// registers (128 of them at U = 8 and BF16: eight warps per SM, whose eight units per lane hide what little there is to wait for; two units per thread
+// in five CTAs of four warps per row took 69 us for 16384 x 2048, where half of the instructions were those of barriers and sums).  Weight is in
+// registers up to two units, else in shared memory.  DB: the sums of dy are wanted too.
 template <typename T, int L, int U, bool DB, bool EDGE, bool TEAMS, int CTAS, int WARPS = ROW_WARPS>
 __global__ void __launch_bounds__(32 * WARPS, CTAS)
 norm_backward_kernel(const NormArgs a, int stages)
