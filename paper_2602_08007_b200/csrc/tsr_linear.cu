@@ -17,22 +17,39 @@ namespace tsr {
 
 // ---- kernels ----------------------------------------------------------------------------------------------------------
 
-// dst[r][0 .. cols) = src[r][..]; dst has a pitch of whole 16-byte units.  A thread writes one unit of eight entries.
+// Operands that are copied, both of a product in one launch.  dst has a pitch of whole 16-byte units; a thread writes one unit of eight entries.
+struct CopyJob {
+    const void *src;
+    bf16 *dst;
+    int64_t lds, ldd, plane, rows;      // plane: entries between the three planes of an FP32 matrix
+    int32_t cols, units;                // units per row
+};
+struct CopyJobs { CopyJob job[2]; int32_t n; };
+// Which unit of which job, and its row and column.
+__device__ __forceinline__ const CopyJob &job_at(const CopyJobs &a, int64_t u, int64_t first, int64_t &r, int &c)
+{
+    const bool second = u >= first;
+    const CopyJob &j = a.job[second];
+    if (second) u -= first;
+    r = u < ((int64_t)1 << 32) ? (int64_t)((uint32_t)u / (uint32_t)j.units) : u / j.units;
+    c = (int)(u - r * j.units) * 8;
+    return j;
+}
 __global__ void __launch_bounds__(256)
-linear_pack_kernel(const bf16 *__restrict__ src, int64_t lds, bf16 *__restrict__ dst, int64_t ldd, int64_t rows, int cols, int units)
+linear_pack_kernel(const __grid_constant__ CopyJobs a)
 {
     pdl_trigger();
     pdl_wait();
-    const int64_t total = rows * units;
-    const bool small = total < ((int64_t)1 << 32);
+    const int64_t first = a.job[0].rows * a.job[0].units, total = first + (a.n > 1 ? a.job[1].rows * a.job[1].units : 0);
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
-        const int64_t r = small ? (int64_t)((uint32_t)u / (uint32_t)units) : u / units;
-        const int c = (int)(u - r * units) * 8;
-        const bf16 *s = src + r * lds + c;
-        bf16 *d = dst + r * ldd + c;
-        if (c + 8 <= cols) *(uint4 *)d = load16_any(s);
+        int64_t r;
+        int c;
+        const CopyJob &j = job_at(a, u, first, r, c);
+        const bf16 *s = (const bf16 *)j.src + r * j.lds + c;
+        bf16 *d = j.dst + r * j.ldd + c;
+        if (c + 8 <= j.cols) *(uint4 *)d = load16_any(s);
         else {
-            for (int i = 0; i < cols - c; ++i) d[i] = s[i];
+            for (int i = 0; i < j.cols - c; ++i) d[i] = s[i];
         }
     }
 }
@@ -63,22 +80,22 @@ __device__ __forceinline__ void store_planes(bf16 *dst, int64_t plane, const flo
 #pragma unroll
     for (int k = 0; k < 3; ++k) *(uint4 *)(dst + k * plane) = make_uint4(w[k][0], w[k][1], w[k][2], w[k][3]);
 }
-// dst: three planes of rows x ldd, `plane` entries apart.  A thread takes eight neighbours of a row.
+// FP32 -> three planes of rows x ldd, `plane` entries apart.
 __global__ void __launch_bounds__(256)
-linear_split_kernel(const float *__restrict__ src, int64_t lds, bf16 *__restrict__ dst, int64_t ldd, int64_t plane, int64_t rows, int cols, int units)
+linear_split_kernel(const __grid_constant__ CopyJobs a)
 {
     pdl_trigger();
     pdl_wait();
-    const int64_t total = rows * units;
-    const bool small = total < ((int64_t)1 << 32);
+    const int64_t first = a.job[0].rows * a.job[0].units, total = first + (a.n > 1 ? a.job[1].rows * a.job[1].units : 0);
     for (int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x; u < total; u += (int64_t)gridDim.x * 256) {
-        const int64_t r = small ? (int64_t)((uint32_t)u / (uint32_t)units) : u / units;
-        const int c = (int)(u - r * units) * 8;
-        const float *s = src + r * lds + c;
+        int64_t r;
+        int c;
+        const CopyJob &j = job_at(a, u, first, r, c);
+        const float *s = (const float *)j.src + r * j.lds + c;
         float v[8];
-        if (c + 8 <= cols) load8_any(s, v);
-        else load8_part(s, cols - c, v);
-        store_planes(dst + r * ldd + c, plane, v);      // (the pitch is whole units: what is written past the last column is zero)
+        if (c + 8 <= j.cols) load8_any(s, v);
+        else load8_part(s, j.cols - c, v);
+        store_planes(j.dst + r * j.ldd + c, j.plane, v);      // (the pitch is whole units: what is written past the last column is zero)
     }
 }
 
@@ -616,6 +633,15 @@ struct Room {      // walks the workspace; with base NULL it only counts
     }
 };
 
+template <typename Kern>
+cudaError_t copy_operands(Kern kernel, const CopyJobs &jobs, int sms, cudaStream_t stream)
+{
+    int64_t units = 0;
+    for (int i = 0; i < jobs.n; ++i) units += jobs.job[i].rows * jobs.job[i].units;
+    if (!units) return cudaSuccess;
+    return launch_dependent(kernel, dim3((unsigned)std::min<int64_t>((units + 255) / 256, (int64_t)sms * 32)), dim3(256), 0, stream, 1, jobs);
+}
+
 // The product's scratch, and (run) its launches.
 tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t stream)
 {
@@ -661,6 +687,7 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
     // operands
     const int planes = p.f32 ? 3 : 1, inner = p.f32 ? 64 : 128;
     const Operand *op[2] = {&p.A, &p.B};
+    CopyJobs jobs = {};
     const int64_t extent[2] = {p.M, p.N};
     for (int i = 0; i < 2; ++i) {
         const Operand &o = *op[i];
@@ -673,11 +700,7 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
         if (!p.f32 && (straddles || !tma_takes(o.p, rows, o.ld, 2))) {
             ld = round_up(cols, 64);
             bf16 *copy = (bf16 *)room.take((size_t)rows * ld * 2);
-            if (run) {
-                const int units = (int)((cols + 7) / 8);
-                const dim3 grid((unsigned)std::min<int64_t>((rows * units + 255) / 256, (int64_t)sms * 32));
-                if (launch_dependent(linear_pack_kernel, grid, dim3(256), 0, stream, 1, (const bf16 *)o.p, o.ld, copy, ld, rows, (int)cols, units) != cudaSuccess) return TSR_ERR_CUDA;
-            }
+            jobs.job[jobs.n++] = {o.p, copy, o.ld, ld, 0, rows, (int)cols, (int)((cols + 7) / 8)};
             at = copy;
         }
         // an MN-major box: 64 entries side by side (128 bytes) x the K block; a K-major one: the K block x the rows of a CTA
@@ -686,6 +709,7 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
         if (!ok) return TSR_ERR_CUDA;
         (i ? g.b_mn : g.a_mn) = o.mn;
     }
+    if (run && copy_operands(linear_pack_kernel, jobs, sms, stream) != cudaSuccess) return TSR_ERR_CUDA;
     g.a_rows = a_rows;
     g.a_boxes = (a_rows + 63) / 64;
     g.b_boxes = (s.width / s.cg + 63) / 64;
@@ -717,18 +741,15 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
     return finish();
 }
 
-// Three BF16 planes of an FP32 matrix (rows x cols) in the workspace, as an operand.
-tsr_status three_planes(const tsr_matrix &m, int64_t rows, int64_t cols, bool mn, Operand *o, Room &room, bool run, int sms, cudaStream_t stream)
+// Three BF16 planes of an FP32 matrix (rows x cols) in the workspace, as an operand; the copy is left to `jobs`.
+void three_planes(const tsr_matrix &m, int64_t rows, int64_t cols, bool mn, Operand *o, Room &room, CopyJobs *jobs)
 {
     o->ld = round_up(std::max<int64_t>(cols, 1), 64);
     o->plane = std::max<int64_t>(rows, 1) * o->ld;
     o->mn = mn;
     bf16 *copy = (bf16 *)room.take((size_t)3 * o->plane * 2);
     o->p = copy;
-    if (!run || rows == 0 || cols == 0) return TSR_OK;
-    const int units = (int)((cols + 7) / 8);
-    const dim3 grid((unsigned)std::min<int64_t>((rows * units + 255) / 256, (int64_t)sms * 32));
-    return launch_dependent(linear_split_kernel, grid, dim3(256), 0, stream, 1, (const float *)m.data, m.ld, copy, o->ld, o->plane, rows, (int)cols, units) == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
+    if (rows && cols) jobs->job[jobs->n++] = {m.data, copy, m.ld, o->ld, o->plane, rows, (int)cols, (int)((cols + 7) / 8)};
 }
 
 constexpr int64_t MOST = 0x7fffffff - 1023;
@@ -784,9 +805,10 @@ tsr_status forward(const tsr_linear_desc *d, const tsr_linear_io *io, void *work
             return (p.f32 ? few_launch<float>(a, n, stream) : few_launch<bf16>(a, n, stream)) == cudaSuccess ? TSR_OK : TSR_ERR_CUDA;
         }
         if (p.f32 && p.M > 0 && p.N > 0 && p.K > 0) {
-            tsr_status e = three_planes(io->x, d->rows, d->ins, false, &p.A, room, run, n, stream);
-            if (e == TSR_OK) e = three_planes(io->weight, d->outs, d->ins, false, &p.B, room, run, n, stream);
-            if (e != TSR_OK) return e;
+            CopyJobs jobs = {};
+            three_planes(io->x, d->rows, d->ins, false, &p.A, room, &jobs);
+            three_planes(io->weight, d->outs, d->ins, false, &p.B, room, &jobs);
+            if (run && copy_operands(linear_split_kernel, jobs, n, stream) != cudaSuccess) return TSR_ERR_CUDA;
         }
         return product(p, room, run, n, stream);
     };
@@ -864,9 +886,10 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
         // FP32: planes of the other operands
         Operand dz_op = {dz.data, dz.ld, false, T * dz.ld}, w_op = {io->weight.data, io->weight.ld, true, 0}, x_op = {io->x.data, io->x.ld, true, 0};
         if (f32 && T > 0 && O > 0 && I > 0) {
-            if (dx) st = three_planes(io->weight, O, I, true, &w_op, room, run, sms, stream);
-            if (st == TSR_OK && dw) st = three_planes(io->x, T, I, true, &x_op, room, run, sms, stream);
-            if (st != TSR_OK) return st;
+            CopyJobs jobs = {};
+            if (dx) three_planes(io->weight, O, I, true, &w_op, room, &jobs);
+            if (dw) three_planes(io->x, T, I, true, &x_op, room, &jobs);
+            if (run && copy_operands(linear_split_kernel, jobs, sms, stream) != cudaSuccess) return TSR_ERR_CUDA;
         }
         // the two products run one after the other: they share what is left of the workspace
         size_t after = room.at;

@@ -333,6 +333,26 @@ def test_many_rows_and_far_offsets(tsr):
     del flat
 
 
+def test_scratch_of_calls_of_one_size(tsr):
+    """The same sizes at another alignment need more scratch (operands are copied), or less again."""
+    T, I, O = 130, 264, 200
+    flat = normal(T * (I + 8) + O * (I + 8) + 64, dtype=BF, seed=1)
+    even = lambda rows, at: torch.as_strided(flat, (rows, I), (I, 1), at)  # noqa: E731
+    odd = lambda rows, at: torch.as_strided(flat, (rows, I), (I + 1, 1), at)  # noqa: E731
+    dy, gb = normal(T, O, dtype=BF, seed=2), torch.empty(O, device="cuda")
+    for view in (even, odd, even, odd):
+        x, w = view(T, 0), view(O, T * (I + 8))
+        y, _ = tsr.linear_forward(x, w)
+        lm.close(y, *[lm.linear(x, w)[i] for i in (0, 2)])
+        for got, (e, s) in zip(tsr.linear_backward(dy, x, w, dbias=gb), lm.linear_grads(dy, x, w)):
+            lm.close(got, e, s)
+    for mx in (even(T, 0), odd(T, 1), even(T, 8)):
+        _, stats = tsr.norm_forward(mx)
+        up = normal(T, I, dtype=BF, seed=3)
+        for got, (e, s) in zip(tsr.norm_backward(up, mx, None, stats, want_dweight=True), lm.norm_grads(up, mx, None, stats)):
+            lm.close(got, e, s)
+
+
 def test_refusals(tsr):
     x, w, v = normal(6, 16), normal(8, 16), normal(16, seed=2)
     y, stats = tsr.norm_forward(x, v)
