@@ -186,7 +186,7 @@ linear_finish_kernel(const __grid_constant__ FinishArgs a)
     }
 }
 
-// Few rows (at most eight): the layer is bound by reading the weight once.  A warp takes four output columns at a time (what it reads of x counts for all
+// Few rows (up to eight at a time): the layer is bound by reading the weight once.  A warp takes four output columns at a time (what it reads of x counts for all
 // of them) and every n-th slice of 256 entries of K, eight per lane at any alignment, against the rows of x in shared memory (FP32, a chunk of K at a
 // time); FP32 stays in FP32 here.  Lanes, then the warps that share columns, join their sums, then a lane per entry runs the epilogue.  One launch,
 // nothing in the workspace.
@@ -254,6 +254,7 @@ linear_few_kernel(const __grid_constant__ FewArgs a)
     pdl_trigger();
     pdl_wait();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, kw = warp % a.along_k, per_cta = 8 / a.along_k * C, tiles = (a.N + per_cta - 1) / per_cta;
+    const int row0 = blockIdx.y * ROWS, rows = min(ROWS, a.M - row0);
     for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
         const int col0 = tile * per_cta + warp / a.along_k * C;
         const T *w[C];
@@ -271,7 +272,7 @@ linear_few_kernel(const __grid_constant__ FewArgs a)
 #pragma unroll
                 for (int r = 0; r < ROWS; ++r)
 #pragma unroll 4
-                    for (int i = threadIdx.x; i < padded; i += 256) xs[r * a.chunk + i] = r < a.M && i < len ? load_f((const T *)a.x + r * a.ldx + k0 + i) : 0.f;
+                    for (int i = threadIdx.x; i < padded; i += 256) xs[r * a.chunk + i] = r < rows && i < len ? load_f((const T *)a.x + (row0 + r) * a.ldx + k0 + i) : 0.f;
                 __syncthreads();
             }
 #pragma unroll 2
@@ -308,14 +309,15 @@ linear_few_kernel(const __grid_constant__ FewArgs a)
             z = 0.f;
             for (int k = 0; k < a.along_k; ++k) z += parts[warp + k][value];
         }
-        if (lane % (32 / VALUES) || r >= a.M || col >= a.N) continue;
+        if (lane % (32 / VALUES) || r >= rows || col >= a.N) continue;
         const LinearEpilogue &e = a.e;
+        const int64_t row = row0 + r;
         if (e.bias) z += load_as(e.bias, col, e.bias_bf16);
-        if (e.pre) store_f((T *)e.pre + r * e.ldp + col, z);
+        if (e.pre) store_f((T *)e.pre + row * e.ldp + col, z);
         z = act_value(e.act, z);
-        if (e.drop.threshold) z = drop_entry(drop_row_key(drop_call_key(e.drop), r), (uint32_t)col, z, e.drop);
-        if (e.res) z += load_f((const T *)e.res + r * e.ldr + col);
-        store_f((T *)e.out + r * e.ldo + col, z);
+        if (e.drop.threshold) z = drop_entry(drop_row_key(drop_call_key(e.drop), row), (uint32_t)col, z, e.drop);
+        if (e.res) z += load_f((const T *)e.res + row * e.ldr + col);
+        store_f((T *)e.out + row * e.ldo + col, z);
     }
 }
 // Rows of a matrix that start on 16 bytes.
@@ -325,9 +327,10 @@ static cudaError_t few_launch(FewArgs a, int sms, cudaStream_t s)
 {
     // as many CTAs as SMs at least, as long as there is K to share
     a.along_k = 1;
-    while (a.along_k < 8 && a.along_k * 256 < a.K && (int64_t)a.N * a.along_k < (int64_t)sms * 2 * 8 * FEW_COLS) a.along_k *= 2;
+    const int groups = (a.M + FEW_ROWS - 1) / FEW_ROWS;
+    while (a.along_k < 8 && a.along_k * 256 < a.K && (int64_t)a.N * a.along_k * groups < (int64_t)sms * 2 * 8 * FEW_COLS) a.along_k *= 2;
     const int per_cta = 8 / a.along_k * FEW_COLS;
-    const dim3 grid((unsigned)std::min((a.N + per_cta - 1) / per_cta, sms * (a.M > 2 ? 2 : 3)));
+    const dim3 grid((unsigned)std::min((a.N + per_cta - 1) / per_cta, sms * (a.M > 2 ? 2 : 3)), groups);
     const int rows = a.M <= 2 ? a.M : a.M <= 4 ? 4 : FEW_ROWS;
     a.chunk = (int)std::min<int64_t>(FEW_SHARED / rows, round_up(a.K, 8));
     const size_t smem = (size_t)rows * a.chunk * 4;
@@ -613,13 +616,16 @@ Shape choose(const Product &p, int sms)
 //   BF16 aligned      2048 -> 2048, 1 row 4.8 / 7.9, 4 rows 7.1 / 7.9, 8 rows 10.4 / 8.0;  2048 -> 32768, 1 row 28.3 / 25.2
 //   BF16 not aligned  2047 -> 2047, 1 row 5.4 / 12.1, 8 rows 11.7 / 14.2;  5461 -> 2048, 4 rows 15.4 / 19.8, 8 rows (x does not fit) 40.9 / 19.7
 //   FP32              2048 -> 2048, 1 row 4.8 / 19.7, 8 rows 10.7 / 20.0;  5461 -> 2048, 4 rows 23.8 / 40.9, 8 rows (does not fit) 47.0 / 41.0
+// Without aligned BF16, more rows go through it in groups of eight while the product is small: one launch instead of two or three (64 x 512 -> 512 FP32
+// 8.2 / 11.2, 64 x 700 -> 700 19.4 / 13.5; BF16 not aligned 64 x 511 -> 512 8.7 / 7.2).
 bool few_rows(const Product &p)
 {
-    if (p.M <= 0 || p.M > FEW_ROWS || p.N <= 0 || p.K <= 0 || p.K > FEW_MOST_K) return false;
+    if (p.M <= 0 || p.M > 8 * FEW_ROWS || p.N <= 0 || p.K <= 0 || p.K > FEW_MOST_K) return false;
     const bool fits = (p.M <= 2 ? p.M : p.M <= 4 ? 4 : FEW_ROWS) * p.K <= FEW_SHARED;
-    if (p.f32) return fits || p.M <= 4;
-    if (!tma_takes(p.B.p, p.N, p.B.ld, 2)) return fits;
-    return fits && p.M <= 4 && (double)p.M * p.N * p.K <= 33554432.0;
+    const double size = (double)p.M * p.N * p.K;
+    if (!p.f32 && tma_takes(p.B.p, p.N, p.B.ld, 2)) return fits && p.M <= 4 && size <= 33554432.0;
+    if (p.M > FEW_ROWS) return fits && size <= (p.f32 ? 16777216.0 : 8388608.0);
+    return fits || (p.f32 && p.M <= 4);
 }
 
 struct Room {      // walks the workspace; with base NULL it only counts
