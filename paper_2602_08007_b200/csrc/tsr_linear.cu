@@ -3,7 +3,7 @@
 //
 //   linear_pack_kernel     BF16 operand whose pitch or address TMA does not take -> workspace with a 128-byte pitch (one pass over it)
 //   linear_split_kernel    FP32 operand -> three BF16 planes whose sum it is
-//   linear_few_kernel      the whole layer for at most eight rows
+//   linear_few_kernel      the whole layer for few rows
 //   linear_dz_kernel       dz = dropout(dy) o act'(pre) and the column sums of dz (the bias's gradient), one pass over dy and pre
 //   linear_finish_kernel   split K: slabs added in order, then the epilogue
 //   column_finish_kernel   partial column sums added in order (bias, and the norm's weight and bias)
