@@ -1,11 +1,15 @@
 // Norm over rows, forward and backward (formulas in tsr.h).  Both passes are bound by HBM: forward reads x and writes y, backward reads
 // x and dy and writes dx, each once; a row stays in registers between its sums and its results.
 //
-// Rows up to 32 KB are worked on by a group of lanes or a team of warps, the next ones in flight.  Distances are formed from the row's first
-// entry and then from means: a large mean costs no digits, and a row of equal entries has variance zero.  Backward: lanes keep their columns
+// Rows up to 32 KB are worked on by a group of lanes or a team of warps, the next ones in flight.  The mean is found in two steps: one sum gives m,
+// the mean to FP32 accuracy, then the distances d = x - m, each rounded to its own size, are summed together with their squares, which
+// corrects mean and variance:  mean = m + e,  e = sum d / n,  variance = sum d^2 / n - e^2  (e is below a unit of m's last place or below 2^-12 of the deviation,
+// so that next to nothing is taken away; where rows are a few units of last place wide, a bit).  Neither a large mean nor single large entries, wherever they stand,
+// cost the others digits.  The first sum is that of distances from the row's first entry, which makes m of a row of equal entries exact and its variance zero.
+// Backward: lanes keep their columns
 // from row to row, so that the sums for dweight and dbias stay in registers; a cluster of CTAs leaves one partial row of them, and
 // column_finish_kernel adds those in order.
-// Measured: forward 16384 x 2048 BF16 25 us (5.4 TB/s of 6.6 that a copy reaches), backward 8192 x 1024 FP32 23 us (4.3), backward without mean 6007 x
+// Measured: forward 16384 x 2048 BF16 25.5 us (5.3 TB/s of 6.6 that a copy reaches), backward 8192 x 1024 FP32 23 us (4.3), backward without mean 6007 x
 // 5461 BF16 59 us (3.4: the rows start at eight different places, teams of eight warps wait for each other, and first and last rows of a CTA are alone).
 // Wider rows, and matrices that do not start at the same place in 16 bytes, are read several times (from L2, mostly), entry by entry; their column
 // sums take a pass of their own.  Those are bound by instructions: 6007 x 5461 from a pitch of 5464 into one of 5461 takes 159 us forward, 234 us
@@ -38,6 +42,26 @@ __device__ __forceinline__ float cta_sum(float x, float *slot)
     for (int w = 0; w < warps; ++w) s += slot[w];
     return s;
 }
+// Two sums at once.
+__device__ __forceinline__ float2 cta_sums(float2 x, float2 *slot)
+{
+    const int warps = (blockDim.x + 31) >> 5;
+    x = make_float2(warp_sum(x.x), warp_sum(x.y));
+    if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = x;
+    __syncthreads();
+    float2 s = make_float2(0.f, 0.f);
+    for (int w = 0; w < warps; ++w) { s.x += slot[w].x; s.y += slot[w].y; }
+    return s;
+}
+// Variance from the means of the squares and of the distances; rounding may leave it below zero, and NaN stays.
+__device__ __forceinline__ float variance_of(float squares, float rest)
+{
+    const float v = fmaf(-rest, rest, squares);
+    return v < 0.f ? 0.f : v;
+}
+__device__ __forceinline__ float finite_or_zero(float x) { return fabsf(x) < INFINITY ? x : 0.f; }
+// The mean as the statistics hold it; that of a row with an infinity is the infinity.
+__device__ __forceinline__ float whole_mean(float mean, float rest) { return fabsf(mean) == INFINITY ? mean : mean + rest; }
 
 constexpr int NORM_STAGES = 8;      // most stages of a ring
 constexpr int MOST_CLUSTER = 8;     // CTAs that add their column sums
@@ -210,24 +234,24 @@ __device__ __forceinline__ void share_params(const NormArgs &a, const RowClass &
         }
     }
 }
-// Squares without those of `empty` places, each of which had distance `mean` from the mean.  The pivot is an entry of the row, so that what is taken
-// away is at most (2 V - 2) mean^2 <= (2 V - 2) squares: four bits at the worst (a row of two entries), none of a row that is long.
+// Sums of distances and squares without those of `empty` places, each at distance `from`.  That is the first entry's own distance, so that at most 2 V - 2
+// squares are taken away from a sum that keeps one more of them: four bits at the worst (a row of two BF16 entries), none of a long row without outliers.
 template <bool EDGE>
-__device__ __forceinline__ float less_empty(float squares, float mean, float empty)
+__device__ __forceinline__ float2 less_empty(float2 s, float from, float empty)
 {
-    if (!EDGE) return squares;
-    const float s = fmaf(-empty * mean, mean, squares);
-    return s < 0.f ? 0.f : s;      // (NaN stays)
+    if (!EDGE) return s;
+    const float e = empty * from;
+    return make_float2(s.x - e, fmaf(-e, from, s.y));
 }
-// v <- v rstd w + b over unit j
+// v <- (v rstd + shift) w + b over unit j
 template <int P>
-__device__ __forceinline__ void normed(float2 (&v)[P], float rstd, const float *w, const float *b, int j, int units)
+__device__ __forceinline__ void normed(float2 (&v)[P], float rstd, float shift, const float *w, const float *b, int j, int units)
 {
 #pragma unroll
     for (int i = 0; i < P; i += 2) {
         const float4 ww = *(const float4 *)(w + shared_at(j, i / 2, units)), bb = *(const float4 *)(b + shared_at(j, i / 2, units));
-        v[i] = fma2(mul2(v[i], pair(rstd)), make_float2(ww.x, ww.y), make_float2(bb.x, bb.y));
-        v[i + 1] = fma2(mul2(v[i + 1], pair(rstd)), make_float2(ww.z, ww.w), make_float2(bb.z, bb.w));
+        v[i] = fma2(fma2(v[i], pair(rstd), pair(shift)), make_float2(ww.x, ww.y), make_float2(bb.x, bb.y));
+        v[i + 1] = fma2(fma2(v[i + 1], pair(rstd), pair(shift)), make_float2(ww.z, ww.w), make_float2(bb.z, bb.w));
     }
 }
 
@@ -290,7 +314,7 @@ norm_forward_kernel(const NormArgs a, int stages)
     extern __shared__ float4 shared[];       // w, b, rings
     __shared__ uint64_t bars[ROW_WARPS * NORM_STAGES];
     __shared__ Edges edges;
-    __shared__ float slots[TEAMS ? 2 : 1][ROW_WARPS];      // sums of a team's warps: of the entries and of the squares, or of the squares by turns
+    __shared__ float2 slots[TEAMS ? 2 : 1][ROW_WARPS];     // sums of a team's warps: the first and the second of a row, or those of one row and the next
     pdl_trigger();
     pdl_wait();
     const int warp = threadIdx.x >> 5;
@@ -311,14 +335,28 @@ norm_forward_kernel(const NormArgs a, int stages)
         ask_row<T>(smem_u32(ring + stage * G * rc.units), ask, rc, smem_u32(bar + stage));
         ask += next_ask;
     };
-    // over the whole row, from every lane's sum
-    auto row_sum = [&](float x, float *slot) -> float {
+    // over the whole row, from every lane's sum; or two at once.  (A team's lanes read its warps' sums side by side: one after the other they took 8000 x 8192
+    // BF16 from 68 to 72 us.)
+    auto row_sum = [&](float x, float2 *slot) -> float {
         x = lanes_sum<L>(x);
         if constexpr (TEAMS) {      // (slots are written again after another barrier at the earliest)
+            if ((threadIdx.x & 31) == 0) slot[warp].x = x;
+            team_sync(rows.group, lanes);
+            x = slot[rows.group * rows.warps + (lane & (rows.warps - 1))].x;
+            for (int o = rows.warps / 2; o; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+        }
+        return x;
+    };
+    auto row_sums = [&](float2 x, float2 *slot) -> float2 {
+        x = lanes_sum<L>(x, lane);
+        if constexpr (TEAMS) {
             if ((threadIdx.x & 31) == 0) slot[warp] = x;
             team_sync(rows.group, lanes);
-            x = 0.f;
-            for (int i = 0; i < rows.warps; ++i) x += slot[rows.group * rows.warps + i];
+            x = slot[rows.group * rows.warps + (lane & (rows.warps - 1))];
+            for (int o = rows.warps / 2; o; o >>= 1) {
+                x.x += __shfl_xor_sync(0xffffffffu, x.x, o);
+                x.y += __shfl_xor_sync(0xffffffffu, x.y, o);
+            }
         }
         return x;
     };
@@ -342,8 +380,8 @@ norm_forward_kernel(const NormArgs a, int stages)
         await_row(smem_u32(bar + stage), phase, gave_up);
         const uint4 *row = ring + stage * G * rc.units;
         const bool mine = G == 1 || turn < left;      // (what a group without a row computes goes nowhere)
-        const T pivot = a.center ? *((const T *)row + rc.shift) : T(0.f);      // also stands in the places that hold no entry
-        const float x0 = load_f(&pivot);
+        const T pivot = a.center ? *((const T *)row + rc.shift) : T(0.f);      // the first entry; also stands in the places that hold none
+        const float x0 = finite_or_zero(load_f(&pivot));
         float2 v[U][P], sum = pair(0.f), q = pair(0.f);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -359,30 +397,47 @@ norm_forward_kernel(const NormArgs a, int stages)
             __syncwarp();
             if (lane == 0 && turn + stages < rows.turns) request(stage);
         }
+        float mean = 0.f, rest = 0.f, shift = 0.f, rstd;
+        if (a.center) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u * lanes + lane >= rc.units) continue;
-            less(v[u], x0);
+            for (int u = 0; u < U; ++u) {
+                if (u * lanes + lane >= rc.units) continue;
 #pragma unroll
-            for (int i = 0; i < P; ++i) sum = add2(sum, v[u][i]);
+                for (int i = 0; i < P; ++i) sum = add2(sum, add2(v[u][i], pair(-x0)));
+            }
+            mean = fmaf(row_sum(sum.x + sum.y, slots[0]), a.inv_n, x0);
+            sum = pair(0.f);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (u * lanes + lane >= rc.units) continue;
+                less(v[u], mean);
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    sum = add2(sum, v[u][i]);
+                    q = fma2(v[u][i], v[u][i], q);
+                }
+            }
+            const float2 s = less_empty<EDGE>(row_sums(make_float2(sum.x + sum.y, q.x + q.y), slots[TEAMS ? 1 : 0]), x0 - mean, empty);
+            rest = s.x * a.inv_n;
+            rstd = rsqrtf(variance_of(s.y * a.inv_n, rest) + a.eps);
+            shift = -rest * rstd;
+        } else {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (u * lanes + lane >= rc.units) continue;
+#pragma unroll
+                for (int i = 0; i < P; ++i) q = fma2(v[u][i], v[u][i], q);
+            }
+            rstd = rsqrtf(fmaf(row_sum(q.x + q.y, slots[TEAMS ? turn & 1 : 0]), a.inv_n, a.eps));
         }
-        const float mean = a.center ? row_sum(sum.x + sum.y, slots[0]) * a.inv_n : 0.f;
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (u * lanes + lane >= rc.units) continue;
-            less(v[u], mean);
-#pragma unroll
-            for (int i = 0; i < P; ++i) q = fma2(v[u][i], v[u][i], q);
-        }
-        const float rstd = rsqrtf(less_empty<EDGE>(row_sum(q.x + q.y, slots[TEAMS && (a.center || turn & 1) ? 1 : 0]), mean, empty) * a.inv_n + a.eps);
         if (TEAMS && lane == 0 && turn + stages < rows.turns) request(stage);
         if (++stage == stages) { stage = 0; phase ^= 1u; }
-        if (stats && lane == 0 && mine) *(float2 *)stats = make_float2(x0 + mean, rstd);
+        if (stats && lane == 0 && mine) *(float2 *)stats = make_float2(whole_mean(mean, rest), rstd);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             const int j = u * lanes + lane;
             if (j >= rc.units || !mine) continue;
-            normed(v[u], rstd, w, b, j, rc.units);
+            normed(v[u], rstd, shift, w, b, j, rc.units);
             store_unit<T>(y, j * V - rc.shift, a.cols, EDGE && at_edge(u, last_u), v[u]);
         }
         y += next_y;
@@ -396,24 +451,31 @@ template <typename T>
 __global__ void __launch_bounds__(1024)
 norm_forward_wide_kernel(const NormArgs a)
 {
-    __shared__ float slots[2][32];
+    __shared__ float slots[32];
+    __shared__ float2 pairs[32];
     pdl_trigger();
     pdl_wait();
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T *x = (const T *)a.x + r * a.ldx;
-        float x0 = 0.f, m0 = 0.f, q = 0.f;
+        float mean = 0.f, rest = 0.f, sum = 0.f, q = 0.f;
         if (a.center) {
-            x0 = load_f(x);
-            for (int c = threadIdx.x; c < a.cols; c += blockDim.x) m0 += load_f(x + c) - x0;
-            m0 = cta_sum(m0, slots[0]) * a.inv_n;
+            const float x0 = finite_or_zero(load_f(x));
+            for (int c = threadIdx.x; c < a.cols; c += blockDim.x) sum += load_f(x + c) - x0;
+            mean = fmaf(cta_sum(sum, slots), a.inv_n, x0);
         }
-        const float mu = x0 + m0;
-        for (int c = threadIdx.x; c < a.cols; c += blockDim.x) { const float d = load_f(x + c) - x0 - m0; q = fmaf(d, d, q); }
-        const float rstd = rsqrtf(cta_sum(q, slots[1]) * a.inv_n + a.eps);
-        if (a.stats && threadIdx.x == 0) { a.stats[2 * r] = mu; a.stats[2 * r + 1] = rstd; }
+        sum = 0.f;
+        for (int c = threadIdx.x; c < a.cols; c += blockDim.x) {
+            const float d = load_f(x + c) - mean;
+            sum += d;
+            q = fmaf(d, d, q);
+        }
+        const float2 s = cta_sums(make_float2(sum, q), pairs);
+        if (a.center) rest = s.x * a.inv_n;
+        const float rstd = rsqrtf(variance_of(s.y * a.inv_n, rest) + a.eps), shift = a.center ? -rest * rstd : 0.f;
+        if (a.stats && threadIdx.x == 0) { a.stats[2 * r] = whole_mean(mean, rest); a.stats[2 * r + 1] = rstd; }
         T *y = (T *)a.y + r * a.ldy;
         for (int c = threadIdx.x; c < a.cols; c += blockDim.x)
-            store_f(y + c, fmaf((load_f(x + c) - x0 - m0) * rstd, param(a.weight, c, a.p_bf16, 1.f), param(a.bias, c, a.p_bf16, 0.f)));
+            store_f(y + c, fmaf(fmaf(load_f(x + c) - mean, rstd, shift), param(a.weight, c, a.p_bf16, 1.f), param(a.bias, c, a.p_bf16, 0.f)));
         __syncthreads();
     }
 }
