@@ -335,7 +335,8 @@ static cudaError_t few_launch(FewArgs a, int sms, cudaStream_t s)
     a.chunk = (int)std::min<int64_t>(FEW_SHARED / rows, round_up(a.K, 8));
     const size_t smem = (size_t)rows * a.chunk * 4;
     const auto launch = [&](auto kernel) {
-        const cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem) : cudaSuccess;
+        // (the same limit in every call: it belongs to the kernel, and other threads may be between here and their launch)
+        const cudaError_t e = smem > 40 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, FEW_SHARED * 4) : cudaSuccess;
         return e == cudaSuccess ? launch_dependent(kernel, grid, dim3(256), smem, s, 1, a) : e;
     };
     if (tma_takes(a.w, a.N, a.ldw, sizeof(T))) {

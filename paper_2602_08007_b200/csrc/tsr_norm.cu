@@ -801,8 +801,8 @@ int ring_stages(int per_sm, size_t fixed, size_t stage)
 template <typename Kern>
 cudaError_t launch_with(Kern kernel, dim3 grid, int threads, size_t smem, cudaStream_t s, const NormArgs &a, int stages, int cluster = 1)
 {
-    if (smem > 40 * 1024) {      // (48 KB less what is static)
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (smem > 40 * 1024) {      // (48 KB less what is static; the limit belongs to the kernel, so all calls set the same: other threads may be between here and their launch)
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, SM_SHARED);
         if (e != cudaSuccess) return e;
     }
     return launch_dependent(kernel, grid, dim3(threads), smem, s, cluster, a, stages);
