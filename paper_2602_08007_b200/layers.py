@@ -14,6 +14,7 @@ import contextlib
 import ctypes
 import functools
 import inspect
+import threading
 import weakref
 from typing import Optional
 
@@ -353,6 +354,7 @@ def _lies(t: torch.Tensor) -> torch.Tensor:
 
 
 _EAGER = weakref.WeakSet()     # graphs (their contexts) that were made outside of a capture and still live
+_EAGER_LOCK = threading.RLock()  # (one that a destructor which runs inside may take again)
 
 
 def _guard_capture(ctx, graph: bool, *tensors):
@@ -364,11 +366,14 @@ def _guard_capture(ctx, graph: bool, *tensors):
         return
     if torch.cuda.is_current_stream_capturing():
         ours = {id(t) for t in leaves}
-        if any(id(t) in ours for other in list(_EAGER) for t in other.leaves):
+        with _EAGER_LOCK:
+            living = list(_EAGER)
+        if any(id(t) in ours for other in living for t in other.leaves):
             raise RuntimeError("a graph of this tensor from outside of the capture is still alive: drop its outputs before capturing")
         return
     ctx.leaves = leaves      # (held by the graph anyway)
-    _EAGER.add(ctx)
+    with _EAGER_LOCK:
+        _EAGER.add(ctx)
 
 
 class _Norm(torch.autograd.Function):

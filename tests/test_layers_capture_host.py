@@ -1,0 +1,83 @@
+"""The guard of captures (a backward pass that is captured beside a living eager graph of the same leaf ends the process), on the CPU: what it sees of
+graphs, with torch's answers about streams replaced."""
+import sys
+import threading
+
+import pytest
+import torch
+
+from paper_2602_08007_b200 import layers
+
+
+class Through(torch.autograd.Function):
+    """A differentiable call with the guard in front, as the layers have it."""
+
+    @staticmethod
+    def forward(ctx, graph, x, w):
+        layers._guard_capture(ctx, graph, x, w)
+        return x * w
+
+    @staticmethod
+    def backward(ctx, dy):
+        return None, dy, dy
+
+
+def through(x, w):
+    return Through.apply(torch.is_grad_enabled(), x, w)
+
+
+@pytest.fixture
+def capturing(monkeypatch):
+    """A switch per thread: whether the current stream is being captured."""
+    state = threading.local()
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: getattr(state, "on", False))
+    return state
+
+
+def leaf():
+    return torch.ones(3, requires_grad=True)
+
+
+def test_a_living_graph_of_the_leaf_is_refused(capturing):
+    w, other = leaf(), leaf()
+    y = through(torch.ones(3), w)
+    capturing.on = True
+    through(torch.ones(3), other)
+    with torch.no_grad():
+        through(torch.ones(3), w)
+    with pytest.raises(RuntimeError, match="still alive"):
+        through(torch.ones(3), w)
+    del y
+    through(torch.ones(3), w)
+
+
+def test_threads_that_make_graphs_do_not_disturb_a_capture(capturing):
+    """Graphs come and go in other threads while a capture looks through those that live."""
+    stop, failed, interval = threading.Event(), [], sys.getswitchinterval()
+    sys.setswitchinterval(1e-6)
+
+    def make():
+        try:
+            held = []
+            while not stop.is_set():
+                held.append(through(torch.ones(3), leaf()))
+                if len(held) > 200:
+                    del held[:100]
+        except Exception as e:
+            failed.append(e)
+
+    threads = [threading.Thread(target=make) for _ in range(3)]
+    for t in threads:
+        t.start()
+    try:
+        capturing.on = True
+        for _ in range(1000):
+            through(torch.ones(3), leaf())
+    except Exception as e:
+        failed.append(e)
+    finally:
+        sys.setswitchinterval(interval)
+        stop.set()
+        for t in threads:
+            t.join()
+    assert not failed
