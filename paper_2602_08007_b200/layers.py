@@ -357,21 +357,37 @@ _EAGER = weakref.WeakSet()     # graphs (their contexts) that were made outside 
 _EAGER_LOCK = threading.RLock()  # (one that a destructor which runs inside may take again)
 
 
+def _leaves(tensors, nodes=()) -> dict:
+    """The leaves that the graphs of tensors and nodes end in, by id (and held, so that the ids stay theirs)."""
+    found, seen, todo = {id(t): t for t in tensors if t.is_leaf}, set(), [t.grad_fn for t in tensors] + list(nodes)
+    while todo:
+        node = todo.pop()
+        if node is None or node in seen:
+            continue
+        seen.add(node)
+        if type(node).__name__ == "AccumulateGrad":
+            found[id(node.variable)] = node.variable
+        try:
+            todo += [n for n, _ in node.next_functions]
+        except RuntimeError:      # (a call that another thread is still in: its node has no edges yet)
+            pass
+    return found
+
+
 def _guard_capture(ctx, graph: bool, *tensors):
     """Torch keeps one gradient accumulator per leaf, bound to the stream of the graph that made it.  A backward pass that is captured
     while an eager graph of the same leaf is alive reaches that stream from within the capture and ends the process, so the capture is refused
-    here, where it can still be an error.  (Seen for leaves that are inputs of these functions themselves.)  graph: whether torch records one."""
-    leaves = [t for t in tensors if graph and t is not None and t.requires_grad and t.is_leaf]
-    if not leaves:
+    here, where it can still be an error: for every leaf that the inputs of these functions are or were computed from, beside every living graph
+    that a call of these functions is part of.  (Graphs of other functions alone are not seen.)  graph: whether torch records one."""
+    tensors = [t for t in tensors if graph and t is not None and t.requires_grad]
+    if not tensors:
         return
     if torch.cuda.is_current_stream_capturing():
-        ours = {id(t) for t in leaves}
         with _EAGER_LOCK:
             living = list(_EAGER)
-        if any(id(t) in ours for other in living for t in other.leaves):
+        if living and _leaves(tensors).keys() & _leaves((), living).keys():
             raise RuntimeError("a graph of this tensor from outside of the capture is still alive: drop its outputs before capturing")
         return
-    ctx.leaves = leaves      # (held by the graph anyway)
     with _EAGER_LOCK:
         _EAGER.add(ctx)
 

@@ -71,7 +71,7 @@ def test_threads_that_make_graphs_do_not_disturb_a_capture(capturing):
         t.start()
     try:
         capturing.on = True
-        for _ in range(1000):
+        for _ in range(300):
             through(torch.ones(3), leaf())
     except Exception as e:
         failed.append(e)
@@ -81,3 +81,29 @@ def test_threads_that_make_graphs_do_not_disturb_a_capture(capturing):
         for t in threads:
             t.join()
     assert not failed
+
+
+def test_leaves_that_reach_a_call_through_others_are_seen(capturing):
+    """A weight that is cast, viewed or computed on the way; a leaf that the input of a call came from; and leaves that have nothing to do with each other."""
+    w, x, other = leaf(), leaf(), leaf()
+    y = through((2 * x).exp(), w.double().float().view(3))
+    capturing.on = True
+    for a, b in ((torch.ones(3), w), (torch.ones(3), w * 3), (x, other), (x.sin(), other.neg())):
+        with pytest.raises(RuntimeError, match="still alive"):
+            through(a, b)
+            pytest.fail("was taken")
+    z = through(other.exp(), other * 2).sum()
+    del y
+    through(x * 2, w.double().float())
+    assert z.requires_grad
+
+
+def test_leaves_are_not_held_beyond_their_graph(capturing):
+    """The guard itself keeps nothing alive."""
+    import weakref
+    w = leaf()
+    y = through(torch.ones(3), w)
+    gone, node = weakref.ref(y.grad_fn), y.grad_fn
+    assert node in layers._EAGER and not any(isinstance(v, (torch.Tensor, list, tuple)) for v in vars(node).values())
+    del y, node
+    assert gone() is None
