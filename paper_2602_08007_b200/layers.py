@@ -353,8 +353,12 @@ def _lies(t: torch.Tensor) -> torch.Tensor:
     return t if _layout(t) is not None else t.contiguous()
 
 
-_EAGER = weakref.WeakSet()     # graphs (their contexts) that were made outside of a capture and still live
+_EAGER = weakref.WeakSet()     # graphs (their contexts) that were made on the default stream, outside of a capture, and still live
 _EAGER_LOCK = threading.RLock()  # (one that a destructor which runs inside may take again)
+
+
+def _on_default_stream(t: torch.Tensor) -> bool:
+    return not t.is_cuda or _current_stream(t.device.index) == 0
 
 
 def _leaves(tensors, nodes=()) -> dict:
@@ -375,10 +379,11 @@ def _leaves(tensors, nodes=()) -> dict:
 
 
 def _guard_capture(ctx, graph: bool, *tensors):
-    """Torch keeps one gradient accumulator per leaf, bound to the stream of the graph that made it.  A backward pass that is captured
-    while an eager graph of the same leaf is alive reaches that stream from within the capture and ends the process, so the capture is refused
-    here, where it can still be an error: for every leaf that the inputs of these functions are or were computed from, beside every living graph
-    that a call of these functions is part of.  (Graphs of other functions alone are not seen.)  graph: whether torch records one."""
+    """Torch keeps one gradient accumulator per leaf, bound to the stream of the graph that made it.  A backward pass that is captured while
+    a graph of the same leaf from the default stream is alive reaches that stream from within the capture, which the default stream does not take, and
+    ends the process.  So the capture is refused here, where it can still be an error: for every leaf that the inputs of these functions are or
+    were computed from, beside every such graph that a call of these functions is part of.  (Graphs of other functions alone are not seen.  Other streams join the
+    capture; a graph of theirs counts where it may share accumulators with one of the default stream.)  graph: whether torch records one."""
     tensors = [t for t in tensors if graph and t is not None and t.requires_grad]
     if not tensors:
         return
@@ -389,7 +394,8 @@ def _guard_capture(ctx, graph: bool, *tensors):
             raise RuntimeError("a graph of this tensor from outside of the capture is still alive: drop its outputs before capturing")
         return
     with _EAGER_LOCK:
-        _EAGER.add(ctx)
+        if len(_EAGER) or _on_default_stream(tensors[0]):
+            _EAGER.add(ctx)
 
 
 class _Norm(torch.autograd.Function):

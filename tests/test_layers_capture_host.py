@@ -107,3 +107,25 @@ def test_leaves_are_not_held_beyond_their_graph(capturing):
     assert node in layers._EAGER and not any(isinstance(v, (torch.Tensor, list, tuple)) for v in vars(node).values())
     del y, node
     assert gone() is None
+
+
+def test_graphs_of_other_streams_are_not_refused(capturing, monkeypatch):
+    """Only the default stream cannot be reached from a capture.  A graph of another stream that may share accumulators with one of the default stream counts as
+    one of its own, even when that one is gone."""
+    where = threading.local()
+    monkeypatch.setattr(layers, "_on_default_stream", lambda t: getattr(where, "default", True))
+    w = leaf()
+    where.default = False
+    y = through(torch.ones(3), w)
+    capturing.on = True
+    through(torch.ones(3), w)
+    capturing.on = False
+    where.default = True
+    z = through(torch.ones(3), w)
+    where.default = False
+    y = through(torch.ones(3), w)
+    del z
+    capturing.on = True
+    with pytest.raises(RuntimeError, match="still alive"):
+        through(torch.ones(3), w)
+    assert y.requires_grad
