@@ -59,8 +59,8 @@ __device__ __forceinline__ float drop_entry(const DropRow &r, uint32_t col, floa
 bool drop_args(const tsr_dropout_desc &d, DropArgs *out);
 
 // ---- activations ------------------------------------------------------------------------------------------------------
-// The exponential and the reciprocal come from the special-function units (2^-22 of the value, and for the exponential 2^-24 of the argument on
-// top): below what FP32 products of a layer lose anyway, and a third of the instructions of the full forms, in kernels bound by them.
+// BF16 layers: the exponential and the reciprocal come from the special-function units (2^-22 of the value, and for the exponential 2^-24 of the argument on
+// top), in kernels bound by instructions; the result is rounded to 2^-9.  FP32 layers take the longer forms further down.
 __device__ __forceinline__ float rcp_f(float x)
 {
     float y;
@@ -131,7 +131,7 @@ __device__ __forceinline__ float2 act_pair(float2 z)
         return add2(make_float2(fmaxf(z.x, 0.f), fmaxf(z.y, 0.f)), p);
     } else return z;
 }
-__device__ __forceinline__ float act_value(int act, float z)
+__device__ __forceinline__ float act_approx(int act, float z)
 {
     switch (act) {
     case TSR_ACT_RELU: return z < 0.f ? 0.f : z;      // (NaN stays)
@@ -141,8 +141,8 @@ __device__ __forceinline__ float act_value(int act, float z)
     default: return z;
     }
 }
-// Derivative.  Beyond the limits it is 0 or 1 to FP32 accuracy, and products of an infinity with zero are kept out; NaN stays.
-__device__ __forceinline__ float act_slope(int act, float z)
+// Derivative.  Beyond the limits it is 0 or 1, and products of an infinity with zero are kept out; NaN stays.
+__device__ __forceinline__ float slope_approx(int act, float z)
 {
     switch (act) {
     case TSR_ACT_RELU: return z > 0.f ? 1.f : z != z ? z : 0.f;
@@ -158,11 +158,98 @@ __device__ __forceinline__ float act_slope(int act, float z)
         return fmaf(c * g * (1.f - g), 1.59576912f * fmaf(0.134145f, c2, 1.f), g);
     }
     case TSR_ACT_SILU: {
-        const float c = limited(z, 80.f), g = sigmoid_f(c);
+        const float c = limited(z, 1e30f), g = sigmoid_f(c);
         return g * fmaf(c, 1.f - g, 1.f);
     }
     default: return 1.f;
     }
+}
+
+// FP32 layers, two values at a time: within a few units of the last place.  2^(x c) from the special-function unit, whose argument in FP32 would be off by
+// 2^-24 of itself: the rest of the product, x c - h, is multiplied on (c2: what c leaves of its constant).  |x c| stays below 128.
+__device__ __forceinline__ float2 exp2_full(float2 x, float c, float c2)
+{
+    const float2 h = mul2(x, pair(c)), l = fma2(x, pair(c2), fma2(x, pair(c), mul2(h, pair(-1.f))));
+    float2 e;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.x) : "f"(h.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e.y) : "f"(h.y));
+    return fma2(e, mul2(l, pair(0.693147181f)), e);
+}
+__device__ __forceinline__ float2 limited(float2 x, float most) { return make_float2(limited(x.x, most), limited(x.y, most)); }
+// e^-x; beyond 88.6 the logistic function is zero and one (a reciprocal below 2^-126 is flushed).
+__device__ __forceinline__ float2 exp_minus(float2 x) { return exp2_full(limited(x, 88.6f), -1.44269504f, -1.92596303e-8f); }
+// 1 / x with a step of Newton's method behind the special-function unit.
+__device__ __forceinline__ float2 rcp_full(float2 x)
+{
+    const float2 r = make_float2(rcp_f(x.x), rcp_f(x.y));
+    return fma2(r, fma2(mul2(x, pair(-1.f)), r, pair(1.f)), r);
+}
+__device__ __forceinline__ float2 logistic_full(float2 x) { return rcp_full(add2(pair(1.f), exp_minus(x))); }
+// Phi(z) and e = exp(-z^2 / 2), |z| <= 16.  Up to |z| = 1 by 1/2 + z Q(z^2), beyond by the tail t P(t) e with t = 1 / (1 + 0.4 |z|), Hastings' form with eight
+// terms, which keeps its digits far below zero.  (Q and P fitted by least squares with Lawson's weights: 3e-10, and 4e-8 of the tail.)
+__device__ __forceinline__ float2 normal_cdf_full(float2 z, float2 &e)
+{
+    const float2 s = mul2(z, z), t = rcp_full(fma2(make_float2(fabsf(z.x), fabsf(z.y)), pair(0.4f), pair(1.f)));
+    e = exp2_full(s, -0.721347520f, -9.62981516e-9f);
+    float2 p = fma2(t, pair(-0.0375880674f), pair(0.190647230f)), q = fma2(s, pair(-7.66467929e-6f), pair(1.13512659e-4f));
+    p = fma2(t, p, pair(-0.352870584f));
+    q = fma2(s, q, pair(-1.18635304e-3f));
+    p = fma2(t, p, pair(0.227039829f));
+    q = fma2(s, q, pair(9.97333135e-3f));
+    p = fma2(t, p, pair(0.00408836780f));
+    q = fma2(s, q, pair(-0.0664903596f));
+    p = fma2(t, p, pair(0.151508555f));
+    q = fma2(s, q, pair(0.398942292f));
+    p = fma2(t, p, pair(0.157496333f));
+    q = fma2(z, q, pair(0.5f));
+    p = mul2(mul2(fma2(t, p, pair(0.159678325f)), t), e);
+    const float2 r = add2(pair(1.f), mul2(p, pair(-1.f)));
+    return make_float2(s.x <= 1.f ? q.x : z.x > 0.f ? r.x : p.x, s.y <= 1.f ? q.y : z.y > 0.f ? r.y : p.y);
+}
+template <int ACT>
+__device__ __forceinline__ float2 act_pair_full(float2 z)
+{
+    if constexpr (ACT == TSR_ACT_GELU) {
+        float2 e;
+        return mul2(z, normal_cdf_full(limited(z, 16.f), e));
+    } else if constexpr (ACT == TSR_ACT_GELU_TANH) return mul2(z, logistic_full(mul2(pair(1.59576912f), fma2(mul2(mul2(z, z), pair(0.044715f)), z, z))));
+    else if constexpr (ACT == TSR_ACT_SILU) return mul2(z, logistic_full(z));
+    else return act_pair<ACT>(z);
+}
+template <int ACT>
+__device__ __forceinline__ float2 slope_pair_full(float2 z)
+{
+    if constexpr (ACT == TSR_ACT_GELU) {
+        const float2 c = limited(z, 16.f);
+        float2 e;
+        const float2 cdf = normal_cdf_full(c, e);
+        return fma2(mul2(c, pair(0.39894228f)), e, cdf);
+    } else if constexpr (ACT == TSR_ACT_GELU_TANH) {
+        const float2 c = limited(z, 16.f), c2 = mul2(c, c), g = logistic_full(mul2(pair(1.59576912f), fma2(mul2(c2, pair(0.044715f)), c, c)));
+        return fma2(mul2(mul2(c, g), fma2(g, pair(-1.f), pair(1.f))), mul2(pair(1.59576912f), fma2(pair(0.134145f), c2, pair(1.f))), g);
+    } else if constexpr (ACT == TSR_ACT_SILU) {
+        const float2 c = limited(z, 1e30f), g = logistic_full(c);
+        return mul2(g, fma2(c, fma2(g, pair(-1.f), pair(1.f)), pair(1.f)));
+    } else return make_float2(slope_approx(ACT, z.x), slope_approx(ACT, z.y));
+}
+__device__ __forceinline__ float act_full(int act, float z)
+{
+    switch (act) {
+    case TSR_ACT_RELU: return act_pair_full<TSR_ACT_RELU>(pair(z)).x;
+    case TSR_ACT_GELU: return act_pair_full<TSR_ACT_GELU>(pair(z)).x;
+    case TSR_ACT_GELU_TANH: return act_pair_full<TSR_ACT_GELU_TANH>(pair(z)).x;
+    case TSR_ACT_SILU: return act_pair_full<TSR_ACT_SILU>(pair(z)).x;
+    default: return z;
+    }
+}
+// T: the layer's type.
+template <typename T>
+__device__ __forceinline__ float act_value(int act, float z) { return sizeof(T) == 4 ? act_full(act, z) : act_approx(act, z); }
+template <typename T, int ACT>
+__device__ __forceinline__ float2 slope_pair(float2 z)
+{
+    if constexpr (sizeof(T) == 4) return slope_pair_full<ACT>(z);
+    else return make_float2(slope_approx(ACT, z.x), slope_approx(ACT, z.y));
 }
 
 // ---- typed access -----------------------------------------------------------------------------------------------------

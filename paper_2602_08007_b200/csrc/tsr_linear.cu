@@ -163,7 +163,7 @@ linear_finish_kernel(const __grid_constant__ FinishArgs a)
 #pragma unroll 1
             for (int j = 0; j < 8; ++j) {
                 // (one copy of the activation's code: rotated through the first place)
-                const float z = act_value(e.act, v[0]);
+                const float z = act_value<T>(e.act, v[0]);
 #pragma unroll
                 for (int i = 0; i < 7; ++i) v[i] = v[i + 1];
                 v[7] = z;
@@ -314,7 +314,7 @@ linear_few_kernel(const __grid_constant__ FewArgs a)
         const int64_t row = row0 + r;
         if (e.bias) z += load_as(e.bias, col, e.bias_bf16);
         if (e.pre) store_f((T *)e.pre + row * e.ldp + col, z);
-        z = act_value(e.act, z);
+        z = act_value<T>(e.act, z);
         if (e.drop.threshold) z = drop_entry(drop_row_key(drop_call_key(e.drop), row), (uint32_t)col, z, e.drop);
         if (e.res) z += load_f((const T *)e.res + row * e.ldr + col);
         store_f((T *)e.out + row * e.ldo + col, z);
@@ -395,7 +395,11 @@ linear_dz_kernel(const DzArgs a)
             }
             if (ACT) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j) g[j] *= act_slope(ACT, z[j]);
+                for (int j = 0; j < 8; j += 2) {
+                    const float2 d = slope_pair<T, ACT>(make_float2(z[j], z[j + 1]));
+                    g[j] *= d.x;
+                    g[j + 1] *= d.y;
+                }
                 pre += 8 * a.ldpre;
             }
             if (a.drop.threshold) {      // last, as a selection: what fell is zero whatever pre holds

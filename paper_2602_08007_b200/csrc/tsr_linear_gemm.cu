@@ -49,13 +49,13 @@ int linear_stages(int stage_bytes, bool pre)
     return n < LG_MAX_STAGES ? n : LG_MAX_STAGES;
 }
 
-template <int ACT>
+template <int ACT, bool F32>
 __device__ __forceinline__ void activate(float (&v)[32])
 {
     if constexpr (ACT != TSR_ACT_NONE) {
 #pragma unroll
         for (int j = 0; j < 32; j += 2) {
-            const float2 z = act_pair<ACT>(make_float2(v[j], v[j + 1]));
+            const float2 x = make_float2(v[j], v[j + 1]), z = F32 ? act_pair_full<ACT>(x) : act_pair<ACT>(x);
             v[j] = z.x;
             v[j + 1] = z.y;
         }
@@ -417,7 +417,7 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
                                                                                  pack_bf16(v[8 * u + 4], v[8 * u + 5]), pack_bf16(v[8 * u + 6], v[8 * u + 7]));
                         }
                     }
-                    if constexpr (FULL) activate<EPI>(v);
+                    if constexpr (FULL) activate<EPI, F32>(v);
                     if (drops) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
