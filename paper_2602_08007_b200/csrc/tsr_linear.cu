@@ -735,6 +735,8 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
     if (s.tail && !encode(&g.tmSlab, slabs, s.tail * s.splits * 128 * s.cg, s.width, s.width, true, 32)) return TSR_ERR_CUDA;
     g.e = p.e;
     g.whole_edge = p.N * os % 16 == 0;
+    for (int i = 0; i < 2 && p.f32; ++i) g.parts[i] = {(const bf16 *)op[i]->p, op[i]->ld, op[i]->plane};
+    g.K = (int)p.K;
     if (s.whole) {
         g.e.out_tma = out_tma;
         g.e.res_tma = res_tma;

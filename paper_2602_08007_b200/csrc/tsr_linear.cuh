@@ -31,6 +31,8 @@ struct alignas(64) LinearGemm : LinearTiles {
     int32_t stages, stage_bytes, b_offset;   // the ring in shared memory
     uint32_t stage_tx;                   // bytes of a stage, of all CTAs of a tile
     int32_t whole_edge;                  // rows of out and pre may be written in whole 16-byte units
+    struct { const bf16 *p; int64_t ld, plane; } parts[2];   // FP32 operands: where their planes lie
+    int32_t K;
     LinearEpilogue e;
 };
 

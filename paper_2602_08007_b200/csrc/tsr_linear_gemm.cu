@@ -14,6 +14,9 @@
 // accumulator is therefore emptied every 128 entries of K into FP32 registers of the epilogue warps, added to nearest.  K blocks are 32 entries there,
 // of which three stages fit beside the boxes.
 //
+// An infinity x = p1 against parts of q of both signs, or zero ones, comes out as NaN where x q is infinite.  So entries that are NaN are formed again from x and q
+// themselves, in FP32 (formed_again): a compare per entry in all other cases.
+//
 // Epilogue: a lane holds a row.  A warp's 32 rows x 128 bytes of output form a box in shared memory (128-byte swizzle: free of bank
 // conflicts when the lanes walk their rows), of which it has two, and a third for pre.  The residual is fetched into the box by TMA
 // while the MMAs still run, the result replaces it in place, and the box leaves by TMA.  Matrices whose pitch or address TMA
@@ -97,6 +100,53 @@ __device__ __forceinline__ void box_to_rows(uint8_t *box, void *dst, int64_t ld,
             else ((bf16 *)dst)[r * ld + c] = *(bf16 *)((uint8_t *)box_unit(box, r, c >> 3) + (c & 7) * 2);
         }
     }
+}
+
+// Eight entries along K of one row of an FP32 operand, from its planes; `mn`: the operand is stored with K as its rows, of which `last` exist.
+__device__ __forceinline__ void whole_entries(const bf16 *p, int64_t ld, int64_t plane, bool mn, int row, int k, int last, float (&v)[8])
+{
+    if (!mn) {      // (rows are padded with zeros to whole units)
+        float part[8];
+        load8(p + row * ld + k, v);
+        load8(p + plane + row * ld + k, part);
+        float rest[8];
+        load8(p + 2 * plane + row * ld + k, rest);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += part[i] + rest[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bf16 *at = p + (int64_t)(k + i) * ld + row;
+            v[i] = k + i < last ? load_f(at) + (load_f(at + plane) + load_f(at + 2 * plane)) : 0.f;
+        }
+    }
+}
+// 32 columns of the warp's 32 rows over the K range of the item; the entries that are NaN are replaced.  It ends where they have all become NaN again.
+__device__ __forceinline__ void formed_again(const LinearGemm &g, int row0, int col0, int first, int last, int lane, float (&v)[32])
+{
+    float s[32];
+#pragma unroll
+    for (int j = 0; j < 32; ++j) s[j] = 0.f;
+    const int row = min(row0 + lane, g.M - 1), col = min(col0 + lane, g.N - 1);
+#pragma unroll 1
+    for (int k = first; k < last; k += 8) {
+        float a[8], b[8];
+        whole_entries(g.parts[0].p, g.parts[0].ld, g.parts[0].plane, g.a_mn, row, k, last, a);
+        whole_entries(g.parts[1].p, g.parts[1].ld, g.parts[1].plane, g.b_mn, col, k, last, b);
+#pragma unroll 1
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) s[j] = fmaf(a[0], __shfl_sync(0xffffffffu, b[0], j), s[j]);
+#pragma unroll
+            for (int n = 0; n < 7; ++n) { a[n] = a[n + 1]; b[n] = b[n + 1]; }
+        }
+        bool open = false;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) open |= v[j] != v[j] && s[j] == s[j];
+        if (!__any_sync(0xffffffffu, open)) break;
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = v[j] != v[j] ? s[j] : v[j];
 }
 
 // One MMA, issued by the lane for which `leader` is set; the whole warp runs through here, so that the descriptors stay in uniform registers.  They are
@@ -473,6 +523,17 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
             if constexpr (PLANES == 3) {
 #pragma unroll 1
                 for (int k = 0; ok && k < cnt; ++k) {      // (one copy of the epilogue's code: the sums move up to the first place)
+                    const int col0 = first_col + 64 * k, ncols = min(32, n_end - col0);
+                    float2 z = pair(0.f);      // NaN where an entry is (or infinite); outside of the matrix there may be anything
+                    if (ncols == 32) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) z = fma2(make_float2(sum[0][j], sum[0][j + 1]), pair(0.f), z);
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) z.x = fmaf(j < ncols ? sum[0][j] : 0.f, 0.f, z.x);
+                    }
+                    z.x += z.y;
+                    if (__any_sync(0xffffffffu, lane < nrows && z.x != z.x)) formed_again(g, row0, col0, tile.kb0 * BK, min(tile.kb1 * BK, g.K), lane, sum[0]);
                     ok = one_box(k, sum[0]);
 #pragma unroll
                     for (int i = 0; i < 3; ++i)
