@@ -2,6 +2,10 @@
 
 Roundings: half a step is 2^-8 of a BF16 value and 2^-24 of an FP32 one.  A tensor-core instruction adds the products of 16 BF16 (8 TF32)
 pairs to the accumulator and keeps 24 bits of the largest term at least: it is off by at most 2^-22 of the sum of magnitudes."""
+
+# FP32 products are six products of three BF16 parts of each operand, added within 128 entries of K by the tensor cores and in FP32 beyond.  The bound of
+# product_slack below, that of two TF32 parts, is wider than what they keep; test_gpu_linear_f32.py checks each of the six and the size of the error.
+# Activations go through the special-function units, in FP32 layers with corrections (test_gpu_layer_activations.py); the bounds below hold for both.
 import math
 
 import numpy as np
