@@ -384,7 +384,7 @@ TSR_API tsr_status tsr_norm_backward(const tsr_norm_desc *desc, tsr_matrix dy, t
  * within about 12 x 2^-24 of the root of their sum of squares, whatever K is (a plain FP32 sum: 1 at K = 16, 11 at 512, 38 at 16384).  Infinite
  * operands give what FP32 products give; an entry below 2^-110 loses bits.
  * A forward call with few rows may run in FP32 throughout instead.
- * Backward:  dz = dropout(dy) o act'(pre) (rounded to the type of x, as an operand), dx = dz weight, dweight = dz^T x,
+ * Backward:  dz = dropout(dy) o act'(pre) (with an activation rounded to the type of x, as an operand), dx = dz weight, dweight = dz^T x,
  * dbias = sum over rows of dz (from FP32); the residual's gradient is dy.  dx, dweight and dbias may each be absent. */
 typedef struct {
     int64_t rows, ins, outs;

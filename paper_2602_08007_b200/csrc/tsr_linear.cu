@@ -153,6 +153,8 @@ linear_finish_kernel(const __grid_constant__ FinishArgs a)
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] += x[j];
             }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= e.scale;
         }
         if (e.bias) {
 #pragma unroll
@@ -351,7 +353,9 @@ static cudaError_t few_launch(FewArgs a, int sms, cudaStream_t s)
     return launch(linear_few_kernel<T, FEW_ROWS, false>);
 }
 
-// dz and its column sums.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row.  dy and pre
+// dz and its column sums.  BF16 layers round dz, as an operand of both products (error of dx and dweight 0.0017 -> 0.0023 of the result, three quarters of
+// which their own rounding brings anyway; two parts would double the products).  Without an activation dz is a selection from dy, rounded by nothing: the factor
+// of dropout is left to the products' epilogue.  A CTA takes 256 columns and a range of rows; a lane eight columns side by side, a warp every eighth row.  dy and pre
 // may lie at any alignment, dz has a pitch of whole 16-byte units.  dz NULL: the sums alone.
 // The grid is what is resident at once (a third more left SMs idle for 40 % of the time), and what hides the loads is the number of warps: unrolled
 // loops were slower, the more so the further (8192 x 5461 with SiLU off the 16-byte grid: 58 us; at an earlier stage 72, unrolled twice 95, four times 131 at three CTAs).
@@ -364,7 +368,8 @@ struct DzArgs {
     int32_t sums_bf16, accumulate;
     int64_t lddy, ldpre, lddz, plane, rows;
     int32_t cols, rows_per;
-    DropArgs drop;
+    DropArgs drop;             // with a factor of 1 where ACT is TSR_ACT_NONE
+    float sum_scale;           // of the sums: the factor there, otherwise 1
 };
 template <typename T, int ACT>
 __global__ void __launch_bounds__(256, DZ_CTAS)
@@ -431,6 +436,7 @@ linear_dz_kernel(const DzArgs a)
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < 8; ++w) s += sums[w][threadIdx.x];
+        s *= a.sum_scale;
         if (a.partial) a.partial[(int64_t)blockIdx.y * a.cols + c] = s;
         else store_as(a.sums, c, a.sums_bf16, a.accumulate ? s + load_as(a.sums, c, a.sums_bf16) : s);
     }
@@ -807,6 +813,7 @@ tsr_status forward(const tsr_linear_desc *d, const tsr_linear_io *io, void *work
     p.e.pre = io->pre.data; p.e.ldp = io->pre.ld;
     p.e.bias = io->bias; p.e.bias_bf16 = d->b_dtype == TSR_BF16;
     p.e.act = d->activation;
+    p.e.scale = 1.f;
     const int sms = device_sms();
     const auto all = [&](Room &room, bool run, int n) -> tsr_status {
         if (few_rows(p)) {
@@ -864,6 +871,7 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
     const int64_t rows_per = T ? round_up((T + most - 1) / most, 8) : 8;
     const int64_t parts = std::max<int64_t>(1, (T + rows_per - 1) / rows_per);
 
+    const float scale = d->activation == TSR_ACT_NONE && drop.threshold ? drop.scale : 1.f;      // applied behind the products and the sums
     tsr_matrix dz = io->dy;
     Product px = {}, pw = {};
     size_t total = 0;
@@ -891,6 +899,8 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             if (direct) { a.sums = io->dbias; a.sums_bf16 = d->gb_dtype == TSR_BF16; a.accumulate = d->accumulate; }
             a.rows = T; a.cols = (int)O; a.rows_per = (int)rows_per;
             a.drop = drop;
+            if (d->activation == TSR_ACT_NONE) a.drop.scale = 1.f;
+            a.sum_scale = scale;
             const dim3 grid((unsigned)col_blocks, (unsigned)parts);
             const cudaError_t rc = f32 ? dz_launch<float>(a, d->activation, grid, stream) : dz_launch<bf16>(a, d->activation, grid, stream);
             if (rc != cudaSuccess) return TSR_ERR_CUDA;
@@ -912,6 +922,7 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             px.f32 = px.out_f32 = f32;
             px.A = dz_op;
             px.B = w_op;
+            px.e.scale = scale;
             px.e.out = io->dx.data; px.e.ldo = io->dx.ld;
             Room own = room;
             st = product(px, own, run, sms, stream);
@@ -926,6 +937,7 @@ tsr_status backward(const tsr_linear_desc *d, const tsr_linear_grads *io, void *
             pw.A = dz_op;
             pw.A.mn = true;
             pw.B = x_op;
+            pw.e.scale = scale;
             pw.e.out = io->dweight.data; pw.e.ldo = io->dweight.ld;
             if (d->accumulate) { pw.e.res = pw.e.out; pw.e.ldr = pw.e.ldo; }
             Room own = room;

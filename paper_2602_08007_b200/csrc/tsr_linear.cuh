@@ -13,6 +13,7 @@ struct LinearEpilogue {
     int32_t bias_bf16, act;
     int32_t out_tma, res_tma, pre_tma;   // the matrix is described by a tensor map
     DropArgs drop;
+    float scale;            // of the product, where there is nothing but a residual besides; 1 otherwise
 };
 
 // Tiles of a product and the work items made of them: the first `whole` tiles one item each, the others `splits` items of kb_per K blocks.

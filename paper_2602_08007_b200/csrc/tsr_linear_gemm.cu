@@ -1,6 +1,6 @@
 // Products of the linear layer on the 5th-generation tensor cores, with the layer's epilogue (formulas in tsr.h).
 //
-//   D[M x N] = A[M x K] B[N x K]^T,   then per entry  z = D + bias;  pre = z;  out = residual + dropout(act(z))
+//   D[M x N] = A[M x K] B[N x K]^T,   then per entry  z = D + bias;  pre = z;  out = residual + dropout(act(z)),  or  out = residual + scale D
 //
 // One persistent CTA per SM (CG = 1, tiles of 128 x width) or one pair of CTAs per two SMs (CG = 2, 256 x width, tcgen05 with
 // cta_group::2).  Either operand is K-major or MN-major (a row-major matrix contracted over its rows, read as it lies), so
@@ -187,7 +187,7 @@ __device__ __forceinline__ void tma_load_3d_pair(uint32_t dst, const CUtensorMap
 }
 
 // PLANES: 1, BF16 operands; 3, FP32 operands in three BF16 planes.  F32: type of out, residual and pre.  EPI: the activation of a full epilogue, or
-// EPI_PLAIN: out = residual + D.  (One kernel for all of them spent a third of its time waiting for instructions.)
+// EPI_PLAIN: out = residual + scale D.  (One kernel for all of them spent a third of its time waiting for instructions.)
 constexpr int EPI_PLAIN = -1;
 template <int CG, int PLANES, bool F32, int EPI>
 __global__ void __cluster_dims__(CG, 1, 1) __launch_bounds__(LG_THREADS, 1)
@@ -468,6 +468,14 @@ linear_gemm_kernel(const __grid_constant__ LinearGemm g)
                         }
                     }
                     if constexpr (FULL) activate<EPI, F32>(v);
+                    if constexpr (!FULL) {
+#pragma unroll
+                        for (int j = 0; j < 32; j += 2) {
+                            const float2 x = mul2(make_float2(v[j], v[j + 1]), pair(e.scale));
+                            v[j] = x.x;
+                            v[j + 1] = x.y;
+                        }
+                    }
                     if (drops) {
 #pragma unroll
                         for (int j = 0; j < 32; j += 2) {
