@@ -12,8 +12,8 @@
 // Measured: forward 16384 x 2048 BF16 25.5 us (5.3 TB/s of 6.6 that a copy reaches), backward 8192 x 1024 FP32 23 us (4.3), backward without mean 6007 x
 // 5461 BF16 59 us (3.4: the rows start at eight different places, teams of eight warps wait for each other, and first and last rows of a CTA are alone).
 // Wider rows, and matrices that do not start at the same place in 16 bytes, are read several times (from L2, mostly), entry by entry; their column
-// sums take a pass of their own.  Those are bound by instructions: 6007 x 5461 from a pitch of 5464 into one of 5461 takes 159 us forward, 234 us
-// backward, against 36 and 68 with both alike.
+// sums take a pass of their own.  Those are bound by instructions: 6007 x 5461 from a pitch of 5464 into one of 5461 takes 152 us forward, 220 us
+// backward with mean and dbias, against 41 and 73 with both alike.
 #include <math.h>
 #include <string.h>
 
@@ -38,9 +38,8 @@ __device__ __forceinline__ float cta_sum(float x, float *slot)
     x = warp_sum(x);
     if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = x;
     __syncthreads();
-    float s = 0.f;
-    for (int w = 0; w < warps; ++w) s += slot[w];
-    return s;
+    const int lane = threadIdx.x & 31;
+    return warp_sum(lane < warps ? slot[lane] : 0.f);
 }
 // Two sums at once.
 __device__ __forceinline__ float2 cta_sums(float2 x, float2 *slot)
@@ -49,9 +48,9 @@ __device__ __forceinline__ float2 cta_sums(float2 x, float2 *slot)
     x = make_float2(warp_sum(x.x), warp_sum(x.y));
     if ((threadIdx.x & 31) == 0) slot[threadIdx.x >> 5] = x;
     __syncthreads();
-    float2 s = make_float2(0.f, 0.f);
-    for (int w = 0; w < warps; ++w) { s.x += slot[w].x; s.y += slot[w].y; }
-    return s;
+    const int lane = threadIdx.x & 31;
+    const float2 s = lane < warps ? slot[lane] : make_float2(0.f, 0.f);
+    return make_float2(warp_sum(s.x), warp_sum(s.y));
 }
 // Variance from the means of the squares and of the distances; rounding may leave it below zero, and NaN stays.
 __device__ __forceinline__ float variance_of(float squares, float rest)
@@ -872,7 +871,9 @@ BackwardForm backward_form(int64_t units)
         f.per_lane = t.per_lane;
         f.team = t.warps;
         f.threads = 32 * t.warps * t.teams;
-        if (t.per_lane == 6) { f.per_lane = 3; f.team *= 2; f.threads *= 2; }      // sixteen warps fit: 6007 x 5461 without dbias 64 us as six units, 58 as three
+        // Sixteen warps of three units in place of eight of six: BF16 up to 12 % less time, FP32 from 8 % less to 5 % longer, at 320 to 1536 units (6007 x 5461 BF16 without dbias
+        // 64 -> 58 us).  In place of five units they take up to 15 % longer (at 320 units with dbias 44 %), of eight (as four) 14 % less to 13 % longer: not there.
+        if (t.per_lane == 6) { f.per_lane = 3; f.team *= 2; f.threads *= 2; }
     }
     f.cluster = f.per_sm == 1 ? 2 : f.per_sm == 2 ? 4 : 8;
     return f;
