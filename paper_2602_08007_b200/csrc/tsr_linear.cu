@@ -712,7 +712,8 @@ tsr_status product(const Product &p, Room &room, bool run, int sms, cudaStream_t
         const void *at = o.p;
         int64_t ld = o.ld;
         // A K-major operand whose rows do not start on 128 bytes costs two lines per row and K block, a fifth of the product's time; copying
-        // it first pays where the other extent is long enough (8192 x 5464 -> 2048: weight copied 190 -> 168 us).
+        // it first pays where the other extent is long enough.  us, as it lies / copied: 8192 x 5464 -> 2048 (the weight) 150 / 134, 8192 x 2056 -> 8192 (both) 220 / 195,
+        // 16384 x 1032 -> 1032 52 / 46, 1500 x 8200 -> 5464 (x) 126 / 108; 4096 x 520 -> 512 13 / 15, 2048 x 5464 -> 2048 (neither by the rule) 48 / 57.
         const bool straddles = !o.mn && rows > 1 && (o.ld % 64 || !aligned_to(o.p, 128)) && p.K >= 512 && extent[1 - i] >= 3200;
         if (!p.f32 && (straddles || !tma_takes(o.p, rows, o.ld, 2))) {
             ld = round_up(cols, 64);

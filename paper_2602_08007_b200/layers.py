@@ -3,7 +3,8 @@ whose gradients the optimizer steps.
 
 Two forms.  norm_forward, norm_backward, linear_forward, linear_backward, dropout_forward and dropout_backward marshal arguments to the C calls: they
 take tensors as they lie (last dimension contiguous; the others collapse to rows of one pitch) and refuse anything else.
-layer_norm, rms_norm, linear and dropout are differentiable torch functions over them, which copy what does not lie that way.
+layer_norm, rms_norm, linear and dropout are differentiable torch functions over them, which copy what does not lie that way.  They have a first derivative
+only (no second one, no vmap, no forward mode) and ignore autocast: an input and its weight have one type.
 
 All of them run on torch's current stream of the tensors' device, or on `stream`; results and scratch come from torch's allocator on that
 stream, so calls on different streams share nothing and a capture keeps its own.  Tensors of the caller need record_stream
